@@ -5,7 +5,7 @@ gfx950 kernels (device calls) or its host packer/planner.  There is no CPU fallb
 the library is missing, importing the binding's functions raises.
 """
 from .binding import (CsbMatrix, CsbRnn, CsbError, CELL_LSTM, CELL_GRU, CELL_LSTMP, CELL_LIGRU, CELL_GRU_RB, VAL_F32, VAL_F16, VAL_BF16, lib, lib_path,
-                      load_library, stream_read, project)
+                      load_library, stream_read, project, delta_chunked, delta_recurrent, adapter_add, verify_drafts)
 
 __all__ = ["CsbMatrix", "CsbRnn", "CsbError", "CELL_LSTM", "CELL_GRU", "CELL_LSTMP", "CELL_LIGRU", "CELL_GRU_RB", "VAL_F32", "VAL_F16", "VAL_BF16", "lib", "lib_path",
-           "load_library", "stream_read", "project"]
+           "load_library", "stream_read", "project", "delta_chunked", "delta_recurrent", "adapter_add", "verify_drafts"]

@@ -1,4 +1,4 @@
-"""ctypes binding with the same names as include/csbrnn.h (argument marshalling only)."""
+"""ctypes binding with the same names as include/csbrnn.h and include/csbrnn_lm.h (argument marshalling only)."""
 from __future__ import annotations
 
 import ctypes as C
@@ -18,14 +18,17 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libcsbrnn.so")
 _lib = None
 
-# every symbol include/csbrnn.h declares
+# every symbol the headers under include/ declare
 SYMBOLS = ["csb_last_error", "csb_pack", "csb_view_get", "csb_unpack", "csb_set_value_format", "csb_value_format", "csb_sharing_model", "csb_plan", "csb_plan_ex", "csb_plan_rows", "csb_plan_stats_get", "csb_plan_validate", "csb_status",
            "csb_device_bytes", "csb_upload", "csb_workspace_bytes", "csb_spmv", "csb_spmv_static_limit", "csb_spmv_static", "csb_spmm", "csb_spmm_bfloat", "csb_spmm_half",
            "csb_debug_stamp_count", "csb_debug_spmv_stamps",
            "csb_debug_stream_read_out_floats", "csb_debug_stream_read", "csb_debug_spmm_columns", "csb_debug_quad_passes", "csb_debug_spmm_force", "csb_debug_spmm_form", "csb_debug_spmm_panel", "csb_debug_rnn_prefers_resident",
            "csb_project_workspace_bytes", "csb_project", "csb_rnn_create_lstmp", "csb_rnn_create_gru_rb",
            "csb_rnn_create", "csb_rnn_device_bytes", "csb_rnn_upload", "csb_rnn_plan_resident", "csb_rnn_stats",
-           "csb_rnn_set_poll_limit", "csb_rnn_status", "csb_rnn_workspace_bytes", "csb_rnn_forward", "csb_free", "csb_rnn_free"]
+           "csb_rnn_set_poll_limit", "csb_rnn_status", "csb_rnn_workspace_bytes", "csb_rnn_forward", "csb_free", "csb_rnn_free",
+           # include/csbrnn_lm.h
+           "csb_delta_recurrent", "csb_delta_workspace_bytes", "csb_delta_chunked", "csb_adapter_workspace_bytes", "csb_adapter_add",
+           "csb_verify_workspace_bytes", "csb_verify_drafts"]
 
 
 class csb_sharing_stats(C.Structure):
@@ -63,6 +66,15 @@ class csb_plan_stats(C.Structure):
                 ("lane_fill", C.c_double), ("nosplit_max_over_mean", C.c_double),
                 ("chunk_max_over_mean", C.c_double), ("whole_tiles", C.c_int32), ("row_owned", C.c_int32),
                 ("rounds", C.c_int32), ("reserved", C.c_int32), ("matvec_bytes", C.c_int64)]
+
+
+class csb_delta_args(C.Structure):
+    _fields_ = [("type", C.c_int32), ("heads_k", C.c_int32), ("heads_v", C.c_int32), ("dk", C.c_int32), ("dv", C.c_int32),
+                ("n_seq", C.c_int32), ("n_tokens", C.c_int64), ("d_q", C.c_void_p), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
+                ("ldq", C.c_int64), ("ldk", C.c_int64), ("ldv", C.c_int64), ("d_g", C.c_void_p), ("d_beta", C.c_void_p),
+                ("ldg", C.c_int64), ("ldbeta", C.c_int64), ("d_start", C.c_void_p), ("d_len", C.c_void_p),
+                ("d_state_in", C.c_void_p), ("d_state_out", C.c_void_p), ("d_slot", C.c_void_p), ("n_states", C.c_int32),
+                ("scale", C.c_float), ("d_out", C.c_void_p), ("ldo", C.c_int64)]
 
 
 def lib_path() -> str:
@@ -136,6 +148,19 @@ def load_library():
     L.csb_rnn_workspace_bytes.argtypes = [C.c_void_p, C.c_int32, C.c_int32]
     L.csb_rnn_workspace_bytes.restype = C.c_size_t
     L.csb_rnn_forward.argtypes = [C.c_void_p] + [C.c_void_p] * 6 + [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
+    L.csb_delta_recurrent.argtypes = [C.POINTER(csb_delta_args), C.c_void_p]
+    L.csb_delta_chunked.argtypes = [C.POINTER(csb_delta_args), C.c_void_p, C.c_void_p]
+    L.csb_delta_workspace_bytes.argtypes = [C.POINTER(csb_delta_args)]
+    L.csb_delta_workspace_bytes.restype = C.c_size_t
+    L.csb_adapter_workspace_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32]
+    L.csb_adapter_workspace_bytes.restype = C.c_size_t
+    L.csb_adapter_add.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int32,
+                                  C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_void_p]
+    L.csb_verify_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
+    L.csb_verify_workspace_bytes.restype = C.c_size_t
+    L.csb_verify_drafts.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64] + [C.c_void_p] * 4 + \
+                                   [C.c_int32] * 3 + [C.c_void_p] * 4
     L.csb_free.argtypes = [C.c_void_p]
     L.csb_free.restype = None
     L.csb_rnn_free.argtypes = [C.c_void_p]
@@ -207,6 +232,144 @@ def project(W, br: int, bc: int, rate: float, out=None, stream=None):
     _check(lib().csb_project(W.data_ptr(), rows, cols, W.stride(0), br, bc, float(rate), out.data_ptr(), out.stride(0),
                              _dptr(ws), _stream_ptr(stream)))
     return out
+
+
+def _val_type(dtype) -> int:
+    """CSB_VAL_* of a torch dtype."""
+    import torch
+    if dtype is torch.bfloat16:
+        return VAL_BF16
+    if dtype is torch.float16:
+        return VAL_F16
+    assert dtype is torch.float32, f"expected a float32, float16 or bfloat16 tensor, got {dtype}"
+    return VAL_F32
+
+
+def _scratch(nbytes: int, device):
+    """A workspace (torch's blocks are 512-byte aligned); freed to the current stream when the caller drops it."""
+    import torch
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _delta(call, q, k, v, g, beta, scale, starts, lens, state, slots, state_out, out, stream):
+    import torch
+    T, HK, DK = q.shape
+    HV, DV = v.shape[1:]
+    i32, f32 = torch.int32, torch.float32
+    assert k.shape == q.shape and v.shape[0] == T and tuple(g.shape) == (T, HV) and tuple(beta.shape) == (T, HV)
+    assert q.dtype is k.dtype is v.dtype and g.dtype is f32 and beta.dtype is f32
+    if out is None:
+        out = torch.empty((T, HV, DV), dtype=v.dtype, device=v.device)
+    assert out.shape == v.shape and out.dtype is v.dtype
+
+    def rows(t, w):                                            # (t, head, j) at t * ld + head * w + j
+        assert t.is_cuda
+        (ld, head, one), n = t.stride(), t.shape
+        assert (one == 1 or n[2] == 1) and (head == w or n[1] == 1), "heads of a token must be contiguous"
+        return max(ld, n[1] * n[2]) if n[0] < 2 else ld
+
+    def per_head(t):
+        assert t.is_cuda and (t.stride(1) == 1 or HV == 1)
+        return max(t.stride(0), HV) if T < 2 else t.stride(0)
+    if starts is not None:
+        N = starts.numel() - 1
+    elif lens is not None:
+        N = lens.numel()
+    elif slots is not None:
+        N = slots.numel()
+    else:
+        N = state.shape[0] if state is not None else 1
+    assert (lens is None or lens.numel() == N) and (slots is None or slots.numel() == N)
+    n_states = 0
+    for s in (state, state_out):
+        if s is not None:
+            assert tuple(s.shape[1:]) == (HV, DK, DV) and (n_states in (0, s.shape[0]))
+            n_states = s.shape[0]
+    a = csb_delta_args(_val_type(q.dtype), HK, HV, DK, DV, N, T, q.data_ptr(), k.data_ptr(), v.data_ptr(), rows(q, DK), rows(k, DK),
+                       rows(v, DV), g.data_ptr(), beta.data_ptr(), per_head(g), per_head(beta), _dptr(starts, i32), _dptr(lens, i32),
+                       _dptr(state, f32), _dptr(state_out, f32), _dptr(slots, i32), n_states,
+                       DK ** -0.5 if scale is None else scale, out.data_ptr(), rows(out, DV))
+    call(a, v.device, _stream_ptr(stream))
+    return out
+
+
+def _delta_chunked(a, device, stream):
+    ws = _scratch(lib().csb_delta_workspace_bytes(a), device)
+    _check(lib().csb_delta_chunked(a, _dptr(ws), stream))
+
+
+def _delta_recurrent(a, device, stream):
+    _check(lib().csb_delta_recurrent(a, stream))
+
+
+_KEEP = object()
+
+
+def delta_chunked(q, k, v, g, beta, scale=None, starts=None, lens=None, state=None, slots=None, state_out=_KEEP, out=None, stream=None):
+    """csb_delta_chunked: the gated delta rule over whole prompts.  q, k [tokens, heads_k, dk], v [tokens, heads_v, dv] (one
+    dtype: float32, float16 or bfloat16; rows of tokens may be strided), g (logarithm of the decay) and beta [tokens, heads_v]
+    float32.  starts [n_seq + 1] int32: where the packed sequences start (None: all of one length, as many as lens, slots or
+    states, or one).  lens [n_seq] int32: only that many tokens of each.  state [n_states, heads_v, dk, dv] float32, slots [n_seq] int32: each
+    sequence's state in it (None: in order).  The last states go to state_out: `state` itself unless another tensor or
+    None (not kept) is given.  scale: dk ** -0.5 unless given.  Returns out [tokens, heads_v, dv] (a new tensor, or `out`)."""
+    return _delta(_delta_chunked, q, k, v, g, beta, scale, starts, lens, state, slots, state if state_out is _KEEP else state_out, out, stream)
+
+
+def delta_recurrent(q, k, v, g, beta, scale=None, starts=None, lens=None, state=None, slots=None, state_out=_KEEP, out=None, stream=None):
+    """csb_delta_recurrent: the same rule token by token, for the few tokens of a decoding step; arguments as delta_chunked."""
+    return _delta(_delta_recurrent, q, k, v, g, beta, scale, starts, lens, state, slots, state if state_out is _KEEP else state_out, out, stream)
+
+
+def adapter_add(Y, X, A, B, ids, starts=None, scales=None, ranks=None, stream=None):
+    """csb_adapter_add: Y[:, n] += scales[a] B[a] (A[a] X[:, n]) for the columns of every request, in place.  X [cols, batch], A [adapters,
+    rank, cols] and B [adapters, rows, rank] of one dtype (float32, float16, bfloat16), Y [rows, batch] float32 (rows of X and Y may be
+    strided).  ids [requests] int32: the adapter of each request, -1 for none; starts [requests + 1] int32: its columns (None: one
+    each).  scales [adapters] float32, ranks [adapters] int32: factor and used ranks of an adapter.  Returns Y."""
+    import torch
+    cols, batch = X.shape
+    n, rank, _ = A.shape
+    rows = Y.shape[0]
+    i32, f32 = torch.int32, torch.float32
+    assert X.is_cuda and Y.is_cuda and Y.shape[1] == batch and Y.dtype is f32 and X.dtype is A.dtype is B.dtype
+    assert A.shape[2] == cols and tuple(B.shape) == (n, rows, rank)
+    (ldx, one_x), (ldy, one_y) = X.stride(), Y.stride()
+    assert batch < 2 or (one_x == 1 and one_y == 1)
+    assert (starts is None or starts.numel() == ids.numel() + 1) and all(t is None or t.numel() == n for t in (scales, ranks))
+    segs = ids.numel()
+    ws = _scratch(max(int(lib().csb_adapter_workspace_bytes(cols, batch, segs, rank)), 256), X.device)
+    _check(lib().csb_adapter_add(_val_type(X.dtype), X.data_ptr(), max(ldx, batch), Y.data_ptr(), max(ldy, batch), rows, cols, batch,
+                                 _dptr(A), _dptr(B), n, rank, _dptr(ranks, i32), _dptr(scales, f32), segs, _dptr(starts, i32),
+                                 _dptr(ids, i32), _dptr(ws), _stream_ptr(stream)))
+    return Y
+
+
+def verify_drafts(p, q, drafts, u, r, counts=None, stream=None):
+    """csb_verify_drafts: p [requests, drafts + 1, vocab] the target's probabilities, q [requests, drafts, vocab] the draft's (None: all
+    of the mass on the drafted token) of one dtype (float32, float16, bfloat16); drafts [requests, n] int32, u [requests, n] and r [requests]
+    float32 numbers in [0, 1); counts [requests] int32: drafts that a request brings (None: n).  Returns (tokens
+    [requests, n + 1] int32: the accepted drafts, the token drawn behind them, -1; accepted [requests] int32)."""
+    import torch
+    N, K1, V = p.shape
+    K = K1 - 1
+    i32, f32 = torch.int32, torch.float32
+
+    def rows(t, n):
+        assert t.is_cuda and t.shape[2] == V and (V == 1 or t.stride(2) == 1)
+        ld = t.stride(1) if n > 1 else max(V, t.stride(0))
+        assert N < 2 or t.stride(0) == n * ld, "rows of the requests must follow each other at one stride"
+        return ld
+    assert tuple(drafts.shape) == (N, K) and tuple(u.shape) == (N, K) and r.numel() == N and (counts is None or counts.numel() == N)
+    ldq = 0
+    if q is not None and K:
+        assert tuple(q.shape[:2]) == (N, K) and q.dtype is p.dtype
+        ldq = rows(q, K)
+    tokens = torch.empty((N, K1), dtype=i32, device=p.device)
+    accepted = torch.empty(N, dtype=i32, device=p.device)
+    ws = _scratch(max(int(lib().csb_verify_workspace_bytes(N, V)), 256), p.device)
+    _check(lib().csb_verify_drafts(_val_type(p.dtype), p.data_ptr(), rows(p, K1), q.data_ptr() if ldq else None, ldq, _dptr(drafts, i32),
+                                   _dptr(u, f32), _dptr(r, f32), _dptr(counts, i32), N, K, V, _dptr(tokens), _dptr(accepted),
+                                   _dptr(ws), _stream_ptr(stream)))
+    return tokens, accepted
 
 
 class CsbMatrix:

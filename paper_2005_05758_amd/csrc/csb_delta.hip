@@ -1,0 +1,208 @@
+// The gated delta rule token by token (csb_delta_recurrent), and the checks of its arguments.
+//
+// Per value head, with the state S in binary32:  S <- e^g S;  u = beta (v - S^T k);  S <- S + k u^T;
+// o = scale S^T q.  The columns of S do not depend on each other, so a wavefront takes 16 of them with
+// all their rows and keeps them in registers from the first token to the last: a state is read once and
+// written once however many tokens a call brings.  Both products are taken from the decayed state before
+// the update, o = scale (S^T q + (k.q) u): one reduction per token instead of two that wait for each other.
+#include "csb_delta.hpp"
+
+namespace csb {
+
+// Lane (x = lane / 16, y = lane % 16) holds the 4 columns from 4 x on of the rows y JN .. y JN + JN - 1, so a sum over
+// rows is JN steps in registers and four rotations of 16 lanes.  VEC: operands that are aligned to 4
+// elements, widths that are multiples of 4.
+template <int VF, int JN, bool VEC>
+__global__ __launch_bounds__(256) void delta_recurrent_kernel(const DeltaDev a, const uint32_t tiles) {
+    using T = typename Elem<VF>::T;
+    using T4 = T __attribute__((ext_vector_type(4)));
+    using f32x4 = float __attribute__((ext_vector_type(4)));
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, x = lane >> 4, y = lane & 15u;
+    const uint32_t tile = blockIdx.x % tiles, rest = blockIdx.x / tiles, h = rest % a.hv, seq = rest / a.hv;
+    const uint32_t col0 = (tile * 4 + wave) * 16;
+    if (col0 >= (uint32_t)a.dv) return;                        // (no barrier in this kernel)
+    const uint32_t col = col0 + 4 * x, row = y * JN, DK = a.dk, DV = a.dv;
+    int64_t first, end, slot;
+    delta_sequence(a, (int)seq, &first, &end, &slot);
+    const size_t state = ((size_t)(slot < 0 ? 0 : slot) * a.hv + h) * DK * DV;
+    f32x4 S[JN];
+#pragma unroll
+    for (int j = 0; j < JN; ++j) {
+        S[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (a.s_in && slot >= 0 && row + j < DK) {
+            const float *p = a.s_in + state + (size_t)(row + j) * DV + col;
+            if constexpr (VEC) {
+                if (col < DV) S[j] = *(const f32x4 *)p;
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) if (col + c < DV) S[j][c] = p[c];
+            }
+        }
+    }
+    struct Token { float k[JN], q[JN], v[4], g, beta; };
+    const uint32_t kh = h / a.group;
+    auto load = [&](int64_t t, Token &w) {
+        const T *kp = (const T *)a.k + t * a.ldk + (size_t)kh * DK + row, *qp = (const T *)a.q + t * a.ldq + (size_t)kh * DK + row;
+        const T *vp = (const T *)a.v + t * a.ldv + (size_t)h * DV + col;
+        if constexpr (VEC) {
+#pragma unroll
+            for (int j = 0; j < JN; j += 4) {
+                T4 kk{}, qq{};
+                if (row + j < DK) { kk = *(const T4 *)(kp + j); qq = *(const T4 *)(qp + j); }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) { w.k[j + c] = (float)kk[c]; w.q[j + c] = (float)qq[c]; }
+            }
+            T4 vv{};
+            if (col < DV) vv = *(const T4 *)vp;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) w.v[c] = (float)vv[c];
+        } else {
+#pragma unroll
+            for (int j = 0; j < JN; ++j) {
+                w.k[j] = row + j < DK ? (float)kp[j] : 0.0f;
+                w.q[j] = row + j < DK ? (float)qp[j] : 0.0f;
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) w.v[c] = col + c < DV ? (float)vp[c] : 0.0f;
+        }
+        w.g = a.g[t * a.ldg + h];
+        w.beta = a.beta[t * a.ldb + h];
+    };
+    Token now, next;
+    if (first < end) load(first, now);
+    for (int64_t t = first; t < end; ++t) {
+        if (t + 1 < end) load(t + 1, next);
+        const float decay = expf(now.g);
+        f32x4 pk{0.0f, 0.0f, 0.0f, 0.0f}, pq = pk;
+        float kq = 0.0f;
+#pragma unroll
+        for (int j = 0; j < JN; ++j) {
+            S[j] *= decay;
+            pk += S[j] * now.k[j];
+            pq += S[j] * now.q[j];
+            kq = fmaf(now.k[j], now.q[j], kq);
+        }
+        kq = row_sum(kq);
+        f32x4 u, o;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            u[c] = now.beta * (now.v[c] - row_sum(pk[c]));
+            o[c] = a.scale * fmaf(kq, u[c], row_sum(pq[c]));
+        }
+#pragma unroll
+        for (int j = 0; j < JN; ++j) S[j] += now.k[j] * u;
+        if (y == 0) {
+            T *op = (T *)a.out + t * a.ldo + (size_t)h * DV + col;
+            if constexpr (VEC) {
+                T4 oo;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) oo[c] = (T)o[c];
+                if (col < DV) *(T4 *)op = oo;
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) if (col + c < DV) op[c] = (T)o[c];
+            }
+        }
+        now = next;
+    }
+    if (!a.s_out || slot < 0) return;
+#pragma unroll
+    for (int j = 0; j < JN; ++j) {
+        if (row + j >= DK) continue;
+        float *p = a.s_out + state + (size_t)(row + j) * DV + col;
+        if constexpr (VEC) {
+            if (col < DV) *(f32x4 *)p = S[j];
+        } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) if (col + c < DV) p[c] = S[j][c];
+        }
+    }
+}
+
+int check_delta(const char *who, const csb_delta_args *a) {
+    const auto fail = [&](int code, const char *what) { set_error(std::string(who) + ": " + what); return code; };
+    if (!a) return fail(CSB_EINVAL, "NULL arguments");
+    if (!known_type(a->type)) return fail(CSB_EINVAL, "unknown type");
+    if (a->n_seq < 0 || a->n_tokens < 0 || a->heads_k < 1 || a->heads_v < 1 || a->dk < 1 || a->dv < 1) return fail(CSB_EINVAL, "bad size");
+    if (a->heads_v % a->heads_k) return fail(CSB_EINVAL, "heads_v is no multiple of heads_k");
+    if (a->dk > 256) return fail(CSB_EUNSUPPORTED, "dk above 256 (a state's rows are held in the registers of 16 lanes)");
+    if (a->n_tokens > 0x7fffffff) return fail(CSB_EUNSUPPORTED, "offsets are 32-bit: more than 2^31 - 1 tokens");
+    if (a->n_tokens && (!a->d_q || !a->d_k || !a->d_v || !a->d_g || !a->d_beta || !a->d_out)) return fail(CSB_EINVAL, "NULL pointer");
+    const int64_t wk = (int64_t)a->heads_k * a->dk, wv = (int64_t)a->heads_v * a->dv;
+    if (a->ldq < wk || a->ldk < wk || a->ldv < wv || a->ldo < wv || a->ldg < a->heads_v || a->ldbeta < a->heads_v)
+        return fail(CSB_EINVAL, "a leading dimension below the width of its rows");
+    if (!a->d_start && a->n_seq && a->n_tokens % a->n_seq) return fail(CSB_EINVAL, "n_tokens is no multiple of n_seq (and there are no offsets)");
+    if ((a->d_state_in || a->d_state_out) && a->n_states < 1) return fail(CSB_EINVAL, "states without room for one");
+    if (((uintptr_t)a->d_state_in | (uintptr_t)a->d_state_out | (uintptr_t)a->d_g | (uintptr_t)a->d_beta) % 4) return fail(CSB_EINVAL, "misaligned pointer");
+    if (((uintptr_t)a->d_q | (uintptr_t)a->d_k | (uintptr_t)a->d_v | (uintptr_t)a->d_out) % type_size(a->type)) return fail(CSB_EINVAL, "misaligned pointer");
+    return CSB_OK;
+}
+
+DeltaDev delta_dev(const csb_delta_args *a) {
+    DeltaDev d{};
+    d.q = a->d_q; d.k = a->d_k; d.v = a->d_v; d.g = a->d_g; d.beta = a->d_beta;
+    d.start = a->d_start; d.len = a->d_len; d.slot = a->d_slot;
+    d.s_in = a->d_state_in; d.s_out = a->d_state_out; d.out = a->d_out;
+    d.ldq = a->ldq; d.ldk = a->ldk; d.ldv = a->ldv; d.ldg = a->ldg; d.ldb = a->ldbeta; d.ldo = a->ldo;
+    d.n_tokens = a->n_tokens;
+    d.each = a->n_seq ? a->n_tokens / a->n_seq : 0;
+    d.hk = a->heads_k; d.hv = a->heads_v; d.group = a->heads_v / a->heads_k;
+    d.dk = a->dk; d.dv = a->dv; d.n_seq = a->n_seq; d.n_states = a->n_states;
+    d.scale = a->scale;
+    return d;
+}
+
+template <int VF, int JN>
+static void launch_recurrent(const DeltaDev &d, bool vec, uint32_t tiles, uint32_t groups, hipStream_t st) {
+    if (vec) hipLaunchKernelGGL((delta_recurrent_kernel<VF, JN, true>), dim3(groups), dim3(256), 0, st, d, tiles);
+    else hipLaunchKernelGGL((delta_recurrent_kernel<VF, JN, false>), dim3(groups), dim3(256), 0, st, d, tiles);
+}
+
+template <int VF>
+static void launch_recurrent(const DeltaDev &d, bool vec, uint32_t tiles, uint32_t groups, hipStream_t st) {
+    if (d.dk <= 64) launch_recurrent<VF, 4>(d, vec, tiles, groups, st);
+    else if (d.dk <= 128) launch_recurrent<VF, 8>(d, vec, tiles, groups, st);
+    else launch_recurrent<VF, 16>(d, vec, tiles, groups, st);
+}
+
+int launch_delta_recurrent(const csb_delta_args *a, hipStream_t st) {
+    const int64_t tiles = ((int64_t)a->dv + 63) / 64;
+    if (tiles * a->heads_v > kMaxWorkgroups || tiles * a->heads_v * a->n_seq > kMaxWorkgroups) {
+        set_error("csb_delta: more than 2^24 workgroups");
+        return CSB_EUNSUPPORTED;
+    }
+    const DeltaDev d = delta_dev(a);
+    const uintptr_t four = 4 * (uintptr_t)type_size(a->type);
+    const bool vec = a->dk % 4 == 0 && a->dv % 4 == 0 && a->ldq % 4 == 0 && a->ldk % 4 == 0 && a->ldv % 4 == 0 && a->ldo % 4 == 0 &&
+                     ((uintptr_t)a->d_q | (uintptr_t)a->d_k | (uintptr_t)a->d_v | (uintptr_t)a->d_out) % four == 0 &&
+                     ((uintptr_t)a->d_state_in | (uintptr_t)a->d_state_out) % 16 == 0;
+    const uint32_t groups = (uint32_t)(tiles * a->heads_v * a->n_seq);
+    switch (a->type) {
+        case CSB_VAL_F32: launch_recurrent<CSB_VAL_F32>(d, vec, (uint32_t)tiles, groups, st); break;
+        case CSB_VAL_F16: launch_recurrent<CSB_VAL_F16>(d, vec, (uint32_t)tiles, groups, st); break;
+        default: launch_recurrent<CSB_VAL_BF16>(d, vec, (uint32_t)tiles, groups, st); break;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_error(std::string("csb_delta: ") + hipGetErrorString(e)); return CSB_EDEVICE; }
+    return CSB_OK;
+}
+
+}  // namespace csb
+
+extern "C" int csb_delta_recurrent(const csb_delta_args *args, void *stream) {
+    const int rc = csb::check_delta("csb_delta_recurrent", args);
+    if (rc != CSB_OK || args->n_seq == 0) return rc;
+    return csb::launch_delta_recurrent(args, (hipStream_t)stream);
+}
+
+extern "C" size_t csb_delta_workspace_bytes(const csb_delta_args *args) {
+    (void)args;
+    return 0;
+}
+
+extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *stream) {
+    (void)d_ws;
+    const int rc = csb::check_delta("csb_delta_chunked", args);
+    if (rc != CSB_OK || args->n_seq == 0) return rc;
+    return csb::launch_delta_recurrent(args, (hipStream_t)stream);
+}

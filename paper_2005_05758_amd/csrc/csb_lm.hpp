@@ -1,0 +1,67 @@
+// What the kernels of the language-model operators share: element types, packed sequences,
+// sums over lanes.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "csb_internal.hpp"
+#include "csbrnn_lm.h"
+
+namespace csb {
+
+constexpr int64_t kMaxWorkgroups = 1 << 24;    // of 256 threads: a grid has fewer than 2^32 threads
+
+inline bool known_type(int32_t type) { return type == CSB_VAL_F32 || type == CSB_VAL_F16 || type == CSB_VAL_BF16; }
+inline int32_t type_size(int32_t type) { return type == CSB_VAL_F32 ? 4 : 2; }
+
+template <int VF> struct Elem;
+template <> struct Elem<CSB_VAL_F32> { using T = float; };
+template <> struct Elem<CSB_VAL_F16> { using T = _Float16; };
+template <> struct Elem<CSB_VAL_BF16> { using T = __bf16; };
+
+// Tiles of `1 << shift` packed places that a sequence's places fall into, numbered so that the number is known from
+// the offsets alone: sequence i has the numbers from (start_i >> shift) + i on.  Its tiles are at most
+// (end_i >> shift) - (start_i >> shift) + 1, so the ranges do not overlap and (total >> shift) + n_seq numbers are enough; those
+// of a range that no tile has do nothing.
+inline int64_t tile_numbers(int64_t total, int64_t n_seq, int shift) { return (total >> shift) + n_seq; }
+
+#ifdef __HIPCC__
+// Where a sequence starts and ends: d_start's offsets, or equal lengths; never outside [0, total].
+__device__ __forceinline__ int64_t clamp64(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
+__device__ __forceinline__ void sequence_range(const int32_t *start, int64_t i, int64_t each, int64_t total, int64_t *first, int64_t *end) {
+    if (start) {
+        *first = clamp64(start[i], 0, total);
+        *end = clamp64(start[i + 1], *first, total);
+    } else {
+        *first = i * each;
+        *end = *first + each;
+    }
+}
+
+// The sequence that tile number `tile` belongs to: one less than the count of sequences whose numbers
+// start at or below it.  All threads of the workgroup call it (one barrier for 256 sequences).
+__device__ __forceinline__ int tile_sequence(const int32_t *start, int n_seq, int64_t total, int shift, int64_t tile) {
+    int n = 0;
+    for (int base = 0; base < n_seq; base += (int)blockDim.x) {
+        const int i = base + (int)threadIdx.x;
+        const int below = __syncthreads_count(i < n_seq && (clamp64(start[i], 0, total) >> shift) + i <= tile);
+        n += below;
+        if (below < (int)blockDim.x) break;
+    }
+    return n - 1;
+}
+
+// Sum over the 16 lanes of a DPP row, in every one of them (a fixed order).
+template <int N> __device__ __forceinline__ float row_rotated(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float row_sum(float v) {
+    v += row_rotated<8>(v);
+    v += row_rotated<4>(v);
+    v += row_rotated<2>(v);
+    v += row_rotated<1>(v);
+    return v;
+}
+#endif
+
+}  // namespace csb
