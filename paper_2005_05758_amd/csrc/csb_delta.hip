@@ -194,15 +194,3 @@ extern "C" int csb_delta_recurrent(const csb_delta_args *args, void *stream) {
     if (rc != CSB_OK || args->n_seq == 0) return rc;
     return csb::launch_delta_recurrent(args, (hipStream_t)stream);
 }
-
-extern "C" size_t csb_delta_workspace_bytes(const csb_delta_args *args) {
-    (void)args;
-    return 0;
-}
-
-extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *stream) {
-    (void)d_ws;
-    const int rc = csb::check_delta("csb_delta_chunked", args);
-    if (rc != CSB_OK || args->n_seq == 0) return rc;
-    return csb::launch_delta_recurrent(args, (hipStream_t)stream);
-}

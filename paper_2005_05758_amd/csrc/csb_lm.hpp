@@ -39,12 +39,12 @@ __device__ __forceinline__ void sequence_range(const int32_t *start, int64_t i, 
 }
 
 // The sequence that tile number `tile` belongs to: one less than the count of sequences whose numbers
-// start at or below it.  All threads of the workgroup call it (one barrier for 256 sequences).
-__device__ __forceinline__ int tile_sequence(const int32_t *start, int n_seq, int64_t total, int shift, int64_t tile) {
+// start at or below it (no offsets: sequences of `each` places).  All threads of the workgroup call it (one barrier for 256 sequences).
+__device__ __forceinline__ int tile_sequence(const int32_t *start, int n_seq, int64_t total, int shift, int64_t tile, int64_t each = 0) {
     int n = 0;
     for (int base = 0; base < n_seq; base += (int)blockDim.x) {
         const int i = base + (int)threadIdx.x;
-        const int below = __syncthreads_count(i < n_seq && (clamp64(start[i], 0, total) >> shift) + i <= tile);
+        const int below = __syncthreads_count(i < n_seq && ((start ? clamp64(start[i], 0, total) : i * each) >> shift) + i <= tile);
         n += below;
         if (below < (int)blockDim.x) break;
     }
