@@ -419,46 +419,59 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(const DeltaDev a
     const int chunks = (int)((end - first + kChunk - 1) >> kChunkShift);
     const int64_t number0 = (first >> kChunkShift) + seq;
 
+    // Offsets within a chunk fit 32 bits (leading dimensions below 2^24): an address is a chunk's base and a lane's offset.
+    const uint32_t ldk = (uint32_t)(a.ldk * sizeof(T)), ldq = (uint32_t)(a.ldq * sizeof(T)), ldv = (uint32_t)(a.ldv * sizeof(T)), ldo = (uint32_t)(a.ldo * sizeof(T));
     // a chunk's operands into LDS; VEC: requested only (the wavefront's count of outstanding operations covers them)
     auto stage = [&](int c, uint32_t at) {
         const int64_t base = first + ((int64_t)c << kChunkShift);
         const uint8_t *block = ws + ((size_t)(number0 + c) * a.hv + h) * P::bytes;
-        constexpr uint32_t rows = 8 * DP, extra = (P::bytes + kFrag - 1) / kFrag;
-#pragma unroll 4
-        for (uint32_t u = wave; u < rows; u += NW) {           // operand u of K, then of Q
-            const bool is_q = u >= 4 * DP;
-            const uint32_t f = is_q ? u - 4 * DP : u, pt = f / DP, dp = f % DP, mm = (m - g) & 15u;
-            const int64_t t = min(base + (int64_t)(32 * (pt >> 1) + 2 * mm + (pt & 1u)), end - 1);   // (past the end M and P have zeros)
-            const T *row = is_q ? (const T *)a.q + t * a.ldq + (size_t)kh * DK : (const T *)a.k + t * a.ldk + (size_t)kh * DK;
-            const int d = (int)(32 * dp + 8 * g);
-            if constexpr (VEC) {                               // past dk the first elements again (the state's rows there are zeros)
+        const uint8_t *kb = (const uint8_t *)((const T *)a.k + base * a.ldk + (size_t)kh * DK);
+        const uint8_t *qb = (const uint8_t *)((const T *)a.q + base * a.ldq + (size_t)kh * DK);
+        const uint32_t last = (uint32_t)min((int64_t)kChunk, end - base) - 1;  // (past the end M and P have zeros)
+        constexpr uint32_t extra = (P::bytes + kFrag - 1) / kFrag;
+#pragma unroll 1
+        for (uint32_t k = 0; k < 4 / NW; ++k) {
+            const uint32_t pt = wave + k * NW;                 // tile (p, t) = (pt / 2, pt % 2)
+            const uint32_t row = min(32 * (pt >> 1) + 2 * ((m - g) & 15u) + (pt & 1u), last);
 #pragma unroll
-                for (uint32_t i = 0; i < L::half; ++i) {
-                    const int e = d + (int)i * 4;
-                    to_lds16(row + (e < DK ? e : 0), at + u * L::frag + i * kFrag);
+            for (uint32_t dp = 0; dp < DP; ++dp) {
+                const uint32_t to = at + (pt * DP + dp) * L::frag;
+                const int d = (int)(32 * dp + 8 * g);
+                if constexpr (VEC) {                           // past dk the first elements again (the state's rows there are zeros)
+#pragma unroll
+                    for (uint32_t i = 0; i < L::half; ++i) {
+                        const uint32_t e = (uint32_t)(d + (int)i * 4 < DK ? d + (int)i * 4 : 0) * (uint32_t)sizeof(T);
+                        to_lds16(kb + (row * ldk + e), to + i * kFrag);
+                        to_lds16(qb + (row * ldq + e), to + L::q + i * kFrag);
+                    }
+                } else {
+                    Row8<VF, false> kv, qv;
+                    kv.load((const T *)(kb + row * ldk), d, DK);
+                    qv.load((const T *)(qb + row * ldq), d, DK);
+#pragma unroll
+                    for (uint32_t i = 0; i < L::half; ++i) {
+                        *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)(to + i * kFrag + lane * 16) = kv.w[i];
+                        *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)(to + L::q + i * kFrag + lane * 16) = qv.w[i];
+                    }
                 }
-            } else {
-                Row8<VF, false> v;
-                v.load(row, d, DK);
-#pragma unroll
-                for (uint32_t i = 0; i < L::half; ++i)
-                    *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)(at + u * L::frag + i * kFrag + lane * 16) = v.w[i];
             }
         }
 #pragma unroll 4
-        for (uint32_t u = wave; u < extra; u += NW)
+        for (uint32_t k = 0; k < (extra + NW - 1) / NW; ++k) {
+            const uint32_t u = wave + k * NW;
             if (u * kFrag + lane * 16 < P::bytes) to_lds16(block + u * kFrag + lane * 16, at + L::m + u * kFrag);
+        }
     };
-    float v_next[2][8];
+    T v_next[2][8];                                            // of the next chunk (past the end the last token's)
+    const uint32_t v_col = ((uint32_t)h * DV + min(col, DV - 1)) * (uint32_t)sizeof(T), o_col = ((uint32_t)h * DV + col) * (uint32_t)sizeof(T);
     auto load_v = [&](int c) {
         const int64_t base = first + ((int64_t)c << kChunkShift);
+        const uint8_t *vb = (const uint8_t *)((const T *)a.v + base * a.ldv);
+        const uint32_t last = (uint32_t)min((int64_t)kChunk, end - base) - 1;
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int64_t t = base + 32 * p + 8 * (int)g + e;
-                v_next[p][e] = mine && t < end ? (float)((const T *)a.v)[t * a.ldv + (size_t)h * DV + col] : 0.0f;
-            }
+            for (int e = 0; e < 8; ++e) v_next[p][e] = *(const T *)(vb + (min(32 * p + 8 * g + e, last) * ldv + v_col));
     };
     u32x4 Sp[DP][3];
     auto split_state = [&]() {
@@ -486,7 +499,9 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(const DeltaDev a
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[p][e] = v_next[p][e];
+            for (int e = 0; e < 8; ++e) v[p][e] = (float)v_next[p][e];
+        const int64_t base = first + ((int64_t)c << kChunkShift);
+        const int count = (int)min((int64_t)kChunk, end - base);
         if (c + 1 < chunks) {
             load_v(c + 1);
             if (ahead) stage(c + 1, lds0 + ((c + 1) & 1) * L::bytes);
@@ -549,7 +564,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(const DeltaDev a
             u32x4 Up[2][3];
             split8<S2>(U[0], Up[0]);
             split8<S2>(U[1], Up[1]);
-            const int64_t base = first + ((int64_t)c << kChunkShift);
+            uint8_t *ob = (uint8_t *)((T *)a.out + base * a.ldo);
 #pragma unroll
             for (int p = 0; p < 2; ++p)
 #pragma unroll
@@ -563,10 +578,23 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(const DeltaDev a
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int row = 32 * p + 8 * (int)g + 2 * r + t;
-                        const float x = row >= bad ? __builtin_nanf("") : a.scale * o[p][t][r];
-                        if (mine && base + row < end) ((T *)a.out)[(base + row) * a.ldo + (size_t)h * DV + col] = (T)x;
+                        o[p][t][r] = row >= bad ? __builtin_nanf("") : a.scale * o[p][t][r];
                     }
                 }
+            if (mine) {
+                if (count == kChunk) {
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) *(T *)(ob + ((32 * p + 8 * g + e) * ldo + o_col)) = (T)o[p][e & 1][e >> 1];
+                } else {
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (32 * p + 8 * (int)g + e < count) *(T *)(ob + ((32 * p + 8 * g + e) * ldo + o_col)) = (T)o[p][e & 1][e >> 1];
+                }
+            }
         }
         u32x4 Up[2][3];
 #pragma unroll
@@ -605,6 +633,8 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(const DeltaDev a
         split_state();
     }
     if (!a.s_out || slot < 0 || !mine) return;
+    int dk = DK;
+    asm volatile("" : "+v"(dk));                               // compared again here: the masks of the first loads would be kept in registers till now
 #pragma unroll
     for (int dp = 0; dp < DP; ++dp)
 #pragma unroll
@@ -612,7 +642,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(const DeltaDev a
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int d = 32 * dp + 8 * (int)g + 2 * r + t;
-                if (d < DK) a.s_out[state + (size_t)d * DV + col] = S[dp][t][r];
+                if (d < dk) a.s_out[state + (size_t)d * DV + col] = S[dp][t][r];
             }
 }
 
@@ -661,6 +691,9 @@ extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *s
     const auto fail = [](int code, const char *what) { set_error(std::string("csb_delta_chunked: ") + what); return code; };
     if (args->n_tokens && !d_ws) return fail(CSB_EINVAL, "NULL pointer");
     if ((uintptr_t)d_ws % 256) return fail(CSB_EINVAL, "workspace not 256-byte aligned");
+    const int64_t most = 0xffffffffll / (4 * kChunk);          // a chunk's offsets are 32-bit, in bytes
+    if (args->n_tokens && (args->ldq > most || args->ldk > most || args->ldv > most || args->ldo > most))
+        return fail(CSB_EUNSUPPORTED, "more than 2^24 - 1 elements from one token to the next");
     const int64_t numbers = tile_numbers(args->n_tokens, args->n_seq, kChunkShift);
     const int64_t pairs = ((int64_t)args->n_seq * args->heads_v + 7) / 8 * 8, wide = ((int64_t)args->dv + 63) / 64, narrow = ((int64_t)args->dv + 15) / 16;
     if (pairs > kMaxWorkgroups || pairs * narrow > kMaxWorkgroups || numbers * ((args->heads_v + 3) / 4) > kMaxWorkgroups)
