@@ -31,6 +31,7 @@ constexpr uint32_t kLower = 6;                 // operands that cover the lower 
 
 using f32x4 = float __attribute__((ext_vector_type(4)));
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
 
@@ -44,24 +45,27 @@ template <int VF> struct Parts {
     static constexpr uint32_t bytes = m_bytes + p_bytes + 512;
 };
 
-// Operand numbers.  Rows come in pairs of tiles: tile (p, t) has the rows 32 p + 2 m + t (m = 0 .. 15), so that the
-// results of a pair leave a lane with eight consecutive rows -- which is how the next product wants them as its other operand.
+// Operand numbers.  The 64 tokens of a chunk are four tiles (p, t) of 16 rows: row m of a tile is token
+// 32 p + 8 (m / 4) + 4 t + m % 4.  A product leaves a lane with four consecutive tokens of a column then, which are one half
+// of the eight consecutive ones that the next product wants from a lane of its other operand.
+__device__ __forceinline__ uint32_t tile_token(uint32_t pt, uint32_t m) { return 32 * (pt >> 1) + 8 * (m >> 2) + 4 * (pt & 1u) + (m & 3u); }
 __device__ __forceinline__ constexpr uint32_t lower_frag(int p, int t, int ks) { return p == 0 ? t : 2 + 2 * t + ks; }
 
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }   // a's in the low half
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 
-// x as N bfloat16 numbers, each the nearest to what is left: exact for N = 3 (8 bits and a sign each), to 2^-18 for N = 2.
-template <int N>
-__device__ __forceinline__ void split8(const float *x, u32x4 *part) {
+// E numbers as N bfloat16 numbers each, every part the nearest to what is left: exact for N = 3 (8 bits and a sign each), to
+// 2^-18 for N = 2.
+template <int N, int E, typename Words>
+__device__ __forceinline__ void split(const float *x, Words *part) {
     using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
-    float rest[8];
+    float rest[E];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rest[i] = x[i];
+    for (int i = 0; i < E; ++i) rest[i] = x[i];
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < E / 2; ++i) {
             const bf16x2 near = {(__bf16)rest[2 * i], (__bf16)rest[2 * i + 1]};
             const uint32_t two = __builtin_bit_cast(uint32_t, near);
             part[n][i] = two;
@@ -72,20 +76,18 @@ __device__ __forceinline__ void split8(const float *x, u32x4 *part) {
         }
 }
 
-// d += a b, over the parts whose product is not below 2^(-8 MOST); the small ones first.
-template <int NA, int NB, int MOST>
-__device__ __forceinline__ f32x4 mma(const u32x4 *a, const u32x4 *b, f32x4 d) {
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 d) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), d, 0, 0, 0);
+}
+
+// f(i, j) for the pairs of parts whose product is not below 2^(-8 MOST), the small ones first.
+template <int NA, int NB, int MOST, typename F>
+__device__ __forceinline__ void part_pairs(const F &f) {
 #pragma unroll
-    for (int s = NA + NB - 2; s >= 0; --s) {
-        if (s > MOST) continue;
+    for (int s = MOST; s >= 0; --s)
 #pragma unroll
-        for (int i = 0; i < NA; ++i) {
-            const int j = s - i;
-            if (j < 0 || j >= NB) continue;
-            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[i]), __builtin_bit_cast(bf16x8, b[j]), d, 0, 0, 0);
-        }
-    }
-    return d;
+        for (int i = 0; i < NA; ++i)
+            if (s - i >= 0 && s - i < NB) f(i, s - i);
 }
 
 // ---- first launch: M and P -----------------------------------------------------------------------
@@ -110,6 +112,8 @@ template <int VF, bool VEC> struct Row8 {
             __builtin_memcpy(w, e, sizeof(e));
         }
     }
+    // the same from a window, the row at byte `at` of it
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, uint32_t at, int d, int dk);
 };
 
 // d += a b^T over 32 elements of the rows, exact products, sums in binary32.
@@ -143,7 +147,7 @@ __device__ __forceinline__ void store_lower(const float (*m)[kLdT], uint8_t *to,
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int ks = 0; ks <= p; ++ks) {
-                const float *row = &m[32 * p + 2 * i + t][32 * ks + 8 * g];
+                const float *row = &m[tile_token(2 * p + t, i)][32 * ks + 8 * g];
                 float x[8];
                 *(f32x4 *)x = *(const f32x4 *)row;
                 *(f32x4 *)(x + 4) = *(const f32x4 *)(row + 4);
@@ -151,7 +155,7 @@ __device__ __forceinline__ void store_lower(const float (*m)[kLdT], uint8_t *to,
                 if constexpr (WHOLE) {
                     part[0] = *(u32x4 *)x;
                     part[1] = *(u32x4 *)(x + 4);
-                } else split8<NP>(x, part);
+                } else split<NP, 8>(x, part);
                 constexpr int n = WHOLE ? 2 : NP;
 #pragma unroll
                 for (int k = 0; k < n; ++k) *(u32x4 *)(to + (lower_frag(p, t, ks) * n + k) * kFrag + lane * 16) = part[k];
@@ -268,64 +272,104 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
 
 // ---- second launch: the chunks of a sequence one after the other ---------------------------------
 
-typedef const __attribute__((address_space(1))) void glb_void_t;
-typedef __attribute__((address_space(3))) void lds_void_t;
-__device__ __forceinline__ void to_lds16(const void *g, uint32_t at) {         // lane l's 16 bytes land at `at` + 16 l
-    __builtin_amdgcn_global_load_lds((glb_void_t *)g, (lds_void_t *)(uintptr_t)at, 16, 0, 0);
-}
 __device__ __forceinline__ u32x4 lds16(uint32_t at) { return *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)at; }
 __device__ __forceinline__ uint32_t lds4(uint32_t at) { return *(const __attribute__((address_space(3))) uint32_t *)(uintptr_t)at; }
-__device__ __forceinline__ f32x4 lds_f4(uint32_t at) { return __builtin_bit_cast(f32x4, lds16(at)); }
+__device__ __forceinline__ void to_lds(uint32_t at, u32x4 v) { *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)at = v; }
+__device__ __forceinline__ void to_lds(uint32_t at, u32x2 v) { *(__attribute__((address_space(3))) u32x2 *)(uintptr_t)at = v; }
+__device__ __forceinline__ void to_lds(uint32_t at, uint32_t v) { *(__attribute__((address_space(3))) uint32_t *)(uintptr_t)at = v; }
+// All that the wavefront wrote to LDS is there, for the whole workgroup.  (Global loads stay in flight: __syncthreads would wait for them.)
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// LDS of a chunk: K's operands, Q's (kDP * 4 each), then the chunk's block of the workspace.
-template <int VF, int DP> struct ChunkLds {
-    static constexpr uint32_t half = VF == CSB_VAL_F32 ? 2 : 1;               // 16-byte words of a lane's eight numbers
-    static constexpr uint32_t frag = half * kFrag, q = 4 * DP * frag, m = 2 * q;
-    static constexpr uint32_t bytes = m + (Parts<VF>::bytes + kFrag - 1) / kFrag * kFrag;
+// Memory from `base` on, `bytes` of it: reads past them give zero, writes past them do nothing, so that every lane may take part in every
+// access and the wavefront knows how many are in flight.
+using window_t = __amdgpu_buffer_rsrc_t;
+constexpr uint32_t kOutside = 0x80000000u;     // an offset past any window
+__device__ __forceinline__ window_t window(const void *base, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000);
+}
+template <int N> struct RawBits { using type = uint32_t; };
+template <> struct RawBits<2> { using type = uint16_t; };
+template <typename T> using raw_t = typename RawBits<sizeof(T)>::type;        // a number as it is stored
+template <typename T> __device__ __forceinline__ raw_t<T> window_load(window_t w, uint32_t at) {
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_raw_buffer_load_b16(w, (int)at, 0, 0);
+    else return __builtin_amdgcn_raw_buffer_load_b32(w, (int)at, 0, 0);
+}
+template <typename T> __device__ __forceinline__ void window_store(window_t w, uint32_t at, T v) {
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), w, (int)at, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), w, (int)at, 0, 0);
+}
+
+template <int VF, bool VEC>
+__device__ __forceinline__ void Row8<VF, VEC>::load(window_t from, uint32_t at, int d, int dk) {
+    if constexpr (VEC) {
+#pragma unroll
+        for (int i = 0; i < words; ++i) {
+            const int e = d + 8 / words * i;
+            w[i] = __builtin_amdgcn_raw_buffer_load_b128(from, (int)(e < dk ? at + e * (uint32_t)sizeof(T) : kOutside), 0, 0);
+        }
+    } else {
+        uint32_t e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = window_load<T>(from, d + i < dk ? at + (d + i) * (uint32_t)sizeof(T) : kOutside);
+#pragma unroll
+        for (int i = 0; i < 4 * words; ++i) w[i / 4][i % 4] = sizeof(T) == 2 ? low_halves(e[2 * i % 8], e[(2 * i + 1) % 8]) : e[i];
+    }
+}
+
+// LDS of a workgroup: the chunk's K, then per 16 columns two regions that S, R, U and e^(G_64 - G) U take in turn -- S's parts and
+// both of U's in one, R's and the next S's in the other, swapped from chunk to chunk, so that nothing is written before
+// a barrier behind its last reader -- and what tells of numbers that are not finite.
+template <int VF, int DP> struct ScanLds {
+    static constexpr uint32_t half = VF == CSB_VAL_F32 ? 2 : 1;               // 16-byte words of a lane's eight numbers of K
+    static constexpr uint32_t frag = half * kFrag, k = 4 * DP * frag;
+    static constexpr uint32_t u_bytes = (2 * Parts<VF>::out + 6) * kFrag;     // U's parts, then e^(G_64 - G) U's
+    static constexpr uint32_t region = 3 * DP * kFrag > u_bytes ? 3 * DP * kFrag : u_bytes;
+    static constexpr uint32_t flags = 2 * region, told = flags + 32, group = told + 2 * 4 * 16 * 4;
+    static constexpr uint32_t bytes(int groups) { return k + groups * group; }
 };
 
-// An operand of K or Q lies in LDS with lane (g, m)'s numbers -- row 2 m + t of its 32 tokens, elements 8 g to 8 g + 7 of its 32 --
-// at place 16 g + (m + g) % 16: the transposed reads below, 4 bytes from 16 places with m % 4 alike, then hit 16 different banks' words.
+// An operand of K lies in LDS with lane (g, m)'s numbers -- row m of its tile, elements 8 g to 8 g + 7 of its 32 -- at place
+// 16 g + (m + g) % 16: the transposed reads below, 4 bytes from 16 places with m % 4 alike, then hit 16 different banks' words.
 __device__ __forceinline__ uint32_t place(uint32_t g, uint32_t m) { return (g * 16 + ((m + g) & 15u)) * 16; }
 
-// The parts of an operand of K or Q (rows of tokens).
-template <int VF>
-__device__ __forceinline__ void row_parts(uint32_t at, u32x4 *part) {
-    if constexpr (VF == CSB_VAL_BF16) part[0] = lds16(at);
+// The parts of an operand of K or Q from its numbers.
+template <int VF, bool VEC>
+__device__ __forceinline__ void row_parts(const Row8<VF, VEC> &row, u32x4 *part) {
+    if constexpr (VF == CSB_VAL_BF16) part[0] = row.w[0];
     else {
         float x[8];
         if constexpr (VF == CSB_VAL_F16) {
-            const f16x8 v = __builtin_bit_cast(f16x8, lds16(at));
+            const f16x8 v = __builtin_bit_cast(f16x8, row.w[0]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
         } else {
-            *(u32x4 *)x = lds16(at);
-            *(u32x4 *)(x + 4) = lds16(at + kFrag);
+            *(u32x4 *)x = row.w[0];
+            *(u32x4 *)(x + 4) = row.w[1];
         }
-        split8<Parts<VF>::in>(x, part);
+        split<Parts<VF>::in, 8>(x, part);
     }
 }
 
 // The parts of K^T for elements 32 dp + 2 m + t (t = 0, 1: part[t]) of the tokens 32 ks + 8 g .. + 7.
 template <int VF, int DP>
-__device__ __forceinline__ void column_parts(uint32_t k_at, int dp, int ks, uint32_t g, uint32_t m, u32x4 part[2][3]) {
-    using L = ChunkLds<VF, DP>;
+__device__ __forceinline__ void column_parts(uint32_t k_at, int dp, int ks, uint32_t g, uint32_t m, u32x4 part[2][Parts<VF>::in]) {
+    using L = ScanLds<VF, DP>;
     if constexpr (VF == CSB_VAL_F32) {
         float x[2][8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint32_t at = k_at + ((2 * ks + (j & 1)) * DP + dp) * L::frag + place(m >> 2, 4 * g + (j >> 1)) + ((m >> 1) & 1u) * kFrag + (m & 1u) * 8;
+            const uint32_t at = k_at + ((2 * ks + (j >> 2)) * DP + dp) * L::frag + place(m >> 2, 4 * g + (j & 3)) + ((m >> 1) & 1u) * kFrag + (m & 1u) * 8;
             x[0][j] = __uint_as_float(lds4(at));
             x[1][j] = __uint_as_float(lds4(at + 4));
         }
-        split8<3>(x[0], part[0]);
-        split8<3>(x[1], part[1]);
+        split<3, 8>(x[0], part[0]);
+        split<3, 8>(x[1], part[1]);
     } else {
         u32x4 both[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t at = k_at + (2 * ks * DP + dp) * L::frag + place(m >> 2, 4 * g + j) + (m & 3u) * 4;
-            const uint32_t even = lds4(at), odd = lds4(at + DP * L::frag);     // tokens 2 j and 2 j + 1
+        for (int j = 0; j < 4; ++j) {                          // tokens 2 j and 2 j + 1
+            const uint32_t at = k_at + ((2 * ks + (j >> 1)) * DP + dp) * L::frag + (m & 3u) * 4;
+            const uint32_t even = lds4(at + place(m >> 2, 4 * g + 2 * (j & 1))), odd = lds4(at + place(m >> 2, 4 * g + 2 * (j & 1) + 1));
             both[0][j] = low_halves(even, odd);
             both[1][j] = high_halves(even, odd);
         }
@@ -337,312 +381,288 @@ __device__ __forceinline__ void column_parts(uint32_t k_at, int dp, int ks, uint
                 float x[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-                split8<2>(x, part[t]);
+                split<2, 8>(x, part[t]);
             }
         }
     }
 }
 
-// The parts of an operand of M (N = 3) or P.
-template <int VF, int N>
-__device__ __forceinline__ void lower_parts(uint32_t at, uint32_t f, uint32_t lane, u32x4 *part) {
-    if constexpr (Parts<VF>::whole) {
-        float x[8];
-        *(u32x4 *)x = lds16(at + 2 * f * kFrag + lane * 16);
-        *(u32x4 *)(x + 4) = lds16(at + (2 * f + 1) * kFrag + lane * 16);
-        split8<3>(x, part);
-    } else {
+// An operand of M (N = 3 parts) or P as it lies in the workspace, and its parts.
+template <int VF, int N> struct Lower {
+    static constexpr int words = Parts<VF>::whole ? 2 : N;
+    u32x4 w[words];
+    __device__ __forceinline__ void load(const uint8_t *from, uint32_t f, uint32_t lane) {
 #pragma unroll
-        for (int n = 0; n < N; ++n) part[n] = lds16(at + (f * N + n) * kFrag + lane * 16);
+        for (int i = 0; i < words; ++i) w[i] = *(const u32x4 *)(from + (f * words + i) * kFrag + lane * 16);
     }
-}
+    __device__ __forceinline__ void parts(u32x4 *part) const {
+        if constexpr (Parts<VF>::whole) {
+            float x[8];
+            *(u32x4 *)x = w[0];
+            *(u32x4 *)(x + 4) = w[1];
+            split<3, 8>(x, part);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) part[i] = w[i];
+        }
+    }
+};
 
-__device__ __forceinline__ bool any_not_finite(const float (*x)[8]) {
+// Takes numbers that are not finite out of a lane's four (tokens from `token` on) and says so: told[column] = the column's first
+// such token of the wavefront's, or kChunk.  Returns whether there were any.
+__device__ __forceinline__ bool take_out(float *x, int token, uint32_t told, uint32_t g, uint32_t m) {
     float z = 0.0f;
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
+    for (int r = 0; r < 4; ++r) z = fmaf(x[r], 0.0f, z);
+    if (__builtin_expect(__ballot(z != 0.0f) == 0, 1)) return false;          // (NaN is not 0 either)
+    int first = kChunk;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z = fmaf(x[p][e], 0.0f, z);
-    return __ballot(z != 0.0f) != 0;                           // (NaN is not 0 either)
+    for (int r = 3; r >= 0; --r)
+        if (!(fabsf(x[r]) < __builtin_inff())) { first = token + r; x[r] = 0.0f; }
+    first = min(first, __shfl_xor(first, 16));
+    first = min(first, __shfl_xor(first, 32));
+    if (g == 0) to_lds(told + m * 4, (uint32_t)first);
+    return true;
 }
 
-// The first token with a number in x that is not finite, over the lanes of a column (at most `before`); x is zero from it on.
-__device__ __forceinline__ int take_out(float (*x)[8], int before, uint32_t g) {
-    int bad = before;
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (!(fabsf(x[p][e]) < __builtin_inff())) bad = min(bad, 32 * p + 8 * (int)g + e);
-    bad = min(bad, __shfl_xor(bad, 16));
-    bad = min(bad, __shfl_xor(bad, 32));
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (32 * p + 8 * (int)g + e >= bad) x[p][e] = 0.0f;
-    return bad;
-}
-
-// A wavefront takes 16 columns of the state of one sequence and value head, NW of them share the chunk's operands in LDS.
-// Lane (g = lane / 16, m = lane % 16) has column m; of every 32 rows of a matrix with 16 columns (S, R, U) it has 8 g .. 8 g + 7.
+// Four wavefronts take 16 columns of the state of one sequence and value head; NG such groups share a chunk's K in LDS.  Wavefront pt of a
+// group makes the rows of tile pt = 2 p + t of the products over tokens (K S, Q S, M R, P U) and holds the state's rows 32 dp .. 32 dp + 31
+// for dp = pt, pt + 4: what one makes and the others multiply with goes through LDS, three barriers a chunk.  Its operands of Q, M and P
+// (and of K as rows) come from global memory into its registers, requested when the chunk before has used them.
+// Lane (g = lane / 16, m = lane % 16) has column m; of a tile over tokens the four from 8 g + 4 t on, of 32 rows of the state 8 g .. 8 g + 7.
 // DP: 32s of dk.  VEC: rows of q and k in aligned 16-byte words.
-template <int VF, int DP, int NW, bool VEC>
-__global__ __launch_bounds__(64 * NW, 1) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
+template <int VF, int DP, int NG, bool VEC>
+__global__ __launch_bounds__(256 * NG) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
     using T = typename Elem<VF>::T;
-    using L = ChunkLds<VF, DP>;
+    using L = ScanLds<VF, DP>;
     using P = Parts<VF>;
-    constexpr bool ahead = VEC && 2 * L::bytes <= 160 * 1024;                  // the next chunk is fetched during this one
-    constexpr int S2 = P::out;
+    constexpr int S2 = P::out, own = (DP + 3) / 4;
     extern __shared__ __align__(16) uint8_t smem[];
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, m = lane & 15u;
+    const uint32_t pt = wave & 3u, group = wave >> 2;
+    const uint32_t k_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
+    const uint32_t group_at = k_at + L::k + group * L::group;
     // workgroups of one sequence and head run on one XCD (they are dealt out by their number modulo 8): its L2 has their operands once
     const uint32_t pair = blockIdx.x / (8 * tiles) * 8 + blockIdx.x % 8, tile = blockIdx.x / 8 % tiles;
     if (pair >= (uint32_t)a.n_seq * a.hv) return;
     const uint32_t h = pair % a.hv, seq = pair / a.hv, kh = h / a.group;
-    const int DK = a.dk, DV = a.dv, col = (int)((tile * NW + wave) * 16 + m);
+    const int DK = a.dk, DV = a.dv, col = (int)((tile * NG + group) * 16 + m);
     const bool mine = col < DV;
-    int64_t first, end, slot;
-    delta_sequence(a, (int)seq, &first, &end, &slot);
+    int64_t first_, end_, slot;
+    delta_sequence(a, (int)seq, &first_, &end_, &slot);
+    const int first = __builtin_amdgcn_readfirstlane((int)first_), end = __builtin_amdgcn_readfirstlane((int)end_);
     const size_t state = (((size_t)(slot < 0 ? 0 : slot) * a.hv + h) * DK) * DV;
-    f32x4 S[DP][2];                                            // [dp][t][r]: row 32 dp + 8 g + 2 r + t
+    f32x4 S[own][2];                                           // [dp / 4][t][r]: row 32 dp + 8 g + 2 r + t
 #pragma unroll
-    for (int dp = 0; dp < DP; ++dp)
+    for (int w = 0; w < own; ++w)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int d = 32 * dp + 8 * (int)g + 2 * r + t;
-                S[dp][t][r] = a.s_in && slot >= 0 && mine && d < DK ? a.s_in[state + (size_t)d * DV + col] : 0.0f;
+                const int d = 32 * ((int)pt + 4 * w) + 8 * (int)g + 2 * r + t;
+                S[w][t][r] = a.s_in && slot >= 0 && mine && d < DK ? a.s_in[state + (size_t)d * DV + col] : 0.0f;
             }
-    const int chunks = (int)((end - first + kChunk - 1) >> kChunkShift);
-    const int64_t number0 = (first >> kChunkShift) + seq;
-
-    // Offsets within a chunk fit 32 bits (leading dimensions below 2^24): an address is a chunk's base and a lane's offset.
+    const int chunks = (int)(((uint32_t)(end - first) + kChunk - 1) >> kChunkShift);
+    const uint8_t *block0 = ws + ((size_t)((uint32_t)(first >> kChunkShift) + seq) * a.hv + h) * P::bytes;
+    // offsets within a chunk fit 31 bits (leading dimensions below 2^23)
     const uint32_t ldk = (uint32_t)(a.ldk * sizeof(T)), ldq = (uint32_t)(a.ldq * sizeof(T)), ldv = (uint32_t)(a.ldv * sizeof(T)), ldo = (uint32_t)(a.ldo * sizeof(T));
-    // a chunk's operands into LDS; VEC: requested only (the wavefront's count of outstanding operations covers them)
-    auto stage = [&](int c, uint32_t at) {
-        const int64_t base = first + ((int64_t)c << kChunkShift);
-        const uint8_t *block = ws + ((size_t)(number0 + c) * a.hv + h) * P::bytes;
-        const uint8_t *kb = (const uint8_t *)((const T *)a.k + base * a.ldk + (size_t)kh * DK);
-        const uint8_t *qb = (const uint8_t *)((const T *)a.q + base * a.ldq + (size_t)kh * DK);
-        const uint32_t last = (uint32_t)min((int64_t)kChunk, end - base) - 1;  // (past the end M and P have zeros)
-        constexpr uint32_t extra = (P::bytes + kFrag - 1) / kFrag;
-#pragma unroll 1
-        for (uint32_t k = 0; k < 4 / NW; ++k) {
-            const uint32_t pt = wave + k * NW;                 // tile (p, t) = (pt / 2, pt % 2)
-            const uint32_t row = min(32 * (pt >> 1) + 2 * ((m - g) & 15u) + (pt & 1u), last);
+    const uint8_t *k0 = (const uint8_t *)((const T *)a.k + (size_t)kh * DK), *q0 = (const uint8_t *)((const T *)a.q + (size_t)kh * DK);
+    const uint8_t *v0 = (const uint8_t *)((const T *)a.v + (size_t)h * DV), *o0 = (const uint8_t *)((const T *)a.out + (size_t)h * DV);
+    const int token = 32 * (int)(pt >> 1) + 8 * (int)g + 4 * (int)(pt & 1u);   // the first of the lane's four
+
+    // what the wavefront needs of a chunk
+    Row8<VF, VEC> kr[DP], qr[DP];
+    raw_t<T> v_0, v_1, v_2, v_3;                               // (an array of them would be packed, two to a register, as soon as they are loaded)
+    Lower<VF, 3> mr[2];
+    Lower<VF, 2> pr[2];
+    f32x4 eg, left;
+    float keep;
+    auto block = [&](int c) { return block0 + (size_t)c * a.hv * P::bytes; };
+    auto decay = [&](int c) { return (const float *)(block(c) + P::m_bytes + P::p_bytes); };
+    const uint32_t row = tile_token(pt, m), v_at = mine ? token * ldv + col * (uint32_t)sizeof(T) : kOutside, o_at = mine ? token * ldo + col * (uint32_t)sizeof(T) : kOutside;
+    auto at_token = [&](const uint8_t *base, int c, uint32_t ld, int width) {  // the chunk's tokens, `width` elements of each
+        const int before = c << kChunkShift, count = min(kChunk, end - first - before);
+        return window(base + (size_t)(first + before) * ld, (uint32_t)(count - 1) * ld + (uint32_t)width * (uint32_t)sizeof(T));
+    };
+    auto load_rows = [&](int c) {                              // (tokens past the end: zeros)
+        const window_t kw = at_token(k0, c, ldk, DK), qw = at_token(q0, c, ldq, DK), vw = at_token(v0, c, ldv, DV);
 #pragma unroll
-            for (uint32_t dp = 0; dp < DP; ++dp) {
-                const uint32_t to = at + (pt * DP + dp) * L::frag;
-                const int d = (int)(32 * dp + 8 * g);
-                if constexpr (VEC) {                           // past dk the first elements again (the state's rows there are zeros)
+        for (int dp = 0; dp < DP; ++dp) kr[dp].load(kw, row * ldk, 32 * dp + 8 * (int)g, DK);
 #pragma unroll
-                    for (uint32_t i = 0; i < L::half; ++i) {
-                        const uint32_t e = (uint32_t)(d + (int)i * 4 < DK ? d + (int)i * 4 : 0) * (uint32_t)sizeof(T);
-                        to_lds16(kb + (row * ldk + e), to + i * kFrag);
-                        to_lds16(qb + (row * ldq + e), to + L::q + i * kFrag);
-                    }
-                } else {
-                    Row8<VF, false> kv, qv;
-                    kv.load((const T *)(kb + row * ldk), d, DK);
-                    qv.load((const T *)(qb + row * ldq), d, DK);
+        for (int dp = 0; dp < DP; ++dp) qr[dp].load(qw, row * ldq, 32 * dp + 8 * (int)g, DK);
+        v_0 = window_load<T>(vw, v_at);
+        v_1 = window_load<T>(vw, v_at + ldv);
+        v_2 = window_load<T>(vw, v_at + 2 * ldv);
+        v_3 = window_load<T>(vw, v_at + 3 * ldv);
+        eg = *(const f32x4 *)(decay(c) + token);
+    };
+    // the first half of the chunk has one operand, the second two
+    const uint32_t f0 = pt < 2 ? pt : 2 * pt - 2, f1 = pt < 2 ? pt : 2 * pt - 1;
+    auto load_m = [&](int c) {
+        mr[0].load(block(c), f0, lane);
+        mr[1].load(block(c), f1, lane);
+        left = *(const f32x4 *)(decay(c) + 64 + token);
+    };
+    auto load_p = [&](int c) {
+        pr[0].load(block(c) + P::m_bytes, f0, lane);
+        pr[1].load(block(c) + P::m_bytes, f1, lane);
+        keep = decay(c)[63];
+    };
+    auto share_state = [&](uint32_t at) {                      // the parts of the wavefront's rows of S
 #pragma unroll
-                    for (uint32_t i = 0; i < L::half; ++i) {
-                        *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)(to + i * kFrag + lane * 16) = kv.w[i];
-                        *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)(to + L::q + i * kFrag + lane * 16) = qv.w[i];
-                    }
-                }
+        for (int w = 0; w < own; ++w)
+            if (DP >= 4 || (int)pt < DP) {
+                float x[8];
+                u32x4 part[3];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = S[w][e & 1][e >> 1];
+                split<3, 8>(x, part);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) to_lds(at + ((pt + 4 * w) * 3 + n) * kFrag + lane * 16, part[n]);
             }
-        }
-#pragma unroll 4
-        for (uint32_t k = 0; k < (extra + NW - 1) / NW; ++k) {
-            const uint32_t u = wave + k * NW;
-            if (u * kFrag + lane * 16 < P::bytes) to_lds16(block + u * kFrag + lane * 16, at + L::m + u * kFrag);
-        }
     };
-    T v_next[2][8];                                            // of the next chunk (past the end the last token's)
-    const uint32_t v_col = ((uint32_t)h * DV + min(col, DV - 1)) * (uint32_t)sizeof(T), o_col = ((uint32_t)h * DV + col) * (uint32_t)sizeof(T);
-    auto load_v = [&](int c) {
-        const int64_t base = first + ((int64_t)c << kChunkShift);
-        const uint8_t *vb = (const uint8_t *)((const T *)a.v + base * a.ldv);
-        const uint32_t last = (uint32_t)min((int64_t)kChunk, end - base) - 1;
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v_next[p][e] = *(const T *)(vb + (min(32 * p + 8 * g + e, last) * ldv + v_col));
-    };
-    u32x4 Sp[DP][3];
-    auto split_state = [&]() {
-#pragma unroll
-        for (int dp = 0; dp < DP; ++dp) {
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = S[dp][e & 1][e >> 1];
-            split8<3>(x, Sp[dp]);
-        }
-    };
-    split_state();
+    // where a lane's four tokens go in an operand over tokens: half (pt & 1) of the place of lane (g, m) of the 32 tokens pt >> 1
+    const uint32_t quad = (pt >> 1) * kFrag + lane * 16 + (pt & 1u) * 8;
+
     if (chunks > 0) {
-        load_v(0);
-        if (ahead) stage(0, lds0);
+        load_rows(0);
+        load_m(0);
+        load_p(0);
+        share_state(group_at);
     }
     for (int c = 0; c < chunks; ++c) {
-        const uint32_t at = ahead ? lds0 + (c & 1) * L::bytes : lds0;
-        if (!ahead) {
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");    // the chunk before is done with
-            stage(c, at);
-        }
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        float v[2][8];
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[p][e] = (float)v_next[p][e];
-        const int64_t base = first + ((int64_t)c << kChunkShift);
-        const int count = (int)min((int64_t)kChunk, end - base);
-        if (c + 1 < chunks) {
-            load_v(c + 1);
-            if (ahead) stage(c + 1, lds0 + ((c + 1) & 1) * L::bytes);
-        }
-        const uint32_t decay = at + L::m + P::m_bytes + P::p_bytes;
-
-        f32x4 ks[2][2], o[2][2];
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-#pragma unroll
-            for (int t = 0; t < 2; ++t) ks[p][t] = o[p][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int dp = 0; dp < DP; ++dp)
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    u32x4 part[3];
-                    const uint32_t f = at + ((2 * p + t) * DP + dp) * L::frag + place(g, m);
-                    row_parts<VF>(f, part);
-                    ks[p][t] = mma<P::in, 3, 2>(part, Sp[dp], ks[p][t]);
-                    row_parts<VF>(f + L::q, part);
-                    o[p][t] = mma<P::in, S2, S2 - 1>(part, Sp[dp], o[p][t]);
-                }
-        float R[2][8];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            float eg[8];
-            *(f32x4 *)eg = lds_f4(decay + (32 * p + 8 * g) * 4);
-            *(f32x4 *)(eg + 4) = lds_f4(decay + (32 * p + 8 * g) * 4 + 16);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                R[p][e] = v[p][e] - eg[e] * ks[p][e & 1][e >> 1];
-                o[p][e & 1][e >> 1] *= eg[e];
-            }
-        }
-        int bad = kChunk;
-        if (any_not_finite(R)) bad = take_out(R, bad, g);      // uniform
-        u32x4 Rp[2][3];
-        split8<3>(R[0], Rp[0]);
-        split8<3>(R[1], Rp[1]);
-        float U[2][8];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                f32x4 u{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int s = 0; s <= p; ++s) {
-                    u32x4 part[3];
-                    lower_parts<VF, 3>(at + L::m, lower_frag(p, t, s), lane, part);
-                    u = mma<3, 3, 2>(part, Rp[s], u);
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) U[p][2 * r + t] = u[r];
-            }
-        }
-        if (any_not_finite(U) || bad < kChunk) bad = take_out(U, bad, g);
-        {
-            u32x4 Up[2][3];
-            split8<S2>(U[0], Up[0]);
-            split8<S2>(U[1], Up[1]);
-            uint8_t *ob = (uint8_t *)((T *)a.out + base * a.ldo);
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-#pragma unroll
-                    for (int s = 0; s <= p; ++s) {
-                        u32x4 part[3];
-                        lower_parts<VF, 2>(at + L::m + P::m_bytes, lower_frag(p, t, s), lane, part);
-                        o[p][t] = mma<S2, S2, S2 - 1>(part, Up[s], o[p][t]);
-                    }
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int row = 32 * p + 8 * (int)g + 2 * r + t;
-                        o[p][t][r] = row >= bad ? __builtin_nanf("") : a.scale * o[p][t][r];
-                    }
-                }
-            if (mine) {
-                if (count == kChunk) {
-#pragma unroll
-                    for (int p = 0; p < 2; ++p)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) *(T *)(ob + ((32 * p + 8 * g + e) * ldo + o_col)) = (T)o[p][e & 1][e >> 1];
-                } else {
-#pragma unroll
-                    for (int p = 0; p < 2; ++p)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (32 * p + 8 * (int)g + e < count) *(T *)(ob + ((32 * p + 8 * g + e) * ldo + o_col)) = (T)o[p][e & 1][e >> 1];
-                }
-            }
-        }
-        u32x4 Up[2][3];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            float left[8];
-            *(f32x4 *)left = lds_f4(decay + 256 + (32 * p + 8 * g) * 4);
-            *(f32x4 *)(left + 4) = lds_f4(decay + 256 + (32 * p + 8 * g) * 4 + 16);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) left[e] *= U[p][e];
-            split8<3>(left, Up[p]);
-        }
-        const float keep = __uint_as_float(lds4(decay + 63 * 4));
+        const uint32_t here = group_at + (c & 1) * L::region, there = group_at + (~c & 1) * L::region;
+        // (behind the last chunk its operands are requested again: what is in flight is known at every wait only if nothing is requested sometimes)
+        const int next = min(c + 1, chunks - 1);
+        lds_barrier();                                         // S is there, and the chunk before is done with
+        f32x4 ks[2], o[2];
+        ks[0] = ks[1] = o[0] = o[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int dp = 0; dp < DP; ++dp) {
-            S[dp][0] *= keep;
-            S[dp][1] *= keep;
+            u32x4 sp[3], part[P::in];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                u32x4 part[2][3];
-                column_parts<VF, DP>(at, dp, s, g, m, part);
-                S[dp][0] = mma<P::in, 3, 2>(part[0], Up[s], S[dp][0]);
-                S[dp][1] = mma<P::in, 3, 2>(part[1], Up[s], S[dp][1]);
+            for (int n = 0; n < 3; ++n) sp[n] = lds16(here + (dp * 3 + n) * kFrag + lane * 16);
+            row_parts<VF, VEC>(kr[dp], part);
+            part_pairs<P::in, 3, 2>([&](int i, int j) { ks[dp & 1] = mfma16(part[i], sp[j], ks[dp & 1]); });
+            row_parts<VF, VEC>(qr[dp], part);
+            part_pairs<P::in, S2, S2 - 1>([&](int i, int j) { o[dp & 1] = mfma16(part[i], sp[j], o[dp & 1]); });
+        }
+#pragma unroll
+        for (int dp = 0; dp < DP; ++dp)                        // K for the transposed reads: the groups share the work
+            if (dp % NG == (int)group)
+#pragma unroll
+                for (uint32_t i = 0; i < L::half; ++i) to_lds(k_at + (pt * DP + dp) * L::frag + i * kFrag + place(g, m), kr[dp].w[i]);
+        float R[4];
+        const raw_t<T> v[4] = {v_0, v_1, v_2, v_3};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) R[r] = fmaf(-eg[r], ks[0][r] + ks[1][r], (float)__builtin_bit_cast(T, v[r]));
+        f32x4 out = (o[0] + o[1]) * eg;
+        asm volatile("" : "+v"(out) :: "memory");              // (here, so that the next chunk's factors can come into the same registers)
+        const bool bad_r = take_out(R, token, group_at + L::told + pt * 64, g, m);
+        {
+            u32x2 part[3];
+            split<3, 4>(R, part);
+#pragma unroll
+            for (int n = 0; n < 3; ++n) to_lds(there + n * 2 * kFrag + quad, part[n]);
+        }
+        if (lane == 0) to_lds(group_at + L::flags + pt * 4, (uint32_t)bad_r);
+        load_rows(next);
+        lds_barrier();                                         // R is there
+        f32x4 u[2];
+        u[0] = u[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        {
+            u32x4 rp[3], part[3];
+            mr[0].parts(part);
+#pragma unroll
+            for (int n = 0; n < 3; ++n) rp[n] = lds16(there + n * 2 * kFrag + lane * 16);
+            part_pairs<3, 3, 2>([&](int i, int j) { u[(i + j) & 1] = mfma16(part[i], rp[j], u[(i + j) & 1]); });
+            if (pt >= 2) {
+                mr[1].parts(part);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) rp[n] = lds16(there + (2 * n + 1) * kFrag + lane * 16);
+                part_pairs<3, 3, 2>([&](int i, int j) { u[(i + j) & 1] = mfma16(part[i], rp[j], u[(i + j) & 1]); });
             }
         }
-        if (DK < 32 * DP || bad < kChunk) {
+        float U[4];
 #pragma unroll
-            for (int dp = 0; dp < DP; ++dp)
+        for (int r = 0; r < 4; ++r) U[r] = u[0][r] + u[1][r];
+        const bool bad_u = take_out(U, token, group_at + L::told + 256 + pt * 64, g, m);
+        {
+            u32x2 part[3];
+            float l[4];
+            split<S2, 4>(U, part);
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+            for (int n = 0; n < S2; ++n) to_lds(here + n * 2 * kFrag + quad, part[n]);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (32 * dp + 8 * (int)g + 2 * r + t >= DK) S[dp][t][r] = 0.0f;
-                        else if (bad < kChunk) S[dp][t][r] = __builtin_nanf("");
-                    }
+            for (int r = 0; r < 4; ++r) l[r] = U[r] * left[r];
+            asm volatile("" : "+v"(l[0]), "+v"(l[1]), "+v"(l[2]), "+v"(l[3]) :: "memory");   // (as above)
+            split<3, 4>(l, part);
+#pragma unroll
+            for (int n = 0; n < 3; ++n) to_lds(here + (S2 + n) * 2 * kFrag + quad, part[n]);
         }
-        split_state();
+        if (lane == 0) to_lds(group_at + L::flags + 16 + pt * 4, (uint32_t)bad_u);
+        load_m(next);
+        lds_barrier();                                         // U is there
+        int bad = kChunk;
+        {
+            const u32x4 r0 = lds16(group_at + L::flags), u0 = lds16(group_at + L::flags + 16);
+            if (__builtin_expect(__ballot((r0[0] | r0[1] | r0[2] | r0[3] | u0[0] | u0[1] | u0[2] | u0[3]) != 0) != 0, 0)) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    if (r0[w]) bad = min(bad, (int)lds4(group_at + L::told + w * 64 + m * 4));
+                    if (u0[w]) bad = min(bad, (int)lds4(group_at + L::told + 256 + w * 64 + m * 4));
+                }
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < own; ++w)
+            if (DP >= 4 || (int)pt < DP) {
+                S[w][0] *= keep;
+                S[w][1] *= keep;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    u32x4 lp[3], part[2][P::in];
+                    column_parts<VF, DP>(k_at, (int)pt + 4 * w, s, g, m, part);
+#pragma unroll
+                    for (int n = 0; n < 3; ++n) lp[n] = lds16(here + ((S2 + n) * 2 + s) * kFrag + lane * 16);
+                    part_pairs<P::in, 3, 2>([&](int i, int j) {
+                        S[w][0] = mfma16(part[0][i], lp[j], S[w][0]);
+                        S[w][1] = mfma16(part[1][i], lp[j], S[w][1]);
+                    });
+                }
+                if (__builtin_expect(__ballot(bad < kChunk) != 0, 0) && bad < kChunk) S[w][0] = S[w][1] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+            }
+        if (c + 1 < chunks) share_state(there);
+        {
+            u32x4 up[3], part[3];
+            pr[0].parts(part);
+#pragma unroll
+            for (int n = 0; n < S2; ++n) up[n] = lds16(here + n * 2 * kFrag + lane * 16);
+            part_pairs<S2, S2, S2 - 1>([&](int i, int j) { out = mfma16(part[i], up[j], out); });
+            if (pt >= 2) {
+                pr[1].parts(part);
+#pragma unroll
+                for (int n = 0; n < S2; ++n) up[n] = lds16(here + (2 * n + 1) * kFrag + lane * 16);
+                part_pairs<S2, S2, S2 - 1>([&](int i, int j) { out = mfma16(part[i], up[j], out); });
+            }
+        }
+        const window_t ow = at_token(o0, c, ldo, DV);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float x = token + r >= bad ? __builtin_nanf("") : a.scale * out[r];
+            window_store<T>(ow, o_at + r * ldo, (T)x);
+        }
+        load_p(next);
     }
     if (!a.s_out || slot < 0 || !mine) return;
-    int dk = DK;
-    asm volatile("" : "+v"(dk));                               // compared again here: the masks of the first loads would be kept in registers till now
 #pragma unroll
-    for (int dp = 0; dp < DP; ++dp)
+    for (int w = 0; w < own; ++w)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int d = 32 * dp + 8 * (int)g + 2 * r + t;
-                if (d < dk) a.s_out[state + (size_t)d * DV + col] = S[dp][t][r];
+                const int d = 32 * ((int)pt + 4 * w) + 8 * (int)g + 2 * r + t;
+                if (d < DK) a.s_out[state + (size_t)d * DV + col] = S[w][t][r];
             }
 }
 
@@ -650,16 +670,15 @@ static size_t chunk_block(int32_t type) {
     return type == CSB_VAL_F32 ? Parts<CSB_VAL_F32>::bytes : Parts<CSB_VAL_BF16>::bytes;
 }
 
-template <int VF, int DP, int NW, bool VEC>
+template <int VF, int DP, int NG, bool VEC>
 static hipError_t launch_scan(const DeltaDev &d, uint8_t *ws, hipStream_t st) {
-    using L = ChunkLds<VF, DP>;
-    const size_t lds = VEC && 2 * L::bytes <= 160 * 1024 ? 2 * L::bytes : L::bytes;
-    static_assert(L::bytes <= 160 * 1024, "a chunk's operands fit the LDS");
-    const uint32_t tiles = (uint32_t)((d.dv + 16 * NW - 1) / (16 * NW)), pairs = (uint32_t)d.n_seq * (uint32_t)d.hv;
-    const auto kern = delta_scan_kernel<VF, DP, NW, VEC>;
+    constexpr size_t lds = ScanLds<VF, DP>::bytes(NG);
+    static_assert(lds <= 160 * 1024, "LDS of a workgroup");
+    const uint32_t tiles = (uint32_t)((d.dv + 16 * NG - 1) / (16 * NG)), pairs = (uint32_t)d.n_seq * (uint32_t)d.hv;
+    const auto kern = delta_scan_kernel<VF, DP, NG, VEC>;
     const hipError_t e = ensure_dynamic_lds((const void *)kern, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3((pairs + 7) / 8 * 8 * tiles), dim3(64 * NW), lds, st, d, (const uint8_t *)ws, tiles);
+    hipLaunchKernelGGL(kern, dim3((pairs + 7) / 8 * 8 * tiles), dim3(256 * NG), lds, st, d, (const uint8_t *)ws, tiles);
     return hipGetLastError();
 }
 
@@ -671,9 +690,11 @@ static hipError_t launch_chunked(const DeltaDev &d, uint8_t *ws, int64_t numbers
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (d.dk <= 64) return one ? launch_scan<VF, 2, 1, VEC>(d, ws, st) : launch_scan<VF, 2, 4, VEC>(d, ws, st);
-    if (d.dk <= 128) return one ? launch_scan<VF, 4, 1, VEC>(d, ws, st) : launch_scan<VF, 4, 4, VEC>(d, ws, st);
-    return one ? launch_scan<VF, 8, 1, VEC>(d, ws, st) : launch_scan<VF, 8, 4, VEC>(d, ws, st);
+    constexpr int wide = 2;                                    // (the registers of more columns would not fit)
+    if (d.dk <= 64) return one ? launch_scan<VF, 2, 1, VEC>(d, ws, st) : launch_scan<VF, 2, wide, VEC>(d, ws, st);
+    if (d.dk <= 128) return one ? launch_scan<VF, 4, 1, VEC>(d, ws, st) : launch_scan<VF, 4, wide, VEC>(d, ws, st);
+    constexpr int widest = VF == CSB_VAL_F32 ? 1 : 2;          // (nor their LDS)
+    return one ? launch_scan<VF, 8, 1, VEC>(d, ws, st) : launch_scan<VF, 8, widest, VEC>(d, ws, st);
 }
 
 }  // namespace csb
@@ -691,9 +712,9 @@ extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *s
     const auto fail = [](int code, const char *what) { set_error(std::string("csb_delta_chunked: ") + what); return code; };
     if (args->n_tokens && !d_ws) return fail(CSB_EINVAL, "NULL pointer");
     if ((uintptr_t)d_ws % 256) return fail(CSB_EINVAL, "workspace not 256-byte aligned");
-    const int64_t most = 0xffffffffll / (4 * kChunk);          // a chunk's offsets are 32-bit, in bytes
+    const int64_t most = (1 << 23) - 1;                        // (a chunk's offsets in bytes are below 2^31)
     if (args->n_tokens && (args->ldq > most || args->ldk > most || args->ldv > most || args->ldo > most))
-        return fail(CSB_EUNSUPPORTED, "more than 2^24 - 1 elements from one token to the next");
+        return fail(CSB_EUNSUPPORTED, "2^23 or more elements from one token to the next");
     const int64_t numbers = tile_numbers(args->n_tokens, args->n_seq, kChunkShift);
     const int64_t pairs = ((int64_t)args->n_seq * args->heads_v + 7) / 8 * 8, wide = ((int64_t)args->dv + 63) / 64, narrow = ((int64_t)args->dv + 15) / 16;
     if (pairs > kMaxWorkgroups || pairs * narrow > kMaxWorkgroups || numbers * ((args->heads_v + 3) / 4) > kMaxWorkgroups)
