@@ -316,6 +316,9 @@ __device__ __forceinline__ void Row8<VF, VEC>::load(window_t from, uint32_t at, 
     }
 }
 
+// Requests to memory stay in the order written: the first chunk's have the order that the loop's have, so that a wait in the loop is for as many.
+__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
+
 // LDS of a workgroup: the chunk's K, then per 16 columns two regions that S, R, U and e^(G_64 - G) U take in turn -- S's parts and
 // both of U's in one, R's and the next S's in the other, swapped from chunk to chunk, so that nothing is written before
 // a barrier behind its last reader -- and what tells of numbers that are not finite.
@@ -425,23 +428,38 @@ __device__ __forceinline__ bool take_out(float *x, int token, uint32_t told, uin
     return true;
 }
 
-// Four wavefronts take 16 columns of the state of one sequence and value head; NG such groups share a chunk's K in LDS.  Wavefront pt of a
-// group makes the rows of tile pt = 2 p + t of the products over tokens (K S, Q S, M R, P U) and holds the state's rows 32 dp .. 32 dp + 31
-// for dp = pt, pt + 4: what one makes and the others multiply with goes through LDS, three barriers a chunk.  Its operands of Q, M and P
-// (and of K as rows) come from global memory into its registers, requested when the chunk before has used them.
+// The column's first token that is not finite in a chunk's R or U, kChunk if none: from what the four wavefronts that made them have told.
+__device__ __forceinline__ int first_bad(u32x4 in_r, u32x4 in_u, uint32_t told, uint32_t m) {
+    int bad = kChunk;
+    if (__builtin_expect(__ballot((in_r[0] | in_r[1] | in_r[2] | in_r[3] | in_u[0] | in_u[1] | in_u[2] | in_u[3]) != 0) != 0, 0)) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if (in_r[w]) bad = min(bad, (int)lds4(told + w * 64 + m * 4));
+            if (in_u[w]) bad = min(bad, (int)lds4(told + 256 + w * 64 + m * 4));
+        }
+    }
+    return bad;
+}
+
+// Eight wavefronts take 16 columns of the state of one sequence and value head; NG such groups share a chunk's K in LDS.  Wavefronts
+// 0 to 3 carry the state: number pt makes the rows of tile pt = 2 p + t of K S and M R and holds the state's rows 32 dp .. 32 dp + 31 for
+// dp = pt, pt + 4.  Wavefronts 4 to 7 make the output's tiles, Q S and P U, beside them.  What one makes and others multiply with goes
+// through LDS, three barriers a chunk.  Operands from global memory (Q, M, P, K as rows) go to the registers of the wavefront that
+// multiplies with them, requested when it has used the chunk's before.
 // Lane (g = lane / 16, m = lane % 16) has column m; of a tile over tokens the four from 8 g + 4 t on, of 32 rows of the state 8 g .. 8 g + 7.
 // DP: 32s of dk.  VEC: rows of q and k in aligned 16-byte words.
 template <int VF, int DP, int NG, bool VEC>
-__global__ __launch_bounds__(256 * NG) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
+__global__ __launch_bounds__(512 * NG) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
     using T = typename Elem<VF>::T;
     using L = ScanLds<VF, DP>;
     using P = Parts<VF>;
     constexpr int S2 = P::out, own = (DP + 3) / 4;
     extern __shared__ __align__(16) uint8_t smem[];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, m = lane & 15u;
-    const uint32_t pt = wave & 3u, group = wave >> 2;
+    const uint32_t pt = wave & 3u, group = wave >> 3;
+    const bool carries = (wave & 4u) == 0;
     const uint32_t k_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
-    const uint32_t group_at = k_at + L::k + group * L::group;
+    const uint32_t group_at = k_at + L::k + group * L::group, flags = group_at + L::flags, told = group_at + L::told;
     // workgroups of one sequence and head run on one XCD (they are dealt out by their number modulo 8): its L2 has their operands once
     const uint32_t pair = blockIdx.x / (8 * tiles) * 8 + blockIdx.x % 8, tile = blockIdx.x / 8 % tiles;
     if (pair >= (uint32_t)a.n_seq * a.hv) return;
@@ -451,6 +469,89 @@ __global__ __launch_bounds__(256 * NG) void delta_scan_kernel(const DeltaDev a, 
     int64_t first_, end_, slot;
     delta_sequence(a, (int)seq, &first_, &end_, &slot);
     const int first = __builtin_amdgcn_readfirstlane((int)first_), end = __builtin_amdgcn_readfirstlane((int)end_);
+    const int chunks = (int)(((uint32_t)(end - first) + kChunk - 1) >> kChunkShift);
+    const uint8_t *block0 = ws + ((size_t)((uint32_t)(first >> kChunkShift) + seq) * a.hv + h) * P::bytes;
+    auto block = [&](int c) { return block0 + (size_t)c * a.hv * P::bytes; };
+    auto decay = [&](int c) { return (const float *)(block(c) + P::m_bytes + P::p_bytes); };
+    const int token = 32 * (int)(pt >> 1) + 8 * (int)g + 4 * (int)(pt & 1u);   // the first of the lane's four
+    const uint32_t row = tile_token(pt, m);                                    // the lane's row of an operand of K or Q
+    const uint32_t f0 = pt < 2 ? pt : 2 * pt - 2, f1 = pt < 2 ? pt : 2 * pt - 1;   // its operands of M or P: one for the first 32 tokens, else two
+    auto window_of = [&](const void *base, int64_t ld, size_t head, int c, int width) {    // the chunk's tokens, `width` elements of each
+        const int before = c << kChunkShift, count = min(kChunk, end - first - before);   // (offsets below 2^31: leading dimensions below 2^23)
+        const uint32_t ldb = (uint32_t)(ld * sizeof(T));
+        return window((const T *)base + (size_t)(first + before) * ld + head, (uint32_t)(count - 1) * ldb + (uint32_t)width * (uint32_t)sizeof(T));
+    };
+    // Behind the last chunk its operands are requested again: what is in flight is known at every wait only if nothing is requested sometimes.
+    auto next_of = [&](int c) { return min(c + 1, chunks - 1); };
+    auto region = [&](int c) { return group_at + (c & 1) * L::region; };
+
+    if (!carries) {
+        const uint32_t ldq = (uint32_t)(a.ldq * sizeof(T)), ldo = (uint32_t)(a.ldo * sizeof(T)), o_at = mine ? token * ldo + col * (uint32_t)sizeof(T) : kOutside;
+        Row8<VF, VEC> qr[DP];
+        Lower<VF, 2> pr[2];
+        f32x4 eg;
+        auto load_rows = [&](int c) {                          // (tokens past the end: zeros)
+            const window_t qw = window_of(a.q, a.ldq, (size_t)kh * DK, c, DK);
+#pragma unroll
+            for (int dp = 0; dp < DP; ++dp) qr[dp].load(qw, row * ldq, 32 * dp + 8 * (int)g, DK);
+            eg = *(const f32x4 *)(decay(c) + token);
+        };
+        auto load_p = [&](int c) {
+            pr[0].load(block(c) + P::m_bytes, f0, lane);
+            pr[1].load(block(c) + P::m_bytes, f1, lane);
+        };
+        if (chunks > 0) {
+            load_rows(0);
+            in_order();
+            load_p(0);
+        }
+        for (int c = 0; c < chunks; ++c) {
+            const uint32_t here = region(c) + lane * 16;
+            lds_barrier();                                     // S is there
+            f32x4 o[S2];
+#pragma unroll
+            for (int n = 0; n < S2; ++n) o[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int dp = 0; dp < DP; ++dp) {
+                u32x4 sp[3], part[3];
+#pragma unroll
+                for (int n = 0; n < S2; ++n) sp[n] = lds16(here + (dp * 3 + n) * kFrag);
+                row_parts<VF, VEC>(qr[dp], part);
+                part_pairs<P::in, S2, S2 - 1>([&](int i, int j) { o[j] = mfma16(part[i], sp[j], o[j]); });
+            }
+            f32x4 out = o[0];
+#pragma unroll
+            for (int n = 1; n < S2; ++n) out += o[n];
+            out *= eg;
+            asm volatile("" : "+v"(out) :: "memory");          // (here, so that the next chunk's factors can come into the same registers)
+            load_rows(next_of(c));
+            lds_barrier();
+            lds_barrier();                                     // U is there
+            const u32x4 r0 = lds16(flags), u0 = lds16(flags + 16);
+            f32x4 more[S2];
+#pragma unroll
+            for (int n = 0; n < S2; ++n) more[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (s == 0 || pt >= 2) {
+                    u32x4 up[3], part[3];
+                    pr[s].parts(part);
+#pragma unroll
+                    for (int n = 0; n < S2; ++n) up[n] = lds16(here + (2 * n + s) * kFrag);
+                    part_pairs<S2, S2, S2 - 1>([&](int i, int j) { more[j] = mfma16(part[i], up[j], more[j]); });
+                }
+#pragma unroll
+            for (int n = 0; n < S2; ++n) out += more[n];
+            const int bad = first_bad(r0, u0, told, m);
+            const window_t ow = window_of(a.out, a.ldo, (size_t)h * DV, c, DV);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) window_store<T>(ow, o_at + r * ldo, (T)(token + r >= bad ? __builtin_nanf("") : a.scale * out[r]));
+            load_p(next_of(c));
+        }
+        return;
+    }
+
+    const uint32_t ldk = (uint32_t)(a.ldk * sizeof(T)), ldv = (uint32_t)(a.ldv * sizeof(T)), v_at = mine ? token * ldv + col * (uint32_t)sizeof(T) : kOutside;
     const size_t state = (((size_t)(slot < 0 ? 0 : slot) * a.hv + h) * DK) * DV;
     f32x4 S[own][2];                                           // [dp / 4][t][r]: row 32 dp + 8 g + 2 r + t
 #pragma unroll
@@ -462,51 +563,25 @@ __global__ __launch_bounds__(256 * NG) void delta_scan_kernel(const DeltaDev a, 
                 const int d = 32 * ((int)pt + 4 * w) + 8 * (int)g + 2 * r + t;
                 S[w][t][r] = a.s_in && slot >= 0 && mine && d < DK ? a.s_in[state + (size_t)d * DV + col] : 0.0f;
             }
-    const int chunks = (int)(((uint32_t)(end - first) + kChunk - 1) >> kChunkShift);
-    const uint8_t *block0 = ws + ((size_t)((uint32_t)(first >> kChunkShift) + seq) * a.hv + h) * P::bytes;
-    // offsets within a chunk fit 31 bits (leading dimensions below 2^23)
-    const uint32_t ldk = (uint32_t)(a.ldk * sizeof(T)), ldq = (uint32_t)(a.ldq * sizeof(T)), ldv = (uint32_t)(a.ldv * sizeof(T)), ldo = (uint32_t)(a.ldo * sizeof(T));
-    const uint8_t *k0 = (const uint8_t *)((const T *)a.k + (size_t)kh * DK), *q0 = (const uint8_t *)((const T *)a.q + (size_t)kh * DK);
-    const uint8_t *v0 = (const uint8_t *)((const T *)a.v + (size_t)h * DV), *o0 = (const uint8_t *)((const T *)a.out + (size_t)h * DV);
-    const int token = 32 * (int)(pt >> 1) + 8 * (int)g + 4 * (int)(pt & 1u);   // the first of the lane's four
-
-    // what the wavefront needs of a chunk
-    Row8<VF, VEC> kr[DP], qr[DP];
+    Row8<VF, VEC> kr[DP];
     raw_t<T> v_0, v_1, v_2, v_3;                               // (an array of them would be packed, two to a register, as soon as they are loaded)
     Lower<VF, 3> mr[2];
-    Lower<VF, 2> pr[2];
     f32x4 eg, left;
     float keep;
-    auto block = [&](int c) { return block0 + (size_t)c * a.hv * P::bytes; };
-    auto decay = [&](int c) { return (const float *)(block(c) + P::m_bytes + P::p_bytes); };
-    const uint32_t row = tile_token(pt, m), v_at = mine ? token * ldv + col * (uint32_t)sizeof(T) : kOutside, o_at = mine ? token * ldo + col * (uint32_t)sizeof(T) : kOutside;
-    auto at_token = [&](const uint8_t *base, int c, uint32_t ld, int width) {  // the chunk's tokens, `width` elements of each
-        const int before = c << kChunkShift, count = min(kChunk, end - first - before);
-        return window(base + (size_t)(first + before) * ld, (uint32_t)(count - 1) * ld + (uint32_t)width * (uint32_t)sizeof(T));
-    };
-    auto load_rows = [&](int c) {                              // (tokens past the end: zeros)
-        const window_t kw = at_token(k0, c, ldk, DK), qw = at_token(q0, c, ldq, DK), vw = at_token(v0, c, ldv, DV);
+    auto load_rows = [&](int c) {
+        const window_t kw = window_of(a.k, a.ldk, (size_t)kh * DK, c, DK), vw = window_of(a.v, a.ldv, (size_t)h * DV, c, DV);
 #pragma unroll
         for (int dp = 0; dp < DP; ++dp) kr[dp].load(kw, row * ldk, 32 * dp + 8 * (int)g, DK);
-#pragma unroll
-        for (int dp = 0; dp < DP; ++dp) qr[dp].load(qw, row * ldq, 32 * dp + 8 * (int)g, DK);
         v_0 = window_load<T>(vw, v_at);
         v_1 = window_load<T>(vw, v_at + ldv);
         v_2 = window_load<T>(vw, v_at + 2 * ldv);
         v_3 = window_load<T>(vw, v_at + 3 * ldv);
         eg = *(const f32x4 *)(decay(c) + token);
     };
-    // the first half of the chunk has one operand, the second two
-    const uint32_t f0 = pt < 2 ? pt : 2 * pt - 2, f1 = pt < 2 ? pt : 2 * pt - 1;
     auto load_m = [&](int c) {
         mr[0].load(block(c), f0, lane);
         mr[1].load(block(c), f1, lane);
         left = *(const f32x4 *)(decay(c) + 64 + token);
-    };
-    auto load_p = [&](int c) {
-        pr[0].load(block(c) + P::m_bytes, f0, lane);
-        pr[1].load(block(c) + P::m_bytes, f1, lane);
-        keep = decay(c)[63];
     };
     auto share_state = [&](uint32_t at) {                      // the parts of the wavefront's rows of S
 #pragma unroll
@@ -526,26 +601,25 @@ __global__ __launch_bounds__(256 * NG) void delta_scan_kernel(const DeltaDev a, 
 
     if (chunks > 0) {
         load_rows(0);
+        in_order();
         load_m(0);
-        load_p(0);
+        in_order();
+        keep = decay(0)[63];
         share_state(group_at);
     }
     for (int c = 0; c < chunks; ++c) {
-        const uint32_t here = group_at + (c & 1) * L::region, there = group_at + (~c & 1) * L::region;
-        // (behind the last chunk its operands are requested again: what is in flight is known at every wait only if nothing is requested sometimes)
-        const int next = min(c + 1, chunks - 1);
+        const uint32_t here = region(c), there = region(c + 1);
         lds_barrier();                                         // S is there, and the chunk before is done with
-        f32x4 ks[2], o[2];
-        ks[0] = ks[1] = o[0] = o[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        f32x4 ks[3];
+#pragma unroll
+        for (int n = 0; n < 3; ++n) ks[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int dp = 0; dp < DP; ++dp) {
             u32x4 sp[3], part[P::in];
 #pragma unroll
             for (int n = 0; n < 3; ++n) sp[n] = lds16(here + (dp * 3 + n) * kFrag + lane * 16);
             row_parts<VF, VEC>(kr[dp], part);
-            part_pairs<P::in, 3, 2>([&](int i, int j) { ks[dp & 1] = mfma16(part[i], sp[j], ks[dp & 1]); });
-            row_parts<VF, VEC>(qr[dp], part);
-            part_pairs<P::in, S2, S2 - 1>([&](int i, int j) { o[dp & 1] = mfma16(part[i], sp[j], o[dp & 1]); });
+            part_pairs<P::in, 3, 2>([&](int i, int j) { ks[j] = mfma16(part[i], sp[j], ks[j]); });   // (a sum of each part: none waits for the one before)
         }
 #pragma unroll
         for (int dp = 0; dp < DP; ++dp)                        // K for the transposed reads: the groups share the work
@@ -555,104 +629,80 @@ __global__ __launch_bounds__(256 * NG) void delta_scan_kernel(const DeltaDev a, 
         float R[4];
         const raw_t<T> v[4] = {v_0, v_1, v_2, v_3};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) R[r] = fmaf(-eg[r], ks[0][r] + ks[1][r], (float)__builtin_bit_cast(T, v[r]));
-        f32x4 out = (o[0] + o[1]) * eg;
-        asm volatile("" : "+v"(out) :: "memory");              // (here, so that the next chunk's factors can come into the same registers)
-        const bool bad_r = take_out(R, token, group_at + L::told + pt * 64, g, m);
+        for (int r = 0; r < 4; ++r) R[r] = fmaf(-eg[r], ks[0][r] + (ks[1][r] + ks[2][r]), (float)__builtin_bit_cast(T, v[r]));
+        const bool bad_r = take_out(R, token, told + pt * 64, g, m);
         {
             u32x2 part[3];
             split<3, 4>(R, part);
 #pragma unroll
             for (int n = 0; n < 3; ++n) to_lds(there + n * 2 * kFrag + quad, part[n]);
         }
-        if (lane == 0) to_lds(group_at + L::flags + pt * 4, (uint32_t)bad_r);
-        load_rows(next);
+        if (lane == 0) to_lds(flags + pt * 4, (uint32_t)bad_r);
+        load_rows(next_of(c));
         lds_barrier();                                         // R is there
-        f32x4 u[2];
-        u[0] = u[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        {
-            u32x4 rp[3], part[3];
-            mr[0].parts(part);
+        f32x4 u[3];
 #pragma unroll
-            for (int n = 0; n < 3; ++n) rp[n] = lds16(there + n * 2 * kFrag + lane * 16);
-            part_pairs<3, 3, 2>([&](int i, int j) { u[(i + j) & 1] = mfma16(part[i], rp[j], u[(i + j) & 1]); });
-            if (pt >= 2) {
-                mr[1].parts(part);
+        for (int n = 0; n < 3; ++n) u[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int n = 0; n < 3; ++n) rp[n] = lds16(there + (2 * n + 1) * kFrag + lane * 16);
-                part_pairs<3, 3, 2>([&](int i, int j) { u[(i + j) & 1] = mfma16(part[i], rp[j], u[(i + j) & 1]); });
+        for (int s = 0; s < 2; ++s)
+            if (s == 0 || pt >= 2) {
+                u32x4 rp[3], part[3];
+                mr[s].parts(part);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) rp[n] = lds16(there + (2 * n + s) * kFrag + lane * 16);
+                part_pairs<3, 3, 2>([&](int i, int j) { u[i] = mfma16(part[i], rp[j], u[i]); });
             }
-        }
         float U[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) U[r] = u[0][r] + u[1][r];
-        const bool bad_u = take_out(U, token, group_at + L::told + 256 + pt * 64, g, m);
+        for (int r = 0; r < 4; ++r) U[r] = u[0][r] + (u[1][r] + u[2][r]);
+        const bool bad_u = take_out(U, token, told + 256 + pt * 64, g, m);
         {
             u32x2 part[3];
             float l[4];
-            split<S2, 4>(U, part);
-#pragma unroll
-            for (int n = 0; n < S2; ++n) to_lds(here + n * 2 * kFrag + quad, part[n]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) l[r] = U[r] * left[r];
             asm volatile("" : "+v"(l[0]), "+v"(l[1]), "+v"(l[2]), "+v"(l[3]) :: "memory");   // (as above)
             split<3, 4>(l, part);
 #pragma unroll
             for (int n = 0; n < 3; ++n) to_lds(here + (S2 + n) * 2 * kFrag + quad, part[n]);
-        }
-        if (lane == 0) to_lds(group_at + L::flags + 16 + pt * 4, (uint32_t)bad_u);
-        load_m(next);
-        lds_barrier();                                         // U is there
-        int bad = kChunk;
-        {
-            const u32x4 r0 = lds16(group_at + L::flags), u0 = lds16(group_at + L::flags + 16);
-            if (__builtin_expect(__ballot((r0[0] | r0[1] | r0[2] | r0[3] | u0[0] | u0[1] | u0[2] | u0[3]) != 0) != 0, 0)) {
+            split<S2, 4>(U, part);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    if (r0[w]) bad = min(bad, (int)lds4(group_at + L::told + w * 64 + m * 4));
-                    if (u0[w]) bad = min(bad, (int)lds4(group_at + L::told + 256 + w * 64 + m * 4));
-                }
-            }
+            for (int n = 0; n < S2; ++n) to_lds(here + n * 2 * kFrag + quad, part[n]);
         }
+        if (lane == 0) to_lds(flags + 16 + pt * 4, (uint32_t)bad_u);
+        load_m(next_of(c));
+        in_order();
+        lds_barrier();                                         // U is there
+        const u32x4 r0 = lds16(flags), u0 = lds16(flags + 16);
 #pragma unroll
         for (int w = 0; w < own; ++w)
             if (DP >= 4 || (int)pt < DP) {
+                f32x4 more[2];                                 // (the second 32 tokens' sums: none waits for the one before)
+                more[0] = more[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
                 S[w][0] *= keep;
                 S[w][1] *= keep;
+                u32x4 lp[2][3], part[2][2][P::in];
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    u32x4 lp[3], part[2][P::in];
-                    column_parts<VF, DP>(k_at, (int)pt + 4 * w, s, g, m, part);
+                    column_parts<VF, DP>(k_at, (int)pt + 4 * w, s, g, m, part[s]);
 #pragma unroll
-                    for (int n = 0; n < 3; ++n) lp[n] = lds16(here + ((S2 + n) * 2 + s) * kFrag + lane * 16);
-                    part_pairs<P::in, 3, 2>([&](int i, int j) {
-                        S[w][0] = mfma16(part[0][i], lp[j], S[w][0]);
-                        S[w][1] = mfma16(part[1][i], lp[j], S[w][1]);
-                    });
+                    for (int n = 0; n < 3; ++n) lp[s][n] = lds16(here + ((S2 + n) * 2 + s) * kFrag + lane * 16);
                 }
-                if (__builtin_expect(__ballot(bad < kChunk) != 0, 0) && bad < kChunk) S[w][0] = S[w][1] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+                part_pairs<P::in, 3, 2>([&](int i, int j) {
+                    S[w][0] = mfma16(part[0][0][i], lp[0][j], S[w][0]);
+                    S[w][1] = mfma16(part[0][1][i], lp[0][j], S[w][1]);
+                    more[0] = mfma16(part[1][0][i], lp[1][j], more[0]);
+                    more[1] = mfma16(part[1][1][i], lp[1][j], more[1]);
+                });
+                S[w][0] += more[0];
+                S[w][1] += more[1];
             }
-        if (c + 1 < chunks) share_state(there);
-        {
-            u32x4 up[3], part[3];
-            pr[0].parts(part);
+        if (first_bad(r0, u0, told, m) < kChunk) {
 #pragma unroll
-            for (int n = 0; n < S2; ++n) up[n] = lds16(here + n * 2 * kFrag + lane * 16);
-            part_pairs<S2, S2, S2 - 1>([&](int i, int j) { out = mfma16(part[i], up[j], out); });
-            if (pt >= 2) {
-                pr[1].parts(part);
-#pragma unroll
-                for (int n = 0; n < S2; ++n) up[n] = lds16(here + (2 * n + 1) * kFrag + lane * 16);
-                part_pairs<S2, S2, S2 - 1>([&](int i, int j) { out = mfma16(part[i], up[j], out); });
-            }
+            for (int w = 0; w < own; ++w) S[w][0] = S[w][1] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
         }
-        const window_t ow = at_token(o0, c, ldo, DV);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float x = token + r >= bad ? __builtin_nanf("") : a.scale * out[r];
-            window_store<T>(ow, o_at + r * ldo, (T)x);
-        }
-        load_p(next);
+        share_state(there);                                    // (behind the last chunk nobody reads it)
+        keep = decay(next_of(c))[63];
     }
     if (!a.s_out || slot < 0 || !mine) return;
 #pragma unroll
@@ -678,7 +728,7 @@ static hipError_t launch_scan(const DeltaDev &d, uint8_t *ws, hipStream_t st) {
     const auto kern = delta_scan_kernel<VF, DP, NG, VEC>;
     const hipError_t e = ensure_dynamic_lds((const void *)kern, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3((pairs + 7) / 8 * 8 * tiles), dim3(256 * NG), lds, st, d, (const uint8_t *)ws, tiles);
+    hipLaunchKernelGGL(kern, dim3((pairs + 7) / 8 * 8 * tiles), dim3(512 * NG), lds, st, d, (const uint8_t *)ws, tiles);
     return hipGetLastError();
 }
 
