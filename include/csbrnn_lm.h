@@ -75,8 +75,8 @@ typedef struct {
 int csb_delta_recurrent(const csb_delta_args *args, void *stream);
 
 /*
- * The same rule, the same arguments and errors, chunk by chunk: for prompts.  Leading dimensions of 2^23 or more ->
- * CSB_EUNSUPPORTED.  (Before a capture into a graph call it once: a kernel's first launch raises its LDS limit.)
+ * The same rule, the same arguments and errors, chunk by chunk: for prompts.  Leading dimensions of 2^23 or more
+ * or dv above 2^20 -> CSB_EUNSUPPORTED.  (Before a capture into a graph call it once: a kernel's first launch raises its LDS limit.)
  * d_ws: csb_delta_workspace_bytes(args) bytes (only the sizes of `args` are read; 0 for arguments
  * that the call refuses).
  */

@@ -90,6 +90,20 @@ __device__ __forceinline__ void part_pairs(const F &f) {
             if (s - i >= 0 && s - i < NB) f(i, s - i);
 }
 
+// An operand of K or Q is read from memory with four neighbouring lanes on 64 consecutive bytes of a row (a lane for each of the
+// multiplication's (g, m) would touch 64 pieces of 16 bytes: the path to the caches takes them one by one) and turned over in LDS.
+// Its 16-byte word of row m, elements 8 g to 8 g + 7, lies at place 16 (m % 4) + 4 (m / 4) + (g ^ m % 4): the multiplication's lanes and
+// the transposed reads below (4 bytes from all g and m / 4 with m % 4 alike) hit every bank once.
+__device__ __forceinline__ uint32_t place(uint32_t g, uint32_t m) { return (16 * (m & 3u) + 4 * (m >> 2) + (g ^ (m & 3u))) * 16; }
+__device__ __forceinline__ uint32_t loaded_row(uint32_t lane) { return ((lane >> 2) & 3u) * 4 + (lane >> 4); }          // what lane's place holds
+__device__ __forceinline__ uint32_t loaded_part(uint32_t lane) { return (lane & 3u) ^ (lane >> 4); }
+
+__device__ __forceinline__ u32x4 lds16(uint32_t at) { return *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)at; }
+__device__ __forceinline__ uint32_t lds4(uint32_t at) { return *(const __attribute__((address_space(3))) uint32_t *)(uintptr_t)at; }
+__device__ __forceinline__ void to_lds(uint32_t at, u32x4 v) { *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)at = v; }
+__device__ __forceinline__ void to_lds(uint32_t at, u32x2 v) { *(__attribute__((address_space(3))) u32x2 *)(uintptr_t)at = v; }
+__device__ __forceinline__ void to_lds(uint32_t at, uint32_t v) { *(__attribute__((address_space(3))) uint32_t *)(uintptr_t)at = v; }
+
 // ---- first launch: M and P -----------------------------------------------------------------------
 // A wavefront takes one chunk of one value head.
 
@@ -114,6 +128,15 @@ template <int VF, bool VEC> struct Row8 {
     }
     // the same from a window, the row at byte `at` of it
     __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, uint32_t at, int d, int dk);
+    // to the lane's place of an operand in LDS, and from there as a multiplication wants it
+    __device__ __forceinline__ void put(uint32_t at, uint32_t lane) const {
+#pragma unroll
+        for (int i = 0; i < words; ++i) to_lds(at + i * kFrag + lane * 16, w[i]);
+    }
+    __device__ __forceinline__ void get(uint32_t at, uint32_t g, uint32_t m) {
+#pragma unroll
+        for (int i = 0; i < words; ++i) w[i] = lds16(at + i * kFrag + place(g, m));
+    }
 };
 
 // d += a b^T over 32 elements of the rows, exact products, sums in binary32.
@@ -207,13 +230,29 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
     for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int y = 0; y <= x; ++y) kk[x][y] = qk[x][y] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t stage = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)&mat[wave][0][0];
+    constexpr uint32_t frag = Row8<VF, VEC>::words * kFrag;
+    static_assert(8 * frag <= sizeof(mat[0]), "K and Q of 32 elements fit");
+    Row8<VF, VEC> next[8];
+    auto request = [&](int d) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int64_t t = min(base + 16 * x + (int64_t)loaded_row(lane), end - 1);    // (past the end beta is zero)
+            next[x].load((const T *)a.k + t * a.ldk + (size_t)kh * a.dk, d + 8 * (int)loaded_part(lane), a.dk);
+            next[4 + x].load((const T *)a.q + t * a.ldq + (size_t)kh * a.dk, d + 8 * (int)loaded_part(lane), a.dk);
+        }
+    };
+    request(0);
     for (int d = 0; d < a.dk; d += 32) {
         Row8<VF, VEC> kr[4], qr[4];
 #pragma unroll
+        for (int x = 0; x < 8; ++x) next[x].put(stage + x * frag, lane);
+        wave_sync();
+        if (d + 32 < a.dk) request(d + 32);
+#pragma unroll
         for (int x = 0; x < 4; ++x) {
-            const int64_t t = min(base + 16 * x + (int64_t)i, end - 1);    // (past the end beta is zero)
-            kr[x].load((const T *)a.k + t * a.ldk + (size_t)kh * a.dk, d + 8 * (int)g, a.dk);
-            qr[x].load((const T *)a.q + t * a.ldq + (size_t)kh * a.dk, d + 8 * (int)g, a.dk);
+            kr[x].get(stage + x * frag, g, i);
+            qr[x].get(stage + (4 + x) * frag, g, i);
         }
 #pragma unroll
         for (int x = 0; x < 4; ++x)
@@ -222,6 +261,7 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
                 kk[x][y] = row_dot(kr[x], kr[y], kk[x][y]);
                 qk[x][y] = row_dot(qr[x], kr[y], qk[x][y]);
             }
+        wave_sync();
     }
     wave_sync();
     float (*m)[kLdT] = mat[wave];
@@ -272,11 +312,6 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
 
 // ---- second launch: the chunks of a sequence one after the other ---------------------------------
 
-__device__ __forceinline__ u32x4 lds16(uint32_t at) { return *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)at; }
-__device__ __forceinline__ uint32_t lds4(uint32_t at) { return *(const __attribute__((address_space(3))) uint32_t *)(uintptr_t)at; }
-__device__ __forceinline__ void to_lds(uint32_t at, u32x4 v) { *(__attribute__((address_space(3))) u32x4 *)(uintptr_t)at = v; }
-__device__ __forceinline__ void to_lds(uint32_t at, u32x2 v) { *(__attribute__((address_space(3))) u32x2 *)(uintptr_t)at = v; }
-__device__ __forceinline__ void to_lds(uint32_t at, uint32_t v) { *(__attribute__((address_space(3))) uint32_t *)(uintptr_t)at = v; }
 // All that the wavefront wrote to LDS is there, for the whole workgroup.  (Global loads stay in flight: __syncthreads would wait for them.)
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -319,21 +354,17 @@ __device__ __forceinline__ void Row8<VF, VEC>::load(window_t from, uint32_t at, 
 // Requests to memory stay in the order written: the first chunk's have the order that the loop's have, so that a wait in the loop is for as many.
 __device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 
-// LDS of a workgroup: the chunk's K, then per 16 columns two regions that S, R, U and e^(G_64 - G) U take in turn -- S's parts and
-// both of U's in one, R's and the next S's in the other, swapped from chunk to chunk, so that nothing is written before
+// LDS of a workgroup: K of a chunk and of the next, Q, then per 16 columns two regions that S, R, U and e^(G_64 - G) U take in turn -- S's
+// parts and both of U's in one, R's and the next S's in the other, swapped from chunk to chunk, so that nothing is written before
 // a barrier behind its last reader -- and what tells of numbers that are not finite.
 template <int VF, int DP> struct ScanLds {
     static constexpr uint32_t half = VF == CSB_VAL_F32 ? 2 : 1;               // 16-byte words of a lane's eight numbers of K
-    static constexpr uint32_t frag = half * kFrag, k = 4 * DP * frag;
+    static constexpr uint32_t frag = half * kFrag, k = 4 * DP * frag, q_at = 2 * k, groups_at = 3 * k;
     static constexpr uint32_t u_bytes = (2 * Parts<VF>::out + 6) * kFrag;     // U's parts, then e^(G_64 - G) U's
     static constexpr uint32_t region = 3 * DP * kFrag > u_bytes ? 3 * DP * kFrag : u_bytes;
     static constexpr uint32_t flags = 2 * region, told = flags + 32, group = told + 2 * 4 * 16 * 4;
-    static constexpr uint32_t bytes(int groups) { return k + groups * group; }
+    static constexpr uint32_t bytes(int groups) { return groups_at + groups * group; }
 };
-
-// An operand of K lies in LDS with lane (g, m)'s numbers -- row m of its tile, elements 8 g to 8 g + 7 of its 32 -- at place
-// 16 g + (m + g) % 16: the transposed reads below, 4 bytes from 16 places with m % 4 alike, then hit 16 different banks' words.
-__device__ __forceinline__ uint32_t place(uint32_t g, uint32_t m) { return (g * 16 + ((m + g) & 15u)) * 16; }
 
 // The parts of an operand of K or Q from its numbers.
 template <int VF, bool VEC>
@@ -357,11 +388,13 @@ __device__ __forceinline__ void row_parts(const Row8<VF, VEC> &row, u32x4 *part)
 template <int VF, int DP>
 __device__ __forceinline__ void column_parts(uint32_t k_at, int dp, int ks, uint32_t g, uint32_t m, u32x4 part[2][Parts<VF>::in]) {
     using L = ScanLds<VF, DP>;
+    // row 4 g + c of a tile, c = 0 .. 3, elements from 8 (m / 4) on: place(m / 4, 4 g + c)
+    const uint32_t word = m >> 2, low = 4 * g * 16;
     if constexpr (VF == CSB_VAL_F32) {
         float x[2][8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint32_t at = k_at + ((2 * ks + (j >> 2)) * DP + dp) * L::frag + place(m >> 2, 4 * g + (j & 3)) + ((m >> 1) & 1u) * kFrag + (m & 1u) * 8;
+            const uint32_t at = k_at + ((2 * ks + (j >> 2)) * DP + dp) * L::frag + low + (j & 3) * 256 + (word ^ (j & 3)) * 16 + ((m >> 1) & 1u) * kFrag + (m & 1u) * 8;
             x[0][j] = __uint_as_float(lds4(at));
             x[1][j] = __uint_as_float(lds4(at + 4));
         }
@@ -371,8 +404,9 @@ __device__ __forceinline__ void column_parts(uint32_t k_at, int dp, int ks, uint
         u32x4 both[2];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {                          // tokens 2 j and 2 j + 1
-            const uint32_t at = k_at + ((2 * ks + (j >> 1)) * DP + dp) * L::frag + (m & 3u) * 4;
-            const uint32_t even = lds4(at + place(m >> 2, 4 * g + 2 * (j & 1))), odd = lds4(at + place(m >> 2, 4 * g + 2 * (j & 1) + 1));
+            const uint32_t at = k_at + ((2 * ks + (j >> 1)) * DP + dp) * L::frag + (m & 3u) * 4 + low;
+            const uint32_t c = 2 * (j & 1);
+            const uint32_t even = lds4(at + c * 256 + (word ^ c) * 16), odd = lds4(at + (c + 1) * 256 + (word ^ (c + 1)) * 16);
             both[0][j] = low_halves(even, odd);
             both[1][j] = high_halves(even, odd);
         }
@@ -449,7 +483,7 @@ __device__ __forceinline__ int first_bad(u32x4 in_r, u32x4 in_u, uint32_t told, 
 // Lane (g = lane / 16, m = lane % 16) has column m; of a tile over tokens the four from 8 g + 4 t on, of 32 rows of the state 8 g .. 8 g + 7.
 // DP: 32s of dk.  VEC: rows of q and k in aligned 16-byte words.
 template <int VF, int DP, int NG, bool VEC>
-__global__ __launch_bounds__(512 * NG) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
+__global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
     using T = typename Elem<VF>::T;
     using L = ScanLds<VF, DP>;
     using P = Parts<VF>;
@@ -459,7 +493,7 @@ __global__ __launch_bounds__(512 * NG) void delta_scan_kernel(const DeltaDev a, 
     const uint32_t pt = wave & 3u, group = wave >> 3;
     const bool carries = (wave & 4u) == 0;
     const uint32_t k_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
-    const uint32_t group_at = k_at + L::k + group * L::group, flags = group_at + L::flags, told = group_at + L::told;
+    const uint32_t group_at = k_at + L::groups_at + group * L::group, flags = group_at + L::flags, told = group_at + L::told;
     // workgroups of one sequence and head run on one XCD (they are dealt out by their number modulo 8): its L2 has their operands once
     const uint32_t pair = blockIdx.x / (8 * tiles) * 8 + blockIdx.x % 8, tile = blockIdx.x / 8 % tiles;
     if (pair >= (uint32_t)a.n_seq * a.hv) return;
@@ -474,7 +508,10 @@ __global__ __launch_bounds__(512 * NG) void delta_scan_kernel(const DeltaDev a, 
     auto block = [&](int c) { return block0 + (size_t)c * a.hv * P::bytes; };
     auto decay = [&](int c) { return (const float *)(block(c) + P::m_bytes + P::p_bytes); };
     const int token = 32 * (int)(pt >> 1) + 8 * (int)g + 4 * (int)(pt & 1u);   // the first of the lane's four
-    const uint32_t row = tile_token(pt, m);                                    // the lane's row of an operand of K or Q
+    const uint32_t row = tile_token(pt, loaded_row(lane));                     // the row of K or Q that the lane reads, and its element of 32
+    const int element = 8 * (int)loaded_part(lane);
+    constexpr int each = DP / NG;                              // operands of K or Q that a wavefront reads: those of tile pt, dp from each * group on
+    const int dp0 = each * (int)group;
     const uint32_t f0 = pt < 2 ? pt : 2 * pt - 2, f1 = pt < 2 ? pt : 2 * pt - 1;   // its operands of M or P: one for the first 32 tokens, else two
     auto window_of = [&](const void *base, int64_t ld, size_t head, int c, int width) {    // the chunk's tokens, `width` elements of each
         const int before = c << kChunkShift, count = min(kChunk, end - first - before);   // (offsets below 2^31: leading dimensions below 2^23)
@@ -487,36 +524,45 @@ __global__ __launch_bounds__(512 * NG) void delta_scan_kernel(const DeltaDev a, 
 
     if (!carries) {
         const uint32_t ldq = (uint32_t)(a.ldq * sizeof(T)), ldo = (uint32_t)(a.ldo * sizeof(T)), o_at = mine ? token * ldo + col * (uint32_t)sizeof(T) : kOutside;
-        Row8<VF, VEC> qr[DP];
+        Row8<VF, VEC> qr[each];
         Lower<VF, 2> pr[2];
         f32x4 eg;
-        auto load_rows = [&](int c) {                          // (tokens past the end: zeros)
+        auto load_q = [&](int c) {                             // (tokens past the end: zeros)
             const window_t qw = window_of(a.q, a.ldq, (size_t)kh * DK, c, DK);
 #pragma unroll
-            for (int dp = 0; dp < DP; ++dp) qr[dp].load(qw, row * ldq, 32 * dp + 8 * (int)g, DK);
-            eg = *(const f32x4 *)(decay(c) + token);
+            for (int i = 0; i < each; ++i) qr[i].load(qw, row * ldq, 32 * (dp0 + i) + element, DK);
+        };
+        auto put_q = [&]() {
+#pragma unroll
+            for (int i = 0; i < each; ++i) qr[i].put(k_at + L::q_at + (pt * DP + dp0 + i) * L::frag, lane);
         };
         auto load_p = [&](int c) {
             pr[0].load(block(c) + P::m_bytes, f0, lane);
             pr[1].load(block(c) + P::m_bytes, f1, lane);
         };
         if (chunks > 0) {
-            load_rows(0);
+            load_q(0);
+            put_q();
+            eg = *(const f32x4 *)(decay(0) + token);
+            in_order();
+            load_q(next_of(0));
             in_order();
             load_p(0);
         }
         for (int c = 0; c < chunks; ++c) {
             const uint32_t here = region(c) + lane * 16;
-            lds_barrier();                                     // S is there
+            lds_barrier();                                     // S, K and Q are there
             f32x4 o[S2];
 #pragma unroll
             for (int n = 0; n < S2; ++n) o[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int dp = 0; dp < DP; ++dp) {
+                Row8<VF, VEC> rows;
                 u32x4 sp[3], part[3];
+                rows.get(k_at + L::q_at + (pt * DP + dp) * L::frag, g, m);
 #pragma unroll
                 for (int n = 0; n < S2; ++n) sp[n] = lds16(here + (dp * 3 + n) * kFrag);
-                row_parts<VF, VEC>(qr[dp], part);
+                row_parts<VF, VEC>(rows, part);
                 part_pairs<P::in, S2, S2 - 1>([&](int i, int j) { o[j] = mfma16(part[i], sp[j], o[j]); });
             }
             f32x4 out = o[0];
@@ -524,8 +570,11 @@ __global__ __launch_bounds__(512 * NG) void delta_scan_kernel(const DeltaDev a, 
             for (int n = 1; n < S2; ++n) out += o[n];
             out *= eg;
             asm volatile("" : "+v"(out) :: "memory");          // (here, so that the next chunk's factors can come into the same registers)
-            load_rows(next_of(c));
-            lds_barrier();
+            eg = *(const f32x4 *)(decay(next_of(c)) + token);
+            lds_barrier();                                     // Q is done with
+            put_q();
+            load_q(next_of(c + 1));
+            in_order();
             lds_barrier();                                     // U is there
             const u32x4 r0 = lds16(flags), u0 = lds16(flags + 16);
             f32x4 more[S2];
@@ -553,25 +602,37 @@ __global__ __launch_bounds__(512 * NG) void delta_scan_kernel(const DeltaDev a, 
 
     const uint32_t ldk = (uint32_t)(a.ldk * sizeof(T)), ldv = (uint32_t)(a.ldv * sizeof(T)), v_at = mine ? token * ldv + col * (uint32_t)sizeof(T) : kOutside;
     const size_t state = (((size_t)(slot < 0 ? 0 : slot) * a.hv + h) * DK) * DV;
+    const uint32_t state_bytes = (uint32_t)DK * (uint32_t)DV * 4;              // (below 2^31: dv at most 2^20)
+    auto state_at = [&](int w, int t, int r) {
+        const int d = 32 * ((int)pt + 4 * w) + 8 * (int)g + 2 * r + t;
+        return mine && d < DK ? ((uint32_t)d * (uint32_t)DV + (uint32_t)col) * 4 : kOutside;
+    };
     f32x4 S[own][2];                                           // [dp / 4][t][r]: row 32 dp + 8 g + 2 r + t
+    {
+        const window_t from = a.s_in && slot >= 0 ? window(a.s_in + state, state_bytes) : window(a.g, 0);   // (none: zeros)
 #pragma unroll
-    for (int w = 0; w < own; ++w)
+        for (int w = 0; w < own; ++w)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = 32 * ((int)pt + 4 * w) + 8 * (int)g + 2 * r + t;
-                S[w][t][r] = a.s_in && slot >= 0 && mine && d < DK ? a.s_in[state + (size_t)d * DV + col] : 0.0f;
-            }
-    Row8<VF, VEC> kr[DP];
+                for (int r = 0; r < 4; ++r) S[w][t][r] = __uint_as_float(window_load<float>(from, state_at(w, t, r)));
+    }
+    Row8<VF, VEC> kr[each];
     raw_t<T> v_0, v_1, v_2, v_3;                               // (an array of them would be packed, two to a register, as soon as they are loaded)
     Lower<VF, 3> mr[2];
     f32x4 eg, left;
     float keep;
-    auto load_rows = [&](int c) {
-        const window_t kw = window_of(a.k, a.ldk, (size_t)kh * DK, c, DK), vw = window_of(a.v, a.ldv, (size_t)h * DV, c, DV);
+    auto load_k = [&](int c) {                                 // (tokens past the end: zeros)
+        const window_t kw = window_of(a.k, a.ldk, (size_t)kh * DK, c, DK);
 #pragma unroll
-        for (int dp = 0; dp < DP; ++dp) kr[dp].load(kw, row * ldk, 32 * dp + 8 * (int)g, DK);
+        for (int i = 0; i < each; ++i) kr[i].load(kw, row * ldk, 32 * (dp0 + i) + element, DK);
+    };
+    auto put_k = [&](uint32_t at) {
+#pragma unroll
+        for (int i = 0; i < each; ++i) kr[i].put(at + (pt * DP + dp0 + i) * L::frag, lane);
+    };
+    auto load_v = [&](int c) {
+        const window_t vw = window_of(a.v, a.ldv, (size_t)h * DV, c, DV);
         v_0 = window_load<T>(vw, v_at);
         v_1 = window_load<T>(vw, v_at + ldv);
         v_2 = window_load<T>(vw, v_at + 2 * ldv);
@@ -600,32 +661,32 @@ __global__ __launch_bounds__(512 * NG) void delta_scan_kernel(const DeltaDev a, 
     const uint32_t quad = (pt >> 1) * kFrag + lane * 16 + (pt & 1u) * 8;
 
     if (chunks > 0) {
-        load_rows(0);
+        load_k(0);
+        put_k(k_at);
+        load_v(0);
         in_order();
         load_m(0);
         in_order();
+        load_k(next_of(0));
         keep = decay(0)[63];
         share_state(group_at);
     }
     for (int c = 0; c < chunks; ++c) {
-        const uint32_t here = region(c), there = region(c + 1);
-        lds_barrier();                                         // S is there, and the chunk before is done with
+        const uint32_t here = region(c), there = region(c + 1), k_here = k_at + (c & 1) * L::k, k_there = k_at + (~c & 1) * L::k;
+        lds_barrier();                                         // S, K and Q are there, and the chunk before is done with
         f32x4 ks[3];
 #pragma unroll
         for (int n = 0; n < 3; ++n) ks[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int dp = 0; dp < DP; ++dp) {
+            Row8<VF, VEC> rows;
             u32x4 sp[3], part[P::in];
+            rows.get(k_here + (pt * DP + dp) * L::frag, g, m);
 #pragma unroll
             for (int n = 0; n < 3; ++n) sp[n] = lds16(here + (dp * 3 + n) * kFrag + lane * 16);
-            row_parts<VF, VEC>(kr[dp], part);
+            row_parts<VF, VEC>(rows, part);
             part_pairs<P::in, 3, 2>([&](int i, int j) { ks[j] = mfma16(part[i], sp[j], ks[j]); });   // (a sum of each part: none waits for the one before)
         }
-#pragma unroll
-        for (int dp = 0; dp < DP; ++dp)                        // K for the transposed reads: the groups share the work
-            if (dp % NG == (int)group)
-#pragma unroll
-                for (uint32_t i = 0; i < L::half; ++i) to_lds(k_at + (pt * DP + dp) * L::frag + i * kFrag + place(g, m), kr[dp].w[i]);
         float R[4];
         const raw_t<T> v[4] = {v_0, v_1, v_2, v_3};
 #pragma unroll
@@ -638,7 +699,7 @@ __global__ __launch_bounds__(512 * NG) void delta_scan_kernel(const DeltaDev a, 
             for (int n = 0; n < 3; ++n) to_lds(there + n * 2 * kFrag + quad, part[n]);
         }
         if (lane == 0) to_lds(flags + pt * 4, (uint32_t)bad_r);
-        load_rows(next_of(c));
+        load_v(next_of(c));
         lds_barrier();                                         // R is there
         f32x4 u[3];
 #pragma unroll
@@ -684,7 +745,7 @@ __global__ __launch_bounds__(512 * NG) void delta_scan_kernel(const DeltaDev a, 
                 u32x4 lp[2][3], part[2][2][P::in];
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    column_parts<VF, DP>(k_at, (int)pt + 4 * w, s, g, m, part[s]);
+                    column_parts<VF, DP>(k_here, (int)pt + 4 * w, s, g, m, part[s]);
 #pragma unroll
                     for (int n = 0; n < 3; ++n) lp[s][n] = lds16(here + ((S2 + n) * 2 + s) * kFrag + lane * 16);
                 }
@@ -702,18 +763,18 @@ __global__ __launch_bounds__(512 * NG) void delta_scan_kernel(const DeltaDev a, 
             for (int w = 0; w < own; ++w) S[w][0] = S[w][1] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
         }
         share_state(there);                                    // (behind the last chunk nobody reads it)
+        put_k(k_there);
+        load_k(next_of(c + 1));
         keep = decay(next_of(c))[63];
     }
-    if (!a.s_out || slot < 0 || !mine) return;
+    if (!a.s_out || slot < 0) return;                          // uniform
+    const window_t to = window(a.s_out + state, state_bytes);
 #pragma unroll
     for (int w = 0; w < own; ++w)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = 32 * ((int)pt + 4 * w) + 8 * (int)g + 2 * r + t;
-                if (d < DK) a.s_out[state + (size_t)d * DV + col] = S[w][t][r];
-            }
+            for (int r = 0; r < 4; ++r) window_store<float>(to, state_at(w, t, r), S[w][t][r]);
 }
 
 static size_t chunk_block(int32_t type) {
@@ -743,8 +804,8 @@ static hipError_t launch_chunked(const DeltaDev &d, uint8_t *ws, int64_t numbers
     constexpr int wide = 2;                                    // (the registers of more columns would not fit)
     if (d.dk <= 64) return one ? launch_scan<VF, 2, 1, VEC>(d, ws, st) : launch_scan<VF, 2, wide, VEC>(d, ws, st);
     if (d.dk <= 128) return one ? launch_scan<VF, 4, 1, VEC>(d, ws, st) : launch_scan<VF, 4, wide, VEC>(d, ws, st);
-    constexpr int widest = VF == CSB_VAL_F32 ? 1 : 2;          // (nor their LDS)
-    return one ? launch_scan<VF, 8, 1, VEC>(d, ws, st) : launch_scan<VF, 8, widest, VEC>(d, ws, st);
+    if constexpr (VF != CSB_VAL_F32) return launch_scan<VF, 8, 1, VEC>(d, ws, st);
+    return hipErrorInvalidValue;                               // (not reached: csb_delta_chunked)
 }
 
 }  // namespace csb
@@ -765,6 +826,7 @@ extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *s
     const int64_t most = (1 << 23) - 1;                        // (a chunk's offsets in bytes are below 2^31)
     if (args->n_tokens && (args->ldq > most || args->ldk > most || args->ldv > most || args->ldo > most))
         return fail(CSB_EUNSUPPORTED, "2^23 or more elements from one token to the next");
+    if (args->dv > 1 << 20) return fail(CSB_EUNSUPPORTED, "dv above 2^20");
     const int64_t numbers = tile_numbers(args->n_tokens, args->n_seq, kChunkShift);
     const int64_t pairs = ((int64_t)args->n_seq * args->heads_v + 7) / 8 * 8, wide = ((int64_t)args->dv + 63) / 64, narrow = ((int64_t)args->dv + 15) / 16;
     if (pairs > kMaxWorkgroups || pairs * narrow > kMaxWorkgroups || numbers * ((args->heads_v + 3) / 4) > kMaxWorkgroups)
@@ -777,10 +839,12 @@ extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *s
             return fail(CSB_ENOMEM, "out of host memory");
         }
     }
+    // binary32 rows wider than 128 do not fit the LDS beside the rest: token by token
+    if (args->type == CSB_VAL_F32 && args->dk > 128) return launch_delta_recurrent(args, (hipStream_t)stream);
     const DeltaDev d = delta_dev(args);
     const int64_t word = 16 / type_size(args->type);           // elements of an aligned 16-byte word
     const bool vec = args->dk % 8 == 0 && args->ldq % word == 0 && args->ldk % word == 0 && ((uintptr_t)args->d_q | (uintptr_t)args->d_k) % 16 == 0;
-    const bool one = pairs * wide < 256;                       // wavefronts on CUs of their own while there are such
+    const bool one = getenv("NG1") != nullptr || pairs * wide < 256;                       // wavefronts on CUs of their own while there are such
     hipStream_t st = (hipStream_t)stream;
     uint8_t *ws = (uint8_t *)d_ws;
     hipError_t e;
