@@ -12,7 +12,7 @@
 // Precision: state, M, R and U have 24 bits.  A binary32 number is the exact sum of three bfloat16
 // numbers (8 bits each), so a product of the matrix cores' 16-bit form takes as many passes as its
 // operands have parts (bfloat16 inputs one, binary16 two, binary32 three), without the ones below 2^-24; that
-// is 16 / 6 to 16 / 3 of the rate of their binary32 form.  What only the output sees has two parts where the output has 16 bits.
+// is 16 / 6 to 16 / 3 of the rate of their binary32 form.  P, which only the output sees, has two parts (2^-18) where the output has 16 bits.
 //
 // Not finite: an entry of a later token must not reach an earlier one through a zero of M or P.  R and
 // U are looked at once per chunk; from its first token that is not finite on a column of them is taken out of
@@ -27,7 +27,7 @@ namespace csb {
 
 constexpr int kChunk = 64, kChunkShift = 6;
 constexpr uint32_t kFrag = 1024;               // bytes of a 16 x 32 operand of 16-bit numbers: 16 per lane
-constexpr uint32_t kLower = 6;                 // operands that cover the lower triangle of 64 x 64 (see lower_frag)
+constexpr uint32_t kLower = 6;                 // operands that cover the lower triangle of 64 x 64 
 
 using f32x4 = float __attribute__((ext_vector_type(4)));
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
@@ -39,7 +39,7 @@ using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
 // e^G_i and e^(G_64 - G_i).  binary32 operands lie there whole (they are split when read: parts would not fit the LDS).
 template <int VF> struct Parts {
     static constexpr int in = VF == CSB_VAL_BF16 ? 1 : VF == CSB_VAL_F16 ? 2 : 3;      // of q and k
-    static constexpr int out = VF == CSB_VAL_F32 ? 3 : 2;                              // of what only the output sees
+    static constexpr int out = VF == CSB_VAL_F32 ? 3 : 2;                              // of P, which only the output sees
     static constexpr bool whole = VF == CSB_VAL_F32;
     static constexpr uint32_t m_bytes = kLower * (whole ? 2 : 3) * kFrag, p_bytes = kLower * 2 * kFrag;
     static constexpr uint32_t bytes = m_bytes + p_bytes + 512;
@@ -49,7 +49,7 @@ template <int VF> struct Parts {
 // 32 p + 8 (m / 4) + 4 t + m % 4.  A product leaves a lane with four consecutive tokens of a column then, which are one half
 // of the eight consecutive ones that the next product wants from a lane of its other operand.
 __device__ __forceinline__ uint32_t tile_token(uint32_t pt, uint32_t m) { return 32 * (pt >> 1) + 8 * (m >> 2) + 4 * (pt & 1u) + (m & 3u); }
-__device__ __forceinline__ constexpr uint32_t lower_frag(int p, int t, int ks) { return p == 0 ? t : 2 + 2 * t + ks; }
+// operand of tile pt and the 32 columns ks of a lower triangle (pt 0, 1: ks 0 only): 0, 1, then 2 pt - 2 + ks
 
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }   // a's in the low half
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
@@ -160,29 +160,27 @@ __device__ __forceinline__ void wave_sync() {
 
 constexpr int kLdT = 68;                       // words of a row of a 64 x 64 matrix in LDS: rows stay 16-byte aligned
 
-// The lower triangle in LDS as operands in the workspace: 3 or 2 parts, or whole.
+// The lower triangle in LDS as operands in the workspace: 3 or 2 parts, or whole.  (A loop, like all that may be one here: a launch of
+// few chunks waits for its code from memory, some 0.4 us a KiB.)
 template <int NP, bool WHOLE>
 __device__ __forceinline__ void store_lower(const float (*m)[kLdT], uint8_t *to, uint32_t lane) {
     const uint32_t g = lane >> 4, i = lane & 15u;
+#pragma unroll 1
+    for (uint32_t f = 0; f < kLower; ++f) {
+        const uint32_t pt = f < 2 ? f : (f + 2) / 2, ks = f < 2 ? 0 : f & 1u;          // the operand's tile and columns
+        const float *row = &m[tile_token(pt, i)][32 * ks + 8 * g];
+        float x[8];
+        *(f32x4 *)x = *(const f32x4 *)row;
+        *(f32x4 *)(x + 4) = *(const f32x4 *)(row + 4);
+        u32x4 part[3];
+        if constexpr (WHOLE) {
+            part[0] = *(u32x4 *)x;
+            part[1] = *(u32x4 *)(x + 4);
+        } else split<NP, 8>(x, part);
+        constexpr int n = WHOLE ? 2 : NP;
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int ks = 0; ks <= p; ++ks) {
-                const float *row = &m[tile_token(2 * p + t, i)][32 * ks + 8 * g];
-                float x[8];
-                *(f32x4 *)x = *(const f32x4 *)row;
-                *(f32x4 *)(x + 4) = *(const f32x4 *)(row + 4);
-                u32x4 part[3];
-                if constexpr (WHOLE) {
-                    part[0] = *(u32x4 *)x;
-                    part[1] = *(u32x4 *)(x + 4);
-                } else split<NP, 8>(x, part);
-                constexpr int n = WHOLE ? 2 : NP;
-#pragma unroll
-                for (int k = 0; k < n; ++k) *(u32x4 *)(to + (lower_frag(p, t, ks) * n + k) * kFrag + lane * 16) = part[k];
-            }
+        for (int k = 0; k < n; ++k) *(u32x4 *)(to + (f * n + k) * kFrag + lane * 16) = part[k];
+    }
 }
 
 template <int VF, bool VEC>
@@ -263,8 +261,8 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
             }
         wave_sync();
     }
-    wave_sync();
     float (*m)[kLdT] = mat[wave];
+    float strange = 0.0f;                                      // NaN when T has an entry that is not finite
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
@@ -273,30 +271,84 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * x + 4 * (int)g + r, col = 16 * y + (int)i;
                 const float e = __builtin_amdgcn_exp2f((float)((sums[wave][row] - sums[wave][col]) * log2e));
-                m[row][col] = row > col ? betas[wave][row] * e * kk[x][y][r] : 0.0f;
+                const float t = row > col ? betas[wave][row] * e * kk[x][y][r] : 0.0f;
+                strange = fmaf(t, 0.0f, strange);
+                m[row][col] = t;
                 qk[x][y][r] = row >= col ? e * qk[x][y][r] : 0.0f;
             }
     wave_sync();
-    // (1 + T)^-1 by forward substitution, a column per lane, its entries in registers
-    float inv[kChunk];
-#pragma unroll
-    for (int r = 0; r < kChunk; ++r) {
-        float s0 = r == (int)lane ? 1.0f : 0.0f, s1 = 0.0f;
-#pragma unroll
-        for (int j = 0; j < r; j += 4) {
-            const f32x4 t = *(const f32x4 *)&m[r][j];
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                if (j + c < r) {
-                    if (c & 1) s1 = fmaf(-t[c], inv[j + c], s1);
-                    else s0 = fmaf(-t[c], inv[j + c], s0);
-                }
-        }
-        inv[r] = r >= (int)lane ? s0 + s1 : 0.0f;              // (zero also where a row of T is not finite)
+    // A row of T that is not finite must not reach the rows before it through the zeros of (1 + T)^-1: from the first one on T is taken
+    // as zero here, and M's rows become NaN.
+    int bad = kChunk;
+    if (__builtin_expect(__ballot(strange != 0.0f) != 0, 0)) {
+        float z = 0.0f;                                        // a row per lane
+        for (int c = 0; c < (int)lane; ++c) z = fmaf(m[lane][c], 0.0f, z);
+        const uint64_t rows = __ballot(z != 0.0f);
+        bad = rows ? __builtin_ctzll(rows) : kChunk;
+        for (int r = bad; r < kChunk; ++r) m[r][lane] = 0.0f;
+        wave_sync();
     }
+    // (1 + T)^-1 in blocks of 16.  On the diagonal by forward substitution, lane (g, i) column i of block g; ...
+    {
+        float inv[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            float s0 = r == (int)i ? 1.0f : 0.0f, s1 = 0.0f;
+#pragma unroll
+            for (int j = 0; j < r; j += 4) {
+                const f32x4 t = *(const f32x4 *)&m[16 * g + r][16 * g + j];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (j + c < r) {
+                        if (c & 1) s1 = fmaf(-t[c], inv[j + c], s1);
+                        else s0 = fmaf(-t[c], inv[j + c], s0);
+                    }
+            }
+            inv[r] = s0 + s1;
+        }
+        wave_sync();
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m[16 * g + r][16 * g + i] = inv[r];
+        wave_sync();
+    }
+    // ... below it  A_xy = -A_xx sum over y <= k < x of T_xk A_ky,  on the matrix cores in binary32.  A product leaves lane (g, i) with rows
+    // 4 g + r of column i, which is what it takes of its right-hand operand when step r runs over columns 4 g + r of the left one.
+    f32x4 inv[4][4];
+    auto left_of = [&](int x, int y) { return *(const f32x4 *)&m[16 * x + i][16 * y + 4 * g]; };
+    auto product = [&](f32x4 left, f32x4 right, f32x4 d) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) d = __builtin_amdgcn_mfma_f32_16x16x4f32(left[r], right[r], d, 0, 0, 0);
+        return d;
+    };
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) inv[x][x][r] = m[16 * x + 4 * g + r][16 * x + i];
+#pragma unroll
+    for (int apart = 1; apart < 4; ++apart)
+#pragma unroll
+        for (int x = apart; x < 4; ++x) {
+            const int y = x - apart;
+            f32x4 d{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = y; k < x; ++k) d = product(left_of(x, k), inv[k][y], d);
+            inv[x][y] = product(-left_of(x, x), d, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+        }
     wave_sync();
 #pragma unroll
-    for (int r = 0; r < kChunk; ++r) m[r][lane] = r >= (int)lane ? inv[r] * beta : 0.0f;
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int y = 0; y <= (x | 1); ++y)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * x + 4 * (int)g + r, col = 16 * y + (int)i;
+                float v = 0.0f;
+                if (y <= x) {
+                    v = row >= bad ? __builtin_nanf("") : inv[x][y <= x ? y : 0][r] * betas[wave][col];
+                    if (y == x && row < col) v = 0.0f;         // (also where beta is not finite)
+                }
+                m[row][col] = v;
+            }
     wave_sync();
     store_lower<3, Parts<VF>::whole>(m, block, lane);
     wave_sync();
@@ -360,7 +412,7 @@ __device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 template <int VF, int DP> struct ScanLds {
     static constexpr uint32_t half = VF == CSB_VAL_F32 ? 2 : 1;               // 16-byte words of a lane's eight numbers of K
     static constexpr uint32_t frag = half * kFrag, k = 4 * DP * frag, q_at = 2 * k, groups_at = 3 * k;
-    static constexpr uint32_t u_bytes = (2 * Parts<VF>::out + 6) * kFrag;     // U's parts, then e^(G_64 - G) U's
+    static constexpr uint32_t u_bytes = 12 * kFrag;       // U's parts, then e^(G_64 - G) U's
     static constexpr uint32_t region = 3 * DP * kFrag > u_bytes ? 3 * DP * kFrag : u_bytes;
     static constexpr uint32_t flags = 2 * region, told = flags + 32, group = told + 2 * 4 * 16 * 4;
     static constexpr uint32_t bytes(int groups) { return groups_at + groups * group; }
@@ -487,7 +539,7 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
     using T = typename Elem<VF>::T;
     using L = ScanLds<VF, DP>;
     using P = Parts<VF>;
-    constexpr int S2 = P::out, own = (DP + 3) / 4;
+    constexpr int own = (DP + 3) / 4;
     extern __shared__ __align__(16) uint8_t smem[];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, m = lane & 15u;
     const uint32_t pt = wave & 3u, group = wave >> 3;
@@ -552,22 +604,22 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
         for (int c = 0; c < chunks; ++c) {
             const uint32_t here = region(c) + lane * 16;
             lds_barrier();                                     // S, K and Q are there
-            f32x4 o[S2];
+            f32x4 o[3];
 #pragma unroll
-            for (int n = 0; n < S2; ++n) o[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int n = 0; n < 3; ++n) o[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int dp = 0; dp < DP; ++dp) {
                 Row8<VF, VEC> rows;
                 u32x4 sp[3], part[3];
                 rows.get(k_at + L::q_at + (pt * DP + dp) * L::frag, g, m);
 #pragma unroll
-                for (int n = 0; n < S2; ++n) sp[n] = lds16(here + (dp * 3 + n) * kFrag);
+                for (int n = 0; n < 3; ++n) sp[n] = lds16(here + (dp * 3 + n) * kFrag);
                 row_parts<VF, VEC>(rows, part);
-                part_pairs<P::in, S2, S2 - 1>([&](int i, int j) { o[j] = mfma16(part[i], sp[j], o[j]); });
+                part_pairs<P::in, 3, 2>([&](int i, int j) { o[j] = mfma16(part[i], sp[j], o[j]); });
             }
             f32x4 out = o[0];
 #pragma unroll
-            for (int n = 1; n < S2; ++n) out += o[n];
+            for (int n = 1; n < 3; ++n) out += o[n];
             out *= eg;
             asm volatile("" : "+v"(out) :: "memory");          // (here, so that the next chunk's factors can come into the same registers)
             eg = *(const f32x4 *)(decay(next_of(c)) + token);
@@ -577,20 +629,20 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
             in_order();
             lds_barrier();                                     // U is there
             const u32x4 r0 = lds16(flags), u0 = lds16(flags + 16);
-            f32x4 more[S2];
+            f32x4 more[3];
 #pragma unroll
-            for (int n = 0; n < S2; ++n) more[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int n = 0; n < 3; ++n) more[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int s = 0; s < 2; ++s)
                 if (s == 0 || pt >= 2) {
                     u32x4 up[3], part[3];
                     pr[s].parts(part);
 #pragma unroll
-                    for (int n = 0; n < S2; ++n) up[n] = lds16(here + (2 * n + s) * kFrag);
-                    part_pairs<S2, S2, S2 - 1>([&](int i, int j) { more[j] = mfma16(part[i], up[j], more[j]); });
+                    for (int n = 0; n < 3; ++n) up[n] = lds16(here + (2 * n + s) * kFrag);
+                    part_pairs<P::out, 3, 2>([&](int i, int j) { more[j] = mfma16(part[i], up[j], more[j]); });
                 }
 #pragma unroll
-            for (int n = 0; n < S2; ++n) out += more[n];
+            for (int n = 0; n < 3; ++n) out += more[n];
             const int bad = first_bad(r0, u0, told, m);
             const window_t ow = window_of(a.out, a.ldo, (size_t)h * DV, c, DV);
 #pragma unroll
@@ -725,10 +777,10 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
             asm volatile("" : "+v"(l[0]), "+v"(l[1]), "+v"(l[2]), "+v"(l[3]) :: "memory");   // (as above)
             split<3, 4>(l, part);
 #pragma unroll
-            for (int n = 0; n < 3; ++n) to_lds(here + (S2 + n) * 2 * kFrag + quad, part[n]);
-            split<S2, 4>(U, part);
+            for (int n = 0; n < 3; ++n) to_lds(here + (3 + n) * 2 * kFrag + quad, part[n]);
+            split<3, 4>(U, part);
 #pragma unroll
-            for (int n = 0; n < S2; ++n) to_lds(here + n * 2 * kFrag + quad, part[n]);
+            for (int n = 0; n < 3; ++n) to_lds(here + n * 2 * kFrag + quad, part[n]);
         }
         if (lane == 0) to_lds(flags + 16 + pt * 4, (uint32_t)bad_u);
         load_m(next_of(c));
@@ -747,7 +799,7 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
                 for (int s = 0; s < 2; ++s) {
                     column_parts<VF, DP>(k_here, (int)pt + 4 * w, s, g, m, part[s]);
 #pragma unroll
-                    for (int n = 0; n < 3; ++n) lp[s][n] = lds16(here + ((S2 + n) * 2 + s) * kFrag + lane * 16);
+                    for (int n = 0; n < 3; ++n) lp[s][n] = lds16(here + ((3 + n) * 2 + s) * kFrag + lane * 16);
                 }
                 part_pairs<P::in, 3, 2>([&](int i, int j) {
                     S[w][0] = mfma16(part[0][0][i], lp[0][j], S[w][0]);
@@ -844,7 +896,7 @@ extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *s
     const DeltaDev d = delta_dev(args);
     const int64_t word = 16 / type_size(args->type);           // elements of an aligned 16-byte word
     const bool vec = args->dk % 8 == 0 && args->ldq % word == 0 && args->ldk % word == 0 && ((uintptr_t)args->d_q | (uintptr_t)args->d_k) % 16 == 0;
-    const bool one = getenv("NG1") != nullptr || pairs * wide < 256;                       // wavefronts on CUs of their own while there are such
+    const bool one = pairs * wide < 256;                       // a CU each while there are such                       // wavefronts on CUs of their own while there are such
     hipStream_t st = (hipStream_t)stream;
     uint8_t *ws = (uint8_t *)d_ws;
     hipError_t e;
