@@ -69,7 +69,7 @@ typedef struct {
  * the few tokens of a decoding step; right for any length.  Bitwise reproducible.
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, heads_v
  * no multiple of heads_k, n_tokens no multiple of n_seq without d_start, an unknown type ->
- * CSB_EINVAL; dk > 256, or more than 2^24 workgroups -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.
+ * CSB_EINVAL; dk > 256, or more than 2^24 parts of 32 columns -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.
  * n_seq = 0 does nothing.
  */
 int csb_delta_recurrent(const csb_delta_args *args, void *stream);

@@ -1,7 +1,7 @@
 // The gated delta rule token by token (csb_delta_recurrent), and the checks of its arguments.
 //
 // Per value head, with the state S in binary32:  S <- e^g S;  u = beta (v - S^T k);  S <- S + k u^T;
-// o = scale S^T q.  The columns of S do not depend on each other, so a wavefront takes 16 of them with
+// o = scale S^T q.  The columns of S do not depend on each other, so a wavefront takes 32 of them with
 // all their rows and keeps them in registers from the first token to the last: a state is read once and
 // written once however many tokens a call brings.  Both products are taken from the decayed state before
 // the update, o = scale (S^T q + (k.q) u): one reduction per token instead of two that wait for each other.
@@ -9,88 +9,99 @@
 
 namespace csb {
 
-// Lane (x = lane / 16, y = lane % 16) holds the 4 columns from 4 x on of the rows y JN .. y JN + JN - 1, so a sum over
-// rows is JN steps in registers and four rotations of 16 lanes.  VEC: operands that are aligned to 4
-// elements, widths that are multiples of 4.
+// Sum over the 8 lanes with the same lane % 8, in every one of them (a fixed order).
+__device__ __forceinline__ float column_sum(float v) {
+    v += row_rotated<8>(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Lane (x = lane % 8, y = lane / 8) holds the 4 columns from 4 x on of the rows y JN .. y JN + JN - 1: eight lanes read 128
+// consecutive bytes of a row.  (16 lanes on 16 rows, 64 bytes of each, were 122 us instead of 43 on 64 requests, 32 heads of 128 x 128.)
+// VEC: operands that are aligned to 4 elements, widths that are multiples of 4.
 template <int VF, int JN, bool VEC>
-__global__ __launch_bounds__(256) void delta_recurrent_kernel(const DeltaDev a, const uint32_t tiles) {
+__global__ __launch_bounds__(256) void delta_recurrent_kernel(const DeltaDev a, const uint32_t tiles, const uint32_t waves) {
     using T = typename Elem<VF>::T;
     using T4 = T __attribute__((ext_vector_type(4)));
     using f32x4 = float __attribute__((ext_vector_type(4)));
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, x = lane >> 4, y = lane & 15u;
-    const uint32_t tile = blockIdx.x % tiles, rest = blockIdx.x / tiles, h = rest % a.hv, seq = rest / a.hv;
-    const uint32_t col0 = (tile * 4 + wave) * 16;
-    if (col0 >= (uint32_t)a.dv) return;                        // (no barrier in this kernel)
-    const uint32_t col = col0 + 4 * x, row = y * JN, DK = a.dk, DV = a.dv;
+    const uint32_t lane = threadIdx.x & 63u, x = lane & 7u, y = lane >> 3;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6));
+    if (wave >= waves) return;                                 // (no barrier in this kernel)
+    const uint32_t rest = wave / tiles, h = rest % a.hv, seq = rest / a.hv;
+    const uint32_t col = (wave % tiles) * 32 + 4 * x, row = y * JN, DK = a.dk, DV = a.dv;
     int64_t first, end, slot;
     delta_sequence(a, (int)seq, &first, &end, &slot);
     const size_t state = ((size_t)(slot < 0 ? 0 : slot) * a.hv + h) * DK * DV;
-    f32x4 S[JN];
-#pragma unroll
-    for (int j = 0; j < JN; ++j) {
-        S[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (a.s_in && slot >= 0 && row + j < DK) {
-            const float *p = a.s_in + state + (size_t)(row + j) * DV + col;
-            if constexpr (VEC) {
-                if (col < DV) S[j] = *(const f32x4 *)p;
-            } else {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) if (col + c < DV) S[j][c] = p[c];
-            }
-        }
-    }
-    struct Token { float k[JN], q[JN], v[4], g, beta; };
+    struct Token { T4 k[JN / 4], q[JN / 4], v; float g, beta; };
     const uint32_t kh = h / a.group;
-    auto load = [&](int64_t t, Token &w) {
-        const T *kp = (const T *)a.k + t * a.ldk + (size_t)kh * DK + row, *qp = (const T *)a.q + t * a.ldq + (size_t)kh * DK + row;
-        const T *vp = (const T *)a.v + t * a.ldv + (size_t)h * DV + col;
+    auto load4 = [&](const T *p, uint32_t at, uint32_t most) {                // p[0 .. 3] as far as at + j < most
+        T4 v{};
         if constexpr (VEC) {
-#pragma unroll
-            for (int j = 0; j < JN; j += 4) {
-                T4 kk{}, qq{};
-                if (row + j < DK) { kk = *(const T4 *)(kp + j); qq = *(const T4 *)(qp + j); }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) { w.k[j + c] = (float)kk[c]; w.q[j + c] = (float)qq[c]; }
-            }
-            T4 vv{};
-            if (col < DV) vv = *(const T4 *)vp;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) w.v[c] = (float)vv[c];
+            if (at < most) v = *(const T4 *)p;
         } else {
 #pragma unroll
-            for (int j = 0; j < JN; ++j) {
-                w.k[j] = row + j < DK ? (float)kp[j] : 0.0f;
-                w.q[j] = row + j < DK ? (float)qp[j] : 0.0f;
-            }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) w.v[c] = col + c < DV ? (float)vp[c] : 0.0f;
+            for (int j = 0; j < 4; ++j) if (at + j < most) v[j] = p[j];
         }
+        return v;
+    };
+    auto load = [&](int64_t t, Token &w) {
+        const T *kp = (const T *)a.k + t * a.ldk + (size_t)kh * DK + row, *qp = (const T *)a.q + t * a.ldq + (size_t)kh * DK + row;
+#pragma unroll
+        for (int j = 0; j < JN / 4; ++j) {
+            w.k[j] = load4(kp + 4 * j, row + 4 * j, DK);
+            w.q[j] = load4(qp + 4 * j, row + 4 * j, DK);
+        }
+        w.v = load4((const T *)a.v + t * a.ldv + (size_t)h * DV + col, col, DV);
         w.g = a.g[t * a.ldg + h];
         w.beta = a.beta[t * a.ldb + h];
     };
-    Token now, next;
+    Token now{}, next{};
     if (first < end) load(first, now);
+    f32x4 S[JN];
+#pragma unroll
+    for (int j = 0; j < JN; ++j) S[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (a.s_in && slot >= 0) {                                 // uniform
+        const float *p = a.s_in + state + (size_t)row * DV + col;
+#pragma unroll
+        for (int j = 0; j < JN; ++j)
+            if (row + j < DK) {
+                if constexpr (VEC) {
+                    if (col < DV) S[j] = *(const f32x4 *)(p + (size_t)j * DV);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) if (col + c < DV) S[j][c] = p[(size_t)j * DV + c];
+                }
+            }
+    }
     for (int64_t t = first; t < end; ++t) {
         if (t + 1 < end) load(t + 1, next);
-        const float decay = expf(now.g);
+        const float decay = __builtin_amdgcn_exp2f((float)((double)now.g * 1.4426950408889634));   // (the argument rounded once)
         f32x4 pk{0.0f, 0.0f, 0.0f, 0.0f}, pq = pk;
         float kq = 0.0f;
 #pragma unroll
         for (int j = 0; j < JN; ++j) {
+            const float k = (float)now.k[j / 4][j % 4], q = (float)now.q[j / 4][j % 4];
             S[j] *= decay;
-            pk += S[j] * now.k[j];
-            pq += S[j] * now.q[j];
-            kq = fmaf(now.k[j], now.q[j], kq);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                pk[c] = fmaf(S[j][c], k, pk[c]);
+                pq[c] = fmaf(S[j][c], q, pq[c]);
+            }
+            kq = fmaf(k, q, kq);
         }
-        kq = row_sum(kq);
+        kq = column_sum(kq);
         f32x4 u, o;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            u[c] = now.beta * (now.v[c] - row_sum(pk[c]));
-            o[c] = a.scale * fmaf(kq, u[c], row_sum(pq[c]));
+            u[c] = now.beta * ((float)now.v[c] - column_sum(pk[c]));
+            o[c] = a.scale * fmaf(kq, u[c], column_sum(pq[c]));
         }
 #pragma unroll
-        for (int j = 0; j < JN; ++j) S[j] += now.k[j] * u;
+        for (int j = 0; j < JN; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) S[j][c] = fmaf((float)now.k[j / 4][j % 4], u[c], S[j][c]);
         if (y == 0) {
             T *op = (T *)a.out + t * a.ldo + (size_t)h * DV + col;
             if constexpr (VEC) {
@@ -106,17 +117,17 @@ __global__ __launch_bounds__(256) void delta_recurrent_kernel(const DeltaDev a, 
         now = next;
     }
     if (!a.s_out || slot < 0) return;
+    float *p = a.s_out + state + (size_t)row * DV + col;
 #pragma unroll
-    for (int j = 0; j < JN; ++j) {
-        if (row + j >= DK) continue;
-        float *p = a.s_out + state + (size_t)(row + j) * DV + col;
-        if constexpr (VEC) {
-            if (col < DV) *(f32x4 *)p = S[j];
-        } else {
+    for (int j = 0; j < JN; ++j)
+        if (row + j < DK) {
+            if constexpr (VEC) {
+                if (col < DV) *(f32x4 *)(p + (size_t)j * DV) = S[j];
+            } else {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) if (col + c < DV) p[c] = S[j][c];
+                for (int c = 0; c < 4; ++c) if (col + c < DV) p[(size_t)j * DV + c] = S[j][c];
+            }
         }
-    }
 }
 
 int check_delta(const char *who, const csb_delta_args *a) {
@@ -153,22 +164,24 @@ DeltaDev delta_dev(const csb_delta_args *a) {
 }
 
 template <int VF, int JN>
-static void launch_recurrent(const DeltaDev &d, bool vec, uint32_t tiles, uint32_t groups, hipStream_t st) {
-    if (vec) hipLaunchKernelGGL((delta_recurrent_kernel<VF, JN, true>), dim3(groups), dim3(256), 0, st, d, tiles);
-    else hipLaunchKernelGGL((delta_recurrent_kernel<VF, JN, false>), dim3(groups), dim3(256), 0, st, d, tiles);
+static void launch_recurrent(const DeltaDev &d, bool vec, uint32_t tiles, uint32_t waves, hipStream_t st) {
+    const uint32_t threads = waves < 1024 ? 64 : 256;          // (few wavefronts: a CU each)
+    const dim3 grid((waves * 64 + threads - 1) / threads);
+    if (vec) hipLaunchKernelGGL((delta_recurrent_kernel<VF, JN, true>), grid, dim3(threads), 0, st, d, tiles, waves);
+    else hipLaunchKernelGGL((delta_recurrent_kernel<VF, JN, false>), grid, dim3(threads), 0, st, d, tiles, waves);
 }
 
 template <int VF>
-static void launch_recurrent(const DeltaDev &d, bool vec, uint32_t tiles, uint32_t groups, hipStream_t st) {
-    if (d.dk <= 64) launch_recurrent<VF, 4>(d, vec, tiles, groups, st);
-    else if (d.dk <= 128) launch_recurrent<VF, 8>(d, vec, tiles, groups, st);
-    else launch_recurrent<VF, 16>(d, vec, tiles, groups, st);
+static void launch_recurrent(const DeltaDev &d, bool vec, uint32_t tiles, uint32_t waves, hipStream_t st) {
+    if (d.dk <= 64) launch_recurrent<VF, 8>(d, vec, tiles, waves, st);
+    else if (d.dk <= 128) launch_recurrent<VF, 16>(d, vec, tiles, waves, st);
+    else launch_recurrent<VF, 32>(d, vec, tiles, waves, st);
 }
 
 int launch_delta_recurrent(const csb_delta_args *a, hipStream_t st) {
-    const int64_t tiles = ((int64_t)a->dv + 63) / 64;
+    const int64_t tiles = ((int64_t)a->dv + 31) / 32;          // 32 columns of a state each: a wavefront's
     if (tiles * a->heads_v > kMaxWorkgroups || tiles * a->heads_v * a->n_seq > kMaxWorkgroups) {
-        set_error("csb_delta: more than 2^24 workgroups");
+        set_error("csb_delta: more than 2^24 wavefronts");
         return CSB_EUNSUPPORTED;
     }
     const DeltaDev d = delta_dev(a);
@@ -176,11 +189,11 @@ int launch_delta_recurrent(const csb_delta_args *a, hipStream_t st) {
     const bool vec = a->dk % 4 == 0 && a->dv % 4 == 0 && a->ldq % 4 == 0 && a->ldk % 4 == 0 && a->ldv % 4 == 0 && a->ldo % 4 == 0 &&
                      ((uintptr_t)a->d_q | (uintptr_t)a->d_k | (uintptr_t)a->d_v | (uintptr_t)a->d_out) % four == 0 &&
                      ((uintptr_t)a->d_state_in | (uintptr_t)a->d_state_out) % 16 == 0;
-    const uint32_t groups = (uint32_t)(tiles * a->heads_v * a->n_seq);
+    const uint32_t waves = (uint32_t)(tiles * a->heads_v * a->n_seq);
     switch (a->type) {
-        case CSB_VAL_F32: launch_recurrent<CSB_VAL_F32>(d, vec, (uint32_t)tiles, groups, st); break;
-        case CSB_VAL_F16: launch_recurrent<CSB_VAL_F16>(d, vec, (uint32_t)tiles, groups, st); break;
-        default: launch_recurrent<CSB_VAL_BF16>(d, vec, (uint32_t)tiles, groups, st); break;
+        case CSB_VAL_F32: launch_recurrent<CSB_VAL_F32>(d, vec, (uint32_t)tiles, waves, st); break;
+        case CSB_VAL_F16: launch_recurrent<CSB_VAL_F16>(d, vec, (uint32_t)tiles, waves, st); break;
+        default: launch_recurrent<CSB_VAL_BF16>(d, vec, (uint32_t)tiles, waves, st); break;
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error(std::string("csb_delta: ") + hipGetErrorString(e)); return CSB_EDEVICE; }

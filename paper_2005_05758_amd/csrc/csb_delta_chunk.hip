@@ -896,7 +896,7 @@ extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *s
     const DeltaDev d = delta_dev(args);
     const int64_t word = 16 / type_size(args->type);           // elements of an aligned 16-byte word
     const bool vec = args->dk % 8 == 0 && args->ldq % word == 0 && args->ldk % word == 0 && ((uintptr_t)args->d_q | (uintptr_t)args->d_k) % 16 == 0;
-    const bool one = pairs * wide < 256;                       // a CU each while there are such                       // wavefronts on CUs of their own while there are such
+    const bool one = pairs * wide < 256;                       // more of them, smaller, while CUs are idle
     hipStream_t st = (hipStream_t)stream;
     uint8_t *ws = (uint8_t *)d_ws;
     hipError_t e;

@@ -51,16 +51,9 @@ __device__ __forceinline__ int tile_sequence(const int32_t *start, int n_seq, in
     return n - 1;
 }
 
-// Sum over the 16 lanes of a DPP row, in every one of them (a fixed order).
+// The value of lane (lane + 16 - N) % 16 of the lane's row of 16.
 template <int N> __device__ __forceinline__ float row_rotated(float v) {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, false));
-}
-__device__ __forceinline__ float row_sum(float v) {
-    v += row_rotated<8>(v);
-    v += row_rotated<4>(v);
-    v += row_rotated<2>(v);
-    v += row_rotated<1>(v);
-    return v;
 }
 #endif
 
