@@ -4,8 +4,10 @@
 // Two launches.  The first takes A X, the long sums (over `cols`), split over the grid and over the wavefronts of
 // a workgroup; each split leaves its partial sums in the workspace.  The second adds the splits up and takes B
 // times that, the short sums (over the rank), into Y: it moves 8 bytes per entry of Y and is bound by that.
-// Both work on tiles of 32 columns, at multiples of 32, of one request: a tile has one adapter, and a column
-// that a neighbour request has too in the same tile is left to that request's own tile.
+// Both work on tiles of 32 columns, at multiples of 32.  A tile has as many adapters as its columns ask for, one in a
+// long request, up to 32 where every column is a request of its own: for each of them the product is made for all 32 columns and
+// kept in its own, so that X and Y are read and written in whole rows of a tile whatever the requests are, and an adapter that several
+// requests of a tile share is read once for them.
 #include <algorithm>
 #include <new>
 
@@ -13,11 +15,11 @@
 
 namespace csb {
 
-constexpr int kAdapterTile = 32, kAdapterShift = 5, kAdapterMaxRank = 128;
+constexpr int kAdapterTile = 32, kAdapterMaxRank = 128;
 
 struct AdapterDev {
     const void *X, *A, *B;
-    float *Y, *t;                              // t [splits][rank][batch]: partial sums of A X
+    float *Y, *t;                              // t [splits][max_rank][batch]: partial sums of A X
     const int32_t *rank, *start, *id;
     const float *scale;
     int64_t ldx, ldy, rows, cols;
@@ -26,142 +28,211 @@ struct AdapterDev {
     int32_t row_group;                         // rows of Y that a workgroup of the second takes
 };
 
-// The columns [c0, c1) of this workgroup's tile that belong to its request, the tile's first column, and the
-// adapter (negative: nothing to do).
-struct AdapterTile {
-    int32_t base, c0, c1, adapter, rank;
-};
-__device__ __forceinline__ AdapterTile adapter_tile(const AdapterDev &a, uint32_t number) {
-    AdapterTile w{0, 0, 0, -1, 0};
-    int64_t first, end, base;
-    int s;
-    if (a.start) {
-        s = tile_sequence(a.start, a.n_seg, a.batch, kAdapterShift, number);
-        if (s < 0) return w;
-        sequence_range(a.start, s, 0, a.batch, &first, &end);
-        base = ((first >> kAdapterShift) + ((int64_t)number - (first >> kAdapterShift) - s)) << kAdapterShift;
-    } else {                                   // one column each: no search
-        s = (int)number;
-        first = number;
-        end = first + 1;
-        base = first & ~(int64_t)(kAdapterTile - 1);
-    }
-    if (base >= end) return w;
-    const int32_t id = a.id[s];
-    if (id < 0 || id >= a.n_adapters) return w;
-    w.base = (int32_t)base;
-    w.c0 = (int32_t)(first > base ? first : base);
-    w.c1 = (int32_t)(end < base + kAdapterTile ? end : base + kAdapterTile);
-    w.rank = a.rank ? min(max(a.rank[id], 0), a.max_rank) : a.max_rank;
-    if (w.c0 < w.c1 && w.rank > 0) w.adapter = id;
-    return w;
-}
-
+using f32x2 = float __attribute__((ext_vector_type(2)));
 using f32x4 = float __attribute__((ext_vector_type(4)));
 using u16x8 = uint16_t __attribute__((ext_vector_type(8)));
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+
+// The adapters of a tile's columns, each once, with the columns that they have (a bit each) and the ranks they use.
+struct AdapterList {
+    int32_t of[kAdapterTile];                  // of a column, -1: none
+    int32_t id[kAdapterTile], rank[kAdapterTile];
+    uint32_t columns[kAdapterTile];
+    int32_t n;
+};
+// Filled by the whole workgroup, for columns base .. base + 31.  (Offsets that do not ascend may name a column twice: one of the two is taken.)
+__device__ __forceinline__ void list_adapters(const AdapterDev &a, int32_t base, AdapterList &w) {
+    if (threadIdx.x < kAdapterTile) {
+        const int32_t col = base + (int32_t)threadIdx.x;
+        w.of[threadIdx.x] = !a.start && col < a.batch ? a.id[col] : -1;
+    }
+    if (a.start) {
+        __syncthreads();
+        for (int32_t s = (int32_t)threadIdx.x; s < a.n_seg; s += (int32_t)blockDim.x) {
+            const int32_t first = min(max(a.start[s], 0), a.batch), end = min(max(a.start[s + 1], first), a.batch);
+            if (first < base + kAdapterTile && end > base)
+                for (int32_t c = max(first, base), id = a.id[s]; c < min(end, base + kAdapterTile); ++c) w.of[c - base] = id;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x < 64) {                    // a lane a column; the first of those with one adapter speaks for all
+        int32_t id = threadIdx.x < kAdapterTile ? w.of[threadIdx.x] : -1;
+        int32_t rank = 0;
+        if (id >= 0 && id < a.n_adapters) rank = a.rank ? min(max(a.rank[id], 0), a.max_rank) : a.max_rank;
+        if (rank == 0) id = -1;
+        uint32_t mine = 0;
+        for (int c = 0; c < kAdapterTile; ++c) {
+            const uint32_t same = (uint32_t)__ballot(id == __builtin_amdgcn_readlane(id, c));
+            if (c == (int)threadIdx.x) mine = same;
+        }
+        const bool speaks = id >= 0 && (int)__builtin_ctz(mine) == (int)threadIdx.x;
+        const uint64_t speakers = __ballot(speaks);
+        if (speaks) {
+            const int at = __popcll(speakers & ((1ull << threadIdx.x) - 1));
+            w.id[at] = id;
+            w.rank[at] = rank;
+            w.columns[at] = mine;
+        }
+        if (threadIdx.x == 0) w.n = __popcll(speakers);
+    }
+    __syncthreads();
+}
 
 // t = A X for one tile: 16 x 16 products on the matrix cores, RT sixteens of ranks by the 32 columns.  A wavefront takes
 // k_wave consecutive columns of A, 32 (16 for binary32) at a time; lane (g = lane / 16, i = lane % 16) holds row i of A at
 // 8 (4) columns from 8 g (4 g) on.  16-bit operands: X comes as pairs of neighbouring columns of Y, so that the first product takes the
 // even and the second the odd ones, and no lane needs another's data to have its 8 consecutive rows of X.
 // AV: rows of A in aligned 16-byte words.  XV: pairs of X in aligned 4-byte words.
-template <int VF, int RT, bool AV, bool XV>
+// MANY: the adapters of a tile are dealt out to gridDim.z workgroups, and a wavefront keeps its part of X (k_wave at most kStay) in registers
+// for all of them; else the steps over X are outermost (a tile of one adapter, rarely two).
+constexpr int kStay = 128;
+template <int VF, int RT, bool AV, bool XV, bool MANY>
 __global__ __launch_bounds__(256) void adapter_down_kernel(const AdapterDev a) {
     using T = typename Elem<VF>::T;
+    constexpr int step = VF == CSB_VAL_F32 ? 16 : 32, per = step / 4;          // columns of A a step, of a lane
     __shared__ float part[4][RT * 16][kAdapterTile];
-    const AdapterTile w = adapter_tile(a, blockIdx.x);
-    if (w.adapter < 0) return;                 // uniform
+    __shared__ AdapterList list;
+    const int32_t base = (int32_t)blockIdx.x * kAdapterTile;
+    list_adapters(a, base, list);
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15u;
     const int64_t k0 = ((int64_t)blockIdx.y * 4 + wave) * a.k_wave, k1 = min(k0 + a.k_wave, a.cols);
-    const T *A = (const T *)a.A + (size_t)w.adapter * a.max_rank * a.cols, *X = (const T *)a.X;
-    f32x4 acc[RT][2];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) acc[r][0] = acc[r][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    if constexpr (VF == CSB_VAL_F32) {
-        const int32_t n0 = w.base + (int32_t)i, n1 = n0 + 16;
-        const bool in0 = n0 >= w.c0 && n0 < w.c1, in1 = n1 >= w.c0 && n1 < w.c1;
-        for (int64_t k = k0; k < k1; k += 16) {
-            const int64_t kg = k + 4 * g;
-            float x0[4], x1[4], v[RT][4];
+    const T *X = (const T *)a.X;
+    // X's operands of one step: binary32 columns i and 16 + i, 16-bit 2 i and 2 i + 1
+    const int32_t n0 = base + (VF == CSB_VAL_F32 ? (int32_t)i : 2 * (int32_t)i), n1 = n0 + (VF == CSB_VAL_F32 ? 16 : 1);
+    const bool in0 = n0 < a.batch, in1 = n1 < a.batch;
+    struct Right { u32x4 w[2]; };
+    auto load_x = [&](int64_t k) {
+        const int64_t kg = k + per * g;
+        Right x;
+        if constexpr (VF == CSB_VAL_F32) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                x0[j] = in0 && kg + j < k1 ? X[(kg + j) * a.ldx + n0] : 0.0f;
-                x1[j] = in1 && kg + j < k1 ? X[(kg + j) * a.ldx + n1] : 0.0f;
+                x.w[0][j] = in0 && kg + j < k1 ? __float_as_uint(X[(kg + j) * a.ldx + n0]) : 0u;
+                x.w[1][j] = in1 && kg + j < k1 ? __float_as_uint(X[(kg + j) * a.ldx + n1]) : 0u;
             }
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const int32_t row = 16 * r + (int32_t)i;
-                const float *p = A + (size_t)row * a.cols + kg;
-                if constexpr (AV) {
-                    f32x4 q{0.0f, 0.0f, 0.0f, 0.0f};
-                    if (row < w.rank && kg < k1) q = *(const f32x4 *)p;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[r][j] = q[j];
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[r][j] = row < w.rank && kg + j < k1 ? p[j] : 0.0f;
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    acc[r][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][j], x0[j], acc[r][0], 0, 0, 0);
-                    acc[r][1] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][j], x1[j], acc[r][1], 0, 0, 0);
-                }
-        }
-    } else {
-        const int32_t n0 = w.base + 2 * (int32_t)i, n1 = n0 + 1;
-        const bool in0 = n0 >= w.c0 && n0 < w.c1, in1 = n1 >= w.c0 && n1 < w.c1;
-        const uint16_t *Xb = (const uint16_t *)X, *Ab = (const uint16_t *)A;
-        for (int64_t k = k0; k < k1; k += 32) {
-            const int64_t kg = k + 8 * g;
-            uint32_t x[8];
-            u32x4 v[RT];
+        } else {
+            uint32_t v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const uint16_t *p = Xb + (kg + j) * a.ldx + n0;
-                x[j] = 0;
+                const uint16_t *p = (const uint16_t *)X + (kg + j) * a.ldx + n0;
+                v[j] = 0;
                 if (kg + j < k1) {
-                    if (XV && in0 && in1) x[j] = *(const uint32_t *)p;
+                    if (XV && in1) v[j] = *(const uint32_t *)p;
                     else {
-                        if (in0) x[j] = p[0];
-                        if (in1) x[j] |= (uint32_t)p[1] << 16;
+                        if (in0) v[j] = p[0];
+                        if (in1) v[j] |= (uint32_t)p[1] << 16;
                     }
                 }
             }
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const int32_t row = 16 * r + (int32_t)i;
-                const uint16_t *p = Ab + (size_t)row * a.cols + kg;
-                v[r] = u32x4{0, 0, 0, 0};
-                if constexpr (AV) {
-                    if (row < w.rank && kg < k1) v[r] = *(const u32x4 *)p;
-                } else if (row < w.rank) {
-                    u16x8 q{0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) if (kg + j < k1) q[j] = p[j];
-                    v[r] = __builtin_bit_cast(u32x4, q);
-                }
-            }
-            u32x4 even, odd;
-#pragma unroll
             for (int j = 0; j < 4; ++j) {
-                even[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x05040100u);
-                odd[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x07060302u);
+                x.w[0][j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x05040100u);
+                x.w[1][j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x07060302u);
             }
-            using T8 = T __attribute__((ext_vector_type(8)));
+        }
+        return x;
+    };
+    auto load_a = [&](const T *A, int rank, int r, int64_t k) {
+        const int64_t kg = k + per * g;
+        const int32_t row = 16 * r + (int32_t)i;
+        const T *p = A + (size_t)row * a.cols + kg;
+        u32x4 v{0, 0, 0, 0};
+        if constexpr (AV) {
+            if (row < rank && kg < k1) v = *(const u32x4 *)p;
+        } else if (row < rank) {
+            if constexpr (VF == CSB_VAL_F32) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (kg + j < k1) v[j] = __float_as_uint(p[j]);
+            } else {
+                u16x8 q{0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) if (kg + j < k1) q[j] = ((const uint16_t *)p)[j];
+                v = __builtin_bit_cast(u32x4, q);
+            }
+        }
+        return v;
+    };
+    auto multiply = [&](u32x4 l, const Right &x, f32x4 *d) {
+        using T8 = T __attribute__((ext_vector_type(16 / sizeof(T))));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (VF == CSB_VAL_F32) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(l[j]), __uint_as_float(x.w[h][j]), d[h], 0, 0, 0);
+            } else if constexpr (VF == CSB_VAL_F16)
+                d[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(T8, l), __builtin_bit_cast(T8, x.w[h]), d[h], 0, 0, 0);
+            else d[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(T8, l), __builtin_bit_cast(T8, x.w[h]), d[h], 0, 0, 0);
+        }
+    };
+    const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 acc[RT][2];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[r][0] = acc[r][1] = zero;
+    uint32_t done = 0;                                         // the columns that this workgroup's adapters have
+    const uint32_t bit0 = 1u << (n0 - base), bit1 = 1u << (n1 - base);
+    if constexpr (MANY) {
+        constexpr int steps = kStay / step;
+        Right x[steps];
+#pragma unroll
+        for (int s = 0; s < steps; ++s) x[s] = load_x(k0 + s * step);
+        auto fetch = [&](int e, u32x4 v[RT][steps]) {
+            const T *A = (const T *)a.A + (size_t)list.id[e] * a.max_rank * a.cols;
+            const int rank = list.rank[e];
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int s = 0; s < steps; ++s) v[r][s] = load_a(A, rank, r, k0 + s * step);
+        };
+        u32x4 v[RT][steps], w[RT][steps];
+        int e = (int)blockIdx.z;
+        if (e < list.n) fetch(e, v);
+        for (; e < list.n; e += (int)gridDim.z) {
+            const int after = e + (int)gridDim.z;
+            if (after < list.n) fetch(after, w);               // the next one's while this one's are multiplied
+            const uint32_t columns = list.columns[e];
+            done |= columns;
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const T8 av = __builtin_bit_cast(T8, v[r]), e = __builtin_bit_cast(T8, even), o = __builtin_bit_cast(T8, odd);
-                if constexpr (VF == CSB_VAL_F16) {
-                    acc[r][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av, e, acc[r][0], 0, 0, 0);
-                    acc[r][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(av, o, acc[r][1], 0, 0, 0);
-                } else {
-                    acc[r][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, e, acc[r][0], 0, 0, 0);
-                    acc[r][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, o, acc[r][1], 0, 0, 0);
-                }
+                f32x4 d[2] = {zero, zero};
+#pragma unroll
+                for (int s = 0; s < steps; ++s) multiply(v[r][s], x[s], d);
+                if (columns & bit0) acc[r][0] = d[0];
+                if (columns & bit1) acc[r][1] = d[1];
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int s = 0; s < steps; ++s) v[r][s] = w[r][s];
+        }
+    } else {
+        for (int e = 0; e < list.n; ++e) {
+            const T *A = (const T *)a.A + (size_t)list.id[e] * a.max_rank * a.cols;
+            const uint32_t columns = list.columns[e];
+            const int rank = list.rank[e];
+            done |= columns;
+            f32x4 d[RT][2];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) d[r][0] = d[r][1] = zero;
+            Right x = load_x(k0);
+            u32x4 v[RT];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) v[r] = load_a(A, rank, r, k0);
+            for (int64_t k = k0; k < k1; k += step) {          // the next step's operands while this one's are multiplied
+                const Right x_next = load_x(k + step);
+                u32x4 v_next[RT];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) v_next[r] = load_a(A, rank, r, k + step);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) multiply(v[r], x, d[r]);
+                x = x_next;
+#pragma unroll
+                for (int r = 0; r < RT; ++r) v[r] = v_next[r];
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                if (columns & bit0) acc[r][0] = d[r][0];
+                if (columns & bit1) acc[r][1] = d[r][1];
             }
         }
     }
@@ -170,122 +241,288 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(const AdapterDev a) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-                part[wave][16 * r + 4 * g + c][VF == CSB_VAL_F32 ? 16 * h + i : 2 * i + h] = acc[r][h][c];
+            for (int c = 0; c < 4; ++c) part[wave][16 * r + 4 * g + c][(h ? n1 : n0) - base] = acc[r][h][c];
     __syncthreads();
     const uint32_t n = threadIdx.x & 31u;
-    const int32_t col = w.base + (int32_t)n;
-    if (col < w.c0 || col >= w.c1) return;
-    for (int32_t r = threadIdx.x >> 5; r < w.rank; r += 8)
-        a.t[((size_t)blockIdx.y * a.max_rank + r) * a.batch + col] = (part[0][r][n] + part[1][r][n]) + (part[2][r][n] + part[3][r][n]);
+    if (!(done >> n & 1u)) return;
+    for (int32_t r = threadIdx.x >> 5; r < a.max_rank; r += 8)  // (past an adapter's ranks: zeros)
+        a.t[((size_t)blockIdx.y * a.max_rank + r) * a.batch + base + n] = (part[0][r][n] + part[1][r][n]) + (part[2][r][n] + part[3][r][n]);
 }
 
-// Y += B t for one tile and row_group rows: t, its splits added up and scaled, sits in LDS; a wavefront takes 16 rows of B at
-// a time.  binary32 products on the matrix cores: t keeps its 24 bits.
-// BV: rows of B in aligned words of 4 elements.
-template <int VF, bool BV>
+// E numbers as 3 bfloat16 numbers each, every part the nearest to what is left: exact (8 bits and a sign each).
+template <int E>
+__device__ __forceinline__ void three_parts(const float *x, uint16_t (*part)[E]) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        float rest = x[e];
+#pragma unroll
+        for (int n = 0; n < 3; ++n) {
+            const __bf16 near = (__bf16)rest;
+            part[n][e] = __builtin_bit_cast(uint16_t, near);
+            rest -= (float)near;
+        }
+    }
+}
+
+// Y += B t for one tile and row_group rows.  t, its splits added up and scaled, goes through LDS into the operands of the matrix cores:
+// tile column h of lane i is column 2 i + h, so that a lane has two neighbouring columns of Y and 16 lanes a whole row of the tile.
+// 16-bit B: t as three bfloat16 parts (24 bits), a third of a pass each against eight for the binary32 form (69 us instead of REPLACED2 on 8192
+// rows x 2048 columns of rank 64); binary16 B as two.  binary32 B: the binary32 form.
+// Wavefronts share the rows where the tile has few adapters and the adapters where it has many (each column has one, so nothing is added up).
+// BV: rows of B in aligned words of 8 (binary32: 4) elements.  YV: pairs of Y in aligned 8-byte words.
+template <int VF, int KS, bool BV, bool YV>
 __global__ __launch_bounds__(256) void adapter_up_kernel(const AdapterDev a) {
     using T = typename Elem<VF>::T;
-    using T4 = T __attribute__((ext_vector_type(4)));
-    __shared__ float t[kAdapterMaxRank][kAdapterTile + 1];
-    const AdapterTile w = adapter_tile(a, blockIdx.x);
-    if (w.adapter < 0) return;                 // uniform
-    const float scale = a.scale ? a.scale[w.adapter] : 1.0f;
-    const int32_t steps = (w.rank + 15) / 16;
+    constexpr int per = VF == CSB_VAL_F32 ? 4 : 8, step = 4 * per;             // ranks of a lane, of a step
+    __shared__ AdapterList list;
+    __shared__ float t[KS * 32][kAdapterTile];
+    __shared__ float many[4][16][kAdapterTile];
+    const int32_t base = (int32_t)blockIdx.x * kAdapterTile;
+    list_adapters(a, base, list);
+    if (list.n == 0) return;                                   // uniform
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15u;
+    uint32_t all = 0;
+    for (int e = 0; e < list.n; ++e) all |= list.columns[e];
     {
         const uint32_t n = threadIdx.x & 31u;
-        const int32_t col = w.base + (int32_t)n;
-        const bool in = col >= w.c0 && col < w.c1;
-        for (int32_t r = threadIdx.x >> 5; r < 16 * steps; r += 8) {
+        const bool in = all >> n & 1u;
+        const float scale = in && a.scale ? a.scale[list.of[n]] : 1.0f;
+        for (int32_t r = threadIdx.x >> 5; r < KS * 32; r += 8) {
             float s = 0.0f;
-            if (in && r < w.rank)
-                for (int32_t p = 0; p < a.splits; ++p) s += a.t[((size_t)p * a.max_rank + r) * a.batch + col];
+            if (in && r < a.max_rank)
+                for (int32_t p = 0; p < a.splits; ++p) s += a.t[((size_t)p * a.max_rank + r) * a.batch + base + n];
             t[r][n] = s * scale;
         }
     }
     __syncthreads();
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15u;
-    const T *B = (const T *)a.B + (size_t)w.adapter * a.rows * a.max_rank;
-    const int32_t n0 = w.base + (int32_t)i, n1 = n0 + 16;
-    const bool in0 = n0 >= w.c0 && n0 < w.c1, in1 = n1 >= w.c0 && n1 < w.c1;
+    // t as right-hand operands, once for all rows: lane (g, i) has ranks 32 s + 8 g .. + 7 of columns 2 i and 2 i + 1
+    u32x4 tp[KS][2][3];
+    float tf[2 * KS][2][4];
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (VF == CSB_VAL_F32) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) tf[2 * s + half][h][j] = t[32 * s + 16 * half + 4 * g + j][2 * i + h];
+            } else {
+                float x[8];
+                uint16_t p[3][8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = t[32 * s + 8 * g + j][2 * i + h];
+                three_parts<8>(x, p);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) __builtin_memcpy(&tp[s][h][n], p[n], 16);
+            }
+        }
+    const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t bit0 = 1u << (2 * i), bit1 = 2u << (2 * i);
+    struct Left { u32x4 w[VF == CSB_VAL_F32 ? 2 * KS : KS]; };
+    constexpr int words = VF == CSB_VAL_F32 ? 2 * KS : KS;
+    auto load_b = [&](int e, int64_t row, int64_t last) {      // the lane's part of row `row` (zeros past the adapter's ranks: what is stored there is not used)
+        const T *p = (const T *)a.B + ((size_t)list.id[e] * a.rows + row) * a.max_rank;
+        const int rank = list.rank[e];
+        Left l;
+#pragma unroll
+        for (int s = 0; s < words; ++s) {
+            const int r = step * s + per * (int)g;
+            T v[per];
+            u32x4 w{0, 0, 0, 0};
+            if constexpr (BV) {
+                if (row < last && r < rank) w = *(const u32x4 *)(p + r);
+                if (r + per > rank) {
+                    __builtin_memcpy(v, &w, 16);
+#pragma unroll
+                    for (int j = 0; j < per; ++j) if (r + j >= rank) v[j] = (T)0.0f;
+                    __builtin_memcpy(&w, v, 16);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < per; ++j) v[j] = row < last && r + j < rank ? p[r + j] : (T)0.0f;
+                __builtin_memcpy(&w, v, 16);
+            }
+            l.w[s] = w;
+        }
+        return l;
+    };
+    auto multiply = [&](const Left &l, f32x4 *d) {
+#pragma unroll
+        for (int s = 0; s < words; ++s) {
+            if constexpr (VF == CSB_VAL_F32) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) d[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(l.w[s][j]), tf[s][h][j], d[h], 0, 0, 0);
+            } else {
+                u32x4 parts[2];
+                constexpr int np = VF == CSB_VAL_F16 ? 2 : 1;
+                if constexpr (VF == CSB_VAL_F16) {             // 11 bits: two parts are exact
+                    float x[8];
+                    uint16_t q[3][8];
+                    const auto v = __builtin_bit_cast(_Float16 __attribute__((ext_vector_type(8))), l.w[s]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
+                    three_parts<8>(x, q);
+                    __builtin_memcpy(&parts[0], q[0], 16);
+                    __builtin_memcpy(&parts[1], q[1], 16);
+                } else parts[0] = l.w[s];
+#pragma unroll
+                for (int n = 2; n >= 0; --n)
+#pragma unroll
+                    for (int b = 0; b < np; ++b)
+                        if (n + b <= 2) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                d[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, parts[b]), __builtin_bit_cast(bf16x8, tp[s][h][n]), d[h], 0, 0, 0);
+                        }
+            }
+        }
+    };
     const int64_t first = (int64_t)blockIdx.y * a.row_group, last = min(first + a.row_group, a.rows);
-    for (int64_t row0 = first + 16 * wave; row0 < last; row0 += 64) {
-        float y0[4], y1[4];
+    const int32_t col = base + 2 * (int32_t)i;
+    const bool in0 = all & bit0, in1 = all & bit1;             // (columns of no adapter are neither read nor written)
+    auto load_y = [&](int64_t row0, f32x2 *y) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const int64_t row = row0 + 4 * g + c;
-            y0[c] = in0 && row < last ? a.Y[row * a.ldy + n0] : 0.0f;
-            y1[c] = in1 && row < last ? a.Y[row * a.ldy + n1] : 0.0f;
-        }
-        f32x4 d0{0.0f, 0.0f, 0.0f, 0.0f}, d1 = d0;
-        const T *p = B + (row0 + i) * a.max_rank;
-        for (int32_t s = 0; s < steps; ++s) {
-            const int32_t r = 16 * s + 4 * (int32_t)g;
-            T4 b{};
-            if (row0 + i < last) {
-                if constexpr (BV) {
-                    if (r < w.rank) b = *(const T4 *)(p + r);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) if (r + j >= w.rank) b[j] = (T)0.0f;   // what is stored past the rank is not used
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) if (r + j < w.rank) b[j] = p[r + j];
+            const float *p = a.Y + row * a.ldy + col;
+            y[c] = f32x2{0.0f, 0.0f};
+            if (row < last) {
+                if (YV && in0 && in1) y[c] = *(const f32x2 *)p;
+                else {
+                    if (in0) y[c][0] = p[0];
+                    if (in1) y[c][1] = p[1];
                 }
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                d0 = __builtin_amdgcn_mfma_f32_16x16x4f32((float)b[j], t[r + j][i], d0, 0, 0, 0);
-                d1 = __builtin_amdgcn_mfma_f32_16x16x4f32((float)b[j], t[r + j][16 + i], d1, 0, 0, 0);
-            }
         }
+    };
+    auto store_y = [&](int64_t row0, const f32x2 *y) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const int64_t row = row0 + 4 * g + c;
-            if (in0 && row < last) a.Y[row * a.ldy + n0] = y0[c] + d0[c];
-            if (in1 && row < last) a.Y[row * a.ldy + n1] = y1[c] + d1[c];
+            float *p = a.Y + row * a.ldy + col;
+            if (row < last) {
+                if (YV && in0 && in1) *(f32x2 *)p = y[c];
+                else {
+                    if (in0) p[0] = y[c][0];
+                    if (in1) p[1] = y[c][1];
+                }
+            }
         }
+    };
+    if (list.n < 4) {                                          // uniform: wavefronts share the rows
+        f32x2 y[4], y_next[4];
+        Left l, l_next;
+        int64_t row0 = first + 16 * wave;
+        if (row0 < last) {
+            load_y(row0, y);
+            l = load_b(0, row0 + i, last);
+        }
+        for (; row0 < last; row0 += 64) {
+            if (row0 + 64 < last) {                            // the next rows while these are multiplied
+                load_y(row0 + 64, y_next);
+                l_next = load_b(0, row0 + 64 + i, last);
+            }
+            f32x4 sum[2] = {zero, zero};
+            for (int e = 0; e < list.n; ++e) {
+                if (e) l = load_b(e, row0 + i, last);
+                f32x4 d[2] = {zero, zero};
+                multiply(l, d);
+                const uint32_t columns = list.columns[e];
+                if (columns & bit0) sum[0] = d[0];
+                if (columns & bit1) sum[1] = d[1];
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) y[c] += f32x2{sum[0][c], sum[1][c]};
+            store_y(row0, y);
+            l = l_next;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) y[c] = y_next[c];
+        }
+        return;
+    }
+    for (int64_t row0 = first; row0 < last; row0 += 16) {      // wavefronts share the adapters
+        f32x2 y[4];
+        if (wave == 0) load_y(row0, y);
+        f32x4 sum[2] = {zero, zero};
+        int e = (int)wave;
+        Left l, l_next;
+        if (e < list.n) l = load_b(e, row0 + i, last);
+        for (; e < list.n; e += 4) {
+            if (e + 4 < list.n) l_next = load_b(e + 4, row0 + i, last);
+            f32x4 d[2] = {zero, zero};
+            multiply(l, d);
+            const uint32_t columns = list.columns[e];
+            if (columns & bit0) sum[0] = d[0];
+            if (columns & bit1) sum[1] = d[1];
+            l = l_next;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) many[wave][4 * g + c][2 * i + h] = sum[h][c];      // (zero where another wavefront's adapter is)
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t r = 4 * g + c, n = 2 * i + h;
+                    y[c][h] += (many[0][r][n] + many[1][r][n]) + (many[2][r][n] + many[3][r][n]);
+                }
+            store_y(row0, y);
+        }
+        __syncthreads();
     }
 }
 
-// How the long sums are split: parts of the grid (at most 16) and columns per wavefront, a multiple of 32.
-static void adapter_split(int64_t cols, int64_t tiles, int32_t *splits, int32_t *k_wave) {
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(16, 1024 / std::max<int64_t>(1, tiles)));
-    const int64_t per = std::max<int64_t>(32, ((cols + want * 4 - 1) / (want * 4) + 31) / 32 * 32);
-    *k_wave = (int32_t)per;
-    *splits = (int32_t)((cols + 4 * per - 1) / (4 * per));
+// Requests of few columns (MANY; ranks up to 64, which the registers hold): parts of the grid that keep X in registers, k_wave = kStay, at most 64 of them; else at most 8
+// (the second launch reads what each leaves), k_wave a multiple of 32.
+static bool adapter_many(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank) { return batch < 8ll * n_seg && rank <= 64 && cols <= 64 * 4 * kStay; }
+static void adapter_split(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank, int32_t *splits, int32_t *k_wave) {
+    const int64_t tiles = (batch + kAdapterTile - 1) / kAdapterTile;
+    if (adapter_many(cols, batch, n_seg, rank)) *k_wave = kStay;
+    else {
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(8, 512 / std::max<int64_t>(1, tiles)));
+        *k_wave = (int32_t)std::max<int64_t>(32, ((cols + want * 4 - 1) / (want * 4) + 31) / 32 * 32);
+    }
+    *splits = (int32_t)((cols + 4ll * *k_wave - 1) / (4ll * *k_wave));
 }
 
-static int64_t adapter_tiles(int32_t batch, int32_t n_seg, bool offsets) {
-    return offsets ? tile_numbers(batch, n_seg, kAdapterShift) : n_seg;
-}
-
-template <int VF, bool AV, bool XV>
+template <int VF, bool AV, bool XV, bool MANY>
 static void launch_down(const AdapterDev &d, dim3 grid, hipStream_t st) {
-    if (d.max_rank <= 16) hipLaunchKernelGGL((adapter_down_kernel<VF, 1, AV, XV>), grid, dim3(256), 0, st, d);
-    else if (d.max_rank <= 32) hipLaunchKernelGGL((adapter_down_kernel<VF, 2, AV, XV>), grid, dim3(256), 0, st, d);
-    else if (d.max_rank <= 64) hipLaunchKernelGGL((adapter_down_kernel<VF, 4, AV, XV>), grid, dim3(256), 0, st, d);
-    else hipLaunchKernelGGL((adapter_down_kernel<VF, 8, AV, XV>), grid, dim3(256), 0, st, d);
+    if (d.max_rank <= 16) hipLaunchKernelGGL((adapter_down_kernel<VF, 1, AV, XV, MANY>), grid, dim3(256), 0, st, d);
+    else if (d.max_rank <= 32) hipLaunchKernelGGL((adapter_down_kernel<VF, 2, AV, XV, MANY>), grid, dim3(256), 0, st, d);
+    else if (MANY || d.max_rank <= 64) hipLaunchKernelGGL((adapter_down_kernel<VF, 4, AV, XV, MANY>), grid, dim3(256), 0, st, d);
+    else if constexpr (!MANY) hipLaunchKernelGGL((adapter_down_kernel<VF, 8, AV, XV, MANY>), grid, dim3(256), 0, st, d);
+}
+template <int VF, bool BV, bool YV>
+static void launch_up(const AdapterDev &d, dim3 grid, hipStream_t st) {
+    if (d.max_rank <= 32) hipLaunchKernelGGL((adapter_up_kernel<VF, 1, BV, YV>), grid, dim3(256), 0, st, d);
+    else if (d.max_rank <= 64) hipLaunchKernelGGL((adapter_up_kernel<VF, 2, BV, YV>), grid, dim3(256), 0, st, d);
+    else hipLaunchKernelGGL((adapter_up_kernel<VF, 4, BV, YV>), grid, dim3(256), 0, st, d);
 }
 
 template <int VF>
-static void launch_adapter(const AdapterDev &d, bool av, bool xv, bool bv, dim3 down, dim3 up, hipStream_t st) {
-    if (av && xv) launch_down<VF, true, true>(d, down, st);
-    else if (av) launch_down<VF, true, false>(d, down, st);
-    else launch_down<VF, false, false>(d, down, st);
-    if (bv) hipLaunchKernelGGL((adapter_up_kernel<VF, true>), up, dim3(256), 0, st, d);
-    else hipLaunchKernelGGL((adapter_up_kernel<VF, false>), up, dim3(256), 0, st, d);
+static void launch_adapter(const AdapterDev &d, bool av, bool xv, bool bv, bool yv, bool many, dim3 down, dim3 up, hipStream_t st) {
+    const bool fast = av && xv;                                // (rows of A or pairs of X that are not aligned: element by element)
+    if (many && fast) launch_down<VF, true, true, true>(d, down, st);
+    else if (many) launch_down<VF, false, false, true>(d, down, st);
+    else if (fast) launch_down<VF, true, true, false>(d, down, st);
+    else launch_down<VF, false, false, false>(d, down, st);
+    if (bv && yv) launch_up<VF, true, true>(d, up, st);
+    else launch_up<VF, false, false>(d, up, st);
 }
 
 }  // namespace csb
 
 extern "C" size_t csb_adapter_workspace_bytes(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank) {
     if (cols <= 0 || batch <= 0 || n_seg <= 0 || rank <= 0 || rank > csb::kAdapterMaxRank) return 0;
-    int32_t splits, k_wave, most = 1;                          // (with offsets there are more tiles and never more splits)
-    csb::adapter_split(cols, csb::adapter_tiles(batch, n_seg, true), &splits, &k_wave);
-    most = std::max(most, splits);
-    csb::adapter_split(cols, csb::adapter_tiles(batch, n_seg, false), &splits, &k_wave);
-    most = std::max(most, splits);
-    return ((size_t)most * (size_t)rank * (size_t)batch * sizeof(float) + 255) / 256 * 256;
+    int32_t splits, k_wave;
+    csb::adapter_split(cols, batch, n_seg, rank, &splits, &k_wave);
+    return ((size_t)splits * (size_t)rank * (size_t)batch * sizeof(float) + 255) / 256 * 256;
 }
 
 extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float *d_Y, int64_t ldy, int64_t rows,
@@ -305,18 +542,21 @@ extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float
     if ((uintptr_t)d_ws % 256) return fail(CSB_EINVAL, "workspace not 256-byte aligned");
     const uintptr_t size = (uintptr_t)type_size(type);
     if (((uintptr_t)d_X | (uintptr_t)d_A | (uintptr_t)d_B) % size || (uintptr_t)d_Y % 4) return fail(CSB_EINVAL, "misaligned pointer");
-    const int64_t tiles = adapter_tiles(batch, n_seg, d_start != nullptr);
+    const int64_t tiles = ((int64_t)batch + kAdapterTile - 1) / kAdapterTile;
     AdapterDev d{};
     d.X = d_X; d.A = d_A; d.B = d_B; d.Y = d_Y; d.t = (float *)d_ws;
     d.rank = d_rank; d.start = d_start; d.id = d_id; d.scale = d_scale;
     d.ldx = ldx; d.ldy = ldy; d.rows = rows; d.cols = cols;
     d.batch = batch; d.n_adapters = n_adapters; d.max_rank = rank; d.n_seg = n_seg;
-    adapter_split(cols, tiles, &d.splits, &d.k_wave);
-    int64_t group = 64;                                        // rows of a workgroup: enough workgroups, and t read by few of them
-    while (group < 512 && tiles * ((rows + 2 * group - 1) / (2 * group)) >= 2048) group *= 2;
+    adapter_split(cols, batch, n_seg, rank, &d.splits, &d.k_wave);
+    const bool many = adapter_many(cols, batch, n_seg, rank);
+    int64_t group = many ? 16 : 64;                            // rows of a workgroup: enough workgroups, and t read by few of them
+    while (group < 512 && tiles * ((rows + 2 * group - 1) / (2 * group)) >= 1024) group *= 2;
     d.row_group = (int32_t)group;
     const int64_t row_groups = (rows + group - 1) / group;
-    if (tiles * std::max<int64_t>(row_groups, d.splits) > kMaxWorkgroups || row_groups > 65535) return fail(CSB_EUNSUPPORTED, "more than 2^24 workgroups");
+    // adapters of a tile over several workgroups while CUs are idle
+    const int64_t deal = many ? std::max<int64_t>(1, std::min<int64_t>(8, 512 / (tiles * d.splits))) : 1;
+    if (tiles * std::max<int64_t>(row_groups, deal * d.splits) > kMaxWorkgroups || row_groups > 65535) return fail(CSB_EUNSUPPORTED, "more than 2^24 workgroups");
     try {
         static const char adapter_user = 0;                    // this entry point as a user of workspaces
         workspace_changed_hands(d_ws, &adapter_user);
@@ -326,13 +566,14 @@ extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float
     const uintptr_t per = type == CSB_VAL_F32 ? 4 : 8;         // elements of a 16-byte word
     const bool av = cols % per == 0 && (uintptr_t)d_A % 16 == 0;
     const bool xv = ldx % 2 == 0 && (uintptr_t)d_X % 4 == 0;
-    const bool bv = rank % 4 == 0 && (uintptr_t)d_B % (4 * size) == 0;
-    const dim3 down((uint32_t)tiles, (uint32_t)d.splits), up((uint32_t)tiles, (uint32_t)row_groups);
+    const bool bv = rank % per == 0 && (uintptr_t)d_B % 16 == 0;
+    const bool yv = ldy % 2 == 0 && (uintptr_t)d_Y % 8 == 0;
+    const dim3 down((uint32_t)tiles, (uint32_t)d.splits, (uint32_t)deal), up((uint32_t)tiles, (uint32_t)row_groups);
     hipStream_t st = (hipStream_t)stream;
     switch (type) {
-        case CSB_VAL_F32: launch_adapter<CSB_VAL_F32>(d, av, true, bv, down, up, st); break;
-        case CSB_VAL_F16: launch_adapter<CSB_VAL_F16>(d, av, xv, bv, down, up, st); break;
-        default: launch_adapter<CSB_VAL_BF16>(d, av, xv, bv, down, up, st); break;
+        case CSB_VAL_F32: launch_adapter<CSB_VAL_F32>(d, av, true, bv, yv, many, down, up, st); break;
+        case CSB_VAL_F16: launch_adapter<CSB_VAL_F16>(d, av, xv, bv, yv, many, down, up, st); break;
+        default: launch_adapter<CSB_VAL_BF16>(d, av, xv, bv, yv, many, down, up, st); break;
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error(std::string("csb_adapter_add: ") + hipGetErrorString(e)); return CSB_EDEVICE; }
