@@ -94,7 +94,6 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(const AdapterDev a) {
     __shared__ float part[4][RT * 16][kAdapterTile];
     __shared__ AdapterList list;
     const int32_t base = (int32_t)blockIdx.x * kAdapterTile;
-    list_adapters(a, base, list);
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15u;
     const int64_t k0 = ((int64_t)blockIdx.y * 4 + wave) * a.k_wave, k1 = min(k0 + a.k_wave, a.cols);
     const T *X = (const T *)a.X;
@@ -175,7 +174,8 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(const AdapterDev a) {
         constexpr int steps = kStay / step;
         Right x[steps];
 #pragma unroll
-        for (int s = 0; s < steps; ++s) x[s] = load_x(k0 + s * step);
+        for (int s = 0; s < steps; ++s) x[s] = load_x(k0 + s * step);          // (requested before the adapters are known)
+        list_adapters(a, base, list);
         auto fetch = [&](int e, u32x4 v[RT][steps]) {
             const T *A = (const T *)a.A + (size_t)list.id[e] * a.max_rank * a.cols;
             const int rank = list.rank[e];
@@ -206,6 +206,7 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(const AdapterDev a) {
                 for (int s = 0; s < steps; ++s) v[r][s] = w[r][s];
         }
     } else {
+        list_adapters(a, base, list);
         for (int e = 0; e < list.n; ++e) {
             const T *A = (const T *)a.A + (size_t)list.id[e] * a.max_rank * a.cols;
             const uint32_t columns = list.columns[e];
@@ -278,21 +279,57 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(const AdapterDev a) {
     __shared__ float t[KS * 32][kAdapterTile];
     __shared__ float many[4][16][kAdapterTile];
     const int32_t base = (int32_t)blockIdx.x * kAdapterTile;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15u;
+    const int64_t first = (int64_t)blockIdx.y * a.row_group, last = min(first + a.row_group, a.rows);
+    const int32_t col = base + 2 * (int32_t)i;
+    const bool there0 = col < a.batch, there1 = col + 1 < a.batch;
+    auto load_y = [&](int64_t row0, f32x2 *y) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int64_t row = row0 + 4 * g + c;
+            const float *p = a.Y + row * a.ldy + col;
+            y[c] = f32x2{0.0f, 0.0f};
+            if (row < last) {
+                if (YV && there1) y[c] = *(const f32x2 *)p;
+                else {
+                    if (there0) y[c][0] = p[0];
+                    if (there1) y[c][1] = p[1];
+                }
+            }
+        }
+    };
+    // What needs no adapter's number is requested before those are known: the first rows of Y, and t, of which a thread adds up ranks r0, r0 + 8,
+    // ... of one column, four splits' loads in flight together.  (t of columns that have no adapter was not written: not used.)
+    f32x2 y[4];
+    load_y(first + 16 * wave, y);
+    const uint32_t tn = threadIdx.x & 31u, r0 = threadIdx.x >> 5;
+    float sum[4 * KS];
+    {
+#pragma unroll
+        for (int k = 0; k < 4 * KS; ++k) sum[k] = 0.0f;
+        const float *p = a.t + min(base + (int32_t)tn, a.batch - 1);
+        const size_t split = (size_t)a.max_rank * a.batch;
+        for (int32_t s = 0; s < a.splits; s += 4) {
+            float v[4][4 * KS];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int k = 0; k < 4 * KS; ++k) v[q][k] = p[min(s + q, a.splits - 1) * split + (size_t)min((int32_t)r0 + 8 * k, a.max_rank - 1) * a.batch];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int k = 0; k < 4 * KS; ++k) sum[k] += s + q < a.splits ? v[q][k] : 0.0f;
+        }
+    }
     list_adapters(a, base, list);
     if (list.n == 0) return;                                   // uniform
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15u;
     uint32_t all = 0;
     for (int e = 0; e < list.n; ++e) all |= list.columns[e];
     {
-        const uint32_t n = threadIdx.x & 31u;
-        const bool in = all >> n & 1u;
-        const float scale = in && a.scale ? a.scale[list.of[n]] : 1.0f;
-        for (int32_t r = threadIdx.x >> 5; r < KS * 32; r += 8) {
-            float s = 0.0f;
-            if (in && r < a.max_rank)
-                for (int32_t p = 0; p < a.splits; ++p) s += a.t[((size_t)p * a.max_rank + r) * a.batch + base + n];
-            t[r][n] = s * scale;
-        }
+        const bool in = all >> tn & 1u;
+        const float scale = in && a.scale ? a.scale[list.of[tn]] : 1.0f;
+#pragma unroll
+        for (int k = 0; k < 4 * KS; ++k) t[r0 + 8 * k][tn] = in && (int32_t)r0 + 8 * k < a.max_rank ? sum[k] * scale : 0.0f;
     }
     __syncthreads();
     // t as right-hand operands, once for all rows: lane (g, i) has ranks 32 s + 8 g .. + 7 of columns 2 i and 2 i + 1
@@ -380,24 +417,7 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(const AdapterDev a) {
             }
         }
     };
-    const int64_t first = (int64_t)blockIdx.y * a.row_group, last = min(first + a.row_group, a.rows);
-    const int32_t col = base + 2 * (int32_t)i;
-    const bool in0 = all & bit0, in1 = all & bit1;             // (columns of no adapter are neither read nor written)
-    auto load_y = [&](int64_t row0, f32x2 *y) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const int64_t row = row0 + 4 * g + c;
-            const float *p = a.Y + row * a.ldy + col;
-            y[c] = f32x2{0.0f, 0.0f};
-            if (row < last) {
-                if (YV && in0 && in1) y[c] = *(const f32x2 *)p;
-                else {
-                    if (in0) y[c][0] = p[0];
-                    if (in1) y[c][1] = p[1];
-                }
-            }
-        }
-    };
+    const bool in0 = all & bit0, in1 = all & bit1;             // (columns of no adapter are not written)
     auto store_y = [&](int64_t row0, const f32x2 *y) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -413,13 +433,10 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(const AdapterDev a) {
         }
     };
     if (list.n < 4) {                                          // uniform: wavefronts share the rows
-        f32x2 y[4], y_next[4];
+        f32x2 y_next[4];
         Left l, l_next;
         int64_t row0 = first + 16 * wave;
-        if (row0 < last) {
-            load_y(row0, y);
-            l = load_b(0, row0 + i, last);
-        }
+        if (row0 < last) l = load_b(0, row0 + i, last);
         for (; row0 < last; row0 += 64) {
             if (row0 + 64 < last) {                            // the next rows while these are multiplied
                 load_y(row0 + 64, y_next);
@@ -444,8 +461,7 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(const AdapterDev a) {
         return;
     }
     for (int64_t row0 = first; row0 < last; row0 += 16) {      // wavefronts share the adapters
-        f32x2 y[4];
-        if (wave == 0) load_y(row0, y);
+        if (wave == 0 && row0 > first) load_y(row0, y);
         f32x4 sum[2] = {zero, zero};
         int e = (int)wave;
         Left l, l_next;
