@@ -272,12 +272,13 @@ __device__ __forceinline__ void three_parts(const float *x, uint16_t (*part)[E])
 // Wavefronts share the rows where the tile has few adapters and the adapters where it has many (each column has one, so nothing is added up).
 // BV: rows of B in aligned words of 8 (binary32: 4) elements.  YV: pairs of Y in aligned 8-byte words.
 template <int VF, int KS, bool BV, bool YV>
-__global__ __launch_bounds__(256) void adapter_up_kernel(const AdapterDev a) {
+__global__ __launch_bounds__(256, KS == 4 ? 2 : 5 - KS) void adapter_up_kernel(const AdapterDev a) {
     using T = typename Elem<VF>::T;
     constexpr int per = VF == CSB_VAL_F32 ? 4 : 8, step = 4 * per;             // ranks of a lane, of a step
     __shared__ AdapterList list;
     __shared__ float t[KS * 32][kAdapterTile];
     __shared__ float many[4][16][kAdapterTile];
+    __shared__ u32x4 tp[VF == CSB_VAL_F32 ? 1 : 6 * KS][64];
     const int32_t base = (int32_t)blockIdx.x * kAdapterTile;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15u;
     const int64_t first = (int64_t)blockIdx.y * a.row_group, last = min(first + a.row_group, a.rows);
@@ -299,24 +300,25 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(const AdapterDev a) {
         }
     };
     // What needs no adapter's number is requested before those are known: the first rows of Y, and t, of which a thread adds up ranks r0, r0 + 8,
-    // ... of one column, four splits' loads in flight together.  (t of columns that have no adapter was not written: not used.)
+    // ... of one column, 16 loads in flight together.  (t of columns that have no adapter was not written: not used.)
     f32x2 y[4];
     load_y(first + 16 * wave, y);
     const uint32_t tn = threadIdx.x & 31u, r0 = threadIdx.x >> 5;
+    constexpr int ahead = 4 / KS;
     float sum[4 * KS];
     {
 #pragma unroll
         for (int k = 0; k < 4 * KS; ++k) sum[k] = 0.0f;
         const float *p = a.t + min(base + (int32_t)tn, a.batch - 1);
         const size_t split = (size_t)a.max_rank * a.batch;
-        for (int32_t s = 0; s < a.splits; s += 4) {
-            float v[4][4 * KS];
+        for (int32_t s = 0; s < a.splits; s += ahead) {
+            float v[ahead][4 * KS];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < ahead; ++q)
 #pragma unroll
                 for (int k = 0; k < 4 * KS; ++k) v[q][k] = p[min(s + q, a.splits - 1) * split + (size_t)min((int32_t)r0 + 8 * k, a.max_rank - 1) * a.batch];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < ahead; ++q)
 #pragma unroll
                 for (int k = 0; k < 4 * KS; ++k) sum[k] += s + q < a.splits ? v[q][k] : 0.0f;
         }
@@ -332,28 +334,21 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(const AdapterDev a) {
         for (int k = 0; k < 4 * KS; ++k) t[r0 + 8 * k][tn] = in && (int32_t)r0 + 8 * k < a.max_rank ? sum[k] * scale : 0.0f;
     }
     __syncthreads();
-    // t as right-hand operands, once for all rows: lane (g, i) has ranks 32 s + 8 g .. + 7 of columns 2 i and 2 i + 1
-    u32x4 tp[KS][2][3];
-    float tf[2 * KS][2][4];
+    // t as right-hand operands, made once for all rows: lane (g, i) has ranks 32 s + 8 g .. + 7 of columns 2 i + h.  They stay in LDS
+    // (their registers would halve the wavefronts of a CU, and with them the rows of Y in flight).
+    if constexpr (VF != CSB_VAL_F32) {
+        for (uint32_t f = wave; f < 2 * KS; f += 4) {
+            const uint32_t s = f / 2, h = f % 2;
+            float x[8];
+            uint16_t p[3][8];
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
+            for (int j = 0; j < 8; ++j) x[j] = t[32 * s + 8 * g + j][2 * i + h];
+            three_parts<8>(x, p);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if constexpr (VF == CSB_VAL_F32) {
-#pragma unroll
-                for (int half = 0; half < 2; ++half)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) tf[2 * s + half][h][j] = t[32 * s + 16 * half + 4 * g + j][2 * i + h];
-            } else {
-                float x[8];
-                uint16_t p[3][8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = t[32 * s + 8 * g + j][2 * i + h];
-                three_parts<8>(x, p);
-#pragma unroll
-                for (int n = 0; n < 3; ++n) __builtin_memcpy(&tp[s][h][n], p[n], 16);
-            }
+            for (int n = 0; n < 3; ++n) __builtin_memcpy(&tp[f * 3 + n][lane], p[n], 16);
         }
+        __syncthreads();
+    }
     const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
     const uint32_t bit0 = 1u << (2 * i), bit1 = 2u << (2 * i);
     struct Left { u32x4 w[VF == CSB_VAL_F32 ? 2 * KS : KS]; };
@@ -389,9 +384,11 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(const AdapterDev a) {
         for (int s = 0; s < words; ++s) {
             if constexpr (VF == CSB_VAL_F32) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < 4; ++j) {
+                    const f32x2 two = *(const f32x2 *)&t[16 * s + 4 * g + j][2 * i];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) d[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(l.w[s][j]), tf[s][h][j], d[h], 0, 0, 0);
+                    for (int h = 0; h < 2; ++h) d[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(l.w[s][j]), two[h], d[h], 0, 0, 0);
+                }
             } else {
                 u32x4 parts[2];
                 constexpr int np = VF == CSB_VAL_F16 ? 2 : 1;
@@ -412,7 +409,7 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(const AdapterDev a) {
                         if (n + b <= 2) {
 #pragma unroll
                             for (int h = 0; h < 2; ++h)
-                                d[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, parts[b]), __builtin_bit_cast(bf16x8, tp[s][h][n]), d[h], 0, 0, 0);
+                                d[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, parts[b]), __builtin_bit_cast(bf16x8, tp[(2 * s + h) * 3 + n][lane]), d[h], 0, 0, 0);
                         }
             }
         }
@@ -567,7 +564,7 @@ extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float
     adapter_split(cols, batch, n_seg, rank, &d.splits, &d.k_wave);
     const bool many = adapter_many(cols, batch, n_seg, rank);
     int64_t group = many ? 16 : 64;                            // rows of a workgroup: enough workgroups, and t read by few of them
-    while (group < 512 && tiles * ((rows + 2 * group - 1) / (2 * group)) >= 1024) group *= 2;
+    while (group < 2048 && tiles * ((rows + 2 * group - 1) / (2 * group)) >= 512) group *= 2;
     d.row_group = (int32_t)group;
     const int64_t row_groups = (rows + group - 1) / group;
     // adapters of a tile over several workgroups while CUs are idle
