@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -17,6 +18,7 @@ VAL_F32, VAL_F16, VAL_BF16 = 0, 1, 2
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libcsbrnn.so")
 _lib = None
+_raw_delta = {}
 
 # every symbol the headers under include/ declare
 SYMBOLS = ["csb_last_error", "csb_pack", "csb_view_get", "csb_unpack", "csb_set_value_format", "csb_value_format", "csb_sharing_model", "csb_plan", "csb_plan_ex", "csb_plan_rows", "csb_plan_stats_get", "csb_plan_validate", "csb_status",
@@ -169,6 +171,12 @@ def load_library():
         fn = getattr(L, name)
         if fn.restype is C.c_int and name not in ("csb_free", "csb_rnn_free"):
             fn.restype = C.c_int
+    # the same entry points taking csb_delta_args as bytes: filling a ctypes structure of 26 fields takes 2 us, a small call's kernel is done in 5
+    for key, name in (("recurrent", "csb_delta_recurrent"), ("chunked", "csb_delta_chunked"), ("workspace", "csb_delta_workspace_bytes")):
+        fn = L[name]
+        fn.argtypes = [C.c_char_p] + [C.c_void_p] * {"recurrent": 1, "chunked": 2, "workspace": 0}[key]
+        fn.restype = C.c_size_t if key == "workspace" else C.c_int
+        _raw_delta[key] = fn
     _lib = L
     return L
 
@@ -251,26 +259,31 @@ def _scratch(nbytes: int, device):
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
-def _delta(call, q, k, v, g, beta, scale, starts, lens, state, slots, state_out, out, stream):
+_DELTA_ARGS = struct.Struct("@6iq3P3q2P2q5PifPq")             # csb_delta_args, as ctypes lays it out
+
+
+def _delta_rows(t, n, w, tokens):
+    """Elements from one token to the next of [tokens, n, w]: (t, head, j) at t * ld + head * w + j."""
+    ld, head, one = t.stride()
+    assert t.is_cuda and (one == 1 or w == 1) and (head == w or n == 1), "heads of a token must be contiguous"
+    return ld if tokens > 1 else max(ld, n * w)
+
+
+def _delta(chunked, q, k, v, g, beta, scale, starts, lens, state, slots, state_out, out, stream):
     import torch
     T, HK, DK = q.shape
-    HV, DV = v.shape[1:]
-    i32, f32 = torch.int32, torch.float32
-    assert k.shape == q.shape and v.shape[0] == T and tuple(g.shape) == (T, HV) and tuple(beta.shape) == (T, HV)
-    assert q.dtype is k.dtype is v.dtype and g.dtype is f32 and beta.dtype is f32
+    Tv, HV, DV = v.shape
+    f32, typ = torch.float32, v.dtype
+    assert T == Tv and k.shape == q.shape and g.shape == beta.shape == (T, HV)
+    assert q.dtype is k.dtype is typ and g.dtype is beta.dtype is f32
     if out is None:
-        out = torch.empty((T, HV, DV), dtype=v.dtype, device=v.device)
-    assert out.shape == v.shape and out.dtype is v.dtype
-
-    def rows(t, w):                                            # (t, head, j) at t * ld + head * w + j
-        assert t.is_cuda
-        (ld, head, one), n = t.stride(), t.shape
-        assert (one == 1 or n[2] == 1) and (head == w or n[1] == 1), "heads of a token must be contiguous"
-        return max(ld, n[1] * n[2]) if n[0] < 2 else ld
-
-    def per_head(t):
-        assert t.is_cuda and (t.stride(1) == 1 or HV == 1)
-        return max(t.stride(0), HV) if T < 2 else t.stride(0)
+        out = torch.empty((T, HV, DV), dtype=typ, device=v.device)
+    else:
+        assert out.shape == v.shape and out.dtype is typ
+    (ldg, one_g), (ldb, one_b) = g.stride(), beta.stride()
+    assert g.is_cuda and beta.is_cuda and (one_g == one_b == 1 or HV == 1)
+    if T < 2:
+        ldg = ldb = HV
     if starts is not None:
         N = starts.numel() - 1
     elif lens is not None:
@@ -281,25 +294,25 @@ def _delta(call, q, k, v, g, beta, scale, starts, lens, state, slots, state_out,
         N = state.shape[0] if state is not None else 1
     assert (lens is None or lens.numel() == N) and (slots is None or slots.numel() == N)
     n_states = 0
-    for s in (state, state_out):
-        if s is not None:
-            assert tuple(s.shape[1:]) == (HV, DK, DV) and (n_states in (0, s.shape[0]))
-            n_states = s.shape[0]
-    a = csb_delta_args(_val_type(q.dtype), HK, HV, DK, DV, N, T, q.data_ptr(), k.data_ptr(), v.data_ptr(), rows(q, DK), rows(k, DK),
-                       rows(v, DV), g.data_ptr(), beta.data_ptr(), per_head(g), per_head(beta), _dptr(starts, i32), _dptr(lens, i32),
-                       _dptr(state, f32), _dptr(state_out, f32), _dptr(slots, i32), n_states,
-                       DK ** -0.5 if scale is None else scale, out.data_ptr(), rows(out, DV))
-    call(a, v.device, _stream_ptr(stream))
+    for t in (state,) if state_out is state else (state, state_out):
+        if t is not None:
+            assert t.shape[1:] == (HV, DK, DV) and n_states in (0, t.shape[0])
+            n_states = t.shape[0]
+    i32 = torch.int32
+    args = (_val_type(typ), HK, HV, DK, DV, N, T, q.data_ptr(), k.data_ptr(), v.data_ptr(), _delta_rows(q, HK, DK, T),
+            _delta_rows(k, HK, DK, T), _delta_rows(v, HV, DV, T), g.data_ptr(), beta.data_ptr(), ldg, ldb, _dptr(starts, i32) or 0,
+            _dptr(lens, i32) or 0, _dptr(state, f32) or 0, (_dptr(state_out, f32) or 0) if state_out is not state else state.data_ptr() if state is not None else 0,
+            _dptr(slots, i32) or 0, n_states, DK ** -0.5 if scale is None else scale, out.data_ptr(), _delta_rows(out, HV, DV, T))
+    lib()
+    raw = _DELTA_ARGS.pack(*args)
+    if chunked:
+        ws = _scratch(_raw_delta["workspace"](raw), v.device)
+        rc = _raw_delta["chunked"](raw, ws.data_ptr() if ws is not None else None, _stream_ptr(stream))
+    else:
+        rc = _raw_delta["recurrent"](raw, _stream_ptr(stream))
+    if rc:
+        _check(rc)
     return out
-
-
-def _delta_chunked(a, device, stream):
-    ws = _scratch(lib().csb_delta_workspace_bytes(a), device)
-    _check(lib().csb_delta_chunked(a, _dptr(ws), stream))
-
-
-def _delta_recurrent(a, device, stream):
-    _check(lib().csb_delta_recurrent(a, stream))
 
 
 _KEEP = object()
@@ -312,12 +325,12 @@ def delta_chunked(q, k, v, g, beta, scale=None, starts=None, lens=None, state=No
     states, or one).  lens [n_seq] int32: only that many tokens of each.  state [n_states, heads_v, dk, dv] float32, slots [n_seq] int32: each
     sequence's state in it (None: in order).  The last states go to state_out: `state` itself unless another tensor or
     None (not kept) is given.  scale: dk ** -0.5 unless given.  Returns out [tokens, heads_v, dv] (a new tensor, or `out`)."""
-    return _delta(_delta_chunked, q, k, v, g, beta, scale, starts, lens, state, slots, state if state_out is _KEEP else state_out, out, stream)
+    return _delta(True, q, k, v, g, beta, scale, starts, lens, state, slots, state if state_out is _KEEP else state_out, out, stream)
 
 
 def delta_recurrent(q, k, v, g, beta, scale=None, starts=None, lens=None, state=None, slots=None, state_out=_KEEP, out=None, stream=None):
     """csb_delta_recurrent: the same rule token by token, for the few tokens of a decoding step; arguments as delta_chunked."""
-    return _delta(_delta_recurrent, q, k, v, g, beta, scale, starts, lens, state, slots, state if state_out is _KEEP else state_out, out, stream)
+    return _delta(False, q, k, v, g, beta, scale, starts, lens, state, slots, state if state_out is _KEEP else state_out, out, stream)
 
 
 def adapter_add(Y, X, A, B, ids, starts=None, scales=None, ranks=None, stream=None):
@@ -327,19 +340,22 @@ def adapter_add(Y, X, A, B, ids, starts=None, scales=None, ranks=None, stream=No
     each).  scales [adapters] float32, ranks [adapters] int32: factor and used ranks of an adapter.  Returns Y."""
     import torch
     cols, batch = X.shape
-    n, rank, _ = A.shape
-    rows = Y.shape[0]
-    i32, f32 = torch.int32, torch.float32
-    assert X.is_cuda and Y.is_cuda and Y.shape[1] == batch and Y.dtype is f32 and X.dtype is A.dtype is B.dtype
-    assert A.shape[2] == cols and tuple(B.shape) == (n, rows, rank)
+    n, rank, A_cols = A.shape
+    rows, Y_batch = Y.shape
+    i32, f32, typ = torch.int32, torch.float32, X.dtype
+    assert X.is_cuda and Y.is_cuda and Y_batch == batch and Y.dtype is f32 and typ is A.dtype is B.dtype
+    assert A_cols == cols and B.shape == (n, rows, rank)
     (ldx, one_x), (ldy, one_y) = X.stride(), Y.stride()
-    assert batch < 2 or (one_x == 1 and one_y == 1)
-    assert (starts is None or starts.numel() == ids.numel() + 1) and all(t is None or t.numel() == n for t in (scales, ranks))
+    assert batch < 2 or one_x == one_y == 1
     segs = ids.numel()
-    ws = _scratch(max(int(lib().csb_adapter_workspace_bytes(cols, batch, segs, rank)), 256), X.device)
-    _check(lib().csb_adapter_add(_val_type(X.dtype), X.data_ptr(), max(ldx, batch), Y.data_ptr(), max(ldy, batch), rows, cols, batch,
-                                 _dptr(A), _dptr(B), n, rank, _dptr(ranks, i32), _dptr(scales, f32), segs, _dptr(starts, i32),
-                                 _dptr(ids, i32), _dptr(ws), _stream_ptr(stream)))
+    assert (starts is None or starts.numel() == segs + 1) and (scales is None or scales.numel() == n) and (ranks is None or ranks.numel() == n)
+    L = lib()
+    ws = torch.empty(max(L.csb_adapter_workspace_bytes(cols, batch, segs, rank), 256), dtype=torch.uint8, device=X.device)
+    rc = L.csb_adapter_add(_val_type(typ), X.data_ptr(), max(ldx, batch), Y.data_ptr(), max(ldy, batch), rows, cols, batch, _dptr(A), _dptr(B),
+                           n, rank, _dptr(ranks, i32), _dptr(scales, f32), segs, _dptr(starts, i32), _dptr(ids, i32), ws.data_ptr(),
+                           _stream_ptr(stream))
+    if rc:
+        _check(rc)
     return Y
 
 
@@ -351,24 +367,28 @@ def verify_drafts(p, q, drafts, u, r, counts=None, stream=None):
     import torch
     N, K1, V = p.shape
     K = K1 - 1
-    i32, f32 = torch.int32, torch.float32
+    i32, f32, typ, dev = torch.int32, torch.float32, p.dtype, p.device
 
     def rows(t, n):
-        assert t.is_cuda and t.shape[2] == V and (V == 1 or t.stride(2) == 1)
-        ld = t.stride(1) if n > 1 else max(V, t.stride(0))
-        assert N < 2 or t.stride(0) == n * ld, "rows of the requests must follow each other at one stride"
+        before, ld, one = t.stride()
+        assert t.is_cuda and (one == 1 or V == 1)
+        if n < 2:
+            ld = max(V, before)
+        assert N < 2 or before == n * ld, "rows of the requests must follow each other at one stride"
         return ld
-    assert tuple(drafts.shape) == (N, K) and tuple(u.shape) == (N, K) and r.numel() == N and (counts is None or counts.numel() == N)
+    assert drafts.shape == u.shape == (N, K) and r.numel() == N and (counts is None or counts.numel() == N)
     ldq = 0
     if q is not None and K:
-        assert tuple(q.shape[:2]) == (N, K) and q.dtype is p.dtype
+        assert q.shape == (N, K, V) and q.dtype is typ
         ldq = rows(q, K)
-    tokens = torch.empty((N, K1), dtype=i32, device=p.device)
-    accepted = torch.empty(N, dtype=i32, device=p.device)
-    ws = _scratch(max(int(lib().csb_verify_workspace_bytes(N, V)), 256), p.device)
-    _check(lib().csb_verify_drafts(_val_type(p.dtype), p.data_ptr(), rows(p, K1), q.data_ptr() if ldq else None, ldq, _dptr(drafts, i32),
-                                   _dptr(u, f32), _dptr(r, f32), _dptr(counts, i32), N, K, V, _dptr(tokens), _dptr(accepted),
-                                   _dptr(ws), _stream_ptr(stream)))
+    tokens = torch.empty((N, K1), dtype=i32, device=dev)
+    accepted = torch.empty(N, dtype=i32, device=dev)
+    L = lib()
+    ws = torch.empty(max(L.csb_verify_workspace_bytes(N, V), 256), dtype=torch.uint8, device=dev)
+    rc = L.csb_verify_drafts(_val_type(typ), p.data_ptr(), rows(p, K1), q.data_ptr() if ldq else None, ldq, _dptr(drafts, i32), _dptr(u, f32),
+                             _dptr(r, f32), _dptr(counts, i32), N, K, V, tokens.data_ptr(), accepted.data_ptr(), ws.data_ptr(), _stream_ptr(stream))
+    if rc:
+        _check(rc)
     return tokens, accepted
 
 

@@ -6,8 +6,8 @@
 // whole units of 2^-38, so the sum of a row, the place of a random number in it and with it the token are the same however
 // the row is split over workgroups.
 //
-// Two launches: the first adds up the units of the row in chunks, the second finds the chunk that the number
-// falls into and the token in it.
+// Vocabularies up to kVerifySmall: one launch, a workgroup a request, the row in registers.  Larger ones: two launches, the
+// first adds up the units of the row in chunks, the second finds the chunk that the number falls into and the token in it.
 #include <algorithm>
 #include <new>
 
@@ -16,7 +16,7 @@
 namespace csb {
 
 constexpr float kUnits = 274877906944.0f;      // 2^38
-constexpr int kVerifyMaxChunks = 1024;
+constexpr int kVerifyMaxChunks = 1024, kVerifyBlocks = 8, kVerifySmall = 16 * 256 * kVerifyBlocks;
 
 struct VerifyDev {
     const void *p, *q;
@@ -68,43 +68,75 @@ template <int VF> struct VerifyRow {
         q = refused && a.q ? (const T *)a.q + ((int64_t)b * a.n_draft + accepted) * a.ldq : nullptr;
         x = refused && !a.q ? a.draft[(int64_t)b * a.n_draft + accepted] : -1;
     }
-    // the weight is p - q, and p - 1 at x
-    __device__ __forceinline__ void at(int32_t v, int64_t *left, int64_t *own) const {
-        const float pv = (float)p[v];
-        const float off = q ? (float)q[v] : v == x ? 1.0f : 0.0f;
-        *left = units(pv - off);
-        *own = units(pv);
+    // four tokens from v on (zeros past `end`): the weights, p - q (p - 1 at x), and p itself
+    __device__ __forceinline__ void at(int32_t v, int32_t end, float *left, float *own) const {
+        using T4 = T __attribute__((ext_vector_type(4), aligned(sizeof(T))));  // (rows start at any element)
+        T4 pv{}, qv{};
+        if (v + 4 <= end) {
+            pv = *(const T4 *)(p + v);
+            if (q) qv = *(const T4 *)(q + v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (v + j < end) {
+                    pv[j] = p[v + j];
+                    if (q) qv[j] = q[v + j];
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float off = q ? (float)qv[j] : v + j == x ? 1.0f : 0.0f;
+            own[j] = (float)pv[j];
+            left[j] = own[j] - off;
+        }
+    }
+    __device__ __forceinline__ void at(int32_t v, int32_t end, int64_t *left, int64_t *own) const {        // ... in units
+        float l[4], o[4];
+        at(v, end, l, o);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { left[j] = units(l[j]); own[j] = units(o[j]); }
     }
 };
 
-__device__ __forceinline__ int64_t wave_sum(int64_t v) {
+template <typename N>
+__device__ __forceinline__ N wave_sum(N v) {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
     return v;
 }
 
+// floor(all * floor(r 2^24) / 2^24), which is below `all`: the units that lie before the token drawn.
+__device__ __forceinline__ int64_t units_before(int64_t all, float r) {
+    const int64_t m = r > 0.0f ? min((int64_t)(fminf(r, 1.0f) * 16777216.0f), (int64_t)16777215) : 0;
+    return (all >> 24) * m + (((all & 0xffffff) * m) >> 24);
+}
+
+// A wavefront adds up one chunk, 1024 tokens at a time: sixteen to a lane, all of their loads in flight.
 template <int VF>
 __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyDev a) {
-    __shared__ int64_t part[4][2];
-    const int b = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int number = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    const int b = number / a.chunks, c = number % a.chunks;
+    if (b >= a.n_req) return;
     const int accepted = accepted_drafts<VF>(a, b, lane);
     const VerifyRow<VF> row(a, b, accepted);
     const int32_t first = c * a.chunk, end = min(first + a.chunk, a.vocab);
     int64_t left = 0, own = 0;
-    for (int32_t v = first + (int32_t)threadIdx.x; v < end; v += 256) {
-        int64_t l, o;
-        row.at(v, &l, &o);
-        left += l;
-        own += o;
+    for (int32_t v = first; v < end; v += 1024) {
+        int64_t l[16], o[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) row.at(v + 256 * i + 4 * lane, end, l + 4 * i, o + 4 * i);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { left += l[i]; own += o[i]; }
     }
     left = wave_sum(left);
     own = wave_sum(own);
-    if (lane == 0) { part[wave][0] = left; part[wave][1] = own; }
-    __syncthreads();
-    if (threadIdx.x < 2)
-        a.sums[((int64_t)b * a.chunks + c) * 2 + threadIdx.x] =
-            part[0][threadIdx.x] + part[1][threadIdx.x] + part[2][threadIdx.x] + part[3][threadIdx.x];
-    if (c == 0 && threadIdx.x == 0) a.accepted_ws[b] = accepted;
+    if (lane == 0) {
+        int64_t *to = a.sums + ((int64_t)b * a.chunks + c) * 2;
+        to[0] = left;
+        to[1] = own;
+        if (c == 0) a.accepted_ws[b] = accepted;
+    }
 }
 
 // Exclusive sum over the workgroup's 256 threads, in thread order; *total: of all.
@@ -143,10 +175,7 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(const VerifyDev a) {
     before[0] = block_before(mine[0], &total[0], part);
     before[1] = block_before(mine[1], &total[1], part);
     const int kind = total[0] > 0 ? 0 : 1;                     // no weight left: p's own
-    const float r = a.r[b];
-    const int64_t m = r > 0.0f ? (int64_t)(fminf(r, 1.0f) * 16777216.0f) : 0;
-    const uint64_t all = (uint64_t)total[kind], mm = (uint64_t)min(m, (int64_t)16777215);
-    const int64_t limit = (int64_t)((all >> 24) * mm + (((all & 0xffffffu) * mm) >> 24));     // floor(all * m / 2^24) < all
+    const int64_t limit = units_before(total[kind], a.r[b]);
     __syncthreads();
     if (before[kind] <= limit && limit < before[kind] + mine[kind]) {          // one thread, if any weight is there
         int64_t s = before[kind];
@@ -159,17 +188,27 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(const VerifyDev a) {
     __syncthreads();
     if (found_chunk >= 0) {                                    // uniform
         const VerifyRow<VF> row(a, b, accepted);
-        const int32_t first = found_chunk * a.chunk, end = min(first + a.chunk, a.vocab), each = (a.chunk + 255) / 256;
-        const int32_t v0 = first + tid * each, v1 = min(v0 + each, end);
-        int64_t sum = 0, all_of_it, w[2];
-        for (int32_t v = v0; v < v1; ++v) { row.at(v, &w[0], &w[1]); sum += w[kind]; }
-        int64_t s = found_before + block_before(sum, &all_of_it, part);
-        if (s <= limit && limit < s + sum)
-            for (int32_t v = v0; v < v1; ++v) {
-                row.at(v, &w[0], &w[1]);
-                if (limit < s + w[kind]) { found_token = v; break; }
-                s += w[kind];
+        const int32_t first = found_chunk * a.chunk, end = min(first + a.chunk, a.vocab);
+        int64_t before_v = found_before;
+        for (int32_t v0 = first; v0 < end; v0 += 1024) {       // four tokens a thread
+            const int32_t v = v0 + 4 * tid;
+            int64_t w[2][4], all_of_it, sum = 0;
+            row.at(v, end, w[0], w[1]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                w[0][j] = kind ? w[1][j] : w[0][j];
+                sum += w[0][j];
             }
+            int64_t s = before_v + block_before(sum, &all_of_it, part);
+            if (s <= limit && limit < s + sum)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (s <= limit && limit < s + w[0][j]) found_token = v + j;
+                    s += w[0][j];
+                }
+            before_v += all_of_it;
+            if (limit < before_v) break;                       // uniform
+        }
         __syncthreads();
     }
     for (int i = tid; i <= a.n_draft; i += 256)
@@ -177,8 +216,83 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(const VerifyDev a) {
     if (tid == 0) a.accepted[b] = accepted;
 }
 
-// Places of a row that a workgroup of the first launch adds up: 1024, or more where that would make more
-// than kVerifyMaxChunks of them.
+// One launch for a request: wavefront w of 16 has the `blocks` times 256 tokens from w * blocks * 256 on, four to a lane and block.
+// Units are added up as whole numbers of binary64: at most 2^15 of 2^38 each, so every sum is exact (and the code half as long: a launch
+// this short waits for its code).
+__device__ __forceinline__ double small_units(float w) { return w > 0.0f ? (double)truncf(fminf(w, 1.0f) * kUnits) : 0.0; }
+template <int VF>
+__global__ __launch_bounds__(1024) void verify_small_kernel(const VerifyDev a, const int32_t blocks) {
+    __shared__ double sums[2][16];
+    __shared__ int32_t token;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const float r = a.r[b];
+    const int accepted = accepted_drafts<VF>(a, b, lane);
+    const VerifyRow<VF> row(a, b, accepted);
+    const int32_t first = wave * blocks * 256 + 4 * lane;
+    float w[kVerifyBlocks][2][4];
+    if (tid == 0) token = -1;
+#pragma unroll
+    for (int i = 0; i < kVerifyBlocks; ++i) {                  // all loads in flight (four blocks at a time: 11.0 us instead of 8.7 at 20011 tokens)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[i][0][j] = w[i][1][j] = 0.0f;
+        if (i < blocks) row.at(first + 256 * i, a.vocab, w[i][0], w[i][1]);
+    }
+    double mine[2] = {0.0, 0.0};
+#pragma unroll
+    for (int i = 0; i < kVerifyBlocks; ++i)
+        if (i < blocks)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { mine[0] += small_units(w[i][0][j]); mine[1] += small_units(w[i][1][j]); }
+    mine[0] = wave_sum(mine[0]);
+    mine[1] = wave_sum(mine[1]);
+    if (lane == 0) { sums[0][wave] = mine[0]; sums[1][wave] = mine[1]; }
+    __syncthreads();
+    double all[2] = {0.0, 0.0}, before[2] = {0.0, 0.0};
+#pragma unroll 4
+    for (int v = 0; v < 16; ++v)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (v < wave) before[k] += sums[k][v];
+            all[k] += sums[k][v];
+        }
+    const bool own = all[0] <= 0.0;                            // no weight left: p's own
+    const double limit = (double)units_before((int64_t)(own ? all[1] : all[0]), r), here = own ? mine[1] : mine[0];
+    double s = own ? before[1] : before[0];
+    if (s <= limit && limit < s + here) {                      // one wavefront, if any weight is there
+#pragma unroll 1
+        for (int i = 0; i < blocks; ++i) {                     // its blocks once more: they are near
+            float l[4], o[4];
+            double x[4], sum = 0.0;
+            row.at(first + 256 * i, a.vocab, l, o);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[j] = small_units(own ? o[j] : l[j]);
+                sum += x[j];
+            }
+            double upto = sum;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const double v = __shfl_up(upto, d);
+                if (lane >= d) upto += v;
+            }
+            double at = s + upto - sum;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (at <= limit && limit < at + x[j]) token = first + 256 * i + j;
+                at += x[j];
+            }
+            s += __shfl(upto, 63);
+            if (limit < s) break;
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i <= a.n_draft; i += 1024)
+        a.tokens[(int64_t)b * (a.n_draft + 1) + i] = i < accepted ? a.draft[(int64_t)b * a.n_draft + i] : i == accepted ? token : -1;
+    if (tid == 0) a.accepted[b] = accepted;
+}
+
+// Tokens of a row that a wavefront of the first launch adds up: 1024, or more where that would make more
+// than kVerifyMaxChunks chunks.
 static void verify_chunks(int32_t vocab, int32_t *chunks, int32_t *chunk) {
     int64_t c = 1024;
     while ((vocab + c - 1) / c > kVerifyMaxChunks) c *= 2;
@@ -188,7 +302,11 @@ static void verify_chunks(int32_t vocab, int32_t *chunks, int32_t *chunk) {
 
 template <int VF>
 static void launch_verify(const VerifyDev &d, hipStream_t st) {
-    hipLaunchKernelGGL(verify_sums_kernel<VF>, dim3((uint32_t)d.n_req * (uint32_t)d.chunks), dim3(256), 0, st, d);
+    if (d.vocab <= kVerifySmall) {
+        hipLaunchKernelGGL(verify_small_kernel<VF>, dim3((uint32_t)d.n_req), dim3(1024), 0, st, d, (d.vocab + 4095) / 4096);
+        return;
+    }
+    hipLaunchKernelGGL(verify_sums_kernel<VF>, dim3(((uint32_t)d.n_req * (uint32_t)d.chunks + 3) / 4), dim3(256), 0, st, d);
     hipLaunchKernelGGL(verify_draw_kernel<VF>, dim3((uint32_t)d.n_req), dim3(256), 0, st, d);
 }
 
