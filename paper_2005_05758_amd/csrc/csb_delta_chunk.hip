@@ -406,15 +406,13 @@ __device__ __forceinline__ void Row8<VF, VEC>::load(window_t from, uint32_t at, 
 // Requests to memory stay in the order written: the first chunk's have the order that the loop's have, so that a wait in the loop is for as many.
 __device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 
-// LDS of a workgroup: K of a chunk and of the next, Q, then per 16 columns two regions that S, R, U and e^(G_64 - G) U take in turn -- S's
-// parts and both of U's in one, R's and the next S's in the other, swapped from chunk to chunk, so that nothing is written before
-// a barrier behind its last reader -- and what tells of numbers that are not finite.
+// LDS of a workgroup: K of a chunk and of the next, Q, then per 16 columns the parts of S, the four wavefronts' parts of K S, R's parts, U's and
+// e^(G_64 - G) U's, and what tells of numbers that are not finite.
 template <int VF, int DP> struct ScanLds {
     static constexpr uint32_t half = VF == CSB_VAL_F32 ? 2 : 1;               // 16-byte words of a lane's eight numbers of K
     static constexpr uint32_t frag = half * kFrag, k = 4 * DP * frag, q_at = 2 * k, groups_at = 3 * k;
-    static constexpr uint32_t u_bytes = 12 * kFrag;       // U's parts, then e^(G_64 - G) U's
-    static constexpr uint32_t region = 3 * DP * kFrag > u_bytes ? 3 * DP * kFrag : u_bytes;
-    static constexpr uint32_t flags = 2 * region, told = flags + 32, group = told + 2 * 4 * 16 * 4;
+    static constexpr uint32_t sums = 3 * DP * kFrag, r = sums + 16 * kFrag, u = r + 6 * kFrag, flags = u + 12 * kFrag, told = flags + 32,
+                              group = told + 2 * 4 * 16 * 4;
     static constexpr uint32_t bytes(int groups) { return groups_at + groups * group; }
 };
 
@@ -527,15 +525,16 @@ __device__ __forceinline__ int first_bad(u32x4 in_r, u32x4 in_u, uint32_t told, 
     return bad;
 }
 
-// Eight wavefronts take 16 columns of the state of one sequence and value head; NG such groups share a chunk's K in LDS.  Wavefronts
-// 0 to 3 carry the state: number pt makes the rows of tile pt = 2 p + t of K S and M R and holds the state's rows 32 dp .. 32 dp + 31 for
-// dp = pt, pt + 4.  Wavefronts 4 to 7 make the output's tiles, Q S and P U, beside them.  What one makes and others multiply with goes
-// through LDS, three barriers a chunk.  Operands from global memory (Q, M, P, K as rows) go to the registers of the wavefront that
-// multiplies with them, requested when it has used the chunk's before.
+// Eight wavefronts take 16 columns of the state of one sequence and value head; NG such groups share a chunk's K and Q in LDS.  Wavefronts
+// 0 to 3 carry the state: number pt holds its rows 32 dp .. 32 dp + 31 for dp = pt, pt + 4, multiplies all of K with them (the four
+// sums are added up where R is made: S itself would be three parts for each of them to read), and makes the rows of tile pt = 2 p + t of R and
+// U = M R.  Wavefronts 4 to 7 make the output's tiles, Q S and P U, a step behind, and fetch K and Q.  What one makes and others multiply
+// with goes through LDS, three barriers a chunk.  M and P go from memory to the registers of the wavefront that multiplies with them,
+// requested when it has used the chunk's before.
 // Lane (g = lane / 16, m = lane % 16) has column m; of a tile over tokens the four from 8 g + 4 t on, of 32 rows of the state 8 g .. 8 g + 7.
 // DP: 32s of dk.  VEC: rows of q and k in aligned 16-byte words.
 template <int VF, int DP, int NG, bool VEC>
-__global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
+__global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
     using T = typename Elem<VF>::T;
     using L = ScanLds<VF, DP>;
     using P = Parts<VF>;
@@ -572,11 +571,11 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
     };
     // Behind the last chunk its operands are requested again: what is in flight is known at every wait only if nothing is requested sometimes.
     auto next_of = [&](int c) { return min(c + 1, chunks - 1); };
-    auto region = [&](int c) { return group_at + (c & 1) * L::region; };
 
     if (!carries) {
         const uint32_t ldq = (uint32_t)(a.ldq * sizeof(T)), ldo = (uint32_t)(a.ldo * sizeof(T)), o_at = mine ? token * ldo + col * (uint32_t)sizeof(T) : kOutside;
-        Row8<VF, VEC> qr[each];
+        const uint32_t ldk = (uint32_t)(a.ldk * sizeof(T));
+        Row8<VF, VEC> qr[each], kr[each];
         Lower<VF, 2> pr[2];
         f32x4 eg;
         auto load_q = [&](int c) {                             // (tokens past the end: zeros)
@@ -584,26 +583,44 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
 #pragma unroll
             for (int i = 0; i < each; ++i) qr[i].load(qw, row * ldq, 32 * (dp0 + i) + element, DK);
         };
+        auto load_k = [&](int c) {
+            const window_t kw = window_of(a.k, a.ldk, (size_t)kh * DK, c, DK);
+#pragma unroll
+            for (int i = 0; i < each; ++i) kr[i].load(kw, row * ldk, 32 * (dp0 + i) + element, DK);
+        };
         auto put_q = [&]() {
 #pragma unroll
             for (int i = 0; i < each; ++i) qr[i].put(k_at + L::q_at + (pt * DP + dp0 + i) * L::frag, lane);
+        };
+        auto put_k = [&](int c) {
+#pragma unroll
+            for (int i = 0; i < each; ++i) kr[i].put(k_at + (c & 1) * L::k + (pt * DP + dp0 + i) * L::frag, lane);
         };
         auto load_p = [&](int c) {
             pr[0].load(block(c) + P::m_bytes, f0, lane);
             pr[1].load(block(c) + P::m_bytes, f1, lane);
         };
         if (chunks > 0) {
+            load_k(0);
             load_q(0);
+            put_k(0);
             put_q();
+            load_k(next_of(0));
+            in_order();
             eg = *(const f32x4 *)(decay(0) + token);
             in_order();
             load_q(next_of(0));
             in_order();
             load_p(0);
+            lds_barrier();                                     // the first K is there
         }
+        const uint32_t here = group_at + lane * 16;
         for (int c = 0; c < chunks; ++c) {
-            const uint32_t here = region(c) + lane * 16;
-            lds_barrier();                                     // S, K and Q are there
+            lds_barrier();                                     // K of the chunk before is done with
+            put_k(c + 1);
+            load_k(next_of(c + 1));
+            in_order();
+            lds_barrier();                                     // S and Q are there
             f32x4 o[3];
 #pragma unroll
             for (int n = 0; n < 3; ++n) o[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -623,11 +640,7 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
             out *= eg;
             asm volatile("" : "+v"(out) :: "memory");          // (here, so that the next chunk's factors can come into the same registers)
             eg = *(const f32x4 *)(decay(next_of(c)) + token);
-            lds_barrier();                                     // Q is done with
-            put_q();
-            load_q(next_of(c + 1));
-            in_order();
-            lds_barrier();                                     // U is there
+            lds_barrier();                                     // U is there, Q done with
             const u32x4 r0 = lds16(flags), u0 = lds16(flags + 16);
             f32x4 more[3];
 #pragma unroll
@@ -638,7 +651,7 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
                     u32x4 up[3], part[3];
                     pr[s].parts(part);
 #pragma unroll
-                    for (int n = 0; n < 3; ++n) up[n] = lds16(here + (2 * n + s) * kFrag);
+                    for (int n = 0; n < 3; ++n) up[n] = lds16(here + L::u + (2 * n + s) * kFrag);
                     part_pairs<P::out, 3, 2>([&](int i, int j) { more[j] = mfma16(part[i], up[j], more[j]); });
                 }
 #pragma unroll
@@ -647,12 +660,15 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
             const window_t ow = window_of(a.out, a.ldo, (size_t)h * DV, c, DV);
 #pragma unroll
             for (int r = 0; r < 4; ++r) window_store<T>(ow, o_at + r * ldo, (T)(token + r >= bad ? __builtin_nanf("") : a.scale * out[r]));
+            put_q();
+            load_q(next_of(c + 1));
+            in_order();
             load_p(next_of(c));
         }
         return;
     }
 
-    const uint32_t ldk = (uint32_t)(a.ldk * sizeof(T)), ldv = (uint32_t)(a.ldv * sizeof(T)), v_at = mine ? token * ldv + col * (uint32_t)sizeof(T) : kOutside;
+    const uint32_t ldv = (uint32_t)(a.ldv * sizeof(T)), v_at = mine ? token * ldv + col * (uint32_t)sizeof(T) : kOutside;
     const size_t state = (((size_t)(slot < 0 ? 0 : slot) * a.hv + h) * DK) * DV;
     const uint32_t state_bytes = (uint32_t)DK * (uint32_t)DV * 4;              // (below 2^31: dv at most 2^20)
     auto state_at = [&](int w, int t, int r) {
@@ -669,20 +685,10 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
 #pragma unroll
                 for (int r = 0; r < 4; ++r) S[w][t][r] = __uint_as_float(window_load<float>(from, state_at(w, t, r)));
     }
-    Row8<VF, VEC> kr[each];
     raw_t<T> v_0, v_1, v_2, v_3;                               // (an array of them would be packed, two to a register, as soon as they are loaded)
     Lower<VF, 3> mr[2];
     f32x4 eg, left;
     float keep;
-    auto load_k = [&](int c) {                                 // (tokens past the end: zeros)
-        const window_t kw = window_of(a.k, a.ldk, (size_t)kh * DK, c, DK);
-#pragma unroll
-        for (int i = 0; i < each; ++i) kr[i].load(kw, row * ldk, 32 * (dp0 + i) + element, DK);
-    };
-    auto put_k = [&](uint32_t at) {
-#pragma unroll
-        for (int i = 0; i < each; ++i) kr[i].put(at + (pt * DP + dp0 + i) * L::frag, lane);
-    };
     auto load_v = [&](int c) {
         const window_t vw = window_of(a.v, a.ldv, (size_t)h * DV, c, DV);
         v_0 = window_load<T>(vw, v_at);
@@ -696,59 +702,76 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
         mr[1].load(block(c), f1, lane);
         left = *(const f32x4 *)(decay(c) + 64 + token);
     };
-    auto share_state = [&](uint32_t at) {                      // the parts of the wavefront's rows of S
+    u32x4 Sp[own][3];                                          // the parts of the wavefront's rows of S
+    auto split_state = [&]() {
 #pragma unroll
-        for (int w = 0; w < own; ++w)
-            if (DP >= 4 || (int)pt < DP) {
-                float x[8];
-                u32x4 part[3];
+        for (int w = 0; w < own; ++w) {
+            float x[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = S[w][e & 1][e >> 1];
-                split<3, 8>(x, part);
+            for (int e = 0; e < 8; ++e) x[e] = S[w][e & 1][e >> 1];
+            split<3, 8>(x, Sp[w]);
+        }
+    };
+    const bool rows_mine = DP >= 4 || (int)pt < DP;
+    // K S over the wavefront's rows of S, for the chunk whose K is at `at`
+    auto share_sums = [&](uint32_t at) {
+        if (!rows_mine) return;                                // uniform
+        f32x4 ks[4];
 #pragma unroll
-                for (int n = 0; n < 3; ++n) to_lds(at + ((pt + 4 * w) * 3 + n) * kFrag + lane * 16, part[n]);
+        for (int n = 0; n < 4; ++n) ks[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < own; ++w) {
+            u32x4 part[4][P::in];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                Row8<VF, VEC> rows;
+                rows.get(at + (n * DP + pt + 4 * w) * L::frag, g, m);
+                row_parts<VF, VEC>(rows, part[n]);
             }
+            part_pairs<P::in, 3, 2>([&](int i, int j) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) ks[n] = mfma16(part[n][i], Sp[w][j], ks[n]);   // (four sums side by side: none waits for the one before)
+            });
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n) to_lds(group_at + L::sums + (n * 4 + pt) * kFrag + lane * 16, __builtin_bit_cast(u32x4, ks[n]));
     };
     // where a lane's four tokens go in an operand over tokens: half (pt & 1) of the place of lane (g, m) of the 32 tokens pt >> 1
     const uint32_t quad = (pt >> 1) * kFrag + lane * 16 + (pt & 1u) * 8;
 
     if (chunks > 0) {
-        load_k(0);
-        put_k(k_at);
         load_v(0);
         in_order();
         load_m(0);
         in_order();
-        load_k(next_of(0));
         keep = decay(0)[63];
-        share_state(group_at);
+        split_state();
+        lds_barrier();                                         // the first K is there
+        share_sums(k_at);
     }
     for (int c = 0; c < chunks; ++c) {
-        const uint32_t here = region(c), there = region(c + 1), k_here = k_at + (c & 1) * L::k, k_there = k_at + (~c & 1) * L::k;
-        lds_barrier();                                         // S, K and Q are there, and the chunk before is done with
-        f32x4 ks[3];
+        const uint32_t k_here = k_at + (c & 1) * L::k, k_there = k_at + (~c & 1) * L::k;
+        lds_barrier();                                         // K S is there
+        f32x4 ks[4];
 #pragma unroll
-        for (int n = 0; n < 3; ++n) ks[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int n = 0; n < (DP < 4 ? DP : 4); ++n) ks[n] = __builtin_bit_cast(f32x4, lds16(group_at + L::sums + (pt * 4 + n) * kFrag + lane * 16));
+        if (rows_mine)                                         // S for the output
 #pragma unroll
-        for (int dp = 0; dp < DP; ++dp) {
-            Row8<VF, VEC> rows;
-            u32x4 sp[3], part[P::in];
-            rows.get(k_here + (pt * DP + dp) * L::frag, g, m);
+            for (int w = 0; w < own; ++w)
 #pragma unroll
-            for (int n = 0; n < 3; ++n) sp[n] = lds16(here + (dp * 3 + n) * kFrag + lane * 16);
-            row_parts<VF, VEC>(rows, part);
-            part_pairs<P::in, 3, 2>([&](int i, int j) { ks[j] = mfma16(part[i], sp[j], ks[j]); });   // (a sum of each part: none waits for the one before)
-        }
+                for (int n = 0; n < 3; ++n) to_lds(group_at + ((pt + 4 * w) * 3 + n) * kFrag + lane * 16, Sp[w][n]);
+        if constexpr (DP < 4) ks[0] += ks[1];
+        else ks[0] = (ks[0] + ks[1]) + (ks[2] + ks[3]);
         float R[4];
         const raw_t<T> v[4] = {v_0, v_1, v_2, v_3};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) R[r] = fmaf(-eg[r], ks[0][r] + (ks[1][r] + ks[2][r]), (float)__builtin_bit_cast(T, v[r]));
+        for (int r = 0; r < 4; ++r) R[r] = fmaf(-eg[r], ks[0][r], (float)__builtin_bit_cast(T, v[r]));
         const bool bad_r = take_out(R, token, told + pt * 64, g, m);
         {
             u32x2 part[3];
             split<3, 4>(R, part);
 #pragma unroll
-            for (int n = 0; n < 3; ++n) to_lds(there + n * 2 * kFrag + quad, part[n]);
+            for (int n = 0; n < 3; ++n) to_lds(group_at + L::r + n * 2 * kFrag + quad, part[n]);
         }
         if (lane == 0) to_lds(flags + pt * 4, (uint32_t)bad_r);
         load_v(next_of(c));
@@ -756,14 +779,23 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
         f32x4 u[3];
 #pragma unroll
         for (int n = 0; n < 3; ++n) u[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        u32x4 rp[2][3], kt[own][2][2][P::in];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (s == 0 || pt >= 2)
+#pragma unroll
+                for (int n = 0; n < 3; ++n) rp[s][n] = lds16(group_at + L::r + (2 * n + s) * kFrag + lane * 16);
+#pragma unroll
+        for (int w = 0; w < own; ++w)                          // K^T waits for nobody
+            if (rows_mine)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) column_parts<VF, DP>(k_here, (int)pt + 4 * w, s, g, m, kt[w][s]);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
             if (s == 0 || pt >= 2) {
-                u32x4 rp[3], part[3];
+                u32x4 part[3];
                 mr[s].parts(part);
-#pragma unroll
-                for (int n = 0; n < 3; ++n) rp[n] = lds16(there + (2 * n + s) * kFrag + lane * 16);
-                part_pairs<3, 3, 2>([&](int i, int j) { u[i] = mfma16(part[i], rp[j], u[i]); });
+                part_pairs<3, 3, 2>([&](int i, int j) { u[i] = mfma16(part[i], rp[s][j], u[i]); });
             }
         float U[4];
 #pragma unroll
@@ -777,10 +809,10 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
             asm volatile("" : "+v"(l[0]), "+v"(l[1]), "+v"(l[2]), "+v"(l[3]) :: "memory");   // (as above)
             split<3, 4>(l, part);
 #pragma unroll
-            for (int n = 0; n < 3; ++n) to_lds(here + (3 + n) * 2 * kFrag + quad, part[n]);
+            for (int n = 0; n < 3; ++n) to_lds(group_at + L::u + (3 + n) * 2 * kFrag + quad, part[n]);
             split<3, 4>(U, part);
 #pragma unroll
-            for (int n = 0; n < 3; ++n) to_lds(here + n * 2 * kFrag + quad, part[n]);
+            for (int n = 0; n < 3; ++n) to_lds(group_at + L::u + n * 2 * kFrag + quad, part[n]);
         }
         if (lane == 0) to_lds(flags + 16 + pt * 4, (uint32_t)bad_u);
         load_m(next_of(c));
@@ -789,23 +821,21 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
         const u32x4 r0 = lds16(flags), u0 = lds16(flags + 16);
 #pragma unroll
         for (int w = 0; w < own; ++w)
-            if (DP >= 4 || (int)pt < DP) {
+            if (rows_mine) {
                 f32x4 more[2];                                 // (the second 32 tokens' sums: none waits for the one before)
                 more[0] = more[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
                 S[w][0] *= keep;
                 S[w][1] *= keep;
-                u32x4 lp[2][3], part[2][2][P::in];
+                u32x4 lp[2][3];
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    column_parts<VF, DP>(k_here, (int)pt + 4 * w, s, g, m, part[s]);
+                for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int n = 0; n < 3; ++n) lp[s][n] = lds16(here + ((3 + n) * 2 + s) * kFrag + lane * 16);
-                }
+                    for (int n = 0; n < 3; ++n) lp[s][n] = lds16(group_at + L::u + ((3 + n) * 2 + s) * kFrag + lane * 16);
                 part_pairs<P::in, 3, 2>([&](int i, int j) {
-                    S[w][0] = mfma16(part[0][0][i], lp[0][j], S[w][0]);
-                    S[w][1] = mfma16(part[0][1][i], lp[0][j], S[w][1]);
-                    more[0] = mfma16(part[1][0][i], lp[1][j], more[0]);
-                    more[1] = mfma16(part[1][1][i], lp[1][j], more[1]);
+                    S[w][0] = mfma16(kt[w][0][0][i], lp[0][j], S[w][0]);
+                    S[w][1] = mfma16(kt[w][0][1][i], lp[0][j], S[w][1]);
+                    more[0] = mfma16(kt[w][1][0][i], lp[1][j], more[0]);
+                    more[1] = mfma16(kt[w][1][1][i], lp[1][j], more[1]);
                 });
                 S[w][0] += more[0];
                 S[w][1] += more[1];
@@ -814,9 +844,8 @@ __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_F32 || DP == 8 ? 1 : 4) voi
 #pragma unroll
             for (int w = 0; w < own; ++w) S[w][0] = S[w][1] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
         }
-        share_state(there);                                    // (behind the last chunk nobody reads it)
-        put_k(k_there);
-        load_k(next_of(c + 1));
+        split_state();
+        share_sums(k_there);                                   // (behind the last chunk nobody reads it)
         keep = decay(next_of(c))[63];
     }
     if (!a.s_out || slot < 0) return;                          // uniform
@@ -853,7 +882,7 @@ static hipError_t launch_chunked(const DeltaDev &d, uint8_t *ws, int64_t numbers
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    constexpr int wide = 2;                                    // (the registers of more columns would not fit)
+    constexpr int wide = VF == CSB_VAL_F32 ? 1 : 2;            // (the registers, or LDS, of more columns would not fit)
     if (d.dk <= 64) return one ? launch_scan<VF, 2, 1, VEC>(d, ws, st) : launch_scan<VF, 2, wide, VEC>(d, ws, st);
     if (d.dk <= 128) return one ? launch_scan<VF, 4, 1, VEC>(d, ws, st) : launch_scan<VF, 4, wide, VEC>(d, ws, st);
     if constexpr (VF != CSB_VAL_F32) return launch_scan<VF, 8, 1, VEC>(d, ws, st);
