@@ -406,14 +406,14 @@ __device__ __forceinline__ void Row8<VF, VEC>::load(window_t from, uint32_t at, 
 // Requests to memory stay in the order written: the first chunk's have the order that the loop's have, so that a wait in the loop is for as many.
 __device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 
-// LDS of a workgroup: K of a chunk and of the next, Q, then per 16 columns the parts of S, the four wavefronts' parts of K S, R's parts, U's and
+// LDS of a workgroup: K of a chunk (NG = 2: and of the next), Q, then per 16 columns the parts of S, the four wavefronts' parts of K S, R's parts, U's and
 // e^(G_64 - G) U's, and what tells of numbers that are not finite.
-template <int VF, int DP> struct ScanLds {
+template <int VF, int DP, int NG> struct ScanLds {
     static constexpr uint32_t half = VF == CSB_VAL_F32 ? 2 : 1;               // 16-byte words of a lane's eight numbers of K
-    static constexpr uint32_t frag = half * kFrag, k = 4 * DP * frag, q_at = 2 * k, groups_at = 3 * k;
+    static constexpr uint32_t frag = half * kFrag, k = 4 * DP * frag, q_at = NG * k, groups_at = q_at + k;
     static constexpr uint32_t sums = 3 * DP * kFrag, r = sums + 16 * kFrag, u = r + 6 * kFrag, flags = u + 12 * kFrag, told = flags + 32,
                               group = told + 2 * 4 * 16 * 4;
-    static constexpr uint32_t bytes(int groups) { return groups_at + groups * group; }
+    static constexpr uint32_t bytes = groups_at + NG * group;
 };
 
 // The parts of an operand of K or Q from its numbers.
@@ -437,7 +437,7 @@ __device__ __forceinline__ void row_parts(const Row8<VF, VEC> &row, u32x4 *part)
 // The parts of K^T for elements 32 dp + 2 m + t (t = 0, 1: part[t]) of the tokens 32 ks + 8 g .. + 7.
 template <int VF, int DP>
 __device__ __forceinline__ void column_parts(uint32_t k_at, int dp, int ks, uint32_t g, uint32_t m, u32x4 part[2][Parts<VF>::in]) {
-    using L = ScanLds<VF, DP>;
+    using L = ScanLds<VF, DP, 1>;                              // (an operand's size)
     // row 4 g + c of a tile, c = 0 .. 3, elements from 8 (m / 4) on: place(m / 4, 4 g + c)
     const uint32_t word = m >> 2, low = 4 * g * 16;
     if constexpr (VF == CSB_VAL_F32) {
@@ -498,10 +498,10 @@ template <int VF, int N> struct Lower {
 // Takes numbers that are not finite out of a lane's four (tokens from `token` on) and says so: told[column] = the column's first
 // such token of the wavefront's, or kChunk.  Returns whether there were any.
 __device__ __forceinline__ bool take_out(float *x, int token, uint32_t told, uint32_t g, uint32_t m) {
-    float z = 0.0f;
+    bool any = false;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) z = fmaf(x[r], 0.0f, z);
-    if (__builtin_expect(__ballot(z != 0.0f) == 0, 1)) return false;          // (NaN is not 0 either)
+    for (int r = 0; r < 4; ++r) any |= __builtin_amdgcn_classf(x[r], 0x207);  // (infinite or NaN)
+    if (__builtin_expect(__ballot(any) == 0, 1)) return false;
     int first = kChunk;
 #pragma unroll
     for (int r = 3; r >= 0; --r)
@@ -536,7 +536,7 @@ __device__ __forceinline__ int first_bad(u32x4 in_r, u32x4 in_u, uint32_t told, 
 template <int VF, int DP, int NG, bool VEC>
 __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
     using T = typename Elem<VF>::T;
-    using L = ScanLds<VF, DP>;
+    using L = ScanLds<VF, DP, NG>;
     using P = Parts<VF>;
     constexpr int own = (DP + 3) / 4;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -594,7 +594,7 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
         };
         auto put_k = [&](int c) {
 #pragma unroll
-            for (int i = 0; i < each; ++i) kr[i].put(k_at + (c & 1) * L::k + (pt * DP + dp0 + i) * L::frag, lane);
+            for (int i = 0; i < each; ++i) kr[i].put(k_at + (c % NG) * L::k + (pt * DP + dp0 + i) * L::frag, lane);
         };
         auto load_p = [&](int c) {
             pr[0].load(block(c) + P::m_bytes, f0, lane);
@@ -602,25 +602,35 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
         };
         if (chunks > 0) {
             load_k(0);
-            load_q(0);
             put_k(0);
-            put_q();
-            load_k(next_of(0));
+            if (NG == 2) load_k(next_of(0));
+            in_order();
+            load_q(0);
+            in_order();
+            if (NG == 1) load_k(next_of(0));
             in_order();
             eg = *(const f32x4 *)(decay(0) + token);
-            in_order();
-            load_q(next_of(0));
             in_order();
             load_p(0);
             lds_barrier();                                     // the first K is there
         }
         const uint32_t here = group_at + lane * 16;
         for (int c = 0; c < chunks; ++c) {
-            lds_barrier();                                     // K of the chunk before is done with
-            put_k(c + 1);
-            load_k(next_of(c + 1));
+            lds_barrier();                                     // Q of the chunk before is done with (NG = 2: and its K)
+            if constexpr (NG == 2) {
+                put_k(c + 1);
+                load_k(next_of(c + 1));
+                in_order();
+            }
+            put_q();
+            load_q(next_of(c));
             in_order();
-            lds_barrier();                                     // S and Q are there
+            lds_barrier();                                     // S and Q are there (NG = 1: K is done with)
+            if constexpr (NG == 1) {
+                put_k(c + 1);
+                load_k(next_of(c + 1));
+                in_order();
+            }
             f32x4 o[3];
 #pragma unroll
             for (int n = 0; n < 3; ++n) o[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -660,9 +670,6 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
             const window_t ow = window_of(a.out, a.ldo, (size_t)h * DV, c, DV);
 #pragma unroll
             for (int r = 0; r < 4; ++r) window_store<T>(ow, o_at + r * ldo, (T)(token + r >= bad ? __builtin_nanf("") : a.scale * out[r]));
-            put_q();
-            load_q(next_of(c + 1));
-            in_order();
             load_p(next_of(c));
         }
         return;
@@ -736,6 +743,15 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
 #pragma unroll
         for (int n = 0; n < 4; ++n) to_lds(group_at + L::sums + (n * 4 + pt) * kFrag + lane * 16, __builtin_bit_cast(u32x4, ks[n]));
     };
+    // K^T for the state: waits for nobody; with one K it is read before the next one takes its place
+    u32x4 kt[own][2][2][P::in];
+    auto transpose_k = [&](uint32_t at) {
+        if (rows_mine)
+#pragma unroll
+            for (int w = 0; w < own; ++w)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) column_parts<VF, DP>(at, (int)pt + 4 * w, s, g, m, kt[w][s]);
+    };
     // where a lane's four tokens go in an operand over tokens: half (pt & 1) of the place of lane (g, m) of the 32 tokens pt >> 1
     const uint32_t quad = (pt >> 1) * kFrag + lane * 16 + (pt & 1u) * 8;
 
@@ -750,7 +766,7 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
         share_sums(k_at);
     }
     for (int c = 0; c < chunks; ++c) {
-        const uint32_t k_here = k_at + (c & 1) * L::k, k_there = k_at + (~c & 1) * L::k;
+        const uint32_t k_here = k_at + (c % NG) * L::k, k_there = k_at + ((c + 1) % NG) * L::k;
         lds_barrier();                                         // K S is there
         f32x4 ks[4];
 #pragma unroll
@@ -774,22 +790,18 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
             for (int n = 0; n < 3; ++n) to_lds(group_at + L::r + n * 2 * kFrag + quad, part[n]);
         }
         if (lane == 0) to_lds(flags + pt * 4, (uint32_t)bad_r);
+        if constexpr (NG == 1) transpose_k(k_here);
         load_v(next_of(c));
         lds_barrier();                                         // R is there
         f32x4 u[3];
 #pragma unroll
         for (int n = 0; n < 3; ++n) u[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        u32x4 rp[2][3], kt[own][2][2][P::in];
+        u32x4 rp[2][3];
 #pragma unroll
         for (int s = 0; s < 2; ++s)
             if (s == 0 || pt >= 2)
 #pragma unroll
                 for (int n = 0; n < 3; ++n) rp[s][n] = lds16(group_at + L::r + (2 * n + s) * kFrag + lane * 16);
-#pragma unroll
-        for (int w = 0; w < own; ++w)                          // K^T waits for nobody
-            if (rows_mine)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) column_parts<VF, DP>(k_here, (int)pt + 4 * w, s, g, m, kt[w][s]);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
             if (s == 0 || pt >= 2) {
@@ -815,6 +827,7 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
             for (int n = 0; n < 3; ++n) to_lds(group_at + L::u + n * 2 * kFrag + quad, part[n]);
         }
         if (lane == 0) to_lds(flags + 16 + pt * 4, (uint32_t)bad_u);
+        if constexpr (NG == 2) transpose_k(k_here);            // (before R, it would be in registers that there are not)
         load_m(next_of(c));
         in_order();
         lds_barrier();                                         // U is there
@@ -845,7 +858,7 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
             for (int w = 0; w < own; ++w) S[w][0] = S[w][1] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
         }
         split_state();
-        share_sums(k_there);                                   // (behind the last chunk nobody reads it)
+        share_sums(k_there);                                // (behind the last chunk nobody reads it)
         keep = decay(next_of(c))[63];
     }
     if (!a.s_out || slot < 0) return;                          // uniform
@@ -864,7 +877,7 @@ static size_t chunk_block(int32_t type) {
 
 template <int VF, int DP, int NG, bool VEC>
 static hipError_t launch_scan(const DeltaDev &d, uint8_t *ws, hipStream_t st) {
-    constexpr size_t lds = ScanLds<VF, DP>::bytes(NG);
+    constexpr size_t lds = ScanLds<VF, DP, NG>::bytes;
     static_assert(lds <= 160 * 1024, "LDS of a workgroup");
     const uint32_t tiles = (uint32_t)((d.dv + 16 * NG - 1) / (16 * NG)), pairs = (uint32_t)d.n_seq * (uint32_t)d.hv;
     const auto kern = delta_scan_kernel<VF, DP, NG, VEC>;
