@@ -491,12 +491,16 @@ __global__ __launch_bounds__(256, KS == 4 ? 2 : 5 - KS) void adapter_up_kernel(c
     }
 }
 
-// Requests of few columns (MANY; ranks up to 64, which the registers hold): parts of the grid that keep X in registers, k_wave = kStay, at most 64 of them; else at most 8
-// (the second launch reads what each leaves), k_wave a multiple of 32.
-static bool adapter_many(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank) { return batch < 8ll * n_seg && rank <= 64 && cols <= 64 * 4 * kStay; }
-static void adapter_split(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank, int32_t *splits, int32_t *k_wave) {
-    const int64_t tiles = (batch + kAdapterTile - 1) / kAdapterTile;
-    if (adapter_many(cols, batch, n_seg, rank)) *k_wave = kStay;
+// Requests of few columns take MANY (ranks up to 64, which the registers hold): k_wave = kStay, at most 64 splits.  Aligned operands below 64 columns a
+// request (64 requests of one column beside 4096 x 4096, rank 16: 17 us instead of 108; 2048 columns beside 8192 x 8192 in requests of 32 66
+// instead of 80, of 512 and rank 64 67 instead of 63); operands read element by element below 8 (300 columns of 665 in requests of 32: 18.5
+// instead of 16).  Else at most 8 splits (the second launch reads what each leaves), k_wave a multiple of 32.
+static bool adapter_many(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank, bool aligned) {
+    return batch < (aligned ? 64ll : 8ll) * n_seg && rank <= 64 && cols <= 64 * 4 * kStay;
+}
+static void adapter_split(int64_t cols, int32_t batch, bool many, int32_t *splits, int32_t *k_wave) {
+    const int64_t tiles = ((int64_t)batch + kAdapterTile - 1) / kAdapterTile;
+    if (many) *k_wave = kStay;
     else {
         const int64_t want = std::max<int64_t>(1, std::min<int64_t>(8, 512 / std::max<int64_t>(1, tiles)));
         *k_wave = (int32_t)std::max<int64_t>(32, ((cols + want * 4 - 1) / (want * 4) + 31) / 32 * 32);
@@ -533,9 +537,13 @@ static void launch_adapter(const AdapterDev &d, bool av, bool xv, bool bv, bool 
 
 extern "C" size_t csb_adapter_workspace_bytes(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank) {
     if (cols <= 0 || batch <= 0 || n_seg <= 0 || rank <= 0 || rank > csb::kAdapterMaxRank) return 0;
-    int32_t splits, k_wave;
-    csb::adapter_split(cols, batch, n_seg, rank, &splits, &k_wave);
-    return ((size_t)splits * (size_t)rank * (size_t)batch * sizeof(float) + 255) / 256 * 256;
+    int32_t most = 1;                                          // (which of the two a call takes goes by its pointers too)
+    for (const bool many : {false, csb::adapter_many(cols, batch, n_seg, rank, true)}) {
+        int32_t splits, k_wave;
+        csb::adapter_split(cols, batch, many, &splits, &k_wave);
+        most = std::max(most, splits);
+    }
+    return ((size_t)most * (size_t)rank * (size_t)batch * sizeof(float) + 255) / 256 * 256;
 }
 
 extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float *d_Y, int64_t ldy, int64_t rows,
@@ -561,8 +569,13 @@ extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float
     d.rank = d_rank; d.start = d_start; d.id = d_id; d.scale = d_scale;
     d.ldx = ldx; d.ldy = ldy; d.rows = rows; d.cols = cols;
     d.batch = batch; d.n_adapters = n_adapters; d.max_rank = rank; d.n_seg = n_seg;
-    adapter_split(cols, batch, n_seg, rank, &d.splits, &d.k_wave);
-    const bool many = adapter_many(cols, batch, n_seg, rank);
+    const uintptr_t per = type == CSB_VAL_F32 ? 4 : 8;         // elements of a 16-byte word
+    const bool av = cols % per == 0 && (uintptr_t)d_A % 16 == 0;
+    const bool xv = type == CSB_VAL_F32 || (ldx % 2 == 0 && (uintptr_t)d_X % 4 == 0);
+    const bool bv = rank % per == 0 && (uintptr_t)d_B % 16 == 0;
+    const bool yv = ldy % 2 == 0 && (uintptr_t)d_Y % 8 == 0;
+    const bool many = adapter_many(cols, batch, n_seg, rank, av && xv);
+    adapter_split(cols, batch, many, &d.splits, &d.k_wave);
     int64_t group = many ? 16 : 64;                            // rows of a workgroup: enough workgroups, and t read by few of them
     while (group < 2048 && tiles * ((rows + 2 * group - 1) / (2 * group)) >= 512) group *= 2;
     d.row_group = (int32_t)group;
@@ -576,15 +589,10 @@ extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float
     } catch (const std::bad_alloc &) {
         return fail(CSB_ENOMEM, "out of host memory");
     }
-    const uintptr_t per = type == CSB_VAL_F32 ? 4 : 8;         // elements of a 16-byte word
-    const bool av = cols % per == 0 && (uintptr_t)d_A % 16 == 0;
-    const bool xv = ldx % 2 == 0 && (uintptr_t)d_X % 4 == 0;
-    const bool bv = rank % per == 0 && (uintptr_t)d_B % 16 == 0;
-    const bool yv = ldy % 2 == 0 && (uintptr_t)d_Y % 8 == 0;
     const dim3 down((uint32_t)tiles, (uint32_t)d.splits, (uint32_t)deal), up((uint32_t)tiles, (uint32_t)row_groups);
     hipStream_t st = (hipStream_t)stream;
     switch (type) {
-        case CSB_VAL_F32: launch_adapter<CSB_VAL_F32>(d, av, true, bv, yv, many, down, up, st); break;
+        case CSB_VAL_F32: launch_adapter<CSB_VAL_F32>(d, av, xv, bv, yv, many, down, up, st); break;
         case CSB_VAL_F16: launch_adapter<CSB_VAL_F16>(d, av, xv, bv, yv, many, down, up, st); break;
         default: launch_adapter<CSB_VAL_BF16>(d, av, xv, bv, yv, many, down, up, st); break;
     }

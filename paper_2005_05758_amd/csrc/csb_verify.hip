@@ -6,7 +6,8 @@
 // whole units of 2^-38, so the sum of a row, the place of a random number in it and with it the token are the same however
 // the row is split over workgroups.
 //
-// Vocabularies up to kVerifySmall: one launch, a workgroup a request, the row in registers.  Larger ones: two launches, the
+// Vocabularies up to kVerifySmall: one launch, a workgroup a request (one request over 20011 tokens 7.6 us instead of 8.7, over 24000 8.4
+// instead of 8.7, over 32768 11.4 instead of 8.4; a call from the host saves a launch besides).  Larger ones: two launches, the
 // first adds up the units of the row in chunks, the second finds the chunk that the number falls into and the token in it.
 #include <algorithm>
 #include <new>
@@ -16,7 +17,7 @@
 namespace csb {
 
 constexpr float kUnits = 274877906944.0f;      // 2^38
-constexpr int kVerifyMaxChunks = 1024, kVerifyBlocks = 8, kVerifySmall = 16 * 256 * kVerifyBlocks;
+constexpr int kVerifyMaxChunks = 1024, kVerifyBlocks = 6, kVerifySmall = 16 * 256 * kVerifyBlocks;
 
 struct VerifyDev {
     const void *p, *q;
@@ -229,35 +230,50 @@ __global__ __launch_bounds__(1024) void verify_small_kernel(const VerifyDev a, c
     const int accepted = accepted_drafts<VF>(a, b, lane);
     const VerifyRow<VF> row(a, b, accepted);
     const int32_t first = wave * blocks * 256 + 4 * lane;
-    float w[kVerifyBlocks][2][4];
     if (tid == 0) token = -1;
-#pragma unroll
-    for (int i = 0; i < kVerifyBlocks; ++i) {                  // all loads in flight (four blocks at a time: 11.0 us instead of 8.7 at 20011 tokens)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[i][0][j] = w[i][1][j] = 0.0f;
-        if (i < blocks) row.at(first + 256 * i, a.vocab, w[i][0], w[i][1]);
-    }
-    double mine[2] = {0.0, 0.0};
-#pragma unroll
-    for (int i = 0; i < kVerifyBlocks; ++i)
-        if (i < blocks)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { mine[0] += small_units(w[i][0][j]); mine[1] += small_units(w[i][1][j]); }
-    mine[0] = wave_sum(mine[0]);
-    mine[1] = wave_sum(mine[1]);
-    if (lane == 0) { sums[0][wave] = mine[0]; sums[1][wave] = mine[1]; }
-    __syncthreads();
-    double all[2] = {0.0, 0.0}, before[2] = {0.0, 0.0};
+    // the wavefront's units, and all of the workgroup's and those before it
+    double mine, all, before;
+    auto share = [&](double units, double *sums) {
+        mine = wave_sum(units);
+        if (lane == 0) sums[wave] = mine;
+        __syncthreads();
+        all = before = 0.0;
 #pragma unroll 4
-    for (int v = 0; v < 16; ++v)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (v < wave) before[k] += sums[k][v];
-            all[k] += sums[k][v];
+        for (int v = 0; v < 16; ++v) {
+            if (v < wave) before += sums[v];
+            all += sums[v];
         }
-    const bool own = all[0] <= 0.0;                            // no weight left: p's own
-    const double limit = (double)units_before((int64_t)(own ? all[1] : all[0]), r), here = own ? mine[1] : mine[0];
-    double s = own ? before[1] : before[0];
+    };
+    {
+        float w[kVerifyBlocks][4], own[4];
+#pragma unroll
+        for (int i = 0; i < kVerifyBlocks; ++i) {              // all loads in flight (four blocks at a time: 11.0 us instead of 8.7 at 20011 tokens)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[i][j] = 0.0f;
+            if (i < blocks) row.at(first + 256 * i, a.vocab, w[i], own);
+        }
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < kVerifyBlocks; ++i)
+            if (i < blocks)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum += small_units(w[i][j]);
+        share(sum, sums[0]);
+    }
+    const bool own = all <= 0.0;                               // uniform: no weight left, so p's own
+    if (own) {
+        double sum = 0.0;
+#pragma unroll 1
+        for (int i = 0; i < blocks; ++i) {
+            float l[4], o[4];
+            row.at(first + 256 * i, a.vocab, l, o);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum += small_units(o[j]);
+        }
+        share(sum, sums[1]);
+    }
+    const double limit = (double)units_before((int64_t)all, r), here = mine;
+    double s = before;
     if (s <= limit && limit < s + here) {                      // one wavefront, if any weight is there
 #pragma unroll 1
         for (int i = 0; i < blocks; ++i) {                     // its blocks once more: they are near
