@@ -97,8 +97,8 @@ int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *stream);
  * What is not finite in a column of X changes that column of Y only.  Bitwise reproducible.
  * d_ws: csb_adapter_workspace_bytes(...) bytes.  Two launches.
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range,
- * n_seg != batch without d_start, an unknown type -> CSB_EINVAL; rank > 128, batch > 2^30, or more than
- * 2^24 workgroups -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.  batch = 0 or n_seg = 0 does nothing.
+ * n_seg != batch without d_start, an unknown type -> CSB_EINVAL; rank > 128, batch > 2^30, rows or cols above
+ * 2^31 - 1, or more than 2^24 workgroups -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.  batch = 0 or n_seg = 0 does nothing.
  */
 size_t csb_adapter_workspace_bytes(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank);
 int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float *d_Y, int64_t ldy, int64_t rows,

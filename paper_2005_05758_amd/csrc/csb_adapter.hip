@@ -267,8 +267,8 @@ __device__ __forceinline__ void three_parts(const float *x, uint16_t (*part)[E])
 
 // Y += B t for one tile and row_group rows.  t, its splits added up and scaled, goes through LDS into the operands of the matrix cores:
 // tile column h of lane i is column 2 i + h, so that a lane has two neighbouring columns of Y and 16 lanes a whole row of the tile.
-// 16-bit B: t as three bfloat16 parts (24 bits), a third of a pass each against eight for the binary32 form (69 us instead of REPLACED2 on 8192
-// rows x 2048 columns of rank 64); binary16 B as two.  binary32 B: the binary32 form.
+// 16-bit B: t as three bfloat16 parts (24 bits), a third of a pass each against eight for the binary32 form (69 us the launch instead of 51 on 8192 rows
+// x 2048 columns of rank 64); binary16 B as two.  binary32 B: the binary32 form.
 // Wavefronts share the rows where the tile has few adapters and the adapters where it has many (each column has one, so nothing is added up).
 // BV: rows of B in aligned words of 8 (binary32: 4) elements.  YV: pairs of Y in aligned 8-byte words.
 template <int VF, int KS, bool BV, bool YV>
@@ -555,7 +555,7 @@ extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float
     if (!known_type(type)) return fail(CSB_EINVAL, "unknown type");
     if (rows <= 0 || cols <= 0 || batch < 0 || n_seg < 0 || n_adapters < 1 || rank < 1) return fail(CSB_EINVAL, "bad size");
     if (rank > kAdapterMaxRank) return fail(CSB_EUNSUPPORTED, "rank above 128 (a tile's sums are held in registers)");
-    if (batch > 1 << 30) return fail(CSB_EUNSUPPORTED, "more than 2^30 columns of X");
+    if (batch > 1 << 30 || rows > 0x7fffffff || cols > 0x7fffffff) return fail(CSB_EUNSUPPORTED, "more than 2^30 columns of X, or 2^31 - 1 rows or columns of a projection");
     if (ldx < batch || ldy < batch) return fail(CSB_EINVAL, "a leading dimension below batch");
     if (!d_start && n_seg != batch) return fail(CSB_EINVAL, "n_seg is not batch (and there are no offsets)");
     if (batch == 0 || n_seg == 0) return CSB_OK;
