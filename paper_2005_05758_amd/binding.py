@@ -4,6 +4,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+import sys
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -244,7 +245,7 @@ def project(W, br: int, bc: int, rate: float, out=None, stream=None):
 
 def _val_type(dtype) -> int:
     """CSB_VAL_* of a torch dtype."""
-    import torch
+    torch = sys.modules["torch"]
     if dtype is torch.bfloat16:
         return VAL_BF16
     if dtype is torch.float16:
@@ -262,19 +263,29 @@ def _scratch(nbytes: int, device):
 _DELTA_ARGS = struct.Struct("@6iq3P3q2P2q5PifPq")             # csb_delta_args, as ctypes lays it out
 
 
+def _raw_stream(stream) -> Optional[int]:
+    """_stream_ptr for callers that hold device tensors: the runtime is initialised, which current_device() would check."""
+    if stream is not None:
+        return stream.cuda_stream or None
+    c = sys.modules["torch"]._C
+    return c._cuda_getCurrentRawStream(c._cuda_getDevice()) or None
+
+
 def _delta_rows(t, n, w, tokens):
     """Elements from one token to the next of [tokens, n, w]: (t, head, j) at t * ld + head * w + j."""
+    if t.is_contiguous() and t.is_cuda:
+        return n * w
     ld, head, one = t.stride()
     assert t.is_cuda and (one == 1 or w == 1) and (head == w or n == 1), "heads of a token must be contiguous"
     return ld if tokens > 1 else max(ld, n * w)
 
 
 def _delta(chunked, q, k, v, g, beta, scale, starts, lens, state, slots, state_out, out, stream):
-    import torch
-    T, HK, DK = q.shape
+    torch = sys.modules["torch"]
+    T, HK, DK = shape = q.shape
     Tv, HV, DV = v.shape
     f32, typ = torch.float32, v.dtype
-    assert T == Tv and k.shape == q.shape and g.shape == beta.shape == (T, HV)
+    assert T == Tv and k.shape == shape and g.shape == beta.shape == (T, HV)
     assert q.dtype is k.dtype is typ and g.dtype is beta.dtype is f32
     if out is None:
         out = torch.empty((T, HV, DV), dtype=typ, device=v.device)
@@ -307,9 +318,9 @@ def _delta(chunked, q, k, v, g, beta, scale, starts, lens, state, slots, state_o
     raw = _DELTA_ARGS.pack(*args)
     if chunked:
         ws = _scratch(_raw_delta["workspace"](raw), v.device)
-        rc = _raw_delta["chunked"](raw, ws.data_ptr() if ws is not None else None, _stream_ptr(stream))
+        rc = _raw_delta["chunked"](raw, ws.data_ptr() if ws is not None else None, _raw_stream(stream))
     else:
-        rc = _raw_delta["recurrent"](raw, _stream_ptr(stream))
+        rc = _raw_delta["recurrent"](raw, _raw_stream(stream))
     if rc:
         _check(rc)
     return out
@@ -338,7 +349,7 @@ def adapter_add(Y, X, A, B, ids, starts=None, scales=None, ranks=None, stream=No
     rank, cols] and B [adapters, rows, rank] of one dtype (float32, float16, bfloat16), Y [rows, batch] float32 (rows of X and Y may be
     strided).  ids [requests] int32: the adapter of each request, -1 for none; starts [requests + 1] int32: its columns (None: one
     each).  scales [adapters] float32, ranks [adapters] int32: factor and used ranks of an adapter.  Returns Y."""
-    import torch
+    torch = sys.modules["torch"]
     cols, batch = X.shape
     n, rank, A_cols = A.shape
     rows, Y_batch = Y.shape
@@ -353,7 +364,7 @@ def adapter_add(Y, X, A, B, ids, starts=None, scales=None, ranks=None, stream=No
     ws = torch.empty(max(L.csb_adapter_workspace_bytes(cols, batch, segs, rank), 256), dtype=torch.uint8, device=X.device)
     rc = L.csb_adapter_add(_val_type(typ), X.data_ptr(), max(ldx, batch), Y.data_ptr(), max(ldy, batch), rows, cols, batch, _dptr(A), _dptr(B),
                            n, rank, _dptr(ranks, i32), _dptr(scales, f32), segs, _dptr(starts, i32), _dptr(ids, i32), ws.data_ptr(),
-                           _stream_ptr(stream))
+                           _raw_stream(stream))
     if rc:
         _check(rc)
     return Y
@@ -364,7 +375,7 @@ def verify_drafts(p, q, drafts, u, r, counts=None, stream=None):
     of the mass on the drafted token) of one dtype (float32, float16, bfloat16); drafts [requests, n] int32, u [requests, n] and r [requests]
     float32 numbers in [0, 1); counts [requests] int32: drafts that a request brings (None: n).  Returns (tokens
     [requests, n + 1] int32: the accepted drafts, the token drawn behind them, -1; accepted [requests] int32)."""
-    import torch
+    torch = sys.modules["torch"]
     N, K1, V = p.shape
     K = K1 - 1
     i32, f32, typ, dev = torch.int32, torch.float32, p.dtype, p.device
@@ -386,7 +397,7 @@ def verify_drafts(p, q, drafts, u, r, counts=None, stream=None):
     L = lib()
     ws = torch.empty(max(L.csb_verify_workspace_bytes(N, V), 256), dtype=torch.uint8, device=dev)
     rc = L.csb_verify_drafts(_val_type(typ), p.data_ptr(), rows(p, K1), q.data_ptr() if ldq else None, ldq, _dptr(drafts, i32), _dptr(u, f32),
-                             _dptr(r, f32), _dptr(counts, i32), N, K, V, tokens.data_ptr(), accepted.data_ptr(), ws.data_ptr(), _stream_ptr(stream))
+                             _dptr(r, f32), _dptr(counts, i32), N, K, V, tokens.data_ptr(), accepted.data_ptr(), ws.data_ptr(), _raw_stream(stream))
     if rc:
         _check(rc)
     return tokens, accepted
