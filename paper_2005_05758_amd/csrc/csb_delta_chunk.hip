@@ -406,11 +406,11 @@ __device__ __forceinline__ void Row8<VF, VEC>::load(window_t from, uint32_t at, 
 // Requests to memory stay in the order written: the first chunk's have the order that the loop's have, so that a wait in the loop is for as many.
 __device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 
-// LDS of a workgroup: K of a chunk (NG = 2: and of the next), Q, then per 16 columns the parts of S, the four wavefronts' parts of K S, R's parts, U's and
+// LDS of a workgroup: K of a chunk (NG = 2: and of the next), Q, e^G_i and e^(G_64 - G_i) of a chunk and of the next, then per 16 columns the parts of S, the four wavefronts' parts of K S, R's parts, U's and
 // e^(G_64 - G) U's, and what tells of numbers that are not finite.
 template <int VF, int DP, int NG> struct ScanLds {
     static constexpr uint32_t half = VF == CSB_VAL_F32 ? 2 : 1;               // 16-byte words of a lane's eight numbers of K
-    static constexpr uint32_t frag = half * kFrag, k = 4 * DP * frag, q_at = NG * k, groups_at = q_at + k;
+    static constexpr uint32_t frag = half * kFrag, k = 4 * DP * frag, q_at = NG * k, decay = q_at + k, groups_at = decay + 1024;
     static constexpr uint32_t sums = 3 * DP * kFrag, r = sums + 16 * kFrag, u = r + 6 * kFrag, flags = u + 12 * kFrag, told = flags + 32,
                               group = told + 2 * 4 * 16 * 4;
     static constexpr uint32_t bytes = groups_at + NG * group;
@@ -577,7 +577,10 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
         const uint32_t ldk = (uint32_t)(a.ldk * sizeof(T));
         Row8<VF, VEC> qr[each], kr[each];
         Lower<VF, 2> pr[2];
-        f32x4 eg;
+        const bool puts_decay = wave == 4;                     // (one wavefront's: 32 lanes hold a chunk's 128 numbers)
+        f32x4 dk;
+        auto load_decay = [&](int c) { if (puts_decay && lane < 32) dk = *(const f32x4 *)(decay(c) + 4 * lane); };
+        auto put_decay = [&](int c) { if (puts_decay && lane < 32) to_lds(k_at + L::decay + (c & 1) * 512 + lane * 16, __builtin_bit_cast(u32x4, dk)); };
         auto load_q = [&](int c) {                             // (tokens past the end: zeros)
             const window_t qw = window_of(a.q, a.ldq, (size_t)kh * DK, c, DK);
 #pragma unroll
@@ -601,7 +604,9 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
             pr[1].load(block(c) + P::m_bytes, f1, lane);
         };
         if (chunks > 0) {
+            load_decay(0);
             load_k(0);
+            put_decay(0);
             put_k(0);
             if (NG == 2) load_k(next_of(0));
             in_order();
@@ -609,7 +614,7 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
             in_order();
             if (NG == 1) load_k(next_of(0));
             in_order();
-            eg = *(const f32x4 *)(decay(0) + token);
+            load_decay(next_of(0));
             in_order();
             load_p(0);
             lds_barrier();                                     // the first K is there
@@ -631,6 +636,10 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
                 load_k(next_of(c + 1));
                 in_order();
             }
+            put_decay(c + 1);
+            load_decay(next_of(c + 1));
+            in_order();
+            const f32x4 eg = __builtin_bit_cast(f32x4, lds16(k_at + L::decay + (c & 1) * 512 + token * 4));
             f32x4 o[3];
 #pragma unroll
             for (int n = 0; n < 3; ++n) o[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -648,8 +657,6 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
 #pragma unroll
             for (int n = 1; n < 3; ++n) out += o[n];
             out *= eg;
-            asm volatile("" : "+v"(out) :: "memory");          // (here, so that the next chunk's factors can come into the same registers)
-            eg = *(const f32x4 *)(decay(next_of(c)) + token);
             lds_barrier();                                     // U is there, Q done with
             const u32x4 r0 = lds16(flags), u0 = lds16(flags + 16);
             f32x4 more[3];
@@ -694,20 +701,16 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
     }
     raw_t<T> v_0, v_1, v_2, v_3;                               // (an array of them would be packed, two to a register, as soon as they are loaded)
     Lower<VF, 3> mr[2];
-    f32x4 eg, left;
-    float keep;
     auto load_v = [&](int c) {
         const window_t vw = window_of(a.v, a.ldv, (size_t)h * DV, c, DV);
         v_0 = window_load<T>(vw, v_at);
         v_1 = window_load<T>(vw, v_at + ldv);
         v_2 = window_load<T>(vw, v_at + 2 * ldv);
         v_3 = window_load<T>(vw, v_at + 3 * ldv);
-        eg = *(const f32x4 *)(decay(c) + token);
     };
     auto load_m = [&](int c) {
         mr[0].load(block(c), f0, lane);
         mr[1].load(block(c), f1, lane);
-        left = *(const f32x4 *)(decay(c) + 64 + token);
     };
     u32x4 Sp[own][3];                                          // the parts of the wavefront's rows of S
     auto split_state = [&]() {
@@ -760,14 +763,15 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
         in_order();
         load_m(0);
         in_order();
-        keep = decay(0)[63];
         split_state();
         lds_barrier();                                         // the first K is there
         share_sums(k_at);
     }
     for (int c = 0; c < chunks; ++c) {
         const uint32_t k_here = k_at + (c % NG) * L::k, k_there = k_at + ((c + 1) % NG) * L::k;
+        const uint32_t decays = k_at + L::decay + (c & 1) * 512;
         lds_barrier();                                         // K S is there
+        const f32x4 eg = __builtin_bit_cast(f32x4, lds16(decays + token * 4));
         f32x4 ks[4];
 #pragma unroll
         for (int n = 0; n < (DP < 4 ? DP : 4); ++n) ks[n] = __builtin_bit_cast(f32x4, lds16(group_at + L::sums + (pt * 4 + n) * kFrag + lane * 16));
@@ -796,6 +800,7 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
         f32x4 u[3];
 #pragma unroll
         for (int n = 0; n < 3; ++n) u[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        const f32x4 left = __builtin_bit_cast(f32x4, lds16(decays + 256 + token * 4));
         u32x4 rp[2][3];
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -818,7 +823,6 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
             float l[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) l[r] = U[r] * left[r];
-            asm volatile("" : "+v"(l[0]), "+v"(l[1]), "+v"(l[2]), "+v"(l[3]) :: "memory");   // (as above)
             split<3, 4>(l, part);
 #pragma unroll
             for (int n = 0; n < 3; ++n) to_lds(group_at + L::u + (3 + n) * 2 * kFrag + quad, part[n]);
@@ -832,6 +836,7 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
         in_order();
         lds_barrier();                                         // U is there
         const u32x4 r0 = lds16(flags), u0 = lds16(flags + 16);
+        const float keep = __uint_as_float(lds4(decays + 63 * 4));
 #pragma unroll
         for (int w = 0; w < own; ++w)
             if (rows_mine) {
@@ -859,7 +864,6 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
         }
         split_state();
         share_sums(k_there);                                // (behind the last chunk nobody reads it)
-        keep = decay(next_of(c))[63];
     }
     if (!a.s_out || slot < 0) return;                          // uniform
     const window_t to = window(a.s_out + state, state_bytes);
@@ -888,19 +892,20 @@ static hipError_t launch_scan(const DeltaDev &d, uint8_t *ws, hipStream_t st) {
 }
 
 template <int VF, bool VEC>
-static hipError_t launch_chunked(const DeltaDev &d, uint8_t *ws, int64_t numbers, bool one, hipStream_t st) {
+static hipError_t launch_chunked(const DeltaDev &d, uint8_t *ws, int64_t numbers, bool few, hipStream_t st) {
     const uint32_t head_groups = (uint32_t)(d.hv + 3) / 4;
     if (d.n_tokens > 0) {
         hipLaunchKernelGGL((delta_prepare_kernel<VF, VEC>), dim3((uint32_t)numbers * head_groups), dim3(256), 0, st, d, ws, head_groups);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    // 32 columns a workgroup instead of 16 where CUs have enough of them: K and Q are fetched once for both (16411 bfloat16 tokens, 8 heads of
-    // 128 x 128: 184 us instead of 212).  Rows of 64 gain nothing by it (118 against 121; binary16 156 against 141), wider or binary32 ones have not the LDS.
+    // 16 columns a workgroup, of which a CU takes two with bfloat16 rows of up to 128 (16411 tokens, 8 heads of 128 x 128: 176 us; 32 columns 181).
+    // binary16 has one part of K and Q more and the registers for one only: 32 columns a workgroup where CUs have enough of them (236 us against
+    // 268).  Rows of 64 gain nothing by that (156 against 141), wider ones have not the LDS.
     if (d.dk <= 64) return launch_scan<VF, 2, 1, VEC>(d, ws, st);
     if (d.dk <= 128) {
-        if constexpr (VF != CSB_VAL_F32)
-            if (!one) return launch_scan<VF, 4, 2, VEC>(d, ws, st);
+        if constexpr (VF == CSB_VAL_F16)
+            if (!few) return launch_scan<VF, 4, 2, VEC>(d, ws, st);
         return launch_scan<VF, 4, 1, VEC>(d, ws, st);
     }
     if constexpr (VF != CSB_VAL_F32) return launch_scan<VF, 8, 1, VEC>(d, ws, st);
@@ -943,14 +948,14 @@ extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *s
     const DeltaDev d = delta_dev(args);
     const int64_t word = 16 / type_size(args->type);           // elements of an aligned 16-byte word
     const bool vec = args->dk % 8 == 0 && args->ldq % word == 0 && args->ldk % word == 0 && ((uintptr_t)args->d_q | (uintptr_t)args->d_k) % 16 == 0;
-    const bool one = pairs * wide < 256;                       // more of them, smaller, while CUs are idle
+    const bool few = pairs * wide < 256;                       // CUs idle with workgroups of more columns
     hipStream_t st = (hipStream_t)stream;
     uint8_t *ws = (uint8_t *)d_ws;
     hipError_t e;
     switch (args->type) {
-        case CSB_VAL_F32: e = vec ? launch_chunked<CSB_VAL_F32, true>(d, ws, numbers, one, st) : launch_chunked<CSB_VAL_F32, false>(d, ws, numbers, one, st); break;
-        case CSB_VAL_F16: e = vec ? launch_chunked<CSB_VAL_F16, true>(d, ws, numbers, one, st) : launch_chunked<CSB_VAL_F16, false>(d, ws, numbers, one, st); break;
-        default: e = vec ? launch_chunked<CSB_VAL_BF16, true>(d, ws, numbers, one, st) : launch_chunked<CSB_VAL_BF16, false>(d, ws, numbers, one, st); break;
+        case CSB_VAL_F32: e = vec ? launch_chunked<CSB_VAL_F32, true>(d, ws, numbers, few, st) : launch_chunked<CSB_VAL_F32, false>(d, ws, numbers, few, st); break;
+        case CSB_VAL_F16: e = vec ? launch_chunked<CSB_VAL_F16, true>(d, ws, numbers, few, st) : launch_chunked<CSB_VAL_F16, false>(d, ws, numbers, few, st); break;
+        default: e = vec ? launch_chunked<CSB_VAL_BF16, true>(d, ws, numbers, few, st) : launch_chunked<CSB_VAL_BF16, false>(d, ws, numbers, few, st); break;
     }
     if (e != hipSuccess) { set_error(std::string("csb_delta_chunked: ") + hipGetErrorString(e)); return CSB_EDEVICE; }
     return CSB_OK;
