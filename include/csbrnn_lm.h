@@ -69,14 +69,18 @@ typedef struct {
  * the few tokens of a decoding step; right for any length.  Bitwise reproducible.
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, heads_v
  * no multiple of heads_k, n_tokens no multiple of n_seq without d_start, an unknown type ->
- * CSB_EINVAL; dk > 256, or more than 2^24 parts of 32 columns -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.
+ * CSB_EINVAL; dk > 256, or more workgroups than a launch takes (n_seq heads_v dv of 2^27
+ * and more) -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.
  * n_seq = 0 does nothing.
  */
 int csb_delta_recurrent(const csb_delta_args *args, void *stream);
 
 /*
- * The same rule, the same arguments and errors, chunk by chunk: for prompts.  Leading dimensions of 2^23 or more
- * or dv above 2^20 -> CSB_EUNSUPPORTED.  (Before a capture into a graph call it once: a kernel's first launch raises its LDS limit.)
+ * The same rule, the same arguments and errors, chunk by chunk: for prompts.  Leading
+ * dimensions of 2^23 or more, dv above 2^20 or n_seq heads_v dv of 2^26 and more -> CSB_EUNSUPPORTED.
+ * Faster than token by token from 16 to 32 tokens a sequence on; binary32 rows of dk above 128 are
+ * taken token by token here too (they do not fit the LDS beside the rest).  Before a capture into a
+ * graph call it once: a kernel's first launch raises its LDS limit.
  * d_ws: csb_delta_workspace_bytes(args) bytes (only the sizes of `args` are read; 0 for arguments
  * that the call refuses).
  */
@@ -98,7 +102,8 @@ int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *stream);
  * d_ws: csb_adapter_workspace_bytes(...) bytes.  Two launches.
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range,
  * n_seg != batch without d_start, an unknown type -> CSB_EINVAL; rank > 128, batch > 2^30, rows or cols above
- * 2^31 - 1, or more than 2^24 workgroups -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.  batch = 0 or n_seg = 0 does nothing.
+ * 2^31 - 1, or more workgroups than a launch takes -> CSB_EUNSUPPORTED; launch failure ->
+ * CSB_EDEVICE.  batch = 0 or n_seg = 0 does nothing.
  */
 size_t csb_adapter_workspace_bytes(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank);
 int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float *d_Y, int64_t ldy, int64_t rows,
@@ -123,8 +128,8 @@ int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float *d_Y, int6
  * d_tokens [n_req][n_draft + 1] receives the accepted drafts, the drawn token and -1 behind it;
  * d_accepted [n_req] the number of accepted drafts.  d_ws: csb_verify_workspace_bytes(...) bytes.
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, an
- * unknown type -> CSB_EINVAL; vocab > 2^24, or more than 2^24 workgroups -> CSB_EUNSUPPORTED; launch failure ->
- * CSB_EDEVICE.  n_req = 0 does nothing; n_draft = 0 samples (d_q, d_draft and d_u may be NULL then).
+ * unknown type -> CSB_EINVAL; vocab > 2^24, n_req > 2^21, or more workgroups than a launch takes ->
+ * CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.  n_req = 0 does nothing; n_draft = 0 samples (d_q, d_draft and d_u may be NULL then).
  */
 size_t csb_verify_workspace_bytes(int32_t n_req, int32_t vocab);
 int csb_verify_drafts(int32_t type, const void *d_p, int64_t ldp, const void *d_q, int64_t ldq,

@@ -267,8 +267,8 @@ __device__ __forceinline__ void three_parts(const float *x, uint16_t (*part)[E])
 
 // Y += B t for one tile and row_group rows.  t, its splits added up and scaled, goes through LDS into the operands of the matrix cores:
 // tile column h of lane i is column 2 i + h, so that a lane has two neighbouring columns of Y and 16 lanes a whole row of the tile.
-// 16-bit B: t as three bfloat16 parts (24 bits), a third of a pass each against eight for the binary32 form (69 us the launch instead of 51 on 8192 rows
-// x 2048 columns of rank 64); binary16 B as two.  binary32 B: the binary32 form.
+// 16-bit B: t as three bfloat16 parts (24 bits), 3 / 16 of the time of the binary32 form; binary16 B as two.  binary32 B: the binary32 form.
+// 8192 rows x 2048 columns of rank 64: 47 us, 2.6 TB/s; bound by the latency of Y's rows, of which 12 wavefronts a CU have 24 KB in flight.
 // Wavefronts share the rows where the tile has few adapters and the adapters where it has many (each column has one, so nothing is added up).
 // BV: rows of B in aligned words of 8 (binary32: 4) elements.  YV: pairs of Y in aligned 8-byte words.
 template <int VF, int KS, bool BV, bool YV>
@@ -578,11 +578,12 @@ extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float
     adapter_split(cols, batch, many, &d.splits, &d.k_wave);
     int64_t group = many ? 16 : 64;                            // rows of a workgroup: enough workgroups, and t read by few of them
     while (group < 2048 && tiles * ((rows + 2 * group - 1) / (2 * group)) >= 512) group *= 2;
+    while ((rows + group - 1) / group > 65535) group *= 2;     // (a launch's second dimension)
     d.row_group = (int32_t)group;
     const int64_t row_groups = (rows + group - 1) / group;
     // adapters of a tile over several workgroups while CUs are idle
     const int64_t deal = many ? std::max<int64_t>(1, std::min<int64_t>(8, 512 / (tiles * d.splits))) : 1;
-    if (tiles * std::max<int64_t>(row_groups, deal * d.splits) > kMaxWorkgroups || row_groups > 65535) return fail(CSB_EUNSUPPORTED, "more than 2^24 workgroups");
+    if (tiles * std::max<int64_t>(row_groups, deal * d.splits) > kMaxWorkgroups) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
     try {
         static const char adapter_user = 0;                    // this entry point as a user of workspaces
         workspace_changed_hands(d_ws, &adapter_user);

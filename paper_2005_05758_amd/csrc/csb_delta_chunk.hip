@@ -105,7 +105,9 @@ __device__ __forceinline__ void to_lds(uint32_t at, u32x2 v) { *(__attribute__((
 __device__ __forceinline__ void to_lds(uint32_t at, uint32_t v) { *(__attribute__((address_space(3))) uint32_t *)(uintptr_t)at = v; }
 
 // ---- first launch: M and P -----------------------------------------------------------------------
-// A wavefront takes one chunk of one value head.
+// A wavefront takes one chunk of one value head.  Bound by its own latency where chunks are few (12.5 us for 64 tokens or for 16 short
+// prompts: loads, the products, then the inverse's dependent steps), by loads and LDS where they are many (512 chunks of 16 heads, 128
+// elements each: 91 us; 280 chunks of 48 prompts and 16 heads: 72 us).
 
 // Eight numbers of a row of q or k from element d on, as they are stored (zeros past dk).
 template <int VF, bool VEC> struct Row8 {
@@ -406,8 +408,9 @@ __device__ __forceinline__ void Row8<VF, VEC>::load(window_t from, uint32_t at, 
 // Requests to memory stay in the order written: the first chunk's have the order that the loop's have, so that a wait in the loop is for as many.
 __device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 
-// LDS of a workgroup: K of a chunk (NG = 2: and of the next), Q, e^G_i and e^(G_64 - G_i) of a chunk and of the next, then per 16 columns the parts of S, the four wavefronts' parts of K S, R's parts, U's and
-// e^(G_64 - G) U's, and what tells of numbers that are not finite.
+// LDS of a workgroup: K of a chunk (NG = 2: and of the next), Q, e^G_i and e^(G_64 - G_i) of a chunk and of the next, then per 16
+// columns the parts of S, the four wavefronts' sums of K S, R's parts, U's and e^(G_64 - G) U's, and what tells of numbers that
+// are not finite.
 template <int VF, int DP, int NG> struct ScanLds {
     static constexpr uint32_t half = VF == CSB_VAL_F32 ? 2 : 1;               // 16-byte words of a lane's eight numbers of K
     static constexpr uint32_t frag = half * kFrag, k = 4 * DP * frag, q_at = NG * k, decay = q_at + k, groups_at = decay + 1024;
@@ -533,6 +536,11 @@ __device__ __forceinline__ int first_bad(u32x4 in_r, u32x4 in_u, uint32_t told, 
 // requested when it has used the chunk's before.
 // Lane (g = lane / 16, m = lane % 16) has column m; of a tile over tokens the four from 8 g + 4 t on, of 32 rows of the state 8 g .. 8 g + 7.
 // DP: 32s of dk.  VEC: rows of q and k in aligned 16-byte words.
+// Bound by what follows on what: K S, R, U and the state wait for each other chunk after chunk, three times through LDS.  32768 tokens
+// of one sequence, 16 heads of 128 x 128: 512 chunks of 1.7 us (3830 clocks) each, 885 us; 48 prompts, 16411 tokens, 16 heads: 260 us, there by
+// the issue of the products and by LDS, with two workgroups a CU.  A sequence's chunks are not split over workgroups: a part would need its
+// product of the chunks' matrices besides, dk columns more beside the state's dv, and a second pass, three times the work, and a full card does
+// 1.9 times the chunks a second that this one sequence does.
 template <int VF, int DP, int NG, bool VEC>
 __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
     using T = typename Elem<VF>::T;
@@ -933,8 +941,8 @@ extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *s
     if (args->dv > 1 << 20) return fail(CSB_EUNSUPPORTED, "dv above 2^20");
     const int64_t numbers = tile_numbers(args->n_tokens, args->n_seq, kChunkShift);
     const int64_t pairs = ((int64_t)args->n_seq * args->heads_v + 7) / 8 * 8, wide = ((int64_t)args->dv + 63) / 64, narrow = ((int64_t)args->dv + 15) / 16;
-    if (pairs > kMaxWorkgroups || pairs * narrow > kMaxWorkgroups || numbers * ((args->heads_v + 3) / 4) > kMaxWorkgroups)
-        return fail(CSB_EUNSUPPORTED, "more than 2^24 workgroups");
+    if (pairs > kMaxWorkgroups || pairs * narrow > kMaxWorkgroups / 4 || numbers * ((args->heads_v + 3) / 4) > kMaxWorkgroups)
+        return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
     if (d_ws) {
         try {
             static const char delta_user = 0;                  // this entry point as a user of workspaces

@@ -8,7 +8,8 @@
 //
 // Vocabularies up to kVerifySmall: one launch, a workgroup a request (one request over 20011 tokens 7.6 us instead of 8.7, over 24000 8.4
 // instead of 8.7, over 32768 11.4 instead of 8.4; a call from the host saves a launch besides).  Larger ones: two launches, the
-// first adds up the units of the row in chunks, the second finds the chunk that the number falls into and the token in it.
+// first adds up the units of the row in chunks, the second finds the chunk that the number falls into and the token in it
+// (64 requests over 131072 tokens, 67 MB: 17 us, 3.9 TB/s, and 4.7).
 #include <algorithm>
 #include <new>
 
@@ -354,7 +355,7 @@ extern "C" int csb_verify_drafts(int32_t type, const void *d_p, int64_t ldp, con
     d.ldp = ldp; d.ldq = ldq; d.n_req = n_req; d.n_draft = n_draft; d.vocab = vocab;
     d.tokens = d_tokens; d.accepted = d_accepted;
     verify_chunks(vocab, &d.chunks, &d.chunk);
-    if ((int64_t)n_req * d.chunks > kMaxWorkgroups) return fail(CSB_EUNSUPPORTED, "more than 2^24 workgroups");
+    if (n_req > 1 << 21 || (int64_t)n_req * d.chunks > kMaxWorkgroups) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
     d.sums = (int64_t *)d_ws;
     d.accepted_ws = (int32_t *)(d.sums + (size_t)n_req * d.chunks * 2);
     try {

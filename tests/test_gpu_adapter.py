@@ -89,6 +89,19 @@ def test_one_column_each(fmt):
     check(fmt, 8, 4096, [1], 1, 16, [0], starts=False)
 
 
+@pytest.mark.parametrize("fmt", sorted(TYPES))
+@pytest.mark.parametrize("rank", [16, 64, 128])
+def test_long_requests(fmt, rank):
+    """Requests of many columns, aligned operands; one long one behind short ones that share its first tile."""
+    check(fmt, 200, 1024, [70, 130], 2, rank, [1, 0], ranks=[rank, rank // 2], seed=rank)
+    check(fmt, 72, 512, [1] * 9 + [1999], 6, rank, [0, 1, 2, 3, 4, 5, 0, -1, 1, 3], seed=rank + 1)
+
+
+def test_tall():
+    """More rows than a launch's second dimension has workgroups of 16 for."""
+    check("bf16", 16 * 65535 + 70, 8, [1, 1], 2, 8, [1, 0])
+
+
 def test_many_requests():
     g = np.random.default_rng(5)
     lengths = [int(x) for x in g.integers(0, 3, 600)]
@@ -207,4 +220,14 @@ def test_refusals():
         adapter_add(Y, X.half(), A, B, ids)
     with pytest.raises(AssertionError):
         adapter_add(Y, X, A, B[:, :31], ids)
+    torch.cuda.synchronize()
+
+
+def test_refusals_of_sizes():
+    X, Y = torch.zeros(64, 8, device="cuda"), torch.zeros(32, 8, device="cuda")
+    A, B = torch.zeros(2, 4, 64, device="cuda"), torch.zeros(2, 32, 4, device="cuda")
+    ids, ws = i32([0] * 8), torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    for rows, cols in ((1 << 31, 64), (32, 1 << 31), (1 << 62, 64)):
+        assert lib().csb_adapter_add(0, X.data_ptr(), 8, Y.data_ptr(), 8, rows, cols, 8, A.data_ptr(), B.data_ptr(), 2, 4, None, None, 8, None,
+                                     ids.data_ptr(), ws.data_ptr(), None) == -4
     torch.cuda.synchronize()

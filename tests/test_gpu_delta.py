@@ -109,6 +109,15 @@ def test_many_sequences(form):
 
 
 @both
+@pytest.mark.parametrize("fmt", sorted(TYPES))
+def test_many_wide_sequences(form, fmt):
+    """Enough sequences and heads for every CU, rows of 65 to 128 elements, the last columns alone in their workgroup."""
+    g = np.random.default_rng(2)
+    lengths = [int(x) for x in g.integers(0, 91, 130)]
+    check(form, fmt, sum(lengths), 1, 2, 100, 48, lengths=lengths, slots=[int(x) for x in g.permutation(133)[:130]], n_states=133, seed=20)
+
+
+@both
 def test_states_from_zero_and_not_kept(form):
     check(form, "bf16", 90, 1, 2, 64, 32, lengths=[70, 20], seed=7, state=False)
     check(form, "f16", 90, 1, 2, 64, 32, lengths=[70, 20], seed=8, keep=False)
@@ -171,6 +180,29 @@ def test_not_finite(form):
     assert not np.isfinite(o[70:100, 1, 3]).any() and not np.isfinite(o[101:, 0:2]).any()
     S, Sc = S.cpu(), Sc.cpu()
     assert torch.equal(S[0], Sc[0]) and torch.equal(S[1, [0, 2, 3]], Sc[1, [0, 2, 3]]) and torch.equal(S[2, 2:], Sc[2, 2:])
+
+
+@both
+@pytest.mark.parametrize("fmt", sorted(TYPES))
+def test_not_finite_gates_and_queries(form, fmt):
+    """A gate or a step that is NaN spoils its value head from its token on, a query its token's output only."""
+    def spoil(q, k, v, g, beta):
+        g[80, 0] = math.nan
+        beta[130, 1] = math.nan
+        beta[150, 1] = math.inf
+        q[20, 0, 7] = math.nan
+    lengths = [100, 70]
+    o, _, S, _ = check(form, fmt, 170, 1, 2, 72, 40, lengths=lengths, seed=21, change=spoil)
+    clean, _, Sc, _ = check(form, fmt, 170, 1, 2, 72, 40, lengths=lengths, seed=21)
+    hit = np.zeros((170, 2), bool)
+    hit[80:100, 0] = hit[130:, 1] = hit[20] = True
+    assert not np.isfinite(o[hit]).any()
+    near = np.zeros((170, 2), bool)                      # tokens of the same chunk before it: right, their bits may differ
+    near[64:80, 0] = near[100:130, 1] = True
+    assert np.array_equal(o[~hit & ~near], clean[~hit & ~near]) and np.isfinite(o[near]).all()
+    S, Sc = S.cpu(), Sc.cpu()
+    assert torch.equal(S[0, 1], Sc[0, 1]) and torch.equal(S[1, 0], Sc[1, 0])
+    assert not torch.isfinite(S[0, 0]).any() and not torch.isfinite(S[1, 1]).any()
 
 
 @both
@@ -288,4 +320,22 @@ def test_refusals():
         delta_recurrent(q.half(), k, v, g, beta)
     with pytest.raises(CsbError):
         delta_recurrent(q, k, v, g, beta, slots=torch.zeros(5, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+
+
+def test_refusals_of_the_chunked_form():
+    """Strides and widths whose offsets would pass 32 bits, more workgroups than a launch takes."""
+    q, k, v, g, beta = (x.cuda() for x in inputs(22, 12, 2, 4, 32, 16, "bf16"))
+    out, ws = torch.empty(12, 4, 16, device="cuda", dtype=torch.bfloat16), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    good = dict(type=2, heads_k=2, heads_v=4, dk=32, dv=16, n_seq=1, n_tokens=12, d_q=q.data_ptr(), d_k=k.data_ptr(), d_v=v.data_ptr(),
+                ldq=64, ldk=64, ldv=64, d_g=g.data_ptr(), d_beta=beta.data_ptr(), ldg=4, ldbeta=4, scale=1.0, d_out=out.data_ptr(), ldo=64)
+
+    def call(d_ws=ws.data_ptr(), **change):
+        return lib().csb_delta_chunked(csb_delta_args(**{**good, **change}), d_ws, None)
+    assert call() == 0
+    for name in ("ldq", "ldk", "ldv", "ldo"):
+        assert call(**{name: 1 << 23}) == -4, name
+    assert call(dv=(1 << 20) + 1, ldv=1 << 22 | 64, ldo=1 << 22 | 64) == -4
+    assert call(n_seq=1 << 24, n_tokens=0) == -4
+    assert call(d_ws=None) == -1 and call(d_ws=ws.data_ptr() + 16) == -1
     torch.cuda.synchronize()

@@ -92,6 +92,23 @@ def test_rows_at_their_edges():
     assert wt[:, 0].tolist() == [5, -1, V - 1, 0, 2, 77, 3, 4, 2] and wa.tolist() == [0] * 9
 
 
+@pytest.mark.parametrize("V", [24575, 24576, 24577, 40000])
+def test_rows_at_their_edges_in_large_vocabularies(V):
+    """The same where one workgroup's share of a row ends and where several take it."""
+    p, q, d, u, r = inputs(V, 6, 1, V, "f32")
+    p[0, 0], u[0] = q[0, 0], 1.0                         # p = q and the draft is refused: p's own weights
+    p[1, 0] = q[1, 0] = 0.0                              # nothing anywhere
+    p[2, 0] = 0.0
+    p[2, 0, V - 1], u[2], r[2] = 1.0, 1.0, 1 - 2.0 ** -24
+    p[3, 0, 1:] = math.nan
+    u[3], r[3] = 1.0, 0.0
+    p[4, 0] = p[4, 1] = 0.0
+    p[4, 0, d[4, 0]] = p[4, 1, 16384] = 1.0              # accepted, the next token one of a kind
+    q[5, 0], u[5] = 1.0, 1.0                             # q above p everywhere
+    check(p, q, d, u, r)
+    check(p, None, d, u, r)
+
+
 def test_drafts_outside_the_vocabulary():
     p, q, d, u, r = inputs(4, 4, 3, 100, "f32")
     d[0, 0], d[1, 1], d[2, 2] = -1, 100, 2 ** 31 - 1
@@ -179,4 +196,13 @@ def test_refusals():
         verify_drafts(p, q[:, :2], d, u, r)
     with pytest.raises(AssertionError):
         verify_drafts(p, q.half(), d, u, r)
+    torch.cuda.synchronize()
+
+
+def test_refusals_of_sizes():
+    p, q, d, u, r = (x.cuda() for x in inputs(9, 2, 3, 64, "f32"))
+    out, ws = torch.empty(64, dtype=torch.int32, device="cuda"), torch.empty(4096, dtype=torch.uint8, device="cuda")
+    for n_req, vocab in (((1 << 21) + 1, 64), (1 << 20, 1 << 24)):
+        assert lib().csb_verify_drafts(0, p.data_ptr(), vocab, q.data_ptr(), vocab, d.data_ptr(), u.data_ptr(), r.data_ptr(), None, n_req, 3, vocab,
+                                       out.data_ptr(), out.data_ptr() + 128, ws.data_ptr(), None) == -4
     torch.cuda.synchronize()
