@@ -28,6 +28,15 @@ struct AdapterDev {
     int32_t row_group;                         // rows of Y that a workgroup of the second takes
 };
 
+// Tiles of the launch's first dimension: neighbours on the same XCD (workgroups are dealt out by their number modulo 8), whose L2 then
+// has whole lines of X and longer pieces of Y's rows.  A multiple of 8 workgroups; -1 for the ones too many.
+__device__ __forceinline__ int32_t tile_here(int32_t batch) {
+    const int32_t tiles = (batch + kAdapterTile - 1) / kAdapterTile, x = (int32_t)blockIdx.x;
+    if (tiles < 16) return x;
+    const int32_t k = x % 8, at = x / 8, each = tiles / 8, more = tiles % 8;
+    return at < each + (k < more) ? k * each + min(k, more) + at : -1;
+}
+
 using f32x2 = float __attribute__((ext_vector_type(2)));
 using f32x4 = float __attribute__((ext_vector_type(4)));
 using u16x8 = uint16_t __attribute__((ext_vector_type(8)));
@@ -93,7 +102,8 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(const AdapterDev a) {
     constexpr int step = VF == CSB_VAL_F32 ? 16 : 32, per = step / 4;          // columns of A a step, of a lane
     __shared__ float part[4][RT * 16][kAdapterTile];
     __shared__ AdapterList list;
-    const int32_t base = (int32_t)blockIdx.x * kAdapterTile;
+    const int32_t tile = tile_here(a.batch), base = tile * kAdapterTile;
+    if (tile < 0) return;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15u;
     const int64_t k0 = ((int64_t)blockIdx.y * 4 + wave) * a.k_wave, k1 = min(k0 + a.k_wave, a.cols);
     const T *X = (const T *)a.X;
@@ -268,19 +278,21 @@ __device__ __forceinline__ void three_parts(const float *x, uint16_t (*part)[E])
 // Y += B t for one tile and row_group rows.  t, its splits added up and scaled, goes through LDS into the operands of the matrix cores:
 // tile column h of lane i is column 2 i + h, so that a lane has two neighbouring columns of Y and 16 lanes a whole row of the tile.
 // 16-bit B: t as three bfloat16 parts (24 bits), 3 / 16 of the time of the binary32 form; binary16 B as two.  binary32 B: the binary32 form.
-// 8192 rows x 2048 columns of rank 64: 47 us, 2.6 TB/s; bound by the latency of Y's rows, of which 12 wavefronts a CU have 24 KB in flight.
+// 8192 rows x 2048 columns of rank 64: 34 us, 4 TB/s, bound by HBM and what starts before it (the adapters' list, t).  With loads that lanes take part
+// in or not, as the edges have them, every wait is for all that is in flight: 48 us.
 // Wavefronts share the rows where the tile has few adapters and the adapters where it has many (each column has one, so nothing is added up).
 // BV: rows of B in aligned words of 8 (binary32: 4) elements.  YV: pairs of Y in aligned 8-byte words.
 template <int VF, int KS, bool BV, bool YV>
-__global__ __launch_bounds__(256, KS == 4 ? 2 : 5 - KS) void adapter_up_kernel(const AdapterDev a) {
+__global__ __launch_bounds__(256, KS == 1 ? 3 : 2) void adapter_up_kernel(const AdapterDev a) {
     using T = typename Elem<VF>::T;
     constexpr int per = VF == CSB_VAL_F32 ? 4 : 8, step = 4 * per;             // ranks of a lane, of a step
     __shared__ AdapterList list;
     __shared__ float t[KS * 32][kAdapterTile];
     __shared__ float many[4][16][kAdapterTile];
     __shared__ u32x4 tp[VF == CSB_VAL_F32 ? 1 : 6 * KS][64];
-    const int32_t base = (int32_t)blockIdx.x * kAdapterTile;
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15u;
+    const int32_t tile = tile_here(a.batch), base = tile * kAdapterTile;
+    if (tile < 0) return;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i = lane & 15u;
     const int64_t first = (int64_t)blockIdx.y * a.row_group, last = min(first + a.row_group, a.rows);
     const int32_t col = base + 2 * (int32_t)i;
     const bool there0 = col < a.batch, there1 = col + 1 < a.batch;
@@ -301,24 +313,43 @@ __global__ __launch_bounds__(256, KS == 4 ? 2 : 5 - KS) void adapter_up_kernel(c
     };
     // What needs no adapter's number is requested before those are known: the first rows of Y, and t, of which a thread adds up ranks r0, r0 + 8,
     // ... of one column, 16 loads in flight together.  (t of columns that have no adapter was not written: not used.)
+    // STREAM: rows of Y and the operands of B are requested `depth` steps of 64 rows ahead, through windows, where the tile allows it.
+    constexpr bool STREAM = BV && YV;
+    constexpr int words = VF == CSB_VAL_F32 ? 2 * KS : KS, depth = KS == 4 ? 2 : 3;
+    struct Left { u32x4 w[words]; };
+    struct Ahead { f32x2 y[4]; Left b[2]; } ahead_of[STREAM ? depth : 1];
+    const bool near = a.ldy < 1 << 25;                         // (offsets in 16 rows of Y stay below 2^31 bytes)
+    const uint32_t y_row = (uint32_t)a.ldy * 4;
+    uint32_t y_at = there1 ? 4 * g * y_row + 8 * i : kOutside;
+    auto y_window = [&](int64_t row0) {                        // of the tile's columns in 16 rows
+        const int n = (int)max(min(last - row0, (int64_t)16), (int64_t)0);
+        return window(a.Y + row0 * a.ldy + base, n ? (uint32_t)(n - 1) * y_row + 4 * min(kAdapterTile, a.batch - base) : 0);
+    };
+    auto request_y = [&](Ahead &to, int64_t row0) {
+        const window_t w = y_window(row0);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) to.y[c] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(w, (int)(y_at + c * y_row), 0, 0));
+    };
+    const int64_t row_first = first + 16 * wave;
     f32x2 y[4];
-    load_y(first + 16 * wave, y);
+    if (STREAM && near) request_y(ahead_of[0], row_first);
+    else load_y(row_first, y);
     const uint32_t tn = threadIdx.x & 31u, r0 = threadIdx.x >> 5;
-    constexpr int ahead = 4 / KS;
+    constexpr int turns = 4 / KS;
     float sum[4 * KS];
     {
 #pragma unroll
         for (int k = 0; k < 4 * KS; ++k) sum[k] = 0.0f;
         const float *p = a.t + min(base + (int32_t)tn, a.batch - 1);
         const size_t split = (size_t)a.max_rank * a.batch;
-        for (int32_t s = 0; s < a.splits; s += ahead) {
-            float v[ahead][4 * KS];
+        for (int32_t s = 0; s < a.splits; s += turns) {
+            float v[turns][4 * KS];
 #pragma unroll
-            for (int q = 0; q < ahead; ++q)
+            for (int q = 0; q < turns; ++q)
 #pragma unroll
                 for (int k = 0; k < 4 * KS; ++k) v[q][k] = p[min(s + q, a.splits - 1) * split + (size_t)min((int32_t)r0 + 8 * k, a.max_rank - 1) * a.batch];
 #pragma unroll
-            for (int q = 0; q < ahead; ++q)
+            for (int q = 0; q < turns; ++q)
 #pragma unroll
                 for (int k = 0; k < 4 * KS; ++k) sum[k] += s + q < a.splits ? v[q][k] : 0.0f;
         }
@@ -327,6 +358,8 @@ __global__ __launch_bounds__(256, KS == 4 ? 2 : 5 - KS) void adapter_up_kernel(c
     if (list.n == 0) return;                                   // uniform
     uint32_t all = 0;
     for (int e = 0; e < list.n; ++e) all |= list.columns[e];
+    const uint32_t bit0 = 1u << (2 * i), bit1 = 2u << (2 * i);
+    const bool in0 = all & bit0, in1 = all & bit1;             // (columns of no adapter are not written)
     {
         const bool in = all >> tn & 1u;
         const float scale = in && a.scale ? a.scale[list.of[tn]] : 1.0f;
@@ -350,9 +383,6 @@ __global__ __launch_bounds__(256, KS == 4 ? 2 : 5 - KS) void adapter_up_kernel(c
         __syncthreads();
     }
     const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
-    const uint32_t bit0 = 1u << (2 * i), bit1 = 2u << (2 * i);
-    struct Left { u32x4 w[VF == CSB_VAL_F32 ? 2 * KS : KS]; };
-    constexpr int words = VF == CSB_VAL_F32 ? 2 * KS : KS;
     auto load_b = [&](int e, int64_t row, int64_t last) {      // the lane's part of row `row` (zeros past the adapter's ranks: what is stored there is not used)
         const T *p = (const T *)a.B + ((size_t)list.id[e] * a.rows + row) * a.max_rank;
         const int rank = list.rank[e];
@@ -414,7 +444,6 @@ __global__ __launch_bounds__(256, KS == 4 ? 2 : 5 - KS) void adapter_up_kernel(c
             }
         }
     };
-    const bool in0 = all & bit0, in1 = all & bit1;             // (columns of no adapter are not written)
     auto store_y = [&](int64_t row0, const f32x2 *y) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -429,16 +458,96 @@ __global__ __launch_bounds__(256, KS == 4 ? 2 : 5 - KS) void adapter_up_kernel(c
             }
         }
     };
+    if constexpr (STREAM) {
+        // One or two adapters, pairs of columns with both or neither in an adapter: a stream.
+        int id[2], rank[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            id[e] = __builtin_amdgcn_readfirstlane(list.id[e < list.n ? e : 0]);
+            rank[e] = __builtin_amdgcn_readfirstlane(e < list.n ? list.rank[e] : 0);
+        }
+        const bool stream = near && list.n <= 2 && !__ballot(in0 != in1);
+        auto request_b = [&](Ahead &to, int64_t row0) {
+            const uint32_t n = (uint32_t)max(min(last - row0, (int64_t)16), (int64_t)0), row = (uint32_t)(a.max_rank * sizeof(T));
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const window_t w = window((const T *)a.B + ((size_t)id[e] * a.rows + row0) * a.max_rank, n * row);
+#pragma unroll
+                for (int s = 0; s < words; ++s) {
+                    const int r = step * s + per * (int)g;
+                    to.b[e].w[s] = __builtin_amdgcn_raw_buffer_load_b128(w, (int)(r < rank[e] ? i * row + r * (uint32_t)sizeof(T) : kOutside), 0, 0);
+                }
+            }
+        };
+        if (stream) {                                          // uniform
+#pragma unroll
+            for (int d = 0; d < depth; ++d) {
+                if (d) request_y(ahead_of[d], row_first + 64 * d);
+                request_b(ahead_of[d], row_first + 64 * d);
+                in_order();
+            }
+            u32x4 kept[2];                                     // of the word in which the adapter's ranks end (what is stored past them is not used)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int ranks = rank[e] % step - per * (int)g;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    kept[e][j] = VF == CSB_VAL_F32 ? (j < ranks ? ~0u : 0) : (2 * j < ranks ? 0xffffu : 0) | (2 * j + 1 < ranks ? 0xffff0000u : 0);
+            }
+            auto cut = [&](Left &l, int e) {
+#pragma unroll
+                for (int s = 0; s < words; ++s) if (s == rank[e] / step) l.w[s] &= kept[e];
+            };
+            y_at = in0 ? y_at : kOutside;
+            const uint32_t columns1 = list.n > 1 ? list.columns[1] : 0;
+            for (int64_t row0 = row_first; row0 < last; row0 += 64 * depth)   // (past `last` the windows are empty)
+#pragma unroll
+                for (int d = 0; d < depth; ++d) {
+                    const int64_t row = row0 + 64 * d;
+                    Ahead &now = ahead_of[d];
+                    f32x4 sum[2] = {zero, zero};
+                    cut(now.b[0], 0);
+                    multiply(now.b[0], sum);
+                    if (list.n > 1) {
+                        f32x4 more[2] = {zero, zero};
+                        cut(now.b[1], 1);
+                        multiply(now.b[1], more);
+                        if (columns1 & bit0) sum[0] = more[0];
+                        if (columns1 & bit1) sum[1] = more[1];
+                    }
+                    const window_t w = y_window(row);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
+                        const f32x2 v = now.y[c] + f32x2{sum[0][c], sum[1][c]};
+                        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), w, (int)(y_at + c * y_row), 0, 0);
+                    }
+                    in_order();
+                    request_y(now, row + 64 * depth);
+                    request_b(now, row + 64 * depth);
+                    in_order();
+                }
+            return;
+        }
+        if (near) {
+            if ((a.batch & 1) && base + kAdapterTile > a.batch) load_y(row_first, y);    // (the last column alone was not requested)
+            else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) y[c] = ahead_of[0].y[c];
+            }
+        }
+    }
     if (list.n < 4) {                                          // uniform: wavefronts share the rows
         f32x2 y_next[4];
         Left l, l_next;
-        int64_t row0 = first + 16 * wave;
+        int64_t row0 = row_first;
         if (row0 < last) l = load_b(0, row0 + i, last);
         for (; row0 < last; row0 += 64) {
             if (row0 + 64 < last) {                            // the next rows while these are multiplied
                 load_y(row0 + 64, y_next);
                 l_next = load_b(0, row0 + 64 + i, last);
             }
+            in_order();                                        // (t's operands are read where they are used)
             f32x4 sum[2] = {zero, zero};
             for (int e = 0; e < list.n; ++e) {
                 if (e) l = load_b(e, row0 + i, last);
@@ -583,14 +692,15 @@ extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float
     const int64_t row_groups = (rows + group - 1) / group;
     // adapters of a tile over several workgroups while CUs are idle
     const int64_t deal = many ? std::max<int64_t>(1, std::min<int64_t>(8, 512 / (tiles * d.splits))) : 1;
-    if (tiles * std::max<int64_t>(row_groups, deal * d.splits) > kMaxWorkgroups) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
+    if ((tiles + 7) * std::max<int64_t>(row_groups, deal * d.splits) > kMaxWorkgroups) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
     try {
         static const char adapter_user = 0;                    // this entry point as a user of workspaces
         workspace_changed_hands(d_ws, &adapter_user);
     } catch (const std::bad_alloc &) {
         return fail(CSB_ENOMEM, "out of host memory");
     }
-    const dim3 down((uint32_t)tiles, (uint32_t)d.splits, (uint32_t)deal), up((uint32_t)tiles, (uint32_t)row_groups);
+    const uint32_t across = (uint32_t)(tiles < 16 ? tiles : (tiles + 7) / 8 * 8);
+    const dim3 down(across, (uint32_t)d.splits, (uint32_t)deal), up(across, (uint32_t)row_groups);
     hipStream_t st = (hipStream_t)stream;
     switch (type) {
         case CSB_VAL_F32: launch_adapter<CSB_VAL_F32>(d, av, xv, bv, yv, many, down, up, st); break;

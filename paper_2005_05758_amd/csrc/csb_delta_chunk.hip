@@ -369,25 +369,6 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
 // All that the wavefront wrote to LDS is there, for the whole workgroup.  (Global loads stay in flight: __syncthreads would wait for them.)
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Memory from `base` on, `bytes` of it: reads past them give zero, writes past them do nothing, so that every lane may take part in every
-// access and the wavefront knows how many are in flight.
-using window_t = __amdgpu_buffer_rsrc_t;
-constexpr uint32_t kOutside = 0x80000000u;     // an offset past any window
-__device__ __forceinline__ window_t window(const void *base, uint32_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000);
-}
-template <int N> struct RawBits { using type = uint32_t; };
-template <> struct RawBits<2> { using type = uint16_t; };
-template <typename T> using raw_t = typename RawBits<sizeof(T)>::type;        // a number as it is stored
-template <typename T> __device__ __forceinline__ raw_t<T> window_load(window_t w, uint32_t at) {
-    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_raw_buffer_load_b16(w, (int)at, 0, 0);
-    else return __builtin_amdgcn_raw_buffer_load_b32(w, (int)at, 0, 0);
-}
-template <typename T> __device__ __forceinline__ void window_store(window_t w, uint32_t at, T v) {
-    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), w, (int)at, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), w, (int)at, 0, 0);
-}
-
 template <int VF, bool VEC>
 __device__ __forceinline__ void Row8<VF, VEC>::load(window_t from, uint32_t at, int d, int dk) {
     if constexpr (VEC) {
@@ -404,9 +385,6 @@ __device__ __forceinline__ void Row8<VF, VEC>::load(window_t from, uint32_t at, 
         for (int i = 0; i < 4 * words; ++i) w[i / 4][i % 4] = sizeof(T) == 2 ? low_halves(e[2 * i % 8], e[(2 * i + 1) % 8]) : e[i];
     }
 }
-
-// Requests to memory stay in the order written: the first chunk's have the order that the loop's have, so that a wait in the loop is for as many.
-__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 
 // LDS of a workgroup: K of a chunk (NG = 2: and of the next), Q, e^G_i and e^(G_64 - G_i) of a chunk and of the next, then per 16
 // columns the parts of S, the four wavefronts' sums of K S, R's parts, U's and e^(G_64 - G) U's, and what tells of numbers that

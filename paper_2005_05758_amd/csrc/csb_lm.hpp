@@ -1,5 +1,5 @@
 // What the kernels of the language-model operators share: element types, packed sequences,
-// sums over lanes.
+// windows of memory, sums over lanes.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -50,6 +50,28 @@ __device__ __forceinline__ int tile_sequence(const int32_t *start, int n_seq, in
     }
     return n - 1;
 }
+
+// Memory from `base` on, `bytes` of it: reads past them give zero, writes past them do nothing, so that every lane may take part in every
+// access and the wavefront knows how many are in flight.
+using window_t = __amdgpu_buffer_rsrc_t;
+constexpr uint32_t kOutside = 0x80000000u;     // an offset past any window
+__device__ __forceinline__ window_t window(const void *base, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000);
+}
+template <int N> struct RawBits { using type = uint32_t; };
+template <> struct RawBits<2> { using type = uint16_t; };
+template <typename T> using raw_t = typename RawBits<sizeof(T)>::type;        // a number as it is stored
+template <typename T> __device__ __forceinline__ raw_t<T> window_load(window_t w, uint32_t at) {
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_raw_buffer_load_b16(w, (int)at, 0, 0);
+    else return __builtin_amdgcn_raw_buffer_load_b32(w, (int)at, 0, 0);
+}
+template <typename T> __device__ __forceinline__ void window_store(window_t w, uint32_t at, T v) {
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), w, (int)at, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), w, (int)at, 0, 0);
+}
+
+// Requests to memory stay in the order written, so that a wait in a loop is for as many of them in its first turn as in the others.
+__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 
 // The value of lane (lane + 16 - N) % 16 of the lane's row of 16.
 template <int N> __device__ __forceinline__ float row_rotated(float v) {
