@@ -600,12 +600,13 @@ __global__ __launch_bounds__(256, KS == 1 ? 3 : 2) void adapter_up_kernel(const 
     }
 }
 
-// Requests of few columns take MANY (ranks up to 64, which the registers hold): k_wave = kStay, at most 64 splits.  Aligned operands below 64 columns a
-// request (64 requests of one column beside 4096 x 4096, rank 16: 17 us instead of 108; 2048 columns beside 8192 x 8192 in requests of 32 66
-// instead of 80, of 512 and rank 64 67 instead of 63); operands read element by element below 8 (300 columns of 665 in requests of 32: 18.5
-// instead of 16).  Else at most 8 splits (the second launch reads what each leaves), k_wave a multiple of 32.
+// Requests of few columns take MANY (ranks up to 64, which the registers hold): k_wave = kStay, at most 64 splits.  Aligned operands below 32
+// columns a request (64 requests of one column beside 4096 x 4096, rank 16: 17 us instead of 109; 2048 columns beside 8192 x 8192 in requests of
+// 16, rank 16, 49 instead of 55, of 32 44 instead of 45, of 32 and rank 64 65 instead of 63, of 512 56 instead of 50); operands read element
+// by element below 8 (300 columns of 665 in requests of 3 18 instead of 35, of 30 20 instead of 17).  Else at most 8 splits (the second launch
+// reads what each leaves), k_wave a multiple of 32.
 static bool adapter_many(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank, bool aligned) {
-    return batch < (aligned ? 64ll : 8ll) * n_seg && rank <= 64 && cols <= 64 * 4 * kStay;
+    return batch < (aligned ? 32ll : 8ll) * n_seg && rank <= 64 && cols <= 64 * 4 * kStay;
 }
 static void adapter_split(int64_t cols, int32_t batch, bool many, int32_t *splits, int32_t *k_wave) {
     const int64_t tiles = ((int64_t)batch + kAdapterTile - 1) / kAdapterTile;

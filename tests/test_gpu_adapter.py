@@ -97,6 +97,14 @@ def test_long_requests(fmt, rank):
     check(fmt, 72, 512, [1] * 9 + [1999], 6, rank, [0, 1, 2, 3, 4, 5, 0, -1, 1, 3], seed=rank + 1)
 
 
+@pytest.mark.parametrize("fmt", sorted(TYPES))
+@pytest.mark.parametrize("rank", [24, 64])
+def test_short_requests_of_many_ranks(fmt, rank):
+    """Several adapters in a tile, aligned operands and others, columns of the projection that end inside a step."""
+    check(fmt, 130, 1048, [5, 9, 30, 1, 16, 3], 4, rank, [3, 0, 2, 3, 1, -1], ranks=[rank, 3, rank - 1, rank // 2], seed=rank)
+    check(fmt, 130, 1047, [5, 9, 3, 1, 6, 3], 4, rank, [3, 0, 2, 3, 1, -1], ranks=[rank, 3, rank - 1, rank // 2], seed=rank)
+
+
 def test_tall():
     """More rows than a launch's second dimension has workgroups of 16 for."""
     check("bf16", 16 * 65535 + 70, 8, [1, 1], 2, 8, [1, 0])
