@@ -41,7 +41,23 @@ using f32x2 = float __attribute__((ext_vector_type(2)));
 using f32x4 = float __attribute__((ext_vector_type(4)));
 using u16x8 = uint16_t __attribute__((ext_vector_type(8)));
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+// the same at any element
+using u32_any = uint32_t __attribute__((aligned(2), may_alias));
+using u32x4_any = uint32_t __attribute__((ext_vector_type(4), aligned(2), may_alias));
+using f32x2_any = float __attribute__((ext_vector_type(2), aligned(4), may_alias));
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+
+// 16 bytes of T from p on, at any element; zeros from element n > 0 on, which are not read.
+template <typename T> __device__ __forceinline__ u32x4 any_words(const T *p, int n) {
+    if (n >= (int)(16 / sizeof(T))) return *(const u32x4_any *)p;
+    u32x4 w{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < (int)(16 / sizeof(T)); ++j) if (j < n) {
+        if constexpr (sizeof(T) == 4) w[j] = __float_as_uint(p[j]);
+        else w[j / 2] |= (uint32_t)((const uint16_t *)p)[j] << 16 * (j % 2);
+    }
+    return w;
+}
 
 // The adapters of a tile's columns, each once, with the columns that they have (a bit each) and the ranks they use.
 struct AdapterList {
@@ -127,11 +143,10 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(const AdapterDev a) {
                 const uint16_t *p = (const uint16_t *)X + (kg + j) * a.ldx + n0;
                 v[j] = 0;
                 if (kg + j < k1) {
-                    if (XV && in1) v[j] = *(const uint32_t *)p;
-                    else {
-                        if (in0) v[j] = p[0];
-                        if (in1) v[j] |= (uint32_t)p[1] << 16;
-                    }
+                    if (in1) {
+                        if constexpr (XV) v[j] = *(const uint32_t *)p;
+                        else v[j] = *(const u32_any *)p;
+                    } else if (in0) v[j] = p[0];
                 }
             }
 #pragma unroll
@@ -149,17 +164,7 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(const AdapterDev a) {
         u32x4 v{0, 0, 0, 0};
         if constexpr (AV) {
             if (row < rank && kg < k1) v = *(const u32x4 *)p;
-        } else if (row < rank) {
-            if constexpr (VF == CSB_VAL_F32) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) if (kg + j < k1) v[j] = __float_as_uint(p[j]);
-            } else {
-                u16x8 q{0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) if (kg + j < k1) q[j] = ((const uint16_t *)p)[j];
-                v = __builtin_bit_cast(u32x4, q);
-            }
-        }
+        } else if (row < rank && kg < k1) v = any_words<T>(p, (int)min(k1 - kg, (int64_t)per));
         return v;
     };
     auto multiply = [&](u32x4 l, const Right &x, f32x4 *d) {
@@ -303,11 +308,10 @@ __global__ __launch_bounds__(256, KS == 1 ? 3 : 2) void adapter_up_kernel(const 
             const float *p = a.Y + row * a.ldy + col;
             y[c] = f32x2{0.0f, 0.0f};
             if (row < last) {
-                if (YV && there1) y[c] = *(const f32x2 *)p;
-                else {
-                    if (there0) y[c][0] = p[0];
-                    if (there1) y[c][1] = p[1];
-                }
+                if (there1) {
+                    if constexpr (YV) y[c] = *(const f32x2 *)p;
+                    else y[c] = *(const f32x2_any *)p;
+                } else if (there0) y[c][0] = p[0];
             }
         }
     };
@@ -400,11 +404,7 @@ __global__ __launch_bounds__(256, KS == 1 ? 3 : 2) void adapter_up_kernel(const 
                     for (int j = 0; j < per; ++j) if (r + j >= rank) v[j] = (T)0.0f;
                     __builtin_memcpy(&w, v, 16);
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < per; ++j) v[j] = row < last && r + j < rank ? p[r + j] : (T)0.0f;
-                __builtin_memcpy(&w, v, 16);
-            }
+            } else if (row < last && r < rank) w = any_words<T>(p + r, rank - r);
             l.w[s] = w;
         }
         return l;
@@ -450,8 +450,10 @@ __global__ __launch_bounds__(256, KS == 1 ? 3 : 2) void adapter_up_kernel(const 
             const int64_t row = row0 + 4 * g + c;
             float *p = a.Y + row * a.ldy + col;
             if (row < last) {
-                if (YV && in0 && in1) *(f32x2 *)p = y[c];
-                else {
+                if (in0 && in1) {
+                    if constexpr (YV) *(f32x2 *)p = y[c];
+                    else *(f32x2_any *)p = y[c];
+                } else {
                     if (in0) p[0] = y[c][0];
                     if (in1) p[1] = y[c][1];
                 }
@@ -537,30 +539,28 @@ __global__ __launch_bounds__(256, KS == 1 ? 3 : 2) void adapter_up_kernel(const 
             }
         }
     }
-    if (list.n < 4) {                                          // uniform: wavefronts share the rows
+    if (list.n < 4 || a.row_group >= 64) {                     // uniform: wavefronts share the rows
         f32x2 y_next[4];
         Left l, l_next;
         int64_t row0 = row_first;
         if (row0 < last) l = load_b(0, row0 + i, last);
         for (; row0 < last; row0 += 64) {
-            if (row0 + 64 < last) {                            // the next rows while these are multiplied
-                load_y(row0 + 64, y_next);
-                l_next = load_b(0, row0 + 64 + i, last);
-            }
-            in_order();                                        // (t's operands are read where they are used)
+            if (row0 + 64 < last) load_y(row0 + 64, y_next);   // the next rows while these are multiplied
             f32x4 sum[2] = {zero, zero};
+            in_order();                                        // (t's operands are read where they are used)
             for (int e = 0; e < list.n; ++e) {
-                if (e) l = load_b(e, row0 + i, last);
+                const bool more = e + 1 < list.n;              // the next adapter's part of B, or of the next rows, while this one is multiplied
+                if (more || row0 + 64 < last) l_next = load_b(more ? e + 1 : 0, row0 + (more ? 0 : 64) + i, last);
                 f32x4 d[2] = {zero, zero};
                 multiply(l, d);
                 const uint32_t columns = list.columns[e];
                 if (columns & bit0) sum[0] = d[0];
                 if (columns & bit1) sum[1] = d[1];
+                l = l_next;
             }
 #pragma unroll
             for (int c = 0; c < 4; ++c) y[c] += f32x2{sum[0][c], sum[1][c]};
             store_y(row0, y);
-            l = l_next;
 #pragma unroll
             for (int c = 0; c < 4; ++c) y[c] = y_next[c];
         }
