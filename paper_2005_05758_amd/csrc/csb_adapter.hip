@@ -108,7 +108,8 @@ __device__ __forceinline__ void list_adapters(const AdapterDev &a, int32_t base,
 // k_wave consecutive columns of A, 32 (16 for binary32) at a time; lane (g = lane / 16, i = lane % 16) holds row i of A at
 // 8 (4) columns from 8 g (4 g) on.  16-bit operands: X comes as pairs of neighbouring columns of Y, so that the first product takes the
 // even and the second the odd ones, and no lane needs another's data to have its 8 consecutive rows of X.
-// AV: rows of A in aligned 16-byte words.  XV: pairs of X in aligned 4-byte words.
+// AV: rows of A in aligned 16-byte words, none of them cut by the row's end.  XV: pairs of X in aligned 4-byte words.  Else the same words at any
+// element (2999 columns of A instead of 3008, rank 40, 776 columns of X: 16 us instead of 11.5; element by element it was 44).
 // MANY: the adapters of a tile are dealt out to gridDim.z workgroups, and a wavefront keeps its part of X (k_wave at most kStay) in registers
 // for all of them; else the steps over X are outermost (a tile of one adapter, rarely two).
 constexpr int kStay = 128;
@@ -285,10 +286,10 @@ __device__ __forceinline__ void three_parts(const float *x, uint16_t (*part)[E])
 // 16-bit B: t as three bfloat16 parts (24 bits), 3 / 16 of the time of the binary32 form; binary16 B as two.  binary32 B: the binary32 form.
 // 8192 rows x 2048 columns of rank 64: 34 us, 4 TB/s, bound by HBM and what starts before it (the adapters' list, t).  With loads that lanes take part
 // in or not, as the edges have them, every wait is for all that is in flight: 48 us.
-// Wavefronts share the rows where the tile has few adapters and the adapters where it has many (each column has one, so nothing is added up).
-// BV: rows of B in aligned words of 8 (binary32: 4) elements.  YV: pairs of Y in aligned 8-byte words.
+// Wavefronts share the rows; of groups below 64 rows, where a tile has 4 adapters or more, the adapters (each column has one, so nothing is added up).
+// BV: rows of B in aligned words of 8 (binary32: 4) elements.  YV: pairs of Y in aligned 8-byte words.  Else words at any element.
 template <int VF, int KS, bool BV, bool YV>
-__global__ __launch_bounds__(256, KS == 1 ? 3 : 2) void adapter_up_kernel(const AdapterDev a) {
+__global__ __launch_bounds__(256, KS == 1 || (KS == 2 && VF != CSB_VAL_F32) ? 3 : 2) void adapter_up_kernel(const AdapterDev a) {
     using T = typename Elem<VF>::T;
     constexpr int per = VF == CSB_VAL_F32 ? 4 : 8, step = 4 * per;             // ranks of a lane, of a step
     __shared__ AdapterList list;
@@ -600,13 +601,12 @@ __global__ __launch_bounds__(256, KS == 1 ? 3 : 2) void adapter_up_kernel(const 
     }
 }
 
-// Requests of few columns take MANY (ranks up to 64, which the registers hold): k_wave = kStay, at most 64 splits.  Aligned operands below 32
-// columns a request (64 requests of one column beside 4096 x 4096, rank 16: 17 us instead of 109; 2048 columns beside 8192 x 8192 in requests of
-// 16, rank 16, 49 instead of 55, of 32 44 instead of 45, of 32 and rank 64 65 instead of 63, of 512 56 instead of 50); operands read element
-// by element below 8 (300 columns of 665 in requests of 3 18 instead of 35, of 30 20 instead of 17).  Else at most 8 splits (the second launch
-// reads what each leaves), k_wave a multiple of 32.
-static bool adapter_many(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank, bool aligned) {
-    return batch < (aligned ? 32ll : 8ll) * n_seg && rank <= 64 && cols <= 64 * 4 * kStay;
+// Below 32 columns a request MANY (ranks up to 64, which the registers hold): k_wave = kStay, at most 64 splits.  64 requests of one column beside
+// 4096 x 4096, rank 16: 17 us instead of 106; 2048 columns beside 8192 x 8192 in requests of 16, rank 16, 49 instead of 55, of 32 44 instead of
+// 45, of 32 and rank 64 64 instead of 63; beside 3001 x 2999, rank 13, requests of 9 21 instead of 27, of 31 23 instead of 24.  Else at most 8 splits
+// (the second launch reads what each leaves), k_wave a multiple of 32.
+static bool adapter_many(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank) {
+    return batch < 32ll * n_seg && rank <= 64 && cols <= 64 * 4 * kStay;
 }
 static void adapter_split(int64_t cols, int32_t batch, bool many, int32_t *splits, int32_t *k_wave) {
     const int64_t tiles = ((int64_t)batch + kAdapterTile - 1) / kAdapterTile;
@@ -634,7 +634,7 @@ static void launch_up(const AdapterDev &d, dim3 grid, hipStream_t st) {
 
 template <int VF>
 static void launch_adapter(const AdapterDev &d, bool av, bool xv, bool bv, bool yv, bool many, dim3 down, dim3 up, hipStream_t st) {
-    const bool fast = av && xv;                                // (rows of A or pairs of X that are not aligned: element by element)
+    const bool fast = av && xv;
     if (many && fast) launch_down<VF, true, true, true>(d, down, st);
     else if (many) launch_down<VF, false, false, true>(d, down, st);
     else if (fast) launch_down<VF, true, true, false>(d, down, st);
@@ -647,13 +647,9 @@ static void launch_adapter(const AdapterDev &d, bool av, bool xv, bool bv, bool 
 
 extern "C" size_t csb_adapter_workspace_bytes(int64_t cols, int32_t batch, int32_t n_seg, int32_t rank) {
     if (cols <= 0 || batch <= 0 || n_seg <= 0 || rank <= 0 || rank > csb::kAdapterMaxRank) return 0;
-    int32_t most = 1;                                          // (which of the two a call takes goes by its pointers too)
-    for (const bool many : {false, csb::adapter_many(cols, batch, n_seg, rank, true)}) {
-        int32_t splits, k_wave;
-        csb::adapter_split(cols, batch, many, &splits, &k_wave);
-        most = std::max(most, splits);
-    }
-    return ((size_t)most * (size_t)rank * (size_t)batch * sizeof(float) + 255) / 256 * 256;
+    int32_t splits, k_wave;
+    csb::adapter_split(cols, batch, csb::adapter_many(cols, batch, n_seg, rank), &splits, &k_wave);
+    return ((size_t)splits * (size_t)rank * (size_t)batch * sizeof(float) + 255) / 256 * 256;
 }
 
 extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float *d_Y, int64_t ldy, int64_t rows,
@@ -684,7 +680,7 @@ extern "C" int csb_adapter_add(int32_t type, const void *d_X, int64_t ldx, float
     const bool xv = type == CSB_VAL_F32 || (ldx % 2 == 0 && (uintptr_t)d_X % 4 == 0);
     const bool bv = rank % per == 0 && (uintptr_t)d_B % 16 == 0;
     const bool yv = ldy % 2 == 0 && (uintptr_t)d_Y % 8 == 0;
-    const bool many = adapter_many(cols, batch, n_seg, rank, av && xv);
+    const bool many = adapter_many(cols, batch, n_seg, rank);
     adapter_split(cols, batch, many, &d.splits, &d.k_wave);
     int64_t group = many ? 16 : 64;                            // rows of a workgroup: enough workgroups, and t read by few of them
     while (group < 2048 && tiles * ((rows + 2 * group - 1) / (2 * group)) >= 512) group *= 2;
