@@ -78,8 +78,8 @@ int csb_delta_recurrent(const csb_delta_args *args, void *stream);
 /*
  * The same rule, the same arguments and errors, chunk by chunk: for prompts.  Leading
  * dimensions of 2^23 or more, dv above 2^20 or n_seq heads_v dv of 2^26 and more -> CSB_EUNSUPPORTED.
- * Faster than token by token from 16 to 32 tokens a sequence on; binary32 rows of dk above 128 are
- * taken token by token here too (they do not fit the LDS beside the rest).  Before a capture into a
+ * Faster than token by token from 16 to 32 tokens a sequence on; binary32 rows of dk above 128
+ * and rows below 16 bytes are taken token by token here too.  Before a capture into a
  * graph call it once: a kernel's first launch raises its LDS limit.
  * d_ws: csb_delta_workspace_bytes(args) bytes (only the sizes of `args` are read; 0 for arguments
  * that the call refuses).

@@ -31,6 +31,7 @@ constexpr uint32_t kLower = 6;                 // operands that cover the lower 
 
 using f32x4 = float __attribute__((ext_vector_type(4)));
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+using u32x4_any = uint32_t __attribute__((ext_vector_type(4), aligned(2), may_alias));     // at any element
 using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
@@ -109,31 +110,40 @@ __device__ __forceinline__ void to_lds(uint32_t at, uint32_t v) { *(__attribute_
 // prompts: loads, the products, then the inverse's dependent steps), by loads and LDS where they are many (512 chunks of 16 heads, 128
 // elements each: 91 us; 280 chunks of 48 prompts and 16 heads: 72 us).
 
-// Eight numbers of a row of q or k from element d on, as they are stored (zeros past dk).
+// Eight numbers of a row of q or k from element d on, as they are stored (zeros past dk).  VEC: 16-byte words that are aligned and never cut by
+// the row's end.  Else they lie at any element, and the last one of a row is read from dk - per on and moved into place when it is used
+// (element by element 4096 tokens of 8 sequences, 8 heads of 121 x 121, took 149 us, of 124 x 124 189; aligned ones of 128 x 128 49).
 template <int VF, bool VEC> struct Row8 {
     using T = typename Elem<VF>::T;
-    static constexpr int words = VF == CSB_VAL_F32 ? 2 : 1;
+    static constexpr int words = VF == CSB_VAL_F32 ? 2 : 1, per = 8 / words;
     u32x4 w[words];
+    static __device__ __forceinline__ int first_of(int e, int dk) { return VEC ? e : min(e, dk - per); }
     __device__ __forceinline__ void load(const T *row, int d, int dk) {
-        if constexpr (VEC) {
 #pragma unroll
-            for (int i = 0; i < words; ++i) {
-                w[i] = u32x4{0, 0, 0, 0};
-                if (d + 8 / words * i < dk) w[i] = *(const u32x4 *)(row + d + 8 / words * i);
+        for (int i = 0; i < words; ++i) {
+            const int e = d + per * i;
+            w[i] = u32x4{0, 0, 0, 0};
+            if (e < dk) {
+                if constexpr (VEC) w[i] = *(const u32x4 *)(row + e);
+                else w[i] = *(const u32x4_any *)(row + first_of(e, dk));
             }
-        } else {
-            T e[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = d + i < dk ? row[d + i] : (T)0.0f;
-            __builtin_memcpy(w, e, sizeof(e));
         }
     }
     // the same from a window, the row at byte `at` of it
     __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, uint32_t at, int d, int dk);
     // to the lane's place of an operand in LDS, and from there as a multiplication wants it
-    __device__ __forceinline__ void put(uint32_t at, uint32_t lane) const {
+    __device__ __forceinline__ void put(uint32_t at, uint32_t lane, int d, int dk) const {
 #pragma unroll
-        for (int i = 0; i < words; ++i) to_lds(at + i * kFrag + lane * 16, w[i]);
+        for (int i = 0; i < words; ++i) {
+            u32x4 v = w[i];
+            if constexpr (!VEC) {
+                const int e = d + per * i, bits = e < dk ? (e - first_of(e, dk)) * (int)sizeof(T) * 8 : 0;     // towards the word's start
+                if (bits & 64) v = u32x4{v[2], v[3], 0, 0};
+                if (bits & 32) v = u32x4{v[1], v[2], v[3], 0};
+                if (sizeof(T) == 2 && (bits & 16)) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+            }
+            to_lds(at + i * kFrag + lane * 16, v);
+        }
     }
     __device__ __forceinline__ void get(uint32_t at, uint32_t g, uint32_t m) {
 #pragma unroll
@@ -246,7 +256,7 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
     for (int d = 0; d < a.dk; d += 32) {
         Row8<VF, VEC> kr[4], qr[4];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) next[x].put(stage + x * frag, lane);
+        for (int x = 0; x < 8; ++x) next[x].put(stage + x * frag, lane, d + 8 * (int)loaded_part(lane), a.dk);
         wave_sync();
         if (d + 32 < a.dk) request(d + 32);
 #pragma unroll
@@ -371,18 +381,10 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 
 template <int VF, bool VEC>
 __device__ __forceinline__ void Row8<VF, VEC>::load(window_t from, uint32_t at, int d, int dk) {
-    if constexpr (VEC) {
 #pragma unroll
-        for (int i = 0; i < words; ++i) {
-            const int e = d + 8 / words * i;
-            w[i] = __builtin_amdgcn_raw_buffer_load_b128(from, (int)(e < dk ? at + e * (uint32_t)sizeof(T) : kOutside), 0, 0);
-        }
-    } else {
-        uint32_t e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = window_load<T>(from, d + i < dk ? at + (d + i) * (uint32_t)sizeof(T) : kOutside);
-#pragma unroll
-        for (int i = 0; i < 4 * words; ++i) w[i / 4][i % 4] = sizeof(T) == 2 ? low_halves(e[2 * i % 8], e[(2 * i + 1) % 8]) : e[i];
+    for (int i = 0; i < words; ++i) {
+        const int e = d + per * i;
+        w[i] = __builtin_amdgcn_raw_buffer_load_b128(from, (int)(e < dk ? at + first_of(e, dk) * (uint32_t)sizeof(T) : kOutside), 0, 0);
     }
 }
 
@@ -579,11 +581,11 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
         };
         auto put_q = [&]() {
 #pragma unroll
-            for (int i = 0; i < each; ++i) qr[i].put(k_at + L::q_at + (pt * DP + dp0 + i) * L::frag, lane);
+            for (int i = 0; i < each; ++i) qr[i].put(k_at + L::q_at + (pt * DP + dp0 + i) * L::frag, lane, 32 * (dp0 + i) + element, DK);
         };
         auto put_k = [&](int c) {
 #pragma unroll
-            for (int i = 0; i < each; ++i) kr[i].put(k_at + (c % NG) * L::k + (pt * DP + dp0 + i) * L::frag, lane);
+            for (int i = 0; i < each; ++i) kr[i].put(k_at + (c % NG) * L::k + (pt * DP + dp0 + i) * L::frag, lane, 32 * (dp0 + i) + element, DK);
         };
         auto load_p = [&](int c) {
             pr[0].load(block(c) + P::m_bytes, f0, lane);
@@ -929,8 +931,8 @@ extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *s
             return fail(CSB_ENOMEM, "out of host memory");
         }
     }
-    // binary32 rows wider than 128 do not fit the LDS beside the rest: token by token
-    if (args->type == CSB_VAL_F32 && args->dk > 128) return launch_delta_recurrent(args, (hipStream_t)stream);
+    // binary32 rows wider than 128 do not fit the LDS beside the rest, rows of less than 16 bytes no word: token by token
+    if ((args->type == CSB_VAL_F32 && args->dk > 128) || args->dk * type_size(args->type) < 16) return launch_delta_recurrent(args, (hipStream_t)stream);
     const DeltaDev d = delta_dev(args);
     const int64_t word = 16 / type_size(args->type);           // elements of an aligned 16-byte word
     const bool vec = args->dk % 8 == 0 && args->ldq % word == 0 && args->ldk % word == 0 && ((uintptr_t)args->d_q | (uintptr_t)args->d_k) % 16 == 0;
