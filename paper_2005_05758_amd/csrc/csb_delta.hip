@@ -22,12 +22,15 @@ __device__ __forceinline__ float column_sum(float v) {
 
 // Lane (x = lane % 8, y = lane / 8) holds the 4 columns from 4 x on of the rows y JN .. y JN + JN - 1: eight lanes read 128
 // consecutive bytes of a row.  (16 lanes on 16 rows, 64 bytes of each, were 122 us instead of 43 on 64 requests, 32 heads of 128 x 128.)
-// VEC: operands that are aligned to 4 elements, widths that are multiples of 4.
+// VEC: operands that are aligned to 4 elements, widths that are multiples of 4.  Else the same words at any element, and element by element where a
+// row ends inside one (32 requests, 96 tokens, 16 heads of 121 x 121: 21 us instead of 35; of 124 x 124 15).
 template <int VF, int JN, bool VEC>
 __global__ __launch_bounds__(256) void delta_recurrent_kernel(const DeltaDev a, const uint32_t tiles, const uint32_t waves) {
     using T = typename Elem<VF>::T;
     using T4 = T __attribute__((ext_vector_type(4)));
     using f32x4 = float __attribute__((ext_vector_type(4)));
+    using T4_any = T __attribute__((ext_vector_type(4), aligned(sizeof(T)), may_alias));
+    using f32x4_any = float __attribute__((ext_vector_type(4), aligned(4), may_alias));
     const uint32_t lane = threadIdx.x & 63u, x = lane & 7u, y = lane >> 3;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6));
     if (wave >= waves) return;                                 // (no barrier in this kernel)
@@ -42,7 +45,8 @@ __global__ __launch_bounds__(256) void delta_recurrent_kernel(const DeltaDev a, 
         T4 v{};
         if constexpr (VEC) {
             if (at < most) v = *(const T4 *)p;
-        } else {
+        } else if (at + 4 <= most) v = *(const T4_any *)p;
+        else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) if (at + j < most) v[j] = p[j];
         }
@@ -66,16 +70,20 @@ __global__ __launch_bounds__(256) void delta_recurrent_kernel(const DeltaDev a, 
     for (int j = 0; j < JN; ++j) S[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (a.s_in && slot >= 0) {                                 // uniform
         const float *p = a.s_in + state + (size_t)row * DV + col;
+        if (VEC ? col < DV : col + 4 <= DV) {
 #pragma unroll
-        for (int j = 0; j < JN; ++j)
-            if (row + j < DK) {
-                if constexpr (VEC) {
-                    if (col < DV) S[j] = *(const f32x4 *)(p + (size_t)j * DV);
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) if (col + c < DV) S[j][c] = p[(size_t)j * DV + c];
+            for (int j = 0; j < JN; ++j)
+                if (row + j < DK) {
+                    if constexpr (VEC) S[j] = *(const f32x4 *)(p + (size_t)j * DV);
+                    else S[j] = *(const f32x4_any *)(p + (size_t)j * DV);
                 }
-            }
+        } else if constexpr (!VEC) {
+#pragma unroll
+            for (int j = 0; j < JN; ++j)
+                if (row + j < DK)
+#pragma unroll
+                    for (int c = 0; c < 3; ++c) if (col + c < DV) S[j][c] = p[(size_t)j * DV + c];
+        }
     }
     for (int64_t t = first; t < end; ++t) {
         if (t + 1 < end) load(t + 1, next);
@@ -120,16 +128,20 @@ __global__ __launch_bounds__(256) void delta_recurrent_kernel(const DeltaDev a, 
     }
     if (!a.s_out || slot < 0) return;
     float *p = a.s_out + state + (size_t)row * DV + col;
+    if (VEC ? col < DV : col + 4 <= DV) {
 #pragma unroll
-    for (int j = 0; j < JN; ++j)
-        if (row + j < DK) {
-            if constexpr (VEC) {
-                if (col < DV) *(f32x4 *)(p + (size_t)j * DV) = S[j];
-            } else {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) if (col + c < DV) p[(size_t)j * DV + c] = S[j][c];
+        for (int j = 0; j < JN; ++j)
+            if (row + j < DK) {
+                if constexpr (VEC) *(f32x4 *)(p + (size_t)j * DV) = S[j];
+                else *(f32x4_any *)(p + (size_t)j * DV) = S[j];
             }
-        }
+    } else if constexpr (!VEC) {
+#pragma unroll
+        for (int j = 0; j < JN; ++j)
+            if (row + j < DK)
+#pragma unroll
+                for (int c = 0; c < 3; ++c) if (col + c < DV) p[(size_t)j * DV + c] = S[j][c];
+    }
 }
 
 int check_delta(const char *who, const csb_delta_args *a) {
