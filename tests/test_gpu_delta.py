@@ -118,6 +118,16 @@ def test_many_wide_sequences(form, fmt):
 
 
 @both
+@pytest.mark.parametrize("fmt", sorted(TYPES))
+@pytest.mark.parametrize("DK", [3, 7, 8, 9, 15, 31, 65, 121, 128])
+def test_widths(form, fmt, DK):
+    """Rows that end anywhere in a word; enough sequences and heads for every CU."""
+    g = np.random.default_rng(DK)
+    lengths = [int(x) for x in g.integers(0, 70, 66)]
+    check(form, fmt, sum(lengths), 2, 4, DK, 20, lengths=lengths, seed=DK)
+
+
+@both
 def test_states_from_zero_and_not_kept(form):
     check(form, "bf16", 90, 1, 2, 64, 32, lengths=[70, 20], seed=7, state=False)
     check(form, "f16", 90, 1, 2, 64, 32, lengths=[70, 20], seed=8, keep=False)
