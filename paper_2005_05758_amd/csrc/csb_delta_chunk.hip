@@ -9,10 +9,10 @@
 // matrix products for the matrix cores instead of 64 dependent steps.  Two launches.  The first makes M and P
 // of every chunk at once; the second takes the chunks of a sequence one after the other, S in registers.
 //
-// Precision: state, M, R and U have 24 bits.  A binary32 number is the exact sum of three bfloat16
+// Precision: state, M, P, R and U have 24 bits.  A binary32 number is the exact sum of three bfloat16
 // numbers (8 bits each), so a product of the matrix cores' 16-bit form takes as many passes as its
 // operands have parts (bfloat16 inputs one, binary16 two, binary32 three), without the ones below 2^-24; that
-// is 16 / 6 to 16 / 3 of the rate of their binary32 form.  P, which only the output sees, has two parts (2^-18) where the output has 16 bits.
+// is 16 / 6 to 16 / 3 of the rate of their binary32 form.
 //
 // Not finite: an entry of a later token must not reach an earlier one through a zero of M or P.  R and
 // U are looked at once per chunk; from its first token that is not finite on a column of them is taken out of
@@ -40,9 +40,8 @@ using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
 // e^G_i and e^(G_64 - G_i).  binary32 operands lie there whole (they are split when read: parts would not fit the LDS).
 template <int VF> struct Parts {
     static constexpr int in = VF == CSB_VAL_BF16 ? 1 : VF == CSB_VAL_F16 ? 2 : 3;      // of q and k
-    static constexpr int out = VF == CSB_VAL_F32 ? 3 : 2;                              // of P, which only the output sees
     static constexpr bool whole = VF == CSB_VAL_F32;
-    static constexpr uint32_t m_bytes = kLower * (whole ? 2 : 3) * kFrag, p_bytes = kLower * 2 * kFrag;
+    static constexpr uint32_t m_bytes = kLower * (whole ? 2 : 3) * kFrag, p_bytes = m_bytes;
     static constexpr uint32_t bytes = m_bytes + p_bytes + 512;
 };
 
@@ -55,8 +54,8 @@ __device__ __forceinline__ uint32_t tile_token(uint32_t pt, uint32_t m) { return
 __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }   // a's in the low half
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 
-// E numbers as N bfloat16 numbers each, every part the nearest to what is left: exact for N = 3 (8 bits and a sign each), to
-// 2^-18 for N = 2.
+// E numbers as N bfloat16 numbers each, every part the nearest to what is left: exact for N = 3 (8 bits and a sign each), and for
+// N = 2 where they have 16 bits or fewer.
 template <int N, int E, typename Words>
 __device__ __forceinline__ void split(const float *x, Words *part) {
     using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
@@ -172,9 +171,9 @@ __device__ __forceinline__ void wave_sync() {
 
 constexpr int kLdT = 68;                       // words of a row of a 64 x 64 matrix in LDS: rows stay 16-byte aligned
 
-// The lower triangle in LDS as operands in the workspace: 3 or 2 parts, or whole.  (A loop, like all that may be one here: a launch of
+// The lower triangle in LDS as operands in the workspace: 3 parts, or whole.  (A loop, like all that may be one here: a launch of
 // few chunks waits for its code from memory, some 0.4 us a KiB.)
-template <int NP, bool WHOLE>
+template <bool WHOLE>
 __device__ __forceinline__ void store_lower(const float (*m)[kLdT], uint8_t *to, uint32_t lane) {
     const uint32_t g = lane >> 4, i = lane & 15u;
 #pragma unroll 1
@@ -188,8 +187,8 @@ __device__ __forceinline__ void store_lower(const float (*m)[kLdT], uint8_t *to,
         if constexpr (WHOLE) {
             part[0] = *(u32x4 *)x;
             part[1] = *(u32x4 *)(x + 4);
-        } else split<NP, 8>(x, part);
-        constexpr int n = WHOLE ? 2 : NP;
+        } else split<3, 8>(x, part);
+        constexpr int n = WHOLE ? 2 : 3;
 #pragma unroll
         for (int k = 0; k < n; ++k) *(u32x4 *)(to + (f * n + k) * kFrag + lane * 16) = part[k];
     }
@@ -362,7 +361,7 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
                 m[row][col] = v;
             }
     wave_sync();
-    store_lower<3, Parts<VF>::whole>(m, block, lane);
+    store_lower<Parts<VF>::whole>(m, block, lane);
     wave_sync();
 #pragma unroll
     for (int x = 0; x < 4; ++x)
@@ -371,7 +370,7 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
 #pragma unroll
             for (int r = 0; r < 4; ++r) m[16 * x + 4 * g + r][16 * y + i] = y <= x ? qk[x][y <= x ? y : 0][r] : 0.0f;
     wave_sync();
-    store_lower<2, Parts<VF>::whole>(m, block + Parts<VF>::m_bytes, lane);
+    store_lower<Parts<VF>::whole>(m, block + Parts<VF>::m_bytes, lane);
 }
 
 // ---- second launch: the chunks of a sequence one after the other ---------------------------------
@@ -457,9 +456,9 @@ __device__ __forceinline__ void column_parts(uint32_t k_at, int dp, int ks, uint
     }
 }
 
-// An operand of M (N = 3 parts) or P as it lies in the workspace, and its parts.
-template <int VF, int N> struct Lower {
-    static constexpr int words = Parts<VF>::whole ? 2 : N;
+// An operand of M or P as it lies in the workspace, and its parts.
+template <int VF> struct Lower {
+    static constexpr int words = Parts<VF>::whole ? 2 : 3;
     u32x4 w[words];
     __device__ __forceinline__ void load(const uint8_t *from, uint32_t f, uint32_t lane) {
 #pragma unroll
@@ -473,7 +472,7 @@ template <int VF, int N> struct Lower {
             split<3, 8>(x, part);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) part[i] = w[i];
+            for (int i = 0; i < 3; ++i) part[i] = w[i];
         }
     }
 };
@@ -521,8 +520,10 @@ __device__ __forceinline__ int first_bad(u32x4 in_r, u32x4 in_u, uint32_t told, 
 // the issue of the products and by LDS, with two workgroups a CU.  A sequence's chunks are not split over workgroups: a part would need its
 // product of the chunks' matrices besides, dk columns more beside the state's dv, and a second pass, three times the work, and a full card does
 // 1.9 times the chunks a second that this one sequence does.
+// bfloat16 with rows of 65 to 128 is held to 128 registers, with which a CU takes two workgroups (140 without: 48 prompts 401 us a call instead of
+// 333, 32768 tokens of one sequence 980 instead of 992).
 template <int VF, int DP, int NG, bool VEC>
-__global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
+__global__ __launch_bounds__(512 * NG, VF == CSB_VAL_BF16 && DP == 4 ? 4 : 2 * NG) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
     using T = typename Elem<VF>::T;
     using L = ScanLds<VF, DP, NG>;
     using P = Parts<VF>;
@@ -564,7 +565,7 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
         const uint32_t ldq = (uint32_t)(a.ldq * sizeof(T)), ldo = (uint32_t)(a.ldo * sizeof(T)), o_at = mine ? token * ldo + col * (uint32_t)sizeof(T) : kOutside;
         const uint32_t ldk = (uint32_t)(a.ldk * sizeof(T));
         Row8<VF, VEC> qr[each], kr[each];
-        Lower<VF, 2> pr[2];
+        Lower<VF> pr[2];
         const bool puts_decay = wave == 4;                     // (one wavefront's: 32 lanes hold a chunk's 128 numbers)
         f32x4 dk;
         auto load_decay = [&](int c) { if (puts_decay && lane < 32) dk = *(const f32x4 *)(decay(c) + 4 * lane); };
@@ -657,7 +658,7 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
                     pr[s].parts(part);
 #pragma unroll
                     for (int n = 0; n < 3; ++n) up[n] = lds16(here + L::u + (2 * n + s) * kFrag);
-                    part_pairs<P::out, 3, 2>([&](int i, int j) { more[j] = mfma16(part[i], up[j], more[j]); });
+                    part_pairs<3, 3, 2>([&](int i, int j) { more[j] = mfma16(part[i], up[j], more[j]); });
                 }
 #pragma unroll
             for (int n = 0; n < 3; ++n) out += more[n];
@@ -688,7 +689,7 @@ __global__ __launch_bounds__(512 * NG, 2 * NG) void delta_scan_kernel(const Delt
                 for (int r = 0; r < 4; ++r) S[w][t][r] = __uint_as_float(window_load<float>(from, state_at(w, t, r)));
     }
     raw_t<T> v_0, v_1, v_2, v_3;                               // (an array of them would be packed, two to a register, as soon as they are loaded)
-    Lower<VF, 3> mr[2];
+    Lower<VF> mr[2];
     auto load_v = [&](int c) {
         const window_t vw = window_of(a.v, a.ldv, (size_t)h * DV, c, DV);
         v_0 = window_load<T>(vw, v_at);
