@@ -1,4 +1,9 @@
-"""ctypes binding with the same names as include/csbrnn.h and include/csbrnn_lm.h (argument marshalling only)."""
+"""ctypes binding with the same names as include/csbrnn.h and include/csbrnn_lm.h (argument marshalling only).
+
+`stream` (None: the current stream) is the stream that a call runs on.  Another one has to be made to wait for what produced the arguments,
+and they have to live until it is done; workspaces and new results are safe on it, and results may be dropped while the
+caller's stream still reads them.
+"""
 from __future__ import annotations
 
 import ctypes as C
@@ -216,9 +221,31 @@ def _stream_ptr(stream=None) -> Optional[int]:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
 
 
+def _elsewhere(stream) -> bool:
+    """Whether `stream` is given and not the current one: a call that allocates goes through _on_stream then."""
+    return stream is not None and stream.cuda_stream != (_stream_ptr() or 0)
+
+
+def _on_stream(stream, call, *args, **kw):
+    """A call that allocates, on another stream than the current one.  Workspaces and new results are blocks of `stream`: from the
+    current stream's, a workspace dropped here could be in use again before `stream` has run the call, and a result could be written while the
+    current stream still works on the block's last content.  The results belong to the caller's stream too: they are not used again before
+    its work on them is done.  (The arguments are the caller's: `stream` has to run behind what made them, and they have to live until it is done.)"""
+    import torch
+    here = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        got = call(*args, **kw)
+    for t in got if isinstance(got, tuple) else (got,):
+        if t is not None:
+            t.record_stream(here)
+    return got
+
+
 def stream_read(buf, out=None, stream=None):
     """csb_debug_stream_read on a device tensor (any dtype, size a multiple of 16 bytes)."""
     import torch
+    if out is None and _elsewhere(stream):
+        return _on_stream(stream, stream_read, buf)
     n = int(lib().csb_debug_stream_read_out_floats())
     if out is None:
         out = torch.empty(n, dtype=torch.float32, device=buf.device)
@@ -231,6 +258,8 @@ def project(W, br: int, bc: int, rate: float, out=None, stream=None):
     """csb_project on a device tensor W [rows][cols] (float32, rows may be strided): returns the
     pruned matrix (a new tensor, or `out`, which may be W itself)."""
     import torch
+    if _elsewhere(stream):
+        return _on_stream(stream, project, W, br, bc, rate, out)
     assert W.dim() == 2 and W.dtype == torch.float32 and W.stride(1) == 1
     rows, cols = W.shape
     if out is None:
@@ -255,7 +284,7 @@ def _val_type(dtype) -> int:
 
 
 def _scratch(nbytes: int, device):
-    """A workspace (torch's blocks are 512-byte aligned); freed to the current stream when the caller drops it."""
+    """A workspace (torch's blocks are 512-byte aligned) of the current stream, which the call has to run on."""
     import torch
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
@@ -263,10 +292,8 @@ def _scratch(nbytes: int, device):
 _DELTA_ARGS = struct.Struct("@6iq3P3q2P2q5PifPq")             # csb_delta_args, as ctypes lays it out
 
 
-def _raw_stream(stream) -> Optional[int]:
-    """_stream_ptr for callers that hold device tensors: the runtime is initialised, which current_device() would check."""
-    if stream is not None:
-        return stream.cuda_stream or None
+def _raw_stream() -> Optional[int]:
+    """_stream_ptr() for callers that hold device tensors: the runtime is initialised, which current_device() would check."""
     c = sys.modules["torch"]._C
     return c._cuda_getCurrentRawStream(c._cuda_getDevice()) or None
 
@@ -281,6 +308,8 @@ def _delta_rows(t, n, w, tokens):
 
 
 def _delta(chunked, q, k, v, g, beta, scale, starts, lens, state, slots, state_out, out, stream):
+    if _elsewhere(stream):
+        return _on_stream(stream, _delta, chunked, q, k, v, g, beta, scale, starts, lens, state, slots, state_out, out, None)
     torch = sys.modules["torch"]
     T, HK, DK = shape = q.shape
     Tv, HV, DV = v.shape
@@ -318,9 +347,9 @@ def _delta(chunked, q, k, v, g, beta, scale, starts, lens, state, slots, state_o
     raw = _DELTA_ARGS.pack(*args)
     if chunked:
         ws = _scratch(_raw_delta["workspace"](raw), v.device)
-        rc = _raw_delta["chunked"](raw, ws.data_ptr() if ws is not None else None, _raw_stream(stream))
+        rc = _raw_delta["chunked"](raw, ws.data_ptr() if ws is not None else None, _raw_stream())
     else:
-        rc = _raw_delta["recurrent"](raw, _raw_stream(stream))
+        rc = _raw_delta["recurrent"](raw, _raw_stream())
     if rc:
         _check(rc)
     return out
@@ -349,6 +378,8 @@ def adapter_add(Y, X, A, B, ids, starts=None, scales=None, ranks=None, stream=No
     rank, cols] and B [adapters, rows, rank] of one dtype (float32, float16, bfloat16), Y [rows, batch] float32 (rows of X and Y may be
     strided).  ids [requests] int32: the adapter of each request, -1 for none; starts [requests + 1] int32: its columns (None: one
     each).  scales [adapters] float32, ranks [adapters] int32: factor and used ranks of an adapter.  Returns Y."""
+    if _elsewhere(stream):
+        return _on_stream(stream, adapter_add, Y, X, A, B, ids, starts, scales, ranks)
     torch = sys.modules["torch"]
     cols, batch = X.shape
     n, rank, A_cols = A.shape
@@ -364,7 +395,7 @@ def adapter_add(Y, X, A, B, ids, starts=None, scales=None, ranks=None, stream=No
     ws = torch.empty(max(L.csb_adapter_workspace_bytes(cols, batch, segs, rank), 256), dtype=torch.uint8, device=X.device)
     rc = L.csb_adapter_add(_val_type(typ), X.data_ptr(), max(ldx, batch), Y.data_ptr(), max(ldy, batch), rows, cols, batch, _dptr(A), _dptr(B),
                            n, rank, _dptr(ranks, i32), _dptr(scales, f32), segs, _dptr(starts, i32), _dptr(ids, i32), ws.data_ptr(),
-                           _raw_stream(stream))
+                           _raw_stream())
     if rc:
         _check(rc)
     return Y
@@ -375,6 +406,8 @@ def verify_drafts(p, q, drafts, u, r, counts=None, stream=None):
     of the mass on the drafted token) of one dtype (float32, float16, bfloat16); drafts [requests, n] int32, u [requests, n] and r [requests]
     float32 numbers in [0, 1); counts [requests] int32: drafts that a request brings (None: n).  Returns (tokens
     [requests, n + 1] int32: the accepted drafts, the token drawn behind them, -1; accepted [requests] int32)."""
+    if _elsewhere(stream):
+        return _on_stream(stream, verify_drafts, p, q, drafts, u, r, counts)
     torch = sys.modules["torch"]
     N, K1, V = p.shape
     K = K1 - 1
@@ -397,7 +430,7 @@ def verify_drafts(p, q, drafts, u, r, counts=None, stream=None):
     L = lib()
     ws = torch.empty(max(L.csb_verify_workspace_bytes(N, V), 256), dtype=torch.uint8, device=dev)
     rc = L.csb_verify_drafts(_val_type(typ), p.data_ptr(), rows(p, K1), q.data_ptr() if ldq else None, ldq, _dptr(drafts, i32), _dptr(u, f32),
-                             _dptr(r, f32), _dptr(counts, i32), N, K, V, tokens.data_ptr(), accepted.data_ptr(), ws.data_ptr(), _raw_stream(stream))
+                             _dptr(r, f32), _dptr(counts, i32), N, K, V, tokens.data_ptr(), accepted.data_ptr(), ws.data_ptr(), _raw_stream())
     if rc:
         _check(rc)
     return tokens, accepted
@@ -501,6 +534,8 @@ class CsbMatrix:
 
     def spmv(self, x, y=None, stream=None):
         import torch
+        if (y is None or self.d_ws is None) and _elsewhere(stream):
+            return _on_stream(stream, self.spmv, x, y)
         if y is None:
             y = torch.empty(self.rows, dtype=torch.float32, device=x.device)
         ws = self._workspace(1, x.device)
@@ -510,6 +545,8 @@ class CsbMatrix:
     def spmv_static(self, x, y=None, stream=None):
         """csb_spmv_static: csb_spmv with the library's built-in buffer in place of a workspace."""
         import torch
+        if y is None and _elsewhere(stream):
+            return _on_stream(stream, self.spmv_static, x)
         if y is None:
             y = torch.empty(self.rows, dtype=torch.float32, device=x.device)
         _check(lib().csb_spmv_static(self._h, _dptr(x, _f32()), _dptr(y, _f32()), _stream_ptr(stream)))
@@ -520,6 +557,8 @@ class CsbMatrix:
         (per wavefront: start, vector staged, first unit landed, same, groups done, after the
         barrier, end; 100 MHz clock).  Tile-based layout: [n_chunks, 8 + 3*16] shader clocks."""
         import torch
+        if _elsewhere(stream):
+            return _on_stream(stream, self.spmv_stamps, x, y)
         if y is None:
             y = torch.empty(self.rows, dtype=torch.float32, device=x.device)
         n = int(lib().csb_debug_stamp_count(self._h))
@@ -532,6 +571,8 @@ class CsbMatrix:
 
     def spmm(self, X, Y=None, stream=None):
         import torch
+        if Y is None and _elsewhere(stream):
+            return _on_stream(stream, self.spmm, X)
         cols, batch = X.shape
         if Y is None:
             Y = torch.empty((self.rows, batch), dtype=torch.float32, device=X.device)
@@ -545,6 +586,8 @@ class CsbMatrix:
     def spmm_bfloat(self, Xb, Y=None, stream=None):
         """Xb: [cols, batch] torch.bfloat16 cuda (rows may be strided, the batch contiguous)."""
         import torch
+        if Y is None and _elsewhere(stream):
+            return _on_stream(stream, self.spmm_bfloat, Xb)
         cols, batch = Xb.shape
         if Y is None:
             Y = torch.empty((self.rows, batch), dtype=torch.float32, device=Xb.device)
@@ -556,6 +599,8 @@ class CsbMatrix:
     def spmm_half(self, Xh, Y=None, stream=None):
         """Xh: [cols, batch] torch.float16 cuda (rows may be strided, the batch contiguous)."""
         import torch
+        if Y is None and _elsewhere(stream):
+            return _on_stream(stream, self.spmm_half, Xh)
         cols, batch = Xh.shape
         if Y is None:
             Y = torch.empty((self.rows, batch), dtype=torch.float32, device=Xh.device)
@@ -657,6 +702,8 @@ class CsbRnn:
     def forward(self, x, h0=None, c0=None, want_hseq=True, stream=None):
         """x: [T, B, I] float32 cuda.  Returns (hseq or None, hT, cT or None)."""
         import torch
+        if _elsewhere(stream):
+            return _on_stream(stream, self.forward, x, h0, c0, want_hseq)
         T, B, I = x.shape
         dev = x.device
         need = self.workspace_bytes(B, T)
@@ -678,6 +725,8 @@ class CsbRnn:
         T, B, I = x.shape
         need = self.workspace_bytes(B, T)
         if self._ws is None or self._ws.numel() * 4 < need:
+            if _elsewhere(stream):
+                return _on_stream(stream, self.forward_into, x, h0, c0, hseq, hT, cT)
             self._ws = torch.empty((need + 3) // 4 + 64, dtype=torch.float32, device=x.device)
         f32 = torch.float32
         _check(lib().csb_rnn_forward(self._h, _dptr(x, f32), _dptr(h0, f32), _dptr(c0, f32), _dptr(hseq, f32), _dptr(hT, f32),
