@@ -79,7 +79,8 @@ int csb_delta_recurrent(const csb_delta_args *args, void *stream);
  * The same rule, the same arguments and errors, chunk by chunk: for prompts.  Leading
  * dimensions of 2^23 or more, dv above 2^20 or n_seq heads_v dv of 2^26 and more -> CSB_EUNSUPPORTED.
  * Faster than token by token from 16 to 32 tokens a sequence on; binary32 rows of dk above 128
- * and rows below 16 bytes are taken token by token here too.  Before a capture into a
+ * and rows below 16 bytes are taken token by token here too.  A chunk of 64 tokens meets the state before its
+ * decays: S^T k with the state before the chunk has to be a binary32 number.  Before a capture into a
  * graph call it once: a kernel's first launch raises its LDS limit.
  * d_ws: csb_delta_workspace_bytes(args) bytes (only the sizes of `args` are read; 0 for arguments
  * that the call refuses).

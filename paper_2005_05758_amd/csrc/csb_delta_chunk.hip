@@ -55,7 +55,8 @@ __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return
 __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 
 // E numbers as N bfloat16 numbers each, every part the nearest to what is left: exact for N = 3 (8 bits and a sign each), and for
-// N = 2 where they have 16 bits or fewer.
+// N = 2 where they have 16 bits or fewer (binary16 numbers).  From 3.3962e38 on the nearest bfloat16 number is infinity: the first of three parts is the largest one
+// there, and what is left fits the other two.
 template <int N, int E, typename Words>
 __device__ __forceinline__ void split(const float *x, Words *part) {
     using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
@@ -66,7 +67,8 @@ __device__ __forceinline__ void split(const float *x, Words *part) {
     for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
-            const bf16x2 near = {(__bf16)rest[2 * i], (__bf16)rest[2 * i + 1]};
+            const auto most = [n](float v) { return N == 3 && n == 0 ? __builtin_amdgcn_fmed3f(v, -kMostBf16, kMostBf16) : v; };
+            const bf16x2 near = {(__bf16)most(rest[2 * i]), (__bf16)most(rest[2 * i + 1])};
             const uint32_t two = __builtin_bit_cast(uint32_t, near);
             part[n][i] = two;
             if (n + 1 < N) {
@@ -521,7 +523,7 @@ __device__ __forceinline__ int first_bad(u32x4 in_r, u32x4 in_u, uint32_t told, 
 // product of the chunks' matrices besides, dk columns more beside the state's dv, and a second pass, three times the work, and a full card does
 // 1.9 times the chunks a second that this one sequence does.
 // bfloat16 with rows of 65 to 128 is held to 128 registers, with which a CU takes two workgroups (140 without: 48 prompts 401 us a call instead of
-// 333, 32768 tokens of one sequence 980 instead of 992).
+// 337, 32768 tokens of one sequence 980 instead of 1010).
 template <int VF, int DP, int NG, bool VEC>
 __global__ __launch_bounds__(512 * NG, VF == CSB_VAL_BF16 && DP == 4 ? 4 : 2 * NG) void delta_scan_kernel(const DeltaDev a, const uint8_t *ws, const uint32_t tiles) {
     using T = typename Elem<VF>::T;

@@ -26,6 +26,8 @@ template <> struct Elem<CSB_VAL_BF16> { using T = __bf16; };
 inline int64_t tile_numbers(int64_t total, int64_t n_seq, int shift) { return (total >> shift) + n_seq; }
 
 #ifdef __HIPCC__
+constexpr float kMostBf16 = 0x1.fep127f;       // the largest bfloat16 number
+
 // Where a sequence starts and ends: d_start's offsets, or equal lengths; never outside [0, total].
 __device__ __forceinline__ int64_t clamp64(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
 __device__ __forceinline__ void sequence_range(const int32_t *start, int64_t i, int64_t each, int64_t total, int64_t *first, int64_t *end) {

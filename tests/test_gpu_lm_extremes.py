@@ -1,0 +1,85 @@
+"""Finite numbers near the end of binary32's range (masks of the type's lowest value among them) through the operators of language
+models: they are numbers like others."""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import lm_reference as ref
+from paper_2005_05758_amd import delta_chunked, delta_recurrent
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+HALF = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}   # half a unit in the last place, of the value
+KEEP = 2.0 ** -20                                                  # of the largest number that an entry is made of: 16 units of 2^-24
+FORMS = {"recurrent": delta_recurrent, "chunked": delta_chunked}
+both = pytest.mark.parametrize("form", sorted(FORMS))
+LOWEST = float(torch.finfo(torch.float32).min)
+
+
+def say(msg):
+    print(msg, flush=True)
+    sys.stdout.flush()
+
+
+def inputs(seed, T, HK, HV, DK, DV, fmt):
+    t = torch.Generator().manual_seed(seed)
+    unit = lambda *s: torch.nn.functional.normalize(torch.randn(*s, generator=t), dim=-1)   # noqa: E731
+    q, k, v = unit(T, HK, DK), unit(T, HK, DK), torch.randn(T, HV, DV, generator=t)
+    g, beta = -torch.rand(T, HV, generator=t) ** 3, torch.sigmoid(torch.randn(T, HV, generator=t))
+    return [x.to(TYPES[fmt]) for x in (q, k, v)] + [g, beta]
+
+
+def run(form, ins, S0):
+    S = S0.cuda()
+    out = FORMS[form](*(x.cuda() for x in ins), scale=0.125, state=S)
+    torch.cuda.synchronize()
+    want, state = ref.delta(*(ref.widen(x) for x in ins), 0.125, [(0, ins[0].shape[0])], [0], ref.widen(S0))
+    return ref.widen(out), ref.widen(S), want, state
+
+
+@both
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])
+@pytest.mark.parametrize("token", [10, 63, 64, 69])
+def test_a_token_of_the_lowest_value(form, fmt, token):
+    """One column of v is the lowest number at one token: tokens before it and other columns do not see it, later ones have it in its size."""
+    say(f"[extremes] {form} {fmt} token {token}")
+    ins = inputs(50, 70, 1, 2, 64, 40, fmt)
+    ins[2][token, 1, 3] = float(torch.finfo(TYPES[fmt]).min)
+    o, s, want, state = run(form, ins, torch.randn(1, 2, 64, 40, generator=torch.Generator().manual_seed(51)))
+    assert np.isfinite(o).all() and np.isfinite(s).all()
+    other = np.ones((2, 40), bool)
+    other[1, 3] = False
+    most = np.abs(want[:, other]).max()
+    assert (np.abs(o - want)[:, other] <= HALF[fmt] * np.abs(want[:, other]) + KEEP * most).all()
+    assert (np.abs(o - want)[:token, 1, 3] <= HALF[fmt] * np.abs(want[:token, 1, 3]) + KEEP * most).all()
+    assert (np.abs(o - want)[token:, 1, 3] <= HALF[fmt] * np.abs(want[token:, 1, 3]) + KEEP * -LOWEST).all()
+    assert np.abs(want[token:, 1, 3]).max() > 1e30
+    columns = s.transpose(0, 1, 3, 2)[0], state.transpose(0, 1, 3, 2)[0]
+    assert (np.abs(columns[0] - columns[1])[other] <= KEEP * np.abs(columns[1][other]).max()).all()
+    assert (np.abs(columns[0] - columns[1])[~other] <= KEEP * -LOWEST).all()
+
+
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])
+def test_a_state_of_the_largest_values(fmt, form="chunked"):
+    """A column of the state that is as large as numbers get (at every sixteenth row, signs in turn) through chunks that hardly decay.  (A chunk's keys
+    meet the state before its decays: that product has to be a binary32 number.)"""
+    say(f"[extremes] {form} {fmt} state")
+    ins = inputs(52, 130, 1, 2, 64, 40, fmt)
+    S0 = torch.randn(1, 2, 64, 40, generator=torch.Generator().manual_seed(53))
+    S0[0, 0, ::16, 7] = -LOWEST * (1 - 2 * (torch.arange(4) % 2)).float()
+    ins[3][:] = -1e-4
+    ins[3][0, 0] = -0.7
+    ins[4][:] = 0.1
+    assert np.abs(ref.widen(ins[1])[:, 0] @ ref.widen(S0)[0, 0]).max() < -LOWEST
+    o, s, want, state = run(form, ins, S0)
+    assert np.isfinite(want).all() and np.abs(want).max() < -LOWEST and np.abs(state).max() < -LOWEST
+    assert np.isfinite(o).all() and np.isfinite(s).all()
+    other = np.ones((2, 40), bool)
+    other[0, 7] = False
+    most = np.abs(want[:, other]).max()
+    assert (np.abs(o - want)[:, other] <= HALF[fmt] * np.abs(want[:, other]) + KEEP * most).all()
+    assert (np.abs(o - want)[:, 0, 7] <= HALF[fmt] * np.abs(want[:, 0, 7]) + KEEP * -LOWEST).all()
+    assert (np.abs(s - state)[0, 0, :, 7] <= KEEP * -LOWEST).all()
