@@ -266,15 +266,16 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(const AdapterDev a) {
         a.t[((size_t)blockIdx.y * a.max_rank + r) * a.batch + base + n] = (part[0][r][n] + part[1][r][n]) + (part[2][r][n] + part[3][r][n]);
 }
 
-// E numbers as 3 bfloat16 numbers each, every part the nearest to what is left: exact (8 bits and a sign each).
-template <int E>
+// E numbers as 3 bfloat16 numbers each, every part the nearest to what is left: exact (8 bits and a sign each).  LARGE: binary32 numbers, of which
+// the nearest to those from 3.3962e38 on is infinity: the first part is the largest number there, and what is left fits the other two.
+template <int E, bool LARGE>
 __device__ __forceinline__ void three_parts(const float *x, uint16_t (*part)[E]) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         float rest = x[e];
 #pragma unroll
         for (int n = 0; n < 3; ++n) {
-            const __bf16 near = (__bf16)rest;
+            const __bf16 near = (__bf16)(LARGE && n == 0 ? __builtin_amdgcn_fmed3f(rest, -kMostBf16, kMostBf16) : rest);
             part[n][e] = __builtin_bit_cast(uint16_t, near);
             rest -= (float)near;
         }
@@ -381,7 +382,7 @@ __global__ __launch_bounds__(256, KS == 1 || (KS == 2 && VF != CSB_VAL_F32) ? 3 
             uint16_t p[3][8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = t[32 * s + 8 * g + j][2 * i + h];
-            three_parts<8>(x, p);
+            three_parts<8, true>(x, p);
 #pragma unroll
             for (int n = 0; n < 3; ++n) __builtin_memcpy(&tp[f * 3 + n][lane], p[n], 16);
         }
@@ -429,7 +430,7 @@ __global__ __launch_bounds__(256, KS == 1 || (KS == 2 && VF != CSB_VAL_F32) ? 3 
                     const auto v = __builtin_bit_cast(_Float16 __attribute__((ext_vector_type(8))), l.w[s]);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
-                    three_parts<8>(x, q);
+                    three_parts<8, false>(x, q);
                     __builtin_memcpy(&parts[0], q[0], 16);
                     __builtin_memcpy(&parts[1], q[1], 16);
                 } else parts[0] = l.w[s];

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import lm_reference as ref
-from paper_2005_05758_amd import delta_chunked, delta_recurrent
+from paper_2005_05758_amd import adapter_add, delta_chunked, delta_recurrent
 
 pytestmark = pytest.mark.gpu
 
@@ -83,3 +83,27 @@ def test_a_state_of_the_largest_values(fmt, form="chunked"):
     assert (np.abs(o - want)[:, other] <= HALF[fmt] * np.abs(want[:, other]) + KEEP * most).all()
     assert (np.abs(o - want)[:, 0, 7] <= HALF[fmt] * np.abs(want[:, 0, 7]) + KEEP * -LOWEST).all()
     assert (np.abs(s - state)[0, 0, :, 7] <= KEEP * -LOWEST).all()
+
+
+@pytest.mark.parametrize("fmt", sorted(TYPES))
+@pytest.mark.parametrize("rank", [4, 8])
+def test_adapters_of_the_largest_sums(fmt, rank):
+    """scale A X of 3.4e38, more than the largest bfloat16 number, on its way to B."""
+    say(f"[extremes] adapter {fmt}")
+    typ = TYPES[fmt]
+    X, A, B = torch.zeros(32, 40, dtype=typ), torch.zeros(1, rank, 32, dtype=typ), torch.zeros(1, 24, rank, dtype=typ)
+    X[0], X[1] = 1.0, 2.0 ** -8
+    A[0, 1, 0], A[0, 1, 1] = 1.9921875, 1.5              # 255 / 128 + 1.5 / 256: 255.75 / 256 of 2
+    X[1, ::2] = -2.0 ** -8
+    B[0, :, 1] = torch.linspace(-1, 1, 24).to(typ)
+    Y = torch.randn(24, 40, generator=torch.Generator().manual_seed(54))
+    scale = torch.full((1,), 2.0 ** 127)
+    got = adapter_add(Y.cuda(), X.cuda(), A.cuda(), B.cuda(), torch.zeros(1, dtype=torch.int32, device="cuda"),
+                      starts=torch.tensor([0, 40], dtype=torch.int32, device="cuda"), scales=scale.cuda())
+    torch.cuda.synchronize()
+    args = [ref.widen(x) for x in (Y, X, A, B)] + [[(0, 40)], [0], ref.widen(scale), [rank]]
+    want, size = ref.adapters(*args), ref.adapter_sizes(*args)
+    t = 2.0 ** 127 * ref.widen(A)[0, 1] @ ref.widen(X)
+    assert t.max() > 3.3962e38 and t.max() < -LOWEST and np.abs(want).max() < -LOWEST
+    y = ref.widen(got)
+    assert np.isfinite(y).all() and (np.abs(y - want) <= (32 + rank + 6) * 2.0 ** -24 * size).all()
