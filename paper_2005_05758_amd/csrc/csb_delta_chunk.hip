@@ -248,7 +248,7 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
     auto request = [&](int d) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-            const int64_t t = min(base + 16 * x + (int64_t)loaded_row(lane), end - 1);    // (past the end beta is zero)
+            const int64_t t = min(base + 16 * x + (int64_t)loaded_row(lane), end - 1);    // (past the end the last one's, with a beta of zero)
             next[x].load((const T *)a.k + t * a.ldk + (size_t)kh * a.dk, d + 8 * (int)loaded_part(lane), a.dk);
             next[4 + x].load((const T *)a.q + t * a.ldq + (size_t)kh * a.dk, d + 8 * (int)loaded_part(lane), a.dk);
         }
@@ -291,14 +291,14 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(const DeltaDev a, ui
             }
     wave_sync();
     // A row of T that is not finite must not reach the rows before it through the zeros of (1 + T)^-1: from the first one on T is taken
-    // as zero here, and M's rows become NaN.
+    // as zero here, and M's rows become NaN.  Rows past the end are zero: only a product of the last key with itself can have made them anything else.
     int bad = kChunk;
     if (__builtin_expect(__ballot(strange != 0.0f) != 0, 0)) {
         float z = 0.0f;                                        // a row per lane
         for (int c = 0; c < (int)lane; ++c) z = fmaf(m[lane][c], 0.0f, z);
-        const uint64_t rows = __ballot(z != 0.0f);
+        const uint64_t rows = __ballot(z != 0.0f && (int)lane < n);
         bad = rows ? __builtin_ctzll(rows) : kChunk;
-        for (int r = bad; r < kChunk; ++r) m[r][lane] = 0.0f;
+        for (int r = min(bad, n); r < kChunk; ++r) m[r][lane] = 0.0f;
         wave_sync();
     }
     // (1 + T)^-1 in blocks of 16.  On the diagonal by forward substitution, lane (g, i) column i of block g; ...

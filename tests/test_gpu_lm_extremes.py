@@ -107,3 +107,24 @@ def test_adapters_of_the_largest_sums(fmt, rank):
     assert t.max() > 3.3962e38 and t.max() < -LOWEST and np.abs(want).max() < -LOWEST
     y = ref.widen(got)
     assert np.isfinite(y).all() and (np.abs(y - want) <= (32 + rank + 6) * 2.0 ** -24 * size).all()
+
+
+@both
+@pytest.mark.parametrize("fmt", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 2, 63, 65])
+def test_a_last_key_whose_square_is_no_number(form, fmt, T):
+    """The last token's key is so long that its square passes binary32; nothing of the formula needs that (S^T k and k u are in range)."""
+    say(f"[extremes] {form} {fmt} long last key, {T} tokens")
+    ins = inputs(55, T, 1, 2, 32, 16, fmt)
+    ins[1][T - 1] = 0.0
+    ins[1][T - 1, 0, 5] = 2.0 ** 65
+    ins[0][T - 1] = 0.0
+    ins[0][T - 1, 0, 6] = 1.0
+    S0 = 0.1 * torch.randn(1, 2, 32, 16, generator=torch.Generator().manual_seed(56))
+    S0[:, :, 5] = 0.0
+    ins[1][:T - 1, 0, 5] = 0.0                           # (no row of the state that the key meets: u = beta v)
+    ins[2][T - 1] = 2.0 ** -60
+    o, s, want, state = run(form, ins, S0)
+    assert np.isfinite(o).all() and np.isfinite(s).all()
+    assert (np.abs(o - want) <= HALF[fmt] * np.abs(want) + KEEP * np.abs(want).max()).all()
+    assert (np.abs(s - state) <= KEEP * np.abs(state).max(axis=(0, 1, 3), keepdims=True)).all() and np.abs(state[0, :, 5]).min() > 1.0
