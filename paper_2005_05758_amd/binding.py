@@ -389,11 +389,12 @@ def adapter_add(Y, X, A, B, ids, starts=None, scales=None, ranks=None, stream=No
     assert A_cols == cols and B.shape == (n, rows, rank)
     (ldx, one_x), (ldy, one_y) = X.stride(), Y.stride()
     assert batch < 2 or one_x == one_y == 1
+    ldx, ldy = ldx if cols > 1 else batch, ldy if rows > 1 else batch          # (one row: its stride says nothing)
     segs = ids.numel()
     assert (starts is None or starts.numel() == segs + 1) and (scales is None or scales.numel() == n) and (ranks is None or ranks.numel() == n)
     L = lib()
     ws = torch.empty(max(L.csb_adapter_workspace_bytes(cols, batch, segs, rank), 256), dtype=torch.uint8, device=X.device)
-    rc = L.csb_adapter_add(_val_type(typ), X.data_ptr(), max(ldx, batch), Y.data_ptr(), max(ldy, batch), rows, cols, batch, _dptr(A), _dptr(B),
+    rc = L.csb_adapter_add(_val_type(typ), X.data_ptr(), ldx, Y.data_ptr(), ldy, rows, cols, batch, _dptr(A), _dptr(B),
                            n, rank, _dptr(ranks, i32), _dptr(scales, f32), segs, _dptr(starts, i32), _dptr(ids, i32), ws.data_ptr(),
                            _raw_stream())
     if rc:
