@@ -1,41 +1,22 @@
 """How many bits the operators of language models keep: inputs at which an operand with 16 bits in place of 24 is outside the
-tolerance."""
+tolerance (tests/test_host_lm_precision.py shows that of each operand)."""
 import sys
 
 import numpy as np
 import pytest
 import torch
 
+import lm_precision as cases
 import lm_reference as ref
-from paper_2005_05758_amd import delta_chunked
+from lm_precision import HALF, TYPES, cancelling
+from paper_2005_05758_amd import adapter_add, delta_chunked
 
 pytestmark = pytest.mark.gpu
-
-TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
-HALF = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}   # half a unit in the last place, of the value
 
 
 def say(msg):
     print(msg, flush=True)
     sys.stdout.flush()
-
-
-def cancelling(seed=40, heads=8, dk=64, dv=4, pairs=16):
-    """Pairs of tokens with keys of their own that write 1 and -1 hardly decayed from one to the other, then tokens that read the sum of
-    a pair: two weights near 1 whose difference, some 2^-13, is the output.  Every number but the decays is exact in all types."""
-    t = torch.Generator().manual_seed(seed)
-    T = 3 * pairs
-    q, k = torch.zeros(T, 1, dk), torch.zeros(T, 1, dk)
-    v, beta = torch.zeros(T, heads, dv), torch.zeros(T, heads)
-    g = -2.0 ** -13 * (1 + torch.rand(T, heads, generator=t))
-    for j in range(pairs):
-        k[2 * j, 0, 2 * j] = k[2 * j + 1, 0, 2 * j + 1] = 1.0
-        v[2 * j], v[2 * j + 1] = 1.0, -1.0
-        beta[2 * j] = beta[2 * j + 1] = 1.0
-        g[2 * j] = -0.04 * torch.rand(heads, generator=t)
-        q[2 * pairs + j, 0, 2 * j] = q[2 * pairs + j, 0, 2 * j + 1] = 1.0
-        k[2 * pairs + j, 0, dk - 1] = 1.0
-    return q, k, v, g, beta
 
 
 @pytest.mark.parametrize("fmt", sorted(TYPES))
@@ -53,3 +34,29 @@ def test_outputs_that_cancel(fmt):
     assert 2.0 ** -13.5 < np.abs(read).min() and np.abs(read).max() < 2.0 ** -11.5
     off = np.abs(got.cpu().double().numpy()[32:] - read)
     assert (off <= 8 * 2.0 ** -24 + HALF[fmt] * np.abs(read) + 2.0 ** -25).all(), (off.max() * 2.0 ** 24, "units of 2^-24")
+
+
+@pytest.mark.parametrize("fmt,DK", cases.HARDLY_DECAYING)
+def test_states_keep_24_bits(fmt, DK):
+    """Every operand between a chunk's products has 24 bits: states, and binary32 outputs, of chunks that hardly decay."""
+    say(f"[precision] states, {fmt}, rows of {DK}")
+    ins, S0, want, state = cases.hardly_decaying(fmt, DK)
+    S = torch.from_numpy(S0[None]).float().cuda()
+    got = delta_chunked(*(x.cuda() for x in ins), scale=cases.SCALE, state=S)
+    torch.cuda.synchronize()
+    assert cases.off(ref.widen(S)[0], state) <= cases.KEEP, cases.off(ref.widen(S)[0], state) / cases.KEEP
+    far = np.abs(ref.widen(got) - want) - HALF[fmt] * np.abs(want)
+    assert far.max() <= cases.KEEP * np.abs(want).max(), far.max() / np.abs(want).max() / cases.KEEP
+
+
+@pytest.mark.parametrize("fmt", sorted(TYPES))
+def test_the_adapters_sums_keep_24_bits(fmt):
+    """A X on its way to B: sums that need all of 24 bits."""
+    say(f"[precision] adapter, {fmt}")
+    Y, X, A, B, want, allowed = cases.exact_adapter(fmt)
+    dev = [torch.from_numpy(x).to(TYPES[fmt]).cuda() for x in (X, A, B)]
+    got = adapter_add(torch.from_numpy(Y).float().cuda(), *dev, torch.zeros(1, dtype=torch.int32, device="cuda"),
+                      starts=torch.tensor([0, X.shape[1]], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    off = np.abs(ref.widen(got) - want)
+    assert (off <= allowed).all(), (off / allowed).max()
