@@ -82,8 +82,8 @@ int csb_delta_recurrent(const csb_delta_args *args, void *stream);
  * and rows below 16 bytes are taken token by token here too.  A chunk of 64 tokens meets the state before its
  * decays: S^T k with the state before the chunk has to be a binary32 number.  Before a capture into a
  * graph call it once: a kernel's first launch raises its LDS limit.
- * d_ws: csb_delta_workspace_bytes(args) bytes (only the sizes of `args` are read; 0 for arguments
- * that the call refuses).
+ * d_ws: csb_delta_workspace_bytes(args) bytes (type, heads_*, dk, dv, n_seq and n_tokens are read; 0 for those
+ * that the call refuses or takes token by token: d_ws may be NULL then).
  */
 size_t csb_delta_workspace_bytes(const csb_delta_args *args);
 int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *stream);

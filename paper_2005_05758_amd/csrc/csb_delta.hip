@@ -144,14 +144,20 @@ __global__ __launch_bounds__(256) void delta_recurrent_kernel(const DeltaDev a, 
     }
 }
 
+Refusal delta_sizes(const csb_delta_args *a) {
+    if (!a) return {CSB_EINVAL, "NULL arguments"};
+    if (!known_type(a->type)) return {CSB_EINVAL, "unknown type"};
+    if (a->n_seq < 0 || a->n_tokens < 0 || a->heads_k < 1 || a->heads_v < 1 || a->dk < 1 || a->dv < 1) return {CSB_EINVAL, "bad size"};
+    if (a->heads_v % a->heads_k) return {CSB_EINVAL, "heads_v is no multiple of heads_k"};
+    if (a->dk > 256) return {CSB_EUNSUPPORTED, "dk above 256 (a state's rows are held in the registers of 8 lanes)"};
+    if (a->n_tokens > 0x7fffffff) return {CSB_EUNSUPPORTED, "offsets are 32-bit: more than 2^31 - 1 tokens"};
+    return {CSB_OK, nullptr};
+}
+
 int check_delta(const char *who, const csb_delta_args *a) {
     const auto fail = [&](int code, const char *what) { set_error(std::string(who) + ": " + what); return code; };
-    if (!a) return fail(CSB_EINVAL, "NULL arguments");
-    if (!known_type(a->type)) return fail(CSB_EINVAL, "unknown type");
-    if (a->n_seq < 0 || a->n_tokens < 0 || a->heads_k < 1 || a->heads_v < 1 || a->dk < 1 || a->dv < 1) return fail(CSB_EINVAL, "bad size");
-    if (a->heads_v % a->heads_k) return fail(CSB_EINVAL, "heads_v is no multiple of heads_k");
-    if (a->dk > 256) return fail(CSB_EUNSUPPORTED, "dk above 256 (a state's rows are held in the registers of 16 lanes)");
-    if (a->n_tokens > 0x7fffffff) return fail(CSB_EUNSUPPORTED, "offsets are 32-bit: more than 2^31 - 1 tokens");
+    const Refusal sizes = delta_sizes(a);
+    if (sizes.code != CSB_OK) return fail(sizes.code, sizes.what);
     if (a->n_tokens && (!a->d_q || !a->d_k || !a->d_v || !a->d_g || !a->d_beta || !a->d_out)) return fail(CSB_EINVAL, "NULL pointer");
     const int64_t wk = (int64_t)a->heads_k * a->dk, wv = (int64_t)a->heads_v * a->dv;
     if (a->ldq < wk || a->ldk < wk || a->ldv < wv || a->ldo < wv || a->ldg < a->heads_v || a->ldbeta < a->heads_v)

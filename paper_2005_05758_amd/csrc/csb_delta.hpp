@@ -17,6 +17,8 @@ struct DeltaDev {                              // the call's arguments as the ke
     float scale;
 };
 
+struct Refusal { int code; const char *what; };                               // CSB_OK: none
+Refusal delta_sizes(const csb_delta_args *a);  // of sizes that neither form takes
 int check_delta(const char *who, const csb_delta_args *a);
 DeltaDev delta_dev(const csb_delta_args *a);
 int launch_delta_recurrent(const csb_delta_args *a, hipStream_t st);

@@ -903,11 +903,26 @@ static hipError_t launch_chunked(const DeltaDev &d, uint8_t *ws, int64_t numbers
     return hipErrorInvalidValue;                               // (not reached: csb_delta_chunked)
 }
 
+// binary32 rows wider than 128 do not fit the LDS beside the rest, rows of less than 16 bytes no word: token by token
+static bool delta_by_token(const csb_delta_args *a) {
+    return (a->type == CSB_VAL_F32 && a->dk > 128) || a->dk * type_size(a->type) < 16;
+}
+
+// Sizes that only the chunks refuse.
+static Refusal chunk_sizes(const csb_delta_args *a) {
+    if (a->dv > 1 << 20) return {CSB_EUNSUPPORTED, "dv above 2^20"};
+    const int64_t pairs = ((int64_t)a->n_seq * a->heads_v + 7) / 8 * 8, narrow = ((int64_t)a->dv + 15) / 16;
+    const int64_t numbers = tile_numbers(a->n_tokens, a->n_seq, kChunkShift);
+    if (pairs > kMaxWorkgroups || pairs * narrow > kMaxWorkgroups / 4 || numbers * (((int64_t)a->heads_v + 3) / 4) > kMaxWorkgroups)
+        return {CSB_EUNSUPPORTED, "more workgroups than a launch takes"};
+    return {CSB_OK, nullptr};
+}
+
 }  // namespace csb
 
 extern "C" size_t csb_delta_workspace_bytes(const csb_delta_args *args) {
     using namespace csb;
-    if (!args || !known_type(args->type) || args->heads_v < 1 || args->n_seq < 1 || args->n_tokens < 1) return 0;
+    if (delta_sizes(args).code != CSB_OK || args->n_seq < 1 || args->n_tokens < 1 || delta_by_token(args) || chunk_sizes(args).code != CSB_OK) return 0;
     return ((size_t)tile_numbers(args->n_tokens, args->n_seq, kChunkShift) * (size_t)args->heads_v * chunk_block(args->type) + 255) / 256 * 256;
 }
 
@@ -915,17 +930,17 @@ extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *s
     using namespace csb;
     const int rc = check_delta("csb_delta_chunked", args);
     if (rc != CSB_OK || args->n_seq == 0) return rc;
+    if (delta_by_token(args)) return launch_delta_recurrent(args, (hipStream_t)stream);
     const auto fail = [](int code, const char *what) { set_error(std::string("csb_delta_chunked: ") + what); return code; };
     if (args->n_tokens && !d_ws) return fail(CSB_EINVAL, "NULL pointer");
     if ((uintptr_t)d_ws % 256) return fail(CSB_EINVAL, "workspace not 256-byte aligned");
     const int64_t most = (1 << 23) - 1;                        // (a chunk's offsets in bytes are below 2^31)
     if (args->n_tokens && (args->ldq > most || args->ldk > most || args->ldv > most || args->ldo > most))
         return fail(CSB_EUNSUPPORTED, "2^23 or more elements from one token to the next");
-    if (args->dv > 1 << 20) return fail(CSB_EUNSUPPORTED, "dv above 2^20");
+    const Refusal sizes = chunk_sizes(args);
+    if (sizes.code != CSB_OK) return fail(sizes.code, sizes.what);
     const int64_t numbers = tile_numbers(args->n_tokens, args->n_seq, kChunkShift);
-    const int64_t pairs = ((int64_t)args->n_seq * args->heads_v + 7) / 8 * 8, wide = ((int64_t)args->dv + 63) / 64, narrow = ((int64_t)args->dv + 15) / 16;
-    if (pairs > kMaxWorkgroups || pairs * narrow > kMaxWorkgroups / 4 || numbers * ((args->heads_v + 3) / 4) > kMaxWorkgroups)
-        return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
+    const int64_t pairs = ((int64_t)args->n_seq * args->heads_v + 7) / 8 * 8, wide = ((int64_t)args->dv + 63) / 64;
     if (d_ws) {
         try {
             static const char delta_user = 0;                  // this entry point as a user of workspaces
@@ -934,8 +949,6 @@ extern "C" int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *s
             return fail(CSB_ENOMEM, "out of host memory");
         }
     }
-    // binary32 rows wider than 128 do not fit the LDS beside the rest, rows of less than 16 bytes no word: token by token
-    if ((args->type == CSB_VAL_F32 && args->dk > 128) || args->dk * type_size(args->type) < 16) return launch_delta_recurrent(args, (hipStream_t)stream);
     const DeltaDev d = delta_dev(args);
     const int64_t word = 16 / type_size(args->type);           // elements of an aligned 16-byte word
     const bool vec = args->dk % 8 == 0 && args->ldq % word == 0 && args->ldk % word == 0 && ((uintptr_t)args->d_q | (uintptr_t)args->d_k) % 16 == 0;
