@@ -69,15 +69,16 @@ typedef struct {
  * the few tokens of a decoding step; right for any length.  Bitwise reproducible.
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, heads_v
  * no multiple of heads_k, n_tokens no multiple of n_seq without d_start, an unknown type ->
- * CSB_EINVAL; dk > 256, or more workgroups than a launch takes (n_seq heads_v dv of 2^27
- * and more) -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.
+ * CSB_EINVAL; dk > 256, n_tokens above 2^31 - 1, or more wavefronts than a launch takes (n_seq heads_v
+ * ceil(dv / 32) of 2^24 and more) -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.
  * n_seq = 0 does nothing.
  */
 int csb_delta_recurrent(const csb_delta_args *args, void *stream);
 
 /*
- * The same rule, the same arguments and errors, chunk by chunk: for prompts.  Leading
- * dimensions of 2^23 or more, dv above 2^20 or n_seq heads_v dv of 2^26 and more -> CSB_EUNSUPPORTED.
+ * The same rule, the same arguments and errors, chunk by chunk: for prompts.  ldq, ldk, ldv or ldo of 2^23 or more,
+ * dv above 2^20, or more workgroups than a launch takes (n_seq heads_v, rounded up to a multiple of 8, times ceil(dv / 16) of 2^22 and more;
+ * (n_tokens / 64 + n_seq) ceil(heads_v / 4) of 2^24 and more) -> CSB_EUNSUPPORTED.
  * Faster than token by token from 16 to 32 tokens a sequence on; binary32 rows of dk above 128
  * and rows below 16 bytes are taken token by token here too.  A chunk of 64 tokens meets the state before its
  * decays: S^T k with the state before the chunk has to be a binary32 number.  Before a capture into a

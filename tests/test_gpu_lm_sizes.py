@@ -30,3 +30,20 @@ def test_token_by_token_without_a_workspace(fmt, dk):
     assert lib().csb_delta_chunked(args, None, None) == 0
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dv", [1, 32, 33])
+def test_the_limits_of_a_launch(dv):
+    """The largest numbers of sequences that the header allows, none of them with a token, and one more."""
+    say(f"[sizes] limits, {dv} columns")
+
+    def args(n_seq, heads=1):
+        return csb_delta_args(type=VAL_BF16, heads_k=1, heads_v=heads, dk=16, dv=dv, n_seq=n_seq, n_tokens=0, ldq=16, ldk=16, ldv=heads * dv, ldg=heads,
+                              ldbeta=heads, ldo=heads * dv, scale=1.0)
+    tiles, narrow = -(-dv // 32), -(-dv // 16)
+    most = ((1 << 24) - 1) // tiles
+    assert lib().csb_delta_recurrent(args(most), None) == 0 and lib().csb_delta_recurrent(args(most + 1), None) == -4
+    assert lib().csb_delta_recurrent(args(most // 3, 3), None) == 0 and lib().csb_delta_recurrent(args(most // 3 + 1, 3), None) == -4
+    most = ((1 << 22) - 1) // narrow // 8 * 8
+    assert lib().csb_delta_chunked(args(most), None, None) == 0 and lib().csb_delta_chunked(args(most + 1), None, None) == -4
+    torch.cuda.synchronize()
