@@ -3,6 +3,9 @@
 `stream` (None: the current stream) is the stream that a call runs on.  Another one has to be made to wait for what produced the arguments,
 and they have to live until it is done; workspaces and new results are safe on it, and results may be dropped while the
 caller's stream still reads them.
+
+Nothing here has a gradient.  The language-model operators (delta_*, adapter_add, verify_drafts) refuse operands that require one while
+gradients are enabled, and operands that are not on the current device.
 """
 from __future__ import annotations
 
@@ -292,18 +295,40 @@ def _scratch(nbytes: int, device):
 _DELTA_ARGS = struct.Struct("@6iq3P3q2P2q5PifPq")             # csb_delta_args, as ctypes lays it out
 
 
-def _raw_stream() -> Optional[int]:
-    """_stream_ptr() for callers that hold device tensors: the runtime is initialised, which current_device() would check."""
-    c = sys.modules["torch"]._C
-    return c._cuda_getCurrentRawStream(c._cuda_getDevice()) or None
+def _operands(floats, *others) -> int:
+    """The current device, on which a call runs and all of its operands lie (None: not given).  The operators have no gradients: as torch does
+    where it is given an `out`, they refuse numbers that ask for one while gradients are enabled, rather than return what has lost it."""
+    assert floats[0].is_cuda
+    torch = sys.modules["torch"]
+    here = torch._C._cuda_getDevice()
+    for t in floats:
+        if t is not None:
+            assert t.get_device() == here, "an operand that is not on the current device"
+            assert not t.requires_grad or not torch.is_grad_enabled(), "no gradients here: an operand requires one (torch.no_grad() or detach())"
+    for t in others:
+        assert t is None or t.get_device() == here, "an operand that is not on the current device"
+    return here
+
+
+def _raw_stream(device: int) -> Optional[int]:
+    """_stream_ptr() for callers that know the current device."""
+    return sys.modules["torch"]._C._cuda_getCurrentRawStream(device) or None
+
+
+def _ptr(t, dtype) -> int:
+    """Address of a contiguous tensor that _operands has seen (None: 0)."""
+    if t is None:
+        return 0
+    assert t.is_contiguous() and t.dtype is dtype, f"expected a contiguous {dtype} tensor"
+    return t.data_ptr()
 
 
 def _delta_rows(t, n, w, tokens):
     """Elements from one token to the next of [tokens, n, w]: (t, head, j) at t * ld + head * w + j."""
-    if t.is_contiguous() and t.is_cuda:
+    if t.is_contiguous():
         return n * w
     ld, head, one = t.stride()
-    assert t.is_cuda and (one == 1 or w == 1) and (head == w or n == 1), "heads of a token must be contiguous"
+    assert (one == 1 or w == 1) and (head == w or n == 1), "heads of a token must be contiguous"
     return ld if tokens > 1 else max(ld, n * w)
 
 
@@ -316,12 +341,14 @@ def _delta(chunked, q, k, v, g, beta, scale, starts, lens, state, slots, state_o
     f32, typ = torch.float32, v.dtype
     assert T == Tv and k.shape == shape and g.shape == beta.shape == (T, HV)
     assert q.dtype is k.dtype is typ and g.dtype is beta.dtype is f32
+    given = out
+    here = _operands((q, k, v, g, beta, state, state_out if state_out is not state else None, out), starts, lens, slots)
     if out is None:
-        out = torch.empty((T, HV, DV), dtype=typ, device=v.device)
+        out = torch.empty_like(v, memory_format=torch.contiguous_format)
     else:
         assert out.shape == v.shape and out.dtype is typ
     (ldg, one_g), (ldb, one_b) = g.stride(), beta.stride()
-    assert g.is_cuda and beta.is_cuda and (one_g == one_b == 1 or HV == 1)
+    assert one_g == one_b == 1 or HV == 1
     if T < 2:
         ldg = ldb = HV
     if starts is not None:
@@ -340,18 +367,21 @@ def _delta(chunked, q, k, v, g, beta, scale, starts, lens, state, slots, state_o
             n_states = t.shape[0]
     i32 = torch.int32
     args = (_val_type(typ), HK, HV, DK, DV, N, T, q.data_ptr(), k.data_ptr(), v.data_ptr(), _delta_rows(q, HK, DK, T),
-            _delta_rows(k, HK, DK, T), _delta_rows(v, HV, DV, T), g.data_ptr(), beta.data_ptr(), ldg, ldb, _dptr(starts, i32) or 0,
-            _dptr(lens, i32) or 0, _dptr(state, f32) or 0, (_dptr(state_out, f32) or 0) if state_out is not state else state.data_ptr() if state is not None else 0,
-            _dptr(slots, i32) or 0, n_states, DK ** -0.5 if scale is None else scale, out.data_ptr(), _delta_rows(out, HV, DV, T))
+            _delta_rows(k, HK, DK, T), _delta_rows(v, HV, DV, T), g.data_ptr(), beta.data_ptr(), ldg, ldb, _ptr(starts, i32),
+            _ptr(lens, i32), _ptr(state, f32), _ptr(state_out, f32), _ptr(slots, i32), n_states, DK ** -0.5 if scale is None else scale, out.data_ptr(), _delta_rows(out, HV, DV, T))
     lib()
     raw = _DELTA_ARGS.pack(*args)
     if chunked:
         ws = _scratch(_raw_delta["workspace"](raw), v.device)
-        rc = _raw_delta["chunked"](raw, ws.data_ptr() if ws is not None else None, _raw_stream())
+        rc = _raw_delta["chunked"](raw, ws.data_ptr() if ws is not None else None, _raw_stream(here))
     else:
-        rc = _raw_delta["recurrent"](raw, _raw_stream())
+        rc = _raw_delta["recurrent"](raw, _raw_stream(here))
     if rc:
         _check(rc)
+    if state_out is not None:                                  # autograd may keep what has changed in place
+        torch._C._increment_version((state_out,))
+    if given is not None:
+        torch._C._increment_version((given,))
     return out
 
 
@@ -385,7 +415,8 @@ def adapter_add(Y, X, A, B, ids, starts=None, scales=None, ranks=None, stream=No
     n, rank, A_cols = A.shape
     rows, Y_batch = Y.shape
     i32, f32, typ = torch.int32, torch.float32, X.dtype
-    assert X.is_cuda and Y.is_cuda and Y_batch == batch and Y.dtype is f32 and typ is A.dtype is B.dtype
+    here = _operands((X, Y, A, B, scales), ids, starts, ranks)
+    assert Y_batch == batch and Y.dtype is f32 and typ is A.dtype is B.dtype
     assert A_cols == cols and B.shape == (n, rows, rank)
     (ldx, one_x), (ldy, one_y) = X.stride(), Y.stride()
     assert batch < 2 or one_x == one_y == 1
@@ -394,11 +425,12 @@ def adapter_add(Y, X, A, B, ids, starts=None, scales=None, ranks=None, stream=No
     assert (starts is None or starts.numel() == segs + 1) and (scales is None or scales.numel() == n) and (ranks is None or ranks.numel() == n)
     L = lib()
     ws = torch.empty(max(L.csb_adapter_workspace_bytes(cols, batch, segs, rank), 256), dtype=torch.uint8, device=X.device)
-    rc = L.csb_adapter_add(_val_type(typ), X.data_ptr(), ldx, Y.data_ptr(), ldy, rows, cols, batch, _dptr(A), _dptr(B),
-                           n, rank, _dptr(ranks, i32), _dptr(scales, f32), segs, _dptr(starts, i32), _dptr(ids, i32), ws.data_ptr(),
-                           _raw_stream())
+    rc = L.csb_adapter_add(_val_type(typ), X.data_ptr(), ldx, Y.data_ptr(), ldy, rows, cols, batch, _ptr(A, typ), _ptr(B, typ),
+                           n, rank, _ptr(ranks, i32), _ptr(scales, f32), segs, _ptr(starts, i32), _ptr(ids, i32), ws.data_ptr(),
+                           _raw_stream(here))
     if rc:
         _check(rc)
+    torch._C._increment_version((Y,))                          # (autograd may keep it as it was)
     return Y
 
 
@@ -413,10 +445,11 @@ def verify_drafts(p, q, drafts, u, r, counts=None, stream=None):
     N, K1, V = p.shape
     K = K1 - 1
     i32, f32, typ, dev = torch.int32, torch.float32, p.dtype, p.device
+    here = _operands((p, q, u, r), drafts, counts)
 
     def rows(t, n):
         before, ld, one = t.stride()
-        assert t.is_cuda and (one == 1 or V == 1)
+        assert one == 1 or V == 1
         if n < 2:
             ld = max(V, before)
         assert N < 2 or before == n * ld, "rows of the requests must follow each other at one stride"
@@ -430,8 +463,8 @@ def verify_drafts(p, q, drafts, u, r, counts=None, stream=None):
     accepted = torch.empty(N, dtype=i32, device=dev)
     L = lib()
     ws = torch.empty(max(L.csb_verify_workspace_bytes(N, V), 256), dtype=torch.uint8, device=dev)
-    rc = L.csb_verify_drafts(_val_type(typ), p.data_ptr(), rows(p, K1), q.data_ptr() if ldq else None, ldq, _dptr(drafts, i32), _dptr(u, f32),
-                             _dptr(r, f32), _dptr(counts, i32), N, K, V, tokens.data_ptr(), accepted.data_ptr(), ws.data_ptr(), _raw_stream())
+    rc = L.csb_verify_drafts(_val_type(typ), p.data_ptr(), rows(p, K1), q.data_ptr() if ldq else None, ldq, _ptr(drafts, i32), _ptr(u, f32),
+                             _ptr(r, f32), _ptr(counts, i32), N, K, V, tokens.data_ptr(), accepted.data_ptr(), ws.data_ptr(), _raw_stream(here))
     if rc:
         _check(rc)
     return tokens, accepted
