@@ -97,10 +97,11 @@ int csb_delta_chunked(const csb_delta_args *args, void *d_ws, void *stream);
  * Request s has the columns d_start[s] .. d_start[s + 1] - 1 (d_start [n_seg + 1], ascending;
  * NULL: one column each, n_seg = batch) and adapter d_id[s]; a number outside [0, n_adapters): none,
  * its columns of Y stay as they are.  Adapter a uses its first d_rank[a] ranks (NULL: all;
- * values are taken into [0, rank]; what is stored past them is not read) and the factor d_scale[a]
+ * values are taken into [0, rank]; what is stored past them is not used) and the factor d_scale[a]
  * (NULL: 1).  Columns that no request has stay as they are.  Offsets outside [0, batch] are taken as the nearer end.
  * Products of 16-bit numbers are exact in binary32 and A X is kept in binary32 on its way to B.
- * What is not finite in a column of X changes that column of Y only.  Bitwise reproducible.
+ * What is not finite in a column of X changes that column of Y only, and in a row of A or B the entries that it is a
+ * factor of only; they are infinite or NaN (with a 16-bit type NaN where the formula has infinity).  Bitwise reproducible.
  * d_ws: csb_adapter_workspace_bytes(...) bytes.  Two launches.
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range,
  * n_seg != batch without d_start, an unknown type -> CSB_EINVAL; rank > 128, batch > 2^30, rows or cols above

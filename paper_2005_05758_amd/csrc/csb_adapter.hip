@@ -286,7 +286,8 @@ __device__ __forceinline__ void three_parts(const float *x, uint16_t (*part)[E])
 // tile column h of lane i is column 2 i + h, so that a lane has two neighbouring columns of Y and 16 lanes a whole row of the tile.
 // 16-bit B: t as three bfloat16 parts (24 bits), 3 / 16 of the time of the binary32 form; binary16 B as two.  binary32 B: the binary32 form.
 // 8192 rows x 2048 columns of rank 64: 34 us, 4 TB/s, bound by HBM and what starts before it (the adapters' list, t).  With loads that lanes take part
-// in or not, as the edges have them, every wait is for all that is in flight: 48 us.
+// in or not, as the edges have them, every wait is for all that is in flight: 48 us.  (Three wavefronts a SIMD up to rank 64, at which 16-bit B of ranks 33
+// to 64 keeps 2 registers of a lane in memory: the call 72 us instead of 74 with two.)
 // Wavefronts share the rows; of groups below 64 rows, where a tile has 4 adapters or more, the adapters (each column has one, so nothing is added up).
 // BV: rows of B in aligned words of 8 (binary32: 4) elements.  YV: pairs of Y in aligned 8-byte words.  Else words at any element.
 template <int VF, int KS, bool BV, bool YV>

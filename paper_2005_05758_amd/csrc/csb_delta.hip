@@ -6,7 +6,7 @@
 // written once however many tokens a call brings.  Both products are taken from the decayed state before
 // the update, o = scale (S^T q + (k.q) u): one reduction per token instead of two that wait for each other.
 // Bound by HBM where requests are many: 64 of them, one token, 32 heads of 128 x 128, 268 MB: 58 us, 4.6 TB/s (43 where
-// the caches hold part of it); by the latency of a launch and one trip to memory for one request (4.8 us).
+// the caches hold part of it); by the latency of a launch and one trip to memory for one request (5.4 us; 4.8 replayed from a graph).
 #include "csb_delta.hpp"
 
 namespace csb {
@@ -23,7 +23,7 @@ __device__ __forceinline__ float column_sum(float v) {
 // Lane (x = lane % 8, y = lane / 8) holds the 4 columns from 4 x on of the rows y JN .. y JN + JN - 1: eight lanes read 128
 // consecutive bytes of a row.  (16 lanes on 16 rows, 64 bytes of each, were 122 us instead of 43 on 64 requests, 32 heads of 128 x 128.)
 // VEC: operands that are aligned to 4 elements, widths that are multiples of 4.  Else the same words at any element, and element by element where a
-// row ends inside one (32 requests, 96 tokens, 16 heads of 121 x 121: 21 us instead of 35; of 124 x 124 15).
+// row ends inside one (32 requests, 96 tokens, 16 heads of 121 x 121: 23 us a call instead of 35; of 124 x 124 17).
 template <int VF, int JN, bool VEC>
 __global__ __launch_bounds__(256) void delta_recurrent_kernel(const DeltaDev a, const uint32_t tiles, const uint32_t waves) {
     using T = typename Elem<VF>::T;

@@ -107,13 +107,13 @@ __device__ __forceinline__ void to_lds(uint32_t at, u32x2 v) { *(__attribute__((
 __device__ __forceinline__ void to_lds(uint32_t at, uint32_t v) { *(__attribute__((address_space(3))) uint32_t *)(uintptr_t)at = v; }
 
 // ---- first launch: M and P -----------------------------------------------------------------------
-// A wavefront takes one chunk of one value head.  Bound by its own latency where chunks are few (12.5 us for 64 tokens or for 16 short
-// prompts: loads, the products, then the inverse's dependent steps), by loads and LDS where they are many (512 chunks of 16 heads, 128
-// elements each: 91 us; 280 chunks of 48 prompts and 16 heads: 72 us).
+// A wavefront takes one chunk of one value head.  Bound by its own latency where chunks are few (13 us for 64 tokens or for 16 short
+// prompts: loads, the products, then the inverse's dependent steps), by the wait for loads where they are many (512 chunks of 16 heads, 128
+// elements each: 95 us, of which wavefronts wait 44 %; 280 chunks of 48 prompts and 16 heads: 77 us).
 
 // Eight numbers of a row of q or k from element d on, as they are stored (zeros past dk).  VEC: 16-byte words that are aligned and never cut by
 // the row's end.  Else they lie at any element, and the last one of a row is read from dk - per on and moved into place when it is used
-// (element by element 4096 tokens of 8 sequences, 8 heads of 121 x 121, took 149 us, of 124 x 124 189; aligned ones of 128 x 128 49).
+// (4096 tokens of 8 sequences, 8 heads of 121 x 121: 59 us, of 124 x 124 50, aligned ones of 128 x 128 47; element by element they were 149, 189 and 49).
 template <int VF, bool VEC> struct Row8 {
     using T = typename Elem<VF>::T;
     static constexpr int words = VF == CSB_VAL_F32 ? 2 : 1, per = 8 / words;
@@ -518,8 +518,8 @@ __device__ __forceinline__ int first_bad(u32x4 in_r, u32x4 in_u, uint32_t told, 
 // Lane (g = lane / 16, m = lane % 16) has column m; of a tile over tokens the four from 8 g + 4 t on, of 32 rows of the state 8 g .. 8 g + 7.
 // DP: 32s of dk.  VEC: rows of q and k in aligned 16-byte words.
 // Bound by what follows on what: K S, R, U and the state wait for each other chunk after chunk, three times through LDS.  32768 tokens
-// of one sequence, 16 heads of 128 x 128: 512 chunks of 1.7 us (3830 clocks) each, 885 us; 48 prompts, 16411 tokens, 16 heads: 260 us, there by
-// the issue of the products and by LDS, with two workgroups a CU.  A sequence's chunks are not split over workgroups: a part would need its
+// of one sequence, 16 heads of 128 x 128: 512 chunks of 1.8 us each, 915 us.  48 prompts, 16411 tokens, 16 heads, two workgroups a CU: 270 us,
+// in which LDS is busy 45 % of the time, the vector issue 49 and the matrix cores 23, and wavefronts wait for 36 (one sequence: 40, 39, 21; 36).  A sequence's chunks are not split over workgroups: a part would need its
 // product of the chunks' matrices besides, dk columns more beside the state's dv, and a second pass, three times the work, and a full card does
 // 1.9 times the chunks a second that this one sequence does.
 // bfloat16 with rows of 65 to 128 is held to 128 registers, with which a CU takes two workgroups (140 without: 48 prompts 401 us a call instead of
@@ -890,9 +890,9 @@ static hipError_t launch_chunked(const DeltaDev &d, uint8_t *ws, int64_t numbers
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    // 16 columns a workgroup, of which a CU takes two with bfloat16 rows of up to 128 (16411 tokens, 8 heads of 128 x 128: 176 us; 32 columns 181).
-    // binary16 has one part of K and Q more and the registers for one only: 32 columns a workgroup where CUs have enough of them (236 us against
-    // 268).  Rows of 64 gain nothing by that (156 against 141), wider ones have not the LDS.
+    // 16 columns a workgroup, of which a CU takes two with bfloat16 rows of up to 128 (16411 tokens, 8 heads of 128 x 128: 174 us; 32 columns 182).
+    // binary16 has one part of K and Q more and the registers for one only: 32 columns a workgroup where CUs have enough of them (232 us against
+    // 270, though it keeps 16 registers of a lane in memory then).  Rows of 64 gain nothing by that (157 against 143), wider ones have not the LDS.
     if (d.dk <= 64) return launch_scan<VF, 2, 1, VEC>(d, ws, st);
     if (d.dk <= 128) {
         if constexpr (VF == CSB_VAL_F16)
