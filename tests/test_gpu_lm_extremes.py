@@ -128,3 +128,36 @@ def test_a_last_key_whose_square_is_no_number(form, fmt, T):
     assert np.isfinite(o).all() and np.isfinite(s).all()
     assert (np.abs(o - want) <= HALF[fmt] * np.abs(want) + KEEP * np.abs(want).max()).all()
     assert (np.abs(s - state) <= KEEP * np.abs(state).max(axis=(0, 1, 3), keepdims=True)).all() and np.abs(state[0, :, 5]).min() > 1.0
+
+
+@pytest.mark.parametrize("fmt", sorted(TYPES))
+@pytest.mark.parametrize("lengths", [[40, 24, 64], [3, 5, 2, 30, 9, 7, 1, 1]])
+@pytest.mark.parametrize("rank", [8, 40])
+def test_adapters_with_weights_that_are_not_finite(fmt, lengths, rank):
+    """An infinite or NaN entry of A changes the columns of that adapter's requests, one of B one row of them; nothing else."""
+    say(f"[extremes] adapter {fmt} weights, {lengths}, rank {rank}")
+    typ, n, batch = TYPES[fmt], 3, sum(lengths)
+    t = torch.Generator().manual_seed(57)
+    X, Y = torch.randn(96, batch, generator=t).to(typ).cuda(), torch.randn(130, batch, generator=t).cuda()
+    A, B = (0.1 * torch.randn(n, rank, 96, generator=t)).to(typ).cuda(), torch.randn(n, 130, rank, generator=t).to(typ).cuda()
+    ids = [i % n for i in range(len(lengths))]
+    starts = torch.tensor(np.concatenate([[0], np.cumsum(lengths)]), dtype=torch.int32, device="cuda")
+    of = torch.tensor(np.repeat(ids, lengths), device="cuda")
+    call = lambda: adapter_add(Y.clone(), X, A, B, torch.tensor(ids, dtype=torch.int32, device="cuda"), starts=starts)   # noqa: E731
+    clean = call()
+    assert torch.isfinite(clean).all()
+    for value in (float("inf"), float("-inf"), float("nan")):
+        keep = B[1, 77, rank - 1].clone()
+        B[1, 77, rank - 1] = value
+        got = call()
+        hit = torch.zeros(130, batch, dtype=torch.bool, device="cuda")
+        hit[77] = of == 1
+        assert torch.equal(got[~hit], clean[~hit]) and not torch.isfinite(got[hit]).any()
+        B[1, 77, rank - 1] = keep
+        keep = A[2, 5, 95].clone()
+        A[2, 5, 95] = value
+        got = call()
+        hit = (of == 2)[None].expand(130, batch)
+        assert torch.equal(got[~hit], clean[~hit]) and not torch.isfinite(got[hit]).any()
+        A[2, 5, 95] = keep
+    torch.cuda.synchronize()
