@@ -1,7 +1,8 @@
 /*
  * csbrnn_lm.h -- operators of recurrent language models beside the pruned products of csbrnn.h:
- * the gated delta rule (a recurrent cell whose state is a matrix), low-rank adapters of many
- * requests added to a shared projection's result, and the verification of drafted tokens.
+ * the gated delta rule (a recurrent cell whose state is a matrix), the selective state space scan and the
+ * short convolution in front of it, norms around a block, low-rank adapters of many requests added to a shared
+ * projection's result, the verification of drafted tokens and the sampling of tokens from logits.
  *
  * The conventions of csbrnn.h hold: int status codes, csb_last_error(), device pointers owned by
  * the caller (prefix d_), nothing allocated on the device, everything enqueued on `stream` (a
@@ -139,6 +140,82 @@ int csb_verify_drafts(int32_t type, const void *d_p, int64_t ldp, const void *d_
                       const int32_t *d_draft, const float *d_u, const float *d_r, const int32_t *d_count,
                       int32_t n_req, int32_t n_draft, int32_t vocab, int32_t *d_tokens, int32_t *d_accepted,
                       void *d_ws, void *stream);
+
+/*
+ * The short causal convolution of a recurrent layer, channel by channel:
+ *     out[t, c] = act(bias[c] + sum_{j < width} w[c][j] x[t - (width - 1) + j, c]),
+ * act(v) = v / (1 + e^-v) with `silu`, else v.  Sequences (d_start, d_len, n_seq, n_tokens), slots and what happens to entries outside
+ * of them are as with the delta rule.  Element (t, c) of x and out is at t * ld + c, both of `type` (CSB_VAL_*); w [channels][width] and
+ * bias [channels] (NULL: zero) are binary32, sums too; `out` is rounded once and must not overlap x.
+ * States hold the width - 1 inputs before a sequence's first token, oldest first, as they are:
+ * [n_states][width - 1][channels] of `type`.  Sequence i starts from state d_slot[i] of d_state_in (d_slot NULL: state i; d_state_in NULL or
+ * a slot outside [0, n_states): zeros) and leaves its last width - 1 inputs in the same place of d_state_out (the same buffer or
+ * another that does not overlap; NULL: not kept).  With width 1 states have no entries, and are neither read nor written.
+ * What is not finite in x or a state stays in its channel, in the width outputs that it is a factor of.
+ * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, out = x, n_tokens no multiple of n_seq
+ * without d_start, an unknown type -> CSB_EINVAL; width > 8, n_tokens above 2^31 - 1, or more workgroups than a launch takes ->
+ * CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.  n_seq = 0 does nothing.  Bitwise reproducible, one launch.
+ */
+typedef struct {
+    int32_t type;                          /* CSB_VAL_*: x, out and the states               */
+    int32_t channels, width;               /* width in [1, 8]                                */
+    int32_t silu;
+    int32_t n_seq;
+    int32_t n_states;
+    int64_t n_tokens;
+    const void *d_x;
+    int64_t ldx;                           /* elements from one token to the next            */
+    const float *d_w, *d_bias;
+    const int32_t *d_start, *d_len;
+    const void *d_state_in;
+    void *d_state_out;
+    const int32_t *d_slot;
+    void *d_out;
+    int64_t ldo;
+} csb_conv_args;
+
+int csb_short_conv(const csb_conv_args *args, void *stream);
+
+/*
+ * The selective state space scan.  Channel c has a state h of n numbers, decays A[c][0 .. n) (below zero in layers of this kind) and reads
+ * B and C of group c / (channels / groups).  Per token, with s = dt[t, c] + dt_bias[c], or ln(1 + e^s) in its place with `softplus`:
+ *     h[j] <- exp(s A[c][j]) h[j] + s x[t, c] B[t, group, j];   y = sum_j C[t, group, j] h[j] + D[c] x[t, c];
+ *     out[t, c] = y, or y z[t, c] / (1 + e^-z[t, c]) where d_z is given.
+ * Element (t, c) of x, dt, z and out is at t * ld + c, (t, group, j) of B and C at t * ld + group * n + j, all of `type`; A [channels][n],
+ * D and dt_bias [channels] (NULL: zeros) and states are binary32, and so is everything computed; `out` is rounded once.  It may be x,
+ * dt or z themselves (the same pointer and leading dimension); it must not overlap them otherwise, nor B and C.
+ * Sequences, slots and states ([n_states][channels][n]) are as with the delta rule.  Long sequences are
+ * split into chunks (by n_tokens, n_seq, channels and n alone): the chunks' own states first, then outputs from what the chunks before leave,
+ * in two launches; else one launch.  Bitwise reproducible.
+ * What is not finite stays in its channel (in B or C: its group's) from its token on; it is infinite or NaN there.
+ * d_ws: csb_scan_workspace_bytes(args) bytes (channels, groups, n, n_seq and n_tokens are read; 0 where there is one launch or a
+ * refusal: d_ws may be NULL then).
+ * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, channels no multiple of groups, n_tokens no
+ * multiple of n_seq without d_start, an unknown type -> CSB_EINVAL; n > 128, n_tokens above 2^31 - 1,
+ * or more workgroups than a launch takes -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.  n_seq = 0 does nothing.
+ */
+typedef struct {
+    int32_t type;                          /* CSB_VAL_*: x, dt, z, B, C and out              */
+    int32_t channels, groups;              /* channels a multiple of groups                  */
+    int32_t n;                             /* numbers of a channel's state, in [1, 128]      */
+    int32_t softplus;
+    int32_t n_seq;
+    int64_t n_tokens;
+    const void *d_x, *d_dt, *d_z, *d_B, *d_C;
+    int64_t ldx, lddt, ldz, ldB, ldC;      /* elements from one token to the next            */
+    const float *d_A, *d_D, *d_dt_bias;
+    const int32_t *d_start, *d_len;
+    const float *d_state_in;
+    float *d_state_out;
+    const int32_t *d_slot;
+    int32_t n_states;
+    int32_t reserved;                      /* 0                                              */
+    void *d_out;
+    int64_t ldo;
+} csb_scan_args;
+
+size_t csb_scan_workspace_bytes(const csb_scan_args *args);
+int csb_selective_scan(const csb_scan_args *args, void *d_ws, void *stream);
 
 #ifdef __cplusplus
 }

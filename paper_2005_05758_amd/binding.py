@@ -4,7 +4,7 @@
 and they have to live until it is done; workspaces and new results are safe on it, and results may be dropped while the
 caller's stream still reads them.
 
-Nothing here has a gradient.  The language-model operators (delta_*, adapter_add, verify_drafts) refuse operands that require one while
+Nothing here has a gradient.  The language-model operators (delta_*, adapter_add, verify_drafts, short_conv, selective_scan, block_norm, sample) refuse operands that require one while
 gradients are enabled, and operands that are not on the current device.
 """
 from __future__ import annotations
@@ -28,6 +28,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libcsbrnn.so")
 _lib = None
 _raw_delta = {}
+_raw = {}
 
 # every symbol the headers under include/ declare
 SYMBOLS = ["csb_last_error", "csb_pack", "csb_view_get", "csb_unpack", "csb_set_value_format", "csb_value_format", "csb_sharing_model", "csb_plan", "csb_plan_ex", "csb_plan_rows", "csb_plan_stats_get", "csb_plan_validate", "csb_status",
@@ -39,7 +40,7 @@ SYMBOLS = ["csb_last_error", "csb_pack", "csb_view_get", "csb_unpack", "csb_set_
            "csb_rnn_set_poll_limit", "csb_rnn_status", "csb_rnn_workspace_bytes", "csb_rnn_forward", "csb_free", "csb_rnn_free",
            # include/csbrnn_lm.h
            "csb_delta_recurrent", "csb_delta_workspace_bytes", "csb_delta_chunked", "csb_adapter_workspace_bytes", "csb_adapter_add",
-           "csb_verify_workspace_bytes", "csb_verify_drafts"]
+           "csb_verify_workspace_bytes", "csb_verify_drafts", "csb_short_conv", "csb_scan_workspace_bytes", "csb_selective_scan"]
 
 
 class csb_sharing_stats(C.Structure):
@@ -86,6 +87,19 @@ class csb_delta_args(C.Structure):
                 ("ldg", C.c_int64), ("ldbeta", C.c_int64), ("d_start", C.c_void_p), ("d_len", C.c_void_p),
                 ("d_state_in", C.c_void_p), ("d_state_out", C.c_void_p), ("d_slot", C.c_void_p), ("n_states", C.c_int32),
                 ("scale", C.c_float), ("d_out", C.c_void_p), ("ldo", C.c_int64)]
+
+
+class csb_conv_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("type", "channels", "width", "silu", "n_seq", "n_states")] + [
+        ("n_tokens", C.c_int64), ("d_x", C.c_void_p), ("ldx", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("d_w", "d_bias", "d_start", "d_len", "d_state_in", "d_state_out", "d_slot", "d_out")] + [("ldo", C.c_int64)]
+
+
+class csb_scan_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("type", "channels", "groups", "n", "softplus", "n_seq")] + [("n_tokens", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("d_x", "d_dt", "d_z", "d_B", "d_C")] + [(n, C.c_int64) for n in ("ldx", "lddt", "ldz", "ldB", "ldC")] + [
+        (n, C.c_void_p) for n in ("d_A", "d_D", "d_dt_bias", "d_start", "d_len", "d_state_in", "d_state_out", "d_slot")] + [
+        ("n_states", C.c_int32), ("reserved", C.c_int32), ("d_out", C.c_void_p), ("ldo", C.c_int64)]
 
 
 def lib_path() -> str:
@@ -172,6 +186,10 @@ def load_library():
     L.csb_verify_workspace_bytes.restype = C.c_size_t
     L.csb_verify_drafts.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64] + [C.c_void_p] * 4 + \
                                    [C.c_int32] * 3 + [C.c_void_p] * 4
+    L.csb_short_conv.argtypes = [C.POINTER(csb_conv_args), C.c_void_p]
+    L.csb_scan_workspace_bytes.argtypes = [C.POINTER(csb_scan_args)]
+    L.csb_scan_workspace_bytes.restype = C.c_size_t
+    L.csb_selective_scan.argtypes = [C.POINTER(csb_scan_args), C.c_void_p, C.c_void_p]
     L.csb_free.argtypes = [C.c_void_p]
     L.csb_free.restype = None
     L.csb_rnn_free.argtypes = [C.c_void_p]
@@ -186,6 +204,11 @@ def load_library():
         fn.argtypes = [C.c_char_p] + [C.c_void_p] * {"recurrent": 1, "chunked": 2, "workspace": 0}[key]
         fn.restype = C.c_size_t if key == "workspace" else C.c_int
         _raw_delta[key] = fn
+    for name, more in (("csb_short_conv", 1), ("csb_scan_workspace_bytes", 0), ("csb_selective_scan", 2)):      # (the same for these)
+        fn = L[name]
+        fn.argtypes = [C.c_char_p] + [C.c_void_p] * more
+        fn.restype = C.c_int if more else C.c_size_t
+        _raw[name] = fn
     _lib = L
     return L
 
@@ -468,6 +491,121 @@ def verify_drafts(p, q, drafts, u, r, counts=None, stream=None):
     if rc:
         _check(rc)
     return tokens, accepted
+
+
+def _rows(t, tokens, width) -> int:
+    """Elements from one token to the next of [tokens, width]."""
+    ld, one = t.stride()
+    assert one == 1 or width == 1, "a token's entries must be contiguous"
+    return ld if tokens > 1 else width
+
+
+def _sequences(starts, lens, slots, state) -> int:
+    """How many packed sequences a call has."""
+    if starts is not None:
+        n = starts.numel() - 1
+    elif lens is not None:
+        n = lens.numel()
+    elif slots is not None:
+        n = slots.numel()
+    else:
+        n = state.shape[0] if state is not None else 1
+    assert (lens is None or lens.numel() == n) and (slots is None or slots.numel() == n)
+    return n
+
+
+def _states(state, state_out, shape) -> int:
+    """How many states a call's tensors have room for."""
+    n = 0
+    for t in (state,) if state_out is state else (state, state_out):
+        if t is not None:
+            assert t.shape[1:] == shape and n in (0, t.shape[0])
+            n = t.shape[0]
+    return n
+
+
+def _changed(*tensors):
+    """Autograd may keep what has changed in place."""
+    torch = sys.modules["torch"]
+    for t in tensors:
+        if t is not None:
+            torch._C._increment_version((t,))
+
+
+_CONV_ARGS = struct.Struct("@6iqPq8Pq")                       # csb_conv_args and csb_scan_args, as ctypes lays them out
+_SCAN_ARGS = struct.Struct("@6iq5P5q8P2iPq")
+
+
+def short_conv(x, weight, bias=None, silu=True, starts=None, lens=None, state=None, slots=None, state_out=_KEEP, out=None, stream=None):
+    """csb_short_conv: the short causal convolution of a recurrent layer, channel by channel, and its activation.  x [tokens, channels]
+    (float32, float16 or bfloat16; rows may be strided), weight [channels, width] (the last column is the token's own) and bias [channels]
+    float32.  starts, lens and slots as delta_chunked; state [n_states, width - 1, channels] of x's dtype: the inputs before each sequence,
+    oldest first.  The last inputs go to state_out: `state` itself unless another tensor or None (not kept) is given.  Returns out [tokens, channels]
+    (a new tensor, or `out`, which must not overlap x)."""
+    if state_out is _KEEP:
+        state_out = state
+    if _elsewhere(stream):
+        return _on_stream(stream, short_conv, x, weight, bias, silu, starts, lens, state, slots, state_out, out)
+    torch = sys.modules["torch"]
+    T, CH = x.shape
+    CW, W = weight.shape
+    f32, i32, typ, given = torch.float32, torch.int32, x.dtype, out
+    here = _operands((x, weight, bias, state, state_out if state_out is not state else None, out), starts, lens, slots)
+    assert CW == CH and (bias is None or bias.numel() == CH)
+    if out is None:
+        out = torch.empty((T, CH), dtype=typ, device=x.device)
+    else:
+        assert out.shape == x.shape and out.dtype is typ
+    N = _sequences(starts, lens, slots, state)
+    n_states = _states(state, state_out, (W - 1, CH))
+    lib()
+    raw = _CONV_ARGS.pack(_val_type(typ), CH, W, bool(silu), N, n_states, T, x.data_ptr(), _rows(x, T, CH), _ptr(weight, f32), _ptr(bias, f32),
+                          _ptr(starts, i32), _ptr(lens, i32), _ptr(state, typ), _ptr(state_out, typ), _ptr(slots, i32), out.data_ptr(),
+                          _rows(out, T, CH))
+    rc = _raw["csb_short_conv"](raw, _raw_stream(here))
+    if rc:
+        _check(rc)
+    _changed(state_out, given)
+    return out
+
+
+def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, starts=None, lens=None, state=None, slots=None, state_out=_KEEP,
+                   out=None, stream=None):
+    """csb_selective_scan: the selective state space scan, for whole prompts and for the few tokens of a decoding step.  x, dt and z [tokens, channels],
+    B and C [tokens, groups, n] of one dtype (float32, float16, bfloat16; rows of tokens may be strided); A [channels, n], D and dt_bias
+    [channels] float32.  A token's step is ln(1 + e^(dt + dt_bias)), or dt + dt_bias without `softplus`; z: the gate (None: none).  starts, lens and slots as
+    delta_chunked; state [n_states, channels, n] float32, the last states go to state_out: `state` itself unless another tensor or None (not
+    kept) is given.  Returns out [tokens, channels] (a new tensor, or `out`, which may be x, dt or z)."""
+    if state_out is _KEEP:
+        state_out = state
+    if _elsewhere(stream):
+        return _on_stream(stream, selective_scan, x, dt, A, B, C, D, z, dt_bias, softplus, starts, lens, state, slots, state_out, out)
+    torch = sys.modules["torch"]
+    T, CH = shape = x.shape
+    _, G, n = B.shape
+    f32, i32, typ, given = torch.float32, torch.int32, x.dtype, out
+    here = _operands((x, dt, A, B, C, D, z, dt_bias, state, state_out if state_out is not state else None, out), starts, lens, slots)
+    assert dt.shape == shape and B.shape == C.shape == (T, G, n) and A.shape == (CH, n) and (z is None or z.shape == shape)
+    assert dt.dtype is B.dtype is C.dtype is typ and (z is None or z.dtype is typ)
+    assert (D is None or D.numel() == CH) and (dt_bias is None or dt_bias.numel() == CH)
+    if out is None:
+        out = torch.empty((T, CH), dtype=typ, device=x.device)
+    else:
+        assert out.shape == shape and out.dtype is typ
+    N = _sequences(starts, lens, slots, state)
+    n_states = _states(state, state_out, (CH, n))
+    lib()
+    raw = _SCAN_ARGS.pack(_val_type(typ), CH, G, n, bool(softplus), N, T, x.data_ptr(), dt.data_ptr(), z.data_ptr() if z is not None else 0,
+                          B.data_ptr(), C.data_ptr(), _rows(x, T, CH), _rows(dt, T, CH), _rows(z, T, CH) if z is not None else 0,
+                          _delta_rows(B, G, n, T), _delta_rows(C, G, n, T), _ptr(A, f32), _ptr(D, f32), _ptr(dt_bias, f32), _ptr(starts, i32),
+                          _ptr(lens, i32), _ptr(state, f32), _ptr(state_out, f32), _ptr(slots, i32), n_states, 0, out.data_ptr(),
+                          _rows(out, T, CH))
+    ws = _scratch(_raw["csb_scan_workspace_bytes"](raw), x.device)
+    rc = _raw["csb_selective_scan"](raw, ws.data_ptr() if ws is not None else None, _raw_stream(here))
+    if rc:
+        _check(rc)
+    _changed(state_out, given)
+    return out
 
 
 class CsbMatrix:

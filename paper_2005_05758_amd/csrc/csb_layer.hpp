@@ -1,0 +1,71 @@
+// What the kernels around a recurrent layer share (convolution, scan, norms): runs of eight elements of any type and alignment, and
+// the functions of gates.
+#pragma once
+
+#include "csb_lm.hpp"
+
+namespace csb {
+
+#ifdef __HIPCC__
+// Eight elements from p[0] on, of which the first `there` are (the others are zeros, or are not stored); p at any element.
+template <int VF> struct Run8 {
+    using T = typename Elem<VF>::T;
+    using T8 = T __attribute__((ext_vector_type(8)));
+    using T8_any = T __attribute__((ext_vector_type(8), aligned(sizeof(T)), may_alias));
+    T8 v;
+    __device__ __forceinline__ void load(const T *p, int there) {
+        if (there >= 8) v = *(const T8_any *)p;
+        else {
+            v = T8{};
+#pragma unroll
+            for (int j = 0; j < 7; ++j) if (j < there) v[j] = p[j];
+        }
+    }
+    __device__ __forceinline__ float operator[](int j) const { return (float)v[j]; }
+    __device__ __forceinline__ void set(int j, float x) { v[j] = (T)x; }
+    __device__ __forceinline__ void store(T *p, int there) const {
+        if (there >= 8) *(T8_any *)p = v;
+        else {
+#pragma unroll
+            for (int j = 0; j < 7; ++j) if (j < there) p[j] = v[j];
+        }
+    }
+};
+
+// e^x for x in [-104, 88], nearer ends taken for others (NaN too), to 2 units of 2^-24: the product with log2 e in two parts, as its rounding alone
+// would be |x| units off.
+__device__ __forceinline__ float exp_within(float x) {
+    x = __builtin_amdgcn_fmed3f(x, -104.0f, 88.0f);
+    const float p = x * 1.44269502162933349609375f;            // log2 e as the sum of two numbers
+    const float rest = fmaf(x, 1.44269502162933349609375f, -p) + x * 1.925963033500011079e-08f;
+    const float e = __builtin_amdgcn_exp2f(p);
+    return fmaf(e, rest * 0.693147182464599609375f, e);
+}
+// 1 / (1 + e^-x), as e^x / (1 + e^x) below zero: it goes to zero there, so that the product with any finite x does.  (NaN gives a
+// number: callers multiply by x, or look for it.)
+__device__ __forceinline__ float sigmoid_within(float x) {
+    const float e = exp_within(-fabsf(x));
+    return (x < 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e);
+}
+__device__ __forceinline__ float silu(float x) { return x * sigmoid_within(x); }
+
+// ln(1 + e^x) = max(x, 0) + ln(1 + e), e = e^-|x| in (0, 1]: 2 atanh(e / (2 + e)), whose series in (e / (2 + e))^2 <= 1/9 is cut where
+// 9^-8 / 17 is left (2^-29): small steps keep all of their digits, which ln(1 + e) of a rounded sum would not.
+__device__ __forceinline__ float softplus(float x) {
+    const float e = exp_within(-fabsf(x)), d = 2.0f + e;
+    float r = __builtin_amdgcn_rcpf(d);
+    r = fmaf(fmaf(-d, r, 1.0f), r, r);
+    const float s = e * r, w = s * s;
+    float p = 1.0f / 15.0f;
+    p = fmaf(p, w, 1.0f / 13.0f);
+    p = fmaf(p, w, 1.0f / 11.0f);
+    p = fmaf(p, w, 1.0f / 9.0f);
+    p = fmaf(p, w, 1.0f / 7.0f);
+    p = fmaf(p, w, 1.0f / 5.0f);
+    p = fmaf(p, w, 1.0f / 3.0f);
+    const float l = 2.0f * fmaf(s * w, p, s);
+    return x != x ? x : fmaxf(x, 0.0f) + l;
+}
+#endif
+
+}  // namespace csb

@@ -11,6 +11,8 @@ namespace csb {
 
 constexpr int64_t kMaxWorkgroups = (1 << 24) - 1;    // of 256 threads: a grid has fewer than 2^32 threads
 
+struct Refusal { int code; const char *what; };                               // CSB_OK: none
+
 inline bool known_type(int32_t type) { return type == CSB_VAL_F32 || type == CSB_VAL_F16 || type == CSB_VAL_BF16; }
 inline int32_t type_size(int32_t type) { return type == CSB_VAL_F32 ? 4 : 2; }
 

@@ -1,0 +1,287 @@
+// The selective state space scan (csb_selective_scan).
+//
+// Per channel c, with a state h of n numbers: h[j] <- exp(s A[j]) h[j] + s x B[j], y = sum_j C[j] h[j] + D x.  The exponentials bind: one of them,
+// two products and two fused products a (token, channel, number), 8 issue slots of which the exponential takes 4.  A channel's numbers lie with
+// four neighbouring lanes, K each, in registers from the first token to the last; a workgroup has 64 channels of one group, whose B and C come
+// through LDS once for all of them.  What is a token's and channel's alone (its step s through softplus, s x, the gate, types) is made once by
+// the lanes together, eight channels of a token each, and handed over through LDS; outputs come back in the same places.
+//
+// Few long sequences are split into chunks of 2^shift tokens: the decays of a chunk are exp(A sum s), so a chunk's effect is that factor and
+// the state that it leaves from zero.  The first launch makes these for all chunks but the last (and keeps the state in front of the first,
+// which the second launch replaces while others still need it), the second starts every chunk from the combination of those before it.
+#include <algorithm>
+#include <new>
+
+#include "csb_layer.hpp"
+
+namespace csb {
+
+constexpr int kScanTile = 32, kScanCols = 64, kScanRow = 2 * kScanCols + 32;      // tokens and channels in LDS; floats of a token's row there
+
+struct ScanDev {
+    const void *x, *dt, *z, *B, *C;
+    const float *A, *D, *bias;
+    const int32_t *start, *len, *slot;
+    const float *s_in;
+    float *s_out;
+    void *out;
+    float *begin, *sums;                       // [tiles][channels][n], [tiles][channels]
+    int64_t ldx, lddt, ldz, ldB, ldC, ldo, n_tokens, each;
+    int32_t channels, per_group, n, n_seq, n_states, softplus, shift, group_tiles, col_tiles;
+};
+
+// The value of lane `lane ^ N` of a lane's four neighbours.
+template <int N> __device__ __forceinline__ float quad_xor(float v) {
+    constexpr int order = N == 1 ? 0xb1 : 0x4e;
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), order, 0xf, 0xf, false));
+}
+
+// OUT: outputs and last states; else what the chunks before the last leave.  FULL: n is 4 K.
+template <int VF, int K, bool FULL, bool OUT>
+__global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
+    using T = typename Elem<VF>::T;
+    using Run = Run8<VF>;
+    __shared__ __attribute__((aligned(16))) float steps[kScanTile * kScanRow];   // s and s x of a token's channels, then y in place of s
+    __shared__ __attribute__((aligned(16))) float Bs[kScanTile * 4 * K];
+    __shared__ __attribute__((aligned(16))) float Cs[OUT ? kScanTile * 4 * K : 4];
+    const int tid = threadIdx.x;
+    const int64_t tile = blockIdx.x / a.col_tiles;
+    const int seq = tile_sequence(a.start, a.n_seq, a.n_tokens, a.shift, tile, a.each);
+    if (seq < 0) return;
+    int64_t first, end;
+    sequence_range(a.start, seq, a.each, a.n_tokens, &first, &end);
+    const int64_t tile0 = (first >> a.shift) + seq, number = tile - tile0;
+    if (a.len) end = first + clamp64(a.len[seq], 0, end - first);
+    const int64_t count = end - first, t0 = number << a.shift, each = (int64_t)1 << a.shift;
+    const bool last = t0 + each >= count;
+    if (number < 0 || (number > 0 && t0 >= count) || (!OUT && last)) return;     // (uniform)
+    const int32_t s = a.slot ? a.slot[seq] : seq;
+    const bool known = s >= 0 && s < a.n_states;
+    const int ct = (int)(blockIdx.x % a.col_tiles), group = ct / a.group_tiles;
+    const int col0 = (ct % a.group_tiles) * kScanCols, cols = min(kScanCols, a.per_group - col0);   // the workgroup's channels in its group
+    const int64_t base = (int64_t)group * a.per_group + col0;                    // its first channel
+
+    // a lane's numbers of a channel
+    const int c = tid >> 2, j0 = (tid & 3) * K;
+    const bool mine = c < cols;
+    auto have = [&](int k) { return FULL || j0 + k < a.n; };
+    const int64_t channel = base + (mine ? c : 0);
+    float A[K], h[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        A[k] = have(k) ? a.A[channel * a.n + j0 + k] * 1.44269502162933349609375f : 0.0f;
+        h[k] = 0.0f;
+    }
+    auto get = [&](const float *p) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) h[k] = have(k) ? p[channel * a.n + j0 + k] : 0.0f;
+    };
+    auto put = [&](float *p) {
+        if (!mine) return;
+#pragma unroll
+        for (int k = 0; k < K; ++k) if (have(k)) p[channel * a.n + j0 + k] = h[k];
+    };
+    const int64_t state = (int64_t)a.channels * a.n;
+    if (number == 0) {
+        if (OUT && !last) get(a.begin + tile * state);         // (kept by the first launch: the last chunk may have replaced it)
+        else if (a.s_in && known) get(a.s_in + s * state);
+        if (!OUT) put(a.begin + tile * state);
+    } else if (OUT) {
+        get(a.begin + (tile0 + 1) * state);
+        for (int64_t i = tile0 + 1; i < tile; ++i) {
+            const float sum = a.sums[i * a.channels + channel];
+            const float *p = a.begin + (i + 1) * state;
+#pragma unroll
+            for (int k = 0; k < K; ++k) h[k] = fmaf(__builtin_amdgcn_exp2f(sum * A[k]), h[k], have(k) ? p[channel * a.n + j0 + k] : 0.0f);
+        }
+    }
+
+    // the same thread makes what eight channels of a token need, and their outputs
+    const int sc = (tid & 7) * 8, st = tid >> 3, there = cols - sc;
+    float bias[8], D[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        bias[i] = a.bias && i < there ? a.bias[base + sc + i] : 0.0f;
+        D[i] = OUT && a.D && i < there ? a.D[base + sc + i] : 0.0f;
+    }
+    const int64_t stop = count < t0 + each ? count : t0 + each;
+    Run x, dt, z;
+    auto load = [&](int64_t t) {
+        x.v = dt.v = z.v = typename Run::T8{};
+        if (t + st < stop && there > 0) {
+            const int64_t at = first + t + st;
+            x.load((const T *)a.x + at * a.ldx + base + sc, there);
+            dt.load((const T *)a.dt + at * a.lddt + base + sc, there);
+            if (OUT && a.z) z.load((const T *)a.z + at * a.ldz + base + sc, there);
+        }
+    };
+    double total = 0.0;
+    for (int64_t t = t0; t < stop; t += kScanTile) {
+        const int live = (int)(stop - t < kScanTile ? stop - t : kScanTile);
+        load(t);
+        float *row = steps + st * kScanRow + 2 * sc;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float d = dt[i] + bias[i];
+            if (a.softplus) d = softplus(d);
+            if (st >= live) d = 0.0f;                          // (past the end: nothing decays, nothing comes in)
+            row[2 * i] = d;
+            row[2 * i + 1] = d * x[i];
+        }
+        for (int i = tid; i < kScanTile * 4 * K; i += 256) {
+            const int tt = i / (4 * K), j = i % (4 * K);
+            const bool in = tt < live && j < a.n;
+            Bs[i] = in ? (float)((const T *)a.B)[(first + t + tt) * a.ldB + (int64_t)group * a.n + j] : 0.0f;
+            if (OUT) Cs[i] = in ? (float)((const T *)a.C)[(first + t + tt) * a.ldC + (int64_t)group * a.n + j] : 0.0f;
+        }
+        __syncthreads();
+        float sum = 0.0f;
+        for (int i = 0; i < live; i += 4) {
+            float y[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float *d = steps + (i + u) * kScanRow + 2 * c, *b = Bs + (i + u) * 4 * K + j0, *cc = Cs + (i + u) * 4 * K + j0;
+                const float step = d[0], in = d[1];
+                y[u] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    h[k] = fmaf(__builtin_amdgcn_exp2f(step * A[k]), h[k], in * b[k]);
+                    if (!FULL) h[k] = have(k) ? h[k] : 0.0f;   // (infinite inputs make NaN of zeros)
+                    if (OUT) y[u] = fmaf(cc[k], h[k], y[u]);
+                }
+                if (!OUT) sum += step;
+            }
+            if (OUT) {                                         // lane q of four gets the sum of token i + q
+                const bool odd = tid & 1, high = tid & 2;
+                const float p0 = (odd ? y[1] : y[0]) + quad_xor<1>(odd ? y[0] : y[1]);
+                const float p1 = (odd ? y[3] : y[2]) + quad_xor<1>(odd ? y[2] : y[3]);
+                steps[(i + (tid & 3)) * kScanRow + 2 * c] = (high ? p1 : p0) + quad_xor<2>(high ? p0 : p1);
+            }
+        }
+        total += sum;
+        __syncthreads();
+        if (OUT && st < live && there > 0) {
+            Run o;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float y = fmaf(D[i], x[i], row[2 * i]);
+                if (a.z) y *= silu(z[i]);
+                o.set(i, y);
+            }
+            o.store((T *)a.out + (first + t + st) * a.ldo + base + sc, there);
+        }
+    }
+    if (OUT) {
+        if (last && a.s_out && known) put(a.s_out + s * state);
+    } else {
+        put(a.begin + (tile + 1) * state);
+        if (mine && (tid & 3) == 0) a.sums[tile * a.channels + channel] = (float)total;
+    }
+}
+
+// Chunks of a call, as a power of two of tokens (31: whole sequences).
+static int scan_shift(const csb_scan_args *a, int64_t col_tiles) {
+    int shift = 31;
+    const int64_t mean = a->n_tokens / a->n_seq;
+    if (a->n_seq * col_tiles < 1024 && mean >= 256) {
+        shift = 7;
+        while (shift < 31 && (mean >> shift) * a->n_seq * col_tiles > 1024) ++shift;
+        if (mean >> shift < 2) shift = 31;
+    }
+    return shift;
+}
+
+struct ScanPlan { int32_t group_tiles; int64_t col_tiles, tiles; int shift; size_t begin, bytes; };
+static Refusal scan_plan(const csb_scan_args *a, ScanPlan *p) {
+    if (!a) return {CSB_EINVAL, "NULL arguments"};
+    if (!known_type(a->type)) return {CSB_EINVAL, "unknown type"};
+    if (a->n_seq < 0 || a->n_tokens < 0 || a->channels < 1 || a->groups < 1 || a->n < 1) return {CSB_EINVAL, "bad size"};
+    if (a->channels % a->groups) return {CSB_EINVAL, "channels is no multiple of groups"};
+    if (a->n > 128) return {CSB_EUNSUPPORTED, "n above 128 (a channel's numbers are held in the registers of 4 lanes)"};
+    if (a->n_tokens > 0x7fffffff) return {CSB_EUNSUPPORTED, "offsets are 32-bit: more than 2^31 - 1 tokens"};
+    *p = ScanPlan{};
+    if (a->n_seq == 0) return {CSB_OK, nullptr};
+    p->group_tiles = (a->channels / a->groups + kScanCols - 1) / kScanCols;
+    p->col_tiles = (int64_t)p->group_tiles * a->groups;
+    p->shift = scan_shift(a, p->col_tiles);
+    p->tiles = tile_numbers(a->n_tokens, a->n_seq, p->shift);
+    if (p->tiles * p->col_tiles > kMaxWorkgroups) return {CSB_EUNSUPPORTED, "more workgroups than a launch takes"};
+    if (p->shift < 31) {
+        p->begin = ((size_t)p->tiles * a->channels * a->n * 4 + 255) / 256 * 256;
+        p->bytes = p->begin + ((size_t)p->tiles * a->channels * 4 + 255) / 256 * 256;
+    }
+    return {CSB_OK, nullptr};
+}
+
+template <int VF, int K, bool FULL>
+static void launch_scan(const ScanDev &d, dim3 grid, hipStream_t st) {
+    if (d.shift < 31) hipLaunchKernelGGL((selective_scan_kernel<VF, K, FULL, false>), grid, dim3(256), 0, st, d);
+    hipLaunchKernelGGL((selective_scan_kernel<VF, K, FULL, true>), grid, dim3(256), 0, st, d);
+}
+template <int VF, int K>
+static void launch_scan(const ScanDev &d, dim3 grid, hipStream_t st) {
+    if (d.n == 4 * K) launch_scan<VF, K, true>(d, grid, st);
+    else launch_scan<VF, K, false>(d, grid, st);
+}
+template <int VF>
+static void launch_scan(const ScanDev &d, dim3 grid, hipStream_t st) {
+    if (d.n <= 16) launch_scan<VF, 4>(d, grid, st);
+    else if (d.n <= 32) launch_scan<VF, 8>(d, grid, st);
+    else if (d.n <= 64) launch_scan<VF, 16>(d, grid, st);
+    else launch_scan<VF, 32>(d, grid, st);
+}
+
+}  // namespace csb
+
+extern "C" size_t csb_scan_workspace_bytes(const csb_scan_args *args) {
+    csb::ScanPlan p;
+    return csb::scan_plan(args, &p).code == CSB_OK ? p.bytes : 0;
+}
+
+extern "C" int csb_selective_scan(const csb_scan_args *a, void *d_ws, void *stream) {
+    using namespace csb;
+    const auto fail = [](int code, const char *what) { set_error(std::string("csb_selective_scan: ") + what); return code; };
+    ScanPlan p;
+    const Refusal sizes = scan_plan(a, &p);
+    if (sizes.code != CSB_OK) return fail(sizes.code, sizes.what);
+    if (!a->d_A || (a->n_tokens && (!a->d_x || !a->d_dt || !a->d_B || !a->d_C || !a->d_out))) return fail(CSB_EINVAL, "NULL pointer");
+    const int64_t w = a->channels, wn = (int64_t)a->groups * a->n;
+    if (a->ldx < w || a->lddt < w || a->ldo < w || (a->d_z && a->ldz < w) || a->ldB < wn || a->ldC < wn)
+        return fail(CSB_EINVAL, "a leading dimension below the width of its rows");
+    if (!a->d_start && a->n_seq && a->n_tokens % a->n_seq) return fail(CSB_EINVAL, "n_tokens is no multiple of n_seq (and there are no offsets)");
+    if ((a->d_state_in || a->d_state_out) && a->n_states < 1) return fail(CSB_EINVAL, "states without room for one");
+    if (((uintptr_t)a->d_x | (uintptr_t)a->d_dt | (uintptr_t)a->d_z | (uintptr_t)a->d_B | (uintptr_t)a->d_C | (uintptr_t)a->d_out) % (uintptr_t)type_size(a->type) ||
+        ((uintptr_t)a->d_A | (uintptr_t)a->d_D | (uintptr_t)a->d_dt_bias | (uintptr_t)a->d_state_in | (uintptr_t)a->d_state_out |
+         (uintptr_t)a->d_start | (uintptr_t)a->d_len | (uintptr_t)a->d_slot) % 4)
+        return fail(CSB_EINVAL, "misaligned pointer");
+    if (a->n_seq == 0) return CSB_OK;
+    if (p.bytes) {
+        if (!d_ws) return fail(CSB_EINVAL, "NULL workspace");
+        if ((uintptr_t)d_ws % 256) return fail(CSB_EINVAL, "workspace not 256-byte aligned");
+        try {
+            static const char scan_user = 0;                   // this entry point as a user of workspaces
+            workspace_changed_hands(d_ws, &scan_user);
+        } catch (const std::bad_alloc &) {
+            return fail(CSB_ENOMEM, "out of host memory");
+        }
+    }
+    ScanDev d{};
+    d.x = a->d_x; d.dt = a->d_dt; d.z = a->d_z; d.B = a->d_B; d.C = a->d_C;
+    d.A = a->d_A; d.D = a->d_D; d.bias = a->d_dt_bias;
+    d.start = a->d_start; d.len = a->d_len; d.slot = a->d_slot; d.s_in = a->d_state_in; d.s_out = a->d_state_out; d.out = a->d_out;
+    d.begin = (float *)d_ws; d.sums = (float *)((char *)d_ws + p.begin);
+    d.ldx = a->ldx; d.lddt = a->lddt; d.ldz = a->ldz; d.ldB = a->ldB; d.ldC = a->ldC; d.ldo = a->ldo;
+    d.n_tokens = a->n_tokens; d.each = a->n_tokens / a->n_seq;
+    d.channels = a->channels; d.per_group = a->channels / a->groups; d.n = a->n; d.n_seq = a->n_seq; d.n_states = a->n_states;
+    d.softplus = a->softplus; d.shift = p.shift; d.group_tiles = p.group_tiles; d.col_tiles = (int32_t)p.col_tiles;
+    const dim3 grid((uint32_t)(p.tiles * p.col_tiles));
+    hipStream_t st = (hipStream_t)stream;
+    switch (a->type) {
+        case CSB_VAL_F32: launch_scan<CSB_VAL_F32>(d, grid, st); break;
+        case CSB_VAL_F16: launch_scan<CSB_VAL_F16>(d, grid, st); break;
+        default: launch_scan<CSB_VAL_BF16>(d, grid, st); break;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(CSB_EDEVICE, hipGetErrorString(e));
+    return CSB_OK;
+}

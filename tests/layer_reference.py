@@ -1,0 +1,88 @@
+"""The operators around a recurrent layer from their definitions, in 64 bits on the host, with what rounding may add to each
+result (test infrastructure).
+
+U = 2^-24 is half a unit in the last place of binary32.  The bounds follow the sums as they are formed: a sum of n terms in any order is
+off by at most n U of its terms' absolute values, a product by U, the card's exponential of a binary32 number by 2 U, its reciprocal by 2 U."""
+import numpy as np
+
+U = 2.0 ** -24
+HALF = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}   # half a unit in the last place, of the value
+TINY = {"f32": 2.0 ** -126, "f16": 2.0 ** -24, "bf16": 2.0 ** -126}   # numbers below the normal ones
+
+
+def widen(t):
+    """A torch tensor of any float type as float64 numbers (every value of the types is one)."""
+    return t.detach().cpu().double().numpy()
+
+
+def sigmoid(x):
+    with np.errstate(over="ignore"):
+        return 1.0 / (1.0 + np.exp(-x))
+
+
+def silu(x):
+    return x * sigmoid(x)
+
+
+def conv(x, w, b, act, ranges, slots, state):
+    """x [T, C], w [C, W], state [n, W - 1, C].  Returns (out, off, state): out is NaN where no sequence has a token."""
+    T, C = x.shape
+    W = w.shape[1]
+    out, off, state = np.full((T, C), np.nan), np.zeros((T, C)), state.copy()
+    for (first, end), s in zip(ranges, slots):
+        v = np.concatenate([state[s] if s >= 0 else np.zeros((W - 1, C)), x[first:end]])
+        n = end - first
+        y = b + sum(v[j:j + n] * w[:, j] for j in range(W))
+        size = np.abs(b) + sum(np.abs(v[j:j + n] * w[:, j]) for j in range(W))
+        out[first:end] = silu(y) if act else y
+        # the sum: W + 1 roundings.  SiLU's slope is at most 1.1; its exponential 4 U (argument and all), sum, reciprocal and product 4 U more
+        off[first:end] = 1.1 * (W + 1) * U * size + 8 * U * np.abs(out[first:end])
+        if s >= 0 and W > 1:
+            state[s] = v[n:]
+    return out, off, state
+
+
+def scan(x, dt, A, B, C, D, z, bias, softplus, ranges, slots, state):
+    """x, dt, z [T, ch], B, C [T, G, n], A [ch, n], state [S, ch, n].  Returns (out, off, state, state_off)."""
+    T, ch = x.shape
+    G, n = B.shape[1:]
+    out, off = np.full((T, ch), np.nan), np.zeros((T, ch))
+    state, soff = state.copy(), np.zeros(state.shape)
+    step = dt + bias
+    # dt + bias: U of it; ln(1 + e^s) has a slope of at most 1 and 12 U of its own (exponential 4, quotient 4, series and sum 4)
+    step_off = U * np.abs(step)
+    if softplus:
+        step = np.maximum(step, 0.0) + np.log1p(np.exp(-np.abs(step)))
+        slope = -np.expm1(-step)
+        step_off = slope * step_off + 12 * U * step
+    gate = silu(z) if z is not None else np.ones((T, ch))
+    for (first, end), s in zip(ranges, slots):
+        h = state[s].copy() if s >= 0 else np.zeros((ch, n))
+        size, e = np.abs(h), np.zeros((ch, n))
+        for t in range(first, end):
+            b, c = (np.repeat(m[t], ch // G, axis=0) for m in (B, C))
+            arg = step[t][:, None] * A
+            a = np.exp(arg)
+            # the argument: A log2 e and the product rounded, the step's error; over chunks the sum of the steps may be 40 U off; then the exponential
+            # and the fused product and sum
+            arg_off = step_off[t][:, None] * np.abs(A) + 43 * U * np.abs(arg)
+            into = step[t][:, None] * x[t][:, None] * b
+            into_off = (step_off[t] * np.abs(x[t]))[:, None] * np.abs(b) + 3 * U * np.abs(into)
+            e = a * e + (arg_off + 4 * U) * a * size + into_off
+            h, size = a * h + into, a * size + np.abs(into)
+            y = (c * h).sum(1) + D * x[t]
+            y_off = (np.abs(c) * e).sum(1) + (n + 3) * U * ((np.abs(c) * size).sum(1) + np.abs(D * x[t]))
+            out[t] = y * gate[t]
+            off[t] = np.abs(gate[t]) * (1.001 * y_off + 9 * U * np.abs(y))
+        if s >= 0:
+            state[s], soff[s] = h, 1.001 * e
+    return out, off, state, soff
+
+
+def within(got, want, off, fmt):
+    """How far entries are outside of what they may be, the type's rounding included (not above 0: fine)."""
+    there = ~np.isnan(want)
+    if not there.any():
+        return 0.0
+    allowed = off[there] + HALF[fmt] * (np.abs(want[there]) + off[there]) + TINY[fmt]
+    return float((np.abs(got[there] - want[there]) - allowed).max())
