@@ -217,6 +217,68 @@ typedef struct {
 size_t csb_scan_workspace_bytes(const csb_scan_args *args);
 int csb_selective_scan(const csb_scan_args *args, void *d_ws, void *stream);
 
+/*
+ * Norms around a block of a model.  Per token, with the block's output y, a gate, the residual stream x, all but one of y and x optional:
+ *     q = y, or y act(gate) with `gate_first`;   p = norm_after(q), times act(gate) where the gate was not first;
+ *     r = x + scale s[j] p[j]   (without x: scale s p; without y: x; s NULL: 1);   out = norm_before(r),
+ * norm(v)[j] = (v[j] - m) / sqrt(mean((v - m)^2) + eps) w[j] + b[j] with m = mean(v) (CSB_NORM_MEAN), or m = 0 (CSB_NORM_RMS; w NULL: 1, b
+ * NULL: 0), CSB_NORM_NONE: v itself; act(v) = v / (1 + e^-v) (CSB_GATE_SILU) or 1 / (1 + e^-v) (CSB_GATE_SIGMOID).
+ * norm_after is taken over `groups` equal parts of a token's entries, each by itself.  Every operand has a type and an order of its own:
+ * element (t, j) is at t * ld + j, or at j * ld + t with `columns`, which is how csb_spmm* take and leave their operands.
+ * d_out of r and of norm_before(r) (both [n_tokens][width]; r may be NULL where norm_before is asked for) are each rounded once, and
+ * norm_before is that of r before its rounding.  An output may be an input itself (same pointer, type, order and ld), and must not overlap one
+ * otherwise.  Products and sums are binary32, a norm's sums binary64: entries of any finite size have their norm.  What is not finite in
+ * a token's entries stays in that token (in its group where there are several).
+ * Errors: NULL, sizes, types or leading dimensions out of range, width no multiple of groups, a gate or norm_after without y, norms or gates unknown ->
+ * CSB_EINVAL; width / groups > 32768, norm_before with several groups, or more workgroups than a launch takes -> CSB_EUNSUPPORTED; launch failure ->
+ * CSB_EDEVICE.  n_tokens = 0 does nothing.  Bitwise reproducible, one launch, no workspace.
+ */
+#define CSB_NORM_NONE 0
+#define CSB_NORM_RMS 1
+#define CSB_NORM_MEAN 2
+#define CSB_GATE_SILU 0
+#define CSB_GATE_SIGMOID 1
+typedef struct {
+    void *d;                               /* NULL: not there                                */
+    int64_t ld;
+    int32_t type;                          /* CSB_VAL_*                                      */
+    int32_t columns;                       /* (t, j) at j * ld + t                           */
+} csb_norm_operand;
+typedef struct {
+    int64_t n_tokens;
+    int32_t width, groups;
+    int32_t after, before;                 /* CSB_NORM_*                                     */
+    int32_t gate_kind, gate_first;         /* CSB_GATE_*                                     */
+    float scale, eps;
+    csb_norm_operand y, gate, x, r, out;
+    const float *d_after_w, *d_after_b, *d_scale, *d_before_w, *d_before_b;      /* [width], or NULL */
+} csb_norm_args;
+
+int csb_block_norm(const csb_norm_args *args, void *stream);
+
+/*
+ * Sampling.  Row i of logits is at d_logits + i * ld, of `type`; NaN counts as -infinity.  With m the row's largest logit and T
+ * = d_temperature[i] (NULL: 1), token v has the weight floor(2^38 e^((logit - m) / T)) in whole units (2^38 for every logit that is m; the
+ * exponential in binary64, to 2^-40 of itself).  T not above zero, or NaN: the first token of the order has all of the weight.  The order is by logit, largest first,
+ * equal ones by their number, lowest first.  Kept are
+ *     the first k = d_top_k[i] tokens of the order (NULL, or k < 1: all);
+ *     of these, the ones with fewer units before them than floor(their units * floor(p 2^24) / 2^24), p = d_top_p[i], and the first (NULL, or p
+ *     not below 1: all);
+ *     of these, the ones of at least floor(min(q, 1) 2^38) units, q = d_min_p[i] (NULL, or q not above 0: all).
+ * Token d_tokens[i] is drawn from what is kept by inversion, as csb_verify_drafts does: the lowest whose cumulated units, by number,
+ * exceed floor(units of the row * floor(r 2^24) / 2^24), r = d_r[i] in [0, 1) given by the caller; -1 where every logit is -infinity or NaN.
+ * d_probs (NULL: not wanted): row i of the distribution drawn from, at d_probs + i * ldprobs, of `type`: units over the row's units, rounded once, zero for
+ * tokens that are not kept; what csb_verify_drafts takes as p and q.  With d_tokens NULL (d_r may be too) only that is made.  It must not overlap the logits,
+ * or be them (same pointer and leading dimension).  Whole units: the result depends neither on the order nor on the split of a sum.
+ * d_ws: csb_sample_workspace_bytes(n_rows, vocab) bytes (0 up to a vocabulary of 24576: d_ws may be NULL then).  One launch up to there, else three to five.
+ * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, an unknown type -> CSB_EINVAL; vocab > 2^24, n_rows > 2^21, or
+ * more workgroups than a launch takes -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.  n_rows = 0 does nothing.
+ */
+size_t csb_sample_workspace_bytes(int32_t n_rows, int32_t vocab);
+int csb_sample(int32_t type, const void *d_logits, int64_t ld, const float *d_temperature, const int32_t *d_top_k,
+               const float *d_top_p, const float *d_min_p, const float *d_r, int32_t n_rows, int32_t vocab,
+               int32_t *d_tokens, void *d_probs, int64_t ldprobs, void *d_ws, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -40,7 +40,8 @@ SYMBOLS = ["csb_last_error", "csb_pack", "csb_view_get", "csb_unpack", "csb_set_
            "csb_rnn_set_poll_limit", "csb_rnn_status", "csb_rnn_workspace_bytes", "csb_rnn_forward", "csb_free", "csb_rnn_free",
            # include/csbrnn_lm.h
            "csb_delta_recurrent", "csb_delta_workspace_bytes", "csb_delta_chunked", "csb_adapter_workspace_bytes", "csb_adapter_add",
-           "csb_verify_workspace_bytes", "csb_verify_drafts", "csb_short_conv", "csb_scan_workspace_bytes", "csb_selective_scan"]
+           "csb_verify_workspace_bytes", "csb_verify_drafts", "csb_short_conv", "csb_scan_workspace_bytes", "csb_selective_scan",
+           "csb_block_norm", "csb_sample_workspace_bytes", "csb_sample"]
 
 
 class csb_sharing_stats(C.Structure):
@@ -100,6 +101,16 @@ class csb_scan_args(C.Structure):
         (n, C.c_void_p) for n in ("d_x", "d_dt", "d_z", "d_B", "d_C")] + [(n, C.c_int64) for n in ("ldx", "lddt", "ldz", "ldB", "ldC")] + [
         (n, C.c_void_p) for n in ("d_A", "d_D", "d_dt_bias", "d_start", "d_len", "d_state_in", "d_state_out", "d_slot")] + [
         ("n_states", C.c_int32), ("reserved", C.c_int32), ("d_out", C.c_void_p), ("ldo", C.c_int64)]
+
+
+class csb_norm_operand(C.Structure):
+    _fields_ = [("d", C.c_void_p), ("ld", C.c_int64), ("type", C.c_int32), ("columns", C.c_int32)]
+
+
+class csb_norm_args(C.Structure):
+    _fields_ = [("n_tokens", C.c_int64)] + [(n, C.c_int32) for n in ("width", "groups", "after", "before", "gate_kind", "gate_first")] + [
+        ("scale", C.c_float), ("eps", C.c_float)] + [(n, csb_norm_operand) for n in ("y", "gate", "x", "r", "out")] + [
+        (n, C.c_void_p) for n in ("d_after_w", "d_after_b", "d_scale", "d_before_w", "d_before_b")]
 
 
 def lib_path() -> str:
@@ -190,6 +201,10 @@ def load_library():
     L.csb_scan_workspace_bytes.argtypes = [C.POINTER(csb_scan_args)]
     L.csb_scan_workspace_bytes.restype = C.c_size_t
     L.csb_selective_scan.argtypes = [C.POINTER(csb_scan_args), C.c_void_p, C.c_void_p]
+    L.csb_block_norm.argtypes = [C.POINTER(csb_norm_args), C.c_void_p]
+    L.csb_sample_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
+    L.csb_sample_workspace_bytes.restype = C.c_size_t
+    L.csb_sample.argtypes = [C.c_int32, C.c_void_p, C.c_int64] + [C.c_void_p] * 5 + [C.c_int32] * 2 + [C.c_void_p] * 2 + [C.c_int64] + [C.c_void_p] * 2
     L.csb_free.argtypes = [C.c_void_p]
     L.csb_free.restype = None
     L.csb_rnn_free.argtypes = [C.c_void_p]
@@ -204,7 +219,7 @@ def load_library():
         fn.argtypes = [C.c_char_p] + [C.c_void_p] * {"recurrent": 1, "chunked": 2, "workspace": 0}[key]
         fn.restype = C.c_size_t if key == "workspace" else C.c_int
         _raw_delta[key] = fn
-    for name, more in (("csb_short_conv", 1), ("csb_scan_workspace_bytes", 0), ("csb_selective_scan", 2)):      # (the same for these)
+    for name, more in (("csb_short_conv", 1), ("csb_scan_workspace_bytes", 0), ("csb_selective_scan", 2), ("csb_block_norm", 1)):      # (the same for these)
         fn = L[name]
         fn.argtypes = [C.c_char_p] + [C.c_void_p] * more
         fn.restype = C.c_int if more else C.c_size_t
@@ -606,6 +621,93 @@ def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, 
         _check(rc)
     _changed(state_out, given)
     return out
+
+
+_NORM_ARGS = struct.Struct("@q6i2f" + "Pq2i" * 5 + "5P")       # csb_norm_args, as ctypes lays it out
+_NORMS = {None: 0, "rms": 1, "mean": 2}
+_GATES = {"silu": 0, "sigmoid": 1}
+
+
+def _order(t, shape):
+    """A csb_norm_operand of [tokens, width]: rows or columns (a transposed view) by its strides."""
+    if t is None:
+        return 0, 0, 0, 0
+    assert t.shape == shape
+    (a, b), (tokens, width) = t.stride(), shape
+    if b == 1 or width == 1:
+        return t.data_ptr(), a if tokens > 1 else width, _val_type(t.dtype), 0
+    assert a == 1 or tokens == 1, "entries of a token, or of all tokens at one place, must be contiguous"
+    return t.data_ptr(), b, _val_type(t.dtype), 1
+
+
+def block_norm(y=None, gate=None, x=None, after=None, after_weight=None, after_bias=None, groups=1, gate_kind="silu", gate_first=False, scale=1.0,
+               scales=None, before=None, before_weight=None, before_bias=None, eps=1e-5, out=None, normed=None, stream=None):
+    """csb_block_norm: norms around a block.  y [tokens, width] is the block's output, x the residual stream (one of them may be None), gate
+    a gate; float32, float16 or bfloat16, each by itself, row by row or transposed views of column by column (a product's operands: Y.t()).
+        p = norm_after(y), times act(gate) behind it, or before it with `gate_first`;  r = x + scale scales p;  n = norm_before(r)
+    after, before: None, "rms" or "mean" (with the mean taken off), their weights and biases and scales [width] float32 (None: ones, zeros).
+    groups: norm_after is over that many equal parts of a token.  gate_kind: "silu" or "sigmoid".  Returns (r, n): new tensors of x's dtype (y's without x)
+    or `out` and `normed`; n is None without a norm before, r is x itself where there is no y and no `out`."""
+    if _elsewhere(stream):
+        return _on_stream(stream, block_norm, y, gate, x, after, after_weight, after_bias, groups, gate_kind, gate_first, scale, scales, before,
+                          before_weight, before_bias, eps, out, normed)
+    torch = sys.modules["torch"]
+    main = x if x is not None else y
+    T, W = shape = main.shape
+    f32 = torch.float32
+    factors = (after_weight, after_bias, scales, before_weight, before_bias)
+    here = _operands((main, y, gate, *factors, out, normed))
+    for w in factors:
+        assert w is None or w.numel() == W
+    assert before is not None or normed is None
+    given, given_n, r = out, normed, out
+    if out is None:
+        if y is None and before is not None:
+            r = x
+        else:
+            r = out = torch.empty((T, W), dtype=main.dtype, device=main.device)
+    if before is not None and normed is None:
+        normed = torch.empty((T, W), dtype=main.dtype, device=main.device)
+    lib()
+    raw = _NORM_ARGS.pack(T, W, groups, _NORMS[after], _NORMS[before], _GATES[gate_kind], bool(gate_first), scale, eps, *_order(y, shape), *_order(gate, shape),
+                          *_order(x, shape), *_order(out, shape), *_order(normed, shape), *(_ptr(w, f32) for w in factors))
+    rc = _raw["csb_block_norm"](raw, _raw_stream(here))
+    if rc:
+        _check(rc)
+    _changed(given, given_n)
+    return r, normed
+
+
+def sample(logits, r=None, temperature=None, top_k=None, top_p=None, min_p=None, probs=False, stream=None):
+    """csb_sample: the next token of every row of logits [rows, vocab] (float32, float16 or bfloat16; rows may be strided) from r [rows] float32, numbers
+    in [0, 1).  temperature (0: the largest logit), top_p, min_p [rows] float32 and top_k [rows] int32 (None: 1, and all).  Returns tokens [rows]
+    int32; with `probs` (tokens, the distribution that they are drawn from [rows, vocab] of logits' dtype, what verify_drafts takes); with r None that alone.
+    probs may be a tensor that the distribution is written to (logits itself among them)."""
+    if _elsewhere(stream):
+        return _on_stream(stream, sample, logits, r, temperature, top_k, top_p, min_p, probs)
+    torch = sys.modules["torch"]
+    R, V = logits.shape
+    i32, f32, typ, dev = torch.int32, torch.float32, logits.dtype, logits.device
+    given = None if isinstance(probs, bool) else probs
+    here = _operands((logits, r, temperature, top_p, min_p, given if given is not logits else None), top_k)
+    for t in (r, temperature, top_k, top_p, min_p):
+        assert t is None or t.numel() == R
+    assert r is not None or probs is not False, "neither tokens nor their distribution"
+    dist = given
+    if given is not None:
+        assert given.shape == logits.shape and given.dtype is typ
+    elif probs:
+        dist = torch.empty((R, V), dtype=typ, device=dev)
+    tokens = torch.empty(R, dtype=i32, device=dev) if r is not None else None
+    L = lib()
+    ws = _scratch(L.csb_sample_workspace_bytes(R, V), dev)
+    rc = L.csb_sample(_val_type(typ), logits.data_ptr(), _rows(logits, R, V), _ptr(temperature, f32), _ptr(top_k, i32), _ptr(top_p, f32), _ptr(min_p, f32),
+                      _ptr(r, f32), R, V, _ptr(tokens, i32), dist.data_ptr() if dist is not None else None, _rows(dist, R, V) if dist is not None else 0,
+                      ws.data_ptr() if ws is not None else None, _raw_stream(here))
+    if rc:
+        _check(rc)
+    _changed(given)
+    return tokens if dist is None else dist if tokens is None else (tokens, dist)
 
 
 class CsbMatrix:

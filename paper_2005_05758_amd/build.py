@@ -9,7 +9,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcsbrnn.so")
-SOURCES = ["csb_pack.cpp", "csb_plan.cpp", "csb_stream.cpp", "csb_quad.cpp", "csb_sharing.cpp", "csb_spmv.hip", "csb_spmv_stream.hip", "csb_spmm.hip", "csb_spmm_quad.hip", "csb_project.hip", "csb_rnn.hip", "csb_delta.hip", "csb_delta_chunk.hip", "csb_adapter.hip", "csb_verify.hip", "csb_conv.hip", "csb_scan.hip"]
+SOURCES = ["csb_pack.cpp", "csb_plan.cpp", "csb_stream.cpp", "csb_quad.cpp", "csb_sharing.cpp", "csb_spmv.hip", "csb_spmv_stream.hip", "csb_spmm.hip", "csb_spmm_quad.hip", "csb_project.hip", "csb_rnn.hip", "csb_delta.hip", "csb_delta_chunk.hip", "csb_adapter.hip", "csb_verify.hip", "csb_conv.hip", "csb_scan.hip", "csb_norm.hip", "csb_sample.hip"]
 
 
 def hipcc() -> str:

@@ -86,3 +86,81 @@ def within(got, want, off, fmt):
         return 0.0
     allowed = off[there] + HALF[fmt] * (np.abs(want[there]) + off[there]) + TINY[fmt]
     return float((np.abs(got[there] - want[there]) - allowed).max())
+
+
+def norm(y, gate, x, after, aw, ab, groups, sigmoid_gate, gate_first, scale, s, before, bw, bb, eps):
+    """All [T, W] or None (weights [W]).  Returns (r, off, n, off): n None without a norm before."""
+    T, W = (x if x is not None else y).shape
+
+    def unit(v, e, kind, w, b, parts):
+        """norm(v) of entries that are off by e, and how far its own are: v - m is off by e's and the mean's, the factor by what its
+        root of a mean square is, 2 U of its own; the product, w and b 4 U more."""
+        if not kind:
+            return v, e
+        v, e = v.reshape(T, parts, -1), e.reshape(T, parts, -1)
+        if kind == "mean":
+            v, e = v - v.mean(-1, keepdims=True), e + e.mean(-1, keepdims=True) + U * np.abs(v - v.mean(-1, keepdims=True))
+        ms = (v * v).mean(-1, keepdims=True) + eps
+        f = 1.0 / np.sqrt(ms)
+        f_off = f * ((np.abs(v) * e).mean(-1, keepdims=True) / ms + 3 * U)
+        out = (v * f).reshape(T, W)
+        off = (e * f + np.abs(v) * f_off).reshape(T, W) + 2 * U * np.abs(out)
+        w, b = w if w is not None else np.ones(W), b if b is not None else np.zeros(W)
+        return out * w + b, off * np.abs(w) + 2 * U * (np.abs(out * w) + np.abs(b))
+    r, off = np.zeros((T, W)), np.zeros((T, W))
+    if y is not None:
+        r = y.copy()
+        act = None
+        if gate is not None:
+            act = sigmoid(gate) if sigmoid_gate else silu(gate)
+        if act is not None and gate_first:
+            r, off = r * act, 9 * U * np.abs(r * act)
+        r, off = unit(r, off, after, aw, ab, groups)
+        if act is not None and not gate_first:
+            r, off = r * act, off * np.abs(act) + 9 * U * np.abs(r * act)
+        m = scale * (s if s is not None else np.ones(W))
+        r, off = r * m, (off + 3 * U * np.abs(r)) * np.abs(m)
+    if x is not None:
+        r = r + x
+        off = off + U * np.abs(r)
+    off = 1.001 * off
+    if not before:
+        return r, off, None, None
+    n, n_off = unit(r, off, before, bw, bb, 1)
+    return r, off, n, 1.001 * n_off
+
+
+UNITS = 2.0 ** 38
+
+
+def sample(s, T, k, p, q, r):
+    """One row s of float64 logits (values of the type); T, k, p, q, r numbers of the types that they are given in.  Returns (token, weights that are kept)."""
+    s = np.where(np.isnan(s), -np.inf, s)
+    V, m = len(s), s.max()
+    kept = np.zeros(V, np.int64)
+    if m == -np.inf:
+        return -1, kept
+    order = np.lexsort((np.arange(V), -s))
+    w = np.zeros(V, np.int64)
+    if T > 0:
+        with np.errstate(all="ignore"):
+            d = (s - m) / T
+            w = np.where(s == m, UNITS, np.where(d > -40, np.floor(np.exp(d) * UNITS), 0.0)).astype(np.int64)
+    else:
+        w[order[0]] = int(UNITS)
+    keep = order
+    if 0 < k < V:
+        keep = keep[:k]
+    if p < 1:
+        units = [int(u) for u in w[keep]]
+        limit, before, n = sum(units) * int(max(p, 0.0) * 2 ** 24) >> 24, 0, 0
+        while n < len(units) and (before < limit or n == 0):
+            before += units[n]
+            n += 1
+        keep = keep[:n]
+    if q > 0:
+        keep = keep[w[keep] >= int(min(q, 1.0) * UNITS)]
+    kept[keep] = w[keep]
+    total = int(kept.sum())
+    limit = total * min(int(max(r, 0.0) * 2 ** 24), 2 ** 24 - 1) >> 24
+    return int(np.searchsorted(np.cumsum(kept), limit, side="right")), kept
