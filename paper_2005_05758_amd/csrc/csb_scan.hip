@@ -17,6 +17,7 @@
 namespace csb {
 
 constexpr int kScanTile = 32, kScanCols = 64, kScanRow = 2 * kScanCols + 32;      // tokens and channels in LDS; floats of a token's row there
+constexpr int kScanFew = 8;                    // tokens a sequence, on average, up to which wavefronts work alone
 
 struct ScanDev {
     const void *x, *dt, *z, *B, *C;
@@ -179,6 +180,80 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
     }
 }
 
+// The same for the few tokens of a decoding step: a wavefront takes 16 channels by itself, without LDS and barriers, and its four lanes a
+// channel make the step alike.  The next token's operands are on their way while one is worked on.
+template <int VF, int K, bool FULL>
+__global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a, const uint32_t waves) {
+    using T = typename Elem<VF>::T;
+    constexpr int W = K < 8 ? K : 8;
+    using TK = T __attribute__((ext_vector_type(W)));
+    using TK_any = T __attribute__((ext_vector_type(W), aligned(sizeof(T)), may_alias));
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (wave >= waves) return;                                 // (no barrier in this kernel)
+    const int seq = (int)(wave / (uint32_t)a.col_tiles), ct = (int)(wave % (uint32_t)a.col_tiles), group = ct / a.group_tiles;
+    int64_t first, end;
+    sequence_range(a.start, seq, a.each, a.n_tokens, &first, &end);
+    if (a.len) end = first + clamp64(a.len[seq], 0, end - first);
+    const int32_t s = a.slot ? a.slot[seq] : seq;
+    const bool known = s >= 0 && s < a.n_states;
+    const int c = (ct % a.group_tiles) * 16 + (int)(lane >> 2), j0 = (int)(lane & 3u) * K;
+    const bool mine = c < a.per_group;
+    const int64_t channel = (int64_t)group * a.per_group + (mine ? c : 0);
+    auto have = [&](int k) { return FULL || j0 + k < a.n; };
+    struct Token { TK b[K / W], c[K / W]; T x, dt, z; };
+    auto numbers = [&](const T *p, TK *v) {
+#pragma unroll
+        for (int i = 0; i < K / W; ++i) {
+            if (FULL || j0 + W * (i + 1) <= a.n) v[i] = *(const TK_any *)(p + W * i);
+            else {
+                v[i] = TK{};
+#pragma unroll
+                for (int j = 0; j < W; ++j) if (have(W * i + j)) v[i][j] = p[W * i + j];
+            }
+        }
+    };
+    auto load = [&](int64_t t, Token &w) {
+        numbers((const T *)a.B + t * a.ldB + (int64_t)group * a.n + j0, w.b);
+        numbers((const T *)a.C + t * a.ldC + (int64_t)group * a.n + j0, w.c);
+        w.x = ((const T *)a.x)[t * a.ldx + channel];
+        w.dt = ((const T *)a.dt)[t * a.lddt + channel];
+        w.z = a.z ? ((const T *)a.z)[t * a.ldz + channel] : (T)0.0f;
+    };
+    Token now{}, next{};
+    if (first < end) load(first, now);
+    float A[K], h[K];
+    const int64_t state = (int64_t)s * a.channels * a.n + channel * a.n + j0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        A[k] = have(k) ? a.A[channel * a.n + j0 + k] * 1.44269502162933349609375f : 0.0f;
+        h[k] = a.s_in && known && have(k) ? a.s_in[state + k] : 0.0f;
+    }
+    const float bias = a.bias ? a.bias[channel] : 0.0f, D = a.D ? a.D[channel] : 0.0f;
+    for (int64_t t = first; t < end; ++t) {
+        if (t + 1 < end) load(t + 1, next);
+        const float x = (float)now.x;
+        float step = (float)now.dt + bias, y = 0.0f;
+        if (a.softplus) step = softplus(step);
+        const float in = step * x;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            h[k] = fmaf(__builtin_amdgcn_exp2f(step * A[k]), h[k], in * (float)now.b[k / W][k % W]);
+            if (!FULL) h[k] = have(k) ? h[k] : 0.0f;
+            y = fmaf((float)now.c[k / W][k % W], h[k], y);
+        }
+        y += quad_xor<1>(y);
+        y += quad_xor<2>(y);
+        y = fmaf(D, x, y);
+        if (a.z) y *= silu((float)now.z);
+        if (mine && (lane & 3u) == 0) ((T *)a.out)[t * a.ldo + channel] = (T)y;
+        now = next;
+    }
+    if (a.s_out && known && mine)
+#pragma unroll
+        for (int k = 0; k < K; ++k) if (have(k)) a.s_out[state + k] = h[k];
+}
+
 // Chunks of a call, as a power of two of tokens (31: whole sequences).
 static int scan_shift(const csb_scan_args *a, int64_t col_tiles) {
     int shift = 31;
@@ -191,7 +266,7 @@ static int scan_shift(const csb_scan_args *a, int64_t col_tiles) {
     return shift;
 }
 
-struct ScanPlan { int32_t group_tiles; int64_t col_tiles, tiles; int shift; size_t begin, bytes; };
+struct ScanPlan { int32_t group_tiles; int64_t col_tiles, tiles; int shift; bool few; size_t begin, bytes; };
 static Refusal scan_plan(const csb_scan_args *a, ScanPlan *p) {
     if (!a) return {CSB_EINVAL, "NULL arguments"};
     if (!known_type(a->type)) return {CSB_EINVAL, "unknown type"};
@@ -201,10 +276,12 @@ static Refusal scan_plan(const csb_scan_args *a, ScanPlan *p) {
     if (a->n_tokens > 0x7fffffff) return {CSB_EUNSUPPORTED, "offsets are 32-bit: more than 2^31 - 1 tokens"};
     *p = ScanPlan{};
     if (a->n_seq == 0) return {CSB_OK, nullptr};
-    p->group_tiles = (a->channels / a->groups + kScanCols - 1) / kScanCols;
+    p->few = a->n_tokens / a->n_seq <= kScanFew;
+    const int cols = p->few ? 16 : kScanCols;
+    p->group_tiles = (a->channels / a->groups + cols - 1) / cols;
     p->col_tiles = (int64_t)p->group_tiles * a->groups;
-    p->shift = scan_shift(a, p->col_tiles);
-    p->tiles = tile_numbers(a->n_tokens, a->n_seq, p->shift);
+    p->shift = p->few ? 31 : scan_shift(a, p->col_tiles);
+    p->tiles = p->few ? a->n_seq : tile_numbers(a->n_tokens, a->n_seq, p->shift);
     if (p->tiles * p->col_tiles > kMaxWorkgroups) return {CSB_EUNSUPPORTED, "more workgroups than a launch takes"};
     if (p->shift < 31) {
         p->begin = ((size_t)p->tiles * a->channels * a->n * 4 + 255) / 256 * 256;
@@ -214,21 +291,25 @@ static Refusal scan_plan(const csb_scan_args *a, ScanPlan *p) {
 }
 
 template <int VF, int K, bool FULL>
-static void launch_scan(const ScanDev &d, dim3 grid, hipStream_t st) {
+static void launch_scan(const ScanDev &d, bool few, dim3 grid, hipStream_t st) {
+    if (few) {
+        hipLaunchKernelGGL((selective_scan_few_kernel<VF, K, FULL>), dim3((grid.x + 3) / 4), dim3(256), 0, st, d, grid.x);
+        return;
+    }
     if (d.shift < 31) hipLaunchKernelGGL((selective_scan_kernel<VF, K, FULL, false>), grid, dim3(256), 0, st, d);
     hipLaunchKernelGGL((selective_scan_kernel<VF, K, FULL, true>), grid, dim3(256), 0, st, d);
 }
 template <int VF, int K>
-static void launch_scan(const ScanDev &d, dim3 grid, hipStream_t st) {
-    if (d.n == 4 * K) launch_scan<VF, K, true>(d, grid, st);
-    else launch_scan<VF, K, false>(d, grid, st);
+static void launch_scan(const ScanDev &d, bool few, dim3 grid, hipStream_t st) {
+    if (d.n == 4 * K) launch_scan<VF, K, true>(d, few, grid, st);
+    else launch_scan<VF, K, false>(d, few, grid, st);
 }
 template <int VF>
-static void launch_scan(const ScanDev &d, dim3 grid, hipStream_t st) {
-    if (d.n <= 16) launch_scan<VF, 4>(d, grid, st);
-    else if (d.n <= 32) launch_scan<VF, 8>(d, grid, st);
-    else if (d.n <= 64) launch_scan<VF, 16>(d, grid, st);
-    else launch_scan<VF, 32>(d, grid, st);
+static void launch_scan(const ScanDev &d, bool few, dim3 grid, hipStream_t st) {
+    if (d.n <= 16) launch_scan<VF, 4>(d, few, grid, st);
+    else if (d.n <= 32) launch_scan<VF, 8>(d, few, grid, st);
+    else if (d.n <= 64) launch_scan<VF, 16>(d, few, grid, st);
+    else launch_scan<VF, 32>(d, few, grid, st);
 }
 
 }  // namespace csb
@@ -277,9 +358,9 @@ extern "C" int csb_selective_scan(const csb_scan_args *a, void *d_ws, void *stre
     const dim3 grid((uint32_t)(p.tiles * p.col_tiles));
     hipStream_t st = (hipStream_t)stream;
     switch (a->type) {
-        case CSB_VAL_F32: launch_scan<CSB_VAL_F32>(d, grid, st); break;
-        case CSB_VAL_F16: launch_scan<CSB_VAL_F16>(d, grid, st); break;
-        default: launch_scan<CSB_VAL_BF16>(d, grid, st); break;
+        case CSB_VAL_F32: launch_scan<CSB_VAL_F32>(d, p.few, grid, st); break;
+        case CSB_VAL_F16: launch_scan<CSB_VAL_F16>(d, p.few, grid, st); break;
+        default: launch_scan<CSB_VAL_BF16>(d, p.few, grid, st); break;
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(CSB_EDEVICE, hipGetErrorString(e));
