@@ -88,6 +88,20 @@ def test_columns(T, W, orders):
     check(T, W, ["f32", "bf16", "f32", "bf16", "f16"], gate=True, orders=orders)
 
 
+@pytest.mark.parametrize("x,columns,n", [("bf16", False, "bf16"), ("f16", False, "f16"), ("f32", False, "f32"), ("f32", False, "bf16"), ("f32", False, "f16"), ("f32", True, "f32"),
+                                         ("f32", True, "bf16"), ("f32", True, "f16"), ("bf16", True, "bf16"), ("bf16", False, "f16")])
+@pytest.mark.parametrize("T,W", [(1, 64), (3, 8200), (300, 96), (600, 1000), (1100, 256), (2100, 64), (5000, 24), (9, 32768), (130, 4096)])
+def test_between_products(x, columns, n, T, W):
+    """What a product leaves (binary32, column by column) and what the next one takes, the residual stream of either order."""
+    orders = "yxrn" if columns else "yn"
+    fmts = ["f32", "f32", x, x, n]
+    check(T, W, fmts, orders=orders)
+    if T < 1000:
+        check(T, W, fmts, orders=orders, after="mean", before="mean", scale=0.3, weights=False)
+        check(T, W, fmts, orders=orders, after=None, before="rms")
+        check(T, W, fmts, orders=orders, after="rms", before=None, x=T > 100)
+
+
 @pytest.mark.parametrize("after,before", itertools.product([None, "rms", "mean"], repeat=2))
 @pytest.mark.parametrize("x", [True, False])
 @pytest.mark.parametrize("orders", ["", "yn"])
