@@ -2,15 +2,17 @@
 //
 // A token's weight is a whole number of units, floor(2^38 e^((logit - max) / T)), so sums of units are the same in any order, and what is kept and
 // drawn depends on nothing but the row and its numbers.  Top-k and top-p keep a beginning of the order by (logit, number); where it ends
-// is searched for without sorting: a histogram of 1024 buckets of (max - logit) / T holds how many tokens and units each has, sums over it
-// find the bucket, and the tokens of that one bucket are split again by their place in the order, 1024 parts at a time, until the part has
-// one token: mostly one or two turns.  (A place is the logit's bits and the token's number in 64 bits, so places differ and ties need no care.)
-// Buckets end where weights are no whole unit: tokens behind them are counted nowhere, they cannot be drawn.
+// is searched for without sorting the row.  Buckets of (max - logit) / T, 1023 of them as far as weights have units, order tokens coarsely:
+//   few:    for k of at most kFewest tokens the k-th largest of the maxima of groups of tokens bounds the k-th token from below; the tokens of the buckets up
+//           to that one's, a few more than k, are ranked against each other, and all else happens among them;
+//   many:   a histogram holds how many tokens and units each bucket has, sums over it find the bucket in which what is kept ends, and the
+//           tokens of that one bucket are split again by their place in the order, 1024 parts at a time, until the part has one token.
+// (A place is the logit's bits and the token's number in 64 bits, so places differ and ties need no care.)  Tokens of the last bucket have no whole unit:
+// they are counted nowhere, and cannot be drawn.  Exponentials are binary64, which this card does as fast as binary32.
 //
-// Exponentials are binary64, which this card does as fast as binary32: a unit is 2^-38 of the largest weight.
-//
-// Vocabularies up to kSampleSmall: one launch, a workgroup a row, its logits and weights in registers.  Larger ones: maxima of chunks; the
-// histogram; the end of what is kept, a workgroup a row, over the tokens of the buckets in question; units of the kept by chunk; the draw.
+// Rows of up to kRowMost bytes: one launch, a workgroup a row, which it holds in LDS.  Larger ones, in chunks of 16384 tokens: maxima of groups; few, or the
+// histogram (rows that nothing is cut of: units of the chunks); the bucket's tokens and the units before it by chunk; the end of what is kept and the draw; the
+// distribution, if it is asked for.  Workgroups whose row is done, or is another's, leave at once.
 #include <algorithm>
 #include <new>
 
@@ -18,9 +20,11 @@
 
 namespace csb {
 
-constexpr int kSampleBlocks = 6, kSampleSmall = 16 * 256 * kSampleBlocks;
-constexpr int kBuckets = 1024, kMaxChunks = 1024, kListMost = 4096;
+constexpr int kRowMost = 98304, kSampleSmall = kRowMost / 4;   // (in bytes; tokens of any type)
+constexpr int kBuckets = 1024, kChunk = 16384, kMaxChunks = 1024, kListMost = 4096, kFewMost = 1024, kFewest = 256;
 constexpr double kUnit = 274877906944.0;       // 2^38
+
+enum RowState : uint32_t { ROW_DONE, ROW_WHOLE, ROW_CUT, ROW_ALONE };    // drawn; nothing is cut; by the histogram; by one workgroup
 
 struct SampleDev {
     const void *logits;
@@ -29,12 +33,12 @@ struct SampleDev {
     int32_t *tokens;
     void *probs;
     int64_t ld, ldp;
-    int32_t rows, vocab, chunks, chunk;
-    // workspace: [rows][chunks], [rows][kBuckets], [rows], [rows][chunks]
-    float *maxes;
-    unsigned long long *units;
-    uint32_t *counts;
-    uint64_t *cuts, *sums;
+    int32_t rows, vocab, chunks;
+    // workspace: [rows][chunks], [rows][chunks][1024], [rows][kBuckets], [rows], [rows][kListMost]
+    float *maxes, *groups;
+    unsigned long long *units, *sums;
+    uint32_t *counts, *listed, *state;
+    uint64_t *ends, *totals, *list;
 };
 
 // What a row's numbers ask for.
@@ -149,6 +153,7 @@ struct SampleShared {
     unsigned long long units[kBuckets], low, high, found, found_units, base_units, part_units[16];
     uint32_t counts[kBuckets], part_counts[16];
     uint32_t bin, bin_count, base_count, listed;
+    int32_t token;
     float part_max[16];
 };
 
@@ -255,39 +260,103 @@ __device__ __forceinline__ uint64_t end_of_kept(SampleShared &sh, const SampleRo
     return end;
 }
 
-// The tokens of a row's bucket: from a list of them in LDS, or from the row each time where there are more than the list holds.
-template <int VF> struct BucketTokens {
-    SampleShared &sh;
-    const SampleRow &row;
-    const void *from;
-    uint64_t *list;
+// ---- reading a row, four tokens at a time: -infinity behind its end ------------------------------------------------------------------------
+template <int VF> struct RowInMemory {
+    const void *p;
     int32_t vocab;
-    int bucket;
-    template <typename Take> __device__ __forceinline__ void scan(Take take) const {
-#pragma unroll 1
-        for (int32_t v0 = 0; v0 < vocab; v0 += 16384) {
-            float s[4][4];
+    __device__ __forceinline__ void operator()(int32_t v, float *s) const { logits4<VF>(p, v, vocab, s); }
+};
+template <int VF> struct RowInLds {
+    using T = typename Elem<VF>::T;
+    using T4 = T __attribute__((ext_vector_type(4)));
+    const T *p;
+    int32_t vocab;                             // (rounded up to four: the rest holds -infinity)
+    __device__ __forceinline__ void operator()(int32_t v, float *s) const {
+        if (v < vocab) {
+            const T4 x = *(const T4 *)(p + v);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) logits4<VF>(from, v0 + 4096 * i + 4 * (int)threadIdx.x, vocab, s[i]);
+            for (int j = 0; j < 4; ++j) s[j] = logit((float)x[j]);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (row.bucket(s[i / 4][i % 4]) == bucket) take(place(s[i / 4][i % 4], v0 + 4096 * (i / 4) + 4 * (int)threadIdx.x + i % 4));
+            for (int j = 0; j < 4; ++j) s[j] = -__builtin_inff();
         }
     }
+};
+
+// Largest of the workgroup's (1024 threads).
+__device__ __forceinline__ float block_max(SampleShared &sh, float m) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    if ((threadIdx.x & 63) == 0) sh.part_max[threadIdx.x >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 16; ++w) m = fmaxf(m, sh.part_max[w]);
+    return m;
+}
+// Sum over the threads below this one; *total: of all.
+__device__ __forceinline__ uint64_t block_before(SampleShared &sh, uint64_t v, uint64_t *total) {
+    const int wave = threadIdx.x >> 6;
+    uint64_t before = before_in_wave(v), all = 0;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) sh.part_units[wave] = before + v;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+        const uint64_t p = sh.part_units[w];
+        if (w < wave) before += p;
+        all += p;
+    }
+    *total = all;
+    return before;
+}
+
+// Tokens of a row in the buckets from `low` to `high`, in a list in LDS in any order; sh.listed: how many there are, which may be more than the list holds.
+template <typename Read>
+__device__ __forceinline__ void list_tokens(SampleShared &sh, const SampleRow &row, const Read &read, int32_t vocab, int low, int high, uint64_t *list) {
+    __syncthreads();
+    if (threadIdx.x == 0) sh.listed = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int32_t v0 = 0; v0 < vocab; v0 += 16384) {
+        float s[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) read(v0 + 4096 * i + 4 * (int)threadIdx.x, s[i]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int b = row.bucket(s[i / 4][i % 4]);
+            if (b >= low && b <= high) {
+                const uint32_t n = atomicAdd(&sh.listed, 1u);
+                if (n < (uint32_t)kListMost) list[n] = place(s[i / 4][i % 4], v0 + 4096 * (i / 4) + 4 * threadIdx.x + i % 4);
+            }
+        }
+    }
+    __syncthreads();
+}
+
+// The tokens of one bucket: from the list, or from the row each time where it does not hold them.
+template <typename Read> struct BucketTokens {
+    SampleShared &sh;
+    const SampleRow &row;
+    const Read &read;
+    int32_t vocab;
+    uint64_t *list;
+    int bucket;
     __device__ __forceinline__ void gather(int b) {
         bucket = b;
-        if (threadIdx.x == 0) sh.listed = 0;
-        __syncthreads();
-        scan([&](uint64_t at) {
-            const uint32_t i = atomicAdd(&sh.listed, 1u);
-            if (i < (uint32_t)kListMost) list[i] = at;
-        });
-        __syncthreads();
+        list_tokens(sh, row, read, vocab, b, b, list);
     }
     template <typename Take> __device__ __forceinline__ void each(Take take) const {
-        if (sh.listed <= (uint32_t)kListMost)                  // (uniform)
+        if (sh.listed <= (uint32_t)kListMost) {                // (uniform)
             for (uint32_t i = threadIdx.x; i < sh.listed; i += 1024) take(list[i], row.weight(logit_at(list[i])));
-        else scan([&](uint64_t at) { take(at, row.weight(logit_at(at))); });
+            return;
+        }
+#pragma unroll 1
+        for (int32_t v = 4 * (int)threadIdx.x; v < vocab; v += 4096) {
+            float s[4];
+            read(v, s);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (row.bucket(s[j]) == bucket) take(place(s[j], v + j), row.weight(s[j]));
+        }
     }
 };
 
@@ -298,42 +367,75 @@ __device__ __forceinline__ double kept_units(const SampleRow &row, float s, int3
     return w < row.least ? 0.0 : w;
 }
 
-// A row in one workgroup: wavefront w has the `blocks` times 256 tokens from w * blocks * 256 on, four to a lane and block.  The row is read again by
-// every phase, from the caches.  Sums of units are whole numbers of binary64: at most 2^15 of 2^38 each.
-template <int VF>
-__global__ __launch_bounds__(1024) void sample_small_kernel(const SampleDev a, const int32_t blocks) {
-    using T = typename Elem<VF>::T;
-    __shared__ SampleShared sh;
-    __shared__ uint64_t list[kListMost];
-    __shared__ double sums[16];
-    __shared__ int32_t token;
-    const int number = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const void *from = (const T *)a.logits + (int64_t)number * a.ld;
-    const int32_t first = wave * blocks * 256 + 4 * lane;
-    float m = -__builtin_inff();
-#pragma unroll
-    for (int i = 0; i < kSampleBlocks; ++i)
-        if (i < blocks) {
-            float s[4];
-            logits4<VF>(from, first + 256 * i, a.vocab, s);
-            m = fmaxf(fmaxf(fmaxf(m, s[0]), fmaxf(s[1], s[2])), s[3]);
-        }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    if (lane == 0) sh.part_max[wave] = m;
+struct Kept { uint64_t end, total; int32_t token; };   // the last token's place, units of all, the token drawn (all threads have them)
+
+// The first k tokens, and all else, among the `n` of the list, which has them; k and n at most kFewMost.
+__device__ __forceinline__ Kept draw_of_few(SampleShared &sh, const SampleRow &row, const uint64_t *list, uint32_t n, uint32_t number) {
+    const uint32_t tid = threadIdx.x;
+    const uint64_t at = tid < n ? list[tid] : 0;
+    const double w = tid < n ? row.weight(logit_at(at)) : 0.0;
+    uint32_t rank = 0;
+    if (tid < n)
+#pragma unroll 8
+        for (uint32_t i = 0; i < n; ++i) rank += list[i] > at;
+    if (tid == 0) { sh.found = ~0ull; sh.token = -1; }
+    if (tid < n) sh.units[rank] = whole(w);
+    __syncthreads();
+    const uint64_t u = tid < n ? sh.units[tid] : 0;
+    uint64_t all;
+    const uint64_t before = block_before(sh, u, &all);
+    const uint32_t most = min((uint32_t)row.k, n);
+    if (tid == most - 1) sh.base_units = before + u;           // units of the first k
+    sh.units[tid] = before;
+    __syncthreads();
+    const uint64_t part = part_of(sh.base_units, row.p);
+    const bool kept = tid < n && rank < most && (row.p == 1u << 24 || sh.units[rank] < (part ? part : 1)) && w >= row.least;
+    const uint64_t mine = kept ? whole(w) : 0;
+    if (kept) atomicMin(&sh.found, (unsigned long long)at);
+    block_before(sh, mine, &all);
+    sh.units[tid] = mine;
+    __syncthreads();
+    const uint64_t limit = part_of(all, number);
+    if (mine) {                                                // by number: larger last words are lower numbers
+        uint64_t below = 0;
+#pragma unroll 4
+        for (uint32_t i = 0; i < n; ++i) below += (uint32_t)list[i] > (uint32_t)at ? sh.units[i] : 0;
+        if (below <= limit && limit < below + mine) sh.token = (int32_t)(0xffffffffu - (uint32_t)at);
+    }
+    __syncthreads();
+    return {sh.found, all, sh.token};
+}
+
+// A bucket that the first k tokens do not reach past, by the maxima of disjoint groups of tokens that `each` names.
+template <typename Each> __device__ __forceinline__ int bucket_of_first(SampleShared &sh, const SampleRow &row, Each each) {
+    const int tid = threadIdx.x;
     sh.counts[tid] = 0;
     sh.units[tid] = 0;
-    if (tid == 0) token = -1;
+    if (tid == 0) { sh.base_count = 0; sh.base_units = 0; sh.bin = kBuckets - 2; }
     __syncthreads();
-    for (int w = 0; w < 16; ++w) m = fmaxf(m, sh.part_max[w]);
-    const SampleRow row(a, number, m);
-    const bool any = m > -__builtin_inff();                    // (uniform)
+    each([&](float m) {
+        const int b = row.bucket(m);
+        if (b < kBuckets - 1) atomicAdd(&sh.counts[b], 1u);
+    });
+    __syncthreads();
+    find_bin<true>(sh, (uint64_t)row.k);
+    return (int)sh.bin;
+}
+
+// A row by one workgroup of 1024 threads.  Wavefront w draws from the `per` tokens from w per on, 256 at a time.
+template <typename Read>
+__device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &row, const Read &read, int32_t vocab, uint64_t *list, uint32_t number) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     uint64_t end = 0;
-    if (any && row.cut()) {
+    if (row.cut()) {
+        __syncthreads();
+        sh.counts[tid] = 0;
+        sh.units[tid] = 0;
+        __syncthreads();
 #pragma unroll 1
-        for (int i = 0; i < blocks; ++i) {
+        for (int32_t v = 4 * tid; v < vocab; v += 4096) {
             float s[4];
-            logits4<VF>(from, first + 256 * i, a.vocab, s);
+            read(v, s);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int b = row.bucket(s[j]);
@@ -344,298 +446,437 @@ __global__ __launch_bounds__(1024) void sample_small_kernel(const SampleDev a, c
             }
         }
         __syncthreads();
-        BucketTokens<VF> tokens{sh, row, from, list, a.vocab, 0};
+        BucketTokens<Read> tokens{sh, row, read, vocab, list, 0};
         end = end_of_kept(sh, row, tokens);
     }
-    auto weights = [&](int i, double *w) {
-        float s[4];
-        logits4<VF>(from, first + 256 * i, a.vocab, s);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = any ? kept_units(row, s[j], first + 256 * i + j, end) : 0.0;
-    };
-    double mine = 0.0;
+    const int32_t per = (vocab + 4095) / 4096 * 256, first = wave * per, stop = min(first + per, vocab);
+    uint64_t mine = 0;
 #pragma unroll 1
-    for (int i = 0; i < blocks; ++i) {
-        double w[4];
-        weights(i, w);
-        mine += w[0] + w[1] + w[2] + w[3];
+    for (int32_t v = first + 4 * lane; v < stop; v += 256) {
+        float s[4];
+        read(v, s);
+        double here = 0.0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) here += kept_units(row, s[j], v + j, end);
+        mine += whole(here);
     }
     mine = sum_of_wave(mine);
-    if (lane == 0) sums[wave] = mine;
     __syncthreads();
-    double all = 0.0, before = 0.0;
-    for (int v = 0; v < 16; ++v) {
-        if (v < wave) before += sums[v];
-        all += sums[v];
+    if (lane == 0) sh.part_units[wave] = mine;
+    if (tid == 0) sh.token = -1;
+    __syncthreads();
+    uint64_t all = 0, before = 0;
+    for (int w = 0; w < 16; ++w) {
+        if (w < wave) before += sh.part_units[w];
+        all += sh.part_units[w];
     }
-    if (a.tokens) {
-        const double limit = (double)part_of((uint64_t)all, draw_number(a.r[number]));
-        if (before <= limit && limit < before + mine) {        // one wavefront, if there is any weight
-            double upto = before;
+    const uint64_t limit = part_of(all, number);
+    if (before <= limit && limit < before + mine) {            // one wavefront, if there is any weight
 #pragma unroll 1
-            for (int i = 0; i < blocks; ++i) {
-                double w[4];
-                weights(i, w);
-                double at = upto + before_in_wave(w[0] + w[1] + w[2] + w[3]);
+        for (int32_t v0 = first; v0 < stop; v0 += 256) {
+            float s[4];
+            uint64_t u[4], sum = 0;
+            read(v0 + 4 * lane, s);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (at <= limit && limit < at + w[j]) token = first + 256 * i + j;
-                    at += w[j];
-                }
-                upto = __shfl(at, 63);
+            for (int j = 0; j < 4; ++j) {
+                u[j] = whole(kept_units(row, s[j], v0 + 4 * lane + j, end));
+                sum += u[j];
+            }
+            uint64_t at = before + before_in_wave(sum);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (at <= limit && limit < at + u[j]) sh.token = v0 + 4 * lane + j;
+                at += u[j];
+            }
+            before = __shfl(at, 63);
+            if (limit < before) break;
+        }
+    }
+    __syncthreads();
+    return {end, all, sh.token};
+}
+
+// The distribution's entries from v on.
+template <int VF>
+__device__ __forceinline__ void probs_of(const SampleRow &row, void *to, int32_t v, int32_t vocab, const float *s, uint64_t end, double per) {
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = per > 0.0 ? (float)(kept_units(row, s[j], v + j, end) * per) : 0.0f;
+    probs4<VF>(to, v, vocab, x);
+}
+
+template <int VF, int BYTES>
+__global__ __launch_bounds__(1024) void sample_small_kernel(const SampleDev a) {
+    using T = typename Elem<VF>::T;
+    using T4 = T __attribute__((ext_vector_type(4)));
+    using T4_any = T __attribute__((ext_vector_type(4), aligned(sizeof(T)), may_alias));
+    __shared__ SampleShared sh;
+    __shared__ uint64_t list[kListMost];
+    __shared__ T4 held[BYTES / sizeof(T4)];
+    const int number = blockIdx.x, tid = threadIdx.x;
+    const T *from = (const T *)a.logits + (int64_t)number * a.ld;
+    float largest = -__builtin_inff();                         // of the thread's tokens
+#pragma unroll
+    for (int i = 0; i < BYTES / (int)sizeof(T4) / 1024; ++i) {
+        const int32_t v = 4 * tid + 4096 * i;
+        if (v < a.vocab) {
+            T4 x;
+            if (v + 4 <= a.vocab) x = *(const T4_any *)(from + v);
+            else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = v + j < a.vocab ? from[v + j] : (T)-__builtin_inff();
+            }
+            held[v / 4] = x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) largest = fmaxf(largest, logit((float)x[j]));
+        }
+    }
+    const float m = block_max(sh, largest);                    // (the barrier is for the row too)
+    const SampleRow row(a, number, m);
+    const RowInLds<VF> read{(const T *)held, a.vocab};
+    const uint32_t r = a.tokens ? draw_number(a.r[number]) : 0;
+    Kept kept{0, 0, -1};
+    if (m > -__builtin_inff()) {                               // (uniform, as all that follows)
+        bool few = false;
+        if (row.k && row.k <= kFewest) {
+            const int b = bucket_of_first(sh, row, [&](auto take) { take(largest); });
+            list_tokens(sh, row, read, a.vocab, 0, b, list);
+            few = sh.listed <= (uint32_t)kFewMost;
+        }
+        kept = few ? draw_of_few(sh, row, list, sh.listed, r) : draw_alone(sh, row, read, a.vocab, list, r);
+    }
+    if (a.tokens && tid == 0) a.tokens[number] = kept.token;
+    if (a.probs) {
+        void *to = (T *)a.probs + (int64_t)number * a.ldp;
+        const double per = kept.total ? 1.0 / (double)kept.total : 0.0;
+#pragma unroll 1
+        for (int32_t v = 4 * tid; v < a.vocab; v += 4096) {
+            float s[4];
+            read(v, s);
+            probs_of<VF>(row, to, v, a.vocab, s, kept.end, per);
+        }
+    }
+}
+
+// ---- larger rows: a workgroup of 1024 threads a chunk, sixteen tokens a thread ---------------------------------------------------------------
+__device__ __forceinline__ float max_of_row(SampleShared &sh, const SampleDev &a, int row) {
+    return block_max(sh, (int)threadIdx.x < a.chunks ? a.maxes[(int64_t)row * a.chunks + threadIdx.x] : -__builtin_inff());
+}
+// Sixteen tokens of a chunk that starts at `first`: numbers first + 4096 (i / 4) + 4 tid + i % 4.
+template <int VF> __device__ __forceinline__ void chunk_tokens(const SampleDev &a, int row, int32_t first, float (*s)[4]) {
+    const void *from = (const typename Elem<VF>::T *)a.logits + (int64_t)row * a.ld;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) logits4<VF>(from, first + 4096 * i + 4 * (int)threadIdx.x, a.vocab, s[i]);
+}
+__device__ __forceinline__ int32_t chunk_number(int32_t first, int i) { return first + 4096 * (i / 4) + 4 * (int)threadIdx.x + i % 4; }
+
+template <int VF>
+__global__ __launch_bounds__(1024) void sample_max_kernel(const SampleDev a) {
+    __shared__ SampleShared sh;
+    const int row = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
+    float s[4][4], m = -__builtin_inff();
+    chunk_tokens<VF>(a, row, c * kChunk, s);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = fmaxf(m, s[i / 4][i % 4]);
+    a.groups[(int64_t)blockIdx.x * 1024 + tid] = m;
+    m = block_max(sh, m);
+    if (tid == 0) a.maxes[blockIdx.x] = m;
+    if (c == 0) {                                              // the row's histogram starts empty
+        a.counts[(int64_t)row * kBuckets + tid] = 0;
+        a.units[(int64_t)row * kBuckets + tid] = 0;
+        if (tid == 0) a.listed[row] = 0;
+    }
+}
+
+// Few tokens by the row's first workgroup; the histogram, or the chunk's units where nothing is cut, by all.
+template <int VF>
+__global__ __launch_bounds__(1024) void sample_first_kernel(const SampleDev a) {
+    __shared__ SampleShared sh;
+    __shared__ uint64_t list[kListMost];
+    const int number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
+    const float m = max_of_row(sh, a, number);
+    const SampleRow row(a, number, m);
+    const bool any = m > -__builtin_inff();
+    if (any && row.k && row.k <= kFewest) {                    // (uniform)
+        if (c) return;
+        const float *groups = a.groups + (int64_t)number * a.chunks * 1024;
+        const int b = bucket_of_first(sh, row, [&](auto take) {
+            for (int i = tid; i < a.chunks * 1024; i += 1024) take(groups[i]);
+        });
+        // the groups that have tokens up to that bucket, then their tokens, four to a thread
+        uint32_t *hits = (uint32_t *)list + kListMost;         // (the list's second half)
+        if (tid == 0) { sh.listed = 0; sh.bin_count = 0; }
+        __syncthreads();
+        for (int i = tid; i < a.chunks * 1024; i += 1024)
+            if (row.bucket(groups[i]) <= b) {
+                const uint32_t n = atomicAdd(&sh.bin_count, 1u);
+                if (n < (uint32_t)kFewMost) hits[n] = i;
+            }
+        __syncthreads();
+        const uint32_t n = sh.bin_count;
+        if (n <= (uint32_t)kFewMost) {
+            const void *from = (const typename Elem<VF>::T *)a.logits + (int64_t)number * a.ld;
+            for (uint32_t i = tid; i < n * 4; i += 1024) {
+                const uint32_t g = hits[i / 4];
+                const int32_t v = (int32_t)(g >> 10) * kChunk + 4096 * (int32_t)(i & 3) + 4 * (int32_t)(g & 1023);
+                float s[4];
+                logits4<VF>(from, v, a.vocab, s);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (row.bucket(s[j]) <= b) {
+                        const uint32_t at = atomicAdd(&sh.listed, 1u);
+                        if (at < (uint32_t)kFewMost) list[at] = place(s[j], v + j);
+                    }
             }
         }
         __syncthreads();
-        if (tid == 0) a.tokens[number] = token;
-    }
-    if (a.probs) {
-        void *to = (T *)a.probs + (int64_t)number * a.ldp;
-        const double per = all > 0.0 ? 1.0 / all : 0.0;
-#pragma unroll 1
-        for (int i = 0; i < blocks; ++i) {
-            double w[4];
-            float x[4];
-            weights(i, w);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = (float)(w[j] * per);
-            probs4<VF>(to, first + 256 * i, a.vocab, x);
-        }
-    }
-}
-
-// ---- larger vocabularies: a workgroup of 256 threads a chunk, sixteen tokens a thread at a time --------------------------------------------
-constexpr int kChunkLeast = 4096;
-
-__device__ __forceinline__ float max_of_row(const SampleDev &a, int row, float *part) {          // by all of 256 or 1024 threads
-    float m = -__builtin_inff();
-    for (int i = threadIdx.x; i < a.chunks; i += blockDim.x) m = fmaxf(m, a.maxes[(int64_t)row * a.chunks + i]);
-#pragma unroll
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
-    __syncthreads();
-    for (int w = 0; w < (int)blockDim.x / 64; ++w) m = fmaxf(m, part[w]);
-    return m;
-}
-
-template <int VF>
-__global__ __launch_bounds__(256) void sample_max_kernel(const SampleDev a) {
-    using T = typename Elem<VF>::T;
-    __shared__ float part[4];
-    const int row = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
-    const void *from = (const T *)a.logits + (int64_t)row * a.ld;
-    const int32_t first = c * a.chunk, end = min(first + a.chunk, a.vocab);
-    float m = -__builtin_inff();
-    for (int32_t v = first; v < end; v += kChunkLeast) {
-        float s[4][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) logits4<VF>(from, v + 1024 * i + 4 * tid, end, s[i]);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) m = fmaxf(m, s[i / 4][i % 4]);
-    }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    if ((tid & 63) == 0) part[tid >> 6] = m;
-    __syncthreads();
-    if (tid == 0) a.maxes[blockIdx.x] = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-    for (int i = c * 256 + tid; i < kBuckets; i += a.chunks * 256) {             // the row's histogram starts empty
-        a.counts[(int64_t)row * kBuckets + i] = 0;
-        a.units[(int64_t)row * kBuckets + i] = 0;
-    }
-}
-
-template <int VF>
-__global__ __launch_bounds__(256) void sample_histogram_kernel(const SampleDev a) {
-    using T = typename Elem<VF>::T;
-    __shared__ unsigned long long units[kBuckets];
-    __shared__ uint32_t counts[kBuckets];
-    __shared__ float part[4];
-    const int number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
-    const float m = max_of_row(a, number, part);
-    const SampleRow row(a, number, m);
-    if (!row.cut() || !(m > -__builtin_inff())) return;        // (uniform)
-    for (int i = tid; i < kBuckets; i += 256) { counts[i] = 0; units[i] = 0; }
-    __syncthreads();
-    const void *from = (const T *)a.logits + (int64_t)number * a.ld;
-    const int32_t first = c * a.chunk, end = min(first + a.chunk, a.vocab);
-    for (int32_t v = first; v < end; v += kChunkLeast) {
-        float s[4][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) logits4<VF>(from, v + 1024 * i + 4 * tid, end, s[i]);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float x = s[i / 4][i % 4];
-            const int b = row.bucket(x);
-            if (b < kBuckets - 1) {
-                atomicAdd(&counts[b], 1u);
-                atomicAdd(&units[b], (unsigned long long)whole(row.weight(x)));
+        const bool few = n <= (uint32_t)kFewMost && sh.listed <= (uint32_t)kFewMost;
+        if (few) {
+            const Kept kept = draw_of_few(sh, row, list, sh.listed, a.tokens ? draw_number(a.r[number]) : 0);
+            if (tid == 0) {
+                if (a.tokens) a.tokens[number] = kept.token;
+                a.ends[number] = kept.end;
+                a.totals[number] = kept.total;
             }
         }
-    }
-    __syncthreads();
-    for (int i = tid; i < kBuckets; i += 256)
-        if (counts[i]) {
-            atomicAdd(&a.counts[(int64_t)number * kBuckets + i], counts[i]);
-            atomicAdd(&a.units[(int64_t)number * kBuckets + i], units[i]);
-        }
-}
-
-template <int VF>
-__global__ __launch_bounds__(1024) void sample_cut_kernel(const SampleDev a) {
-    using T = typename Elem<VF>::T;
-    __shared__ SampleShared sh;
-    __shared__ uint64_t list[kListMost];
-    const int number = blockIdx.x, tid = threadIdx.x;
-    const float m = max_of_row(a, number, sh.part_max);
-    const SampleRow row(a, number, m);
-    if (!row.cut() || !(m > -__builtin_inff())) {              // (uniform)
-        if (tid == 0) a.cuts[number] = 0;
+        if (tid == 0) a.state[number] = few ? ROW_DONE : ROW_ALONE;
         return;
     }
-    sh.counts[tid] = a.counts[(int64_t)number * kBuckets + tid];
-    sh.units[tid] = a.units[(int64_t)number * kBuckets + tid];
-    __syncthreads();
-    BucketTokens<VF> tokens{sh, row, (const T *)a.logits + (int64_t)number * a.ld, list, a.vocab, 0};
-    const uint64_t end = end_of_kept(sh, row, tokens);
-    if (tid == 0) a.cuts[number] = end;
-}
-
-template <int VF>
-__global__ __launch_bounds__(256) void sample_sums_kernel(const SampleDev a, const bool cut) {
-    using T = typename Elem<VF>::T;
-    __shared__ float part[4];
-    __shared__ uint64_t parts[4];
-    const int number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
-    const float m = max_of_row(a, number, part);
-    const SampleRow row(a, number, m);
-    const uint64_t last = cut ? a.cuts[number] : 0;
-    const void *from = (const T *)a.logits + (int64_t)number * a.ld;
-    const int32_t first = c * a.chunk, end = min(first + a.chunk, a.vocab);
-    uint64_t sum = 0;
-    if (m > -__builtin_inff())                                 // (uniform)
-        for (int32_t v = first; v < end; v += kChunkLeast) {
-            float s[4][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) logits4<VF>(from, v + 1024 * i + 4 * tid, end, s[i]);
-            double here = 0.0;                                 // (16 weights: exact)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) here += kept_units(row, s[i / 4][i % 4], v + 1024 * (i / 4) + 4 * tid + i % 4, last);
-            sum += whole(here);
+    // (one of the two ends: of both the second is known when the first is)
+    const uint32_t state = !any ? ROW_DONE : !row.cut() ? ROW_WHOLE : row.k && row.p < 1u << 24 ? ROW_ALONE : ROW_CUT;
+    if (c == 0 && tid == 0) {
+        a.state[number] = state;
+        if (!any) {
+            if (a.tokens) a.tokens[number] = -1;
+            a.ends[number] = a.totals[number] = 0;
         }
-    sum = sum_of_wave(sum);
-    if ((tid & 63) == 0) parts[tid >> 6] = sum;
-    __syncthreads();
-    if (tid == 0) a.sums[blockIdx.x] = parts[0] + parts[1] + parts[2] + parts[3];
-}
-
-// The draw in the chunk that the number falls into, and the distribution, chunk by chunk (a workgroup each).
-template <int VF>
-__global__ __launch_bounds__(256) void sample_draw_kernel(const SampleDev a, const bool cut) {
-    using T = typename Elem<VF>::T;
-    __shared__ float part[4];
-    __shared__ uint64_t all_parts[4], before_parts[4];
-    const int number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    uint64_t all = 0, before = 0;
-    for (int i = tid; i < a.chunks; i += 256) {
-        const uint64_t s = a.sums[(int64_t)number * a.chunks + i];
-        all += s;
-        if (i < c) before += s;
     }
-    all = sum_of_wave(all);
-    before = sum_of_wave(before);
-    if (lane == 0) { all_parts[wave] = all; before_parts[wave] = before; }
-    __syncthreads();
-    all = all_parts[0] + all_parts[1] + all_parts[2] + all_parts[3];
-    before = before_parts[0] + before_parts[1] + before_parts[2] + before_parts[3];
-    const uint64_t here = a.sums[blockIdx.x], limit = a.tokens ? part_of(all, draw_number(a.r[number])) : 0;
-    const bool mine = a.tokens && before <= limit && limit < before + here;      // (uniform)
-    if (a.tokens && c == 0 && all == 0 && tid == 0) a.tokens[number] = -1;
-    if (!mine && !a.probs) return;
-    const float m = max_of_row(a, number, part);
-    const SampleRow row(a, number, m);
-    const bool any = m > -__builtin_inff();
-    const uint64_t last = cut ? a.cuts[number] : 0;
-    const double per = all ? 1.0 / (double)all : 0.0;
-    const void *from = (const T *)a.logits + (int64_t)number * a.ld;
-    void *to = (T *)a.probs + (int64_t)number * a.ldp;
-    const int32_t first = c * a.chunk, end = min(first + a.chunk, a.vocab);
-    for (int32_t v0 = first; v0 < end; v0 += 1024) {           // four tokens a thread
-        const int32_t v = v0 + 4 * tid;
-        float s[4], x[4];
-        double w[4], sum = 0.0;
-        logits4<VF>(from, v, end, s);
+    if (state == ROW_DONE || state == ROW_ALONE) return;
+    float s[4][4];
+    chunk_tokens<VF>(a, number, c * kChunk, s);
+    if (state == ROW_WHOLE) {
+        double here = 0.0;                                     // (16 weights: exact)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            w[j] = any ? kept_units(row, s[j], v + j, last) : 0.0;
-            sum += w[j];
-            x[j] = (float)(w[j] * per);
+        for (int i = 0; i < 16; ++i) here += kept_units(row, s[i / 4][i % 4], chunk_number(c * kChunk, i), 0);
+        uint64_t all;
+        block_before(sh, whole(here), &all);
+        if (tid == 0) a.sums[blockIdx.x] = all;
+        return;
+    }
+    sh.counts[tid] = 0;
+    sh.units[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float x = s[i / 4][i % 4];
+        const int b = row.bucket(x);
+        if (b < kBuckets - 1) {
+            atomicAdd(&sh.counts[b], 1u);
+            atomicAdd(&sh.units[b], (unsigned long long)whole(row.weight(x)));
         }
-        if (a.probs) probs4<VF>(to, v, end, x);
-        if (mine) {
-            const uint64_t own = whole(sum);
-            uint64_t at = before + before_in_wave(own);
-            __syncthreads();
-            if (lane == 63) all_parts[wave] = at - before + own;
-            __syncthreads();
-            for (int k = 0; k < 4; ++k) {
-                if (k < wave) at += all_parts[k];
-                before += all_parts[k];
-            }
+    }
+    __syncthreads();
+    if (sh.counts[tid]) {
+        atomicAdd(&a.counts[(int64_t)number * kBuckets + tid], sh.counts[tid]);
+        atomicAdd(&a.units[(int64_t)number * kBuckets + tid], sh.units[tid]);
+    }
+}
+
+// The row's histogram in LDS, and the bucket in which what is kept ends (kBuckets: nothing is cut); sh.base_*: what lies before it.  *target: of find_bin.
+__device__ __forceinline__ int bucket_of_row(SampleShared &sh, const SampleDev &a, int number, const SampleRow &row, uint64_t *target) {
+    const int tid = threadIdx.x;
+    __syncthreads();
+    sh.counts[tid] = a.counts[(int64_t)number * kBuckets + tid];
+    const uint64_t u = sh.units[tid] = a.units[(int64_t)number * kBuckets + tid];
+    if (tid == 0) { sh.base_count = 0; sh.base_units = 0; sh.bin = kBuckets; }
+    uint64_t all;
+    block_before(sh, u, &all);
+    if (row.k) find_bin<true>(sh, *target = (uint64_t)row.k);
+    else {
+        const uint64_t part = part_of(all, row.p);
+        find_bin<false>(sh, *target = part ? part : 1);
+    }
+    return (int)sh.bin;
+}
+
+// Rows that are cut: the tokens of the bucket in which what is kept ends, in any order, and the units of the chunk before it.
+template <int VF>
+__global__ __launch_bounds__(1024) void sample_bucket_kernel(const SampleDev a) {
+    __shared__ SampleShared sh;
+    const int number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
+    if (a.state[number] != ROW_CUT) return;
+    float s[4][4];
+    chunk_tokens<VF>(a, number, c * kChunk, s);
+    const float m = max_of_row(sh, a, number);
+    const SampleRow row(a, number, m);
+    uint64_t target;
+    const int bucket = bucket_of_row(sh, a, number, row, &target);
+    double here = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float x = s[i / 4][i % 4];
+        const int b = row.bucket(x);
+        if (b < bucket) here += kept_units(row, x, 0, 0);
+        else if (b == bucket) {
+            const uint32_t n = atomicAdd(&a.listed[number], 1u);
+            if (n < (uint32_t)kListMost) a.list[(int64_t)number * kListMost + n] = place(x, chunk_number(c * kChunk, i));
+        }
+    }
+    uint64_t all;
+    block_before(sh, whole(here), &all);
+    if (tid == 0) a.sums[blockIdx.x] = all;
+}
+
+// Tokens of a bucket, in a list alone.
+struct ListedTokens {
+    const SampleRow &row;
+    const uint64_t *list;
+    uint32_t n;
+    template <typename Take> __device__ __forceinline__ void each(Take take) const {
+        for (uint32_t i = threadIdx.x; i < n; i += 1024) take(list[i], row.weight(logit_at(list[i])));
+    }
+};
+
+template <int VF>
+__global__ __launch_bounds__(1024) void sample_draw_kernel(const SampleDev a) {
+    __shared__ SampleShared sh;
+    __shared__ uint64_t list[kListMost];
+    __shared__ unsigned long long sums[kMaxChunks];
+    const int number = blockIdx.x, tid = threadIdx.x;
+    const uint32_t state = a.state[number];
+    if (state == ROW_DONE) return;
+    const float m = max_of_row(sh, a, number);
+    const SampleRow row(a, number, m);
+    const uint32_t r = a.tokens ? draw_number(a.r[number]) : 0;
+    const uint32_t listed = state == ROW_CUT ? a.listed[number] : 0;
+    if (state == ROW_ALONE || listed > (uint32_t)kListMost) {
+        const RowInMemory<VF> read{(const typename Elem<VF>::T *)a.logits + (int64_t)number * a.ld, a.vocab};
+        const Kept kept = draw_alone(sh, row, read, a.vocab, list, r);
+        if (tid == 0) {
+            if (a.tokens) a.tokens[number] = kept.token;
+            a.ends[number] = kept.end;
+            a.totals[number] = kept.total;
+        }
+        return;
+    }
+    uint64_t end = 0;
+    sums[tid] = tid < a.chunks ? a.sums[(int64_t)number * a.chunks + tid] : 0;
+    if (state == ROW_CUT) {
+        for (uint32_t i = tid; i < listed; i += 1024) list[i] = a.list[(int64_t)number * kListMost + i];
+        uint64_t target;
+        const int bucket = bucket_of_row(sh, a, number, row, &target);
+        if (bucket < kBuckets) {
+            const ListedTokens tokens{row, list, listed};
+            if (row.k) find_token<true>(sh, target, tokens);
+            else find_token<false>(sh, target, tokens);
+            end = sh.found;
+            for (uint32_t i = tid; i < listed; i += 1024)
+                if (list[i] >= end) {
+                    const uint32_t v = 0xffffffffu - (uint32_t)list[i];
+                    atomicAdd(&sums[v / kChunk], (unsigned long long)whole(kept_units(row, logit_at(list[i]), v, end)));
+                }
+        }
+    }
+    __syncthreads();
+    uint64_t all;
+    const uint64_t here = sums[tid], before = block_before(sh, here, &all), limit = part_of(all, r);
+    if (tid == 0) {
+        a.ends[number] = end;
+        a.totals[number] = all;
+    }
+    if (!a.tokens) return;
+    if (tid == 0) { sh.bin = kMaxChunks; sh.token = -1; }
+    __syncthreads();
+    if (before <= limit && limit < before + here) { sh.bin = tid; sh.base_units = before; }
+    __syncthreads();
+    const uint32_t c = sh.bin;
+    if (c < (uint32_t)kMaxChunks) {                            // (any weight)
+        uint64_t from = sh.base_units;
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {                          // 4096 tokens by number, four a thread
+            const int32_t v = (int32_t)c * kChunk + 4096 * i + 4 * tid;
+            float s[4];
+            uint64_t u[4], sum = 0, part;
+            logits4<VF>((const typename Elem<VF>::T *)a.logits + (int64_t)number * a.ld, v, a.vocab, s);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint64_t u = whole(w[j]);
-                if (at <= limit && limit < at + u) a.tokens[number] = v + j;
-                at += u;
+                u[j] = whole(kept_units(row, s[j], v + j, end));
+                sum += u[j];
             }
+            uint64_t at = from + block_before(sh, sum, &part);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (at <= limit && limit < at + u[j]) sh.token = v + j;
+                at += u[j];
+            }
+            from += part;
+            if (limit < from) break;                           // (uniform)
         }
     }
+    __syncthreads();
+    if (tid == 0) a.tokens[number] = sh.token;
 }
 
-// Tokens of a chunk: kChunkLeast, or more where that would make more than kMaxChunks.
-static void sample_chunks(int32_t vocab, int32_t *chunks, int32_t *chunk) {
-    int64_t c = kChunkLeast;
-    while ((vocab + c - 1) / c > kMaxChunks) c *= 2;
-    *chunk = (int32_t)c;
-    *chunks = (int32_t)((vocab + c - 1) / c);
+template <int VF>
+__global__ __launch_bounds__(1024) void sample_probs_kernel(const SampleDev a) {
+    __shared__ SampleShared sh;
+    const int number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks;
+    float s[4][4];
+    chunk_tokens<VF>(a, number, c * kChunk, s);
+    const float m = max_of_row(sh, a, number);
+    const SampleRow row(a, number, m);
+    const uint64_t end = a.ends[number], all = a.totals[number];
+    const double per = all ? 1.0 / (double)all : 0.0;
+    void *to = (typename Elem<VF>::T *)a.probs + (int64_t)number * a.ldp;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) probs_of<VF>(row, to, chunk_number(c * kChunk, 4 * i), a.vocab, s[i], end, per);
 }
 
-struct SamplePlaces { size_t maxes, units, counts, cuts, sums, bytes; };
+struct SamplePlaces { size_t maxes, groups, units, sums, counts, listed, state, ends, totals, list, bytes; };
 static SamplePlaces sample_places(int64_t rows, int64_t chunks) {
     SamplePlaces p{};
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
     p.units = take((size_t)rows * kBuckets * 8);
+    p.list = take((size_t)rows * kListMost * 8);
     p.sums = take((size_t)rows * chunks * 8);
-    p.cuts = take((size_t)rows * 8);
+    p.ends = take((size_t)rows * 8);
+    p.totals = take((size_t)rows * 8);
     p.counts = take((size_t)rows * kBuckets * 4);
+    p.groups = take((size_t)rows * chunks * 1024 * 4);
     p.maxes = take((size_t)rows * chunks * 4);
+    p.listed = take((size_t)rows * 4);
+    p.state = take((size_t)rows * 4);
     p.bytes = at;
     return p;
 }
+static int32_t sample_chunks(int32_t vocab) { return (vocab + kChunk - 1) / kChunk; }       // (at most kMaxChunks)
 
 template <int VF>
 static void launch_sample(const SampleDev &d, hipStream_t st) {
-    if (d.vocab <= kSampleSmall) {
-        hipLaunchKernelGGL(sample_small_kernel<VF>, dim3((uint32_t)d.rows), dim3(1024), 0, st, d, (d.vocab + 4095) / 4096);
+    const int64_t bytes = (int64_t)d.vocab * (VF == CSB_VAL_F32 ? 4 : 2);
+    const dim3 block(1024), rows((uint32_t)d.rows), grid((uint32_t)d.rows * (uint32_t)d.chunks);
+    if (bytes <= kRowMost / 3) {
+        hipLaunchKernelGGL((sample_small_kernel<VF, kRowMost / 3>), rows, block, 0, st, d);
         return;
     }
-    const dim3 grid((uint32_t)d.rows * (uint32_t)d.chunks), block(256);
-    const bool cut = d.top_k || d.top_p || d.temperature;      // (a temperature of zero cuts too)
-    hipLaunchKernelGGL(sample_max_kernel<VF>, grid, block, 0, st, d);
-    if (cut) {
-        hipLaunchKernelGGL(sample_histogram_kernel<VF>, grid, block, 0, st, d);
-        hipLaunchKernelGGL(sample_cut_kernel<VF>, dim3((uint32_t)d.rows), dim3(1024), 0, st, d);
+    if (bytes <= kRowMost) {
+        hipLaunchKernelGGL((sample_small_kernel<VF, kRowMost>), rows, block, 0, st, d);
+        return;
     }
-    hipLaunchKernelGGL(sample_sums_kernel<VF>, grid, block, 0, st, d, cut);
-    hipLaunchKernelGGL(sample_draw_kernel<VF>, grid, block, 0, st, d, cut);
+    hipLaunchKernelGGL(sample_max_kernel<VF>, grid, block, 0, st, d);
+    hipLaunchKernelGGL(sample_first_kernel<VF>, grid, block, 0, st, d);
+    if (d.top_k || d.top_p || d.temperature)                   // (a temperature of zero cuts too)
+        hipLaunchKernelGGL(sample_bucket_kernel<VF>, grid, block, 0, st, d);
+    hipLaunchKernelGGL(sample_draw_kernel<VF>, rows, block, 0, st, d);
+    if (d.probs) hipLaunchKernelGGL(sample_probs_kernel<VF>, grid, block, 0, st, d);
 }
 
 }  // namespace csb
 
 extern "C" size_t csb_sample_workspace_bytes(int32_t n_rows, int32_t vocab) {
     if (n_rows <= 0 || vocab <= csb::kSampleSmall) return 0;
-    int32_t chunks, chunk;
-    csb::sample_chunks(vocab, &chunks, &chunk);
-    return csb::sample_places(n_rows, chunks).bytes;
+    return csb::sample_places(n_rows, csb::sample_chunks(vocab)).bytes;
 }
 
 extern "C" int csb_sample(int32_t type, const void *d_logits, int64_t ld, const float *d_temperature, const int32_t *d_top_k,
@@ -655,15 +896,16 @@ extern "C" int csb_sample(int32_t type, const void *d_logits, int64_t ld, const 
     SampleDev d{};
     d.logits = d_logits; d.ld = ld; d.temperature = d_temperature; d.top_k = d_top_k; d.top_p = d_top_p; d.min_p = d_min_p; d.r = d_r;
     d.rows = n_rows; d.vocab = vocab; d.tokens = d_tokens; d.probs = d_probs; d.ldp = ldprobs;
-    sample_chunks(vocab, &d.chunks, &d.chunk);
-    if (n_rows > 1 << 21 || (int64_t)n_rows * d.chunks > kMaxWorkgroups) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
-    if (vocab > kSampleSmall) {
+    d.chunks = sample_chunks(vocab);
+    if (n_rows > 1 << 21 || (int64_t)n_rows * d.chunks > kMaxWorkgroups / 4) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
+    if ((int64_t)vocab * type_size(type) > kRowMost) {
         if (!d_ws) return fail(CSB_EINVAL, "NULL workspace");
         if ((uintptr_t)d_ws % 256) return fail(CSB_EINVAL, "workspace not 256-byte aligned");
         const SamplePlaces p = sample_places(n_rows, d.chunks);
         char *ws = (char *)d_ws;
-        d.units = (unsigned long long *)(ws + p.units); d.sums = (uint64_t *)(ws + p.sums); d.cuts = (uint64_t *)(ws + p.cuts);
-        d.counts = (uint32_t *)(ws + p.counts); d.maxes = (float *)(ws + p.maxes);
+        d.units = (unsigned long long *)(ws + p.units); d.sums = (unsigned long long *)(ws + p.sums); d.list = (uint64_t *)(ws + p.list);
+        d.ends = (uint64_t *)(ws + p.ends); d.totals = (uint64_t *)(ws + p.totals); d.counts = (uint32_t *)(ws + p.counts);
+        d.groups = (float *)(ws + p.groups); d.maxes = (float *)(ws + p.maxes); d.listed = (uint32_t *)(ws + p.listed); d.state = (uint32_t *)(ws + p.state);
         try {
             static const char sample_user = 0;                 // this entry point as a user of workspaces
             workspace_changed_hands(d_ws, &sample_user);
