@@ -10,7 +10,7 @@
 // (A place is the logit's bits and the token's number in 64 bits, so places differ and ties need no care.)  Tokens of the last bucket have no whole unit:
 // they are counted nowhere, and cannot be drawn.  Exponentials are binary64, which this card does as fast as binary32.
 //
-// Rows of up to kRowMost bytes: one launch, a workgroup a row, which it holds in LDS.  Larger ones, in chunks of 16384 tokens: maxima of groups; few, or the
+// Rows of up to kRowSmall bytes, and of kRowMost with top-k: one launch, a workgroup a row, which it holds in LDS.  Others, in chunks of 16384 tokens: maxima of groups; few, or the
 // histogram (rows that nothing is cut of: units of the chunks); the bucket's tokens and the units before it by chunk; the end of what is kept and the draw; the
 // distribution, if it is asked for.  Workgroups whose row is done, or is another's, leave at once.
 #include <algorithm>
@@ -20,7 +20,7 @@
 
 namespace csb {
 
-constexpr int kRowMost = 98304, kSampleSmall = kRowMost / 4;   // (in bytes; tokens of any type)
+constexpr int kRowMost = 98304, kRowSmall = kRowMost / 3;      // bytes of a row that a workgroup may hold, and of one that it always does
 constexpr int kBuckets = 1024, kChunk = 16384, kMaxChunks = 1024, kListMost = 4096, kFewMost = 1024, kFewest = 256;
 constexpr double kUnit = 274877906944.0;       // 2^38
 
@@ -131,21 +131,36 @@ template <int VF> __device__ __forceinline__ void probs4(void *row, int32_t v, i
     }
 }
 
-template <typename N> __device__ __forceinline__ N sum_of_wave(N v) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+// v moved to other lanes: by CTRL, in the rows of 16 lanes of ROWS; zero where no lane's comes.
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, true); }
+template <int CTRL, int ROWS> __device__ __forceinline__ uint64_t moved(uint64_t v) {
+    return (uint64_t)moved<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)v);
+}
+// Sum over the lanes up to this one: within rows of 16, then over the rows.
+template <typename N> __device__ __forceinline__ N upto_in_wave(N v) {
+    v += moved<0x111, 0xf>(v);
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);
+    v += moved<0x143, 0xc>(v);
     return v;
 }
-// Sum over the lanes below this one.
-template <typename N> __device__ __forceinline__ N before_in_wave(N v) {
-    N upto = v;
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const N o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
-    }
-    return upto - v;
+template <typename N> __device__ __forceinline__ N before_in_wave(N v) { return upto_in_wave(v) - v; }
+template <typename N> __device__ __forceinline__ N of_lane(N v, int lane) {
+    if constexpr (sizeof(N) == 8) return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+    else return (N)__builtin_amdgcn_readlane((int)v, lane);
+}
+template <typename N> __device__ __forceinline__ N sum_of_wave(N v) { return of_lane(upto_in_wave(v), 63); }
+__device__ __forceinline__ uint64_t max_of_wave(uint64_t v) {  // (0: none)
+    const auto larger = [](uint64_t x, uint64_t y) { return x > y ? x : y; };
+    v = larger(v, moved<0x111, 0xf>(v));
+    v = larger(v, moved<0x112, 0xf>(v));
+    v = larger(v, moved<0x114, 0xf>(v));
+    v = larger(v, moved<0x118, 0xf>(v));
+    v = larger(v, moved<0x142, 0xa>(v));
+    v = larger(v, moved<0x143, 0xc>(v));
+    return of_lane(v, 63);
 }
 
 // A workgroup's memory for the searches of a row.
@@ -157,19 +172,43 @@ struct SampleShared {
     float part_max[16];
 };
 
+// Sum over the threads below this one; *total: of all.
+__device__ __forceinline__ uint64_t block_before(SampleShared &sh, uint64_t v, uint64_t *total) {
+    const int wave = threadIdx.x >> 6;
+    uint64_t before = before_in_wave(v), all = 0;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) sh.part_units[wave] = before + v;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+        const uint64_t p = sh.part_units[w];
+        if (w < wave) before += p;
+        all += p;
+    }
+    *total = all;
+    return before;
+}
+
 // The bin, of counts and units in LDS by thread, in which what is kept ends: of `target` tokens (BY_COUNT), or of those with fewer
-// than `target` units before them; counted from what sh.base_* hold, which is moved up to the bin.  1024 threads, all of them.
-template <bool BY_COUNT> __device__ __forceinline__ void find_bin(SampleShared &sh, uint64_t target) {
+// than `target` units before them; counted from what sh.base_* hold, which is moved up to the bin (UNITS: units too).  1024 threads, all of them.
+template <bool BY_COUNT, bool UNITS = true> __device__ __forceinline__ void find_bin(SampleShared &sh, uint64_t target) {
     const int tid = threadIdx.x, wave = tid >> 6;
     const uint32_t c = sh.counts[tid];
-    const uint64_t u = sh.units[tid];
-    uint32_t cb = before_in_wave(c);
-    uint64_t ub = before_in_wave(u);
-    if ((tid & 63) == 63) { sh.part_counts[wave] = cb + c; sh.part_units[wave] = ub + u; }
+    const uint64_t u = UNITS ? sh.units[tid] : 0;
+    uint32_t cb = BY_COUNT ? before_in_wave(c) : 0;
+    uint64_t ub = UNITS ? before_in_wave(u) : 0;
+    if ((tid & 63) == 63) {
+        if (BY_COUNT) sh.part_counts[wave] = cb + c;
+        if (UNITS) sh.part_units[wave] = ub + u;
+    }
     __syncthreads();
     cb += sh.base_count;
     ub += sh.base_units;
-    for (int w = 0; w < wave; ++w) { cb += sh.part_counts[w]; ub += sh.part_units[w]; }
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+        if (BY_COUNT) cb += w < wave ? sh.part_counts[w] : 0;
+        if (UNITS) ub += w < wave ? sh.part_units[w] : 0;
+    }
     __syncthreads();                                           // (base_* are read)
     if (BY_COUNT ? cb < target && cb + c >= target : ub < target && ub + u >= target) {   // one thread, or none
         sh.bin = tid;
@@ -188,7 +227,9 @@ template <bool BY_COUNT, typename Tokens> __device__ __forceinline__ void find_t
     __syncthreads();
     uint64_t low = ~0ull, high = 0;
     tokens.each([&](uint64_t at, double) { low = at < low ? at : low; high = at > high ? at : high; });
-    if (low <= high) { atomicMin(&sh.low, (unsigned long long)low); atomicMax(&sh.high, (unsigned long long)high); }
+    low = ~max_of_wave(~low);
+    high = max_of_wave(high);
+    if ((tid & 63) == 0 && low <= high) { atomicMin(&sh.low, (unsigned long long)low); atomicMax(&sh.high, (unsigned long long)high); }
     __syncthreads();
     low = sh.low;
     high = sh.high;
@@ -235,9 +276,7 @@ __device__ __forceinline__ uint64_t end_of_kept(SampleShared &sh, const SampleRo
     };
     restore();
     uint64_t end = 0, units;
-    find_bin<false>(sh, ~0ull);                                // (no bin: part_units are of use)
-    units = 0;
-    for (int w = 0; w < 16; ++w) units += sh.part_units[w];
+    block_before(sh, u, &units);
     if (row.k) {
         find_bin<true>(sh, (uint64_t)row.k);
         if (sh.bin < kBuckets) {                               // (uniform) else fewer tokens than k have units
@@ -293,23 +332,6 @@ __device__ __forceinline__ float block_max(SampleShared &sh, float m) {
     for (int w = 0; w < 16; ++w) m = fmaxf(m, sh.part_max[w]);
     return m;
 }
-// Sum over the threads below this one; *total: of all.
-__device__ __forceinline__ uint64_t block_before(SampleShared &sh, uint64_t v, uint64_t *total) {
-    const int wave = threadIdx.x >> 6;
-    uint64_t before = before_in_wave(v), all = 0;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 63) sh.part_units[wave] = before + v;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-        const uint64_t p = sh.part_units[w];
-        if (w < wave) before += p;
-        all += p;
-    }
-    *total = all;
-    return before;
-}
-
 // Tokens of a row in the buckets from `low` to `high`, in a list in LDS in any order; sh.listed: how many there are, which may be more than the list holds.
 template <typename Read>
 __device__ __forceinline__ void list_tokens(SampleShared &sh, const SampleRow &row, const Read &read, int32_t vocab, int low, int high, uint64_t *list) {
@@ -374,10 +396,14 @@ __device__ __forceinline__ Kept draw_of_few(SampleShared &sh, const SampleRow &r
     const uint32_t tid = threadIdx.x;
     const uint64_t at = tid < n ? list[tid] : 0;
     const double w = tid < n ? row.weight(logit_at(at)) : 0.0;
-    uint32_t rank = 0;
+    uint32_t rank = 0, turn = 0;                               // by place, and by number: larger last words are lower numbers
     if (tid < n)
 #pragma unroll 8
-        for (uint32_t i = 0; i < n; ++i) rank += list[i] > at;
+        for (uint32_t i = 0; i < n; ++i) {
+            const uint64_t other = list[i];
+            rank += other > at;
+            turn += (uint32_t)other > (uint32_t)at;
+        }
     if (tid == 0) { sh.found = ~0ull; sh.token = -1; }
     if (tid < n) sh.units[rank] = whole(w);
     __syncthreads();
@@ -390,18 +416,17 @@ __device__ __forceinline__ Kept draw_of_few(SampleShared &sh, const SampleRow &r
     __syncthreads();
     const uint64_t part = part_of(sh.base_units, row.p);
     const bool kept = tid < n && rank < most && (row.p == 1u << 24 || sh.units[rank] < (part ? part : 1)) && w >= row.least;
-    const uint64_t mine = kept ? whole(w) : 0;
-    if (kept) atomicMin(&sh.found, (unsigned long long)at);
-    block_before(sh, mine, &all);
-    sh.units[tid] = mine;
+    const uint64_t mine = kept ? whole(w) : 0, last = ~max_of_wave(kept ? ~at : 0);
+    if ((tid & 63) == 0) atomicMin(&sh.found, (unsigned long long)last);
     __syncthreads();
-    const uint64_t limit = part_of(all, number);
-    if (mine) {                                                // by number: larger last words are lower numbers
-        uint64_t below = 0;
-#pragma unroll 4
-        for (uint32_t i = 0; i < n; ++i) below += (uint32_t)list[i] > (uint32_t)at ? sh.units[i] : 0;
-        if (below <= limit && limit < below + mine) sh.token = (int32_t)(0xffffffffu - (uint32_t)at);
-    }
+    sh.units[tid] = 0;
+    __syncthreads();
+    if (tid < n) sh.units[turn] = mine;
+    __syncthreads();
+    const uint64_t own = sh.units[tid], below = block_before(sh, own, &all), limit = part_of(all, number);
+    if (below <= limit && limit < below + own) sh.bin = tid;   // one thread: there is a token of some weight
+    __syncthreads();
+    if (tid < n && turn == sh.bin) sh.token = (int32_t)(0xffffffffu - (uint32_t)at);
     __syncthreads();
     return {sh.found, all, sh.token};
 }
@@ -410,7 +435,6 @@ __device__ __forceinline__ Kept draw_of_few(SampleShared &sh, const SampleRow &r
 template <typename Each> __device__ __forceinline__ int bucket_of_first(SampleShared &sh, const SampleRow &row, Each each) {
     const int tid = threadIdx.x;
     sh.counts[tid] = 0;
-    sh.units[tid] = 0;
     if (tid == 0) { sh.base_count = 0; sh.base_units = 0; sh.bin = kBuckets - 2; }
     __syncthreads();
     each([&](float m) {
@@ -418,7 +442,7 @@ template <typename Each> __device__ __forceinline__ int bucket_of_first(SampleSh
         if (b < kBuckets - 1) atomicAdd(&sh.counts[b], 1u);
     });
     __syncthreads();
-    find_bin<true>(sh, (uint64_t)row.k);
+    find_bin<true, false>(sh, (uint64_t)row.k);
     return (int)sh.bin;
 }
 
@@ -440,7 +464,7 @@ __device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &ro
             for (int j = 0; j < 4; ++j) {
                 const int b = row.bucket(s[j]);
                 if (b < kBuckets - 1) {
-                    atomicAdd(&sh.counts[b], 1u);
+                    if (row.k) atomicAdd(&sh.counts[b], 1u);
                     atomicAdd(&sh.units[b], (unsigned long long)whole(row.weight(s[j])));
                 }
             }
@@ -601,12 +625,14 @@ __global__ __launch_bounds__(1024) void sample_first_kernel(const SampleDev a) {
         if (c) return;
         const float *groups = a.groups + (int64_t)number * a.chunks * 1024;
         const int b = bucket_of_first(sh, row, [&](auto take) {
+#pragma unroll 8
             for (int i = tid; i < a.chunks * 1024; i += 1024) take(groups[i]);
         });
         // the groups that have tokens up to that bucket, then their tokens, four to a thread
         uint32_t *hits = (uint32_t *)list + kListMost;         // (the list's second half)
         if (tid == 0) { sh.listed = 0; sh.bin_count = 0; }
         __syncthreads();
+#pragma unroll 8
         for (int i = tid; i < a.chunks * 1024; i += 1024)
             if (row.bucket(groups[i]) <= b) {
                 const uint32_t n = atomicAdd(&sh.bin_count, 1u);
@@ -671,13 +697,13 @@ __global__ __launch_bounds__(1024) void sample_first_kernel(const SampleDev a) {
         const float x = s[i / 4][i % 4];
         const int b = row.bucket(x);
         if (b < kBuckets - 1) {
-            atomicAdd(&sh.counts[b], 1u);
+            if (row.k) atomicAdd(&sh.counts[b], 1u);
             atomicAdd(&sh.units[b], (unsigned long long)whole(row.weight(x)));
         }
     }
     __syncthreads();
-    if (sh.counts[tid]) {
-        atomicAdd(&a.counts[(int64_t)number * kBuckets + tid], sh.counts[tid]);
+    if (sh.units[tid] || sh.counts[tid]) {
+        if (row.k) atomicAdd(&a.counts[(int64_t)number * kBuckets + tid], sh.counts[tid]);
         atomicAdd(&a.units[(int64_t)number * kBuckets + tid], sh.units[tid]);
     }
 }
@@ -712,16 +738,25 @@ __global__ __launch_bounds__(1024) void sample_bucket_kernel(const SampleDev a) 
     uint64_t target;
     const int bucket = bucket_of_row(sh, a, number, row, &target);
     double here = 0.0;
+    uint32_t mine = 0;                                         // which of the sixteen are the bucket's
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const float x = s[i / 4][i % 4];
         const int b = row.bucket(x);
         if (b < bucket) here += kept_units(row, x, 0, 0);
-        else if (b == bucket) {
-            const uint32_t n = atomicAdd(&a.listed[number], 1u);
-            if (n < (uint32_t)kListMost) a.list[(int64_t)number * kListMost + n] = place(x, chunk_number(c * kChunk, i));
-        }
+        else if (b == bucket) mine |= 1u << i;
     }
+    uint64_t total;
+    uint32_t at = (uint32_t)block_before(sh, (uint64_t)__builtin_popcount(mine), &total);
+    if (tid == 0) sh.listed = total ? atomicAdd(&a.listed[number], (uint32_t)total) : 0;     // a place for the workgroup's
+    __syncthreads();
+    at += sh.listed;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (mine >> i & 1) {
+            if (at < (uint32_t)kListMost) a.list[(int64_t)number * kListMost + at] = place(s[i / 4][i % 4], chunk_number(c * kChunk, i));
+            ++at;
+        }
     uint64_t all;
     block_before(sh, whole(here), &all);
     if (tid == 0) a.sums[blockIdx.x] = all;
@@ -852,15 +887,19 @@ static SamplePlaces sample_places(int64_t rows, int64_t chunks) {
 }
 static int32_t sample_chunks(int32_t vocab) { return (vocab + kChunk - 1) / kChunk; }       // (at most kMaxChunks)
 
+static bool one_workgroup(const SampleDev &d, int64_t bytes) { return bytes <= kRowSmall || (bytes <= kRowMost && d.top_k); }
+
 template <int VF>
 static void launch_sample(const SampleDev &d, hipStream_t st) {
     const int64_t bytes = (int64_t)d.vocab * (VF == CSB_VAL_F32 ? 4 : 2);
     const dim3 block(1024), rows((uint32_t)d.rows), grid((uint32_t)d.rows * (uint32_t)d.chunks);
-    if (bytes <= kRowMost / 3) {
-        hipLaunchKernelGGL((sample_small_kernel<VF, kRowMost / 3>), rows, block, 0, st, d);
+    if (bytes <= kRowSmall) {
+        hipLaunchKernelGGL((sample_small_kernel<VF, kRowSmall>), rows, block, 0, st, d);
         return;
     }
-    if (bytes <= kRowMost) {
+    // one workgroup a row: where few tokens are asked for it takes half as long as several launches; where their share is, its exponentials take
+    // longer than those of many workgroups (165 rows of 32003, top-p and the distribution: 79 us instead of 45)
+    if (one_workgroup(d, bytes)) {
         hipLaunchKernelGGL((sample_small_kernel<VF, kRowMost>), rows, block, 0, st, d);
         return;
     }
@@ -875,7 +914,7 @@ static void launch_sample(const SampleDev &d, hipStream_t st) {
 }  // namespace csb
 
 extern "C" size_t csb_sample_workspace_bytes(int32_t n_rows, int32_t vocab) {
-    if (n_rows <= 0 || vocab <= csb::kSampleSmall) return 0;
+    if (n_rows <= 0 || vocab <= csb::kRowSmall / 4) return 0;
     return csb::sample_places(n_rows, csb::sample_chunks(vocab)).bytes;
 }
 
@@ -898,7 +937,7 @@ extern "C" int csb_sample(int32_t type, const void *d_logits, int64_t ld, const 
     d.rows = n_rows; d.vocab = vocab; d.tokens = d_tokens; d.probs = d_probs; d.ldp = ldprobs;
     d.chunks = sample_chunks(vocab);
     if (n_rows > 1 << 21 || (int64_t)n_rows * d.chunks > kMaxWorkgroups / 4) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
-    if ((int64_t)vocab * type_size(type) > kRowMost) {
+    if (!one_workgroup(d, (int64_t)vocab * type_size(type))) {
         if (!d_ws) return fail(CSB_EINVAL, "NULL workspace");
         if ((uintptr_t)d_ws % 256) return fail(CSB_EINVAL, "workspace not 256-byte aligned");
         const SamplePlaces p = sample_places(n_rows, d.chunks);
