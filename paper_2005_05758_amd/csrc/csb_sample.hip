@@ -41,6 +41,13 @@ struct SampleDev {
     uint64_t *ends, *totals, *list;
 };
 
+// a b + c, the constant in scalar registers (the compiler copies it to vector registers each time, to add to it there: three instructions instead of one).
+__device__ __forceinline__ double fma_of_constant(double a, double b, double c) {
+    double d;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "s"(c));
+    return d;
+}
+
 // What a row's numbers ask for.
 struct SampleRow {
     float m, per_bucket;
@@ -68,18 +75,18 @@ struct SampleRow {
     // units of a token; whole, below 2^39
     __device__ __forceinline__ double weight(float s) const {
         const double y = ((double)s - (double)m) * per_bit, n = __builtin_rint(y), f = y - n;
-        double e = 4.4455382718708110e-10;                              // (ln 2)^i / i!: e^(f ln 2), |f| <= 1/2, to 2^-42
-        e = __builtin_fma(e, f, 7.0549116208011233e-09);
-        e = __builtin_fma(e, f, 1.0178086009239699e-07);
-        e = __builtin_fma(e, f, 1.3215486790144309e-06);
-        e = __builtin_fma(e, f, 1.5252733804059840e-05);
-        e = __builtin_fma(e, f, 1.5403530393381609e-04);
-        e = __builtin_fma(e, f, 1.3333558146428443e-03);
-        e = __builtin_fma(e, f, 9.6181291076284772e-03);
-        e = __builtin_fma(e, f, 5.5504108664821580e-02);
-        e = __builtin_fma(e, f, 2.4022650695910071e-01);
-        e = __builtin_fma(e, f, 6.9314718055994531e-01);
-        e = __builtin_fma(e, f, 1.0);
+        double e = 4.4455382718708110e-10;                     // (ln 2)^i / i!: e^(f ln 2), |f| <= 1/2, to 2^-42
+        e = fma_of_constant(e, f, 7.0549116208011233e-09);
+        e = fma_of_constant(e, f, 1.0178086009239699e-07);
+        e = fma_of_constant(e, f, 1.3215486790144309e-06);
+        e = fma_of_constant(e, f, 1.5252733804059840e-05);
+        e = fma_of_constant(e, f, 1.5403530393381609e-04);
+        e = fma_of_constant(e, f, 1.3333558146428443e-03);
+        e = fma_of_constant(e, f, 9.6181291076284772e-03);
+        e = fma_of_constant(e, f, 5.5504108664821580e-02);
+        e = fma_of_constant(e, f, 2.4022650695910071e-01);
+        e = fma_of_constant(e, f, 6.9314718055994531e-01);
+        e = fma_of_constant(e, f, 1.0);
         const double w = __builtin_floor(__builtin_amdgcn_ldexp(e, (int)n + 38));
         return s == m ? kUnit : y > -40.0 ? w : 0.0;           // (infinite logits, and NaN of infinite temperatures)
     }
