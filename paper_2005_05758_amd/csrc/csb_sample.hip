@@ -10,9 +10,9 @@
 // (A place is the logit's bits and the token's number in 64 bits, so places differ and ties need no care.)  Tokens of the last bucket have no whole unit:
 // they are counted nowhere, and cannot be drawn.  Exponentials are binary64, which this card does as fast as binary32.
 //
-// Rows of up to kRowSmall bytes, and of kRowMost with top-k: one launch, a workgroup a row, which it holds in LDS.  Others, in chunks of 16384 tokens: maxima of groups; few, or the
-// histogram (rows that nothing is cut of: units of the chunks); the bucket's tokens and the units before it by chunk; the end of what is kept and the draw; the
-// distribution, if it is asked for.  Workgroups whose row is done, or is another's, leave at once.
+// Rows of up to kRowSmall bytes, and of kRowMost with top-k: one launch, a workgroup a row, which it holds in LDS.  Others, in chunks of 4096 tokens: maxima of groups; few; of the other
+// rows the histogram (where nothing is cut: units of the chunks), the bucket's tokens and the units before it by chunk, the end of what is kept and the
+// draw; the distribution, if it is asked for.
 #include <algorithm>
 #include <new>
 
@@ -21,10 +21,10 @@
 namespace csb {
 
 constexpr int kRowMost = 98304, kRowSmall = kRowMost / 3;      // bytes of a row that a workgroup may hold, and of one that it always does
-constexpr int kBuckets = 1024, kChunk = 16384, kMaxChunks = 1024, kListMost = 4096, kFewMost = 1024, kFewest = 256;
+constexpr int kBuckets = 1024, kChunk = 4096, kMaxChunks = 4096, kListMost = 4096, kFewMost = 1024, kFewest = 256;
 constexpr double kUnit = 274877906944.0;       // 2^38
 
-enum RowState : uint32_t { ROW_DONE, ROW_WHOLE, ROW_CUT, ROW_ALONE };    // drawn; nothing is cut; by the histogram; by one workgroup
+enum RowState : uint32_t { ROW_WHOLE, ROW_CUT, ROW_ALONE };    // nothing is cut; by the histogram; by one workgroup
 
 struct SampleDev {
     const void *logits;
@@ -34,10 +34,10 @@ struct SampleDev {
     void *probs;
     int64_t ld, ldp;
     int32_t rows, vocab, chunks;
-    // workspace: [rows][chunks], [rows][chunks][1024], [rows][kBuckets], [rows], [rows][kListMost]
+    // workspace: [rows][chunks], [rows][chunks][256], [rows][kBuckets], [rows], [rows][kListMost]; the rows that are not few (NULL: all of them), how many
     float *maxes, *groups;
     unsigned long long *units, *sums;
-    uint32_t *counts, *listed, *state;
+    uint32_t *counts, *listed, *others, *n_others;
     uint64_t *ends, *totals, *list;
 };
 
@@ -75,18 +75,16 @@ struct SampleRow {
     // units of a token; whole, below 2^39
     __device__ __forceinline__ double weight(float s) const {
         const double y = ((double)s - (double)m) * per_bit, n = __builtin_rint(y), f = y - n;
-        double e = 4.4455382718708110e-10;                     // (ln 2)^i / i!: e^(f ln 2), |f| <= 1/2, to 2^-42
-        e = fma_of_constant(e, f, 7.0549116208011233e-09);
-        e = fma_of_constant(e, f, 1.0178086009239699e-07);
-        e = fma_of_constant(e, f, 1.3215486790144309e-06);
-        e = fma_of_constant(e, f, 1.5252733804059840e-05);
-        e = fma_of_constant(e, f, 1.5403530393381609e-04);
-        e = fma_of_constant(e, f, 1.3333558146428443e-03);
-        e = fma_of_constant(e, f, 9.6181291076284772e-03);
-        e = fma_of_constant(e, f, 5.5504108664821580e-02);
-        e = fma_of_constant(e, f, 2.4022650695910071e-01);
-        e = fma_of_constant(e, f, 6.9314718055994531e-01);
-        e = fma_of_constant(e, f, 1.0);
+        double e = 1.0205905413765595e-07;                   // 2^f for |f| <= 1/2 to 2^-45, through ten of Chebyshev's points
+        e = fma_of_constant(e, f, 1.325964524488711e-06);
+        e = fma_of_constant(e, f, 1.5252672924850737e-05);
+        e = fma_of_constant(e, f, 0.0001540343375125101);
+        e = fma_of_constant(e, f, 0.0013333558200794592);
+        e = fma_of_constant(e, f, 0.009618129193934313);
+        e = fma_of_constant(e, f, 0.05550410866465167);
+        e = fma_of_constant(e, f, 0.2402265069564034);
+        e = fma_of_constant(e, f, 0.6931471805599462);
+        e = fma_of_constant(e, f, 1.0000000000000135);
         const double w = __builtin_floor(__builtin_amdgcn_ldexp(e, (int)n + 38));
         return s == m ? kUnit : y > -40.0 ? w : 0.0;           // (infinite logits, and NaN of infinite temperatures)
     }
@@ -389,9 +387,16 @@ template <typename Read> struct BucketTokens {
     }
 };
 
-// Units of a token of a row whose kept end at `end`.
-__device__ __forceinline__ double kept_units(const SampleRow &row, float s, int32_t v, uint64_t end) {
-    if (place(s, (uint32_t)v) < end) return 0.0;
+// The last token that is kept (its place 0: nothing is cut).
+struct SampleEnd {
+    float s;
+    uint32_t v;
+    __device__ __forceinline__ explicit SampleEnd(uint64_t end) : s(end ? logit_at(end) : -__builtin_inff()), v(end ? 0xffffffffu - (uint32_t)end : 0xffffffffu) {}
+    __device__ __forceinline__ bool keeps(float x, int32_t number) const { return x > s || (x == s && (uint32_t)number <= v); }
+};
+// Units of a token of a row.
+__device__ __forceinline__ double kept_units(const SampleRow &row, float s, int32_t v, const SampleEnd &end) {
+    if (!end.keeps(s, v)) return 0.0;
     const double w = row.weight(s);
     return w < row.least ? 0.0 : w;
 }
@@ -480,6 +485,7 @@ __device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &ro
         BucketTokens<Read> tokens{sh, row, read, vocab, list, 0};
         end = end_of_kept(sh, row, tokens);
     }
+    const SampleEnd last(end);
     const int32_t per = (vocab + 4095) / 4096 * 256, first = wave * per, stop = min(first + per, vocab);
     uint64_t mine = 0;
 #pragma unroll 1
@@ -488,7 +494,7 @@ __device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &ro
         read(v, s);
         double here = 0.0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) here += kept_units(row, s[j], v + j, end);
+        for (int j = 0; j < 4; ++j) here += kept_units(row, s[j], v + j, last);
         mine += whole(here);
     }
     mine = sum_of_wave(mine);
@@ -510,7 +516,7 @@ __device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &ro
             read(v0 + 4 * lane, s);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                u[j] = whole(kept_units(row, s[j], v0 + 4 * lane + j, end));
+                u[j] = whole(kept_units(row, s[j], v0 + 4 * lane + j, last));
                 sum += u[j];
             }
             uint64_t at = before + before_in_wave(sum);
@@ -529,7 +535,7 @@ __device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &ro
 
 // The distribution's entries from v on.
 template <int VF>
-__device__ __forceinline__ void probs_of(const SampleRow &row, void *to, int32_t v, int32_t vocab, const float *s, uint64_t end, double per) {
+__device__ __forceinline__ void probs_of(const SampleRow &row, void *to, int32_t v, int32_t vocab, const float *s, const SampleEnd &end, double per) {
     float x[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = per > 0.0 ? (float)(kept_units(row, s[j], v + j, end) * per) : 0.0f;
@@ -580,78 +586,118 @@ __global__ __launch_bounds__(1024) void sample_small_kernel(const SampleDev a) {
     if (a.probs) {
         void *to = (T *)a.probs + (int64_t)number * a.ldp;
         const double per = kept.total ? 1.0 / (double)kept.total : 0.0;
+        const SampleEnd last(kept.end);
 #pragma unroll 1
         for (int32_t v = 4 * tid; v < a.vocab; v += 4096) {
             float s[4];
             read(v, s);
-            probs_of<VF>(row, to, v, a.vocab, s, kept.end, per);
+            probs_of<VF>(row, to, v, a.vocab, s, last, per);
         }
     }
 }
 
-// ---- larger rows: a workgroup of 1024 threads a chunk, sixteen tokens a thread ---------------------------------------------------------------
-__device__ __forceinline__ float max_of_row(SampleShared &sh, const SampleDev &a, int row) {
-    return block_max(sh, (int)threadIdx.x < a.chunks ? a.maxes[(int64_t)row * a.chunks + threadIdx.x] : -__builtin_inff());
+// ---- larger rows: a workgroup of 256 threads a chunk, sixteen tokens a thread -----------------------------------------------------------------
+__device__ __forceinline__ float max_of_wave(float m) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    return m;
 }
-// Sixteen tokens of a chunk that starts at `first`: numbers first + 4096 (i / 4) + 4 tid + i % 4.
-template <int VF> __device__ __forceinline__ void chunk_tokens(const SampleDev &a, int row, int32_t first, float (*s)[4]) {
+// The row's largest logit, by every wavefront for itself.
+__device__ __forceinline__ float max_of_row(const SampleDev &a, int row) {
+    float m = -__builtin_inff();
+    for (int i = threadIdx.x & 63; i < a.chunks; i += 64) m = fmaxf(m, a.maxes[(int64_t)row * a.chunks + i]);
+    return max_of_wave(m);
+}
+// Sixteen tokens of a chunk: numbers chunk_number(c, 0 .. 15).
+__device__ __forceinline__ int32_t chunk_number(int c, int i) { return c * kChunk + 1024 * (i / 4) + 4 * (int)threadIdx.x + i % 4; }
+template <int VF> __device__ __forceinline__ void chunk_tokens(const SampleDev &a, int row, int c, float (*s)[4]) {
     const void *from = (const typename Elem<VF>::T *)a.logits + (int64_t)row * a.ld;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) logits4<VF>(from, first + 4096 * i + 4 * (int)threadIdx.x, a.vocab, s[i]);
+    for (int i = 0; i < 4; ++i) logits4<VF>(from, chunk_number(c, 4 * i), a.vocab, s[i]);
 }
-__device__ __forceinline__ int32_t chunk_number(int32_t first, int i) { return first + 4096 * (i / 4) + 4 * (int)threadIdx.x + i % 4; }
+// The chunks of rows that are not few, by all workgroups in turn: work(row, chunk).  (The barrier is between two turns' use of LDS.)
+template <typename Work> __device__ __forceinline__ void for_other_chunks(const SampleDev &a, Work work) {
+    const uint32_t n = (a.others ? *a.n_others : (uint32_t)a.rows) * (uint32_t)a.chunks;
+    for (uint32_t i = blockIdx.x; i < n; i += gridDim.x) {     // (uniform)
+        const uint32_t row = i / (uint32_t)a.chunks;
+        work(a.others ? (int)a.others[row] : (int)row, (int)(i % (uint32_t)a.chunks));
+        __syncthreads();
+    }
+}
+__device__ __forceinline__ RowState state_of(const SampleRow &row) {      // (few that were too many, and both ends: the second is known when the first is)
+    return !row.cut() ? ROW_WHOLE : row.k && (row.k <= kFewest || row.p < 1u << 24) ? ROW_ALONE : ROW_CUT;
+}
+// Sum over 256 threads.
+__device__ __forceinline__ uint64_t sum_of_256(uint64_t v, uint64_t *part) {
+    v = sum_of_wave(v);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return part[0] + part[1] + part[2] + part[3];
+}
 
 template <int VF>
-__global__ __launch_bounds__(1024) void sample_max_kernel(const SampleDev a) {
-    __shared__ SampleShared sh;
+__global__ __launch_bounds__(256) void sample_max_kernel(const SampleDev a) {
+    __shared__ float part[4];
     const int row = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
     float s[4][4], m = -__builtin_inff();
-    chunk_tokens<VF>(a, row, c * kChunk, s);
+    chunk_tokens<VF>(a, row, c, s);
 #pragma unroll
     for (int i = 0; i < 16; ++i) m = fmaxf(m, s[i / 4][i % 4]);
-    a.groups[(int64_t)blockIdx.x * 1024 + tid] = m;
-    m = block_max(sh, m);
-    if (tid == 0) a.maxes[blockIdx.x] = m;
+    a.groups[(int64_t)blockIdx.x * 256 + tid] = m;
+    m = max_of_wave(m);
+    if ((tid & 63) == 0) part[tid >> 6] = m;
+    __syncthreads();
+    if (tid == 0) a.maxes[blockIdx.x] = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
     if (c == 0) {                                              // the row's histogram starts empty
-        a.counts[(int64_t)row * kBuckets + tid] = 0;
-        a.units[(int64_t)row * kBuckets + tid] = 0;
+#pragma unroll
+        for (int i = 0; i < kBuckets / 256; ++i) {
+            a.counts[(int64_t)row * kBuckets + 256 * i + tid] = 0;
+            a.units[(int64_t)row * kBuckets + 256 * i + tid] = 0;
+        }
         if (tid == 0) a.listed[row] = 0;
+        if (row == 0 && tid == 0) *a.n_others = 0;
     }
 }
 
-// Few tokens by the row's first workgroup; the histogram, or the chunk's units where nothing is cut, by all.
+// Few tokens; the other rows are noted.
 template <int VF>
-__global__ __launch_bounds__(1024) void sample_first_kernel(const SampleDev a) {
+__global__ __launch_bounds__(1024) void sample_few_kernel(const SampleDev a) {
     __shared__ SampleShared sh;
-    __shared__ uint64_t list[kListMost];
-    const int number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
-    const float m = max_of_row(sh, a, number);
+    __shared__ uint64_t list[kFewMost];
+    __shared__ uint32_t hits[kFewMost];
+    const int number = blockIdx.x, tid = threadIdx.x, n_groups = a.chunks * 256;
+    const float *groups = a.groups + (int64_t)number * n_groups;
+    float g[8];                                                // the first 8192 groups stay in registers
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = 1024 * i + tid < n_groups ? groups[1024 * i + tid] : -__builtin_inff();
+    const float m = max_of_row(a, number);
     const SampleRow row(a, number, m);
-    const bool any = m > -__builtin_inff();
-    if (any && row.k && row.k <= kFewest) {                    // (uniform)
-        if (c) return;
-        const float *groups = a.groups + (int64_t)number * a.chunks * 1024;
-        const int b = bucket_of_first(sh, row, [&](auto take) {
-#pragma unroll 8
-            for (int i = tid; i < a.chunks * 1024; i += 1024) take(groups[i]);
-        });
+    bool few = m == -__builtin_inff();                         // (nothing to draw from)
+    Kept kept{0, 0, -1};
+    if (!few && row.k && row.k <= kFewest) {                   // (uniform)
+        const auto each = [&](auto take) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) take(g[i], 1024 * i + tid);
+#pragma unroll 1
+            for (int i = 8192 + tid; i < n_groups; i += 1024) take(groups[i], i);
+        };
+        const int b = bucket_of_first(sh, row, [&](auto take) { each([&](float m, int) { take(m); }); });
         // the groups that have tokens up to that bucket, then their tokens, four to a thread
-        uint32_t *hits = (uint32_t *)list + kListMost;         // (the list's second half)
         if (tid == 0) { sh.listed = 0; sh.bin_count = 0; }
         __syncthreads();
-#pragma unroll 8
-        for (int i = tid; i < a.chunks * 1024; i += 1024)
-            if (row.bucket(groups[i]) <= b) {
+        each([&](float m, int i) {
+            if (row.bucket(m) <= b) {
                 const uint32_t n = atomicAdd(&sh.bin_count, 1u);
                 if (n < (uint32_t)kFewMost) hits[n] = i;
             }
+        });
         __syncthreads();
         const uint32_t n = sh.bin_count;
         if (n <= (uint32_t)kFewMost) {
             const void *from = (const typename Elem<VF>::T *)a.logits + (int64_t)number * a.ld;
             for (uint32_t i = tid; i < n * 4; i += 1024) {
-                const uint32_t g = hits[i / 4];
-                const int32_t v = (int32_t)(g >> 10) * kChunk + 4096 * (int32_t)(i & 3) + 4 * (int32_t)(g & 1023);
+                const uint32_t h = hits[i / 4];
+                const int32_t v = (int32_t)(h >> 8) * kChunk + 1024 * (int32_t)(i & 3) + 4 * (int32_t)(h & 255);
                 float s[4];
                 logits4<VF>(from, v, a.vocab, s);
 #pragma unroll
@@ -663,110 +709,138 @@ __global__ __launch_bounds__(1024) void sample_first_kernel(const SampleDev a) {
             }
         }
         __syncthreads();
-        const bool few = n <= (uint32_t)kFewMost && sh.listed <= (uint32_t)kFewMost;
-        if (few) {
-            const Kept kept = draw_of_few(sh, row, list, sh.listed, a.tokens ? draw_number(a.r[number]) : 0);
-            if (tid == 0) {
-                if (a.tokens) a.tokens[number] = kept.token;
-                a.ends[number] = kept.end;
-                a.totals[number] = kept.total;
-            }
-        }
-        if (tid == 0) a.state[number] = few ? ROW_DONE : ROW_ALONE;
-        return;
+        few = n <= (uint32_t)kFewMost && sh.listed <= (uint32_t)kFewMost;
+        if (few) kept = draw_of_few(sh, row, list, sh.listed, a.tokens ? draw_number(a.r[number]) : 0);
     }
-    // (one of the two ends: of both the second is known when the first is)
-    const uint32_t state = !any ? ROW_DONE : !row.cut() ? ROW_WHOLE : row.k && row.p < 1u << 24 ? ROW_ALONE : ROW_CUT;
-    if (c == 0 && tid == 0) {
-        a.state[number] = state;
-        if (!any) {
-            if (a.tokens) a.tokens[number] = -1;
-            a.ends[number] = a.totals[number] = 0;
-        }
-    }
-    if (state == ROW_DONE || state == ROW_ALONE) return;
-    float s[4][4];
-    chunk_tokens<VF>(a, number, c * kChunk, s);
-    if (state == ROW_WHOLE) {
-        double here = 0.0;                                     // (16 weights: exact)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) here += kept_units(row, s[i / 4][i % 4], chunk_number(c * kChunk, i), 0);
-        uint64_t all;
-        block_before(sh, whole(here), &all);
-        if (tid == 0) a.sums[blockIdx.x] = all;
-        return;
-    }
-    sh.counts[tid] = 0;
-    sh.units[tid] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float x = s[i / 4][i % 4];
-        const int b = row.bucket(x);
-        if (b < kBuckets - 1) {
-            if (row.k) atomicAdd(&sh.counts[b], 1u);
-            atomicAdd(&sh.units[b], (unsigned long long)whole(row.weight(x)));
-        }
-    }
-    __syncthreads();
-    if (sh.units[tid] || sh.counts[tid]) {
-        if (row.k) atomicAdd(&a.counts[(int64_t)number * kBuckets + tid], sh.counts[tid]);
-        atomicAdd(&a.units[(int64_t)number * kBuckets + tid], sh.units[tid]);
-    }
+    if (tid) return;
+    if (few) {
+        if (a.tokens) a.tokens[number] = kept.token;
+        a.ends[number] = kept.end;
+        a.totals[number] = kept.total;
+    } else a.others[atomicAdd(a.n_others, 1u)] = number;
 }
 
-// The row's histogram in LDS, and the bucket in which what is kept ends (kBuckets: nothing is cut); sh.base_*: what lies before it.  *target: of find_bin.
-__device__ __forceinline__ int bucket_of_row(SampleShared &sh, const SampleDev &a, int number, const SampleRow &row, uint64_t *target) {
+// The histogram of rows that are cut; the chunk's units of those that are not.
+template <int VF>
+__global__ __launch_bounds__(256) void sample_histogram_kernel(const SampleDev a) {
+    __shared__ unsigned long long bins[kBuckets];              // units, and from 2^51 on tokens: both of 4096 tokens of 2^38 at most
+    __shared__ uint64_t part[4];
     const int tid = threadIdx.x;
-    __syncthreads();
-    sh.counts[tid] = a.counts[(int64_t)number * kBuckets + tid];
-    const uint64_t u = sh.units[tid] = a.units[(int64_t)number * kBuckets + tid];
-    if (tid == 0) { sh.base_count = 0; sh.base_units = 0; sh.bin = kBuckets; }
-    uint64_t all;
-    block_before(sh, u, &all);
-    if (row.k) find_bin<true>(sh, *target = (uint64_t)row.k);
-    else {
-        const uint64_t part = part_of(all, row.p);
-        find_bin<false>(sh, *target = part ? part : 1);
+    for_other_chunks(a, [&](int number, int c) {
+        float s[4][4];
+        chunk_tokens<VF>(a, number, c, s);
+        const float m = max_of_row(a, number);
+        const SampleRow row(a, number, m);
+        const RowState state = state_of(row);
+        const bool any = m > -__builtin_inff();
+        if (state == ROW_ALONE) return;
+        if (state == ROW_WHOLE || !any) {
+            const SampleEnd all(0);
+            double here = 0.0;                                 // (16 weights: exact)
+#pragma unroll 4
+            for (int i = 0; i < 16; ++i) here += any ? kept_units(row, s[i / 4][i % 4], 0, all) : 0.0;
+            const uint64_t sum = sum_of_256(whole(here), part);
+            if (tid == 0) a.sums[(int64_t)number * a.chunks + c] = sum;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kBuckets / 256; ++i) bins[256 * i + tid] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float x = s[i / 4][i % 4];
+            const int b = row.bucket(x);
+            if (b < kBuckets - 1) atomicAdd(&bins[b], (unsigned long long)(whole(row.weight(x)) + (1ull << 51)));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kBuckets / 256; ++i) {
+            const unsigned long long v = bins[256 * i + tid];
+            if (v) {
+                if (row.k) atomicAdd(&a.counts[(int64_t)number * kBuckets + 256 * i + tid], (uint32_t)(v >> 51));
+                atomicAdd(&a.units[(int64_t)number * kBuckets + 256 * i + tid], v & ((1ull << 51) - 1));
+            }
+        }
+    });
+}
+
+// The bucket in which what is kept of a row ends, by 256 threads, four buckets each (kBuckets: nothing is cut).
+__device__ __forceinline__ int bucket_of_256(const SampleDev &a, int number, const SampleRow &row, uint64_t *part, int *found) {
+    const int tid = threadIdx.x, wave = tid >> 6;
+    uint64_t u[4], mine = 0, all = 0, before;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        u[i] = row.k ? a.counts[(int64_t)number * kBuckets + 4 * tid + i] : a.units[(int64_t)number * kBuckets + 4 * tid + i];
+        mine += u[i];
     }
-    return (int)sh.bin;
+    before = before_in_wave(mine);
+    if ((tid & 63) == 63) part[wave] = before + mine;
+    if (tid == 0) *found = kBuckets;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) before += part[w];
+        all += part[w];
+    }
+    const uint64_t share = part_of(all, row.p), target = row.k ? (uint64_t)row.k : share ? share : 1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (before < target && before + u[i] >= target) *found = 4 * tid + i;    // one thread, or none
+        before += u[i];
+    }
+    __syncthreads();
+    return *found;
 }
 
 // Rows that are cut: the tokens of the bucket in which what is kept ends, in any order, and the units of the chunk before it.
 template <int VF>
-__global__ __launch_bounds__(1024) void sample_bucket_kernel(const SampleDev a) {
-    __shared__ SampleShared sh;
-    const int number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
-    if (a.state[number] != ROW_CUT) return;
-    float s[4][4];
-    chunk_tokens<VF>(a, number, c * kChunk, s);
-    const float m = max_of_row(sh, a, number);
-    const SampleRow row(a, number, m);
-    uint64_t target;
-    const int bucket = bucket_of_row(sh, a, number, row, &target);
-    double here = 0.0;
-    uint32_t mine = 0;                                         // which of the sixteen are the bucket's
+__global__ __launch_bounds__(256) void sample_bucket_kernel(const SampleDev a) {
+    __shared__ float kept[kChunk];
+    __shared__ uint64_t part[4];
+    __shared__ int found;
+    __shared__ uint32_t n_kept, at;
+    const int tid = threadIdx.x;
+    for_other_chunks(a, [&](int number, int c) {
+        float s[4][4];
+        chunk_tokens<VF>(a, number, c, s);
+        const float m = max_of_row(a, number);
+        const SampleRow row(a, number, m);
+        if (state_of(row) != ROW_CUT || !(m > -__builtin_inff())) return;
+        if (tid == 0) n_kept = 0;
+        const int bucket = bucket_of_256(a, number, row, part, &found);
+        uint32_t mine = 0;                                     // which of the sixteen are the bucket's
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float x = s[i / 4][i % 4];
-        const int b = row.bucket(x);
-        if (b < bucket) here += kept_units(row, x, 0, 0);
-        else if (b == bucket) mine |= 1u << i;
-    }
-    uint64_t total;
-    uint32_t at = (uint32_t)block_before(sh, (uint64_t)__builtin_popcount(mine), &total);
-    if (tid == 0) sh.listed = total ? atomicAdd(&a.listed[number], (uint32_t)total) : 0;     // a place for the workgroup's
-    __syncthreads();
-    at += sh.listed;
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (mine >> i & 1) {
-            if (at < (uint32_t)kListMost) a.list[(int64_t)number * kListMost + at] = place(s[i / 4][i % 4], chunk_number(c * kChunk, i));
-            ++at;
+        for (int i = 0; i < 16; ++i) {
+            const float x = s[i / 4][i % 4];
+            const int b = row.bucket(x);
+            if (b == bucket) mine |= 1u << i;
+            if (b < bucket && b < kBuckets - 1) kept[atomicAdd(&n_kept, 1u)] = x;
         }
-    uint64_t all;
-    block_before(sh, whole(here), &all);
-    if (tid == 0) a.sums[blockIdx.x] = all;
+        const uint32_t count = __builtin_popcount(mine), below = before_in_wave(count);
+        __syncthreads();
+        if ((tid & 63) == 63) part[tid >> 6] = below + count;
+        __syncthreads();
+        if (tid == 0) {
+            const uint32_t total = (uint32_t)(part[0] + part[1] + part[2] + part[3]);
+            at = total ? atomicAdd(&a.listed[number], total) : 0;               // a place for the workgroup's
+        }
+        __syncthreads();
+        uint32_t to = at + below;
+        for (int w = 0; w < (tid >> 6); ++w) to += (uint32_t)part[w];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (mine >> i & 1) {
+                if (to < (uint32_t)kListMost) a.list[(int64_t)number * kListMost + to] = place(s[i / 4][i % 4], chunk_number(c, i));
+                ++to;
+            }
+        const SampleEnd none(0);
+        uint64_t sum = 0;                                      // the weights of the kept alone, side by side
+        const uint32_t n = n_kept;
+        for (uint32_t i = tid; i < n; i += 256) sum += whole(kept_units(row, kept[i], 0, none));
+        __syncthreads();                                       // (part is read)
+        sum = sum_of_256(sum, part);
+        if (tid == 0) a.sums[(int64_t)number * a.chunks + c] = sum;
+    });
 }
 
 // Tokens of a bucket, in a list alone.
@@ -784,11 +858,13 @@ __global__ __launch_bounds__(1024) void sample_draw_kernel(const SampleDev a) {
     __shared__ SampleShared sh;
     __shared__ uint64_t list[kListMost];
     __shared__ unsigned long long sums[kMaxChunks];
-    const int number = blockIdx.x, tid = threadIdx.x;
-    const uint32_t state = a.state[number];
-    if (state == ROW_DONE) return;
-    const float m = max_of_row(sh, a, number);
+    const int tid = threadIdx.x;
+    if (a.others && blockIdx.x >= *a.n_others) return;
+    const int number = a.others ? (int)a.others[blockIdx.x] : (int)blockIdx.x;
+    const float m = max_of_row(a, number);
     const SampleRow row(a, number, m);
+    const bool any = m > -__builtin_inff();
+    const RowState state = any ? state_of(row) : ROW_WHOLE;
     const uint32_t r = a.tokens ? draw_number(a.r[number]) : 0;
     const uint32_t listed = state == ROW_CUT ? a.listed[number] : 0;
     if (state == ROW_ALONE || listed > (uint32_t)kListMost) {
@@ -802,79 +878,120 @@ __global__ __launch_bounds__(1024) void sample_draw_kernel(const SampleDev a) {
         return;
     }
     uint64_t end = 0;
-    sums[tid] = tid < a.chunks ? a.sums[(int64_t)number * a.chunks + tid] : 0;
+#pragma unroll
+    for (int i = 0; i < kMaxChunks / 1024; ++i) {
+        const int c = 1024 * i + tid;
+        sums[c] = any && c < a.chunks ? a.sums[(int64_t)number * a.chunks + c] : 0;
+    }
     if (state == ROW_CUT) {
         for (uint32_t i = tid; i < listed; i += 1024) list[i] = a.list[(int64_t)number * kListMost + i];
-        uint64_t target;
-        const int bucket = bucket_of_row(sh, a, number, row, &target);
-        if (bucket < kBuckets) {
+        sh.counts[tid] = a.counts[(int64_t)number * kBuckets + tid];
+        const uint64_t u = sh.units[tid] = a.units[(int64_t)number * kBuckets + tid];
+        if (tid == 0) { sh.base_count = 0; sh.base_units = 0; sh.bin = kBuckets; }
+        uint64_t all, target = (uint64_t)row.k;
+        block_before(sh, u, &all);
+        if (row.k) find_bin<true>(sh, target);
+        else {
+            const uint64_t share = part_of(all, row.p);
+            target = share ? share : 1;
+            find_bin<false>(sh, target);
+        }
+        if (sh.bin < (uint32_t)kBuckets) {                     // (uniform)
             const ListedTokens tokens{row, list, listed};
             if (row.k) find_token<true>(sh, target, tokens);
             else find_token<false>(sh, target, tokens);
             end = sh.found;
-            for (uint32_t i = tid; i < listed; i += 1024)
-                if (list[i] >= end) {
-                    const uint32_t v = 0xffffffffu - (uint32_t)list[i];
-                    atomicAdd(&sums[v / kChunk], (unsigned long long)whole(kept_units(row, logit_at(list[i]), v, end)));
-                }
+            const SampleEnd last(end);
+            for (uint32_t i = tid; i < listed; i += 1024) {
+                const uint32_t v = 0xffffffffu - (uint32_t)list[i];
+                const uint64_t w = whole(kept_units(row, logit_at(list[i]), v, last));
+                if (w) atomicAdd(&sums[v / kChunk], (unsigned long long)w);
+            }
         }
     }
     __syncthreads();
-    uint64_t all;
-    const uint64_t here = sums[tid], before = block_before(sh, here, &all), limit = part_of(all, r);
+    uint64_t all, mine[kMaxChunks / 1024], sum = 0;            // four chunks a thread
+#pragma unroll
+    for (int i = 0; i < kMaxChunks / 1024; ++i) sum += mine[i] = sums[kMaxChunks / 1024 * tid + i];
+    uint64_t before = block_before(sh, sum, &all);
+    const uint64_t limit = part_of(all, r);
     if (tid == 0) {
         a.ends[number] = end;
         a.totals[number] = all;
+        sh.bin = kMaxChunks;
+        sh.token = -1;
     }
     if (!a.tokens) return;
-    if (tid == 0) { sh.bin = kMaxChunks; sh.token = -1; }
     __syncthreads();
-    if (before <= limit && limit < before + here) { sh.bin = tid; sh.base_units = before; }
+#pragma unroll
+    for (int i = 0; i < kMaxChunks / 1024; ++i) {
+        if (before <= limit && limit < before + mine[i]) { sh.bin = kMaxChunks / 1024 * tid + i; sh.base_units = before; }
+        before += mine[i];
+    }
     __syncthreads();
-    const uint32_t c = sh.bin;
-    if (c < (uint32_t)kMaxChunks) {                            // (any weight)
-        uint64_t from = sh.base_units;
+    if (sh.bin < (uint32_t)kMaxChunks) {                       // (uniform: any weight) the chunk's tokens, four a thread
+        const int32_t v = (int32_t)sh.bin * kChunk + 4 * tid;
+        const SampleEnd last(end);
+        float s[4];
+        uint64_t u[4], here = 0, total;
+        logits4<VF>((const typename Elem<VF>::T *)a.logits + (int64_t)number * a.ld, v, a.vocab, s);
 #pragma unroll 1
-        for (int i = 0; i < 4; ++i) {                          // 4096 tokens by number, four a thread
-            const int32_t v = (int32_t)c * kChunk + 4096 * i + 4 * tid;
-            float s[4];
-            uint64_t u[4], sum = 0, part;
-            logits4<VF>((const typename Elem<VF>::T *)a.logits + (int64_t)number * a.ld, v, a.vocab, s);
+        for (int j = 0; j < 4; ++j) here += u[j] = whole(kept_units(row, s[j], v + j, last));
+        uint64_t at = sh.base_units + block_before(sh, here, &total);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                u[j] = whole(kept_units(row, s[j], v + j, end));
-                sum += u[j];
-            }
-            uint64_t at = from + block_before(sh, sum, &part);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (at <= limit && limit < at + u[j]) sh.token = v + j;
-                at += u[j];
-            }
-            from += part;
-            if (limit < from) break;                           // (uniform)
+        for (int j = 0; j < 4; ++j) {
+            if (at <= limit && limit < at + u[j]) sh.token = v + j;
+            at += u[j];
         }
     }
     __syncthreads();
     if (tid == 0) a.tokens[number] = sh.token;
 }
 
+// The distribution: zeros, and in their places the kept, side by side.
 template <int VF>
-__global__ __launch_bounds__(1024) void sample_probs_kernel(const SampleDev a) {
-    __shared__ SampleShared sh;
-    const int number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks;
+__global__ __launch_bounds__(256) void sample_probs_kernel(const SampleDev a) {
+    using T = typename Elem<VF>::T;
+    using T4 = T __attribute__((ext_vector_type(4)));
+    __shared__ T4 out[kChunk / 4];
+    __shared__ float kept[kChunk];
+    __shared__ uint16_t places[kChunk];
+    __shared__ uint32_t n_kept;
+    const int number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
     float s[4][4];
-    chunk_tokens<VF>(a, number, c * kChunk, s);
-    const float m = max_of_row(sh, a, number);
+    chunk_tokens<VF>(a, number, c, s);
+    const float m = max_of_row(a, number);
     const SampleRow row(a, number, m);
-    const uint64_t end = a.ends[number], all = a.totals[number];
-    const double per = all ? 1.0 / (double)all : 0.0;
-    void *to = (typename Elem<VF>::T *)a.probs + (int64_t)number * a.ldp;
+    const SampleEnd last(a.ends[number]);
+    const uint64_t all = a.totals[number];
+    if (tid == 0) n_kept = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) probs_of<VF>(row, to, chunk_number(c * kChunk, 4 * i), a.vocab, s[i], end, per);
+    for (int i = 0; i < 4; ++i) out[256 * i + tid] = T4{};
+    __syncthreads();
+    if (all) {                                                 // (uniform)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (last.keeps(s[i / 4][i % 4], chunk_number(c, i))) {
+                const uint32_t n = atomicAdd(&n_kept, 1u);
+                kept[n] = s[i / 4][i % 4];
+                places[n] = (uint16_t)(1024 * (i / 4) + 4 * tid + i % 4);
+            }
+        __syncthreads();
+        const double per = 1.0 / (double)all;
+        const SampleEnd none(0);
+        for (uint32_t i = tid; i < n_kept; i += 256) ((T *)out)[places[i]] = (T)(float)(kept_units(row, kept[i], 0, none) * per);
+        __syncthreads();
+    }
+    void *to = (T *)a.probs + (int64_t)number * a.ldp;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const T4 x = out[256 * i + tid];
+        const float y[4] = {(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
+        probs4<VF>(to, chunk_number(c, 4 * i), a.vocab, y);
+    }
 }
 
-struct SamplePlaces { size_t maxes, groups, units, sums, counts, listed, state, ends, totals, list, bytes; };
+struct SamplePlaces { size_t maxes, groups, units, sums, counts, listed, others, n_others, ends, totals, list, bytes; };
 static SamplePlaces sample_places(int64_t rows, int64_t chunks) {
     SamplePlaces p{};
     size_t at = 0;
@@ -885,10 +1002,11 @@ static SamplePlaces sample_places(int64_t rows, int64_t chunks) {
     p.ends = take((size_t)rows * 8);
     p.totals = take((size_t)rows * 8);
     p.counts = take((size_t)rows * kBuckets * 4);
-    p.groups = take((size_t)rows * chunks * 1024 * 4);
+    p.groups = take((size_t)rows * chunks * 256 * 4);
     p.maxes = take((size_t)rows * chunks * 4);
     p.listed = take((size_t)rows * 4);
-    p.state = take((size_t)rows * 4);
+    p.others = take((size_t)rows * 4);
+    p.n_others = take(4);
     p.bytes = at;
     return p;
 }
@@ -899,7 +1017,7 @@ static bool one_workgroup(const SampleDev &d, int64_t bytes) { return bytes <= k
 template <int VF>
 static void launch_sample(const SampleDev &d, hipStream_t st) {
     const int64_t bytes = (int64_t)d.vocab * (VF == CSB_VAL_F32 ? 4 : 2);
-    const dim3 block(1024), rows((uint32_t)d.rows), grid((uint32_t)d.rows * (uint32_t)d.chunks);
+    const dim3 block(1024), rows((uint32_t)d.rows);
     if (bytes <= kRowSmall) {
         hipLaunchKernelGGL((sample_small_kernel<VF, kRowSmall>), rows, block, 0, st, d);
         return;
@@ -910,12 +1028,14 @@ static void launch_sample(const SampleDev &d, hipStream_t st) {
         hipLaunchKernelGGL((sample_small_kernel<VF, kRowMost>), rows, block, 0, st, d);
         return;
     }
-    hipLaunchKernelGGL(sample_max_kernel<VF>, grid, block, 0, st, d);
-    hipLaunchKernelGGL(sample_first_kernel<VF>, grid, block, 0, st, d);
-    if (d.top_k || d.top_p || d.temperature)                   // (a temperature of zero cuts too)
-        hipLaunchKernelGGL(sample_bucket_kernel<VF>, grid, block, 0, st, d);
+    const int64_t chunks = (int64_t)d.rows * d.chunks;
+    const dim3 few(256), all((uint32_t)chunks), some((uint32_t)std::min<int64_t>(chunks, d.others ? 1024 : chunks));
+    hipLaunchKernelGGL(sample_max_kernel<VF>, all, few, 0, st, d);
+    if (d.others) hipLaunchKernelGGL(sample_few_kernel<VF>, rows, block, 0, st, d);
+    hipLaunchKernelGGL(sample_histogram_kernel<VF>, some, few, 0, st, d);
+    if (d.top_k || d.top_p || d.temperature) hipLaunchKernelGGL(sample_bucket_kernel<VF>, some, few, 0, st, d);
     hipLaunchKernelGGL(sample_draw_kernel<VF>, rows, block, 0, st, d);
-    if (d.probs) hipLaunchKernelGGL(sample_probs_kernel<VF>, grid, block, 0, st, d);
+    if (d.probs) hipLaunchKernelGGL(sample_probs_kernel<VF>, all, few, 0, st, d);
 }
 
 }  // namespace csb
@@ -943,7 +1063,7 @@ extern "C" int csb_sample(int32_t type, const void *d_logits, int64_t ld, const 
     d.logits = d_logits; d.ld = ld; d.temperature = d_temperature; d.top_k = d_top_k; d.top_p = d_top_p; d.min_p = d_min_p; d.r = d_r;
     d.rows = n_rows; d.vocab = vocab; d.tokens = d_tokens; d.probs = d_probs; d.ldp = ldprobs;
     d.chunks = sample_chunks(vocab);
-    if (n_rows > 1 << 21 || (int64_t)n_rows * d.chunks > kMaxWorkgroups / 4) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
+    if (n_rows > 1 << 21 || (int64_t)n_rows * d.chunks > kMaxWorkgroups) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
     if (!one_workgroup(d, (int64_t)vocab * type_size(type))) {
         if (!d_ws) return fail(CSB_EINVAL, "NULL workspace");
         if ((uintptr_t)d_ws % 256) return fail(CSB_EINVAL, "workspace not 256-byte aligned");
@@ -951,7 +1071,9 @@ extern "C" int csb_sample(int32_t type, const void *d_logits, int64_t ld, const 
         char *ws = (char *)d_ws;
         d.units = (unsigned long long *)(ws + p.units); d.sums = (unsigned long long *)(ws + p.sums); d.list = (uint64_t *)(ws + p.list);
         d.ends = (uint64_t *)(ws + p.ends); d.totals = (uint64_t *)(ws + p.totals); d.counts = (uint32_t *)(ws + p.counts);
-        d.groups = (float *)(ws + p.groups); d.maxes = (float *)(ws + p.maxes); d.listed = (uint32_t *)(ws + p.listed); d.state = (uint32_t *)(ws + p.state);
+        d.groups = (float *)(ws + p.groups); d.maxes = (float *)(ws + p.maxes); d.listed = (uint32_t *)(ws + p.listed);
+        d.n_others = (uint32_t *)(ws + p.n_others);
+        if (d_top_k || d_temperature) d.others = (uint32_t *)(ws + p.others);  // (a temperature of zero asks for one token)
         try {
             static const char sample_user = 0;                 // this entry point as a user of workspaces
             workspace_changed_hands(d_ws, &sample_user);
