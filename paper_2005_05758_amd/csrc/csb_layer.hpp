@@ -7,14 +7,22 @@
 namespace csb {
 
 #ifdef __HIPCC__
+// A vector at the address of any element.  (By a copy: an alignment given to a vector type's alias in its declaration is not taken up, and of an address
+// that is the same for all lanes the scalar unit then reads whole words, the low bits left out.)
+template <typename V, typename T> __device__ __forceinline__ V load_any(const T *p) {
+    V v;
+    __builtin_memcpy(&v, p, sizeof(V));
+    return v;
+}
+template <typename V, typename T> __device__ __forceinline__ void store_any(T *p, const V &v) { __builtin_memcpy(p, &v, sizeof(V)); }
+
 // Eight elements from p[0] on, of which the first `there` are (the others are zeros, or are not stored); p at any element.
 template <int VF> struct Run8 {
     using T = typename Elem<VF>::T;
     using T8 = T __attribute__((ext_vector_type(8)));
-    using T8_any = T __attribute__((ext_vector_type(8), aligned(sizeof(T)), may_alias));
     T8 v;
     __device__ __forceinline__ void load(const T *p, int there) {
-        if (there >= 8) v = *(const T8_any *)p;
+        if (there >= 8) v = load_any<T8>(p);
         else {
             v = T8{};
 #pragma unroll
@@ -24,7 +32,7 @@ template <int VF> struct Run8 {
     __device__ __forceinline__ float operator[](int j) const { return (float)v[j]; }
     __device__ __forceinline__ void set(int j, float x) { v[j] = (T)x; }
     __device__ __forceinline__ void store(T *p, int there) const {
-        if (there >= 8) *(T8_any *)p = v;
+        if (there >= 8) store_any(p, v);
         else {
 #pragma unroll
             for (int j = 0; j < 7; ++j) if (j < there) p[j] = v[j];

@@ -44,7 +44,7 @@ template <bool NEAR, bool WHOLE, bool ROWS_ONLY> struct NormAccess {
     __device__ __forceinline__ bool by_columns() const { return !ROWS_ONLY && o.columns; }
     // entries j .. j + 7, the first `there` of them
     __device__ __forceinline__ Raw8 load(int64_t j, int there) const {
-        using u32x4 = uint32_t __attribute__((ext_vector_type(4), aligned(2), may_alias));
+        using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
         Raw8 r{};
         const bool half = o.type != CSB_VAL_F32;               // (uniform, as the order)
         if (WHOLE && there <= 0) return r;
@@ -70,7 +70,7 @@ template <bool NEAR, bool WHOLE, bool ROWS_ONLY> struct NormAccess {
         } else if (half) {
             const uint16_t *p = (const uint16_t *)o.d + t * o.ld + j;
             if (WHOLE || there >= 8) {
-                const u32x4 v = *(const u32x4 *)p;
+                const u32x4 v = load_any<u32x4>(p);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) r.w[i] = v[i];
             } else {
@@ -80,7 +80,7 @@ template <bool NEAR, bool WHOLE, bool ROWS_ONLY> struct NormAccess {
         } else {
             const uint32_t *p = (const uint32_t *)o.d + t * o.ld + j;
             if (WHOLE || there >= 8) {
-                const u32x4 v = *(const u32x4 *)p, u = *(const u32x4 *)(p + 4);
+                const u32x4 v = load_any<u32x4>(p), u = load_any<u32x4>(p + 4);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) { r.w[i] = v[i]; r.w[4 + i] = u[i]; }
             } else {
@@ -109,7 +109,7 @@ template <bool NEAR, bool WHOLE, bool ROWS_ONLY> struct NormAccess {
         }
     }
     __device__ __forceinline__ void store(int64_t j, int there, const float *v) const {
-        using u32x4 = uint32_t __attribute__((ext_vector_type(4), aligned(2), may_alias));
+        using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
         if (WHOLE && there <= 0) return;
         const bool half = o.type != CSB_VAL_F32;
         uint32_t b[8];
@@ -137,7 +137,7 @@ template <bool NEAR, bool WHOLE, bool ROWS_ONLY> struct NormAccess {
         const int64_t from = columns ? j * o.ld + t : t * o.ld + j, by = columns ? o.ld : 1;
         if (half) {
             uint16_t *p = (uint16_t *)o.d + from;
-            if (!columns && (WHOLE || there >= 8)) *(u32x4 *)p = u32x4{b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16};
+            if (!columns && (WHOLE || there >= 8)) store_any(p, u32x4{b[0] | b[1] << 16, b[2] | b[3] << 16, b[4] | b[5] << 16, b[6] | b[7] << 16});
             else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) if (WHOLE || i < there) p[i * by] = (uint16_t)b[i];
@@ -145,8 +145,8 @@ template <bool NEAR, bool WHOLE, bool ROWS_ONLY> struct NormAccess {
         } else {
             uint32_t *p = (uint32_t *)o.d + from;
             if (!columns && (WHOLE || there >= 8)) {
-                *(u32x4 *)p = u32x4{b[0], b[1], b[2], b[3]};
-                *(u32x4 *)(p + 4) = u32x4{b[4], b[5], b[6], b[7]};
+                store_any(p, u32x4{b[0], b[1], b[2], b[3]});
+                store_any(p + 4, u32x4{b[4], b[5], b[6], b[7]});
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) if (WHOLE || i < there) p[i * by] = b[i];
@@ -156,10 +156,10 @@ template <bool NEAR, bool WHOLE, bool ROWS_ONLY> struct NormAccess {
 };
 // Eight factors: `fill` where there is no vector of them; zeros behind the row's end, so that what is not there stays zero.
 template <bool WHOLE> __device__ __forceinline__ void norm_factors(const float *p, int64_t j, int there, float fill, float *v) {
-    using f32x4 = float __attribute__((ext_vector_type(4), aligned(4), may_alias));
+    using f32x4 = float __attribute__((ext_vector_type(4)));
     if (WHOLE ? there > 0 : there >= 8) {
         if (p) {
-            const f32x4 a = *(const f32x4 *)(p + j), b = *(const f32x4 *)(p + j + 4);
+            const f32x4 a = load_any<f32x4>(p + j), b = load_any<f32x4>(p + j + 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
         } else {
@@ -536,7 +536,7 @@ __global__ __launch_bounds__(1024) void block_norm_product_kernel(const NormDev 
                     const uint32_t from = at(a.x, sizeof(X), j0);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) run.v[j] = __builtin_bit_cast(X, window_load<X>(xw, from + j * x_step));
-                } else if (there > 0) run.v = *(const typename Run8<VFX>::T8_any *)(xp + j0);
+                } else if (there > 0) run.v = load_any<typename Run8<VFX>::T8>(xp + j0);
             }
             norm_factors<true>(a.s, j0, a.width - j0, 1.0f, s);
             if (a.after) {
@@ -557,7 +557,7 @@ __global__ __launch_bounds__(1024) void block_norm_product_kernel(const NormDev 
                     const uint32_t to = at(a.r, sizeof(X), j0);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) window_store<X>(rw, to + j * r_step, run.v[j]);
-                } else if (there > 0) *(typename Run8<VFX>::T8_any *)(rp + j0) = run.v;
+                } else if (there > 0) store_any(rp + j0, run.v);
             }
         }
     if (!a.before) return;

@@ -10,7 +10,7 @@
 // (A place is the logit's bits and the token's number in 64 bits, so places differ and ties need no care.)  Tokens of the last bucket have no whole unit:
 // they are counted nowhere, and cannot be drawn.  Exponentials are binary64, which this card does as fast as binary32.
 //
-// Rows of up to kRowSmall bytes, and of kRowMost with top-k: one launch, a workgroup a row, which it holds in LDS.  Others, in chunks of 4096 tokens: maxima of groups; few; of the other
+// Rows of up to kRowMost bytes: one launch, a workgroup a row, which it holds in LDS.  Others, in chunks of 4096 tokens: maxima of groups; few; of the other
 // rows the histogram (where nothing is cut: units of the chunks), the bucket's tokens and the units before it by chunk, the end of what is kept and the
 // draw; the distribution, if it is asked for.
 #include <algorithm>
@@ -20,8 +20,8 @@
 
 namespace csb {
 
-constexpr int kRowMost = 98304, kRowSmall = kRowMost / 3;      // bytes of a row that a workgroup may hold, and of one that it always does
-constexpr int kBuckets = 1024, kChunk = 4096, kMaxChunks = 4096, kListMost = 4096, kFewMost = 1024, kFewest = 256;
+constexpr int kRowMost = 98304, kRowSmall = kRowMost / 3;      // bytes of a row that a workgroup holds; of one that leaves room for another workgroup
+constexpr int kBuckets = 1024, kChunk = 4096, kMaxChunks = 4096, kListMost = 4096, kFewMost = 1024, kFewest = 256, kRankMost = 320;
 constexpr double kUnit = 274877906944.0;       // 2^38
 
 enum RowState : uint32_t { ROW_WHOLE, ROW_CUT, ROW_ALONE };    // nothing is cut; by the histogram; by one workgroup
@@ -110,10 +110,10 @@ __device__ __forceinline__ uint32_t draw_number(float r) { return r > 0.0f ? min
 // Four logits from v on; -infinity past `end`.
 template <int VF> __device__ __forceinline__ void logits4(const void *row, int32_t v, int32_t end, float *s) {
     using T = typename Elem<VF>::T;
-    using T4 = T __attribute__((ext_vector_type(4), aligned(sizeof(T)), may_alias));
+    using T4 = T __attribute__((ext_vector_type(4)));
     const T *p = (const T *)row + v;
     if (v + 4 <= end) {
-        const T4 x = *(const T4 *)p;
+        const T4 x = load_any<T4>(p);
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[j] = logit((float)x[j]);
     } else {
@@ -123,13 +123,13 @@ template <int VF> __device__ __forceinline__ void logits4(const void *row, int32
 }
 template <int VF> __device__ __forceinline__ void probs4(void *row, int32_t v, int32_t end, const float *x) {
     using T = typename Elem<VF>::T;
-    using T4 = T __attribute__((ext_vector_type(4), aligned(sizeof(T)), may_alias));
+    using T4 = T __attribute__((ext_vector_type(4)));
     T *p = (T *)row + v;
     if (v + 4 <= end) {
         T4 y;
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = (T)x[j];
-        *(T4 *)p = y;
+        store_any(p, y);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) if (v + j < end) p[j] = (T)x[j];
@@ -266,40 +266,59 @@ template <bool BY_COUNT, typename Tokens> __device__ __forceinline__ void find_t
     __syncthreads();
 }
 
+// The same among the `n` tokens of a list in LDS, at most kRankMost: ranked against each other, then one sum (n^2 / 16 clocks: a search by parts
+// takes as long from 400 tokens on).
+template <bool BY_COUNT> __device__ __forceinline__ void find_ranked(SampleShared &sh, const SampleRow &row, uint64_t target, const uint64_t *list, uint32_t n) {
+    const uint32_t tid = threadIdx.x;
+    const uint64_t at = tid < n ? list[tid] : 0;
+    uint32_t rank = 0;
+    if (tid < n)
+#pragma unroll 8
+        for (uint32_t i = 0; i < n; ++i) rank += list[i] > at;
+    if (tid < n) sh.units[rank] = whole(row.weight(logit_at(at)));
+    const uint32_t base_count = sh.base_count;
+    const uint64_t base_units = sh.base_units;
+    __syncthreads();
+    if (tid == 0) { sh.found = 0; sh.found_units = 0; sh.bin = kBuckets; }
+    const uint64_t u = tid < n ? sh.units[tid] : 0;
+    uint64_t all, before = block_before(sh, u, &all) + base_units;
+    if (tid < n && (BY_COUNT ? base_count + tid + 1 == target : before < target && before + u >= target)) {     // one thread
+        sh.bin = tid;
+        sh.found_units = before + u;
+    }
+    __syncthreads();
+    if (tid < n && rank == sh.bin) sh.found = at;
+    __syncthreads();
+}
+
 // Where what is kept of a row ends: the last token's place (0: nothing is cut).  sh.units and sh.counts hold the row's histogram.
 template <typename Tokens>
 __device__ __forceinline__ uint64_t end_of_kept(SampleShared &sh, const SampleRow &row, Tokens &tokens) {
     const int tid = threadIdx.x;
     const uint32_t c = sh.counts[tid];
     const uint64_t u = sh.units[tid];
-    auto restore = [&] {                                       // the histogram again (a search uses its place), from the start
+    uint64_t units, target = (uint64_t)row.k, end = 0;
+    block_before(sh, u, &units);
+#pragma unroll 1
+    for (int turn = row.k ? 0 : 1; turn < (row.p < 1u << 24 ? 2 : 1); ++turn) {  // (uniform) by count, then by share of what that leaves
         __syncthreads();
-        sh.counts[tid] = c;
+        sh.counts[tid] = c;                                    // (a search uses their place)
         sh.units[tid] = u;
         if (tid == 0) { sh.base_count = 0; sh.base_units = 0; sh.bin = kBuckets; }
         __syncthreads();
-    };
-    restore();
-    uint64_t end = 0, units;
-    block_before(sh, u, &units);
-    if (row.k) {
-        find_bin<true>(sh, (uint64_t)row.k);
-        if (sh.bin < kBuckets) {                               // (uniform) else fewer tokens than k have units
-            tokens.gather((int)sh.bin);
-            find_token<true>(sh, (uint64_t)row.k, tokens);
-            end = sh.found;
-            units = sh.found_units;
+        if (turn == 0) find_bin<true>(sh, target);
+        else {
+            const uint64_t share = part_of(units, row.p);
+            target = share ? share : 1;
+            find_bin<false>(sh, target);
         }
-    }
-    if (row.p < 1u << 24) {
-        const uint64_t part = part_of(units, row.p), target = part ? part : 1;
-        restore();
-        find_bin<false>(sh, target);
-        if (sh.bin < kBuckets) {
-            tokens.gather((int)sh.bin);
-            find_token<false>(sh, target, tokens);
-            end = sh.found;
-        }
+        if (sh.bin >= (uint32_t)kBuckets) continue;            // (uniform) fewer tokens than k have units
+        tokens.gather((int)sh.bin);
+        const bool few = sh.listed <= (uint32_t)kRankMost;
+        if (turn == 0) few ? find_ranked<true>(sh, row, target, tokens.list, sh.listed) : find_token<true>(sh, target, tokens);
+        else few ? find_ranked<false>(sh, row, target, tokens.list, sh.listed) : find_token<false>(sh, target, tokens);
+        end = sh.found;
+        units = sh.found_units;
     }
     return end;
 }
@@ -458,6 +477,33 @@ template <typename Each> __device__ __forceinline__ int bucket_of_first(SampleSh
     return (int)sh.bin;
 }
 
+// Tokens of one wavefront that come one by one to some lanes, worked on 64 at a time: `buffer` holds 128 of them.
+template <typename Item> struct WaveStream {
+    Item *buffer;
+    uint32_t held = 0;
+    template <typename Work> __device__ __forceinline__ void add(bool mine, const Item &item, Work work) {
+        const uint64_t who = __ballot(mine);
+        if (mine) buffer[held + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = item;
+        held += (uint32_t)__builtin_popcountll(who);
+        if (held >= 64) {                                      // (uniform in the wavefront, whose own LDS accesses stay in order)
+            const uint32_t lane = threadIdx.x & 63;
+            __builtin_amdgcn_wave_barrier();
+            const Item first = buffer[lane], next = buffer[64 + lane];
+            __builtin_amdgcn_wave_barrier();
+            work(first, true);
+            held -= 64;
+            if (lane < held) buffer[lane] = next;
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    template <typename Work> __device__ __forceinline__ void rest(Work work) {
+        __builtin_amdgcn_wave_barrier();
+        const bool there = (threadIdx.x & 63) < held;
+        work(buffer[threadIdx.x & 63], there);
+        held = 0;
+    }
+};
+
 // A row by one workgroup of 1024 threads.  Wavefront w draws from the `per` tokens from w per on, 256 at a time.
 template <typename Read>
 __device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &row, const Read &read, int32_t vocab, uint64_t *list, uint32_t number) {
@@ -488,15 +534,20 @@ __device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &ro
     const SampleEnd last(end);
     const int32_t per = (vocab + 4095) / 4096 * 256, first = wave * per, stop = min(first + per, vocab);
     uint64_t mine = 0;
+    __syncthreads();                                           // (the list's place is the streams' now)
+    WaveStream<float> stream{(float *)list + 128 * wave};
+    const auto add_up = [&](float x, bool there) {
+        const double w = row.weight(x);
+        if (there && w >= row.least) mine += whole(w);
+    };
 #pragma unroll 1
-    for (int32_t v = first + 4 * lane; v < stop; v += 256) {
+    for (int32_t v0 = first; v0 < stop; v0 += 256) {
         float s[4];
-        read(v, s);
-        double here = 0.0;
+        read(v0 + 4 * lane, s);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) here += kept_units(row, s[j], v + j, last);
-        mine += whole(here);
+        for (int j = 0; j < 4; ++j) stream.add(s[j] > -__builtin_inff() && last.keeps(s[j], v0 + 4 * lane + j), s[j], add_up);
     }
+    stream.rest(add_up);
     mine = sum_of_wave(mine);
     __syncthreads();
     if (lane == 0) sh.part_units[wave] = mine;
@@ -533,20 +584,10 @@ __device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &ro
     return {end, all, sh.token};
 }
 
-// The distribution's entries from v on.
-template <int VF>
-__device__ __forceinline__ void probs_of(const SampleRow &row, void *to, int32_t v, int32_t vocab, const float *s, const SampleEnd &end, double per) {
-    float x[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = per > 0.0 ? (float)(kept_units(row, s[j], v + j, end) * per) : 0.0f;
-    probs4<VF>(to, v, vocab, x);
-}
-
 template <int VF, int BYTES>
 __global__ __launch_bounds__(1024) void sample_small_kernel(const SampleDev a) {
     using T = typename Elem<VF>::T;
     using T4 = T __attribute__((ext_vector_type(4)));
-    using T4_any = T __attribute__((ext_vector_type(4), aligned(sizeof(T)), may_alias));
     __shared__ SampleShared sh;
     __shared__ uint64_t list[kListMost];
     __shared__ T4 held[BYTES / sizeof(T4)];
@@ -558,7 +599,7 @@ __global__ __launch_bounds__(1024) void sample_small_kernel(const SampleDev a) {
         const int32_t v = 4 * tid + 4096 * i;
         if (v < a.vocab) {
             T4 x;
-            if (v + 4 <= a.vocab) x = *(const T4_any *)(from + v);
+            if (v + 4 <= a.vocab) x = load_any<T4>(from + v);
             else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] = v + j < a.vocab ? from[v + j] : (T)-__builtin_inff();
@@ -584,14 +625,36 @@ __global__ __launch_bounds__(1024) void sample_small_kernel(const SampleDev a) {
     }
     if (a.tokens && tid == 0) a.tokens[number] = kept.token;
     if (a.probs) {
-        void *to = (T *)a.probs + (int64_t)number * a.ldp;
+        // zeros in the row's place, the kept over them, side by side
+        T *to = (T *)a.probs + (int64_t)number * a.ldp;
         const double per = kept.total ? 1.0 / (double)kept.total : 0.0;
         const SampleEnd last(kept.end);
+        struct Item { float s; int32_t v; };
+        __syncthreads();
+        WaveStream<Item> stream{(Item *)list + 128 * (tid >> 6)};
+        const auto set = [&](const Item &x, bool there) {
+            const double w = row.weight(x.s);
+            if (there) ((T *)held)[x.v] = (T)(float)(w < row.least ? 0.0 : w * per);
+        };
 #pragma unroll 1
-        for (int32_t v = 4 * tid; v < a.vocab; v += 4096) {
+        for (int32_t v0 = 0; v0 < a.vocab; v0 += 4096) {
+            const int32_t v = v0 + 4 * tid;
             float s[4];
             read(v, s);
-            probs_of<VF>(row, to, v, a.vocab, s, last, per);
+            if (v < a.vocab) held[v / 4] = T4{};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) stream.add(kept.total && s[j] > -__builtin_inff() && last.keeps(s[j], v + j), Item{s[j], v + j}, set);
+        }
+        stream.rest(set);
+        __syncthreads();
+#pragma unroll 1
+        for (int32_t v = 4 * tid; v < a.vocab; v += 4096) {
+            const T4 x = held[v / 4];
+            if (v + 4 <= a.vocab) store_any(to + v, x);
+            else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (v + j < a.vocab) to[v + j] = x[j];
+            }
         }
     }
 }
@@ -898,8 +961,9 @@ __global__ __launch_bounds__(1024) void sample_draw_kernel(const SampleDev a) {
         }
         if (sh.bin < (uint32_t)kBuckets) {                     // (uniform)
             const ListedTokens tokens{row, list, listed};
-            if (row.k) find_token<true>(sh, target, tokens);
-            else find_token<false>(sh, target, tokens);
+            const bool few = listed <= (uint32_t)kRankMost;
+            if (row.k) few ? find_ranked<true>(sh, row, target, list, listed) : find_token<true>(sh, target, tokens);
+            else few ? find_ranked<false>(sh, row, target, list, listed) : find_token<false>(sh, target, tokens);
             end = sh.found;
             const SampleEnd last(end);
             for (uint32_t i = tid; i < listed; i += 1024) {
@@ -953,10 +1017,9 @@ template <int VF>
 __global__ __launch_bounds__(256) void sample_probs_kernel(const SampleDev a) {
     using T = typename Elem<VF>::T;
     using T4 = T __attribute__((ext_vector_type(4)));
+    struct Item { float s; int32_t v; };
     __shared__ T4 out[kChunk / 4];
-    __shared__ float kept[kChunk];
-    __shared__ uint16_t places[kChunk];
-    __shared__ uint32_t n_kept;
+    __shared__ Item items[4 * 128];
     const int number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
     float s[4][4];
     chunk_tokens<VF>(a, number, c, s);
@@ -964,24 +1027,21 @@ __global__ __launch_bounds__(256) void sample_probs_kernel(const SampleDev a) {
     const SampleRow row(a, number, m);
     const SampleEnd last(a.ends[number]);
     const uint64_t all = a.totals[number];
-    if (tid == 0) n_kept = 0;
+    const double per = all ? 1.0 / (double)all : 0.0;
+    WaveStream<Item> stream{items + 128 * (tid >> 6)};
+    const auto set = [&](const Item &x, bool there) {          // (the wavefront's own tokens: behind its zeros)
+        const double w = row.weight(x.s);
+        if (there) ((T *)out)[x.v] = (T)(float)(w < row.least ? 0.0 : w * per);
+    };
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[256 * i + tid] = T4{};
-    __syncthreads();
-    if (all) {                                                 // (uniform)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (last.keeps(s[i / 4][i % 4], chunk_number(c, i))) {
-                const uint32_t n = atomicAdd(&n_kept, 1u);
-                kept[n] = s[i / 4][i % 4];
-                places[n] = (uint16_t)(1024 * (i / 4) + 4 * tid + i % 4);
-            }
-        __syncthreads();
-        const double per = 1.0 / (double)all;
-        const SampleEnd none(0);
-        for (uint32_t i = tid; i < n_kept; i += 256) ((T *)out)[places[i]] = (T)(float)(kept_units(row, kept[i], 0, none) * per);
-        __syncthreads();
+    for (int i = 0; i < 16; ++i) {
+        const float x = s[i / 4][i % 4];
+        stream.add(all && x > -__builtin_inff() && last.keeps(x, chunk_number(c, i)), Item{x, 1024 * (i / 4) + 4 * tid + i % 4}, set);
     }
+    stream.rest(set);
+    __syncthreads();
     void *to = (T *)a.probs + (int64_t)number * a.ldp;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -1012,8 +1072,6 @@ static SamplePlaces sample_places(int64_t rows, int64_t chunks) {
 }
 static int32_t sample_chunks(int32_t vocab) { return (vocab + kChunk - 1) / kChunk; }       // (at most kMaxChunks)
 
-static bool one_workgroup(const SampleDev &d, int64_t bytes) { return bytes <= kRowSmall || (bytes <= kRowMost && d.top_k); }
-
 template <int VF>
 static void launch_sample(const SampleDev &d, hipStream_t st) {
     const int64_t bytes = (int64_t)d.vocab * (VF == CSB_VAL_F32 ? 4 : 2);
@@ -1022,9 +1080,7 @@ static void launch_sample(const SampleDev &d, hipStream_t st) {
         hipLaunchKernelGGL((sample_small_kernel<VF, kRowSmall>), rows, block, 0, st, d);
         return;
     }
-    // one workgroup a row: where few tokens are asked for it takes half as long as several launches; where their share is, its exponentials take
-    // longer than those of many workgroups (165 rows of 32003, top-p and the distribution: 79 us instead of 45)
-    if (one_workgroup(d, bytes)) {
+    if (bytes <= kRowMost) {
         hipLaunchKernelGGL((sample_small_kernel<VF, kRowMost>), rows, block, 0, st, d);
         return;
     }
@@ -1041,7 +1097,7 @@ static void launch_sample(const SampleDev &d, hipStream_t st) {
 }  // namespace csb
 
 extern "C" size_t csb_sample_workspace_bytes(int32_t n_rows, int32_t vocab) {
-    if (n_rows <= 0 || vocab <= csb::kRowSmall / 4) return 0;
+    if (n_rows <= 0 || vocab <= csb::kRowMost / 4) return 0;
     return csb::sample_places(n_rows, csb::sample_chunks(vocab)).bytes;
 }
 
@@ -1064,7 +1120,7 @@ extern "C" int csb_sample(int32_t type, const void *d_logits, int64_t ld, const 
     d.rows = n_rows; d.vocab = vocab; d.tokens = d_tokens; d.probs = d_probs; d.ldp = ldprobs;
     d.chunks = sample_chunks(vocab);
     if (n_rows > 1 << 21 || (int64_t)n_rows * d.chunks > kMaxWorkgroups) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
-    if (!one_workgroup(d, (int64_t)vocab * type_size(type))) {
+    if ((int64_t)vocab * type_size(type) > kRowMost) {
         if (!d_ws) return fail(CSB_EINVAL, "NULL workspace");
         if ((uintptr_t)d_ws % 256) return fail(CSB_EINVAL, "workspace not 256-byte aligned");
         const SamplePlaces p = sample_places(n_rows, d.chunks);

@@ -180,14 +180,14 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
     }
 }
 
-// The same for the few tokens of a decoding step: a wavefront takes 16 channels by itself, without LDS and barriers, and its four lanes a
-// channel make the step alike.  The next token's operands are on their way while one is worked on.
-template <int VF, int K, bool FULL>
+// The same for the few tokens of a decoding step: P lanes a channel, K numbers each, a wavefront 64 / P channels by itself, without LDS and barriers.
+// The next token's operands are on their way while one is worked on.  (Four lanes a channel, as above, make its step and gate four times: 64
+// requests of one token, 4096 channels of 16 numbers, 14 us instead of 10.)
+template <int VF, int K, int P, bool FULL>
 __global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a, const uint32_t waves) {
     using T = typename Elem<VF>::T;
-    constexpr int W = K < 8 ? K : 8;
-    using TK = T __attribute__((ext_vector_type(W)));
-    using TK_any = T __attribute__((ext_vector_type(W), aligned(sizeof(T)), may_alias));
+    using Run = Run8<VF>;
+    using f32x4 = float __attribute__((ext_vector_type(4)));
     const uint32_t lane = threadIdx.x & 63u;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     if (wave >= waves) return;                                 // (no barrier in this kernel)
@@ -197,39 +197,48 @@ __global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a
     if (a.len) end = first + clamp64(a.len[seq], 0, end - first);
     const int32_t s = a.slot ? a.slot[seq] : seq;
     const bool known = s >= 0 && s < a.n_states;
-    const int c = (ct % a.group_tiles) * 16 + (int)(lane >> 2), j0 = (int)(lane & 3u) * K;
+    const int c = (ct % a.group_tiles) * (64 / P) + (int)(lane / P), j0 = (int)(lane % P) * K;
     const bool mine = c < a.per_group;
     const int64_t channel = (int64_t)group * a.per_group + (mine ? c : 0);
-    auto have = [&](int k) { return FULL || j0 + k < a.n; };
-    struct Token { TK b[K / W], c[K / W]; T x, dt, z; };
-    auto numbers = [&](const T *p, TK *v) {
-#pragma unroll
-        for (int i = 0; i < K / W; ++i) {
-            if (FULL || j0 + W * (i + 1) <= a.n) v[i] = *(const TK_any *)(p + W * i);
-            else {
-                v[i] = TK{};
-#pragma unroll
-                for (int j = 0; j < W; ++j) if (have(W * i + j)) v[i][j] = p[W * i + j];
-            }
-        }
-    };
+    const int there = FULL ? K : a.n - j0;                     // of the lane's K numbers
+    struct Token { Run b[K / 8], c[K / 8]; T x, dt, z; };
     auto load = [&](int64_t t, Token &w) {
-        numbers((const T *)a.B + t * a.ldB + (int64_t)group * a.n + j0, w.b);
-        numbers((const T *)a.C + t * a.ldC + (int64_t)group * a.n + j0, w.c);
+        const T *b = (const T *)a.B + t * a.ldB + (int64_t)group * a.n + j0, *cc = (const T *)a.C + t * a.ldC + (int64_t)group * a.n + j0;
+#pragma unroll
+        for (int i = 0; i < K / 8; ++i) {
+            w.b[i].load(b + 8 * i, FULL ? 8 : there - 8 * i);
+            w.c[i].load(cc + 8 * i, FULL ? 8 : there - 8 * i);
+        }
         w.x = ((const T *)a.x)[t * a.ldx + channel];
         w.dt = ((const T *)a.dt)[t * a.lddt + channel];
         w.z = a.z ? ((const T *)a.z)[t * a.ldz + channel] : (T)0.0f;
+    };
+    auto numbers = [&](const float *p, float *v) {
+#pragma unroll
+        for (int i = 0; i < K / 4; ++i) {
+            if (FULL || 4 * i + 4 <= there) {
+                const f32x4 x = load_any<f32x4>(p + 4 * i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[4 * i + j] = x[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[4 * i + j] = 4 * i + j < there ? p[4 * i + j] : 0.0f;
+            }
+        }
     };
     Token now{}, next{};
     if (first < end) load(first, now);
     float A[K], h[K];
     const int64_t state = (int64_t)s * a.channels * a.n + channel * a.n + j0;
+    if (a.s_in && known) numbers(a.s_in + state, h);           // (uniform)
+    else {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        A[k] = have(k) ? a.A[channel * a.n + j0 + k] * 1.44269502162933349609375f : 0.0f;
-        h[k] = a.s_in && known && have(k) ? a.s_in[state + k] : 0.0f;
+        for (int k = 0; k < K; ++k) h[k] = 0.0f;
     }
+    numbers(a.A + channel * a.n + j0, A);
     const float bias = a.bias ? a.bias[channel] : 0.0f, D = a.D ? a.D[channel] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) A[k] *= 1.44269502162933349609375f;
     for (int64_t t = first; t < end; ++t) {
         if (t + 1 < end) load(t + 1, next);
         const float x = (float)now.x;
@@ -238,20 +247,28 @@ __global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a
         const float in = step * x;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            h[k] = fmaf(__builtin_amdgcn_exp2f(step * A[k]), h[k], in * (float)now.b[k / W][k % W]);
-            if (!FULL) h[k] = have(k) ? h[k] : 0.0f;
-            y = fmaf((float)now.c[k / W][k % W], h[k], y);
+            h[k] = fmaf(__builtin_amdgcn_exp2f(step * A[k]), h[k], in * now.b[k / 8][k % 8]);
+            if (!FULL) h[k] = k < there ? h[k] : 0.0f;         // (infinite inputs make NaN of zeros)
+            y = fmaf(now.c[k / 8][k % 8], h[k], y);
         }
-        y += quad_xor<1>(y);
-        y += quad_xor<2>(y);
+        if constexpr (P > 1) y += quad_xor<1>(y);
+        if constexpr (P > 2) y += quad_xor<2>(y);
+        if constexpr (P > 4) y += __shfl_xor(y, 4);
         y = fmaf(D, x, y);
         if (a.z) y *= silu((float)now.z);
-        if (mine && (lane & 3u) == 0) ((T *)a.out)[t * a.ldo + channel] = (T)y;
+        if (mine && lane % P == 0) ((T *)a.out)[t * a.ldo + channel] = (T)y;
         now = next;
     }
     if (a.s_out && known && mine)
 #pragma unroll
-        for (int k = 0; k < K; ++k) if (have(k)) a.s_out[state + k] = h[k];
+        for (int i = 0; i < K / 4; ++i) {
+            float *p = a.s_out + state + 4 * i;
+            if (FULL || 4 * i + 4 <= there) store_any(p, f32x4{h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]});
+            else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (4 * i + j < there) p[j] = h[4 * i + j];
+            }
+        }
 }
 
 // Chunks of a call, as a power of two of tokens (31: whole sequences).
@@ -266,6 +283,8 @@ static int scan_shift(const csb_scan_args *a, int64_t col_tiles) {
     return shift;
 }
 
+static int scan_lanes(int32_t n) { return n <= 16 ? 1 : n <= 32 ? 2 : n <= 64 ? 4 : 8; }     // a channel, of the kernel for few tokens
+
 struct ScanPlan { int32_t group_tiles; int64_t col_tiles, tiles; int shift; bool few; size_t begin, bytes; };
 static Refusal scan_plan(const csb_scan_args *a, ScanPlan *p) {
     if (!a) return {CSB_EINVAL, "NULL arguments"};
@@ -277,7 +296,7 @@ static Refusal scan_plan(const csb_scan_args *a, ScanPlan *p) {
     *p = ScanPlan{};
     if (a->n_seq == 0) return {CSB_OK, nullptr};
     p->few = a->n_tokens / a->n_seq <= kScanFew;
-    const int cols = p->few ? 16 : kScanCols;
+    const int cols = p->few ? 64 / scan_lanes(a->n) : kScanCols;
     p->group_tiles = (a->channels / a->groups + cols - 1) / cols;
     p->col_tiles = (int64_t)p->group_tiles * a->groups;
     p->shift = p->few ? 31 : scan_shift(a, p->col_tiles);
@@ -290,26 +309,36 @@ static Refusal scan_plan(const csb_scan_args *a, ScanPlan *p) {
     return {CSB_OK, nullptr};
 }
 
+template <int VF, int K, int P>
+static void launch_scan_few(const ScanDev &d, uint32_t waves, hipStream_t st) {
+    if (d.n == K * P) hipLaunchKernelGGL((selective_scan_few_kernel<VF, K, P, true>), dim3((waves + 3) / 4), dim3(256), 0, st, d, waves);
+    else hipLaunchKernelGGL((selective_scan_few_kernel<VF, K, P, false>), dim3((waves + 3) / 4), dim3(256), 0, st, d, waves);
+}
 template <int VF, int K, bool FULL>
-static void launch_scan(const ScanDev &d, bool few, dim3 grid, hipStream_t st) {
-    if (few) {
-        hipLaunchKernelGGL((selective_scan_few_kernel<VF, K, FULL>), dim3((grid.x + 3) / 4), dim3(256), 0, st, d, grid.x);
-        return;
-    }
+static void launch_scan(const ScanDev &d, dim3 grid, hipStream_t st) {
     if (d.shift < 31) hipLaunchKernelGGL((selective_scan_kernel<VF, K, FULL, false>), grid, dim3(256), 0, st, d);
     hipLaunchKernelGGL((selective_scan_kernel<VF, K, FULL, true>), grid, dim3(256), 0, st, d);
 }
 template <int VF, int K>
-static void launch_scan(const ScanDev &d, bool few, dim3 grid, hipStream_t st) {
-    if (d.n == 4 * K) launch_scan<VF, K, true>(d, few, grid, st);
-    else launch_scan<VF, K, false>(d, few, grid, st);
+static void launch_scan(const ScanDev &d, dim3 grid, hipStream_t st) {
+    if (d.n == 4 * K) launch_scan<VF, K, true>(d, grid, st);
+    else launch_scan<VF, K, false>(d, grid, st);
 }
 template <int VF>
 static void launch_scan(const ScanDev &d, bool few, dim3 grid, hipStream_t st) {
-    if (d.n <= 16) launch_scan<VF, 4>(d, few, grid, st);
-    else if (d.n <= 32) launch_scan<VF, 8>(d, few, grid, st);
-    else if (d.n <= 64) launch_scan<VF, 16>(d, few, grid, st);
-    else launch_scan<VF, 32>(d, few, grid, st);
+    if (few) {
+        switch (scan_lanes(d.n)) {
+            case 1: d.n <= 8 ? launch_scan_few<VF, 8, 1>(d, grid.x, st) : launch_scan_few<VF, 16, 1>(d, grid.x, st); break;
+            case 2: launch_scan_few<VF, 16, 2>(d, grid.x, st); break;
+            case 4: launch_scan_few<VF, 16, 4>(d, grid.x, st); break;
+            default: launch_scan_few<VF, 16, 8>(d, grid.x, st); break;
+        }
+        return;
+    }
+    if (d.n <= 16) launch_scan<VF, 4>(d, grid, st);
+    else if (d.n <= 32) launch_scan<VF, 8>(d, grid, st);
+    else if (d.n <= 64) launch_scan<VF, 16>(d, grid, st);
+    else launch_scan<VF, 32>(d, grid, st);
 }
 
 }  // namespace csb

@@ -93,6 +93,14 @@ def test_one_sequence(fmt, T, C, G, n):
 
 
 @types
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 16, 17, 32, 33, 60, 64, 65, 128])
+def test_few_tokens(fmt, n):
+    """Decoding: a few tokens of every request, of drafts of different lengths."""
+    check(fmt, 11, 70, 2, n, lengths=[1, 4, 0, 2, 3, 1], slots=[5, 0, 3, -1, 7, 1], n_states=8, seed=n)
+    check(fmt, 12, 130, 1, n, lengths=[4, 4, 4], lens=[1, 4, 0], seed=n + 1)
+
+
+@types
 def test_packed_sequences(fmt):
     lengths = [1, 0, 64, 3, 128, 65, 0, 0, 31, 2]
     check(fmt, sum(lengths), 70, 2, 16, lengths=lengths, seed=3)
