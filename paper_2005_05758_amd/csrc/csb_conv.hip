@@ -4,11 +4,13 @@
 // Bound by HBM: every input is read once, every output written once; the W - 1 inputs before a tile come from the caches.  A thread
 // has eight channels (their W weights in registers) and walks down kConvRun tokens with the last W - 1 inputs in registers.  The first tile of
 // a sequence also makes its new state: it alone reads the old one, so a state may be replaced in place while later tiles run.
+#include <type_traits>
+
 #include "csb_layer.hpp"
 
 namespace csb {
 
-constexpr int kConvRun = 16;
+constexpr int kConvRun = 16, kConvAhead = 4;
 
 struct ConvDev {
     const void *x;
@@ -50,32 +52,52 @@ __global__ __launch_bounds__(256) void short_conv_kernel(const ConvDev a) {
     };
     const int64_t t0 = (number << a.shift) + row * kConvRun, t1 = t0 + kConvRun < count ? t0 + kConvRun : count;
     if (t0 < count) {
-        float w[W][8], bias[8];
-        Run v[W];
+        float w[W][8], bias[8], v[W][8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) bias[i] = a.bias && i < there ? a.bias[c + i] : 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int j = 0; j < W; ++j) w[j][i] = i < there ? a.w[(int64_t)(c + i) * W + j] : 0.0f;
+        auto widen = [&](const Run &r, float *to) {
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j) v[j] = input(t0 - (W - 1) + j);
-        T *out = (T *)a.out + first * a.ldo + c;
-#pragma unroll 4
-        for (int64_t t = t0; t < t1; ++t) {
-            v[W - 1].load(x + t * a.ldx, there);
-            Run o;
+            for (int i = 0; i < 8; ++i) to[i] = r[i];
+        };
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float y = bias[i];
+        for (int j = 0; j < W - 1; ++j) widen(input(t0 - (W - 1) + j), v[j]);
+        const T *from = x + t0 * a.ldx;
+        T *out = (T *)a.out + (first + t0) * a.ldo + c;
+        const int n = (int)(t1 - t0);
+        // kConvAhead tokens are requested together
+        auto tokens = [&](auto whole, int count) {
+            Run in[kConvAhead];
 #pragma unroll
-                for (int j = 0; j < W; ++j) y = fmaf(w[j][i], v[j][i], y);
-                o.set(i, a.silu ? silu(y) : y);
-            }
-            o.store(out + t * a.ldo, there);
+            for (int k = 0; k < kConvAhead; ++k)
+                if (whole || k < count) in[k].load(from + k * a.ldx, there);
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) v[j] = v[j + 1];
-        }
+            for (int k = 0; k < kConvAhead; ++k)
+                if (whole || k < count) {
+                    widen(in[k], v[W - 1]);
+                    Run o;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float y = bias[i];
+#pragma unroll
+                        for (int j = 0; j < W; ++j) y = fmaf(w[j][i], v[j][i], y);
+                        o.set(i, a.silu ? silu<VF>(y) : y);
+                    }
+                    o.store(out + k * a.ldo, there);
+#pragma unroll
+                    for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[j][i] = v[j + 1][i];
+                }
+            from += kConvAhead * a.ldx;
+            out += kConvAhead * a.ldo;
+        };
+        int t = 0;
+        for (; t + kConvAhead <= n; t += kConvAhead) tokens(std::true_type{}, kConvAhead);
+        if (t < n) tokens(std::false_type{}, n - t);
     }
     if (W > 1 && number == 0 && row == 0 && a.s_out && known) {
         Run v[W];

@@ -55,7 +55,13 @@ __device__ __forceinline__ float sigmoid_within(float x) {
     const float e = exp_within(-fabsf(x));
     return (x < 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e);
 }
-__device__ __forceinline__ float silu(float x) { return x * sigmoid_within(x); }
+// The same for results that are rounded to 16 bits: the argument of the exponential rounded once, 1.3 |x| units of 2^-24 off (2^-12 of a result's rounding for |x| up to 8),
+// half as many instructions.
+template <int VF> __device__ __forceinline__ float sigmoid_for(float x) {
+    if constexpr (VF == CSB_VAL_F32) return sigmoid_within(x);
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269502162933349609375f));
+}
+template <int VF> __device__ __forceinline__ float silu(float x) { return x * sigmoid_for<VF>(x); }
 
 // ln(1 + e^x) = max(x, 0) + ln(1 + e), e = e^-|x| in (0, 1]: 2 atanh(e / (2 + e)), whose series in (e / (2 + e))^2 <= 1/9 is cut where
 // 9^-8 / 17 is left (2^-29): small steps keep all of their digits, which ln(1 + e) of a rounded sum would not.

@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 float y = fmaf(D[i], x[i], row[2 * i]);
-                if (a.z) y *= silu(z[i]);
+                if (a.z) y *= silu<VF>(z[i]);
                 o.set(i, y);
             }
             o.store((T *)a.out + (first + t + st) * a.ldo + base + sc, there);
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a
         if constexpr (P > 2) y += quad_xor<2>(y);
         if constexpr (P > 4) y += __shfl_xor(y, 4);
         y = fmaf(D, x, y);
-        if (a.z) y *= silu((float)now.z);
+        if (a.z) y *= silu<VF>((float)now.z);
         if (mine && lane % P == 0) ((T *)a.out)[t * a.ldo + channel] = (T)y;
         now = next;
     }

@@ -24,7 +24,13 @@ def silu(x):
     return x * sigmoid(x)
 
 
-def conv(x, w, b, act, ranges, slots, state):
+def gate_off(fmt, x):
+    """What SiLU is off of its value: the exponential 4 U (argument and all), sum, reciprocal and product 4 U more; where it is rounded to 16 bits afterwards its
+    argument x log2 e is two numbers' rounded product, U of |x| log2 e of ln 2 each: 1 + 1/4 |x| U (log2 e's own rounding is below U / 4)."""
+    return (8 + (0.0 if fmt == "f32" else 1.25) * np.abs(x)) * U
+
+
+def conv(x, w, b, act, ranges, slots, state, fmt):
     """x [T, C], w [C, W], state [n, W - 1, C].  Returns (out, off, state): out is NaN where no sequence has a token."""
     T, C = x.shape
     W = w.shape[1]
@@ -35,14 +41,14 @@ def conv(x, w, b, act, ranges, slots, state):
         y = b + sum(v[j:j + n] * w[:, j] for j in range(W))
         size = np.abs(b) + sum(np.abs(v[j:j + n] * w[:, j]) for j in range(W))
         out[first:end] = silu(y) if act else y
-        # the sum: W + 1 roundings.  SiLU's slope is at most 1.1; its exponential 4 U (argument and all), sum, reciprocal and product 4 U more
-        off[first:end] = 1.1 * (W + 1) * U * size + 8 * U * np.abs(out[first:end])
+        # the sum: W + 1 roundings.  SiLU's slope is at most 1.1
+        off[first:end] = 1.1 * (W + 1) * U * size + gate_off(fmt, y) * np.abs(out[first:end])
         if s >= 0 and W > 1:
             state[s] = v[n:]
     return out, off, state
 
 
-def scan(x, dt, A, B, C, D, z, bias, softplus, ranges, slots, state):
+def scan(x, dt, A, B, C, D, z, bias, softplus, ranges, slots, state, fmt):
     """x, dt, z [T, ch], B, C [T, G, n], A [ch, n], state [S, ch, n].  Returns (out, off, state, state_off)."""
     T, ch = x.shape
     G, n = B.shape[1:]
@@ -73,7 +79,7 @@ def scan(x, dt, A, B, C, D, z, bias, softplus, ranges, slots, state):
             y = (c * h).sum(1) + D * x[t]
             y_off = (np.abs(c) * e).sum(1) + (n + 3) * U * ((np.abs(c) * size).sum(1) + np.abs(D * x[t]))
             out[t] = y * gate[t]
-            off[t] = np.abs(gate[t]) * (1.001 * y_off + 9 * U * np.abs(y))
+            off[t] = np.abs(gate[t]) * (1.001 * y_off + (U + (gate_off(fmt, z[t]) if z is not None else 0.0)) * np.abs(y))
         if s >= 0:
             state[s], soff[s] = h, 1.001 * e
     return out, off, state, soff

@@ -45,7 +45,7 @@ def check(fmt, T, C, W, lengths=None, lens=None, slots=None, n_states=None, seed
     S0 = torch.randn(n_states, W - 1, C, generator=torch.Generator().manual_seed(seed + 1)).to(TYPES[fmt])
     where = [s if 0 <= s < n_states else -1 for s in slots] if slots is not None else list(range(N))
     with np.errstate(invalid="ignore"):
-        want, off, ws = ref.conv(ref.widen(x), ref.widen(w), ref.widen(b) if bias else np.zeros(C), silu, ranges, where if state else [-1] * N, ref.widen(S0))
+        want, off, ws = ref.conv(ref.widen(x), ref.widen(w), ref.widen(b) if bias else np.zeros(C), silu, ranges, where if state else [-1] * N, ref.widen(S0), fmt)
     xd = place(x) if place else x.cuda()
     S = S0.cuda() if state else None
     out = torch.full((T, C), 7.0, dtype=TYPES[fmt], device="cuda")

@@ -61,7 +61,7 @@ def check(fmt, T, C, G, n, lengths=None, lens=None, slots=None, n_states=None, s
     wide = [ref.widen(v) if v is not None else None for v in ins]
     with np.errstate(all="ignore"):
         want, off, ws, ws_off = ref.scan(*wide[:5], wide[5] if wide[5] is not None else np.zeros(C), wide[6], wide[7] if wide[7] is not None else np.zeros(C),
-                                         softplus, ranges, where if state else [-1] * N, ref.widen(S0))
+                                         softplus, ranges, where if state else [-1] * N, ref.widen(S0), fmt)
     dev = [v.cuda() if v is not None else None for v in ins]
     if place:
         dev = place(dev)
