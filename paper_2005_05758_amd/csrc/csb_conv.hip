@@ -10,7 +10,7 @@
 
 namespace csb {
 
-constexpr int kConvRun = 16, kConvAhead = 4;
+constexpr int kConvRun = 32, kConvAhead = 4;
 
 struct ConvDev {
     const void *x;
@@ -53,12 +53,29 @@ __global__ __launch_bounds__(256) void short_conv_kernel(const ConvDev a) {
     const int64_t t0 = (number << a.shift) + row * kConvRun, t1 = t0 + kConvRun < count ? t0 + kConvRun : count;
     if (t0 < count) {
         float w[W][8], bias[8], v[W][8];
+        const float *wp = a.w + (int64_t)c * W;
+        if (there >= 8) {
+            using f32x4 = float __attribute__((ext_vector_type(4)));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bias[i] = a.bias && i < there ? a.bias[c + i] : 0.0f;
+            for (int k = 0; k < 2 * W; ++k) {
+                const f32x4 x = load_any<f32x4>(wp + 4 * k);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+                for (int e = 0; e < 4; ++e) w[(4 * k + e) % W][(4 * k + e) / W] = x[e];
+            }
 #pragma unroll
-            for (int j = 0; j < W; ++j) w[j][i] = i < there ? a.w[(int64_t)(c + i) * W + j] : 0.0f;
+            for (int k = 0; k < 2; ++k) {
+                const f32x4 x = a.bias ? load_any<f32x4>(a.bias + c + 4 * k) : f32x4{};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) bias[4 * k + e] = x[e];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                bias[i] = a.bias && i < there ? a.bias[c + i] : 0.0f;
+#pragma unroll
+                for (int j = 0; j < W; ++j) w[j][i] = i < there ? wp[i * W + j] : 0.0f;
+            }
+        }
         auto widen = [&](const Run &r, float *to) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) to[i] = r[i];

@@ -63,21 +63,16 @@ template <int VF> __device__ __forceinline__ float sigmoid_for(float x) {
 }
 template <int VF> __device__ __forceinline__ float silu(float x) { return x * sigmoid_for<VF>(x); }
 
-// ln(1 + e^x) = max(x, 0) + ln(1 + e), e = e^-|x| in (0, 1]: 2 atanh(e / (2 + e)), whose series in (e / (2 + e))^2 <= 1/9 is cut where
-// 9^-8 / 17 is left (2^-29): small steps keep all of their digits, which ln(1 + e) of a rounded sum would not.
+// ln(1 + e^x) = max(x, 0) + ln(1 + e), e = e^-|x| in (0, 1]: 2 atanh(s), s = e / (2 + e), as 2 s (1 + w p(w)), w = s^2 <= 1/9, p through five of Chebyshev's points
+// (2^-29): small steps keep all of their digits, which ln(1 + e) of a rounded sum would not.
 __device__ __forceinline__ float softplus(float x) {
-    const float e = exp_within(-fabsf(x)), d = 2.0f + e;
-    float r = __builtin_amdgcn_rcpf(d);
-    r = fmaf(fmaf(-d, r, 1.0f), r, r);
-    const float s = e * r, w = s * s;
-    float p = 1.0f / 15.0f;
-    p = fmaf(p, w, 1.0f / 13.0f);
-    p = fmaf(p, w, 1.0f / 11.0f);
-    p = fmaf(p, w, 1.0f / 9.0f);
-    p = fmaf(p, w, 1.0f / 7.0f);
-    p = fmaf(p, w, 1.0f / 5.0f);
-    p = fmaf(p, w, 1.0f / 3.0f);
-    const float l = 2.0f * fmaf(s * w, p, s);
+    const float e = exp_within(-fabsf(x)), s = e * __builtin_amdgcn_rcpf(2.0f + e), w = s * s;
+    float p = 0.11612164974212646f;
+    p = fmaf(p, w, 0.1085328757762909f);
+    p = fmaf(p, w, 0.142961785197258f);
+    p = fmaf(p, w, 0.19999852776527405f);
+    p = fmaf(p, w, 0.3333333432674408f);
+    const float l = fmaf(s + s, w * p, s + s);
     return x != x ? x : fmaxf(x, 0.0f) + l;
 }
 #endif

@@ -1,8 +1,10 @@
 // The selective state space scan (csb_selective_scan).
 //
-// Per channel c, with a state h of n numbers: h[j] <- exp(s A[j]) h[j] + s x B[j], y = sum_j C[j] h[j] + D x.  The exponentials bind: one of them,
-// two products and two fused products a (token, channel, number), 8 issue slots of which the exponential takes 4.  A channel's numbers lie with
-// four neighbouring lanes, K each, in registers from the first token to the last; a workgroup has 64 channels of one group, whose B and C come
+// Per channel c, with a state h of n numbers: h[j] <- exp(s A[j]) h[j] + s x B[j], y = sum_j C[j] h[j] + D x.  The issue of vector instructions binds: an
+// exponential (4 slots), two products and two fused ones a (token, channel, number).  (s x B is a product of a number of the channel's and one of the group's:
+// matrix instructions of 4 x 4 numbers made it and its sum with the decayed state in binary32, but each token waited for its own: 632 us instead of 548
+// on 16384 tokens of 4096 channels.)
+// A channel's numbers lie with four lanes, K each, in registers from the first token to the last; a workgroup has 64 channels of one group, whose B and C come
 // through LDS once for all of them.  What is a token's and channel's alone (its step s through softplus, s x, the gate, types) is made once by
 // the lanes together, eight channels of a token each, and handed over through LDS; outputs come back in the same places.
 //
@@ -31,10 +33,15 @@ struct ScanDev {
     int32_t channels, per_group, n, n_seq, n_states, softplus, shift, group_tiles, col_tiles;
 };
 
-// The value of lane `lane ^ N` of a lane's four neighbours.
-template <int N> __device__ __forceinline__ float quad_xor(float v) {
-    constexpr int order = N == 1 ? 0xb1 : 0x4e;
-    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), order, 0xf, 0xf, false));
+// Lane q 16 + c gets the sum over the lanes c, 16 + c, 32 + c, 48 + c of y[q].
+__device__ __forceinline__ float sum_of_rows(const float *y) {
+    const auto even = [](float a, float b) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    };
+    const float low = even(y[0], y[1]), high = even(y[2], y[3]);
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(low), __float_as_uint(high), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 // OUT: outputs and last states; else what the chunks before the last leave.  FULL: n is 4 K.
@@ -63,7 +70,7 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
     const int64_t base = (int64_t)group * a.per_group + col0;                    // its first channel
 
     // a lane's numbers of a channel
-    const int c = tid >> 2, j0 = (tid & 3) * K;
+    const int q = (tid >> 4) & 3, c = (tid >> 6) * 16 + (tid & 15), j0 = q * K;
     const bool mine = c < cols;
     auto have = [&](int k) { return FULL || j0 + k < a.n; };
     const int64_t channel = base + (mine ? c : 0);
@@ -152,12 +159,7 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
                 }
                 if (!OUT) sum += step;
             }
-            if (OUT) {                                         // lane q of four gets the sum of token i + q
-                const bool odd = tid & 1, high = tid & 2;
-                const float p0 = (odd ? y[1] : y[0]) + quad_xor<1>(odd ? y[0] : y[1]);
-                const float p1 = (odd ? y[3] : y[2]) + quad_xor<1>(odd ? y[2] : y[3]);
-                steps[(i + (tid & 3)) * kScanRow + 2 * c] = (high ? p1 : p0) + quad_xor<2>(high ? p0 : p1);
-            }
+            if (OUT) steps[(i + q) * kScanRow + 2 * c] = sum_of_rows(y);         // of token i + q
         }
         total += sum;
         __syncthreads();
@@ -176,8 +178,14 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
         if (last && a.s_out && known) put(a.s_out + s * state);
     } else {
         put(a.begin + (tile + 1) * state);
-        if (mine && (tid & 3) == 0) a.sums[tile * a.channels + channel] = (float)total;
+        if (mine && q == 0) a.sums[tile * a.channels + channel] = (float)total;
     }
+}
+
+// The value of lane `lane ^ N` of a lane's four neighbours.
+template <int N> __device__ __forceinline__ float quad_xor(float v) {
+    constexpr int order = N == 1 ? 0xb1 : 0x4e;
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), order, 0xf, 0xf, false));
 }
 
 // The same for the few tokens of a decoding step: P lanes a channel, K numbers each, a wavefront 64 / P channels by itself, without LDS and barriers.
