@@ -19,6 +19,7 @@
 namespace csb {
 
 constexpr int kScanTile = 32, kScanCols = 64, kScanRow = 2 * kScanCols + 32;      // tokens and channels in LDS; floats of a token's row there
+constexpr int kScanMany = 1024;                // workgroups that are enough for the card
 constexpr int kScanFew = 8;                    // tokens a sequence, on average, up to which wavefronts work alone
 
 struct ScanDev {
@@ -96,6 +97,7 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
         if (!OUT) put(a.begin + tile * state);
     } else if (OUT) {
         get(a.begin + (tile0 + 1) * state);
+#pragma unroll 4
         for (int64_t i = tile0 + 1; i < tile; ++i) {
             const float sum = a.sums[i * a.channels + channel];
             const float *p = a.begin + (i + 1) * state;
@@ -113,35 +115,45 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
         D[i] = OUT && a.D && i < there ? a.D[base + sc + i] : 0.0f;
     }
     const int64_t stop = count < t0 + each ? count : t0 + each;
-    Run x, dt, z;
+    Run x, z, next_x, next_dt, next_z;                         // a tile's operands are requested while the one before is worked on
+    T next_B[K / 2], next_C[K / 2];
     auto load = [&](int64_t t) {
-        x.v = dt.v = z.v = typename Run::T8{};
+        next_x.v = next_dt.v = next_z.v = typename Run::T8{};
         if (t + st < stop && there > 0) {
             const int64_t at = first + t + st;
-            x.load((const T *)a.x + at * a.ldx + base + sc, there);
-            dt.load((const T *)a.dt + at * a.lddt + base + sc, there);
-            if (OUT && a.z) z.load((const T *)a.z + at * a.ldz + base + sc, there);
+            next_x.load((const T *)a.x + at * a.ldx + base + sc, there);
+            next_dt.load((const T *)a.dt + at * a.lddt + base + sc, there);
+            if (OUT && a.z) next_z.load((const T *)a.z + at * a.ldz + base + sc, there);
+        }
+#pragma unroll
+        for (int i = 0; i < K / 2; ++i) {
+            const int e = tid + 256 * i, tt = e / (4 * K), j = e % (4 * K);
+            const bool in = t + tt < stop && j < a.n;
+            next_B[i] = in ? ((const T *)a.B)[(first + t + tt) * a.ldB + (int64_t)group * a.n + j] : (T)0.0f;
+            if (OUT) next_C[i] = in ? ((const T *)a.C)[(first + t + tt) * a.ldC + (int64_t)group * a.n + j] : (T)0.0f;
         }
     };
     double total = 0.0;
+    load(t0);
     for (int64_t t = t0; t < stop; t += kScanTile) {
         const int live = (int)(stop - t < kScanTile ? stop - t : kScanTile);
-        load(t);
         float *row = steps + st * kScanRow + 2 * sc;
+        x = next_x;
+        z = next_z;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float d = dt[i] + bias[i];
+            float d = next_dt[i] + bias[i];
             if (a.softplus) d = softplus(d);
             if (st >= live) d = 0.0f;                          // (past the end: nothing decays, nothing comes in)
             row[2 * i] = d;
             row[2 * i + 1] = d * x[i];
         }
-        for (int i = tid; i < kScanTile * 4 * K; i += 256) {
-            const int tt = i / (4 * K), j = i % (4 * K);
-            const bool in = tt < live && j < a.n;
-            Bs[i] = in ? (float)((const T *)a.B)[(first + t + tt) * a.ldB + (int64_t)group * a.n + j] : 0.0f;
-            if (OUT) Cs[i] = in ? (float)((const T *)a.C)[(first + t + tt) * a.ldC + (int64_t)group * a.n + j] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < K / 2; ++i) {
+            Bs[tid + 256 * i] = (float)next_B[i];
+            if (OUT) Cs[tid + 256 * i] = (float)next_C[i];
         }
+        if (t + kScanTile < stop) load(t + kScanTile);
         __syncthreads();
         float sum = 0.0f;
         for (int i = 0; i < live; i += 4) {
@@ -279,16 +291,16 @@ __global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a
         }
 }
 
-// Chunks of a call, as a power of two of tokens (31: whole sequences).
+// Chunks of a call, as a power of two of tokens (31: whole sequences).  Sequences and channels that give every CU four workgroups are not split (a split costs
+// the chunks' own states beside the outputs: twice the exponentials).  Others are, as finely as makes that many, but no finer than 128 chunks
+// a sequence, whose states every later chunk combines (16384 tokens of 64 channels in 512 chunks 93 us, in 128 56), and no coarser than 512 tokens
+// (16384 tokens of 4096 channels in 16 chunks 519 us, in 32 492).
 static int scan_shift(const csb_scan_args *a, int64_t col_tiles) {
-    int shift = 31;
-    const int64_t mean = a->n_tokens / a->n_seq;
-    if (a->n_seq * col_tiles < 1024 && mean >= 256) {
-        shift = 7;
-        while (shift < 31 && (mean >> shift) * a->n_seq * col_tiles > 1024) ++shift;
-        if (mean >> shift < 2) shift = 31;
-    }
-    return shift;
+    const int64_t mean = a->n_tokens / a->n_seq, tiles = a->n_seq * col_tiles;
+    if (tiles >= kScanMany || mean < 2 * kScanTile) return 31;
+    int shift = 5;
+    while ((mean >> shift) > 128 || (shift < 9 && (mean >> shift) * tiles > kScanMany)) ++shift;
+    return mean >> shift < 2 ? 31 : shift;
 }
 
 static int scan_lanes(int32_t n) { return n <= 16 ? 1 : n <= 32 ? 2 : n <= 64 ? 4 : 8; }     // a channel, of the kernel for few tokens
