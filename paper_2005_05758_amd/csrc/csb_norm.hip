@@ -19,8 +19,9 @@ struct NormDev {
     const float *aw, *ab, *s, *bw, *bb;
     int64_t tokens, tiles;                     // tiles: of tokens, where lanes are tokens
     int32_t width, groups, after, before, sigmoid, gate_first;   // width: of a group
+    int32_t plain_gate, plain_scale;           // results are rounded to 16 bits; nothing is scaled
     float scale;
-    double eps;
+    double eps, per;                           // per: 1 / width
 };
 
 struct Raw8 { uint32_t w[8]; };                // eight entries as they are stored: one a word, or two of 16 bits in each of the first four (rows)
@@ -177,7 +178,7 @@ template <typename Access> __device__ __forceinline__ void gate_factors(const No
     gate.widen(raw, g);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float x = g[j], s = sigmoid_within(x);
+        const float x = g[j], s = a.plain_gate ? sigmoid_for<CSB_VAL_BF16>(x) : sigmoid_within(x);
         g[j] = a.sigmoid ? (x != x ? x : s) : x * s;
     }
 }
@@ -299,10 +300,10 @@ struct RowNorm {
             for (int j = 0; j < 7; ++j) if (j < there) one_more(v[j]);
         }
     }
-    __device__ __forceinline__ void finish(int kind, int width, double eps) {
-        double square = q / width;
+    __device__ __forceinline__ void finish(int kind, double per, double eps) {
+        double square = q * per;
         if (kind == CSB_NORM_MEAN) {
-            mean = p / width;
+            mean = p * per;
             square = __builtin_fmax(square - mean * mean, 0.0);
             mean += shift;
             if (p != p) square = p;
@@ -315,8 +316,19 @@ struct RowNorm {
         one = large ? 0x1p-80f : 1.0f;
         factor = (float)(large ? y * 0x1p80 : y);
     }
-    __device__ __forceinline__ float of(int kind, float v) const {
-        return (kind == CSB_NORM_MEAN ? (float)(((double)v - mean) * one) : v * one) * factor;
+    // eight entries (without the branch where the loads of many runs are to be in flight beside it)
+    __device__ __forceinline__ float of(int kind, float v) const { return (kind == CSB_NORM_MEAN ? (float)(((double)v - mean) * one) : v * one) * factor; }
+    __device__ __forceinline__ void of(int kind, float *v) const {
+        if (kind == CSB_NORM_MEAN) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = (float)(((double)v[j] - mean) * one) * factor;
+        } else if (__all(one == 1.0f)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= factor;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = v[j] * one * factor;
+        }
     }
 };
 
@@ -341,14 +353,15 @@ __global__ __launch_bounds__(THREADS) void block_norm_kernel(const NormDev a) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) n.add<WHOLE>(kind, v[i], a.width - at(i));
         rows.sum(kind, n.p, n.q);
-        n.finish(kind, a.width, a.eps);
+        n.finish(kind, a.per, a.eps);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float w[8], b[8];
+            n.of(kind, v[i]);
             norm_factors<WHOLE>(weight, base + at(i), a.width - at(i), 1.0f, w);
             norm_factors<WHOLE>(bias, base + at(i), a.width - at(i), 0.0f, b);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = fmaf(n.of(kind, v[i][j]), w[j], b[j]);
+            for (int j = 0; j < 8; ++j) v[i][j] = fmaf(v[i][j], w[j], b[j]);
         }
     };
     Raw8 y[NV], g[NV], x[NV];
@@ -380,9 +393,11 @@ __global__ __launch_bounds__(THREADS) void block_norm_kernel(const NormDev a) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[i][j] *= f[j];
             }
-            norm_factors<WHOLE>(a.s, base + at(i), a.width - at(i), 1.0f, f);
+            if (!a.plain_scale) {
+                norm_factors<WHOLE>(a.s, base + at(i), a.width - at(i), 1.0f, f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] *= a.scale * f[j];
+                for (int j = 0; j < 8; ++j) v[i][j] *= a.scale * f[j];
+            }
         }
     }
 #pragma unroll
@@ -438,10 +453,11 @@ __global__ __launch_bounds__(THREADS) void block_norm_long_kernel(const NormDev 
                     float w[8];
                     if (a.after) {
                         float b[8];
+                        after.of(a.after, v);
                         norm_factors<WHOLE>(a.aw, base + j0, there, 1.0f, w);
                         norm_factors<WHOLE>(a.ab, base + j0, there, 0.0f, b);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] = fmaf(after.of(a.after, v[j]), w[j], b[j]);
+                        for (int j = 0; j < 8; ++j) v[j] = fmaf(v[j], w[j], b[j]);
                     }
                     norm_factors<WHOLE>(a.s, base + j0, there, 1.0f, w);
 #pragma unroll
@@ -466,20 +482,21 @@ __global__ __launch_bounds__(THREADS) void block_norm_long_kernel(const NormDev 
                 if (a.r.d) ra.store(base + j0, there, v);
                 if (a.before) {
                     float w[8];
+                    before.of(a.before, v);
                     norm_factors<WHOLE>(a.bw, j0, there, 1.0f, w);
                     norm_factors<WHOLE>(a.bb, j0, there, 0.0f, f);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = fmaf(before.of(a.before, v[j]), w[j], f[j]);
+                    for (int j = 0; j < 8; ++j) v[j] = fmaf(v[j], w[j], f[j]);
                     oa.store(j0, there, v);
                 }
             }
         }
         if (phase == AFTER) {
             rows.sum(norm, after.p, after.q);
-            after.finish(a.after, a.width, a.eps);
+            after.finish(a.after, a.per, a.eps);
         } else if (phase == BEFORE) {
             rows.sum(norm, before.p, before.q);
-            before.finish(a.before, a.width, a.eps);
+            before.finish(a.before, a.per, a.eps);
         }
     }
 }
@@ -517,7 +534,7 @@ __global__ __launch_bounds__(1024) void block_norm_product_kernel(const NormDev 
 #pragma unroll
         for (int i = 0; i < NV; ++i) if (i * L * 8 < a.width) n.add<true>(kind, v[i], a.width - first(i));
         rows.sum(kind, n.p, n.q);
-        n.finish(kind, a.width, a.eps);
+        n.finish(kind, a.per, a.eps);
     };
     RowNorm after, before;
     if (a.after) sums(a.after, after);
@@ -712,7 +729,9 @@ extern "C" int csb_block_norm(const csb_norm_args *a, void *stream) {
     d.aw = a->d_after_w; d.ab = a->d_after_b; d.s = a->d_scale; d.bw = a->d_before_w; d.bb = a->d_before_b;
     d.tokens = a->n_tokens; d.width = a->width / a->groups; d.groups = a->groups;
     d.after = a->after; d.before = a->before; d.sigmoid = a->gate_kind == CSB_GATE_SIGMOID; d.gate_first = a->gate_first;
-    d.scale = a->scale; d.eps = a->eps;
+    d.scale = a->scale; d.eps = a->eps; d.per = 1.0 / d.width;
+    d.plain_scale = !a->d_scale && a->scale == 1.0f;
+    d.plain_gate = (!d.r.d || d.r.type != CSB_VAL_F32) && (!d.out.d || d.out.type != CSB_VAL_F32);
     if (!launch_norm(d, columns, far, (hipStream_t)stream)) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(CSB_EDEVICE, hipGetErrorString(e));

@@ -94,8 +94,8 @@ def within(got, want, off, fmt):
     return float((np.abs(got[there] - want[there]) - allowed).max())
 
 
-def norm(y, gate, x, after, aw, ab, groups, sigmoid_gate, gate_first, scale, s, before, bw, bb, eps):
-    """All [T, W] or None (weights [W]).  Returns (r, off, n, off): n None without a norm before."""
+def norm(y, gate, x, after, aw, ab, groups, sigmoid_gate, gate_first, scale, s, before, bw, bb, eps, fmt):
+    """All [T, W] or None (weights [W]); fmt: "f32" where one of the results is.  Returns (r, off, n, off): n None without a norm before."""
     T, W = (x if x is not None else y).shape
 
     def unit(v, e, kind, w, b, parts):
@@ -120,10 +120,10 @@ def norm(y, gate, x, after, aw, ab, groups, sigmoid_gate, gate_first, scale, s, 
         if gate is not None:
             act = sigmoid(gate) if sigmoid_gate else silu(gate)
         if act is not None and gate_first:
-            r, off = r * act, 9 * U * np.abs(r * act)
+            r, off = r * act, (U + gate_off(fmt, gate)) * np.abs(r * act)
         r, off = unit(r, off, after, aw, ab, groups)
         if act is not None and not gate_first:
-            r, off = r * act, off * np.abs(act) + 9 * U * np.abs(r * act)
+            r, off = r * act, off * np.abs(act) + (U + gate_off(fmt, gate)) * np.abs(r * act)
         m = scale * (s if s is not None else np.ones(W))
         r, off = r * m, (off + 3 * U * np.abs(r)) * np.abs(m)
     if x is not None:

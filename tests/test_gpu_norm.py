@@ -66,7 +66,7 @@ def check(T, W, fmts="bf16", y=True, gate=False, x=True, after="rms", before="rm
     v = {k: ref.widen(v) if v is not None else None for k, v in given.items()}
     with np.errstate(all="ignore"):
         r, r_off, n, n_off = ref.norm(v["y"], v["g"], v["x"], after, w[0], w[1], groups, gate_kind == "sigmoid", gate_first, np.float32(scale), w[2], before,
-                                      w[3], w[4], float(np.float32(eps)))
+                                      w[3], w[4], float(np.float32(eps)), "f32" if "f32" in (fmts["r"], fmts["n"] if before else fmts["r"]) else "bf16")
     if change is None:
         assert ref.within(ref.widen(out), r, r_off, fmts["r"]) <= 0
         assert n is None or ref.within(ref.widen(normed), n, n_off, fmts["n"]) <= 0
