@@ -187,11 +187,14 @@ int csb_short_conv(const csb_conv_args *args, void *stream);
  * Sequences, slots and states ([n_states][channels][n]) are as with the delta rule.  Long sequences are
  * split into chunks (by n_tokens, n_seq, channels and n alone): the chunks' own states first, then outputs from what the chunks before leave,
  * in two launches; else one launch.  Bitwise reproducible.
- * What is not finite stays in its channel (in B or C: its group's) from its token on; it is infinite or NaN there.
+ * What is not finite stays in its channel (in B or C: its group's) from its token on; it is infinite or NaN there.  Products s A are expected at or below
+ * zero: a chunk over which a state would grow by 2^128 counts as infinite growth.
  * d_ws: csb_scan_workspace_bytes(args) bytes (channels, groups, n, n_seq and n_tokens are read; 0 where there is one launch or a
  * refusal: d_ws may be NULL then).
+ * Few tokens, chunks or neither is decided by the mean length of a call's sequences, which is all that the host knows: a few long prompts take longer
+ * in one call with many single tokens than in a call of their own.
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, channels no multiple of groups, n_tokens no
- * multiple of n_seq without d_start, an unknown type -> CSB_EINVAL; n > 128, n_tokens above 2^31 - 1,
+ * multiple of n_seq without d_start, out at the address of B, C or of an x, dt, z with another leading dimension, an unknown type -> CSB_EINVAL; n > 128, n_tokens above 2^31 - 1,
  * or more workgroups than a launch takes -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.  n_seq = 0 does nothing.
  */
 typedef struct {
@@ -229,8 +232,8 @@ int csb_selective_scan(const csb_scan_args *args, void *d_ws, void *stream);
  * norm_before is that of r before its rounding.  An output may be an input itself (same pointer, type, order and ld), and must not overlap one
  * otherwise.  Products and sums are binary32, a norm's sums binary64: entries of any finite size have their norm.  What is not finite in
  * a token's entries stays in that token (in its group where there are several).
- * Errors: NULL, sizes, types or leading dimensions out of range, width no multiple of groups, a gate or norm_after without y, norms or gates unknown ->
- * CSB_EINVAL; width / groups > 32768, norm_before with several groups, or more workgroups than a launch takes -> CSB_EUNSUPPORTED; launch failure ->
+ * Errors: NULL, sizes, types or leading dimensions out of range, eps below zero or not finite, width no multiple of groups, a gate or norm_after without y, norms or gates
+ * unknown, an output at the address of an input of another type, order or ld -> CSB_EINVAL; width / groups > 32768, norm_before with several groups, or more workgroups than a launch takes -> CSB_EUNSUPPORTED; launch failure ->
  * CSB_EDEVICE.  n_tokens = 0 does nothing.  Bitwise reproducible, one launch, no workspace.
  */
 #define CSB_NORM_NONE 0
@@ -268,8 +271,8 @@ int csb_block_norm(const csb_norm_args *args, void *stream);
  * Token d_tokens[i] is drawn from what is kept by inversion, as csb_verify_drafts does: the lowest whose cumulated units, by number,
  * exceed floor(units of the row * floor(r 2^24) / 2^24), r = d_r[i] in [0, 1) given by the caller; -1 where every logit is -infinity or NaN.
  * d_probs (NULL: not wanted): row i of the distribution drawn from, at d_probs + i * ldprobs, of `type`: units over the row's units, rounded once, zero for
- * tokens that are not kept; what csb_verify_drafts takes as p and q.  With d_tokens NULL (d_r may be too) only that is made.  It must not overlap the logits,
- * or be them (same pointer and leading dimension).  Whole units: the result depends neither on the order nor on the split of a sum.
+ * tokens that are not kept; what csb_verify_drafts takes as p and q.  With d_tokens NULL (d_r may be too) only that is made.  It may be the
+ * logits themselves (same pointer and leading dimension), and must not overlap them otherwise.  Whole units: the result depends neither on the order nor on the split of a sum.
  * d_ws: csb_sample_workspace_bytes(n_rows, vocab) bytes (0 up to a vocabulary of 24576: d_ws may be NULL then).  One launch where a row has up to 98304
  * bytes, else three to six.
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, an unknown type -> CSB_EINVAL; vocab > 2^24, n_rows > 2^21, or

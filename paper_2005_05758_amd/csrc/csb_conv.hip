@@ -36,8 +36,9 @@ __global__ __launch_bounds__(256) void short_conv_kernel(const ConvDev a) {
     const int64_t count = end - first;
     if (number < 0 || (number > 0 && (number << a.shift) >= count)) return;
     const int lane = threadIdx.x & (a.lanes - 1), row = threadIdx.x / a.lanes;
-    const int c = ((int)(blockIdx.x % a.col_tiles) * a.lanes + lane) * 8, there = a.channels - c;
-    if (there <= 0) return;
+    const int64_t c = ((int64_t)(blockIdx.x % a.col_tiles) * a.lanes + lane) * 8;
+    if (c >= a.channels) return;
+    const int there = a.channels - (int)c;
     const int32_t s = a.slot ? a.slot[seq] : seq;
     const bool known = s >= 0 && s < a.n_states;
     const T *x = (const T *)a.x + first * a.ldx + c;
@@ -53,7 +54,7 @@ __global__ __launch_bounds__(256) void short_conv_kernel(const ConvDev a) {
     const int64_t t0 = (number << a.shift) + row * kConvRun, t1 = t0 + kConvRun < count ? t0 + kConvRun : count;
     if (t0 < count) {
         float w[W][8], bias[8], v[W][8];
-        const float *wp = a.w + (int64_t)c * W;
+        const float *wp = a.w + c * W;
         if (there >= 8) {
             using f32x4 = float __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -167,8 +168,8 @@ extern "C" int csb_short_conv(const csb_conv_args *a, void *stream) {
     const int64_t runs = ((int64_t)a->channels + 7) / 8;       // of eight channels
     d.lanes = 64;
     while (d.lanes > 1 && d.lanes / 2 >= runs) d.lanes /= 2;
-    // rows of threads on runs of tokens one behind the other: none but the first where a sequence has no more than a run on average
-    const int rows = a->n_tokens / a->n_seq <= kConvRun ? 1 : 256 / 64;
+    // rows of threads on runs of tokens one behind the other: a wavefront where a sequence has no more than a run on average
+    const int rows = a->n_tokens / a->n_seq <= kConvRun ? 64 / d.lanes : 256 / 64;
     d.col_tiles = (int32_t)((runs + d.lanes - 1) / d.lanes);
     d.shift = 0;
     while ((1 << d.shift) < rows * kConvRun) ++d.shift;

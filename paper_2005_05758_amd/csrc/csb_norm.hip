@@ -702,7 +702,7 @@ extern "C" int csb_block_norm(const csb_norm_args *a, void *stream) {
     for (int kind : {a->after, a->before})
         if (kind != CSB_NORM_NONE && kind != CSB_NORM_RMS && kind != CSB_NORM_MEAN) return fail(CSB_EINVAL, "unknown norm");
     if (a->gate_kind != CSB_GATE_SILU && a->gate_kind != CSB_GATE_SIGMOID) return fail(CSB_EINVAL, "unknown gate");
-    if (!(a->eps >= 0.0f)) return fail(CSB_EINVAL, "eps below zero");
+    if (!(a->eps >= 0.0f && a->eps <= 0x1.fffffep127f)) return fail(CSB_EINVAL, "eps below zero or not finite");
     if (a->width / a->groups > 32768) return fail(CSB_EUNSUPPORTED, "more than 32768 entries under one norm (a row stays in a workgroup's registers)");
     if (a->before && a->groups > 1) return fail(CSB_EUNSUPPORTED, "norm_before with several groups");
     if (a->n_tokens == 0) return CSB_OK;
@@ -724,6 +724,10 @@ extern "C" int csb_block_norm(const csb_norm_args *a, void *stream) {
         columns |= o.columns != 0;
         far |= o.columns && o.ld > 0x7fffffff / type_size(o.type) / a->width;
     }
+    for (int i = 0; i < 3; ++i)
+        for (int o = 3; o < 5; ++o)
+            if (to[i]->d && to[i]->d == to[o]->d && (to[i]->ld != to[o]->ld || to[i]->type != to[o]->type || to[i]->columns != to[o]->columns))
+                return fail(CSB_EINVAL, "an output in place of an input of another type, order or leading dimension");
     for (const float *p : {a->d_after_w, a->d_after_b, a->d_scale, a->d_before_w, a->d_before_b})
         if ((uintptr_t)p % 4) return fail(CSB_EINVAL, "misaligned pointer");
     d.aw = a->d_after_w; d.ab = a->d_after_b; d.s = a->d_scale; d.bw = a->d_before_w; d.bb = a->d_before_b;

@@ -50,7 +50,7 @@ __device__ __forceinline__ double fma_of_constant(double a, double b, double c) 
 
 // What a row's numbers ask for.
 struct SampleRow {
-    float m, per_bucket;
+    float m, per_bucket, part, part_of_m;      // (part: of logits, so that no difference of two overflows where the temperature makes numbers of such)
     double per_bit;                            // log2 e / T
     int32_t k;                                 // 0: all
     uint32_t p;                                // floor(top_p 2^24); 2^24: all
@@ -65,11 +65,14 @@ struct SampleRow {
         least = mp > 0.0f ? __builtin_floor((double)fminf(mp, 1.0f) * kUnit) : 0.0;
         if (T > 0.0f) {
             per_bit = 1.4426950408889634 / (double)T;
-            per_bucket = (float)((kBuckets - 1) / 26.5 / (double)T);           // e^-26.5 2^38 < 1
+            part = T > 0x1p60f ? 0.5f : 1.0f;
+            per_bucket = (float)((kBuckets - 1) / 26.5 / part / (double)T);    // e^-26.5 2^38 < 1
         } else {
             per_bit = per_bucket = __builtin_inff();           // the largest alone,
             k = 1;                                             // and the first of them
+            part = 1.0f;
         }
+        part_of_m = m * part;
     }
     __device__ __forceinline__ bool cut() const { return k || p < 1u << 24; }
     // units of a token; whole, below 2^39
@@ -88,7 +91,7 @@ struct SampleRow {
         const double w = __builtin_floor(__builtin_amdgcn_ldexp(e, (int)n + 38));
         return s == m ? kUnit : y > -40.0 ? w : 0.0;           // (infinite logits, and NaN of infinite temperatures)
     }
-    __device__ __forceinline__ int bucket(float s) const { return s == m ? 0 : (int)fminf((m - s) * per_bucket, (float)(kBuckets - 1)); }
+    __device__ __forceinline__ int bucket(float s) const { return s == m ? 0 : (int)fminf(fmaf(s, -part, part_of_m) * per_bucket, (float)(kBuckets - 1)); }
 };
 
 __device__ __forceinline__ uint64_t whole(double w) { return __builtin_bit_cast(uint64_t, w + 0x1p52) & 0xfffffffffffffull; }
@@ -1112,6 +1115,7 @@ extern "C" int csb_sample(int32_t type, const void *d_logits, int64_t ld, const 
     if (ld < vocab || (d_probs && ldprobs < vocab)) return fail(CSB_EINVAL, "a leading dimension below the vocabulary");
     if (n_rows == 0) return CSB_OK;
     if (!d_logits || (!d_tokens && !d_probs) || (d_tokens && !d_r)) return fail(CSB_EINVAL, "NULL pointer");
+    if (d_probs == d_logits && ldprobs != ld) return fail(CSB_EINVAL, "the distribution in place of the logits at another leading dimension");
     if (((uintptr_t)d_logits | (uintptr_t)d_probs) % (uintptr_t)type_size(type) ||
         ((uintptr_t)d_temperature | (uintptr_t)d_top_k | (uintptr_t)d_top_p | (uintptr_t)d_min_p | (uintptr_t)d_r | (uintptr_t)d_tokens) % 4)
         return fail(CSB_EINVAL, "misaligned pointer");

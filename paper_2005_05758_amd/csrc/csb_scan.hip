@@ -217,7 +217,8 @@ __global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a
     if (a.len) end = first + clamp64(a.len[seq], 0, end - first);
     const int32_t s = a.slot ? a.slot[seq] : seq;
     const bool known = s >= 0 && s < a.n_states;
-    const int c = (ct % a.group_tiles) * (64 / P) + (int)(lane / P), j0 = (int)(lane % P) * K;
+    const int64_t c = (int64_t)(ct % a.group_tiles) * (64 / P) + lane / P;
+    const int j0 = (int)(lane % P) * K;
     const bool mine = c < a.per_group;
     const int64_t channel = (int64_t)group * a.per_group + (mine ? c : 0);
     const int there = FULL ? K : a.n - j0;                     // of the lane's K numbers
@@ -378,6 +379,9 @@ extern "C" int csb_selective_scan(const csb_scan_args *a, void *d_ws, void *stre
     const int64_t w = a->channels, wn = (int64_t)a->groups * a->n;
     if (a->ldx < w || a->lddt < w || a->ldo < w || (a->d_z && a->ldz < w) || a->ldB < wn || a->ldC < wn)
         return fail(CSB_EINVAL, "a leading dimension below the width of its rows");
+    if (a->n_tokens && ((a->d_out == a->d_x && a->ldo != a->ldx) || (a->d_out == a->d_dt && a->ldo != a->lddt) || (a->d_out == a->d_z && a->ldo != a->ldz) ||
+                        a->d_out == a->d_B || a->d_out == a->d_C))
+        return fail(CSB_EINVAL, "out in place of x, dt or z at another leading dimension, or of B or C");
     if (!a->d_start && a->n_seq && a->n_tokens % a->n_seq) return fail(CSB_EINVAL, "n_tokens is no multiple of n_seq (and there are no offsets)");
     if ((a->d_state_in || a->d_state_out) && a->n_states < 1) return fail(CSB_EINVAL, "states without room for one");
     if (((uintptr_t)a->d_x | (uintptr_t)a->d_dt | (uintptr_t)a->d_z | (uintptr_t)a->d_B | (uintptr_t)a->d_C | (uintptr_t)a->d_out) % (uintptr_t)type_size(a->type) ||
