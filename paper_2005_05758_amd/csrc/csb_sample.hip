@@ -15,6 +15,7 @@
 // draw; the distribution, if it is asked for.
 #include <algorithm>
 #include <new>
+#include <type_traits>
 
 #include "csb_layer.hpp"
 
@@ -77,7 +78,14 @@ struct SampleRow {
     __device__ __forceinline__ bool cut() const { return k || p < 1u << 24; }
     // units of a token; whole, below 2^39
     __device__ __forceinline__ double weight(float s) const {
-        const double y = ((double)s - (double)m) * per_bit, n = __builtin_rint(y), f = y - n;
+        double y;
+        const double w = weight_within(s, &y);
+        return s == m ? kUnit : y > -40.0 ? w : 0.0;           // (infinite logits, and NaN of infinite temperatures)
+    }
+    // the same for finite ones; y: the weight's binary logarithm, 38 taken off
+    __device__ __forceinline__ double weight_within(float s, double *log) const {
+        const double y = ((double)s - (double)m) * per_bit, t = y + (0x1.8p52 + 38.0), f = y - (t - (0x1.8p52 + 38.0));  // (t: the nearest whole number, and its 32 bits)
+        *log = y;
         double e = 1.0205905413765595e-07;                   // 2^f for |f| <= 1/2 to 2^-45, through ten of Chebyshev's points
         e = fma_of_constant(e, f, 1.325964524488711e-06);
         e = fma_of_constant(e, f, 1.5252672924850737e-05);
@@ -88,8 +96,12 @@ struct SampleRow {
         e = fma_of_constant(e, f, 0.2402265069564034);
         e = fma_of_constant(e, f, 0.6931471805599462);
         e = fma_of_constant(e, f, 1.0000000000000135);
-        const double w = __builtin_floor(__builtin_amdgcn_ldexp(e, (int)n + 38));
-        return s == m ? kUnit : y > -40.0 ? w : 0.0;           // (infinite logits, and NaN of infinite temperatures)
+        return __builtin_floor(__builtin_amdgcn_ldexp(e, (int)(uint32_t)__builtin_bit_cast(uint64_t, t)));
+    }
+    // a logit that no token up to bucket b is below (others may be above it, none of them infinite): the rounding of bucket() is 2^-22 of it, of the difference 2^-22 of m
+    __device__ __forceinline__ float least_of(int b) const {
+        const float t = m - (float)(b + 1) * 1.0001f / (per_bucket * part) - fabsf(m) * 0x1p-22f;
+        return t > -0x1.fffffep127f ? t : -0x1.fffffep127f;
     }
     __device__ __forceinline__ int bucket(float s) const { return s == m ? 0 : (int)fminf(fmaf(s, -part, part_of_m) * per_bucket, (float)(kBuckets - 1)); }
 };
@@ -173,28 +185,33 @@ __device__ __forceinline__ uint64_t max_of_wave(uint64_t v) {  // (0: none)
 
 // A workgroup's memory for the searches of a row.
 struct SampleShared {
-    unsigned long long units[kBuckets], low, high, found, found_units, base_units, part_units[16];
+    unsigned long long units[kBuckets], low, high, found, found_units, base_units;
+    uint64_t part_units[16];
     uint32_t counts[kBuckets], part_counts[16];
-    uint32_t bin, bin_count, base_count, listed;
+    uint64_t few_units[64];
+    uint32_t bin, bin_count, base_count, listed, few_tokens[64];
     int32_t token;
     float part_max[16];
 };
 
+// Of sixteen numbers, one for each wavefront: the sum of those before the caller's; *all: of all.
+template <typename N> __device__ __forceinline__ N before_of_waves(const N *parts, N *all) {
+    N v = parts[threadIdx.x & 15];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    v += moved<0x111, 0xf>(v);
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    *all = of_lane(v, 15);
+    return wave ? of_lane(v, wave - 1) : 0;
+}
 // Sum over the threads below this one; *total: of all.
 __device__ __forceinline__ uint64_t block_before(SampleShared &sh, uint64_t v, uint64_t *total) {
-    const int wave = threadIdx.x >> 6;
-    uint64_t before = before_in_wave(v), all = 0;
+    const uint64_t before = before_in_wave(v);
     __syncthreads();
-    if ((threadIdx.x & 63) == 63) sh.part_units[wave] = before + v;
+    if ((threadIdx.x & 63) == 63) sh.part_units[threadIdx.x >> 6] = before + v;
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-        const uint64_t p = sh.part_units[w];
-        if (w < wave) before += p;
-        all += p;
-    }
-    *total = all;
-    return before;
+    return before + before_of_waves(sh.part_units, total);
 }
 
 // The bin, of counts and units in LDS by thread, in which what is kept ends: of `target` tokens (BY_COUNT), or of those with fewer
@@ -210,13 +227,12 @@ template <bool BY_COUNT, bool UNITS = true> __device__ __forceinline__ void find
         if (UNITS) sh.part_units[wave] = ub + u;
     }
     __syncthreads();
+    uint32_t all_counts;
+    uint64_t all_units;
     cb += sh.base_count;
     ub += sh.base_units;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-        if (BY_COUNT) cb += w < wave ? sh.part_counts[w] : 0;
-        if (UNITS) ub += w < wave ? sh.part_units[w] : 0;
-    }
+    if (BY_COUNT) cb += before_of_waves(sh.part_counts, &all_counts);
+    if (UNITS) ub += before_of_waves(sh.part_units, &all_units);
     __syncthreads();                                           // (base_* are read)
     if (BY_COUNT ? cb < target && cb + c >= target : ub < target && ub + u >= target) {   // one thread, or none
         sh.bin = tid;
@@ -225,6 +241,30 @@ template <bool BY_COUNT, bool UNITS = true> __device__ __forceinline__ void find
         sh.base_units = ub;
     }
     __syncthreads();
+}
+
+// The same for a share of all units: returns the target.  sh.base_count: about how many tokens the buckets up to the bin have, by the units that a token has in the
+// middle of a bucket (1.4 % off where a bucket's tokens lie at one of its ends).
+__device__ __forceinline__ uint64_t find_share(SampleShared &sh, uint32_t p, uint64_t *all) {
+    const int tid = threadIdx.x;
+    const uint64_t u = sh.units[tid];
+    const uint32_t about = (uint32_t)((float)u * __builtin_amdgcn_exp2f((float)tid * (float)(26.5 / (kBuckets - 1) * 1.4426950408889634) + (float)(0.5 * 26.5 / (kBuckets - 1) * 1.4426950408889634 - 38.0)) + 0.9f);
+    const uint32_t count = before_in_wave(about) + about;
+    if ((tid & 63) == 63) sh.part_counts[tid >> 6] = count;
+    const uint64_t before = block_before(sh, u, all), share = part_of(*all, p), target = share ? share : 1;
+    if (before < target && before + u >= target) {
+        sh.bin = tid;
+        sh.bin_count = count;
+        sh.base_units = before;
+    }
+    __syncthreads();
+    uint32_t total;
+    if (tid >> 6 == (int)(sh.bin >> 6)) {
+        const uint32_t below = before_of_waves(sh.part_counts, &total);
+        if ((tid & 63) == 0) sh.base_count = below + sh.bin_count;
+    }
+    __syncthreads();
+    return target;
 }
 
 // The last token kept, among those that tokens.each names (calls its argument with places and units): sh.found, and the units up to and
@@ -300,30 +340,31 @@ __device__ __forceinline__ uint64_t end_of_kept(SampleShared &sh, const SampleRo
     const int tid = threadIdx.x;
     const uint32_t c = sh.counts[tid];
     const uint64_t u = sh.units[tid];
-    uint64_t units, target = (uint64_t)row.k, end = 0;
-    block_before(sh, u, &units);
+    uint64_t units = 0, target = (uint64_t)row.k, end = 0;
+    if (tid == 0) { sh.base_count = 0; sh.base_units = 0; sh.bin = kBuckets; }
+    __syncthreads();
+    if (row.k) find_bin<true>(sh, target);
+    else target = find_share(sh, row.p, &units);
 #pragma unroll 1
-    for (int turn = row.k ? 0 : 1; turn < (row.p < 1u << 24 ? 2 : 1); ++turn) {  // (uniform) by count, then by share of what that leaves
+    for (bool by_count = row.k != 0;; by_count = false) {      // (uniform) by count, then by share of what that leaves
+        if (sh.bin < (uint32_t)kBuckets) {                     // (uniform; else fewer tokens than k have units)
+            tokens.gather((int)sh.bin, by_count ? sh.base_count + sh.bin_count : row.k ? 0 : sh.base_count);
+            const bool few = sh.listed <= (uint32_t)kRankMost;
+            if (by_count) few ? find_ranked<true>(sh, row, target, tokens.near(), sh.listed) : find_token<true>(sh, target, tokens);
+            else few ? find_ranked<false>(sh, row, target, tokens.near(), sh.listed) : find_token<false>(sh, target, tokens);
+            end = sh.found;
+            units = sh.found_units;
+        } else if (by_count) block_before(sh, u, &units);
+        if (!by_count || row.p == 1u << 24) return end;
+        const uint64_t share = part_of(units, row.p);
+        target = share ? share : 1;
         __syncthreads();
         sh.counts[tid] = c;                                    // (a search uses their place)
         sh.units[tid] = u;
         if (tid == 0) { sh.base_count = 0; sh.base_units = 0; sh.bin = kBuckets; }
         __syncthreads();
-        if (turn == 0) find_bin<true>(sh, target);
-        else {
-            const uint64_t share = part_of(units, row.p);
-            target = share ? share : 1;
-            find_bin<false>(sh, target);
-        }
-        if (sh.bin >= (uint32_t)kBuckets) continue;            // (uniform) fewer tokens than k have units
-        tokens.gather((int)sh.bin);
-        const bool few = sh.listed <= (uint32_t)kRankMost;
-        if (turn == 0) few ? find_ranked<true>(sh, row, target, tokens.list, sh.listed) : find_token<true>(sh, target, tokens);
-        else few ? find_ranked<false>(sh, row, target, tokens.list, sh.listed) : find_token<false>(sh, target, tokens);
-        end = sh.found;
-        units = sh.found_units;
+        find_bin<false>(sh, target);
     }
-    return end;
 }
 
 // ---- reading a row, four tokens at a time: -infinity behind its end ------------------------------------------------------------------------
@@ -331,6 +372,7 @@ template <int VF> struct RowInMemory {
     const void *p;
     int32_t vocab;
     __device__ __forceinline__ void operator()(int32_t v, float *s) const { logits4<VF>(p, v, vocab, s); }
+    __device__ __forceinline__ void raw(int32_t v, float *s) const { logits4<VF>(p, v, vocab, s); }
 };
 template <int VF> struct RowInLds {
     using T = typename Elem<VF>::T;
@@ -338,10 +380,16 @@ template <int VF> struct RowInLds {
     const T *p;
     int32_t vocab;                             // (rounded up to four: the rest holds -infinity)
     __device__ __forceinline__ void operator()(int32_t v, float *s) const {
+        raw(v, s);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = logit(s[j]);
+    }
+    // as they are: NaN may be among them, and -0
+    __device__ __forceinline__ void raw(int32_t v, float *s) const {
         if (v < vocab) {
             const T4 x = *(const T4 *)(p + v);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[j] = logit((float)x[j]);
+            for (int j = 0; j < 4; ++j) s[j] = (float)x[j];
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[j] = -__builtin_inff();
@@ -359,43 +407,79 @@ __device__ __forceinline__ float block_max(SampleShared &sh, float m) {
     for (int w = 0; w < 16; ++w) m = fmaxf(m, sh.part_max[w]);
     return m;
 }
-// Tokens of a row in the buckets from `low` to `high`, in a list in LDS in any order; sh.listed: how many there are, which may be more than the list holds.
-template <typename Read>
-__device__ __forceinline__ void list_tokens(SampleShared &sh, const SampleRow &row, const Read &read, int32_t vocab, int low, int high, uint64_t *list) {
+// The tokens of a row that take() wants, in a list in LDS in any order; sh.listed: how many there are, which may be more than the list holds.
+template <typename Read, typename Take>
+__device__ __forceinline__ void list_tokens(SampleShared &sh, const Read &read, int32_t vocab, uint64_t *list, Take take) {
     __syncthreads();
     if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
 #pragma unroll 1
     for (int32_t v0 = 0; v0 < vocab; v0 += 16384) {
         float s[4][4];
+        uint32_t mine = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) read(v0 + 4096 * i + 4 * (int)threadIdx.x, s[i]);
+        for (int i = 0; i < 4; ++i) read.raw(v0 + 4096 * i + 4 * (int)threadIdx.x, s[i]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int b = row.bucket(s[i / 4][i % 4]);
-            if (b >= low && b <= high) {
-                const uint32_t n = atomicAdd(&sh.listed, 1u);
-                if (n < (uint32_t)kListMost) list[n] = place(s[i / 4][i % 4], v0 + 4096 * (i / 4) + 4 * threadIdx.x + i % 4);
-            }
-        }
+        for (int i = 0; i < 16; ++i) mine += take(s[i / 4][i % 4]);
+        const uint32_t upto = upto_in_wave(mine);
+        uint32_t at = 0;
+        if ((threadIdx.x & 63) == 63 && upto) at = atomicAdd(&sh.listed, upto);
+        at = of_lane(at, 63) + upto - mine;
+        if (mine)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (take(s[i / 4][i % 4])) {
+                    if (at < (uint32_t)kListMost) list[at] = place(s[i / 4][i % 4] + 0.0f, v0 + 4096 * (i / 4) + 4 * threadIdx.x + i % 4);
+                    ++at;
+                }
     }
     __syncthreads();
 }
 
-// The tokens of one bucket: from the list, or from the row each time where it does not hold them.
+// The tokens of one bucket: from a list of all tokens up to it, from a list of its own, or from the row each time where neither holds them.
 template <typename Read> struct BucketTokens {
     SampleShared &sh;
     const SampleRow &row;
     const Read &read;
     int32_t vocab;
-    uint64_t *list;
-    int bucket;
-    __device__ __forceinline__ void gather(int b) {
+    uint64_t *list, *own;                      // of kListMost, of kRankMost
+    uint32_t upto = ~0u;                       // tokens in the first; more than it holds: it has the bucket's
+    int bucket = 0;
+    __device__ __forceinline__ bool whole() const { return upto <= (uint32_t)kListMost; }
+    // `about`: how many tokens there are up to bucket b, more or less
+    __device__ __forceinline__ void gather(int b, uint32_t about) {
         bucket = b;
-        list_tokens(sh, row, read, vocab, b, b, list);
+        if (upto == ~0u && about <= (uint32_t)kListMost) {
+            const float least = row.least_of(b);
+            list_tokens(sh, read, vocab, list, [&](float s) { return s >= least; });
+            upto = sh.listed;
+        }
+        if (!whole()) {
+            list_tokens(sh, read, vocab, list, [&](float s) { return row.bucket(s) == bucket; });
+            return;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) sh.listed = 0;
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < upto; i += 1024) {
+            const uint64_t at = list[i];
+            if (row.bucket(logit_at(at)) == bucket) {
+                const uint32_t n = atomicAdd(&sh.listed, 1u);
+                if (n < (uint32_t)kRankMost) own[n] = at;
+            }
+        }
+        __syncthreads();
     }
+    __device__ __forceinline__ const uint64_t *near() const { return whole() ? own : list; }      // at most kRankMost of them
     template <typename Take> __device__ __forceinline__ void each(Take take) const {
-        if (sh.listed <= (uint32_t)kListMost) {                // (uniform)
+        if (whole()) {                                         // (uniform)
+            for (uint32_t i = threadIdx.x; i < upto; i += 1024) {
+                const float s = logit_at(list[i]);
+                if (row.bucket(s) == bucket) take(list[i], row.weight(s));
+            }
+            return;
+        }
+        if (sh.listed <= (uint32_t)kListMost) {
             for (uint32_t i = threadIdx.x; i < sh.listed; i += 1024) take(list[i], row.weight(logit_at(list[i])));
             return;
         }
@@ -423,7 +507,7 @@ __device__ __forceinline__ double kept_units(const SampleRow &row, float s, int3
     return w < row.least ? 0.0 : w;
 }
 
-struct Kept { uint64_t end, total; int32_t token; };   // the last token's place, units of all, the token drawn (all threads have them)
+struct Kept { uint64_t end, total; int32_t token; uint32_t listed; };   // the last token's place, units of all, the token drawn; tokens in a list that has all kept (0: none has)
 
 // The first k tokens, and all else, among the `n` of the list, which has them; k and n at most kFewMost.
 __device__ __forceinline__ Kept draw_of_few(SampleShared &sh, const SampleRow &row, const uint64_t *list, uint32_t n, uint32_t number) {
@@ -462,7 +546,53 @@ __device__ __forceinline__ Kept draw_of_few(SampleShared &sh, const SampleRow &r
     __syncthreads();
     if (tid < n && turn == sh.bin) sh.token = (int32_t)(0xffffffffu - (uint32_t)at);
     __syncthreads();
-    return {sh.found, all, sh.token};
+    return {sh.found, all, sh.token, n};
+}
+
+// The same where the last token is known, from a list of up to kListMost with all that are kept.
+__device__ __forceinline__ Kept draw_of_list(SampleShared &sh, const SampleRow &row, int32_t vocab, const uint64_t *list, uint32_t n, uint64_t end, uint32_t number) {
+    const uint32_t tid = threadIdx.x;
+    const int bits = 32 - __builtin_clz((uint32_t)vocab), shift = bits > 10 ? bits - 10 : 0;      // 1024 parts of the numbers, of up to 2^shift
+    __syncthreads();
+    sh.units[tid] = 0;
+    if (tid == 0) { sh.token = -1; sh.listed = 0; }
+    __syncthreads();
+    uint64_t u[kListMost / 1024];
+    uint32_t v[kListMost / 1024];
+#pragma unroll
+    for (int i = 0; i < kListMost / 1024; ++i) {
+        u[i] = 0;
+        v[i] = 0;
+        if (1024 * i + tid < n) {
+            const uint64_t at = list[1024 * i + tid];
+            const double w = row.weight(logit_at(at));
+            if (at >= end && w >= row.least) u[i] = whole(w);
+            v[i] = 0xffffffffu - (uint32_t)at;
+            if (u[i]) atomicAdd(&sh.units[v[i] >> shift], (unsigned long long)u[i]);
+        }
+    }
+    __syncthreads();
+    const uint64_t part = sh.units[tid];
+    uint64_t all;
+    const uint64_t before = block_before(sh, part, &all), limit = part_of(all, number);
+    if (before <= limit && limit < before + part) { sh.bin = tid; sh.base_units = before; }       // one thread: the first token has some weight
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kListMost / 1024; ++i)
+        if (u[i] && v[i] >> shift == sh.bin) {
+            const uint32_t to = atomicAdd(&sh.listed, 1u);
+            sh.few_units[to] = u[i];
+            sh.few_tokens[to] = v[i];
+        }
+    __syncthreads();
+    if (tid < sh.listed) {
+        const uint32_t own = sh.few_tokens[tid];
+        uint64_t upto = sh.base_units;
+        for (uint32_t i = 0; i < sh.listed; ++i) upto += sh.few_tokens[i] <= own ? sh.few_units[i] : 0;
+        if (upto > limit && limit >= upto - sh.few_units[tid]) sh.token = (int32_t)own;
+    }
+    __syncthreads();
+    return {end, all, sh.token, n};
 }
 
 // A bucket that the first k tokens do not reach past, by the maxima of disjoint groups of tokens that `each` names.
@@ -507,32 +637,40 @@ template <typename Item> struct WaveStream {
     }
 };
 
-// A row by one workgroup of 1024 threads.  Wavefront w draws from the `per` tokens from w per on, 256 at a time.
+// Where what is kept of a row ends, by one workgroup of 1024 threads.
+template <typename Read> __device__ __forceinline__ uint64_t cut_row(SampleShared &sh, const SampleRow &row, const Read &read, int32_t vocab, BucketTokens<Read> &tokens) {
+    const int tid = threadIdx.x;
+    __syncthreads();
+    sh.counts[tid] = 0;
+    sh.units[tid] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int32_t v = 4 * tid; v < vocab; v += 4096) {
+        float s[4];
+        double y;
+        read.raw(v, s);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int b = row.bucket(s[j]);                    // (the last one for NaN)
+            if (b < kBuckets - 1) {
+                if (row.k) atomicAdd(&sh.counts[b], 1u);
+                const double w = row.weight_within(s[j], &y);
+                atomicAdd(&sh.units[b], (unsigned long long)whole(s[j] == row.m ? kUnit : w));
+            }
+        }
+    }
+    __syncthreads();
+    return end_of_kept(sh, row, tokens);
+}
+
+// A row in memory by one workgroup.  Wavefront w draws from the `per` tokens from w per on, 256 at a time.
 template <typename Read>
-__device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &row, const Read &read, int32_t vocab, uint64_t *list, uint32_t number) {
+__device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &row, const Read &read, int32_t vocab, uint64_t *list, uint64_t *own, uint32_t number) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     uint64_t end = 0;
     if (row.cut()) {
-        __syncthreads();
-        sh.counts[tid] = 0;
-        sh.units[tid] = 0;
-        __syncthreads();
-#pragma unroll 1
-        for (int32_t v = 4 * tid; v < vocab; v += 4096) {
-            float s[4];
-            read(v, s);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int b = row.bucket(s[j]);
-                if (b < kBuckets - 1) {
-                    if (row.k) atomicAdd(&sh.counts[b], 1u);
-                    atomicAdd(&sh.units[b], (unsigned long long)whole(row.weight(s[j])));
-                }
-            }
-        }
-        __syncthreads();
-        BucketTokens<Read> tokens{sh, row, read, vocab, list, 0};
-        end = end_of_kept(sh, row, tokens);
+        BucketTokens<Read> tokens{sh, row, read, vocab, list, own};
+        end = cut_row(sh, row, read, vocab, tokens);
     }
     const SampleEnd last(end);
     const int32_t per = (vocab + 4095) / 4096 * 256, first = wave * per, stop = min(first + per, vocab);
@@ -584,71 +722,137 @@ __device__ __forceinline__ Kept draw_alone(SampleShared &sh, const SampleRow &ro
         }
     }
     __syncthreads();
-    return {end, all, sh.token};
+    return {end, all, sh.token, 0};
+}
+
+// A row in LDS of which any number of tokens is kept: their units once, in registers for the distribution.  Run i of the row is tokens 4096 i and on, four a thread.
+template <int VF, int RUNS>
+__device__ __forceinline__ Kept draw_of_many(SampleShared &sh, const SampleRow &row, const RowInLds<VF> &read, int32_t vocab, uint64_t end, uint32_t number, void *probs) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const SampleEnd last(end);
+    using Units = typename std::conditional<VF == CSB_VAL_F32, double, float>::type;       // (to 2^-24 of themselves for results of 16 bits, whose rounding is 2^-12 at least)
+    Units units[RUNS][4];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i)
+        if (4096 * i < vocab) {                                // (uniform)
+            const int32_t v = 4096 * i + 4 * tid;
+            float s[4];
+            double sum = 0.0;                                  // (of 256 weights at most: exact)
+            read.raw(v, s);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                double w = row.weight(s[j]);
+                if (!(w >= row.least && last.keeps(s[j], v + j))) w = 0.0;
+                sum += w;
+                units[i][j] = (Units)w;
+            }
+            const uint64_t all = sum_of_wave(whole(sum));
+            if (lane == 0) sh.units[16 * i + wave] = all;
+        }
+    if (tid == 0) { sh.token = -1; sh.bin = kBuckets; }
+    __syncthreads();
+    const uint64_t part = tid < 16 * RUNS && 4096 * (tid / 16) < vocab ? sh.units[tid] : 0;
+    uint64_t all;
+    const uint64_t before = block_before(sh, part, &all), limit = part_of(all, number);
+    if (before <= limit && limit < before + part) { sh.bin = tid; sh.base_units = before; }
+    __syncthreads();
+    if (wave == 0 && sh.bin < (uint32_t)kBuckets) {            // the run's 256 tokens, by one wavefront
+        const int32_t v = 256 * (int)sh.bin + 4 * lane;
+        float s[4];
+        uint64_t u[4], sum = 0;
+        read(v, s);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum += u[j] = whole(kept_units(row, s[j], v + j, last));
+        uint64_t at = sh.base_units + before_in_wave(sum);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (at <= limit && limit < at + u[j]) sh.token = v + j;
+            at += u[j];
+        }
+    }
+    if (probs) {
+        const double per = all ? 1.0 / (double)all : 0.0;
+#pragma unroll
+        for (int i = 0; i < RUNS; ++i) {
+            const int32_t v = 4096 * i + 4 * tid;
+            float x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = (float)((double)units[i][j] * per);
+            if (v < vocab) probs4<VF>(probs, v, vocab, x);
+        }
+    }
+    __syncthreads();
+    return {end, all, sh.token, 0};
 }
 
 template <int VF, int BYTES>
 __global__ __launch_bounds__(1024) void sample_small_kernel(const SampleDev a) {
     using T = typename Elem<VF>::T;
     using T4 = T __attribute__((ext_vector_type(4)));
+    constexpr int RUNS = BYTES / (int)sizeof(T4) / 1024;
     __shared__ SampleShared sh;
-    __shared__ uint64_t list[kListMost];
+    __shared__ uint64_t list[kListMost], own[kRankMost];
     __shared__ T4 held[BYTES / sizeof(T4)];
     const int number = blockIdx.x, tid = threadIdx.x;
     const T *from = (const T *)a.logits + (int64_t)number * a.ld;
+    T *to = a.probs ? (T *)a.probs + (int64_t)number * a.ldp : nullptr;
+    T4 x[RUNS];
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i) {
+        const int32_t v = 4 * tid + 4096 * i;
+        if (v + 4 <= a.vocab) x[i] = load_any<T4>(from + v);
+        else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i][j] = v + j < a.vocab ? from[v + j] : (T)-__builtin_inff();
+        }
+    }
     float largest = -__builtin_inff();                         // of the thread's tokens
 #pragma unroll
-    for (int i = 0; i < BYTES / (int)sizeof(T4) / 1024; ++i) {
+    for (int i = 0; i < RUNS; ++i) {
         const int32_t v = 4 * tid + 4096 * i;
-        if (v < a.vocab) {
-            T4 x;
-            if (v + 4 <= a.vocab) x = load_any<T4>(from + v);
-            else {
+        if (v < a.vocab) held[v / 4] = x[i];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = v + j < a.vocab ? from[v + j] : (T)-__builtin_inff();
-            }
-            held[v / 4] = x;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) largest = fmaxf(largest, logit((float)x[j]));
-        }
+        for (int j = 0; j < 4; ++j) largest = fmaxf(largest, logit((float)x[i][j]));
     }
     const float m = block_max(sh, largest);                    // (the barrier is for the row too)
     const SampleRow row(a, number, m);
     const RowInLds<VF> read{(const T *)held, a.vocab};
     const uint32_t r = a.tokens ? draw_number(a.r[number]) : 0;
-    Kept kept{0, 0, -1};
-    if (m > -__builtin_inff()) {                               // (uniform, as all that follows)
+    Kept kept{0, 0, -1, 0};
+    bool zeros = true;                                         // (all of what follows is uniform)
+    if (m > -__builtin_inff()) {
         bool few = false;
         if (row.k && row.k <= kFewest) {
             const int b = bucket_of_first(sh, row, [&](auto take) { take(largest); });
-            list_tokens(sh, row, read, a.vocab, 0, b, list);
+            const float least = row.least_of(b);
+            list_tokens(sh, read, a.vocab, list, [&](float s) { return s >= least; });
             few = sh.listed <= (uint32_t)kFewMost;
+            if (few) kept = draw_of_few(sh, row, list, sh.listed, r);
         }
-        kept = few ? draw_of_few(sh, row, list, sh.listed, r) : draw_alone(sh, row, read, a.vocab, list, r);
+        if (!few) {
+            uint64_t end = 0;
+            BucketTokens<RowInLds<VF>> tokens{sh, row, read, a.vocab, list, own};
+            if (row.cut()) end = cut_row(sh, row, read, a.vocab, tokens);
+            if (end && tokens.whole()) kept = draw_of_list(sh, row, a.vocab, list, tokens.upto, end, r);
+            else {
+                kept = draw_of_many<VF, RUNS>(sh, row, read, a.vocab, end, r, to);
+                zeros = false;
+            }
+        }
     }
     if (a.tokens && tid == 0) a.tokens[number] = kept.token;
-    if (a.probs) {
-        // zeros in the row's place, the kept over them, side by side
-        T *to = (T *)a.probs + (int64_t)number * a.ldp;
+    if (to && zeros) {                                         // zeros in the row's place, the kept over them
         const double per = kept.total ? 1.0 / (double)kept.total : 0.0;
-        const SampleEnd last(kept.end);
-        struct Item { float s; int32_t v; };
         __syncthreads();
-        WaveStream<Item> stream{(Item *)list + 128 * (tid >> 6)};
-        const auto set = [&](const Item &x, bool there) {
-            const double w = row.weight(x.s);
-            if (there) ((T *)held)[x.v] = (T)(float)(w < row.least ? 0.0 : w * per);
-        };
 #pragma unroll 1
-        for (int32_t v0 = 0; v0 < a.vocab; v0 += 4096) {
-            const int32_t v = v0 + 4 * tid;
-            float s[4];
-            read(v, s);
-            if (v < a.vocab) held[v / 4] = T4{};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) stream.add(kept.total && s[j] > -__builtin_inff() && last.keeps(s[j], v + j), Item{s[j], v + j}, set);
+        for (int32_t v = 4 * tid; v < a.vocab; v += 4096) held[v / 4] = T4{};
+        __syncthreads();
+        for (uint32_t i = tid; i < kept.listed; i += 1024) {
+            const uint64_t at = list[i];
+            const double w = row.weight(logit_at(at));
+            if (at >= kept.end) ((T *)held)[0xffffffffu - (uint32_t)at] = (T)(float)(w < row.least ? 0.0 : w * per);
         }
-        stream.rest(set);
         __syncthreads();
 #pragma unroll 1
         for (int32_t v = 4 * tid; v < a.vocab; v += 4096) {
@@ -739,7 +943,7 @@ __global__ __launch_bounds__(1024) void sample_few_kernel(const SampleDev a) {
     const float m = max_of_row(a, number);
     const SampleRow row(a, number, m);
     bool few = m == -__builtin_inff();                         // (nothing to draw from)
-    Kept kept{0, 0, -1};
+    Kept kept{0, 0, -1, 0};
     if (!few && row.k && row.k <= kFewest) {                   // (uniform)
         const auto each = [&](auto take) {
 #pragma unroll
@@ -922,7 +1126,7 @@ struct ListedTokens {
 template <int VF>
 __global__ __launch_bounds__(1024) void sample_draw_kernel(const SampleDev a) {
     __shared__ SampleShared sh;
-    __shared__ uint64_t list[kListMost];
+    __shared__ uint64_t list[kListMost], own[kRankMost];
     __shared__ unsigned long long sums[kMaxChunks];
     const int tid = threadIdx.x;
     if (a.others && blockIdx.x >= *a.n_others) return;
@@ -935,7 +1139,7 @@ __global__ __launch_bounds__(1024) void sample_draw_kernel(const SampleDev a) {
     const uint32_t listed = state == ROW_CUT ? a.listed[number] : 0;
     if (state == ROW_ALONE || listed > (uint32_t)kListMost) {
         const RowInMemory<VF> read{(const typename Elem<VF>::T *)a.logits + (int64_t)number * a.ld, a.vocab};
-        const Kept kept = draw_alone(sh, row, read, a.vocab, list, r);
+        const Kept kept = draw_alone(sh, row, read, a.vocab, list, own, r);
         if (tid == 0) {
             if (a.tokens) a.tokens[number] = kept.token;
             a.ends[number] = kept.end;
