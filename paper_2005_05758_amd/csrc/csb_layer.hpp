@@ -64,16 +64,19 @@ template <int VF> __device__ __forceinline__ float sigmoid_for(float x) {
 template <int VF> __device__ __forceinline__ float silu(float x) { return x * sigmoid_for<VF>(x); }
 
 // ln(1 + e^x) = max(x, 0) + ln(1 + e), e = e^-|x| in (0, 1]: 2 atanh(s), s = e / (2 + e), as 2 s (1 + w p(w)), w = s^2 <= 1/9, p through five of Chebyshev's points
-// (2^-29): small steps keep all of their digits, which ln(1 + e) of a rounded sum would not.
-__device__ __forceinline__ float softplus(float x) {
-    const float e = exp_within(-fabsf(x)), s = e * __builtin_amdgcn_rcpf(2.0f + e), w = s * s;
+// (2^-29): small steps keep all of their digits, which ln(1 + e) of a rounded sum would not.  From 16 bits, whose rounding of x is 2^12 times as much and
+// more, the argument of the exponential is rounded once (1.25 |x| units of 2^-24 of the result): 17 instructions' time instead of 24.
+template <int VF> __device__ __forceinline__ float softplus_from(float x) {
+    constexpr bool SHORT = VF != CSB_VAL_F32;
+    const float e = SHORT ? __builtin_amdgcn_exp2f(fabsf(x) * -1.44269502162933349609375f) : exp_within(-fabsf(x));
+    const float s = e * __builtin_amdgcn_rcpf(2.0f + e), w = s * s;
     float p = 0.11612164974212646f;
     p = fmaf(p, w, 0.1085328757762909f);
     p = fmaf(p, w, 0.142961785197258f);
     p = fmaf(p, w, 0.19999852776527405f);
     p = fmaf(p, w, 0.3333333432674408f);
-    const float l = fmaf(s + s, w * p, s + s);
-    return x != x ? x : fmaxf(x, 0.0f) + l;
+    const float l = fmaf(s + s, w * p, s + s), y = fmaxf(x, 0.0f) + l;
+    return SHORT || x == x ? y : x;                            // (without limits of the exponential's argument NaN stays)
 }
 #endif
 

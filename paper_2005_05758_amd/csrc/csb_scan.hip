@@ -106,6 +106,12 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
         }
     }
 
+    // Two channels of a token, 16 bytes, lie together in LDS, those of eight channels turned by `turn`, so that neighbouring threads' are in banks of their own:
+    // of sixteen threads eight have the even token's, eight the odd one's, whose row is 32 banks on.
+    using f32x4 = float __attribute__((ext_vector_type(4)));
+    using f32x2 = float __attribute__((ext_vector_type(2)));
+    const auto pair = [](int channel, int token) { return (channel >> 3 << 4) + (((channel >> 1) + (channel >> 5) + 2 * token) & 3) * 4; };
+    const int even = pair(c, 0) + 2 * (c & 1), odd = pair(c, 1) + 2 * (c & 1);
     // the same thread makes what eight channels of a token need, and their outputs
     const int sc = (tid & 7) * 8, st = tid >> 3, there = cols - sc;
     float bias[8], D[8];
@@ -117,36 +123,61 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
     const int64_t stop = count < t0 + each ? count : t0 + each;
     Run x, z, next_x, next_dt, next_z;                         // a tile's operands are requested while the one before is worked on
     T next_B[K / 2], next_C[K / 2];
+    // whole: all 64 channels, and all of a tile's tokens: nothing to ask for each thread
+    const bool wide = FULL && cols == kScanCols;
+    const int bt = tid / (4 * K), bj = tid % (4 * K);
+    constexpr int STEP = 256 / (4 * K);                        // tokens of B and C that the workgroup loads at a time
+    const int64_t from = first + t0 + st, from_b = first + t0 + bt, at_b = (int64_t)group * a.n + bj;
+    const T *px = (const T *)a.x + from * a.ldx + base + sc, *pdt = (const T *)a.dt + from * a.lddt + base + sc;
+    const T *pz = OUT && a.z ? (const T *)a.z + from * a.ldz + base + sc : nullptr;
+    const T *pB = (const T *)a.B + from_b * a.ldB + at_b, *pC = (const T *)a.C + from_b * a.ldC + at_b;
+    T *po = (T *)a.out + from * a.ldo + base + sc;
     auto load = [&](int64_t t) {
-        next_x.v = next_dt.v = next_z.v = typename Run::T8{};
-        if (t + st < stop && there > 0) {
-            const int64_t at = first + t + st;
-            next_x.load((const T *)a.x + at * a.ldx + base + sc, there);
-            next_dt.load((const T *)a.dt + at * a.lddt + base + sc, there);
-            if (OUT && a.z) next_z.load((const T *)a.z + at * a.ldz + base + sc, there);
-        }
+        if (wide && t + kScanTile <= stop) {
+            next_x.load(px, 8);
+            next_dt.load(pdt, 8);
+            if (OUT && a.z) next_z.load(pz, 8);
 #pragma unroll
-        for (int i = 0; i < K / 2; ++i) {
-            const int e = tid + 256 * i, tt = e / (4 * K), j = e % (4 * K);
-            const bool in = t + tt < stop && j < a.n;
-            next_B[i] = in ? ((const T *)a.B)[(first + t + tt) * a.ldB + (int64_t)group * a.n + j] : (T)0.0f;
-            if (OUT) next_C[i] = in ? ((const T *)a.C)[(first + t + tt) * a.ldC + (int64_t)group * a.n + j] : (T)0.0f;
+            for (int i = 0; i < K / 2; ++i) {
+                next_B[i] = pB[i * STEP * a.ldB];
+                if (OUT) next_C[i] = pC[i * STEP * a.ldC];
+            }
+        } else {
+            next_x.v = next_dt.v = next_z.v = typename Run::T8{};
+            if (t + st < stop && there > 0) {
+                next_x.load(px, there);
+                next_dt.load(pdt, there);
+                if (OUT && a.z) next_z.load(pz, there);
+            }
+#pragma unroll
+            for (int i = 0; i < K / 2; ++i) {
+                const bool in = t + bt + i * STEP < stop && bj < a.n;
+                next_B[i] = in ? pB[i * STEP * a.ldB] : (T)0.0f;
+                if (OUT) next_C[i] = in ? pC[i * STEP * a.ldC] : (T)0.0f;
+            }
         }
+        px += kScanTile * a.ldx;
+        pdt += kScanTile * a.lddt;
+        pB += kScanTile * a.ldB;
+        if (OUT) { pz += kScanTile * a.ldz; pC += kScanTile * a.ldC; }
     };
     double total = 0.0;
     load(t0);
     for (int64_t t = t0; t < stop; t += kScanTile) {
         const int live = (int)(stop - t < kScanTile ? stop - t : kScanTile);
-        float *row = steps + st * kScanRow + 2 * sc;
+        float *row = steps + st * kScanRow;
         x = next_x;
         z = next_z;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float d = next_dt[i] + bias[i];
-            if (a.softplus) d = softplus(d);
-            if (st >= live) d = 0.0f;                          // (past the end: nothing decays, nothing comes in)
-            row[2 * i] = d;
-            row[2 * i + 1] = d * x[i];
+        for (int i = 0; i < 8; i += 2) {
+            float d[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                d[k] = next_dt[i + k] + bias[i + k];
+                if (a.softplus) d[k] = softplus_from<VF>(d[k]);
+            }
+            if (live < kScanTile && st >= live) d[0] = d[1] = 0.0f;              // (past the end: nothing decays, nothing comes in)
+            *(f32x4 *)(row + pair(sc + i, st)) = f32x4{d[0], d[0] * x[i], d[1], d[1] * x[i + 1]};
         }
 #pragma unroll
         for (int i = 0; i < K / 2; ++i) {
@@ -156,35 +187,55 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
         if (t + kScanTile < stop) load(t + kScanTile);
         __syncthreads();
         float sum = 0.0f;
+        float *e = steps + even, *o = steps + odd, *to = steps + q * kScanRow + (q & 1 ? odd : even) + (q >> 1);
+        const float *b = Bs + j0, *cc = Cs + j0;
         for (int i = 0; i < live; i += 4) {
             float y[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const float *d = steps + (i + u) * kScanRow + 2 * c, *b = Bs + (i + u) * 4 * K + j0, *cc = Cs + (i + u) * 4 * K + j0;
-                const float step = d[0], in = d[1];
+                const float *d = (u & 1 ? o : e) + u * kScanRow;
+                const f32x2 both = *(const f32x2 *)d;
+                const float step = both[0], in = both[1];
                 y[u] = 0.0f;
+                f32x4 bu[K / 4], cu[K / 4];
+#pragma unroll
+                for (int k = 0; k < K / 4; ++k) {
+                    bu[k] = *(const f32x4 *)(b + u * 4 * K + 4 * k);
+                    if (OUT) cu[k] = *(const f32x4 *)(cc + u * 4 * K + 4 * k);
+                }
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    h[k] = fmaf(__builtin_amdgcn_exp2f(step * A[k]), h[k], in * b[k]);
+                    h[k] = fmaf(__builtin_amdgcn_exp2f(step * A[k]), h[k], in * bu[k / 4][k % 4]);
                     if (!FULL) h[k] = have(k) ? h[k] : 0.0f;   // (infinite inputs make NaN of zeros)
-                    if (OUT) y[u] = fmaf(cc[k], h[k], y[u]);
+                    if (OUT) y[u] = fmaf(cu[k / 4][k % 4], h[k], y[u]);
                 }
                 if (!OUT) sum += step;
             }
-            if (OUT) steps[(i + q) * kScanRow + 2 * c] = sum_of_rows(y);         // of token i + q
+            // of token i + q, in place of the step, or of its product: other banks for the third and fourth
+            if (OUT) *to = sum_of_rows(y);
+            e += 4 * kScanRow;
+            o += 4 * kScanRow;
+            to += 4 * kScanRow;
+            b += 16 * K;
+            cc += 16 * K;
         }
         total += sum;
         __syncthreads();
-        if (OUT && st < live && there > 0) {
+        if (OUT && (live == kScanTile || st < live) && (wide || there > 0)) {
             Run o;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float y = fmaf(D[i], x[i], row[2 * i]);
-                if (a.z) y *= silu<VF>(z[i]);
-                o.set(i, y);
+            for (int i = 0; i < 8; i += 2) {
+                const f32x4 from = *(const f32x4 *)(row + pair(sc + i, st));
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float y = fmaf(D[i + k], x[i + k], st & 2 ? from[2 * k + 1] : from[2 * k]);
+                    if (a.z) y *= silu<VF>(z[i + k]);
+                    o.set(i + k, y);
+                }
             }
-            o.store((T *)a.out + (first + t + st) * a.ldo + base + sc, there);
+            o.store(po, wide ? 8 : there);
         }
+        if (OUT) po += kScanTile * a.ldo;
     }
     if (OUT) {
         if (last && a.s_out && known) put(a.s_out + s * state);
@@ -264,7 +315,7 @@ __global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a
         if (t + 1 < end) load(t + 1, next);
         const float x = (float)now.x;
         float step = (float)now.dt + bias, y = 0.0f;
-        if (a.softplus) step = softplus(step);
+        if (a.softplus) step = softplus_from<VF>(step);
         const float in = step * x;
 #pragma unroll
         for (int k = 0; k < K; ++k) {

@@ -55,12 +55,15 @@ def scan(x, dt, A, B, C, D, z, bias, softplus, ranges, slots, state, fmt):
     out, off = np.full((T, ch), np.nan), np.zeros((T, ch))
     state, soff = state.copy(), np.zeros(state.shape)
     step = dt + bias
-    # dt + bias: U of it; ln(1 + e^s) has a slope of at most 1 and 12 U of its own (exponential 4, quotient 4, series and sum 4)
+    # dt + bias: U of it; ln(1 + e^s) has a slope of at most 1 and 12 U of its own (exponential 4, quotient 4, series and sum 4).  From 16 bits the
+    # exponential's argument is two numbers' rounded product: e^-|s| is 1.25 |s| U more off, and ln(1 + e) that times e / (1 + e) <= ln(1 + e)
     step_off = U * np.abs(step)
     if softplus:
+        with np.errstate(invalid="ignore"):
+            short = 0.0 if fmt == "f32" else np.where(np.abs(step) < 1000, 1.25 * np.abs(step) * np.log1p(np.exp(-np.abs(step))), 0.0) * U
         step = np.maximum(step, 0.0) + np.log1p(np.exp(-np.abs(step)))
         slope = -np.expm1(-step)
-        step_off = slope * step_off + 12 * U * step
+        step_off = slope * step_off + 12 * U * step + short
     gate = silu(z) if z is not None else np.ones((T, ch))
     for (first, end), s in zip(ranges, slots):
         h = state[s].copy() if s >= 0 else np.zeros((ch, n))
