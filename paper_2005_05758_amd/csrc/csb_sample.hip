@@ -98,12 +98,24 @@ struct SampleRow {
         e = fma_of_constant(e, f, 1.0000000000000135);
         return __builtin_floor(__builtin_amdgcn_ldexp(e, (int)(uint32_t)__builtin_bit_cast(uint64_t, t)));
     }
+    // four at a time, side by side and for all lanes, whatever they are used for: one by one each instruction waits for the one before
+    __device__ __forceinline__ void weights_within(const float *s, double *w, double *log) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = weight_within(s[j], log + j);
+        asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = s[j] == m ? kUnit : w[j];
+    }
     // a logit that no token up to bucket b is below (others may be above it, none of them infinite): the rounding of bucket() is 2^-22 of it, of the difference 2^-22 of m
     __device__ __forceinline__ float least_of(int b) const {
         const float t = m - (float)(b + 1) * 1.0001f / (per_bucket * part) - fabsf(m) * 0x1p-22f;
         return t > -0x1.fffffep127f ? t : -0x1.fffffep127f;
     }
-    __device__ __forceinline__ int bucket(float s) const { return s == m ? 0 : (int)fminf(fmaf(s, -part, part_of_m) * per_bucket, (float)(kBuckets - 1)); }
+    __device__ __forceinline__ int bucket(float s) const {
+        float b = fminf(fmaf(s, -part, part_of_m) * per_bucket, (float)(kBuckets - 1));
+        asm("" : "+v"(b));                                     // (a choice of two numbers, no branch around one)
+        return (int)(s == m ? 0.0f : b);
+    }
 };
 
 __device__ __forceinline__ uint64_t whole(double w) { return __builtin_bit_cast(uint64_t, w + 0x1p52) & 0xfffffffffffffull; }
@@ -647,15 +659,15 @@ template <typename Read> __device__ __forceinline__ uint64_t cut_row(SampleShare
 #pragma unroll 1
     for (int32_t v = 4 * tid; v < vocab; v += 4096) {
         float s[4];
-        double y;
+        double w[4], log[4];
         read.raw(v, s);
+        row.weights_within(s, w, log);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int b = row.bucket(s[j]);                    // (the last one for NaN)
             if (b < kBuckets - 1) {
                 if (row.k) atomicAdd(&sh.counts[b], 1u);
-                const double w = row.weight_within(s[j], &y);
-                atomicAdd(&sh.units[b], (unsigned long long)whole(s[j] == row.m ? kUnit : w));
+                atomicAdd(&sh.units[b], (unsigned long long)whole(w[j]));
             }
         }
     }
@@ -738,14 +750,16 @@ __device__ __forceinline__ Kept draw_of_many(SampleShared &sh, const SampleRow &
         if (4096 * i < vocab) {                                // (uniform)
             const int32_t v = 4096 * i + 4 * tid;
             float s[4];
-            double sum = 0.0;                                  // (of 256 weights at most: exact)
+            double w[4], log[4], sum = 0.0;                    // (of 256 weights at most: exact)
             read.raw(v, s);
+            row.weights_within(s, w, log);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                double w = row.weight(s[j]);
-                if (!(w >= row.least && last.keeps(s[j], v + j))) w = 0.0;
-                sum += w;
-                units[i][j] = (Units)w;
+                const bool more = s[j] > last.s, same = s[j] == last.s, before = (uint32_t)(v + j) <= last.v;
+                const bool kept = (more | (same & before)) & ((log[j] > -40.0) | (s[j] == row.m)) & (w[j] >= row.least);
+                const double u = kept ? w[j] : 0.0;
+                sum += u;
+                units[i][j] = (Units)u;
             }
             const uint64_t all = sum_of_wave(whole(sum));
             if (lane == 0) sh.units[16 * i + wave] = all;
