@@ -35,10 +35,10 @@ struct SampleDev {
     void *probs;
     int64_t ld, ldp;
     int32_t rows, vocab, chunks;
-    // workspace: [rows][chunks], [rows][chunks][256], [rows][kBuckets], [rows], [rows][kListMost]; the rows that are not few (NULL: all of them), how many
+    // workspace: [rows][chunks], [rows][chunks][256], [rows][kBuckets] (units, or tokens where k cuts), [rows], [rows][kListMost], [rows] (NULL: no row is few)
     float *maxes, *groups;
-    unsigned long long *units, *sums;
-    uint32_t *counts, *listed, *others, *n_others;
+    unsigned long long *histogram, *sums;
+    uint32_t *listed, *done;
     uint64_t *ends, *totals, *list;
 };
 
@@ -56,7 +56,9 @@ struct SampleRow {
     int32_t k;                                 // 0: all
     uint32_t p;                                // floor(top_p 2^24); 2^24: all
     double least;                              // units that min-p asks for
-    __device__ __forceinline__ SampleRow(const SampleDev &a, int row, float max) : m(max) {
+    __device__ __forceinline__ SampleRow(const SampleDev &a, int row, float max) : SampleRow(a, row) { largest(max); }
+    // what does not need the largest logit
+    __device__ __forceinline__ SampleRow(const SampleDev &a, int row) {
         const float T = a.temperature ? a.temperature[row] : 1.0f;
         k = a.top_k ? a.top_k[row] : 0;
         if (k < 1 || k >= a.vocab) k = 0;
@@ -73,6 +75,9 @@ struct SampleRow {
             k = 1;                                             // and the first of them
             part = 1.0f;
         }
+    }
+    __device__ __forceinline__ void largest(float max) {
+        m = max;
         part_of_m = m * part;
     }
     __device__ __forceinline__ bool cut() const { return k || p < 1u << 24; }
@@ -893,30 +898,14 @@ __device__ __forceinline__ float max_of_row(const SampleDev &a, int row) {
     return max_of_wave(m);
 }
 // Sixteen tokens of a chunk: numbers chunk_number(c, 0 .. 15).
-__device__ __forceinline__ int32_t chunk_number(int c, int i) { return c * kChunk + 1024 * (i / 4) + 4 * (int)threadIdx.x + i % 4; }
+__device__ __forceinline__ int32_t chunk_number(int c, int i) { return c * kChunk + 1024 * (i / 4) + 4 * (int)(threadIdx.x & 255) + i % 4; }
 template <int VF> __device__ __forceinline__ void chunk_tokens(const SampleDev &a, int row, int c, float (*s)[4]) {
     const void *from = (const typename Elem<VF>::T *)a.logits + (int64_t)row * a.ld;
 #pragma unroll
     for (int i = 0; i < 4; ++i) logits4<VF>(from, chunk_number(c, 4 * i), a.vocab, s[i]);
 }
-// The chunks of rows that are not few, by all workgroups in turn: work(row, chunk).  (The barrier is between two turns' use of LDS.)
-template <typename Work> __device__ __forceinline__ void for_other_chunks(const SampleDev &a, Work work) {
-    const uint32_t n = (a.others ? *a.n_others : (uint32_t)a.rows) * (uint32_t)a.chunks;
-    for (uint32_t i = blockIdx.x; i < n; i += gridDim.x) {     // (uniform)
-        const uint32_t row = i / (uint32_t)a.chunks;
-        work(a.others ? (int)a.others[row] : (int)row, (int)(i % (uint32_t)a.chunks));
-        __syncthreads();
-    }
-}
 __device__ __forceinline__ RowState state_of(const SampleRow &row) {      // (few that were too many, and both ends: the second is known when the first is)
     return !row.cut() ? ROW_WHOLE : row.k && (row.k <= kFewest || row.p < 1u << 24) ? ROW_ALONE : ROW_CUT;
-}
-// Sum over 256 threads.
-__device__ __forceinline__ uint64_t sum_of_256(uint64_t v, uint64_t *part) {
-    v = sum_of_wave(v);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return part[0] + part[1] + part[2] + part[3];
 }
 
 template <int VF>
@@ -934,22 +923,18 @@ __global__ __launch_bounds__(256) void sample_max_kernel(const SampleDev a) {
     if (tid == 0) a.maxes[blockIdx.x] = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
     if (c == 0) {                                              // the row's histogram starts empty
 #pragma unroll
-        for (int i = 0; i < kBuckets / 256; ++i) {
-            a.counts[(int64_t)row * kBuckets + 256 * i + tid] = 0;
-            a.units[(int64_t)row * kBuckets + 256 * i + tid] = 0;
-        }
+        for (int i = 0; i < kBuckets / 256; ++i) a.histogram[(int64_t)row * kBuckets + 256 * i + tid] = 0;
         if (tid == 0) a.listed[row] = 0;
-        if (row == 0 && tid == 0) *a.n_others = 0;
     }
 }
 
-// Few tokens; the other rows are noted.
-template <int VF>
-__global__ __launch_bounds__(1024) void sample_few_kernel(const SampleDev a) {
-    __shared__ SampleShared sh;
-    __shared__ uint64_t list[kFewMost];
-    __shared__ uint32_t hits[kFewMost];
-    const int number = blockIdx.x, tid = threadIdx.x, n_groups = a.chunks * 256;
+// Few tokens of a row.
+struct FewShared { SampleShared sh; uint64_t list[kFewMost]; uint32_t hits[kFewMost]; };
+template <int VF> __device__ __forceinline__ void draw_few_row(const SampleDev &a, FewShared &few_shared, int number) {
+    SampleShared &sh = few_shared.sh;
+    uint64_t *list = few_shared.list;
+    uint32_t *hits = few_shared.hits;
+    const int tid = threadIdx.x, n_groups = a.chunks * 256;
     const float *groups = a.groups + (int64_t)number * n_groups;
     float g[8];                                                // the first 8192 groups stay in registers
 #pragma unroll
@@ -997,55 +982,73 @@ __global__ __launch_bounds__(1024) void sample_few_kernel(const SampleDev a) {
         if (few) kept = draw_of_few(sh, row, list, sh.listed, a.tokens ? draw_number(a.r[number]) : 0);
     }
     if (tid) return;
+    a.done[number] = few;
     if (few) {
         if (a.tokens) a.tokens[number] = kept.token;
         a.ends[number] = kept.end;
         a.totals[number] = kept.total;
-    } else a.others[atomicAdd(a.n_others, 1u)] = number;
+    }
 }
 
-// The histogram of rows that are cut; the chunk's units of those that are not.
-template <int VF>
-__global__ __launch_bounds__(256) void sample_histogram_kernel(const SampleDev a) {
-    __shared__ unsigned long long bins[kBuckets];              // units, and from 2^51 on tokens: both of 4096 tokens of 2^38 at most
-    __shared__ uint64_t part[4];
+// The histogram of a row that is cut, the chunks' units of one that is not: four chunks by 1024 threads.
+struct HistogramShared { unsigned long long bins[kBuckets]; uint64_t part[16]; };
+template <int VF> __device__ __forceinline__ void count_chunks(const SampleDev &a, HistogramShared &sh, int number, int c) {
     const int tid = threadIdx.x;
-    for_other_chunks(a, [&](int number, int c) {
-        float s[4][4];
-        chunk_tokens<VF>(a, number, c, s);
-        const float m = max_of_row(a, number);
-        const SampleRow row(a, number, m);
-        const RowState state = state_of(row);
-        const bool any = m > -__builtin_inff();
-        if (state == ROW_ALONE) return;
-        if (state == ROW_WHOLE || !any) {
-            const SampleEnd all(0);
-            double here = 0.0;                                 // (16 weights: exact)
+    float s[4][4];
+    SampleRow row(a, number);
+    const RowState state = state_of(row);
+    if (state == ROW_ALONE) return;                            // (uniform)
+    chunk_tokens<VF>(a, number, c, s);                         // (past the row's last chunk: of no weight)
+    const float m = max_of_row(a, number);
+    row.largest(m);
+    const bool any = m > -__builtin_inff();
+    if (state == ROW_WHOLE || !any) {
+        const SampleEnd all(0);
+        double here = 0.0;                                     // (16 weights: exact)
 #pragma unroll 4
-            for (int i = 0; i < 16; ++i) here += any ? kept_units(row, s[i / 4][i % 4], 0, all) : 0.0;
-            const uint64_t sum = sum_of_256(whole(here), part);
-            if (tid == 0) a.sums[(int64_t)number * a.chunks + c] = sum;
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < kBuckets / 256; ++i) bins[256 * i + tid] = 0;
+        for (int i = 0; i < 16; ++i) here += any ? kept_units(row, s[i / 4][i % 4], 0, all) : 0.0;
+        const uint64_t sum = sum_of_wave(whole(here));
+        if ((tid & 63) == 0) sh.part[tid >> 6] = sum;
         __syncthreads();
+        const uint64_t *of_chunk = sh.part + (tid >> 8) * 4;
+        if ((tid & 255) == 0 && c < a.chunks) a.sums[(int64_t)number * a.chunks + c] = of_chunk[0] + of_chunk[1] + of_chunk[2] + of_chunk[3];
+        return;
+    }
+    sh.bins[tid] = 0;
+    __syncthreads();
+    if (row.k) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const float x = s[i / 4][i % 4];
-            const int b = row.bucket(x);
-            if (b < kBuckets - 1) atomicAdd(&bins[b], (unsigned long long)(whole(row.weight(x)) + (1ull << 51)));
+            const int b = row.bucket(s[i / 4][i % 4]);
+            if (b < kBuckets - 1) atomicAdd(&sh.bins[b], 1ull);
         }
-        __syncthreads();
+    } else {
 #pragma unroll
-        for (int i = 0; i < kBuckets / 256; ++i) {
-            const unsigned long long v = bins[256 * i + tid];
-            if (v) {
-                if (row.k) atomicAdd(&a.counts[(int64_t)number * kBuckets + 256 * i + tid], (uint32_t)(v >> 51));
-                atomicAdd(&a.units[(int64_t)number * kBuckets + 256 * i + tid], v & ((1ull << 51) - 1));
+        for (int i = 0; i < 4; ++i) {
+            double w[4], log[4];
+            row.weights_within(s[i], w, log);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int b = row.bucket(s[i][j]);
+                if (b < kBuckets - 1) atomicAdd(&sh.bins[b], (unsigned long long)whole(w[j]));
             }
         }
-    });
+    }
+    __syncthreads();
+    const unsigned long long v = sh.bins[tid];
+    if (v) atomicAdd(&a.histogram[(int64_t)number * kBuckets + tid], v);
+}
+
+// Workgroups of few rows, and beside them those of other rows' chunks.
+template <int VF>
+__global__ __launch_bounds__(1024) void sample_few_kernel(const SampleDev a) {
+    __shared__ union { FewShared few; HistogramShared histogram; } shared;
+    const uint32_t few_rows = a.done ? (uint32_t)a.rows : 0u, quarters = (uint32_t)(a.chunks + 3) / 4;
+    if (blockIdx.x < few_rows) draw_few_row<VF>(a, shared.few, (int)blockIdx.x);
+    else {
+        const uint32_t i = blockIdx.x - few_rows;
+        count_chunks<VF>(a, shared.histogram, (int)(i / quarters), (int)(i % quarters) * 4 + (int)(threadIdx.x >> 8));
+    }
 }
 
 // The bucket in which what is kept of a row ends, by 256 threads, four buckets each (kBuckets: nothing is cut).
@@ -1054,7 +1057,7 @@ __device__ __forceinline__ int bucket_of_256(const SampleDev &a, int number, con
     uint64_t u[4], mine = 0, all = 0, before;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        u[i] = row.k ? a.counts[(int64_t)number * kBuckets + 4 * tid + i] : a.units[(int64_t)number * kBuckets + 4 * tid + i];
+        u[i] = a.histogram[(int64_t)number * kBuckets + 4 * tid + i];
         mine += u[i];
     }
     before = before_in_wave(mine);
@@ -1083,48 +1086,50 @@ __global__ __launch_bounds__(256) void sample_bucket_kernel(const SampleDev a) {
     __shared__ uint64_t part[4];
     __shared__ int found;
     __shared__ uint32_t n_kept, at;
-    const int tid = threadIdx.x;
-    for_other_chunks(a, [&](int number, int c) {
-        float s[4][4];
-        chunk_tokens<VF>(a, number, c, s);
-        const float m = max_of_row(a, number);
-        const SampleRow row(a, number, m);
-        if (state_of(row) != ROW_CUT || !(m > -__builtin_inff())) return;
-        if (tid == 0) n_kept = 0;
-        const int bucket = bucket_of_256(a, number, row, part, &found);
-        uint32_t mine = 0;                                     // which of the sixteen are the bucket's
+    const int tid = threadIdx.x, number = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks;
+    float s[4][4];
+    SampleRow row(a, number);
+    if (state_of(row) != ROW_CUT) return;                      // (uniform)
+    chunk_tokens<VF>(a, number, c, s);
+    const float m = max_of_row(a, number);
+    if (!(m > -__builtin_inff())) return;
+    row.largest(m);
+    if (tid == 0) n_kept = 0;
+    const int bucket = bucket_of_256(a, number, row, part, &found);
+    uint32_t mine = 0;                                     // which of the sixteen are the bucket's
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float x = s[i / 4][i % 4];
-            const int b = row.bucket(x);
-            if (b == bucket) mine |= 1u << i;
-            if (b < bucket && b < kBuckets - 1) kept[atomicAdd(&n_kept, 1u)] = x;
-        }
-        const uint32_t count = __builtin_popcount(mine), below = before_in_wave(count);
-        __syncthreads();
-        if ((tid & 63) == 63) part[tid >> 6] = below + count;
-        __syncthreads();
-        if (tid == 0) {
-            const uint32_t total = (uint32_t)(part[0] + part[1] + part[2] + part[3]);
-            at = total ? atomicAdd(&a.listed[number], total) : 0;               // a place for the workgroup's
-        }
-        __syncthreads();
-        uint32_t to = at + below;
-        for (int w = 0; w < (tid >> 6); ++w) to += (uint32_t)part[w];
+    for (int i = 0; i < 16; ++i) {
+        const float x = s[i / 4][i % 4];
+        const int b = row.bucket(x);
+        if (b == bucket) mine |= 1u << i;
+        if (b < bucket && b < kBuckets - 1) kept[atomicAdd(&n_kept, 1u)] = x;
+    }
+    const uint32_t count = __builtin_popcount(mine), below = before_in_wave(count);
+    __syncthreads();
+    if ((tid & 63) == 63) part[tid >> 6] = below + count;
+    __syncthreads();
+    if (tid == 0) {
+        const uint32_t total = (uint32_t)(part[0] + part[1] + part[2] + part[3]);
+        at = total ? atomicAdd(&a.listed[number], total) : 0;               // a place for the workgroup's
+    }
+    __syncthreads();
+    uint32_t to = at + below;
+    for (int w = 0; w < (tid >> 6); ++w) to += (uint32_t)part[w];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (mine >> i & 1) {
-                if (to < (uint32_t)kListMost) a.list[(int64_t)number * kListMost + to] = place(s[i / 4][i % 4], chunk_number(c, i));
-                ++to;
-            }
-        const SampleEnd none(0);
-        uint64_t sum = 0;                                      // the weights of the kept alone, side by side
-        const uint32_t n = n_kept;
-        for (uint32_t i = tid; i < n; i += 256) sum += whole(kept_units(row, kept[i], 0, none));
-        __syncthreads();                                       // (part is read)
-        sum = sum_of_256(sum, part);
-        if (tid == 0) a.sums[(int64_t)number * a.chunks + c] = sum;
-    });
+    for (int i = 0; i < 16; ++i)
+        if (mine >> i & 1) {
+            if (to < (uint32_t)kListMost) a.list[(int64_t)number * kListMost + to] = place(s[i / 4][i % 4], chunk_number(c, i));
+            ++to;
+        }
+    const SampleEnd none(0);
+    uint64_t sum = 0;                                      // the weights of the kept alone, side by side
+    const uint32_t n = n_kept;
+    for (uint32_t i = tid; i < n; i += 256) sum += whole(kept_units(row, kept[i], 0, none));
+    __syncthreads();                                       // (part is read)
+    sum = sum_of_wave(sum);
+    if ((tid & 63) == 0) part[tid >> 6] = sum;
+    __syncthreads();
+    if (tid == 0) a.sums[(int64_t)number * a.chunks + c] = part[0] + part[1] + part[2] + part[3];
 }
 
 // Tokens of a bucket, in a list alone.
@@ -1143,14 +1148,20 @@ __global__ __launch_bounds__(1024) void sample_draw_kernel(const SampleDev a) {
     __shared__ uint64_t list[kListMost], own[kRankMost];
     __shared__ unsigned long long sums[kMaxChunks];
     const int tid = threadIdx.x;
-    if (a.others && blockIdx.x >= *a.n_others) return;
-    const int number = a.others ? (int)a.others[blockIdx.x] : (int)blockIdx.x;
+    const int number = blockIdx.x;
+    // (requested together: what a row does not have is not used)
+    const uint32_t done = a.done ? a.done[number] : 0, r = a.tokens ? draw_number(a.r[number]) : 0;
+    const uint64_t histogram = a.histogram[(int64_t)number * kBuckets + tid];
+    uint32_t listed = a.listed[number];
     const float m = max_of_row(a, number);
     const SampleRow row(a, number, m);
+    uint64_t of_chunks[kMaxChunks / 1024];
+#pragma unroll
+    for (int i = 0; i < kMaxChunks / 1024; ++i) of_chunks[i] = 1024 * i + tid < a.chunks ? a.sums[(int64_t)number * a.chunks + 1024 * i + tid] : 0;
+    if (done) return;
     const bool any = m > -__builtin_inff();
     const RowState state = any ? state_of(row) : ROW_WHOLE;
-    const uint32_t r = a.tokens ? draw_number(a.r[number]) : 0;
-    const uint32_t listed = state == ROW_CUT ? a.listed[number] : 0;
+    if (state != ROW_CUT) listed = 0;
     if (state == ROW_ALONE || listed > (uint32_t)kListMost) {
         const RowInMemory<VF> read{(const typename Elem<VF>::T *)a.logits + (int64_t)number * a.ld, a.vocab};
         const Kept kept = draw_alone(sh, row, read, a.vocab, list, own, r);
@@ -1163,14 +1174,11 @@ __global__ __launch_bounds__(1024) void sample_draw_kernel(const SampleDev a) {
     }
     uint64_t end = 0;
 #pragma unroll
-    for (int i = 0; i < kMaxChunks / 1024; ++i) {
-        const int c = 1024 * i + tid;
-        sums[c] = any && c < a.chunks ? a.sums[(int64_t)number * a.chunks + c] : 0;
-    }
+    for (int i = 0; i < kMaxChunks / 1024; ++i) sums[1024 * i + tid] = any ? of_chunks[i] : 0;
     if (state == ROW_CUT) {
         for (uint32_t i = tid; i < listed; i += 1024) list[i] = a.list[(int64_t)number * kListMost + i];
-        sh.counts[tid] = a.counts[(int64_t)number * kBuckets + tid];
-        const uint64_t u = sh.units[tid] = a.units[(int64_t)number * kBuckets + tid];
+        const uint64_t u = sh.units[tid] = row.k ? 0 : histogram;
+        sh.counts[tid] = row.k ? (uint32_t)histogram : 0;
         if (tid == 0) { sh.base_count = 0; sh.base_units = 0; sh.bin = kBuckets; }
         uint64_t all, target = (uint64_t)row.k;
         block_before(sh, u, &all);
@@ -1272,26 +1280,26 @@ __global__ __launch_bounds__(256) void sample_probs_kernel(const SampleDev a) {
     }
 }
 
-struct SamplePlaces { size_t maxes, groups, units, sums, counts, listed, others, n_others, ends, totals, list, bytes; };
+struct SamplePlaces { size_t maxes, groups, histogram, sums, listed, done, ends, totals, list, bytes; };
 static SamplePlaces sample_places(int64_t rows, int64_t chunks) {
     SamplePlaces p{};
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
-    p.units = take((size_t)rows * kBuckets * 8);
+    p.histogram = take((size_t)rows * kBuckets * 8);
     p.list = take((size_t)rows * kListMost * 8);
     p.sums = take((size_t)rows * chunks * 8);
     p.ends = take((size_t)rows * 8);
     p.totals = take((size_t)rows * 8);
-    p.counts = take((size_t)rows * kBuckets * 4);
     p.groups = take((size_t)rows * chunks * 256 * 4);
     p.maxes = take((size_t)rows * chunks * 4);
     p.listed = take((size_t)rows * 4);
-    p.others = take((size_t)rows * 4);
-    p.n_others = take(4);
+    p.done = take((size_t)rows * 4);
     p.bytes = at;
     return p;
 }
 static int32_t sample_chunks(int32_t vocab) { return (vocab + kChunk - 1) / kChunk; }       // (at most kMaxChunks)
+
+static int64_t first_workgroups(int64_t rows, int32_t chunks, bool few) { return rows * ((chunks + 3) / 4) + (few ? rows : 0); }   // of sample_few_kernel
 
 template <int VF>
 static void launch_sample(const SampleDev &d, hipStream_t st) {
@@ -1306,11 +1314,11 @@ static void launch_sample(const SampleDev &d, hipStream_t st) {
         return;
     }
     const int64_t chunks = (int64_t)d.rows * d.chunks;
-    const dim3 few(256), all((uint32_t)chunks), some((uint32_t)std::min<int64_t>(chunks, d.others ? 1024 : chunks));
+    const int64_t first = first_workgroups(d.rows, d.chunks, d.done);
+    const dim3 few(256), all((uint32_t)chunks);
     hipLaunchKernelGGL(sample_max_kernel<VF>, all, few, 0, st, d);
-    if (d.others) hipLaunchKernelGGL(sample_few_kernel<VF>, rows, block, 0, st, d);
-    hipLaunchKernelGGL(sample_histogram_kernel<VF>, some, few, 0, st, d);
-    if (d.top_k || d.top_p || d.temperature) hipLaunchKernelGGL(sample_bucket_kernel<VF>, some, few, 0, st, d);
+    hipLaunchKernelGGL(sample_few_kernel<VF>, dim3((uint32_t)first), block, 0, st, d);
+    if (d.top_k || d.top_p || d.temperature) hipLaunchKernelGGL(sample_bucket_kernel<VF>, all, few, 0, st, d);
     hipLaunchKernelGGL(sample_draw_kernel<VF>, rows, block, 0, st, d);
     if (d.probs) hipLaunchKernelGGL(sample_probs_kernel<VF>, all, few, 0, st, d);
 }
@@ -1343,15 +1351,15 @@ extern "C" int csb_sample(int32_t type, const void *d_logits, int64_t ld, const 
     d.chunks = sample_chunks(vocab);
     if (n_rows > 1 << 21 || (int64_t)n_rows * d.chunks > kMaxWorkgroups) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");
     if ((int64_t)vocab * type_size(type) > kRowMost) {
+        if (first_workgroups(n_rows, d.chunks, true) >= 1 << 22) return fail(CSB_EUNSUPPORTED, "more workgroups than a launch takes");     // (of 1024 threads)
         if (!d_ws) return fail(CSB_EINVAL, "NULL workspace");
         if ((uintptr_t)d_ws % 256) return fail(CSB_EINVAL, "workspace not 256-byte aligned");
         const SamplePlaces p = sample_places(n_rows, d.chunks);
         char *ws = (char *)d_ws;
-        d.units = (unsigned long long *)(ws + p.units); d.sums = (unsigned long long *)(ws + p.sums); d.list = (uint64_t *)(ws + p.list);
-        d.ends = (uint64_t *)(ws + p.ends); d.totals = (uint64_t *)(ws + p.totals); d.counts = (uint32_t *)(ws + p.counts);
+        d.histogram = (unsigned long long *)(ws + p.histogram); d.sums = (unsigned long long *)(ws + p.sums); d.list = (uint64_t *)(ws + p.list);
+        d.ends = (uint64_t *)(ws + p.ends); d.totals = (uint64_t *)(ws + p.totals);
         d.groups = (float *)(ws + p.groups); d.maxes = (float *)(ws + p.maxes); d.listed = (uint32_t *)(ws + p.listed);
-        d.n_others = (uint32_t *)(ws + p.n_others);
-        if (d_top_k || d_temperature) d.others = (uint32_t *)(ws + p.others);  // (a temperature of zero asks for one token)
+        if (d_top_k || d_temperature) d.done = (uint32_t *)(ws + p.done);  // (a temperature of zero asks for one token)
         try {
             static const char sample_user = 0;                 // this entry point as a user of workspaces
             workspace_changed_hands(d_ws, &sample_user);
