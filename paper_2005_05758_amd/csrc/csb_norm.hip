@@ -19,7 +19,7 @@ struct NormDev {
     const float *aw, *ab, *s, *bw, *bb;
     int64_t tokens, tiles;                     // tiles: of tokens, where lanes are tokens
     int32_t width, groups, after, before, sigmoid, gate_first;   // width: of a group
-    int32_t plain_gate, plain_scale;           // results are rounded to 16 bits; nothing is scaled
+    int32_t plain_gate, plain_scale, past;     // results are rounded to 16 bits; nothing is scaled; x and r go past the caches
     float scale;
     double eps, per;                           // per: 1 / width
 };
@@ -553,7 +553,10 @@ __global__ __launch_bounds__(1024) void block_norm_product_kernel(const NormDev 
                     const uint32_t from = at(a.x, sizeof(X), j0);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) run.v[j] = __builtin_bit_cast(X, window_load<X>(xw, from + j * x_step));
-                } else if (there > 0) run.v = load_any<typename Run8<VFX>::T8>(xp + j0);
+                } else if (there > 0) {
+                    if (a.past) run.v = __builtin_nontemporal_load((const typename Run8<VFX>::T8 *)(xp + j0));
+                    else run.v = load_any<typename Run8<VFX>::T8>(xp + j0);
+                }
             }
             norm_factors<true>(a.s, j0, a.width - j0, 1.0f, s);
             if (a.after) {
@@ -574,7 +577,10 @@ __global__ __launch_bounds__(1024) void block_norm_product_kernel(const NormDev 
                     const uint32_t to = at(a.r, sizeof(X), j0);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) window_store<X>(rw, to + j * r_step, run.v[j]);
-                } else if (there > 0) store_any(rp + j0, run.v);
+                } else if (there > 0) {
+                    if (a.past) __builtin_nontemporal_store(run.v, (typename Run8<VFX>::T8 *)(rp + j0));
+                    else store_any(rp + j0, run.v);
+                }
             }
         }
     if (!a.before) return;
@@ -633,6 +639,10 @@ static bool launch_norm_product(NormDev &d, hipStream_t st) {
 }
 template <int VFX, bool XCOLS, int VFN>
 static bool launch_norm_product(NormDev &d, hipStream_t st) {
+    // x and r row by row, read and written once, of more bytes than the L2 caches hold take the place of the columns' pieces there, which are put together from
+    // several workgroups' (2048 tokens of 8192 entries without norm_before 38 us, past the caches 30); smaller ones are found there by what comes next
+    const auto whole = [](const NormOperand &o) { return !o.d || ((uintptr_t)o.d % 16 == 0 && o.ld % 8 == 0); };
+    d.past = !XCOLS && d.tokens * d.width * (int64_t)sizeof(typename Elem<VFX>::T) >= 32 << 20 && whole(d.x) && whole(d.r);
     // tokens side by side: as many as leave every CU a workgroup, and as registers hold
     int tb = 1;
     while (tb < 16 && d.tokens > 256 * tb && (int64_t)d.width * tb * 2 <= 65536) tb *= 2;

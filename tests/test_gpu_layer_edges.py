@@ -115,3 +115,21 @@ def test_rows_of_one_token_and_one_entry():
         assert torch.equal(r, want_r) and torch.equal(n, want_n)
     w = torch.randn(64, 4, device="cuda")
     assert torch.equal(short_conv(x[2:3], w), short_conv(x[2:3].clone(), w))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_rows_that_go_past_the_caches(dtype):
+    """A norm between products of more than 32 MiB: what it leaves is what its halves, which are below that, leave."""
+    say("[edges] 4100 tokens of 4104 entries")
+    T, W = 4100, 4104
+    y, x = torch.randn(W, T, device="cuda"), torch.randn(T, W, device="cuda").to(dtype)
+    whole, halves = [], []
+    for into, parts in ((whole, [slice(0, T)]), (halves, [slice(0, T // 2), slice(T // 2, T)])):
+        r, n = torch.empty_like(x), torch.empty(W, T, device="cuda", dtype=dtype)
+        for p in parts:
+            block_norm(y[:, p].t(), x=x[p], before="rms", out=r[p], normed=n[:, p].t())
+        into += [r, n]
+    # sums of another order are 2^-50 off: results are the same number, or one of two neighbours where they lie between them
+    assert torch.equal(whole[0], halves[0])
+    off = (whole[1].float() - halves[1].float()).abs()
+    assert (off <= torch.finfo(dtype).eps * halves[1].float().abs()).all() and int((off > 0).sum()) <= T * W // 10000
