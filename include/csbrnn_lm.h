@@ -274,7 +274,7 @@ int csb_block_norm(const csb_norm_args *args, void *stream);
  * tokens that are not kept; what csb_verify_drafts takes as p and q.  With d_tokens NULL (d_r may be too) only that is made.  It may be the
  * logits themselves (same pointer and leading dimension), and must not overlap them otherwise.  Whole units: the result depends neither on the order nor on the split of a sum.
  * d_ws: csb_sample_workspace_bytes(n_rows, vocab) bytes (0 up to a vocabulary of 24576: d_ws may be NULL then).  One launch where a row has up to 98304
- * bytes, else three to six.
+ * bytes, else three to five.
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, an unknown type -> CSB_EINVAL; vocab > 2^24, n_rows > 2^21, or
  * more workgroups than a launch takes -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.  n_rows = 0 does nothing.
  */

@@ -10,9 +10,13 @@
 // (A place is the logit's bits and the token's number in 64 bits, so places differ and ties need no care.)  Tokens of the last bucket have no whole unit:
 // they are counted nowhere, and cannot be drawn.  Exponentials are binary64, which this card does as fast as binary32.
 //
-// Rows of up to kRowMost bytes: one launch, a workgroup a row, which it holds in LDS.  Others, in chunks of 4096 tokens: maxima of groups; few; of the other
-// rows the histogram (where nothing is cut: units of the chunks), the bucket's tokens and the units before it by chunk, the end of what is kept and the
-// draw; the distribution, if it is asked for.
+// Rows of up to kRowMost bytes: one launch, a workgroup a row, which it holds in LDS; what is kept goes into a list there if it fits, else its units stay in registers, so
+// that the row is passed over twice or three times and no more (165 rows of 32003 bfloat16 tokens, top-p and their distributions, 40 us; by the kernels for larger rows
+// 56).  Others, in chunks of 4096 tokens: maxima of groups; few, and beside them the histogram of the other rows (where nothing is cut: units of the chunks); the
+// bucket's tokens and the units before it by chunk; the end of what is kept and the draw; the distribution, if it is asked for.  (64 rows of 131071 binary32
+// tokens, four rows in five few: 44 us; all by histograms, or alone where two cuts are asked for: 135.)
+// Bound by the issue of vector instructions where all of a row counts (36 a token and pass, 22 of them for the exponential), else by latencies: each launch is a chain of
+// trips to memory and of barriers.
 #include <algorithm>
 #include <new>
 #include <type_traits>

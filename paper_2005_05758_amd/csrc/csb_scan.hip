@@ -1,9 +1,10 @@
 // The selective state space scan (csb_selective_scan).
 //
 // Per channel c, with a state h of n numbers: h[j] <- exp(s A[j]) h[j] + s x B[j], y = sum_j C[j] h[j] + D x.  The issue of vector instructions binds: an
-// exponential (4 slots), two products and two fused ones a (token, channel, number).  (s x B is a product of a number of the channel's and one of the group's:
-// matrix instructions of 4 x 4 numbers made it and its sum with the decayed state in binary32, but each token waited for its own: 632 us instead of 548
-// on 16384 tokens of 4096 channels.)
+// exponential (8.4 clocks of a SIMD), two products (2.4) and two fused ones (4.2) a (token, channel, number), and 45 instructions a (token, channel) around them: 16384
+// tokens of 4096 channels of 16 numbers take 433 us, the card's SIMDs busy all the time.  (s x B is a product of a number of the channel's and one of the
+// group's: matrix instructions of 4 x 4 numbers made it and its sum with the decayed state in binary32, but each token waited for its own, 632 us instead of
+// the 548 that it took then.)
 // A channel's numbers lie with four lanes, K each, in registers from the first token to the last; a workgroup has 64 channels of one group, whose B and C come
 // through LDS once for all of them.  What is a token's and channel's alone (its step s through softplus, s x, the gate, types) is made once by
 // the lanes together, eight channels of a token each, and handed over through LDS; outputs come back in the same places.
@@ -20,7 +21,8 @@ namespace csb {
 
 constexpr int kScanTile = 32, kScanCols = 64, kScanRow = 2 * kScanCols + 32;      // tokens and channels in LDS; floats of a token's row there
 constexpr int kScanMany = 1024;                // workgroups that are enough for the card
-constexpr int kScanFew = 8;                    // tokens a sequence, on average, up to which wavefronts work alone
+// Tokens a sequence, on average, up to which wavefronts work alone: 64 sequences of 4096 channels, 8 tokens each: 21 us, 33 in tiles; 16: 31 and 37; 32: 51 and 46.
+constexpr int kScanFew = 16;
 
 struct ScanDev {
     const void *x, *dt, *z, *B, *C;
@@ -253,7 +255,7 @@ template <int N> __device__ __forceinline__ float quad_xor(float v) {
 
 // The same for the few tokens of a decoding step: P lanes a channel, K numbers each, a wavefront 64 / P channels by itself, without LDS and barriers.
 // The next token's operands are on their way while one is worked on.  (Four lanes a channel, as above, make its step and gate four times: 64
-// requests of one token, 4096 channels of 16 numbers, 14 us instead of 10.)
+// requests of one token, 4096 channels of 16 numbers, 13.8 us instead of 11.9.)
 template <int VF, int K, int P, bool FULL>
 __global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a, const uint32_t waves) {
     using T = typename Elem<VF>::T;
@@ -345,8 +347,8 @@ __global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a
 
 // Chunks of a call, as a power of two of tokens (31: whole sequences).  Sequences and channels that give every CU four workgroups are not split (a split costs
 // the chunks' own states beside the outputs: twice the exponentials).  Others are, as finely as makes that many, but no finer than 128 chunks
-// a sequence, whose states every later chunk combines (16384 tokens of 64 channels in 512 chunks 93 us, in 128 56), and no coarser than 512 tokens
-// (16384 tokens of 4096 channels in 16 chunks 519 us, in 32 492).
+// a sequence, whose states every later chunk combines (16384 tokens of 64 channels in 512 chunks 86 us, in 128 52), and no coarser than 512 tokens
+// (16384 tokens of 4096 channels in 16 chunks 465 us, in 32 439).
 static int scan_shift(const csb_scan_args *a, int64_t col_tiles) {
     const int64_t mean = a->n_tokens / a->n_seq, tiles = a->n_seq * col_tiles;
     if (tiles >= kScanMany || mean < 2 * kScanTile) return 31;
