@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import test_gpu_sample as samples
+import test_gpu_scan as scans
 from paper_2005_05758_amd import block_norm, selective_scan, short_conv
 
 pytestmark = pytest.mark.gpu
@@ -133,3 +134,44 @@ def test_rows_that_go_past_the_caches(dtype):
     assert torch.equal(whole[0], halves[0])
     off = (whole[1].float() - halves[1].float()).abs()
     assert (off <= torch.finfo(dtype).eps * halves[1].float().abs()).all() and int((off > 0).sum()) <= T * W // 10000
+
+
+def odd_views(dev):
+    """Rows of tokens at odd strides, from the second element of a buffer on."""
+    out = []
+    for v in dev:
+        if v is None or v.dim() < 2 or v is dev[2]:     # (A is whole)
+            out.append(v)
+            continue
+        width = v[0].numel()
+        buf = torch.zeros(v.shape[0] * (width + 7) + 8, dtype=v.dtype, device="cuda")
+        rows = buf[1:1 + v.shape[0] * (width + 7)].view(v.shape[0], width + 7)[:, :width]
+        rows.copy_(v.reshape(v.shape[0], width))
+        out.append(rows if v.dim() == 2 else rows.unflatten(1, tuple(v.shape[1:])))
+    return out
+
+
+@pytest.mark.parametrize("fmt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("place", [None, odd_views])
+def test_scans_of_whole_tiles_of_channels(fmt, place):
+    """64 channels of a group and all of their numbers: chunks of one tile, of several, whole sequences of several tiles, and what is left of them."""
+    scans.check(fmt, 700, 192, 1, 16, seed=41, place=place)
+    scans.check(fmt, 4200, 64, 1, 16, lengths=[4197], seed=42, place=place)
+    scans.check(fmt, 300, 128, 2, 64, lengths=[150, 33, 64, 1, 20, 32], seed=43, place=place, softplus=False, without=(6,))
+    lengths = [40, 64, 97, 33, 32, 31, 0, 128, 70] * 3
+    scans.check(fmt, sum(lengths), 64 * 40, 1, 16, lengths=lengths, lens=[n - (n > 50) for n in lengths], seed=44, place=place)
+
+
+@pytest.mark.parametrize("fmt,V", [("f32", 24576), ("f32", 24577), ("bf16", 49152), ("bf16", 49153), ("f16", 4096), ("f32", 8193), ("bf16", 16385)])
+def test_rows_of_which_much_is_kept(fmt, V):
+    """Flat and even rows, whose kept tokens fit into no list, at the sizes where the forms change."""
+    t = torch.Generator().manual_seed(V)
+    r = torch.tensor([0.0, 0.3, 0.999, 0.5, 0.7, 1 - 2.0 ** -24])
+    flat = (0.5 * torch.randn(6, V, generator=t)).to(samples.TYPES[fmt])
+    flat[4] = 1.25                                       # all equal
+    flat[5, ::2] = -math.inf
+    samples.check(flat, r)
+    samples.check(flat, r, top_p=[0.9, 0.999, 0.5, 0.01, 0.6, 0.97])
+    samples.check(flat, r, top_k=[V - 1, 5000, 4096, 4097, 2000, V // 2 - 3])
+    samples.check(flat, r, top_k=[V // 2, 3000, 300, 257, 256, 0], top_p=[0.99, 0.9, 0.8, 0.5, 0.3, 1.5], min_p=[0.01, 0.1, 0.3, 0.0, 0.5, 0.2], temperature=[0.3, 0.5, 1.0, 2.0, 1.0, 0.7])
+    samples.check(flat, r, min_p=[0.01, 0.1, 0.3, 0.9, 1.0, 0.2])
