@@ -371,7 +371,7 @@ static Refusal scan_plan(const csb_scan_args *a, ScanPlan *p) {
     if (a->n_seq == 0) return {CSB_OK, nullptr};
     p->few = a->n_tokens / a->n_seq <= kScanFew;
     const int cols = p->few ? 64 / scan_lanes(a->n) : kScanCols;
-    p->group_tiles = (a->channels / a->groups + cols - 1) / cols;
+    p->group_tiles = (int32_t)(((int64_t)a->channels / a->groups + cols - 1) / cols);      // (32 bits do not hold cols more than the most channels)
     p->col_tiles = (int64_t)p->group_tiles * a->groups;
     p->shift = p->few ? 31 : scan_shift(a, p->col_tiles);
     p->tiles = p->few ? a->n_seq : tile_numbers(a->n_tokens, a->n_seq, p->shift);
