@@ -188,7 +188,8 @@ int csb_short_conv(const csb_conv_args *args, void *stream);
  * split into chunks (by n_tokens, n_seq, channels and n alone): the chunks' own states first, then outputs from what the chunks before leave,
  * in two launches; else one launch.  Bitwise reproducible.
  * What is not finite stays in its channel (in B or C: its group's) from its token on; it is infinite or NaN there.  Products s A are expected at or below
- * zero: a chunk over which a state would grow by 2^128 counts as infinite growth.
+ * zero: a chunk over which a state would grow by 2^128 counts as infinite growth.  Decays from -2.3e38 down, -infinity among them, count as the lowest numbers: with a
+ * step of zero the state stays as it is, with others of 1e-36 and more nothing is left of it.
  * d_ws: csb_scan_workspace_bytes(args) bytes (channels, groups, n, n_seq and n_tokens are read; 0 where there is one launch or a
  * refusal: d_ws may be NULL then).
  * Few tokens, chunks or neither is decided by the mean length of a call's sequences, which is all that the host knows: a few long prompts take longer

@@ -36,6 +36,13 @@ struct ScanDev {
     int32_t channels, per_group, n, n_seq, n_states, softplus, shift, group_tiles, col_tiles;
 };
 
+// A decay as the exponentials of base 2 take it.  From -2.36e38 down, -infinity among them, it counts as the lowest number: steps of zero, which the places behind a
+// sequence's end have too, keep the state then (their products with -infinity would be NaN).
+__device__ __forceinline__ float decay_of(float A) {
+    const float d = A * 1.44269502162933349609375f;
+    return d < -0x1.fffffep127f ? -0x1.fffffep127f : d;        // (NaN stays)
+}
+
 // Lane q 16 + c gets the sum over the lanes c, 16 + c, 32 + c, 48 + c of y[q].
 __device__ __forceinline__ float sum_of_rows(const float *y) {
     const auto even = [](float a, float b) {
@@ -80,7 +87,7 @@ __global__ __launch_bounds__(256) void selective_scan_kernel(const ScanDev a) {
     float A[K], h[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        A[k] = have(k) ? a.A[channel * a.n + j0 + k] * 1.44269502162933349609375f : 0.0f;
+        A[k] = have(k) ? decay_of(a.A[channel * a.n + j0 + k]) : 0.0f;
         h[k] = 0.0f;
     }
     auto get = [&](const float *p) {
@@ -312,7 +319,7 @@ __global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a
     numbers(a.A + channel * a.n + j0, A);
     const float bias = a.bias ? a.bias[channel] : 0.0f, D = a.D ? a.D[channel] : 0.0f;
 #pragma unroll
-    for (int k = 0; k < K; ++k) A[k] *= 1.44269502162933349609375f;
+    for (int k = 0; k < K; ++k) A[k] = decay_of(A[k]);
     for (int64_t t = first; t < end; ++t) {
         if (t + 1 < end) load(t + 1, next);
         const float x = (float)now.x;
