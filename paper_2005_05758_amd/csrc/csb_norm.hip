@@ -314,6 +314,7 @@ struct RowNorm {
         double y = __builtin_amdgcn_rsq(e);                    // two steps of Newton's: all digits of binary32, and more
         y = y * __builtin_fma(-0.5 * e * y, y, 1.5);
         y = y * __builtin_fma(-0.5 * e * y, y, 1.5);
+        y = e == __builtin_inf() ? 0.0 : y;                    // (a step makes NaN of it: zero times infinity)
         const bool large = e > 0x1p150;                        // a factor below binary32's normal numbers: in two parts
         one = large ? 0x1p-80f : 1.0f;
         factor = (float)(large ? y * 0x1p80 : y);
