@@ -233,7 +233,7 @@ int csb_selective_scan(const csb_scan_args *args, void *d_ws, void *stream);
  * norm_before is that of r before its rounding.  An output may be an input itself (same pointer, type, order and ld), and must not overlap one
  * otherwise.  Products and sums are binary32, a norm's sums binary64: entries of any finite size have their norm.  What is not finite in
  * a token's entries stays in that token (in its group where there are several): beside infinite entries CSB_NORM_RMS leaves zeros (times w, and b) of the finite ones and
- * NaN of them.
+ * NaN of them, CSB_NORM_MEAN NaN of all.
  * Errors: NULL, sizes, types or leading dimensions out of range, eps below zero or not finite, width no multiple of groups, a gate or norm_after without y, norms or gates
  * unknown, an output at the address of an input of another type, order or ld -> CSB_EINVAL; width / groups > 32768, norm_before with several groups, or more workgroups than a launch takes -> CSB_EUNSUPPORTED; launch failure ->
  * CSB_EDEVICE.  n_tokens = 0 does nothing.  Bitwise reproducible, one launch, no workspace.

@@ -306,9 +306,8 @@ struct RowNorm {
         double square = q * per;
         if (kind == CSB_NORM_MEAN) {
             mean = p * per;
-            square = __builtin_fmax(square - mean * mean, 0.0);
+            square = __builtin_fmax(square - mean * mean, 0.0) + (p - p);        // (NaN where a sum is not finite: a maximum drops it)
             mean += shift;
-            if (p != p) square = p;
         }
         const double e = square + eps;
         double y = __builtin_amdgcn_rsq(e);                    // two steps of Newton's: all digits of binary32, and more

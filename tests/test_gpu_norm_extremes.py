@@ -75,3 +75,16 @@ def test_nan_and_a_mean_square(form, W, fmt):
     assert bool(torch.isnan(r[3]).all()) and bool(torch.isnan(n[[3, 14]]).all()) and int(torch.isnan(r[14]).sum()) == 1
     rest = [t for t in range(T) if t not in (3, 14)]
     assert bool(torch.isfinite(r[rest]).all()) and bool(torch.isfinite(n[rest]).all())
+
+
+@pytest.mark.parametrize("fmt", sorted(TYPES))
+@forms
+def test_entries_that_are_not_finite_and_a_mean(form, W, fmt):
+    """A token whose mean is not finite has no norm: all of its entries are NaN, wherever the one that spoils it lies."""
+    for value in (math.inf, -math.inf, math.nan):
+        y, x, factors = operands(form, W, fmt)
+        y[3, W // 2], y[9, 0], x[14, W - 1], x[17, 0], y[20, 1], y[20, W - 2] = value, value, value, value, value, -value
+        r, n = run(form, y, x, factors, "mean", "mean")
+        assert bool(torch.isnan(r[[3, 9, 20]]).all()) and bool(torch.isnan(n[[3, 9, 14, 17, 20]]).all())
+        rest = [t for t in range(T) if t not in (3, 9, 14, 17, 20)]
+        assert bool(torch.isfinite(r[rest]).all()) and bool(torch.isfinite(n[rest]).all())
