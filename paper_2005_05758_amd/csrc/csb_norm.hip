@@ -287,7 +287,7 @@ struct RowNorm {
                 sum = fmaf(v[j], v[j], sum);
             }
             const bool fine = most == 0.0f ? sum == 0.0f : most > 0x1p-50f && most < 0x1p60f;
-            if (__builtin_expect(__all(fine), 1)) { q += sum; return; }
+            if (__builtin_expect(fine, 1)) { q += sum; return; }       // (each lane as if alone: a token does not depend on others of its wavefront)
         }
         auto one_more = [&](float x) {
             const double d = (double)x - shift;
@@ -313,10 +313,12 @@ struct RowNorm {
         double y = __builtin_amdgcn_rsq(e);                    // two steps of Newton's: all digits of binary32, and more
         y = y * __builtin_fma(-0.5 * e * y, y, 1.5);
         y = y * __builtin_fma(-0.5 * e * y, y, 1.5);
-        y = e == __builtin_inf() ? 0.0 : y;                    // (a step makes NaN of it: zero times infinity)
-        const bool large = e > 0x1p150;                        // a factor below binary32's normal numbers: in two parts
-        one = large ? 0x1p-80f : 1.0f;
-        factor = (float)(large ? y * 0x1p80 : y);
+        one = 1.0f;
+        if (__builtin_expect(e > 0x1p150, 0)) {                // a factor below binary32's normal numbers: in two parts
+            one = 0x1p-80f;
+            y = e == __builtin_inf() ? 0.0 : y * 0x1p80;       // (of zero a step makes NaN: infinity times it)
+        }
+        factor = (float)y;
     }
     // eight entries (without the branch where the loads of many runs are to be in flight beside it)
     __device__ __forceinline__ float of(int kind, float v) const { return (kind == CSB_NORM_MEAN ? (float)(((double)v - mean) * one) : v * one) * factor; }

@@ -1,4 +1,5 @@
-"""Norms of entries that are not finite: what the definition gives for the other entries of their token."""
+"""Norms of entries that are not finite, or far outside of the others' size: what the definition gives for the other entries of their token, and the same bits for
+every other token."""
 import math
 
 import numpy as np
@@ -88,3 +89,19 @@ def test_entries_that_are_not_finite_and_a_mean(form, W, fmt):
         assert bool(torch.isnan(r[[3, 9, 20]]).all()) and bool(torch.isnan(n[[3, 9, 14, 17, 20]]).all())
         rest = [t for t in range(T) if t not in (3, 9, 14, 17, 20)]
         assert bool(torch.isfinite(r[rest]).all()) and bool(torch.isfinite(n[rest]).all())
+
+
+@forms
+@pytest.mark.parametrize("kind", ["rms", "mean"])
+def test_other_tokens_keep_their_bits(form, W, kind):
+    """Next to tokens with infinities, NaN, entries whose squares leave binary32, and entries that are all but nothing."""
+    y, x, factors = operands(form, W, "f32", seed=1, tokens=600)       # (more tokens side by side in a wavefront than of 24)
+    clean = run(form, y, x, factors, kind, kind)
+    values = [math.inf, math.nan, 1e25, 1e-25, -math.inf, 3e38, 1e-38]
+    spoiled = list(range(3, 600, 19))
+    for t in spoiled:
+        y[t], x[t] = values[t % 7], -values[t % 7]
+    got = run(form, y, x, factors, kind, kind)
+    rest = [t for t in range(600) if t not in spoiled]
+    for a, b in zip(got, clean):
+        assert torch.equal(a[rest], b[rest])
