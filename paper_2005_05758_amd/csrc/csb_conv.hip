@@ -5,6 +5,7 @@
 // bfloat16 channels, width 4: 61 us, 4.4 TB/s).  A thread has eight channels (their W weights in registers) and walks down kConvRun tokens with the last W - 1
 // inputs in registers, kConvAhead tokens requested together (one by one that call took 97 us, four together 80; the weights in 16-byte words and runs of 32 tokens
 // took it to 66).  The first tile of a sequence also makes its new state: it alone reads the old one, so a state may be replaced in place while later tiles run.
+#include <algorithm>
 #include <type_traits>
 
 #include "csb_layer.hpp"
@@ -169,8 +170,9 @@ extern "C" int csb_short_conv(const csb_conv_args *a, void *stream) {
     const int64_t runs = ((int64_t)a->channels + 7) / 8;       // of eight channels
     d.lanes = 64;
     while (d.lanes > 1 && d.lanes / 2 >= runs) d.lanes /= 2;
-    // rows of threads on runs of tokens one behind the other: a wavefront where a sequence has no more than a run on average
-    const int rows = a->n_tokens / a->n_seq <= kConvRun ? 64 / d.lanes : 256 / 64;
+    // rows of threads on runs of tokens one behind the other: four, or one where a sequence has no more than a run on average, and a wavefront at least (the
+    // workgroup looks for its sequence with all of its threads: 4096 sequences of 64 tokens, 8 channels, 64 us, by four threads 500)
+    const int rows = std::max(64 / d.lanes, a->n_tokens / a->n_seq <= kConvRun ? 1 : 4);
     d.col_tiles = (int32_t)((runs + d.lanes - 1) / d.lanes);
     d.shift = 0;
     while ((1 << d.shift) < rows * kConvRun) ++d.shift;
