@@ -182,18 +182,20 @@ int csb_short_conv(const csb_conv_args *args, void *stream);
  *     h[j] <- exp(s A[c][j]) h[j] + s x[t, c] B[t, group, j];   y = sum_j C[t, group, j] h[j] + D[c] x[t, c];
  *     out[t, c] = y, or y z[t, c] / (1 + e^-z[t, c]) where d_z is given.
  * Element (t, c) of x, dt, z and out is at t * ld + c, (t, group, j) of B and C at t * ld + group * n + j, all of `type`; A [channels][n],
- * D and dt_bias [channels] (NULL: zeros) and states are binary32, and so is everything computed; `out` is rounded once.  It may be x,
+ * D and dt_bias [channels] (NULL: zeros) and states are binary32, and so is everything computed; `out` is rounded once.  A step through softplus is off by 12 units of 2^-24 of
+ * itself (with 16-bit operands by 1.25 |dt + dt_bias| more below zero), which states keep.  `out` may be x,
  * dt or z themselves (the same pointer and leading dimension); it must not overlap them otherwise, nor B and C.
  * Sequences, slots and states ([n_states][channels][n]) are as with the delta rule.  Long sequences are
- * split into chunks (by n_tokens, n_seq, channels and n alone): the chunks' own states first, then outputs from what the chunks before leave,
- * in two launches; else one launch.  Bitwise reproducible.
+ * split into chunks: the chunks' own states first, then outputs from what the chunks before leave, in two launches; else one launch.  Whether and how goes by n_tokens, n_seq,
+ * channels and n of the call, so a sequence's last bits depend on how many others, and how long ones, share its call.  The same call is bitwise reproducible.
  * What is not finite stays in its channel (in B or C: its group's) from its token on; it is infinite or NaN there.  Products s A are expected at or below
- * zero: a chunk over which a state would grow by 2^128 counts as infinite growth.  Decays from -2.3e38 down, -infinity among them, count as the lowest numbers: with a
+ * zero: a chunk over which a state would grow by 2^128 counts as infinite growth.  Decays from -2.36e38 down, -infinity among them, count as the lowest numbers: with a
  * step of zero the state stays as it is, with others of 1e-36 and more nothing is left of it.
  * d_ws: csb_scan_workspace_bytes(args) bytes (channels, groups, n, n_seq and n_tokens are read; 0 where there is one launch or a
  * refusal: d_ws may be NULL then).
  * Few tokens, chunks or neither is decided by the mean length of a call's sequences, which is all that the host knows: a few long prompts take longer
- * in one call with many single tokens than in a call of their own.
+ * in one call with many single tokens than in a call of their own (4096 channels, n = 16, bfloat16: a prompt of 2048 tokens among 255 single ones 1900 us, the two apart 76 and 34;
+ * one of 8192 among 47 of 100, which are not split for it, 1050, apart 246 and 99).
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, channels no multiple of groups, n_tokens no
  * multiple of n_seq without d_start, out at the address of B, C or of an x, dt, z with another leading dimension, an unknown type -> CSB_EINVAL; n > 128, n_tokens above 2^31 - 1,
  * or more workgroups than a launch takes -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.  n_seq = 0 does nothing.
@@ -272,11 +274,11 @@ int csb_block_norm(const csb_norm_args *args, void *stream);
  *     of these, the ones of at least floor(min(q, 1) 2^38) units, q = d_min_p[i] (NULL, or q not above 0: all).
  * Token d_tokens[i] is drawn from what is kept by inversion, as csb_verify_drafts does: the lowest whose cumulated units, by number,
  * exceed floor(units of the row * floor(r 2^24) / 2^24), r = d_r[i] in [0, 1) given by the caller; -1 where every logit is -infinity or NaN.
- * d_probs (NULL: not wanted): row i of the distribution drawn from, at d_probs + i * ldprobs, of `type`: units over the row's units, rounded once, zero for
+ * d_probs (NULL: not wanted): row i of the distribution drawn from, at d_probs + i * ldprobs, of `type`: units over the row's units, rounded to binary32 and that to `type`, zero for
  * tokens that are not kept; what csb_verify_drafts takes as p and q.  With d_tokens NULL (d_r may be too) only that is made.  It may be the
  * logits themselves (same pointer and leading dimension), and must not overlap them otherwise.  Whole units: the result depends neither on the order nor on the split of a sum.
  * d_ws: csb_sample_workspace_bytes(n_rows, vocab) bytes (0 up to a vocabulary of 24576: d_ws may be NULL then).  One launch where a row has up to 98304
- * bytes, else three to five.
+ * bytes, which needs no workspace either (d_ws may be NULL for 16-bit logits up to a vocabulary of 49152), else three to five.
  * Errors: NULL (the optional pointers excepted), sizes or leading dimensions out of range, an unknown type -> CSB_EINVAL; vocab > 2^24, n_rows > 2^21, or
  * more workgroups than a launch takes -> CSB_EUNSUPPORTED; launch failure -> CSB_EDEVICE.  n_rows = 0 does nothing.
  */

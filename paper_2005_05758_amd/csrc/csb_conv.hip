@@ -2,9 +2,9 @@
 // the inputs before a sequence's first token from its state.
 //
 // Bound by HBM: every input is read once, every output written once; the W - 1 inputs before a tile come from the caches (48 packed prompts, 16411 tokens of 4096
-// bfloat16 channels, width 4: 61 us, 4.4 TB/s).  A thread has eight channels (their W weights in registers) and walks down kConvRun tokens with the last W - 1
+// bfloat16 channels, width 4: 62 us, 4.3 TB/s; a call among others 68).  A thread has eight channels (their W weights in registers) and walks down kConvRun tokens with the last W - 1
 // inputs in registers, kConvAhead tokens requested together (one by one that call took 97 us, four together 80; the weights in 16-byte words and runs of 32 tokens
-// took it to 66).  The first tile of a sequence also makes its new state: it alone reads the old one, so a state may be replaced in place while later tiles run.
+// took it to 68).  The first tile of a sequence also makes its new state: it alone reads the old one, so a state may be replaced in place while later tiles run.
 #include <algorithm>
 #include <type_traits>
 

@@ -64,8 +64,9 @@ template <int VF> __device__ __forceinline__ float sigmoid_for(float x) {
 template <int VF> __device__ __forceinline__ float silu(float x) { return x * sigmoid_for<VF>(x); }
 
 // ln(1 + e^x) = max(x, 0) + ln(1 + e), e = e^-|x| in (0, 1]: 2 atanh(s), s = e / (2 + e), as 2 s (1 + w p(w)), w = s^2 <= 1/9, p through five of Chebyshev's points
-// (2^-29): small steps keep all of their digits, which ln(1 + e) of a rounded sum would not.  From 16 bits, whose rounding of x is 2^12 times as much and
-// more, the argument of the exponential is rounded once (1.25 |x| units of 2^-24 of the result): 17 instructions' time instead of 24.
+// (2^-29): small steps keep all of their digits, which ln(1 + e) of a rounded sum would not.  From 16 bits the argument of the
+// exponential is rounded once, 17 instructions' time instead of 24: 1.25 |x| units of 2^-24 of the result more (x below zero), a 2^12th and less of what the rounding of a 16-bit
+// number as large as x makes.  States, which are binary32, keep that.
 template <int VF> __device__ __forceinline__ float softplus_from(float x) {
     constexpr bool SHORT = VF != CSB_VAL_F32;
     const float e = SHORT ? __builtin_amdgcn_exp2f(fabsf(x) * -1.44269502162933349609375f) : exp_within(-fabsf(x));

@@ -4,7 +4,7 @@
 // group of one), NV runs of eight entries each.  Where all operands are row by row a row's lanes are neighbours; where one is column by column
 // (a product's operand) neighbouring lanes are neighbouring tokens, eight of them, so that columns are read and written 16 or 32
 // bytes at a time, and the workgroups of neighbouring tokens share an XCD, whose L2 puts these pieces together: their number bounds those calls.
-// (16411 tokens of 16 heads of 128, gated, binary16, row by row: 44 us, 4.6 TB/s; 2048 tokens of 8192 entries between products: 55, of which 24 are the
+// (16411 tokens of 16 heads of 128, gated, binary16, row by row: 45 us, 4.5 TB/s; 2048 tokens of 8192 entries between products: 58, of which 24 are the
 // 33 MB that are written 16 bytes at a time.)
 //
 // Sums are binary64, as fast here as binary32: entries of 1e20 have squares there, and the variance may be taken from sums of v - v[0] and its
@@ -643,11 +643,13 @@ static bool launch_norm_product(NormDev &d, hipStream_t st) {
 }
 template <int VFX, bool XCOLS, int VFN>
 static bool launch_norm_product(NormDev &d, hipStream_t st) {
-    // x and r row by row, read and written once, of more bytes than the L2 caches hold take the place of the columns' pieces there, which are put together from
-    // several workgroups' (2048 tokens of 8192 entries without norm_before 38 us, past the caches 30); smaller ones are found there by what comes next
+    // x and r row by row, read and written once, of as many bytes as the L2 caches hold (32 MiB) and more take the place of the columns' pieces there, which are put together
+    // from several workgroups'; smaller ones are found there by what comes next.  Through the caches and past them, operands of 16 bits that change from call to call:
+    // 1024 tokens of 8192 entries 31 and 32 us, 4096 of 4088 51 and 55, 4096 of 4096 51 and 50, 2048 of 8192 60 and 56 (without norm_before 44 and 33), 2560 99 and 96 (73 and 51).
+    // (The other way round for the same operands again and again, 2048 of 8192 39 and 46; tall ones of 24 MiB gain already, 1536 of 8192 52 and 42.)
     const auto whole = [](const NormOperand &o) { return !o.d || ((uintptr_t)o.d % 16 == 0 && o.ld % 8 == 0); };
     d.past = !XCOLS && d.tokens * d.width * (int64_t)sizeof(typename Elem<VFX>::T) >= 32 << 20 && whole(d.x) && whole(d.r);
-    // tokens side by side: as many as leave every CU a workgroup, and as registers hold (2048 tokens of 8192 entries by eights 56 us, by fours 79; by the kernel for any operands 100)
+    // tokens side by side: as many as leave every CU a workgroup, and as registers hold (2048 tokens of 8192 entries by eights 58 us, by fours 79; of 8191 by the kernel for any operands 107)
     int tb = 1;
     while (tb < 16 && d.tokens > 256 * tb && (int64_t)d.width * tb * 2 <= 65536) tb *= 2;
     switch (tb) {
@@ -717,7 +719,7 @@ extern "C" int csb_block_norm(const csb_norm_args *a, void *stream) {
         if (kind != CSB_NORM_NONE && kind != CSB_NORM_RMS && kind != CSB_NORM_MEAN) return fail(CSB_EINVAL, "unknown norm");
     if (a->gate_kind != CSB_GATE_SILU && a->gate_kind != CSB_GATE_SIGMOID) return fail(CSB_EINVAL, "unknown gate");
     if (!(a->eps >= 0.0f && a->eps <= 0x1.fffffep127f)) return fail(CSB_EINVAL, "eps below zero or not finite");
-    if (a->width / a->groups > 32768) return fail(CSB_EUNSUPPORTED, "more than 32768 entries under one norm (a row stays in a workgroup's registers)");
+    if (a->width / a->groups > 32768) return fail(CSB_EUNSUPPORTED, "more than 32768 entries under one norm");
     if (a->before && a->groups > 1) return fail(CSB_EUNSUPPORTED, "norm_before with several groups");
     if (a->n_tokens == 0) return CSB_OK;
     if (!a->y.d && !a->x.d) return fail(CSB_EINVAL, "NULL pointer: neither y nor x");

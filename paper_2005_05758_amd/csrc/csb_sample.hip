@@ -11,10 +11,10 @@
 // they are counted nowhere, and cannot be drawn.  Exponentials are binary64, which this card does as fast as binary32.
 //
 // Rows of up to kRowMost bytes: one launch, a workgroup a row, which it holds in LDS; what is kept goes into a list there if it fits, else its units stay in registers, so
-// that the row is passed over twice or three times and no more (165 rows of 32003 bfloat16 tokens, top-p and their distributions, 40 us; by the kernels for larger rows
+// that the row is passed over twice or three times and no more (165 rows of 32003 bfloat16 tokens, top-p and their distributions, 38 us; by the kernels for larger rows
 // 56).  Others, in chunks of 4096 tokens: maxima of groups; few, and beside them the histogram of the other rows (where nothing is cut: units of the chunks); the
 // bucket's tokens and the units before it by chunk; the end of what is kept and the draw; the distribution, if it is asked for.  (64 rows of 131071 binary32
-// tokens, four rows in five few: 44 us; all by histograms, or alone where two cuts are asked for: 135.)
+// tokens, four rows in five few: 43 us; all few, k of 40, 23; by histograms, k of 1000, 45, top-p of 0.9 61; alone, both of these, 126; nothing cut 31.)
 // Bound by the issue of vector instructions where all of a row counts (36 a token and pass, 22 of them for the exponential), else by latencies: each launch is a chain of
 // trips to memory and of barriers.
 #include <algorithm>

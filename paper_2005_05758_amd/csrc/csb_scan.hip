@@ -2,7 +2,7 @@
 //
 // Per channel c, with a state h of n numbers: h[j] <- exp(s A[j]) h[j] + s x B[j], y = sum_j C[j] h[j] + D x.  The issue of vector instructions binds: an
 // exponential (8.4 clocks of a SIMD), two products (2.4) and two fused ones (4.2) a (token, channel, number), and 45 instructions a (token, channel) around them: 16384
-// tokens of 4096 channels of 16 numbers take 433 us, the card's SIMDs busy all the time.  (s x B is a product of a number of the channel's and one of the
+// tokens of 4096 channels of 16 numbers take 448 us, the card's SIMDs busy all the time.  (s x B is a product of a number of the channel's and one of the
 // group's: matrix instructions of 4 x 4 numbers made it and its sum with the decayed state in binary32, but each token waited for its own, 632 us instead of
 // the 548 that it took then.)
 // A channel's numbers lie with four lanes, K each, in registers from the first token to the last; a workgroup has 64 channels of one group, whose B and C come
@@ -22,6 +22,8 @@ namespace csb {
 constexpr int kScanTile = 32, kScanCols = 64, kScanRow = 2 * kScanCols + 32;      // tokens and channels in LDS; floats of a token's row there
 constexpr int kScanMany = 1024;                // workgroups that are enough for the card
 // Tokens a sequence, on average, up to which wavefronts work alone: 64 sequences of 4096 channels, 8 tokens each: 21 us, 33 in tiles; 16: 31 and 37; 32: 51 and 46.
+// All that the host knows is the mean: 255 single tokens and a prompt of 2048 (4096 channels, n = 16) are 1900 us in one call, 34 and 76 in two; and sequences
+// that are enough for the card are not split: 47 prompts of 100 tokens and one of 8192 are 1050 us, 99 and 246 in two.
 constexpr int kScanFew = 16;
 
 struct ScanDev {
@@ -355,7 +357,7 @@ __global__ __launch_bounds__(256) void selective_scan_few_kernel(const ScanDev a
 // Chunks of a call, as a power of two of tokens (31: whole sequences).  Sequences and channels that give every CU four workgroups are not split (a split costs
 // the chunks' own states beside the outputs: twice the exponentials).  Others are, as finely as makes that many, but no finer than 128 chunks
 // a sequence, whose states every later chunk combines (16384 tokens of 64 channels in 512 chunks 86 us, in 128 52), and no coarser than 512 tokens
-// (16384 tokens of 4096 channels in 16 chunks 465 us, in 32 439).
+// (16384 tokens of 4096 channels take 6 % longer in 16 chunks than in 32).
 static int scan_shift(const csb_scan_args *a, int64_t col_tiles) {
     const int64_t mean = a->n_tokens / a->n_seq, tiles = a->n_seq * col_tiles;
     if (tiles >= kScanMany || mean < 2 * kScanTile) return 31;
